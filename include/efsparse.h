@@ -429,6 +429,90 @@ ef_status ef_hard_threshold_noalloc(const float* g, float* e, float gamma, float
                                     ef_stream_t stream);
 
 /*
+ * ef_vocab_loss — softmax cross entropy of hidden states against a vocabulary,
+ * without the logits in memory: the loss whose gradient the steps above
+ * compress.
+ *
+ *     z = h w^T + bias,   lse[i] = log sum_v exp(z[i][v]),
+ *     loss[i] = lse[i] - z[i][target[i]]
+ *
+ *   h          [in]  bf16[n][d], rows ldh elements apart (ldh >= d).
+ *   w          [in]  bf16[v][d], rows ldw elements apart (ldw >= d).
+ *   bias       [in]  bf16[v] or NULL. -inf rules a word out.
+ *   target     [in]  int64[n]; a negative target skips its row: loss 0,
+ *                    lse 0, and nothing of its row of h is used. A target >= v
+ *                    is latched as EF_ERR_BAD_INPUT and its row is skipped.
+ *   n, v, d    0 <= n <= 2^30, 1 <= v <= 2^30, 1 <= d <= 2^20.
+ *   loss_out   [out] fp32[n].  lse_out [out] fp32[n].
+ *
+ * h, w, bias may start at any 2-byte boundary; rows on 16-byte boundaries
+ * (ldw a multiple of 8, w 16-byte aligned) save a copy of w. Products are
+ * exact, sums fp32. A word of logit -inf has probability 0: a target on one
+ * has loss +inf; a row of nothing else has lse -inf. NaN and +inf logits make
+ * the row's loss and lse NaN. The outputs must not overlap an input.
+ */
+ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
+                        const uint16_t* bias, const int64_t* target, uint64_t n, uint64_t v,
+                        uint64_t d, float* loss_out, float* lse_out, ef_stream_t stream);
+
+/*
+ * ef_vocab_loss_grad — gradient of sum_i row_scale[i] loss[i]:
+ *
+ *     G[i][v] = row_scale[i] (exp(z[i][v] - lse[i]) - [v = target[i]])
+ *     dh = G w,   dw = G^T h,   dbias[v] = sum_i G[i][v]
+ *
+ *   lse        [in]  fp32[n], as written by ef_vocab_loss for the same inputs.
+ *   row_scale  [in]  fp32[n] (1/n for the mean).
+ *   dh_out     [out] bf16[n][d], rows lddh apart; zero where target < 0.
+ *   dw_out     [out] bf16[v][d], rows lddw apart.
+ *   dbias_out  [out] bf16[v] or NULL (needs bias).
+ *   The other arguments as for ef_vocab_loss. The outputs are overwritten and
+ *   must not overlap an input or one another.
+ *
+ * G is rounded to bf16 (relative 2^-9) before its products, which are summed
+ * in fp32 and rounded once. A row whose lse is -inf has no gradient. Scratch:
+ * G for a piece of the vocabulary, at most 1 GB (or 4096 n bytes if that is
+ * more), the gathered h, and w where its rows are not 16-byte aligned.
+ */
+ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
+                             const uint16_t* bias, const int64_t* target, const float* lse,
+                             const float* row_scale, uint64_t n, uint64_t v, uint64_t d,
+                             uint16_t* dh_out, uint64_t lddh, uint16_t* dw_out, uint64_t lddw,
+                             uint16_t* dbias_out, ef_stream_t stream);
+
+/*
+ * ef_orthogonalize — the orthogonalised update of n_mat weight matrices, for
+ * example after an exchange: momentum, then five Newton-Schulz steps that
+ * bring every singular value of the direction near 1 (into about [0.7, 1.2])
+ * and leave its singular vectors:
+ *
+ *     m <- momentum m + u (one fmaf),  U = u + m   (without m: U = u)
+ *     X = U / |U|_F,  five times, on the shorter side:
+ *     A = X X^T,  X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ *     out = X
+ *
+ *   n_mat      0 <= n_mat <= 4096. The following are HOST arrays of n_mat.
+ *   rows, cols at most 2^20 each; a matrix without entries is passed over.
+ *   u          [in]  DEVICE pointers, fp32 or bf16 (u_type) [rows][ld_u].
+ *   m          [in/out] DEVICE pointers, fp32 [rows][ld_m], or NULL.
+ *   momentum   finite; unused without m.
+ *   out        [out] DEVICE pointers, bf16 [rows][ld_out].
+ *   Row strides are in elements, at least cols. Pointers are aligned to their
+ *   elements; nothing that is written may overlap anything else.
+ *
+ * Products have fp16 operands (scaled, 11 bits) and fp32 sums; the result is
+ * within about 2e-3 of the exact one (2-norm, relative), before its rounding
+ * to bf16. |U|_F is summed in fp32 pairs: |U|_F^2 must be within the range of
+ * fp32 (a matrix whose squares all underflow gives 0, as a zero matrix does).
+ * A NaN or infinity makes its whole matrix NaN. Equal inputs give equal bits.
+ * Scratch: about 8 bytes per entry and 4 per entry of the small squares.
+ */
+ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t* cols,
+                           const void* const* u, const uint64_t* ld_u, ef_grad_type u_type,
+                           float* const* m, const uint64_t* ld_m, float momentum,
+                           uint16_t* const* out, const uint64_t* ld_out, ef_stream_t stream);
+
+/*
  * ef_check_status — synchronise `stream`, then return and clear the device-side
  * error latched by earlier calls on that stream (EF_OK if none).
  */

@@ -19,12 +19,15 @@ from ._binding import (  # noqa: F401
     EfError,
     ef_check_status,
     ef_hard_threshold,
+    ef_orthogonalize,
     ef_scaled_round,
     ef_kernel_launches,
     ef_test_set_lookback_fault,
     ef_test_set_stream_kernel,
     ef_topk,
     ef_topk_layerwise,
+    ef_vocab_loss,
+    ef_vocab_loss_grad,
     ef_workspace_release,
     library_path,
     int_aggregate,

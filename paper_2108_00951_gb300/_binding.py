@@ -78,6 +78,10 @@ def load_library(build_if_missing: bool = True):
             "sparse_aggregate_apply_tiled": [u32, ctypes.POINTER(vp), ctypes.POINTER(vp),
                                              ctypes.POINTER(vp), vp, u64, f32, vp, vp, f32, f32,
                                              vp],
+            "ef_vocab_loss": [vp, u64, vp, u64, vp, vp, u64, u64, u64, vp, vp, vp],
+            "ef_vocab_loss_grad": [vp, u64, vp, u64, vp, vp, vp, vp, u64, u64, u64, vp, u64, vp,
+                                   u64, vp, vp],
+            "ef_orthogonalize": [u32, vp, vp, vp, vp, ctypes.c_int, vp, vp, f32, vp, vp, vp],
             "ef_check_status": [vp],
             "ef_workspace_release": [],
         }
@@ -349,6 +353,100 @@ def int_aggregate(q_list, d, scale_log2, dense_out, stream=None):
     _check(lib.int_aggregate(n, arr, int(d), int(scale_log2),
                              _dev(dense_out, "dense_out", torch.float32, d), _stream(stream)),
            "int_aggregate")
+
+
+def _rows(t, name, dtype, rows, cols):
+    """(device pointer, row stride in elements) of a CUDA matrix of this dtype
+    and shape whose rows are contiguous; 0 for an empty one."""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
+    if t.numel() == 0:
+        return 0, max(cols, 1)
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError("the rows of %s overlap" % name)
+    return t.data_ptr(), ld
+
+
+def _vocab_inputs(h, w, target, bias):
+    if not isinstance(h, _Tensor) or not isinstance(w, _Tensor) or h.dim() != 2 or w.dim() != 2:
+        raise TypeError("h and w must be matrices")
+    n, d = h.shape
+    v = w.shape[0]
+    return (n, v, d, (*_rows(h, "h", torch.bfloat16, n, d), *_rows(w, "w", torch.bfloat16, v, d),
+                      None if bias is None else _dev(bias, "bias", torch.bfloat16, v),
+                      _dev(target, "target", torch.int64, n)))
+
+
+def ef_vocab_loss(h, w, target, loss_out, lse_out, bias=None, stream=None):
+    """Softmax cross entropy of hidden states against a vocabulary, without the
+    logits in memory (``ef_vocab_loss``).
+
+    ``h`` bfloat16 [n, d] and ``w`` bfloat16 [v, d], rows contiguous at any row
+    stride; ``target`` int64 [n], a negative one skips its row; ``bias``
+    optional bfloat16 [v]; ``loss_out``, ``lse_out`` float32 [>= n].
+    """
+    lib = load_library()
+    n, v, d, head = _vocab_inputs(h, w, target, bias)
+    _check(lib.ef_vocab_loss(*head, n, v, d, _dev(loss_out, "loss_out", torch.float32, n),
+                             _dev(lse_out, "lse_out", torch.float32, n), _stream(stream)),
+           "ef_vocab_loss")
+
+
+def ef_vocab_loss_grad(h, w, target, lse, row_scale, dh_out, dw_out, bias=None, dbias_out=None,
+                       stream=None):
+    """Gradient of ``sum(row_scale * loss)`` (``ef_vocab_loss_grad``): ``lse`` as
+    written by ``ef_vocab_loss``, ``row_scale`` float32 [n]; ``dh_out`` bfloat16
+    [n, d], ``dw_out`` bfloat16 [v, d], rows contiguous at any row stride;
+    ``dbias_out`` optional bfloat16 [>= v] (needs ``bias``)."""
+    lib = load_library()
+    n, v, d, head = _vocab_inputs(h, w, target, bias)
+    _check(lib.ef_vocab_loss_grad(
+        *head, _dev(lse, "lse", torch.float32, n), _dev(row_scale, "row_scale", torch.float32, n),
+        n, v, d, *_rows(dh_out, "dh_out", torch.bfloat16, n, d),
+        *_rows(dw_out, "dw_out", torch.bfloat16, v, d),
+        None if dbias_out is None else _dev(dbias_out, "dbias_out", torch.bfloat16, v),
+        _stream(stream)), "ef_vocab_loss_grad")
+
+
+def ef_orthogonalize(updates, outs, momenta=None, momentum=0.0, stream=None):
+    """Orthogonalised updates of a list of weight matrices (``ef_orthogonalize``):
+    momentum (``momenta`` optional: float32 matrices, updated in place), then
+    five Newton-Schulz steps. ``updates`` float32 or bfloat16 matrices of one
+    dtype, ``outs`` bfloat16 matrices of the same shapes; rows contiguous at
+    any row stride."""
+    lib = load_library()
+    n = len(updates)
+    if len(outs) != n or (momenta is not None and len(momenta) != n):
+        raise ValueError("updates, outs and momenta differ in length")
+    if n == 0:
+        return
+    if not all(isinstance(t, _Tensor) and t.dim() == 2 for t in updates):
+        raise TypeError("updates must be matrices")
+    dtype = updates[0].dtype
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise TypeError("updates must be float32 or bfloat16")
+    shapes = [t.shape for t in updates]
+    u = [_rows(t, "updates", dtype, *s) for t, s in zip(updates, shapes)]
+    out = [_rows(t, "outs", torch.bfloat16, *s) for t, s in zip(outs, shapes)]
+    m = None
+    if momenta is not None:
+        m = [_rows(t, "momenta", torch.float32, *s) for t, s in zip(momenta, shapes)]
+    words = ctypes.c_uint64 * n
+
+    def column(rows, i):
+        return words(*[r[i] for r in rows])
+    _check(lib.ef_orthogonalize(
+        n, column(shapes, 0), column(shapes, 1), column(u, 0), column(u, 1),
+        int(dtype is torch.bfloat16), None if m is None else column(m, 0),
+        None if m is None else column(m, 1), _real(momentum), column(out, 0), column(out, 1),
+        _stream(stream)), "ef_orthogonalize")
 
 
 def ef_check_status(stream=None) -> int:

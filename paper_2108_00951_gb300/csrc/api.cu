@@ -2,12 +2,15 @@
 // argument checks, the per-(device, stream) workspaces, and status reporting.
 // Every compute step runs in the kernels of ht.cu, topk.cu, topk_layerwise.cu
 // and aggregate.cu.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <utility>
+#include <vector>
 
 #include "efsparse.h"
 #include "internal.h"
@@ -116,9 +119,36 @@ ef_status acquire_workspace(cudaStream_t stream, uint32_t tiles, uint32_t cand_c
     ws->ht_last_tiles = 0;
     ws->dirty = false;
     if (ws->lw) ws->lw->valid = false;  // re-upload the tables, re-zero their counters
+    if (ws->model_base &&
+        cudaMemsetAsync(ws->model_base, 0, kModelArrivalBytes, stream) != cudaSuccess)
+      return EF_ERR_CUDA;
   }
   *out = ws;
   return EF_OK;
+}
+
+// The workspace of (current device, stream) with `bytes` of model scratch.
+// Growth synchronises the stream once; the arrival counters start at zero.
+ef_status acquire_model_scratch(cudaStream_t stream, size_t bytes, Workspace** out) {
+  const ef_status st = acquire_workspace(stream, 0, 0, 0, 0, out);
+  if (st != EF_OK) return st;
+  Workspace* ws = *out;
+  std::lock_guard<std::mutex> lk(g_mu);
+  if (ws->model_base && ws->model_bytes >= bytes) return EF_OK;
+  if (ws->model_base) {
+    if (cudaStreamSynchronize(stream) != cudaSuccess) return EF_ERR_CUDA;
+    cudaFree(ws->model_base);
+    ws->model_base = nullptr;
+    ws->model_bytes = 0;
+  }
+  void* p = nullptr;
+  if (cudaMalloc(&p, kModelArrivalBytes + bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return EF_ERR_NO_MEMORY;
+  }
+  ws->model_base = static_cast<char*>(p);
+  ws->model_bytes = bytes;
+  return cudaMemsetAsync(p, 0, kModelArrivalBytes, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
 }
 
 ef_status finish_launch(cudaError_t err, Workspace* ws) {
@@ -287,6 +317,125 @@ ef_status topk_layerwise_entry(const void* g, bool bf16, float* e, float gamma, 
   return finish_launch(launch_topk_layerwise(g, bf16, e, gamma, static_cast<uint32_t>(d),
                                              idx_out, val_out, count_out, err_out, *ws, info),
                        ws);
+}
+
+// Bytes a matrix of 16-bit elements spans.
+size_t span16(uint64_t rows, uint64_t cols, uint64_t ld) {
+  return rows ? static_cast<size_t>((rows - 1) * ld + cols) * 2 : 0;
+}
+
+constexpr uint64_t kMaxRows = 1u << 30, kMaxWords = 1u << 30, kMaxWidth = 1u << 20;
+constexpr uint64_t kMaxLd = 1ull << 36;
+constexpr uint64_t kMaxSide = 1u << 20;   // rows or columns of a matrix to orthogonalise
+constexpr uint32_t kMaxMatrices = 4096;
+
+// What the loss and its gradient check alike.
+bool vocab_inputs_ok(const VocabCall& c, uint64_t n, uint64_t v, uint64_t d) {
+  if (n > kMaxRows || v == 0 || v > kMaxWords || d == 0 || d > kMaxWidth) return false;
+  if (c.ldh < d || c.ldw < d || c.ldh > kMaxLd || c.ldw > kMaxLd) return false;
+  if (!c.w || !aligned(c.w, 2) || !aligned(c.bias, 2) || !aligned(c.lse, 4)) return false;
+  if (n && (!c.h || !c.target || !c.lse || !aligned(c.h, 2) || !aligned(c.target, 8))) return false;
+  return true;
+}
+
+ef_status vocab_entry(VocabCall c, uint64_t n, uint64_t v, uint64_t d, bool gradient,
+                      cudaStream_t stream) {
+  if (!vocab_inputs_ok(c, n, v, d)) return EF_ERR_INVALID_ARG;
+  c.n = static_cast<uint32_t>(n);
+  c.v = static_cast<uint32_t>(v);
+  c.d = static_cast<uint32_t>(d);
+  const void* in[] = {c.h, c.w, c.bias, c.target, gradient ? c.lse : nullptr, c.row_scale};
+  const size_t in_n[] = {span16(n, d, c.ldh), span16(v, d, c.ldw), v * 2, n * 8, n * 4, n * 4};
+  const void* outs[3];
+  size_t out_n[3];
+  if (gradient) {
+    if (!c.dw || !aligned(c.dw, 2) || c.lddw < d || c.lddw > kMaxLd) return EF_ERR_INVALID_ARG;
+    if (!aligned(c.dbias, 2) || (c.dbias && !c.bias)) return EF_ERR_INVALID_ARG;
+    if (n && (!c.dh || !aligned(c.dh, 2) || c.lddh < d || c.lddh > kMaxLd || !c.row_scale ||
+              !aligned(c.row_scale, 4)))
+      return EF_ERR_INVALID_ARG;
+    outs[0] = c.dh, out_n[0] = span16(n, d, c.lddh);
+    outs[1] = c.dw, out_n[1] = span16(v, d, c.lddw);
+    outs[2] = c.dbias, out_n[2] = v * 2;
+  } else {
+    if (n == 0) return EF_OK;
+    if (!c.loss || !aligned(c.loss, 4)) return EF_ERR_INVALID_ARG;
+    outs[0] = c.loss, out_n[0] = n * 4;
+    outs[1] = c.lse, out_n[1] = n * 4;
+    outs[2] = nullptr, out_n[2] = 0;
+  }
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 6; ++i)
+      if (overlaps(outs[o], out_n[o], in[i], in_n[i])) return EF_ERR_INVALID_ARG;
+    for (int q = o + 1; q < 3; ++q)
+      if (overlaps(outs[o], out_n[o], outs[q], out_n[q])) return EF_ERR_INVALID_ARG;
+  }
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
+  DeviceInfo info;
+  ef_status st = device_info(dev, &info);
+  if (st != EF_OK) return st;
+  Workspace* ws = nullptr;
+  st = acquire_model_scratch(stream, vocab_scratch(c, gradient, info), &ws);
+  if (st != EF_OK) return st;
+  return finish_launch(gradient ? launch_vocab_loss_grad(c, *ws, info)
+                                : launch_vocab_loss(c, *ws, info),
+                       ws);
+}
+
+ef_status orthogonalize_entry(uint32_t n, const uint64_t* rows, const uint64_t* cols,
+                              const void* const* u, const uint64_t* ld_u, bool bf16,
+                              float* const* m, const uint64_t* ld_m, float momentum,
+                              uint16_t* const* out, const uint64_t* ld_out,
+                              cudaStream_t stream) {
+  if (n > kMaxMatrices || !std::isfinite(momentum)) return EF_ERR_INVALID_ARG;
+  if (n == 0) return EF_OK;
+  if (!rows || !cols || !u || !ld_u || !out || !ld_out || (m && !ld_m)) return EF_ERR_INVALID_ARG;
+  const size_t usz = bf16 ? 2 : 4;
+  std::vector<OrthoMat> mats(n);
+  std::vector<std::pair<uintptr_t, std::pair<uintptr_t, bool>>> spans;  // begin, (end, written)
+  auto span = [&](const void* p, uint64_t r, uint64_t c, uint64_t ld, size_t size, bool written) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    spans.push_back({at, {at + ((r - 1) * ld + c) * size, written}});
+  };
+  for (uint32_t i = 0; i < n; ++i) {
+    OrthoMat& t = mats[i];
+    if (rows[i] > kMaxSide || cols[i] > kMaxSide) return EF_ERR_INVALID_ARG;
+    t.rows = static_cast<uint32_t>(rows[i]);
+    t.cols = static_cast<uint32_t>(cols[i]);
+    t.u = u[i];
+    t.m = m ? m[i] : nullptr;
+    t.out = out[i];
+    t.ld_u = ld_u[i];
+    t.ld_m = m ? ld_m[i] : 0;
+    t.ld_out = ld_out[i];
+    if (t.rows == 0 || t.cols == 0) continue;
+    if (!t.u || !t.out || (m && !t.m)) return EF_ERR_INVALID_ARG;
+    if (!aligned(t.u, usz) || !aligned(t.m, 4) || !aligned(t.out, 2)) return EF_ERR_INVALID_ARG;
+    if (t.ld_u < t.cols || t.ld_out < t.cols || (m && t.ld_m < t.cols)) return EF_ERR_INVALID_ARG;
+    if (t.ld_u > kMaxLd || t.ld_out > kMaxLd || t.ld_m > kMaxLd) return EF_ERR_INVALID_ARG;
+    span(t.u, t.rows, t.cols, t.ld_u, usz, false);
+    if (m) span(t.m, t.rows, t.cols, t.ld_m, 4, true);
+    span(t.out, t.rows, t.cols, t.ld_out, 2, true);
+  }
+  if (spans.empty()) return EF_OK;
+  // nothing written may overlap anything else: by start, the furthest end so far
+  std::sort(spans.begin(), spans.end());
+  uintptr_t end_any = 0, end_written = 0;
+  for (const auto& s : spans) {
+    if (s.first < (s.second.second ? end_any : end_written)) return EF_ERR_INVALID_ARG;
+    if (s.second.first > end_any) end_any = s.second.first;
+    if (s.second.second && s.second.first > end_written) end_written = s.second.first;
+  }
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
+  DeviceInfo info;
+  ef_status st = device_info(dev, &info);
+  if (st != EF_OK) return st;
+  Workspace* ws = nullptr;
+  st = acquire_model_scratch(stream, ortho_scratch(mats.data(), n, info), &ws);
+  if (st != EF_OK) return st;
+  return finish_launch(launch_orthogonalize(mats.data(), n, bf16, momentum, *ws, info), ws);
 }
 
 }  // namespace
@@ -562,6 +711,56 @@ ef_status int_aggregate(uint32_t n, const int32_t* const* q, uint64_t d, int32_t
       launch_int_aggregate(n, q, static_cast<uint32_t>(d), scale_log2, dense_out, *ws), ws);
 }
 
+ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
+                        const uint16_t* bias, const int64_t* target, uint64_t n, uint64_t v,
+                        uint64_t d, float* loss_out, float* lse_out, ef_stream_t stream) {
+  efs::VocabCall c = {};
+  c.h = h;
+  c.w = w;
+  c.bias = bias;
+  c.target = target;
+  c.ldh = ldh;
+  c.ldw = ldw;
+  c.loss = loss_out;
+  c.lse = lse_out;
+  return efs::vocab_entry(c, n, v, d, false, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
+                             const uint16_t* bias, const int64_t* target, const float* lse,
+                             const float* row_scale, uint64_t n, uint64_t v, uint64_t d,
+                             uint16_t* dh_out, uint64_t lddh, uint16_t* dw_out, uint64_t lddw,
+                             uint16_t* dbias_out, ef_stream_t stream) {
+  efs::VocabCall c = {};
+  c.h = h;
+  c.w = w;
+  c.bias = bias;
+  c.target = target;
+  c.ldh = ldh;
+  c.ldw = ldw;
+  c.lse = const_cast<float*>(lse);
+  c.row_scale = row_scale;
+  c.dh = dh_out;
+  c.lddh = lddh;
+  c.dw = dw_out;
+  c.lddw = lddw;
+  c.dbias = dbias_out;
+  return efs::vocab_entry(c, n, v, d, true, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t* cols,
+                           const void* const* u, const uint64_t* ld_u, ef_grad_type u_type,
+                           float* const* m, const uint64_t* ld_m, float momentum,
+                           uint16_t* const* out, const uint64_t* ld_out, ef_stream_t stream) {
+  if (u_type != EF_GRAD_F32 && u_type != EF_GRAD_BF16) return EF_ERR_INVALID_ARG;
+  try {
+    return efs::orthogonalize_entry(n_mat, rows, cols, u, ld_u, u_type == EF_GRAD_BF16, m, ld_m,
+                                    momentum, out, ld_out, reinterpret_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return EF_ERR_NO_MEMORY;
+  }
+}
+
 ef_status ef_check_status(ef_stream_t stream) {
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (cudaStreamSynchronize(s) != cudaSuccess) return EF_ERR_CUDA;
@@ -613,6 +812,7 @@ ef_status ef_workspace_release(void) {
   for (auto it = efs::g_workspaces.begin(); it != efs::g_workspaces.end();) {
     if (it->first.first == dev) {
       if (it->second->base) cudaFree(it->second->base);
+      if (it->second->model_base) cudaFree(it->second->model_base);
       if (it->second->density_host) cudaFreeHost(it->second->density_host);
       if (it->second->lw) {
         if (it->second->lw->dev) cudaFree(it->second->lw->dev);

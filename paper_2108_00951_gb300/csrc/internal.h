@@ -116,6 +116,9 @@ struct LwPlan {
          total = 0;
 };
 
+constexpr uint32_t kModelArrivals = 1u << 16;
+constexpr size_t kModelArrivalBytes = sizeof(uint32_t) * kModelArrivals;
+
 struct Workspace {
   int device = -1;
   cudaStream_t stream = nullptr;
@@ -143,6 +146,12 @@ struct Workspace {
   uint32_t* density_dev = nullptr;
   bool dirty = false;          // header must be re-cleared (failed launch or device timeout)
   LwPlan* lw = nullptr;        // layer-wise Top-k tables (created on first use)
+  // Scratch of the language-model operators: arrival counters (zero between
+  // launches), then what a call lays out for itself.
+  char* model_base = nullptr;
+  size_t model_bytes = 0;
+  uint32_t* model_arrivals() const { return reinterpret_cast<uint32_t*>(model_base); }
+  char* model_scratch() const { return model_base + kModelArrivalBytes; }
 
   // Regions after the header, each 256-byte aligned.
   static size_t align(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -238,6 +247,38 @@ cudaError_t launch_scaled_round(const void* g, bool g_bf16, float* e, float gamm
                                 Workspace& ws, const DeviceInfo& dev);
 cudaError_t launch_int_aggregate(uint32_t n, const int32_t* const* q, uint32_t d, int m,
                                  float* dense_out, Workspace& ws);
+
+// The language-model operators (vocab.cu, ortho.cu). Each *_scratch is the
+// model scratch its call needs, in bytes.
+struct VocabCall {
+  const uint16_t* h;      // [n][ldh] bf16
+  const uint16_t* w;      // [v][ldw] bf16
+  const uint16_t* bias;   // bf16 [v] or nullptr
+  const int64_t* target;  // [n]
+  uint64_t ldh, ldw;
+  uint32_t n, v, d;
+  float* loss;            // loss call: [n]
+  float* lse;             // [n]: written by the loss call, read by the gradient's
+  const float* row_scale; // gradient call: [n]
+  uint16_t* dh;           // [n][lddh] bf16
+  uint16_t* dw;           // [v][lddw] bf16
+  uint16_t* dbias;        // bf16 [v] or nullptr
+  uint64_t lddh, lddw;
+};
+size_t vocab_scratch(const VocabCall& c, bool gradient, const DeviceInfo& dev);
+cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
+cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
+
+struct OrthoMat {
+  const void* u;   // fp32 or bf16 [rows][ld_u]
+  float* m;        // fp32 [rows][ld_m] or nullptr
+  uint16_t* out;   // bf16 [rows][ld_out]
+  uint64_t ld_u, ld_m, ld_out;
+  uint32_t rows, cols;
+};
+size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev);
+cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
+                                 Workspace& ws, const DeviceInfo& dev);
 
 // Launch bookkeeping.
 // A launch that may begin while the previous kernel on the stream finishes
