@@ -9,22 +9,29 @@
 // which drives every singular value of U towards 1 (into about [0.7, 1.2])
 // and leaves the singular vectors.
 //
-// All matrices of a call go through each product together: a launch holds
-// the tiles of every matrix. A and B are symmetric: only tiles that reach the
-// diagonal are formed, entries above it are mirrored.
+// All fifteen products of a call run in one cooperative launch, a grid barrier
+// between, each over the tiles of every matrix. A and B are symmetric: only
+// tiles that reach the diagonal are formed, entries above it are mirrored.
 //
-// Operands are fp16 with power-of-two scales (X 2^14, A and B 2^13: |X| <= 1,
-// so nothing overflows), which keeps 11 bits where bf16 keeps 8: the steps
-// amplify small singular values up to 485 times, and with them any rounding.
-// X is kept as a pair H + L of fp16 (22 bits): the products read H, the
-// linear term a X reads both, so that directions the products hardly touch
-// keep their bits. B's diagonal, -2.8 to 0, is kept as B + 2 I, whose entries
-// round finer; the term -2 I moves into the linear term. Relative error of the result
-// against 64 bits about 1e-3 (bf16 operands: 1e-2), below the rounding of the
-// bf16 output.
+// Operands are fp16 with power-of-two scales (X 2^14, A and B 2^13: |X| <= 1.3
+// throughout, so nothing overflows), which keeps 11 bits where bf16 keeps 8:
+// the steps amplify small singular values up to 485 times, and with them any
+// rounding. The linear term a X is taken from an fp32 copy, so that directions
+// the products hardly touch keep their bits; and B is kept as
+// B + 2 I, whose diagonal (-0.8 to 2 instead of -2.8 to 0) rounds finer, the
+// term -2 X moving into the linear one. Relative error of the result against
+// 64 bits about 1e-3 (bf16 operands: 1e-2), below the rounding of the bf16
+// output. A matrix whose shorter side is at most kExactSide has fewer
+// roundings to average over: its operands are pairs hi + lo of fp16 (22 bits)
+// and its products three (hi hi + hi lo + lo hi), within 1e-4; they are small
+// enough for that to cost little.
+//
+// The fp32 copies lie in blocks of 128 rows x 32 columns, four columns of all
+// rows together, as the epilogues read and write them: contiguous per warp.
 #include "product.cuh"
 
 #include <algorithm>
+#include <memory>
 #include <vector>
 
 #include <cuda_fp16.h>
@@ -35,22 +42,32 @@ namespace {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f, kNsShift = 2.0f;
 constexpr float kScaleX = 16384.0f, kScaleA = 8192.0f;
 constexpr int kSteps = 5;
+constexpr uint32_t kExactSide = 128;
 
-// ---- momentum, norm, and the first H + L
-constexpr uint32_t kSegment = 256;   // columns of a row that a warp takes at a time
+// Element (row, col .. col + 3) of a matrix in blocks: float4 units.
+__device__ __forceinline__ uint64_t block_at(uint32_t row, uint32_t col, uint32_t chunks) {
+  return (static_cast<uint64_t>(row / kTileM) * chunks + col / 32) * (8 * kTileM) +
+         (col % 32) / 4 * kTileM + row % kTileM;
+}
+
+// ---- momentum, norm, and the first X
 constexpr uint32_t kMaxParts = 512;  // partial sums of squares per matrix
 constexpr uint32_t kPrepMats = 48;   // matrices per launch
+constexpr uint32_t kPrepCols = 64;   // a CTA takes blocks of 128 rows x 64 columns
 
 struct PrepMat {
   const void* u;
   float* m;
-  uint16_t* hi;   // fp16, rows ld_x apart
-  uint16_t* lo;
   uint16_t* out;  // where the last step writes
+  float* x;       // X in blocks, scaled
+  uint16_t* hi;   // X in fp16, rows ld_x apart
+  uint16_t* lo;   // what hi leaves (exact matrices), or nullptr
   uint64_t ld_u, ld_m, ld_out;
   uint32_t rows, cols, ld_x;
+  uint32_t chunks;         // 32-column blocks of a row of x
+  uint32_t blocks, blocks_n;
+  uint32_t blocks_per_cta;
   uint32_t index;          // in the groups' order
-  uint32_t units_per_cta;  // (row, segment) units
   uint32_t cta0;           // its first CTA of the launch
   uint32_t part0;          // its first partial sum
   uint32_t parts;
@@ -58,7 +75,6 @@ struct PrepMat {
 struct PrepArgs {
   PrepMat mat[kPrepMats];
   uint32_t mats;
-  uint32_t bf16;
   float mu;
   FF* parts;
   uint16_t** outs;     // tables of the results, by index
@@ -71,95 +87,80 @@ __device__ __forceinline__ uint32_t prep_mat(const PrepArgs& a) {
   return i;
 }
 
-// The direction U at 8 columns of a row: 8 in a row per lane where the rows
-// allow 16-byte accesses (col0 = first column of the lane's 8), else 32 apart.
+// The direction U at four columns of a row (zeros past the matrix).
 // kFirst: also writes the momentum back.
 template <bool kBf16, bool kFirst>
-__device__ __forceinline__ void direction(const PrepMat& t, float mu, uint32_t row, uint32_t seg,
-                                          bool vec, float (&x)[8], uint32_t (&col)[8]) {
-  const uint32_t lane = threadIdx.x & 31;
-  const uint32_t c0 = seg * kSegment;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) col[j] = vec ? c0 + lane * 8 + j : c0 + j * 32 + lane;
-  const uint64_t base_u = row * t.ld_u, base_m = row * t.ld_m;
-  const uint16_t* ub = static_cast<const uint16_t*>(t.u) + base_u;
-  const float* uf = static_cast<const float*>(t.u) + base_u;
-  if (vec && col[0] + 8 <= t.cols) {
+__device__ __forceinline__ float4 direction(const PrepMat& t, float mu, uint32_t row, uint32_t col,
+                                            bool vec) {
+  float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (row >= t.rows || col >= t.cols) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const uint16_t* ub = static_cast<const uint16_t*>(t.u) + row * t.ld_u + col;
+  const float* uf = static_cast<const float*>(t.u) + row * t.ld_u + col;
+  float* m = t.m ? t.m + row * t.ld_m + col : nullptr;
+  if (vec && col + 4 <= t.cols) {
     if (kBf16) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(ub + col[0]));
-      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+      const uint2 w = __ldg(reinterpret_cast<const uint2*>(ub));
+      x[0] = __uint_as_float(w.x << 16), x[1] = __uint_as_float(w.x & 0xffff0000u);
+      x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
+    } else {
+      const float4 p = __ldg(reinterpret_cast<const float4*>(uf));
+      x[0] = p.x, x[1] = p.y, x[2] = p.z, x[3] = p.w;
+    }
+    if (m) {
+      const float4 q = *reinterpret_cast<const float4*>(m);
+      float mv[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(ws[j] << 16);
-        x[2 * j + 1] = __uint_as_float(ws[j] & 0xffff0000u);
-      }
-    } else {
-      const float4 p = __ldg(reinterpret_cast<const float4*>(uf + col[0]));
-      const float4 q = __ldg(reinterpret_cast<const float4*>(uf + col[0]) + 1);
-      x[0] = p.x, x[1] = p.y, x[2] = p.z, x[3] = p.w;
-      x[4] = q.x, x[5] = q.y, x[6] = q.z, x[7] = q.w;
-    }
-    if (t.m) {
-      float4* mp = reinterpret_cast<float4*>(t.m + base_m + col[0]);
-      float4 p = mp[0], q = mp[1];
-      float mv[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
         if (kFirst) mv[j] = __fmaf_rn(mu, mv[j], x[j]);
         x[j] = __fadd_rn(x[j], mv[j]);
       }
-      if (kFirst) {
-        mp[0] = make_float4(mv[0], mv[1], mv[2], mv[3]);
-        mp[1] = make_float4(mv[4], mv[5], mv[6], mv[7]);
-      }
+      if (kFirst) *reinterpret_cast<float4*>(m) = make_float4(mv[0], mv[1], mv[2], mv[3]);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = 0.0f;
-      if (col[j] < t.cols) {
-        x[j] = kBf16 ? bf16_bits_to_f32(__ldg(ub + col[j])) : __ldg(uf + col[j]);
-        if (t.m) {
-          float* mp = t.m + base_m + col[j];
-          float mv = *mp;
-          if (kFirst) {
-            mv = __fmaf_rn(mu, mv, x[j]);
-            *mp = mv;
-          }
-          x[j] = __fadd_rn(x[j], mv);
+    for (int j = 0; j < 4; ++j) {
+      if (col + j >= t.cols) continue;
+      x[j] = kBf16 ? bf16_bits_to_f32(__ldg(ub + j)) : __ldg(uf + j);
+      if (m) {
+        float mv = m[j];
+        if (kFirst) {
+          mv = __fmaf_rn(mu, mv, x[j]);
+          m[j] = mv;
         }
+        x[j] = __fadd_rn(x[j], mv);
       }
     }
   }
+  return make_float4(x[0], x[1], x[2], x[3]);
 }
 
-__device__ __forceinline__ bool prep_vec(const PrepMat& t, bool bf16) {
-  const uint32_t size = bf16 ? 2 : 4;
-  return reinterpret_cast<uintptr_t>(t.u) % 16 == 0 && t.ld_u * size % 16 == 0 &&
+template <bool kBf16>
+__device__ __forceinline__ bool prep_vec(const PrepMat& t) {
+  constexpr uint32_t size = kBf16 ? 2 : 4;
+  return reinterpret_cast<uintptr_t>(t.u) % (4 * size) == 0 && t.ld_u % 4 == 0 &&
          reinterpret_cast<uintptr_t>(t.m) % 16 == 0 && t.ld_m % 4 == 0;
 }
 
-// Momentum and the sum of squares: fp32 over 8 entries, float-float from there
-// (fixed order).
+// Momentum and the sum of squares: fp32 over 8 rows' four entries, float-float
+// from there (fixed order). A warp takes two rows of 64 columns at a time.
 template <bool kBf16>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__ PrepArgs a) {
   __shared__ FF s_ff[32];
   griddep_wait();
   const PrepMat& t = a.mat[prep_mat(a)];
-  const uint32_t cta = blockIdx.x - t.cta0, segs = (t.cols + kSegment - 1) / kSegment;
-  const uint64_t units = static_cast<uint64_t>(t.rows) * segs;
-  const uint64_t lo = static_cast<uint64_t>(cta) * t.units_per_cta;
-  const uint64_t hi = lo + t.units_per_cta < units ? lo + t.units_per_cta : units;
-  const bool vec = prep_vec(t, kBf16);
+  const uint32_t cta = blockIdx.x - t.cta0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t lo = cta * t.blocks_per_cta, hi = min(lo + t.blocks_per_cta, t.blocks);
+  const bool vec = prep_vec<kBf16>(t);
   FF total{0.0f, 0.0f};
-  for (uint64_t i = lo + (threadIdx.x >> 5); i < hi; i += 8) {
-    float x[8];
-    uint32_t col[8];
-    direction<kBf16, true>(t, a.mu, static_cast<uint32_t>(i / segs),
-                           static_cast<uint32_t>(i % segs), vec, x, col);
+  for (uint32_t b = lo; b < hi; ++b) {
+    const uint32_t row0 = b / t.blocks_n * kTileM + warp * 16 + (lane >> 4);
+    const uint32_t col = b % t.blocks_n * kPrepCols + (lane & 15u) * 4;
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = __fmaf_rn(x[j], x[j], s);
+    for (uint32_t i = 0; i < 8; ++i) {
+      const float4 x = direction<kBf16, true>(t, a.mu, row0 + 2 * i, col, vec);
+      s = __fmaf_rn(x.x, x.x, __fmaf_rn(x.y, x.y, __fmaf_rn(x.z, x.z, __fmaf_rn(x.w, x.w, s))));
+    }
     total = ff_add(total, FF{s, 0.0f});
   }
   total = block_sum_ff(total, s_ff);
@@ -172,18 +173,24 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__
   }
 }
 
-// X = U / |U|_F as H + L, scaled by 2^14.
+__device__ __forceinline__ uint16_t half_bits(float x) {
+  return __half_as_ushort(__float2half_rn(x));
+}
+__device__ __forceinline__ float half_rest(float x) {
+  return __fsub_rn(x, __half2float(__float2half_rn(x)));
+}
+
+// X = U / |U|_F, scaled: fp16 rows and, through shared memory, fp32 blocks.
 template <bool kBf16>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ PrepArgs a) {
   __shared__ FF s_ff[32];
   __shared__ float s_inv;
+  __shared__ float4 s_x[kPrepCols / 4][kTileM + 1];
   griddep_wait();
   const PrepMat& t = a.mat[prep_mat(a)];
-  const uint32_t cta = blockIdx.x - t.cta0, segs = (t.cols + kSegment - 1) / kSegment;
-  const uint64_t units = static_cast<uint64_t>(t.rows) * segs;
-  const uint64_t lo = static_cast<uint64_t>(cta) * t.units_per_cta;
-  const uint64_t hi = lo + t.units_per_cta < units ? lo + t.units_per_cta : units;
-  const bool vec = prep_vec(t, kBf16);
+  const uint32_t cta = blockIdx.x - t.cta0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t lo = cta * t.blocks_per_cta, hi = min(lo + t.blocks_per_cta, t.blocks);
+  const bool vec = prep_vec<kBf16>(t);
   const FF sum = sum_parts_ff(a.parts + t.part0, t.parts, s_ff);
   if (threadIdx.x == 0) {
     const double n = sqrt(ff_to_double(sum));
@@ -191,187 +198,180 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
   }
   __syncthreads();
   const float inv = s_inv;
-  for (uint64_t i = lo + (threadIdx.x >> 5); i < hi; i += 8) {
-    float x[8];
-    uint32_t col[8];
-    const uint32_t row = static_cast<uint32_t>(i / segs);
-    direction<kBf16, false>(t, a.mu, row, static_cast<uint32_t>(i % segs), vec, x, col);
-    uint16_t h[8], l[8];
+  for (uint32_t b = lo; b < hi; ++b) {
+    const uint32_t tile = b / t.blocks_n, col0 = b % t.blocks_n * kPrepCols;
+    const uint32_t unit = lane & 15u, col = col0 + unit * 4;
+    float4 x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float y = __fmul_rn(x[j], inv);
-      const __half hh = __float2half_rn(y);
-      h[j] = __half_as_ushort(hh);
-      l[j] = __half_as_ushort(__float2half_rn(__fsub_rn(y, __half2float(hh))));
-    }
-    uint16_t* to_h = t.hi + static_cast<uint64_t>(row) * t.ld_x;
-    uint16_t* to_l = t.lo + static_cast<uint64_t>(row) * t.ld_x;
-    if (vec && col[0] + 8 <= t.cols) {
-      *reinterpret_cast<uint4*>(to_h + col[0]) =
-          make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
-      *reinterpret_cast<uint4*>(to_l + col[0]) =
-          make_uint4(l[0] | (l[1] << 16), l[2] | (l[3] << 16), l[4] | (l[5] << 16), l[6] | (l[7] << 16));
-    } else {
+    for (uint32_t i = 0; i < 8; ++i)
+      x[i] = direction<kBf16, false>(t, a.mu, tile * kTileM + warp * 16 + (lane >> 4) + 2 * i, col, vec);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (col[j] < t.cols) {
-          to_h[col[j]] = h[j];
-          to_l[col[j]] = l[j];
-        }
-    }
-  }
-}
-
-// ---- the three products' epilogues
-__device__ __forceinline__ float2 half2_at(uint32_t w) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
-
-// 32 fp16 of a row from scratch (rows padded to 8 columns: 16-byte accesses;
-// columns past the padding are left alone).
-__device__ __forceinline__ void load_half_row(const uint16_t* p, uint32_t left, float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (static_cast<uint32_t>(8 * j) < left) w = __ldcg(reinterpret_cast<const uint4*>(p) + j);
-    const float2 a = half2_at(w.x), b = half2_at(w.y), c = half2_at(w.z), d = half2_at(w.w);
-    v[8 * j] = a.x, v[8 * j + 1] = a.y, v[8 * j + 2] = b.x, v[8 * j + 3] = b.y;
-    v[8 * j + 4] = c.x, v[8 * j + 5] = c.y, v[8 * j + 6] = d.x, v[8 * j + 7] = d.y;
-  }
-}
-__device__ __forceinline__ void store_half_row(uint16_t* p, uint32_t left, const float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (static_cast<uint32_t>(8 * j) < left)
-      *(reinterpret_cast<uint4*>(p) + j) =
-          make_uint4(pack_f16(v[8 * j], v[8 * j + 1]), pack_f16(v[8 * j + 2], v[8 * j + 3]),
-                     pack_f16(v[8 * j + 4], v[8 * j + 5]), pack_f16(v[8 * j + 6], v[8 * j + 7]));
-}
-
-// The symmetric products: out = A (kSecond: out = B + 2 I), entries on and
-// below the diagonal stored as computed, those below also mirrored.
-template <bool kSecond>
-struct SymmetricEpilogue {
-  struct Params {
-    const uint16_t* a;  // kSecond: A
-    uint16_t* out;
-    uint32_t ld;
-    uint64_t batch_ld;
-  };
-  struct Smem {};
-  static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row, Smem&,
-                                              const ProductAcc& acc) {
-    const uint32_t r = it.m0 + row;
-    const uint64_t base = it.batch * e.batch_ld;
-    uint16_t* out = e.out + base;
-    for (uint32_t c = 0; c < acc.chunks; ++c) {
-      float v[32];
-      acc.load(c, v);
-      const uint32_t col0 = it.n0 + c * 32;
-      if (r >= p.m || col0 > r) continue;
-      if (kSecond) {
-        float a[32];
-        load_half_row(e.a + base + static_cast<uint64_t>(r) * e.ld + col0, e.ld - col0, a);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          v[j] = __fmaf_rn(kNsB, a[j], __fmul_rn(v[j], kNsC / kScaleA));
-          if (col0 + j == r) v[j] = __fmaf_rn(kNsShift, kScaleA, v[j]);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = __fmul_rn(v[j], kScaleA / (kScaleX * kScaleX));
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t r = warp * 16 + (lane >> 4) + 2 * i, row = tile * kTileM + r;
+      const float4 y = make_float4(__fmul_rn(x[i].x, inv), __fmul_rn(x[i].y, inv),
+                                   __fmul_rn(x[i].z, inv), __fmul_rn(x[i].w, inv));
+      s_x[unit][r] = y;
+      if (row < t.rows && col < t.ld_x) {  // rows are padded to 8 columns
+        const uint64_t at = static_cast<uint64_t>(row) * t.ld_x + col;
+        *reinterpret_cast<uint2*>(t.hi + at) = make_uint2(pack_f16(y.x, y.y), pack_f16(y.z, y.w));
+        if (t.lo)
+          *reinterpret_cast<uint2*>(t.lo + at) =
+              make_uint2(pack_f16(half_rest(y.x), half_rest(y.y)),
+                         pack_f16(half_rest(y.z), half_rest(y.w)));
       }
-      if (col0 + 31 <= r) {
-        store_half_row(out + static_cast<uint64_t>(r) * e.ld + col0, 32, v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (col0 + j <= r)
-            out[static_cast<uint64_t>(r) * e.ld + col0 + j] = __half_as_ushort(__float2half_rn(v[j]));
-      }
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (col0 + j < r)
-          out[static_cast<uint64_t>(col0 + j) * e.ld + r] = __half_as_ushort(__float2half_rn(v[j]));
     }
+    __syncthreads();
+    float4* to = reinterpret_cast<float4*>(t.x);
+    for (uint32_t i = threadIdx.x; i < kPrepCols / 4 * kTileM; i += 256) {
+      const uint32_t u = i / kTileM, r = i % kTileM;
+      if (col0 + u * 4 < t.chunks * 32)
+        to[block_at(tile * kTileM + r, col0 + u * 4, t.chunks)] = s_x[u][r];
+    }
+    __syncthreads();
   }
-};
+}
 
-constexpr uint32_t kOrthoGroups = 16;  // shapes per launch
+// ---- the products' epilogues
+enum : uint32_t { kFormA = 0, kFormB = 1, kFormX = 2 };
 
-// X <- a X + B X, as H + L; the last step writes the result in bf16.
+// 32 fp32 of the thread's row from blocks, and back.
+__device__ __forceinline__ void load_block(const float4* p, float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 x = __ldcg(p + j * kTileM);
+    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
+  }
+}
+__device__ __forceinline__ void keep_block(float4* p, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    __stcg(p + j * kTileM, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+}
+__device__ __forceinline__ void pack_row(const float (&v)[32], uint32_t (&w)[16]) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) w[j] = pack_f16(v[2 * j], v[2 * j + 1]);
+}
+
 struct StepEpilogue {
   struct Params {
-    const uint16_t *h, *l;
-    uint16_t *h_out, *l_out;
-    uint32_t ld;
-    uint64_t batch_ld;
-    uint16_t* const* outs;  // the last step: device table of the results, by batch
+    uint32_t form;
+    uint32_t exact;         // operands have a second plane
+    uint32_t ld;            // of the fp16 result: rows padded to 8 columns
+    uint32_t chunks;        // 32-column blocks of a row of `blocks`
+    uint64_t plane;         // fp16 elements of a plane
+    uint64_t batch_blocks;  // floats of a matrix in blocks
+    uint16_t* to;           // the fp16 result [batch][planes][rows][ld]
+    float* blocks;          // A: written by kFormA, read by kFormB; X: both
+    uint16_t* const* outs;  // the last step's results, by batch
     const uint64_t* ld_outs;
+    uint32_t last_phase;
   };
   struct Smem {
-    uint32_t turn[4][32 * 17];
+    TurnSmem turn;
   };
-  static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row, Smem& s,
-                                              const ProductAcc& acc) {
-    const uint32_t lane = threadIdx.x & 31;
-    const uint32_t r = it.m0 + row;
-    const bool real = r < p.m;
-    const uint64_t base = it.batch * e.batch_ld + static_cast<uint64_t>(real ? r : 0) * e.ld;
-    uint16_t* out = nullptr;
-    uint64_t ld_out = 0;
-    if (e.outs) {
-      out = e.outs[it.batch];
-      ld_out = e.ld_outs[it.batch];
-    }
-    const bool vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && ld_out % 8 == 0;
-    uint32_t* turn = s.turn[(threadIdx.x >> 5) & 3u];
-    for (uint32_t c = 0; c < acc.chunks; ++c) {
-      float v[32], x[32];
-      acc.load(c, v);
-      const uint32_t col0 = it.n0 + c * 32;
-      if (col0 >= p.n) continue;  // (uniform: the last chunk may lie past the columns)
-      const uint32_t left = real ? e.ld - col0 : 0;
-      load_half_row(e.l + base + col0, left, x);
+
+  // A 32 x 32 block of a symmetric matrix on or below the diagonal, and its
+  // mirror image.
+  static __device__ __forceinline__ void store_symmetric(uint16_t* out, uint32_t ld, uint32_t n,
+                                                         uint32_t r, uint32_t col0,
+                                                         const float (&v)[32], Smem& s) {
+    const uint32_t lane = threadIdx.x & 31, r0 = r - lane;
+    if (r0 >= n) return;  // (uniform)
+    uint32_t w[16];
+    pack_row(v, w);
+    if (col0 == r0) mirror_block(s.turn, w);
+    const uint32_t cols = ld - col0;
+    store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, [&](uint32_t i) -> uint16_t* {
+      return r0 + i < n ? out + static_cast<uint64_t>(r0 + i) * ld + col0 : nullptr;
+    });
+    if (col0 < r0 && r < n) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        v[j] = __fmaf_rn(kNsA, x[j], __fmul_rn(v[j], 1.0f / kScaleA));
-      load_half_row(e.h + base + col0, left, x);
+        out[static_cast<uint64_t>(col0 + j) * ld + r] = half_bits(v[j]);
+    }
+  }
+
+  static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
+                                              const ProductItem& it, uint32_t row, uint32_t,
+                                              Smem& s, const ProductAcc& acc, uint32_t phase) {
+    const uint32_t r = it.m0 + row, r0 = it.m0 + (row & ~31u);
+    const uint32_t planes = e.exact ? 2 : 1;
+    float4* blocks = reinterpret_cast<float4*>(e.blocks + it.batch * e.batch_blocks) +
+                     static_cast<uint64_t>(it.m0 / kTileM) * e.chunks * (8 * kTileM) + row;
+    uint16_t* to = e.to + it.batch * planes * e.plane;
+    const bool last = e.form == kFormX && phase == e.last_phase;
+    uint16_t* out = nullptr;
+    uint64_t ld_out = 0;
+    uint32_t align = 0;
+    if (last) {
+      out = e.outs[it.batch];
+      ld_out = e.ld_outs[it.batch];
+      const uint64_t low = reinterpret_cast<uintptr_t>(out) | (ld_out * 2);
+      align = low % 16 == 0 ? 16 : low % 4 == 0 ? 4 : 2;
+    }
+    const bool rows_exist = r0 < p.m;
+    for (uint32_t c = acc.c0; c < acc.c1; ++c) {
+      const uint32_t col0 = it.n0 + c * 32;
+      float4* mine = blocks + static_cast<uint64_t>(col0 / 32) * (8 * kTileM);
+      const bool live = rows_exist && col0 < p.n && (e.form == kFormX || col0 <= r0 + 31);
+      float x[32], v[32];
+      if (live && e.form != kFormA) load_block(mine, x);  // in flight beside the accumulators
+      acc.load(c, v);
+      if (!live) continue;  // (uniform)
+      if (e.form == kFormX) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = __fmaf_rn(kNsA - kNsShift, x[j], v[j]);
-      if (!e.outs) {
-        if (real) {
-          store_half_row(e.h_out + base + col0, left, v);
+        for (int j = 0; j < 32; ++j) {
+          // the operand's rounding of x stands in the term that B + 2 I took over
+          const float h = __half2float(__float2half_rn(x[j]));
+          const float op = e.exact ? __fadd_rn(h, __half2float(__float2half_rn(__fsub_rn(x[j], h)))) : h;
+          v[j] = __fmaf_rn(v[j], 1.0f / kScaleA, __fmaf_rn(kNsA, x[j], __fmul_rn(-kNsShift, op)));
+        }
+        uint32_t w[16];
+        if (last) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            v[j] = __fsub_rn(v[j], __half2float(__float2half_rn(v[j])));
-          store_half_row(e.l_out + base + col0, left, v);
+          for (int j = 0; j < 16; ++j)
+            w[j] = pack_bf16(__fmul_rn(v[2 * j], 1.0f / kScaleX), __fmul_rn(v[2 * j + 1], 1.0f / kScaleX));
+          store_block(s.turn, w, p.n - col0, align, [&](uint32_t i) -> uint16_t* {
+            return r0 + i < p.m ? out + (r0 + i) * ld_out + col0 : nullptr;
+          });
+          continue;
+        }
+        keep_block(mine, v);
+        const uint32_t cols = e.ld - col0;
+        auto rows = [&](uint32_t i) -> uint16_t* {
+          return r0 + i < p.m ? to + static_cast<uint64_t>(r0 + i) * e.ld + col0 : nullptr;
+        };
+        pack_row(v, w);
+        store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, rows);
+        if (e.exact) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = half_rest(v[j]);
+          pack_row(v, w);
+          to += e.plane;
+          store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, rows);
+          to -= e.plane;
         }
         continue;
       }
-      uint32_t w[16];
+      if (e.form == kFormA) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        w[j] = pack_bf16(__fmul_rn(v[2 * j], 1.0f / kScaleX), __fmul_rn(v[2 * j + 1], 1.0f / kScaleX));
-      if (vec && col0 + 32 <= p.n) {
-        if (real) {
-          uint4* to = reinterpret_cast<uint4*>(out + r * ld_out + col0);
+        for (int j = 0; j < 32; ++j) v[j] = __fmul_rn(v[j], kScaleA / (kScaleX * kScaleX));
+        keep_block(mine, v);
+      } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+        for (int j = 0; j < 32; ++j) {
+          // A as its products read it: errors of b A and c A A cancel in part
+          const float a = e.exact ? x[j] : __half2float(__float2half_rn(x[j]));
+          v[j] = __fmaf_rn(kNsB, a, __fmul_rn(v[j], kNsC / kScaleA));
+          if (col0 + j == r) v[j] = __fmaf_rn(kNsShift, kScaleA, v[j]);
         }
-        continue;
       }
-      __syncwarp();
+      store_symmetric(to, e.ld, p.n, r, col0, v, s);
+      if (e.exact) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) turn[lane * 17 + j] = w[j];
-      __syncwarp();
-      const uint32_t r0 = r - lane, rows = p.m - min(p.m, r0);
-      if (col0 + lane < p.n)
-        for (uint32_t i = 0; i < 32 && i < rows; ++i)
-          out[(r0 + i) * ld_out + col0 + lane] = reinterpret_cast<const uint16_t*>(turn + i * 17)[lane];
+        for (int j = 0; j < 32; ++j) v[j] = half_rest(v[j]);
+        store_symmetric(to + e.plane, e.ld, p.n, r, col0, v, s);
+      }
     }
   }
 };
@@ -379,23 +379,76 @@ struct StepEpilogue {
 constexpr size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 constexpr uint32_t round_up(uint32_t x, uint32_t to) { return (x + to - 1) / to * to; }
 
-// Matrices of one shape: consecutive in scratch, one entry of a launch.
+// Entries of a launch, per group: A from either X, B, and X from either X.
+enum : uint32_t { kEntryA = 0, kEntryB = 2, kEntryX = 3, kEntries = 5 };
+constexpr uint32_t kOrthoGroups = 12;  // shapes per launch, at most
+
+// Matrices of one shape: consecutive in scratch.
 struct Group {
-  uint32_t rows = 0, cols = 0, side = 0, ld_x = 0, ld_s = 0;
+  uint32_t rows = 0, cols = 0, side = 0, ld_x = 0, ld_s = 0, planes = 1;
   std::vector<uint32_t> mats;
-  size_t hi[2] = {0, 0}, lo[2] = {0, 0}, a = 0, b = 0;  // scratch offsets
-  uint32_t first = 0;  // its first matrix, in the groups' order
+  size_t half[2] = {0, 0}, x = 0, a = 0, a_blocks = 0, b = 0;  // scratch offsets
+  uint64_t x_floats = 0, a_floats = 0;  // of one matrix in blocks
+  uint32_t first = 0;                   // its first matrix, in the groups' order
+  bool left() const { return rows <= cols; }
 };
 
 struct Plan {
   std::vector<Group> groups;
-  // of each phase and group: A, B, X
-  std::vector<ProductShape> shape[3];
   size_t parts = 0, outs = 0, ld_outs = 0, join = 0, total = 0;
+  bool pair = false;
 };
 
-Plan make_plan(const OrthoMat* mats, uint32_t n, uint32_t sms) {
+uint64_t block_floats(uint32_t rows, uint32_t cols) {
+  return static_cast<uint64_t>(round_up(rows, kTileM)) * round_up(cols, 32);
+}
+
+// The shapes of a launch's products for `count` groups from `g0`; returns the
+// bytes of the scratch that joining K parts takes.
+template <class Args>
+size_t shape_products(Args& args, const Plan& plan, size_t g0, uint32_t count, double sms) {
+  double work[3] = {0.0, 0.0, 0.0};
+  auto cost = [](const Group& g, int form) {
+    const double s = g.side, x = static_cast<double>(g.rows) * g.cols;
+    return g.mats.size() * (g.planes * 2 - 1) *
+           (form == kFormA ? x * s * 0.5 : form == kFormB ? s * s * s * 0.5 : x * s);
+  };
+  for (uint32_t i = 0; i < count; ++i)
+    for (int f = 0; f < 3; ++f) work[f] += cost(plan.groups[g0 + i], f);
+  for (uint32_t i = 0; i < count; ++i) {
+    const Group& g = plan.groups[g0 + i];
+    const uint32_t batch = static_cast<uint32_t>(g.mats.size()), terms = g.planes * 2 - 1;
+    const uint32_t deep = g.left() ? g.cols : g.rows;
+    for (int f = 0; f < 3; ++f) {
+      ProductShape s = {};
+      double mine = cost(g, f) / work[f] * sms;
+      if (mine < 1.0) mine = 1.0;
+      if (f == kFormA) plan_product(s, {g.side, g.side, deep, batch, true, plan.pair, mine, 16, terms});
+      if (f == kFormB) plan_product(s, {g.side, g.side, g.side, batch, true, plan.pair, mine, 8, terms});
+      if (f == kFormX) plan_product(s, {g.rows, g.cols, g.side, batch, false, plan.pair, mine, 1, terms});
+      if (f == kFormA) args.shape[kEntryA * count + i] = args.shape[(kEntryA + 1) * count + i] = s;
+      if (f == kFormB) args.shape[kEntryB * count + i] = s;
+      if (f == kFormX) args.shape[kEntryX * count + i] = args.shape[(kEntryX + 1) * count + i] = s;
+    }
+  }
+  args.phases = 3 * kSteps;
+  for (uint32_t ph = 0; ph < args.phases; ++ph) {
+    const uint32_t form = ph % 3, from = (ph / 3) & 1u;
+    const uint32_t entry = form == kFormA ? kEntryA + from : form == kFormB ? kEntryB : kEntryX + from;
+    args.first[ph] = entry * count;
+    args.problems[ph] = count;
+  }
+  return number_items(args, plan.pair);
+}
+
+// Kernel parameters for 1, 4 or kOrthoGroups shapes: a launch copies them.
+template <int kGroups>
+using StepArgs = ProductArgs<StepEpilogue, static_cast<int>(kEntries) * kGroups>;
+
+Plan make_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
   Plan p;
+  const double sms = dev.sm_count;
+  double items = 0.0;
   for (uint32_t i = 0; i < n; ++i) {
     if (mats[i].rows == 0 || mats[i].cols == 0) continue;
     Group* g = nullptr;
@@ -409,9 +462,15 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, uint32_t sms) {
       g->side = g->rows < g->cols ? g->rows : g->cols;
       g->ld_x = round_up(g->cols, 8);
       g->ld_s = round_up(g->side, 8);
+      g->planes = g->side <= kExactSide ? 2 : 1;
     }
     g->mats.push_back(i);
+    const double pairs = (g->side + 255) / 256;
+    items += pairs * (pairs + 1) / 2;
   }
+  // Pairs of CTAs (256 x 256 tiles) once the symmetric products, which have the
+  // fewest tiles, fill them.
+  p.pair = items >= sms / 2;
   // the deepest products first: their tiles take longest
   std::stable_sort(p.groups.begin(), p.groups.end(), [](const Group& x, const Group& y) {
     return x.side != y.side ? x.side > y.side
@@ -425,55 +484,30 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, uint32_t sms) {
     return here;
   };
   uint32_t all = 0;
-  double work[3] = {0.0, 0.0, 0.0};
-  auto cost = [](const Group& g, int phase) {
-    const double s = g.side, x = static_cast<double>(g.rows) * g.cols;
-    return g.mats.size() * (phase == 0 ? x * s * 0.5 : phase == 1 ? s * s * s * 0.5 : x * s);
-  };
   for (Group& g : p.groups) {
     const size_t batch = g.mats.size();
-    const size_t x = 2ull * batch * g.rows * g.ld_x, s = 2ull * batch * g.side * g.ld_s;
-    for (int i = 0; i < 2; ++i) {
-      g.hi[i] = take(x);
-      g.lo[i] = take(x);
-    }
+    const size_t x = 2ull * batch * g.planes * g.rows * g.ld_x;
+    const size_t s = 2ull * batch * g.planes * g.side * g.ld_s;
+    g.x_floats = block_floats(g.rows, g.cols);
+    g.a_floats = block_floats(g.side, g.side);
+    for (int i = 0; i < 2; ++i) g.half[i] = take(x);
+    g.x = take(4 * batch * g.x_floats);
     g.a = take(s);
+    g.a_blocks = take(4 * batch * g.a_floats);
     g.b = take(s);
     g.first = all;
     all += static_cast<uint32_t>(batch);
-    for (int ph = 0; ph < 3; ++ph) work[ph] += cost(g, ph);
   }
   p.parts = take(sizeof(FF) * kMaxParts * all);
   p.outs = take(8ull * all);
   p.ld_outs = take(8ull * all);
   size_t join = 0;
-  for (int ph = 0; ph < 3; ++ph) {
-    size_t slots = 0, chunks = 0, most = 0;
-    for (size_t i = 0; i < p.groups.size(); ++i) {
-      const Group& g = p.groups[i];
-      ProductShape s = {};
-      const double share = cost(g, ph) / work[ph] * sms;
-      const uint32_t mine = share < 1.0 ? 1u : static_cast<uint32_t>(share);
-      const uint32_t batch = static_cast<uint32_t>(g.mats.size());
-      const uint32_t splits = 8;
-      if (ph == 0)
-        plan_product(s, g.side, g.side, g.rows < g.cols ? g.cols : g.rows, batch, true, mine, splits);
-      else if (ph == 1)
-        plan_product(s, g.side, g.side, g.side, batch, true, mine, splits);
-      else
-        plan_product(s, g.rows, g.cols, g.side, batch, false, mine, splits);
-      if (s.splits > 1) {
-        slots += static_cast<size_t>(s.tiles) * s.batch * s.splits;
-        if ((s.bn + 31) / 32 > chunks) chunks = (s.bn + 31) / 32;
-      }
-      p.shape[ph].push_back(s);
-      if (i % kOrthoGroups == kOrthoGroups - 1 || i + 1 == p.groups.size()) {  // one launch
-        const size_t bytes = 4ull * kTileM * 32 * chunks * slots;
-        if (bytes > most) most = bytes;
-        slots = chunks = 0;
-      }
-    }
-    if (most > join) join = most;
+  for (size_t g0 = 0; g0 < p.groups.size(); g0 += kOrthoGroups) {
+    const size_t left = p.groups.size() - g0;
+    std::unique_ptr<StepArgs<kOrthoGroups>> args(new StepArgs<kOrthoGroups>());
+    const size_t bytes =
+        shape_products(*args, p, g0, static_cast<uint32_t>(left < kOrthoGroups ? left : kOrthoGroups), sms);
+    if (bytes > join) join = bytes;
   }
   p.join = take(join);
   p.total = at;
@@ -489,29 +523,10 @@ cudaError_t launch_prep(Fn fn, PrepArgs& a, uint32_t ctas, cudaStream_t stream) 
   return e;
 }
 
-bool operand(CUtensorMap* map, const char* base, uint64_t cols, uint64_t rows, uint64_t ld,
-             uint64_t batch, uint32_t box) {
-  return make_map(map, base, false, cols, rows, ld, batch, rows * ld, box);
-}
-
-}  // namespace
-
-size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
-  return make_plan(mats, n, static_cast<uint32_t>(dev.sm_count)).total;
-}
-
-cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
-                                 Workspace& ws, const DeviceInfo& dev) {
-  const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
-  const Plan plan = make_plan(mats, n, sms);
-  if (plan.groups.empty()) return cudaSuccess;
-  char* base = ws.model_scratch();
-  auto half = [&](size_t off) { return reinterpret_cast<uint16_t*>(base + off); };
-  cudaError_t err = cudaSuccess;
-
-  // momentum, norms, X
+// Momentum, norms and the first X of every matrix.
+cudaError_t prepare(const OrthoMat* mats, const Plan& plan, bool bf16, float mu, char* base,
+                    Workspace& ws) {
   PrepArgs prep = {};
-  prep.bf16 = bf16 ? 1u : 0u;
   prep.mu = mu;
   prep.parts = reinterpret_cast<FF*>(base + plan.parts);
   prep.outs = reinterpret_cast<uint16_t**>(base + plan.outs);
@@ -531,87 +546,129 @@ cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, fl
     for (size_t b = 0; b < g.mats.size(); ++b, ++index) {
       const OrthoMat& m = mats[g.mats[b]];
       PrepMat& t = prep.mat[prep.mats++];
-      const uint64_t units = static_cast<uint64_t>(m.rows) * ((m.cols + kSegment - 1) / kSegment);
-      uint64_t per = (units + kMaxParts - 1) / kMaxParts;
-      if (per < 32) per = 32;  // 4 a warp
       t.u = m.u;
       t.m = m.m;
       t.out = m.out;
-      t.ld_out = m.ld_out;
-      t.index = index;
-      t.hi = half(g.hi[0]) + b * g.rows * g.ld_x;
-      t.lo = half(g.lo[0]) + b * g.rows * g.ld_x;
       t.ld_u = m.ld_u;
       t.ld_m = m.ld_m;
+      t.ld_out = m.ld_out;
+      t.x = reinterpret_cast<float*>(base + g.x) + b * g.x_floats;
+      t.hi = reinterpret_cast<uint16_t*>(base + g.half[0]) +
+             b * g.planes * g.rows * static_cast<uint64_t>(g.ld_x);
+      t.lo = g.planes == 2 ? t.hi + g.rows * static_cast<uint64_t>(g.ld_x) : nullptr;
       t.rows = m.rows;
       t.cols = m.cols;
       t.ld_x = g.ld_x;
-      t.units_per_cta = static_cast<uint32_t>(per);
+      t.chunks = round_up(g.cols, 32) / 32;
+      t.blocks_n = (m.cols + kPrepCols - 1) / kPrepCols;
+      t.blocks = (m.rows + kTileM - 1) / kTileM * t.blocks_n;
+      t.blocks_per_cta = (t.blocks + kMaxParts - 1) / kMaxParts;
+      t.index = index;
       t.cta0 = ctas;
       t.part0 = index * kMaxParts;
-      t.parts = static_cast<uint32_t>((units + per - 1) / per);
+      t.parts = (t.blocks + t.blocks_per_cta - 1) / t.blocks_per_cta;
       ctas += t.parts;
-      if (prep.mats == kPrepMats && (err = flush()) != cudaSuccess) return err;
-    }
-  }
-  if ((err = flush()) != cudaSuccess) return err;
-
-  const size_t groups = plan.groups.size();
-  for (int step = 0; step < kSteps; ++step) {
-    const int from = step & 1, to = from ^ 1;
-    const bool last = step == kSteps - 1;
-    for (int ph = 0; ph < 3; ++ph) {
-      for (size_t g0 = 0; g0 < groups; g0 += kOrthoGroups) {
-        const size_t g1 = g0 + kOrthoGroups < groups ? g0 + kOrthoGroups : groups;
-        ProductArgs<SymmetricEpilogue<false>, kOrthoGroups> pa = {};
-        ProductArgs<SymmetricEpilogue<true>, kOrthoGroups> pb = {};
-        ProductArgs<StepEpilogue, kOrthoGroups> px = {};
-        for (size_t i = g0; i < g1; ++i) {
-          const Group& g = plan.groups[i];
-          const bool left = g.rows <= g.cols;
-          const uint64_t batch = g.mats.size();
-          const char *x = base + g.hi[from], *a = base + g.a, *b = base + g.b;
-          ProductShape s = plan.shape[ph][i];
-          bool ok;
-          if (ph == 0) {
-            s.a_mn = s.b_mn = left ? 0u : 1u;
-            ok = operand(&s.a, x, g.cols, g.rows, g.ld_x, batch, left ? kTileM : 64) &&
-                 operand(&s.b, x, g.cols, g.rows, g.ld_x, batch, left ? s.bn : 64);
-            pa.shape[i - g0] = s;
-            pa.epi[i - g0] = {nullptr, half(g.a), g.ld_s, static_cast<uint64_t>(g.side) * g.ld_s};
-          } else if (ph == 1) {
-            ok = operand(&s.a, a, g.side, g.side, g.ld_s, batch, kTileM) &&
-                 operand(&s.b, a, g.side, g.side, g.ld_s, batch, s.bn);
-            pb.shape[i - g0] = s;
-            pb.epi[i - g0] = {half(g.a), half(g.b), g.ld_s, static_cast<uint64_t>(g.side) * g.ld_s};
-          } else {
-            if (left) {  // B X: X is MN-major
-              s.b_mn = 1;
-              ok = operand(&s.a, b, g.side, g.side, g.ld_s, batch, kTileM) &&
-                   operand(&s.b, x, g.cols, g.rows, g.ld_x, batch, 64);
-            } else {  // X B: B is symmetric, its rows are its columns
-              ok = operand(&s.a, x, g.cols, g.rows, g.ld_x, batch, kTileM) &&
-                   operand(&s.b, b, g.side, g.side, g.ld_s, batch, s.bn);
-            }
-            px.shape[i - g0] = s;
-            px.epi[i - g0] = {half(g.hi[from]), half(g.lo[from]), half(g.hi[to]), half(g.lo[to]),
-                              g.ld_x, static_cast<uint64_t>(g.rows) * g.ld_x,
-                              last ? prep.outs + g.first : nullptr,
-                              last ? prep.ld_outs + g.first : nullptr};
-          }
-          if (!ok) return cudaErrorInvalidValue;
-        }
-        float* join = reinterpret_cast<float*>(base + plan.join);
-        const uint32_t count = static_cast<uint32_t>(g1 - g0);
-        pa.problems = pb.problems = px.problems = count;
-        pa.parts = pb.parts = px.parts = join;
-        err = ph == 0 ? launch_product(pa, ws, dev)
-                      : ph == 1 ? launch_product(pb, ws, dev) : launch_product(px, ws, dev);
-        if (err != cudaSuccess) return err;
+      if (prep.mats == kPrepMats) {
+        const cudaError_t e = flush();
+        if (e != cudaSuccess) return e;
       }
     }
   }
-  return cudaSuccess;
+  return flush();
+}
+
+// The products of `count` groups from `g0`, all steps.
+template <int kGroups>
+cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Workspace& ws,
+                  const DeviceInfo& dev) {
+  std::unique_ptr<StepArgs<kGroups>> held(new StepArgs<kGroups>());
+  StepArgs<kGroups>& args = *held;
+  shape_products(args, plan, g0, count, dev.sm_count);
+  const bool pair = plan.pair;
+  bool ok = true;
+  for (uint32_t i = 0; i < count; ++i) {
+    const Group& g = plan.groups[g0 + i];
+    const bool left = g.left();
+    const uint64_t batch = g.mats.size() * g.planes;
+    auto map = [&](CUtensorMap* to, size_t at, bool square, uint32_t box) {
+      const uint32_t rows = square ? g.side : g.rows, cols = square ? g.side : g.cols;
+      const uint32_t ld = square ? g.ld_s : g.ld_x;
+      ok = ok && make_map(to, base + at, false, cols, rows, ld, batch,
+                          static_cast<uint64_t>(rows) * ld, box);
+    };
+    StepEpilogue::Params e = {};
+    e.exact = g.planes == 2 ? 1u : 0u;
+    e.last_phase = 3 * kSteps - 1;
+    e.outs = reinterpret_cast<uint16_t* const*>(base + plan.outs) + g.first;
+    e.ld_outs = reinterpret_cast<const uint64_t*>(base + plan.ld_outs) + g.first;
+    for (uint32_t from = 0; from < 2; ++from) {
+      {
+        ProductShape& s = args.shape[(kEntryA + from) * count + i];
+        s.a_mn = s.b_mn = left ? 0u : 1u;
+        map(&s.a, g.half[from], false, kTileM);
+        map(&s.b, g.half[from], false, left ? b_box(s, pair) : kTileK);
+        e.form = kFormA;
+        e.ld = g.ld_s;
+        e.chunks = round_up(g.side, 32) / 32;
+        e.plane = static_cast<uint64_t>(g.side) * g.ld_s;
+        e.batch_blocks = g.a_floats;
+        e.to = reinterpret_cast<uint16_t*>(base + g.a);
+        e.blocks = reinterpret_cast<float*>(base + g.a_blocks);
+        args.epi[(kEntryA + from) * count + i] = e;
+      }
+      if (from == 0) {
+        ProductShape& s = args.shape[kEntryB * count + i];
+        map(&s.a, g.a, true, kTileM);
+        map(&s.b, g.a, true, b_box(s, pair));
+        e.form = kFormB;
+        e.to = reinterpret_cast<uint16_t*>(base + g.b);
+        args.epi[kEntryB * count + i] = e;
+      }
+      ProductShape& s = args.shape[(kEntryX + from) * count + i];
+      if (left) {  // B X: X is MN-major
+        s.b_mn = 1;
+        map(&s.a, g.b, true, kTileM);
+        map(&s.b, g.half[from], false, kTileK);
+      } else {  // X B: B is symmetric, its rows are its columns
+        map(&s.a, g.half[from], false, kTileM);
+        map(&s.b, g.b, true, b_box(s, pair));
+      }
+      e.form = kFormX;
+      e.ld = g.ld_x;
+      e.chunks = round_up(g.cols, 32) / 32;
+      e.plane = static_cast<uint64_t>(g.rows) * g.ld_x;
+      e.batch_blocks = g.x_floats;
+      e.to = reinterpret_cast<uint16_t*>(base + g.half[from ^ 1u]);
+      e.blocks = reinterpret_cast<float*>(base + g.x);
+      args.epi[(kEntryX + from) * count + i] = e;
+    }
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  args.parts = reinterpret_cast<float*>(base + plan.join);
+  return pair ? launch_product<StepEpilogue, kEntries * kGroups, true>(args, ws, dev)
+              : launch_product<StepEpilogue, kEntries * kGroups, false>(args, ws, dev);
+}
+
+}  // namespace
+
+size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
+  return make_plan(mats, n, dev).total;
+}
+
+cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
+                                 Workspace& ws, const DeviceInfo& dev) {
+  const Plan plan = make_plan(mats, n, dev);
+  if (plan.groups.empty()) return cudaSuccess;
+  char* base = ws.model_scratch();
+  cudaError_t e = prepare(mats, plan, bf16, mu, base, ws);
+  for (size_t g0 = 0; g0 < plan.groups.size() && e == cudaSuccess; g0 += kOrthoGroups) {
+    const size_t left = plan.groups.size() - g0;
+    const uint32_t count = static_cast<uint32_t>(left < kOrthoGroups ? left : kOrthoGroups);
+    e = count == 1 ? steps<1>(plan, g0, count, base, ws, dev)
+        : count <= 4 ? steps<4>(plan, g0, count, base, ws, dev)
+                     : steps<kOrthoGroups>(plan, g0, count, base, ws, dev);
+  }
+  return e;
 }
 
 }  // namespace efs

@@ -1,5 +1,7 @@
 // product.cu — host side of the tensor-core products: tensor maps and the
 // choice of tile width and K parts.
+#include <cmath>
+
 #include "product.cuh"
 
 namespace efs {
@@ -38,51 +40,48 @@ bool make_map(CUtensorMap* map, const void* base, bool bf16, uint64_t cols, uint
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The time of a launch is its longest CTA's: whole tiles per CTA, each of its
-// 64-deep steps (2 cycles per column on the tensor cores, or the cycles that
-// filling shared memory takes for narrow tiles) plus a start that does not
-// overlap, and for K parts the join by one CTA (8 cycles per column and part).
-void plan_product(ProductShape& p, uint32_t m, uint32_t n, uint32_t k, uint32_t batch,
-                  bool lower, uint32_t sms, uint32_t max_splits) {
-  p.m = m;
-  p.n = n;
-  p.k = k;
-  p.batch = batch;
-  p.lower = lower ? 1u : 0u;
-  p.tiles_m = (m + kTileM - 1) / kTileM;
+// The time of a launch is its longest CTA's (or pair's): whole tiles, each of
+// its 128-deep steps (4 cycles per column on the tensor cores, or the cycles
+// that a CTA's share of A and B takes from L2 at 64 bytes a cycle) plus what a
+// tile costs beside them, and for joined K parts the join by one CTA, which
+// reads them at about 64 bytes a cycle too.
+void plan_product(ProductShape& p, const ProductWant& w) {
+  const uint32_t rows = w.pair ? 2 * kTileM : kTileM;
+  p.m = w.m;
+  p.n = w.n;
+  p.k = w.k;
+  p.batch = w.batch;
+  p.lower = w.lower ? 1u : 0u;
+  p.terms = w.terms;
+  p.join = 1;
+  p.tiles_m = (w.m + rows - 1) / rows;
   p.group_m = p.tiles_m ? p.tiles_m : 1;
-  const uint64_t kts = (k + kTileK - 1) / kTileK;
+  const double units = w.pair ? w.sms / 2 : w.sms;
+  const uint32_t kts = (w.k + kTileK - 1) / kTileK * w.terms;
   double best = 0.0;
-  uint32_t best_bn = 0, best_splits = 1;
+  p.bn = 0;
   const uint32_t widths[] = {256, 192, 128, 64};
   for (uint32_t bn : widths) {
-    if (lower && bn % kTileM) continue;  // rows of tiles pair up to a tile's width
-    if (bn > (lower ? 128u : 64u) && bn >= 2 * n) continue;
-    const uint64_t tiles_n = (n + bn - 1) / bn, q = bn / kTileM ? bn / kTileM : 1;
-    const uint64_t groups = (p.tiles_m + q - 1) / q;
-    const uint64_t tiles = (lower ? q * groups * (groups + 1) / 2 : p.tiles_m * tiles_n) * batch;
-    const double step = bn * 2.0 > (kTileM + bn) * 1.5 ? bn * 2.0 : (kTileM + bn) * 1.5;
-    for (uint32_t s = 1; s <= max_splits && s <= (kts ? kts : 1); ++s) {
-      if (s > 1 && tiles > 4 * sms) break;  // nothing to gain (and scratch tiles stay few)
-      const double waves = static_cast<double>((tiles * s + sms - 1) / sms);
+    if (w.lower ? bn != rows : bn > 64 && bn >= 2 * w.n) continue;
+    const double tiles = (w.lower ? p.tiles_m * (p.tiles_m + 1.0) / 2.0
+                                  : p.tiles_m * static_cast<double>((w.n + bn - 1) / bn)) * w.batch;
+    const double mma = 4.0 * bn, load = 4.0 * (kTileM + (w.pair ? bn / 2 : bn));
+    const double step = mma > load ? mma : load;
+    for (uint32_t s = 1; s <= w.max_splits && s <= (kts ? kts : 1); ++s) {
+      if (s > 1 && tiles > 2 * units) break;  // nothing to gain
+      const double waves = ceil(tiles * s / units);
       const double deep = static_cast<double>((kts + s - 1) / s);
-      const double t = waves * (deep * step + 1500.0 + 4.0 * bn) + (s > 1 ? (s + 1) * 8.0 * bn + 2000.0 : 0.0);
-      if (best_bn == 0 || t < best * 0.999) {
+      const double t = waves * (deep * step + 1500.0 + 6.0 * bn) +
+                       (s > 1 ? (s + 1) * 8.0 * bn + 2500.0 : 0.0);
+      if (p.bn == 0 || t < best * 0.999) {
         best = t;
-        best_bn = bn;
-        best_splits = s;
+        p.bn = bn;
+        p.splits = s;
       }
     }
   }
-  p.bn = best_bn;
-  p.splits = best_splits;
-  p.tiles_n = (n + p.bn - 1) / p.bn;
-  if (lower) {
-    const uint32_t q = p.bn / kTileM, groups = (p.tiles_m + q - 1) / q;
-    p.tiles = q * groups * (groups + 1) / 2;
-  } else {
-    p.tiles = p.tiles_m * p.tiles_n;
-  }
+  p.tiles_n = (w.n + p.bn - 1) / p.bn;
+  p.tiles = w.lower ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
 }
 
 }  // namespace efs

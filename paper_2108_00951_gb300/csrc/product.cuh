@@ -1,20 +1,30 @@
 // product.cuh — tiled matrix products D = A B^T on the tensor cores with an
 // epilogue of the caller's: persistent CTAs, one per SM, each a TMA producer
-// warp, an MMA warp and four epilogue warps.
+// warp, an MMA warp and eight epilogue warps; two CTAs can work as a pair.
 //
-// A CTA walks over the work items of up to a few products ("problems") in one
-// launch. An item is one 128 x bn tile of D, or one of `splits` parts of its
-// K axis. The producer fills a ring of shared-memory stages (64 of K each)
-// with 128-byte-swizzled tiles; the MMA warp multiplies them into one of two
-// accumulators in tensor memory, so the epilogue of one tile runs under the
-// products of the next. Either operand may be stored K-major (rows along K)
-// or MN-major (rows along M or N), so no operand is ever transposed in
-// memory.
+// A CTA (or pair) walks over the work items of a few products ("problems") in
+// one launch. An item is one tile of D, 128 (a pair: 256) x bn, or one of
+// `splits` parts of its K axis. The producer fills a ring of shared-memory
+// stages (128 of K each) with 128-byte-swizzled tiles; the MMA warp multiplies
+// them into one of two accumulators in tensor memory, so the epilogue of one
+// tile runs under the products of the next. Either operand may be stored
+// K-major (rows along K) or MN-major (rows along M or N), so no operand is
+// ever transposed in memory.
+//
+// What bounds it: an SM takes about 64 bytes a cycle from L2 (measured on a
+// GB300: 130 GB/s in boxes of 16 KB; in boxes of 8 KB, 104 to 108), and a
+// 128 x 256 tile needs 96 a cycle at the tensor cores' full rate (8192
+// operations a cycle, 512 cycles per 64 of K). A pair shares its B tile, each
+// CTA loading half: 64 bytes a cycle. Stages are 128 of K deep so that every
+// box has 16 KB, K-major (64 k x 128 rows) or MN-major (64 x 128 k).
 //
 // Parts of K are joined without waiting: each part writes its fp32
 // accumulators to scratch and counts itself in; the last part to arrive adds
 // all parts in their order (so the sum does not depend on which was last) and
 // runs the epilogue.
+//
+// A launch may have several phases with a grid barrier between (a cooperative
+// launch): what one phase's epilogues write the next one's TMA reads.
 //
 // Every wait on an mbarrier is bounded (tma.cuh); one that runs out latches a
 // timeout, and the CTA ends without its results.
@@ -25,94 +35,111 @@
 
 namespace efs {
 
-constexpr int kTileM = 128;        // rows of a tile: lanes of tensor memory
-constexpr int kTileNMax = 256;     // columns of a tile, at most
-constexpr int kTileK = 64;         // one 128-byte swizzle row of 16-bit elements
-constexpr int kProductStages = 4;  // 48 KB each: 192 KB in flight per SM
-constexpr int kProductThreads = 192;
-constexpr uint32_t kStageABytes = kTileM * kTileK * 2;
-constexpr uint32_t kStageBBytes = kTileNMax * kTileK * 2;
-constexpr uint32_t kStageBytes = kStageABytes + kStageBBytes;
-constexpr uint32_t kBoxMnBytes = 64 * kTileK * 2;  // an MN-major box: 64 elements x 64 k
+constexpr uint32_t kTileM = 128;    // rows of a CTA's tile: lanes of tensor memory
+constexpr uint32_t kTileNMax = 256; // columns of a tile, at most
+constexpr uint32_t kTileK = 128;    // per stage: two 128-byte swizzle rows of 16-bit elements
+constexpr uint32_t kEpilogueWarps = 8;
+constexpr uint32_t kProductThreads = (2 + kEpilogueWarps) * 32;
+constexpr uint32_t kBoxMnBytes = 64 * kTileK * 2;  // an MN-major box: 64 elements x 128 k
+
+// Stages of the ring: 192 KB either way.
+template <bool kPair>
+struct Ring {
+  static constexpr uint32_t kStages = kPair ? 3 : 2;
+  static constexpr uint32_t kABytes = kTileM * kTileK * 2;
+  static constexpr uint32_t kBBytes = (kPair ? kTileNMax / 2 : kTileNMax) * kTileK * 2;
+  static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+  static constexpr uint32_t kBytes = kStages * kStageBytes;
+};
 
 // One product of a launch. The tensor maps are 3-D (innermost, rows, batch);
-// a K-major operand's box is {64, rows of the tile}, an MN-major one's {64, 64}.
+// a K-major operand's box is {64, rows a CTA loads}, an MN-major one's {64, 128}.
+// With terms = 3 each operand is a sum hi + lo of two planes (batch entries
+// 2 i and 2 i + 1 of its map), and D = hi hi + hi lo + lo hi.
 struct ProductShape {
   CUtensorMap a, b;
   uint32_t m, n, k;
-  uint32_t a_mn, b_mn, bf16;
-  uint32_t bn;                // columns per tile: a multiple of 16 (MN-major B: of 64)
+  uint32_t a_mn, b_mn, bf16, terms;
+  uint32_t bn;                // columns per tile: a multiple of 64
   uint32_t tiles_m, tiles_n, batch, splits;
   uint32_t group_m;           // tiles are walked in groups of this many tile rows
-  uint32_t lower;             // only tiles that reach the diagonal or below it
+  uint32_t lower;             // square tiles on and below the diagonal only
   uint32_t tiles;             // per batch entry
-  uint32_t item0;             // this problem's first work item of the launch
-  uint32_t slot0;             // its first scratch tile (splits > 1)
+  uint32_t item0;             // this problem's first work item of its phase
+  uint32_t part0;             // its first scratch tile (splits > 1)
+  uint32_t join;              // parts are joined here (else the epilogue gets each)
   const uint32_t* count;      // device: rows that exist (nullptr: all)
   uint32_t count_is_k;        // the count bounds K (else M)
 };
 
 struct ProductItem {
-  uint32_t batch, tm, tn, m0, n0, n_eff, k0, kt, slot, split;
+  uint32_t batch, tn, m0, n0, n_eff, k, k0, kt, kts, part, split;
   bool skip;
 };
 
-__device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint32_t item) {
+template <bool kPair>
+__device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint32_t item,
+                                                    uint32_t rank) {
+  constexpr uint32_t kRows = kPair ? 2 * kTileM : kTileM;
   ProductItem it;
   uint32_t r = item - p.item0;
   it.split = r % p.splits;
   r /= p.splits;
   it.batch = r / p.tiles;
   r -= it.batch * p.tiles;
-  if (p.lower) {
-    // row group g (bn / 128 tile rows) holds q (g + 1) tiles, after q g (g + 1) / 2 others
-    const uint32_t q = p.bn / kTileM;
-    uint32_t g = static_cast<uint32_t>(sqrtf(2.0f * static_cast<float>(r / q) + 0.25f) - 0.5f);
-    while (q * (g + 1) * (g + 2) / 2 <= r) ++g;
-    while (q * g * (g + 1) / 2 > r) --g;
-    const uint32_t rem = r - q * g * (g + 1) / 2;
-    it.tm = q * g + rem / (g + 1);
-    it.tn = rem % (g + 1);
+  uint32_t tm;
+  if (p.lower) {  // tile row i holds i + 1 tiles
+    uint32_t i = static_cast<uint32_t>(sqrtf(2.0f * static_cast<float>(r) + 0.25f) - 0.5f);
+    while ((i + 1) * (i + 2) / 2 <= r) ++i;
+    while (i * (i + 1) / 2 > r) --i;
+    tm = i;
+    it.tn = r - i * (i + 1) / 2;
   } else {
     const uint32_t per = p.group_m * p.tiles_n;
     const uint32_t g = r / per, in = r - g * per;
     const uint32_t rows = min(p.group_m, p.tiles_m - g * p.group_m);
     it.tn = in / rows;
-    it.tm = g * p.group_m + in % rows;
+    tm = g * p.group_m + in % rows;
   }
-  it.m0 = it.tm * kTileM;
+  it.m0 = tm * kRows;
   it.n0 = it.tn * p.bn;
-  it.n_eff = min(p.bn, (p.n - min(p.n, it.n0) + 15u) & ~15u);
-  it.skip = it.tm >= p.tiles_m;
+  it.n_eff = min(p.bn, (p.n - min(p.n, it.n0) + 31u) & ~31u);
+  it.skip = false;
   uint32_t k = p.k;
   if (p.count) {
     const uint32_t c = *p.count;
     if (p.count_is_k) k = min(k, c);
-    else it.skip |= it.m0 >= c;
+    else it.skip = it.m0 >= c;
   }
-  const uint32_t kts = (k + kTileK - 1) / kTileK;
-  const uint32_t lo = static_cast<uint32_t>(static_cast<uint64_t>(kts) * it.split / p.splits);
-  const uint32_t hi = static_cast<uint32_t>(static_cast<uint64_t>(kts) * (it.split + 1) / p.splits);
-  it.k0 = lo * kTileK;
-  it.kt = hi - lo;
-  it.slot = p.slot0 + (it.batch * p.tiles + r) * p.splits;  // its parts: slot .. slot + splits - 1
+  it.m0 += rank * kTileM;
+  it.k = k;
+  it.kts = (k + kTileK - 1) / kTileK;
+  const uint64_t all = static_cast<uint64_t>(it.kts) * p.terms;
+  it.k0 = static_cast<uint32_t>(all * it.split / p.splits);
+  it.kt = static_cast<uint32_t>(all * (it.split + 1) / p.splits) - it.k0;
+  it.part = p.part0 + ((it.batch * p.tiles + r) * (kPair ? 2 : 1) + rank) * p.splits;
   return it;
 }
+
+constexpr uint32_t kMaxPhases = 16;
 
 template <class Epi, int kMaxProblems>
 struct ProductArgs {
   ProductShape shape[kMaxProblems];
   typename Epi::Params epi[kMaxProblems];
-  uint32_t problems, items;
+  uint32_t phases;
+  uint32_t first[kMaxPhases], problems[kMaxPhases], items[kMaxPhases];  // of each phase
   float* parts;         // scratch tiles of split items
   uint32_t* arrivals;   // by the tile's first scratch tile; zero between launches
   uint32_t part_chunks; // 32-column chunks per scratch tile
   uint32_t* error;
+  uint32_t entries;     // problems in shape[]
+  uint32_t* barrier;    // grid barrier: arrivals, CTAs finished (zero between launches)
   uint64_t wait_ns;
 };
 
 struct ProductSmem {
-  uint64_t full[kProductStages], empty[kProductStages], acc_full[2], acc_empty[2];
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2];
   uint32_t tmem, last;
 };
 
@@ -120,12 +147,18 @@ struct ProductSmem {
 // row at a time, in order, from tensor memory or as the sum of the K parts.
 struct ProductAcc {
   uint32_t tmem;            // address of the accumulator, the warp's lanes
-  uint64_t* release;        // arrived on after the last chunk was read
+  uint32_t release;         // barrier arrived on after the warp's last chunk was read
+  uint32_t c0, c1;          // the warp's chunks
   const float* parts;       // != nullptr: sum `splits` scratch tiles instead
   uint64_t part_stride;     // floats from one part to the next
-  uint32_t splits, chunks;
+  uint32_t splits;
   bool none;                // K is empty: zeros
 
+  __device__ __forceinline__ void arrive() const {
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive_cluster(release);
+  }
   // All lanes of the warp call it alike.
   __device__ __forceinline__ void load(uint32_t c, float (&v)[32]) const {
     __syncwarp();
@@ -135,11 +168,12 @@ struct ProductAcc {
     } else if (parts) {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+      const float* src = parts + static_cast<uint64_t>(c) * (32 * kTileM);
+#pragma unroll 2
       for (uint32_t s = 0; s < splits; ++s) {
-        const float* src = parts + s * part_stride + static_cast<uint64_t>(c) * (32 * kTileM);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float4 x = __ldcg(reinterpret_cast<const float4*>(src) + j * kTileM);
+          const float4 x = __ldcg(reinterpret_cast<const float4*>(src + s * part_stride) + j * kTileM);
           v[4 * j] = __fadd_rn(v[4 * j], x.x);
           v[4 * j + 1] = __fadd_rn(v[4 * j + 1], x.y);
           v[4 * j + 2] = __fadd_rn(v[4 * j + 2], x.z);
@@ -148,188 +182,332 @@ struct ProductAcc {
       }
     } else {
       tmem_load_32(tmem + c * 32, v);
-      if (c + 1 == chunks) {
-        tc_fence_before();
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(release);
-      }
+      if (c + 1 == c1) arrive();
     }
   }
 };
 
-template <class Epi, int kMaxProblems>
+// Barrier of all CTAs of a cooperative launch: `target` arrivals since the
+// launch began. One word is counted up and polled.
+__device__ __forceinline__ bool phase_barrier(uint32_t* word, uint32_t target, uint64_t limit_ns) {
+  __syncthreads();
+  bool ok = true;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    atomicAdd(word, 1u);
+    const uint64_t t0 = global_timer_ns();
+    uint32_t polls = 0;
+    while (static_cast<int32_t>(ld_acquire_u32(word) - target) < 0) {
+      if ((++polls & 63u) == 0 && (polls > (1u << 26) || global_timer_ns() - t0 > limit_ns)) {
+        ok = false;
+        break;
+      }
+    }
+    __threadfence();
+  }
+  return __syncthreads_and(ok);
+}
+
+template <class Epi, int kMaxProblems, bool kPair>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const __grid_constant__ ProductArgs<Epi, kMaxProblems> args) {
+  using R = Ring<kPair>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ ProductSmem s;
-  __shared__ typename Epi::Smem epi_smem;
+  __shared__ typename Epi::Smem epi_smem[kEpilogueWarps];
   uint8_t* stages = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = kPair ? cluster_rank() : 0u;
+  const uint32_t unit = kPair ? blockIdx.x >> 1 : blockIdx.x;
+  const uint32_t units = kPair ? gridDim.x >> 1 : gridDim.x;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kProductStages; ++i) {
+    for (uint32_t i = 0; i < R::kStages; ++i) {
       mbar_init(&s.full[i], 1);
       mbar_init(&s.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.acc_full[i], 1);
-      mbar_init(&s.acc_empty[i], 4);
+      mbar_init(&s.acc_empty[i], kEpilogueWarps * (kPair ? 2 : 1));
     }
     mbar_init_fence();
   }
-  if (warp == 1) tmem_alloc(&s.tmem, 512);
+  if (warp == 0)
+    for (uint32_t i = lane; i < args.entries; i += 32) {
+      prefetch_tensormap(&args.shape[i].a);
+      prefetch_tensormap(&args.shape[i].b);
+    }
+  if (warp == 1) tmem_alloc<kPair>(&s.tmem, 512);
   tc_fence_before();
   __syncthreads();
+  if (kPair) cluster_sync();
   tc_fence_after();
   const uint32_t tmem = s.tmem;
   griddep_wait();
   bool ok = true;
+  uint32_t stage = 0, phase = 0;    // ring position (producer, MMA)
+  uint32_t acc = 0, acc_phase = 0;  // accumulator (MMA, epilogue)
 
-  if (warp == 0) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0, prob = 0;
-      for (uint32_t item = blockIdx.x; item < args.items && ok; item += gridDim.x) {
-        while (prob + 1 < args.problems && item >= args.shape[prob + 1].item0) ++prob;
-        const ProductShape& p = args.shape[prob];
-        const ProductItem it = product_item(p, item);
-        if (it.skip) continue;
-        const uint32_t b_boxes = (it.n_eff + 63) / 64;
-        const uint32_t bytes = kStageABytes + (p.b_mn ? b_boxes * kBoxMnBytes : p.bn * kTileK * 2);
-        for (uint32_t kt = 0; kt < it.kt; ++kt) {
-          if (!mbar_wait(&s.empty[stage], phase ^ 1u, args.wait_ns)) {
-            ok = false;
-            break;
-          }
-          uint8_t* a = stages + stage * kStageBytes;
-          uint8_t* b = a + kStageABytes;
-          const uint32_t k = it.k0 + kt * kTileK;
-          mbar_arrive_expect_tx(&s.full[stage], bytes);
-          if (p.a_mn) {
-            tma_load_3d(a, &p.a, it.m0, k, it.batch, &s.full[stage]);
-            tma_load_3d(a + kBoxMnBytes, &p.a, it.m0 + 64, k, it.batch, &s.full[stage]);
-          } else {
-            tma_load_3d(a, &p.a, k, it.m0, it.batch, &s.full[stage]);
-          }
-          if (p.b_mn) {
-            for (uint32_t x = 0; x < b_boxes; ++x)
-              tma_load_3d(b + x * kBoxMnBytes, &p.b, it.n0 + 64 * x, k, it.batch, &s.full[stage]);
-          } else {
-            tma_load_3d(b, &p.b, k, it.n0, it.batch, &s.full[stage]);
-          }
-          if (++stage == kProductStages) {
-            stage = 0;
-            phase ^= 1u;
+  for (uint32_t ph = 0; ph < args.phases; ++ph) {
+    const uint32_t prob0 = args.first[ph], prob1 = prob0 + args.problems[ph];
+    const uint32_t items = args.items[ph];
+    uint32_t prob = prob0;
+    if (warp == 0) {
+      if (lane == 0) {
+        fence_proxy_async();  // operands of this phase may come from the last one's epilogues
+        for (uint32_t item = unit; item < items && ok; item += units) {
+          while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
+          const ProductShape& p = args.shape[prob];
+          const ProductItem it = product_item<kPair>(p, item, rank);
+          if (it.skip) continue;
+          const uint32_t half = kPair ? it.n_eff / 2 : it.n_eff;  // columns of B this CTA loads
+          const uint32_t b_boxes = (half + 63) / 64, n0 = it.n0 + rank * half;
+          const uint32_t b_rows = p.bn / (kPair ? 2 : 1);
+          const uint32_t planes = p.terms > 1 ? 2 : 1;
+          uint32_t term = it.k0 / max(it.kts, 1u), kk = it.k0 - term * it.kts;
+          for (uint32_t kt = 0; kt < it.kt; ++kt) {
+            if (!mbar_wait(&s.empty[stage], phase ^ 1u, args.wait_ns)) {
+              ok = false;
+              break;
+            }
+            uint8_t* a = stages + stage * R::kStageBytes;
+            uint8_t* b = a + R::kABytes;
+            const uint32_t k = kk * kTileK;
+            const bool second = k + 64 < it.k;  // a K-major operand's other 64 of K
+            const uint32_t za = it.batch * planes + (term == 2), zb = it.batch * planes + (term == 1);
+            const uint32_t bar = kPair ? cluster_addr(&s.full[stage], 0) : smem_u32(&s.full[stage]);
+            if (rank == 0) {
+              const uint32_t a_bytes = p.a_mn || second ? R::kABytes : R::kABytes / 2;
+              const uint32_t b_bytes = p.b_mn ? b_boxes * kBoxMnBytes : b_rows * (second ? 256u : 128u);
+              mbar_arrive_expect_tx(&s.full[stage], (a_bytes + b_bytes) * (kPair ? 2 : 1));
+            }
+            if (p.a_mn) {
+              tma_load_3d<kPair>(a, &p.a, it.m0, k, za, bar);
+              tma_load_3d<kPair>(a + kBoxMnBytes, &p.a, it.m0 + 64, k, za, bar);
+            } else {
+              tma_load_3d<kPair>(a, &p.a, k, it.m0, za, bar);
+              if (second) tma_load_3d<kPair>(a + R::kABytes / 2, &p.a, k + 64, it.m0, za, bar);
+            }
+            if (p.b_mn) {
+              for (uint32_t x = 0; x < b_boxes; ++x)
+                tma_load_3d<kPair>(b + x * kBoxMnBytes, &p.b, n0 + 64 * x, k, zb, bar);
+            } else {
+              tma_load_3d<kPair>(b, &p.b, k, n0, zb, bar);
+              if (second) tma_load_3d<kPair>(b + b_rows * 128, &p.b, k + 64, n0, zb, bar);
+            }
+            if (++stage == R::kStages) {
+              stage = 0;
+              phase ^= 1u;
+            }
+            if (++kk == it.kts) {
+              kk = 0;
+              ++term;
+            }
           }
         }
       }
-    }
-  } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0, prob = 0, acc = 0, acc_phase = 0;
-      for (uint32_t item = blockIdx.x; item < args.items && ok; item += gridDim.x) {
-        while (prob + 1 < args.problems && item >= args.shape[prob + 1].item0) ++prob;
-        const ProductShape& p = args.shape[prob];
-        const ProductItem it = product_item(p, item);
-        if (it.skip || it.kt == 0) continue;
-        if (!mbar_wait(&s.acc_empty[acc], acc_phase ^ 1u, args.wait_ns)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const uint32_t idesc = mma_idesc(p.bf16, p.a_mn, p.b_mn, kTileM, it.n_eff);
-        const uint32_t d = tmem + acc * kTileNMax;
-        // 16 of K: 32 bytes along a K-major row, 16 rows of an MN-major tile
-        const uint32_t a_step = (p.a_mn ? 2048u : 32u) >> 4, b_step = (p.b_mn ? 2048u : 32u) >> 4;
-        for (uint32_t kt = 0; kt < it.kt; ++kt) {
-          if (!mbar_wait(&s.full[stage], phase, args.wait_ns)) {
+    } else if (warp == 1) {
+      if (lane == 0 && rank == 0) {
+        for (uint32_t item = unit; item < items && ok; item += units) {
+          while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
+          const ProductShape& p = args.shape[prob];
+          const ProductItem it = product_item<kPair>(p, item, rank);
+          if (it.skip || it.kt == 0) continue;
+          if (!mbar_wait(&s.acc_empty[acc], acc_phase ^ 1u, args.wait_ns)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t a = smem_u32(stages + stage * kStageBytes);
-          const uint64_t da = smem_desc(a, p.a_mn ? kBoxMnBytes : 16, 1024);
-          const uint64_t db = smem_desc(a + kStageABytes, p.b_mn ? kBoxMnBytes : 16, 1024);
-#pragma unroll
-          for (uint32_t j = 0; j < kTileK / 16; ++j)
-            mma_f16(d, da + j * a_step, db + j * b_step, idesc, kt > 0 || j > 0);
-          mma_commit(&s.empty[stage]);
-          if (++stage == kProductStages) {
-            stage = 0;
-            phase ^= 1u;
+          const uint32_t idesc =
+              mma_idesc(p.bf16, p.a_mn, p.b_mn, kPair ? 2 * kTileM : kTileM, it.n_eff);
+          const uint32_t d = tmem + acc * kTileNMax;
+          // 16 of K: 32 bytes along a K-major row (the second 64 of K follow the
+          // first 64's rows), 16 rows of an MN-major tile
+          const uint32_t a_step = (p.a_mn ? 2048u : 32u) >> 4, b_step = (p.b_mn ? 2048u : 32u) >> 4;
+          const uint32_t b_rows = p.bn / (kPair ? 2 : 1);
+          const uint32_t a_half = (p.a_mn ? 4 * 2048u : R::kABytes / 2) >> 4;
+          const uint32_t b_half = (p.b_mn ? 4 * 2048u : b_rows * 128) >> 4;
+          uint32_t kk = it.k0 % max(it.kts, 1u);
+          for (uint32_t kt = 0; kt < it.kt; ++kt) {
+            if (!mbar_wait(&s.full[stage], phase, args.wait_ns)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t a = smem_u32(stages + stage * R::kStageBytes);
+            const uint64_t da = smem_desc(a, p.a_mn ? kBoxMnBytes : 16, 1024);
+            const uint64_t db = smem_desc(a + R::kABytes, p.b_mn ? kBoxMnBytes : 16, 1024);
+            const uint32_t steps = min(kTileK / 16, (it.k - kk * kTileK + 15) / 16);
+            for (uint32_t j = 0; j < steps; ++j)
+              mma_f16<kPair>(d, da + (j >> 2) * a_half + (j & 3u) * a_step,
+                             db + (j >> 2) * b_half + (j & 3u) * b_step, idesc, kt > 0 || j > 0);
+            if (++kk == it.kts) kk = 0;
+            mma_commit<kPair>(&s.empty[stage]);
+            if (++stage == R::kStages) {
+              stage = 0;
+              phase ^= 1u;
+            }
+          }
+          mma_commit<kPair>(&s.acc_full[acc]);
+          if (++acc == 2) {
+            acc = 0;
+            acc_phase ^= 1u;
           }
         }
-        mma_commit(&s.acc_full[acc]);
-        if (++acc == 2) {
-          acc = 0;
-          acc_phase ^= 1u;
+      }
+    } else {
+      const uint32_t quarter = warp & 3u;  // the lanes of tensor memory this warp may read
+      const uint32_t half = (warp - 2) >> 2;
+      const uint32_t row = quarter * 32 + lane;
+      for (uint32_t item = unit; item < items; item += units) {
+        while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
+        const ProductShape& p = args.shape[prob];
+        const ProductItem it = product_item<kPair>(p, item, rank);
+        if (it.skip) continue;
+        const uint32_t chunks = it.n_eff / 32, mid = (chunks + 1) / 2;
+        ProductAcc from;
+        from.c0 = half ? mid : 0;
+        from.c1 = half ? chunks : mid;
+        from.none = it.kt == 0;
+        from.parts = nullptr;
+        from.splits = p.splits;
+        from.tmem = tmem + acc * kTileNMax + ((quarter * 32) << 16);
+        from.release = kPair ? cluster_addr(&s.acc_empty[acc], 0) : smem_u32(&s.acc_empty[acc]);
+        if (!from.none && ok) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[acc], acc_phase, args.wait_ns));
+          tc_fence_after();
+          if (++acc == 2) {
+            acc = 0;
+            acc_phase ^= 1u;
+          }
         }
+        // a warp whose wait ran out stays for the barriers of the others, with
+        // zeros (the call's results are void: the timeout is latched)
+        from.none |= !ok;
+        if (!from.none && from.c0 == from.c1) from.arrive();
+        if (p.splits > 1 && p.join) {
+          const uint64_t tile_floats = static_cast<uint64_t>(args.part_chunks) * 32 * kTileM;
+          float* mine = args.parts + static_cast<uint64_t>(it.part) * tile_floats + row * 4;
+          float* dst = mine + it.split * tile_floats;
+          for (uint32_t c = from.c0; c < from.c1; ++c) {
+            float v[32];
+            from.load(c, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              __stcg(reinterpret_cast<float4*>(dst + static_cast<uint64_t>(c) * (32 * kTileM)) + j * kTileM,
+                     make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+          }
+          __threadfence();
+          asm volatile("bar.sync 2, 256;" ::: "memory");
+          if (warp == 2 && lane == 0) {
+            const uint32_t before = atomicAdd(&args.arrivals[it.part], 1u);
+            s.last = before == p.splits - 1 ? 1u : 0u;
+            if (s.last) args.arrivals[it.part] = 0;  // ready for the next launch
+            __threadfence();
+          }
+          asm volatile("bar.sync 2, 256;" ::: "memory");
+          const bool last = s.last != 0;
+          asm volatile("bar.sync 2, 256;" ::: "memory");  // s.last is read before it is written again
+          if (!last) continue;
+          __threadfence();
+          from.parts = mine;
+          from.part_stride = tile_floats;
+          from.none = false;
+        }
+        Epi::tile(p, args.epi[prob], it, row, half, epi_smem[warp - 2], from, ph);
       }
     }
-  } else {
-    const uint32_t quarter = warp & 3u;  // the lanes of tensor memory this warp may read
-    const uint32_t row = quarter * 32 + lane;
-    uint32_t prob = 0, acc = 0, acc_phase = 0;
-    for (uint32_t item = blockIdx.x; item < args.items; item += gridDim.x) {
-      while (prob + 1 < args.problems && item >= args.shape[prob + 1].item0) ++prob;
-      const ProductShape& p = args.shape[prob];
-      const ProductItem it = product_item(p, item);
-      if (it.skip) continue;
-      ProductAcc from;
-      from.chunks = (it.n_eff + 31) / 32;
-      from.none = it.kt == 0;
-      from.parts = nullptr;
-      from.splits = p.splits;
-      from.tmem = tmem + acc * kTileNMax + ((quarter * 32) << 16);
-      from.release = &s.acc_empty[acc];
-      if (!from.none && ok) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[acc], acc_phase, args.wait_ns));
-        tc_fence_after();
-        if (++acc == 2) {
-          acc = 0;
-          acc_phase ^= 1u;
-        }
-      }
-      // a warp whose wait ran out stays for the barriers of the others, with
-      // zeros (the call's results are void: the timeout is latched)
-      from.none |= !ok;
-      if (p.splits > 1) {
-        const uint64_t tile_floats = static_cast<uint64_t>(args.part_chunks) * 32 * kTileM;
-        float* mine = args.parts + static_cast<uint64_t>(it.slot) * tile_floats + row * 4;
-        float* dst = mine + it.split * tile_floats;
-        for (uint32_t c = 0; c < from.chunks; ++c) {
-          float v[32];
-          from.load(c, v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            __stcg(reinterpret_cast<float4*>(dst + static_cast<uint64_t>(c) * (32 * kTileM)) + j * kTileM,
-                   make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-        }
-        __threadfence();
-        asm volatile("bar.sync 2, 128;" ::: "memory");
-        if (warp == 2 && lane == 0) {
-          const uint32_t before = atomicAdd(&args.arrivals[it.slot], 1u);
-          s.last = before == p.splits - 1 ? 1u : 0u;
-          if (s.last) args.arrivals[it.slot] = 0;  // ready for the next launch
-          __threadfence();
-        }
-        asm volatile("bar.sync 2, 128;" ::: "memory");
-        const bool last = s.last != 0;
-        asm volatile("bar.sync 2, 128;" ::: "memory");  // s.last is read before it is written again
-        if (!last) continue;
-        __threadfence();
-        from.parts = mine;
-        from.part_stride = tile_floats;
-        from.none = false;
-      }
-      Epi::tile(p, args.epi[prob], it, row, epi_smem, from);
+    __syncwarp();
+    if (ph + 1 < args.phases) {
+      ok = __syncthreads_and(ok);
+      fence_proxy_async();
+      if (!phase_barrier(args.barrier, gridDim.x * (ph + 1), args.wait_ns)) ok = false;
+      if (!ok) break;
     }
   }
   if (!ok) atomicOr(args.error, kDevErrTimeout);
+  if (args.phases > 1 && threadIdx.x == 0 &&
+      atomicAdd(&args.barrier[1], 1u) == gridDim.x - 1) {  // all are past the last barrier
+    args.barrier[0] = 0;
+    args.barrier[1] = 0;
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (kPair) cluster_sync();  // the other CTA's shared memory may be in use until here
   tc_fence_after();
-  if (warp == 1) tmem_free(tmem, 512);
+  if (warp == 1) tmem_free<kPair>(tmem, 512);
+}
+
+// ------------------------------------------- epilogues' stores of 16-bit rows
+// A warp's 32 x 32 block of 16-bit values, each lane holding one row as 16
+// words, through 2 KB of shared memory, so that stores cover whole sectors:
+// 4 lanes per row with 16-byte rows (kVec16), 16 lanes per row with 4-byte
+// rows, 32 with 2-byte ones. `rows(i)` gives the destination of block row i
+// (nullptr: none).
+struct TurnSmem {
+  alignas(16) uint4 unit[32 * 4];
+};
+template <class RowFn>
+__device__ __forceinline__ void store_block(TurnSmem& t, const uint32_t (&w)[16], uint32_t cols,
+                                            uint32_t align, RowFn rows) {
+  const uint32_t lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (uint32_t u = 0; u < 4; ++u)
+    t.unit[lane * 4 + (u ^ ((lane >> 1) & 3u))] =
+        make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+  __syncwarp();
+  if (align >= 16 && cols >= 32) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      const uint32_t r = i * 8 + (lane >> 2), u = lane & 3u;
+      uint16_t* to = rows(r);
+      const uint4 x = t.unit[r * 4 + (u ^ ((r >> 1) & 3u))];
+      if (to) *reinterpret_cast<uint4*>(to + u * 8) = x;
+    }
+  } else if (align >= 4) {
+    const uint32_t col = (lane & 15u) * 2;
+#pragma unroll 8
+    for (uint32_t i = 0; i < 16; ++i) {
+      const uint32_t r = i * 2 + (lane >> 4);
+      uint16_t* to = rows(r);
+      const uint32_t x = reinterpret_cast<const uint32_t*>(
+          &t.unit[r * 4 + ((col >> 3) ^ ((r >> 1) & 3u))])[(col >> 1) & 3u];
+      if (to && col + 1 < cols) *reinterpret_cast<uint32_t*>(to + col) = x;
+      else if (to && col < cols) to[col] = static_cast<uint16_t>(x);
+    }
+  } else {
+#pragma unroll 8
+    for (uint32_t r = 0; r < 32; ++r) {
+      uint16_t* to = rows(r);
+      const uint16_t x = reinterpret_cast<const uint16_t*>(
+          &t.unit[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3u))])[lane & 7u];
+      if (to && lane < cols) to[lane] = x;
+    }
+  }
+}
+// A lane's row of a symmetric 32 x 32 block of which entries up to the diagonal
+// are given: the others are read from the rows that mirror them.
+__device__ __forceinline__ void mirror_block(TurnSmem& t, uint32_t (&w)[16]) {
+  const uint32_t lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (uint32_t u = 0; u < 4; ++u)
+    t.unit[lane * 4 + (u ^ ((lane >> 1) & 3u))] =
+        make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+  __syncwarp();
+#pragma unroll
+  for (uint32_t j = 0; j < 32; ++j) {
+    const uint32_t x = reinterpret_cast<const uint16_t*>(
+        &t.unit[j * 4 + ((lane >> 3) ^ ((j >> 1) & 3u))])[lane & 7u];
+    if (j > lane) w[j / 2] = j & 1u ? (w[j / 2] & 0xffffu) | (x << 16) : (w[j / 2] & 0xffff0000u) | x;
+  }
+}
+// The largest of 16, 4, 2 that every row of 16-bit elements starts on.
+inline uint32_t row_align(const void* p, uint64_t ld) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p) | (ld * 2);
+  return x % 16 == 0 ? 16 : x % 4 == 0 ? 4 : 2;
 }
 
 // ------------------------------------------------------------- host side
@@ -344,41 +522,92 @@ inline bool tma_rows(const void* p, uint64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0;
 }
 
-// Fills bn, tiles, splits of a product of m x n x k (batch of them) on `sms` SMs.
-void plan_product(ProductShape& p, uint32_t m, uint32_t n, uint32_t k, uint32_t batch,
-                  bool lower, uint32_t sms, uint32_t max_splits);
+// Fills bn, tiles, splits of a product of m x n x k (batch of them) on `sms`
+// SMs, by CTAs or pairs.
+struct ProductWant {
+  uint32_t m, n, k, batch;
+  bool lower, pair;
+  double sms;
+  uint32_t max_splits, terms;
+};
+void plan_product(ProductShape& p, const ProductWant& w);
+// Rows and columns of B a CTA loads at a time (the box of a K-major operand).
+inline uint32_t b_box(const ProductShape& p, bool pair) { return pair ? p.bn / 2 : p.bn; }
 
-template <class Epi, int kMaxProblems>
+// Numbers the items of each phase's problems and the scratch tiles of split
+// ones; returns the scratch tiles' bytes.
+template <class Args>
+size_t number_items(Args& args, bool pair) {
+  size_t most = 0;
+  uint32_t chunks = 0;
+  for (uint32_t ph = 0; ph < args.phases; ++ph) {
+    uint32_t items = 0, parts = 0;
+    for (uint32_t i = args.first[ph]; i < args.first[ph] + args.problems[ph]; ++i) {
+      ProductShape& p = args.shape[i];
+      p.item0 = items;
+      p.part0 = parts;
+      items += p.tiles * p.batch * p.splits;
+      if (p.splits > 1 && p.join) {
+        parts += p.tiles * p.batch * p.splits * (pair ? 2 : 1);
+        chunks = p.bn / 32 > chunks ? p.bn / 32 : chunks;
+      }
+    }
+    args.items[ph] = items;
+    most = parts > most ? parts : most;
+  }
+  args.part_chunks = chunks;
+  for (uint32_t ph = 0; ph < args.phases; ++ph)
+    if (args.first[ph] + args.problems[ph] > args.entries)
+      args.entries = args.first[ph] + args.problems[ph];
+  return most > kModelArrivals - 2 ? ~static_cast<size_t>(0) : most * chunks * 32 * kTileM * 4;
+}
+
+// The caller has numbered the items and set args.parts.
+template <class Epi, int kMaxProblems, bool kPair>
 cudaError_t launch_product(ProductArgs<Epi, kMaxProblems>& args, Workspace& ws,
                            const DeviceInfo& dev) {
-  uint32_t items = 0, slots = 0, chunks = 0;
-  for (uint32_t i = 0; i < args.problems; ++i) {
-    ProductShape& p = args.shape[i];
-    p.item0 = items;
-    p.slot0 = slots;
-    items += p.tiles * p.batch * p.splits;
-    if (p.splits > 1) {
-      // slots are indexed slot * splits within the problem's share of the scratch
-      slots += p.tiles * p.batch * p.splits;
-      chunks = (p.bn + 31) / 32 > chunks ? (p.bn + 31) / 32 : chunks;
-    }
-  }
+  uint32_t items = 0;
+  for (uint32_t ph = 0; ph < args.phases; ++ph)
+    items = args.items[ph] > items ? args.items[ph] : items;
   if (items == 0) return cudaSuccess;
-  if (slots > kModelArrivals) return cudaErrorInvalidValue;
-  args.items = items;
-  args.part_chunks = chunks;
   args.arrivals = ws.model_arrivals();
   args.error = ws.u32(kOffError);
+  args.barrier = ws.model_arrivals() + kModelArrivals - 2;
   args.wait_ns = wait_limit_ns();
-  auto fn = product_kernel<Epi, kMaxProblems>;
-  constexpr uint32_t smem = kProductStages * kStageBytes + 1024;
-  static_assert(smem <= 220 * 1024, "stages fit beside the static shared memory");
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
-  void* params[] = {&args};
-  e = launch_pdl(reinterpret_cast<const void*>(fn), dim3(items < sms ? items : sms),
-                 kProductThreads, smem, ws.stream, params, false);
+  auto fn = product_kernel<Epi, kMaxProblems, kPair>;
+  constexpr uint32_t smem = Ring<kPair>::kBytes + 1024;
+  static_assert(smem + sizeof(typename Epi::Smem) * kEpilogueWarps + 512 <= 227 * 1024,
+                "stages and epilogue buffers fit an SM");
+  static_assert(sizeof(args) <= 32764, "kernel parameters");
+  static bool ready[64] = {};  // per device: opted into the ring's shared memory
+  if (ws.device >= 64 || !ready[ws.device]) {
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (ws.device < 64) ready[ws.device] = true;
+  }
+  const uint32_t sms = static_cast<uint32_t>(dev.sm_count), per = kPair ? 2 : 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((items < sms / per ? items : sms / per) * per);
+  cfg.blockDim = dim3(kProductThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = ws.stream;
+  cudaLaunchAttribute attr[3];
+  uint32_t n = 0;
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  if (args.phases > 1) {
+    attr[n].id = cudaLaunchAttributeCooperative;
+    attr[n++].val.cooperative = 1;
+  }
+  if (kPair) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = 2;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, args);
   if (e == cudaSuccess) count_launch();
   return e;
 }

@@ -138,24 +138,25 @@ struct LossEpilogue {
     const uint16_t* bias;
     const int32_t* targets;
     const uint32_t* count;
-    float2* pairs;     // [row][tile]
+    float2* pairs;     // [row][half tile]
     float* at_target;  // [row]
   };
   struct Smem {
-    alignas(16) float bias[4][32];
+    alignas(16) float bias[32];
   };
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row, Smem& s,
-                                              const ProductAcc& acc) {
+                                              const ProductItem& it, uint32_t row,
+                                              uint32_t half, Smem& s, const ProductAcc& acc,
+                                              uint32_t) {
     const uint32_t r = it.m0 + row;
     const bool real = r < *e.count;
     const int32_t target = real ? e.targets[r] : -1;
     float m = -INFINITY, sum = 0.0f;
-    for (uint32_t c = 0; c < acc.chunks; ++c) {
+    for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
-      add_bias(v, e.bias, col0, p.n, s.bias[(threadIdx.x >> 5) & 3u]);
+      add_bias(v, e.bias, col0, p.n, s.bias);
       if (col0 + 32 > p.n) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = col0 + j < p.n ? v[j] : -INFINITY;
@@ -182,7 +183,8 @@ struct LossEpilogue {
       sum = __fmaf_rn(sum, scale, rest);
       m = higher;
     }
-    if (real) e.pairs[static_cast<uint64_t>(r) * p.tiles_n + it.tn] = make_float2(m, sum);
+    if (real)
+      e.pairs[(static_cast<uint64_t>(r) * p.tiles_n + it.tn) * 2 + half] = make_float2(m, sum);
   }
 };
 
@@ -239,11 +241,13 @@ struct GradEpilogue {
     uint32_t v0;               // the piece's first word
   };
   struct Smem {
-    alignas(16) float bias[4][32];
+    alignas(16) float bias[32];
+    TurnSmem turn;
   };
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row, Smem& s,
-                                              const ProductAcc& acc) {
+                                              const ProductItem& it, uint32_t row,
+                                              uint32_t half, Smem& s, const ProductAcc& acc,
+                                              uint32_t) {
     const uint32_t r = it.m0 + row;
     const bool real = r < *e.count;
     float scale = 0.0f, shift = 0.0f;
@@ -257,12 +261,11 @@ struct GradEpilogue {
       target = static_cast<uint32_t>(e.targets[r]) - e.v0;
       dead = lse == -INFINITY;  // no word has a probability
     }
-    uint16_t* out = e.g + static_cast<uint64_t>(r) * e.ld_g + it.n0;
-    for (uint32_t c = 0; c < acc.chunks; ++c) {
+    for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
-      add_bias(v, e.bias, col0, p.n, s.bias[(threadIdx.x >> 5) & 3u]);
+      add_bias(v, e.bias, col0, p.n, s.bias);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         v[j] = __fmul_rn(exp2_fast(__fmaf_rn(v[j], kLog2e, shift)), scale);
@@ -277,17 +280,26 @@ struct GradEpilogue {
         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
       }
       // columns past the piece lie past the tensor map's extent: never read
+      uint32_t w[16];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<uint4*>(out + c * 32 + 8 * j) =
-            make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
-                       pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+      for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+      uint16_t* out = e.g + static_cast<uint64_t>(r & ~31u) * e.ld_g + col0;
+      store_block(s.turn, w, 32, 16, [&](uint32_t i) { return out + i * e.ld_g; });
     }
   }
 };
 
-// Epilogue of dh and dw: rows of bf16 at any alignment, optionally through an
-// fp32 sum over pieces, optionally one more column that goes elsewhere (db).
+// Blocks of fp32 sums, 128 rows x 32 columns, four columns of all rows
+// together: a warp's accesses are contiguous.
+__device__ __forceinline__ float4* sum_block(float* sums, uint32_t row_tile, uint32_t chunks,
+                                             uint32_t chunk, uint32_t row) {
+  return reinterpret_cast<float4*>(sums) +
+         (static_cast<uint64_t>(row_tile) * chunks + chunk) * (8 * kTileM) + row;
+}
+
+// Epilogue of dh and dw: rows of bf16 at any alignment, optionally one more
+// column that goes elsewhere (db); or fp32 sums, one set per K part, added to
+// over the pieces of the vocabulary.
 struct StoreEpilogue {
   struct Params {
     uint16_t* out;
@@ -295,45 +307,40 @@ struct StoreEpilogue {
     const uint32_t* row_map;  // or nullptr
     const uint32_t* count;    // rows that exist (with row_map)
     uint32_t rows, cols;
+    uint32_t align;           // of out's rows, in bytes
     uint16_t* extra;          // column `cols`, by row (or nullptr)
-    float* sum;               // [row][ld_sum] (or nullptr)
-    uint32_t ld_sum;
-    uint32_t first, last;     // of the pieces
-    uint32_t vec;             // rows start at 16-byte boundaries
+    float* sums;              // != nullptr: sums instead of out
+    uint64_t part_floats;     // from one part's sums to the next
+    uint32_t sum_chunks;      // 32-column chunks of a row
+    uint32_t first;           // the sums start here
   };
   struct Smem {
-    uint32_t turn[4][32 * 17];
+    TurnSmem turn;
   };
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row, Smem& s,
-                                              const ProductAcc& acc) {
-    const uint32_t lane = threadIdx.x & 31;
+                                              const ProductItem& it, uint32_t row, uint32_t,
+                                              Smem& s, const ProductAcc& acc, uint32_t) {
     const uint32_t r = it.m0 + row;
     const bool real = r < (e.row_map ? *e.count : e.rows);
     const uint32_t dst = real ? (e.row_map ? e.row_map[r] : r) : 0xffffffffu;
-    uint32_t* turn = s.turn[(threadIdx.x >> 5) & 3u];
-    for (uint32_t c = 0; c < acc.chunks; ++c) {
+    for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
-      if (e.sum) {
-        float4* sum = reinterpret_cast<float4*>(e.sum + static_cast<uint64_t>(r) * e.ld_sum + col0);
-        if (!e.first) {
+      if (e.sums) {
+        float4* sum = sum_block(e.sums + it.split * e.part_floats, it.m0 / kTileM, e.sum_chunks,
+                                col0 / 32, row);
+        if (real) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float4 x = __ldcg(sum + j);
-            v[4 * j] = __fadd_rn(x.x, v[4 * j]);
-            v[4 * j + 1] = __fadd_rn(x.y, v[4 * j + 1]);
-            v[4 * j + 2] = __fadd_rn(x.z, v[4 * j + 2]);
-            v[4 * j + 3] = __fadd_rn(x.w, v[4 * j + 3]);
+            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (!e.first) x = __ldcg(sum + j * kTileM);
+            __stcg(sum + j * kTileM,
+                   make_float4(__fadd_rn(x.x, v[4 * j]), __fadd_rn(x.y, v[4 * j + 1]),
+                               __fadd_rn(x.z, v[4 * j + 2]), __fadd_rn(x.w, v[4 * j + 3])));
           }
         }
-        if (!e.last) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            __stcg(sum + j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-          continue;
-        }
+        continue;
       }
       if (e.extra && real && e.cols - col0 < 32u) {
         float x = 0.0f;
@@ -341,33 +348,58 @@ struct StoreEpilogue {
         for (int j = 0; j < 32; ++j) x = e.cols - col0 == static_cast<uint32_t>(j) ? v[j] : x;
         e.extra[dst] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
       }
+      if (col0 >= e.cols) continue;
       uint32_t w[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-      if (e.vec && col0 + 32 <= e.cols) {
-        if (real) {
-          uint4* to = reinterpret_cast<uint4*>(e.out + static_cast<uint64_t>(dst) * e.ld + col0);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-        }
-        continue;
-      }
-      // through shared memory: a row's 32 columns are one store of the warp
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 16; ++j) turn[lane * 17 + j] = w[j];
-      __syncwarp();
-      const bool in = col0 + lane < e.cols;
-      for (uint32_t i = 0; i < 32; ++i) {
+      store_block(s.turn, w, e.cols - col0, e.align, [&](uint32_t i) -> uint16_t* {
         const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
-        if (to != 0xffffffffu && in)
-          e.out[static_cast<uint64_t>(to) * e.ld + col0 + lane] =
-              reinterpret_cast<const uint16_t*>(turn + i * 17)[lane];
-      }
+        return to == 0xffffffffu ? nullptr : e.out + static_cast<uint64_t>(to) * e.ld + col0;
+      });
     }
   }
 };
+
+// dh from its sums: parts added in order, rounded, rows scattered. A CTA takes
+// a block of 128 rows x 32 columns.
+__global__ void __launch_bounds__(128)
+    vocab_dh_kernel(const float* __restrict__ sums, uint64_t part_floats, uint32_t parts,
+                    uint32_t chunks, const uint32_t* __restrict__ row_map,
+                    const uint32_t* __restrict__ count, uint16_t* __restrict__ dh, uint64_t ld,
+                    uint32_t cols, uint32_t align) {
+  __shared__ TurnSmem turn[4];
+  griddep_wait();
+  const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
+  const uint32_t r = tile * kTileM + threadIdx.x;
+  if (tile * kTileM >= *count) return;
+  const bool real = r < *count;
+  const uint32_t dst = real ? row_map[r] : 0xffffffffu;
+  float v[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+  if (real) {
+#pragma unroll 2
+    for (uint32_t s = 0; s < parts; ++s) {
+      const float4* x = sum_block(const_cast<float*>(sums) + s * part_floats, tile, chunks, chunk,
+                                  threadIdx.x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float4 y = __ldcg(x + j * kTileM);
+        v[4 * j] = __fadd_rn(v[4 * j], y.x);
+        v[4 * j + 1] = __fadd_rn(v[4 * j + 1], y.y);
+        v[4 * j + 2] = __fadd_rn(v[4 * j + 2], y.z);
+        v[4 * j + 3] = __fadd_rn(v[4 * j + 3], y.w);
+      }
+    }
+  }
+  uint32_t w[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  store_block(turn[threadIdx.x >> 5], w, cols - chunk * 32, align, [&](uint32_t i) -> uint16_t* {
+    const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
+    return to == 0xffffffffu ? nullptr : dh + static_cast<uint64_t>(to) * ld + chunk * 32;
+  });
+}
 
 constexpr uint32_t round_up(uint32_t x, uint32_t to) { return (x + to - 1) / to * to; }
 constexpr size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -384,18 +416,30 @@ uint32_t piece_words(uint32_t rows, uint32_t v) {
   return round_up(static_cast<uint32_t>((v + pieces - 1) / pieces), kTileNMax);
 }
 
-struct VocabLayout {
+// Pairs of CTAs from more than one tile of 128 rows on: a pair's tile has 256
+// rows, and with half of them empty it does half the work per SM.
+bool use_pairs(const VocabCall& c) { return c.n > kTileM; }
+
+struct VocabPlan {
   uint32_t rows;    // rows of the gathered h: n rounded up to whole tiles
-  uint32_t ld_h, ld_w, ld_g, piece, ld_sum;
-  size_t row_map, targets, count, h, w, pairs, at_target, g, sum, parts, total;
-  uint32_t pair_tiles;
+  uint32_t ld_h, ld_w, ld_g, piece;
+  ProductShape logits, dh, dw;
+  uint32_t sum_chunks, sum_parts;  // of dh's sums (0: dh is stored directly)
+  uint64_t part_floats;
+  // scratch offsets
+  size_t row_map, targets, count, h, w, pairs, at_target, g, sums, total;
 };
 
-VocabLayout vocab_layout(const VocabCall& c, bool gradient, size_t part_bytes,
-                         uint32_t pair_tiles) {
-  VocabLayout l = {};
-  l.rows = round_up(c.n ? c.n : 1, kTileM);
-  l.ld_h = round_up(c.d + (c.dbias ? 1 : 0), 8);
+// The products' plans and the scratch. dh has few tiles and the whole piece as
+// its K axis: it is cut along K where tiles are few, the parts (and the
+// pieces) added up in fp32 and joined by a kernel of their own.
+VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
+  VocabPlan l = {};
+  const double sms = dev.sm_count;
+  const bool pair = use_pairs(c);
+  const uint32_t n = c.n ? c.n : 1, dn = c.d + (c.dbias ? 1 : 0);
+  l.rows = round_up(n, 2 * kTileM);
+  l.ld_h = round_up(dn, 8);
   l.ld_w = round_up(c.d, 8);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -408,44 +452,26 @@ VocabLayout vocab_layout(const VocabCall& c, bool gradient, size_t part_bytes,
   l.count = take(4);
   l.h = take(2ull * l.rows * l.ld_h);
   if (!tma_rows(c.w, c.ldw)) l.w = take(2ull * c.v * l.ld_w);
+  l.piece = gradient ? piece_words(l.rows, c.v) : c.v;
+  plan_product(l.logits, {n, l.piece, c.d, 1, false, pair, sms, 1, 1});
   if (gradient) {
-    l.piece = piece_words(l.rows, c.v);
     l.ld_g = round_up(l.piece, kTileNMax);  // epilogues write whole tiles
     l.g = take(2ull * l.rows * l.ld_g);
-    if (l.piece < c.v) {
-      l.ld_sum = round_up(c.d, kTileNMax);
-      l.sum = take(4ull * l.rows * l.ld_sum);
+    plan_product(l.dh, {n, c.d, l.piece, 1, false, pair, sms, 32, 1});
+    plan_product(l.dw, {l.piece, dn, n, 1, false, pair, sms, 1, 1});
+    l.dh.join = 0;
+    if (l.dh.splits > 1 || l.piece < c.v) {
+      l.sum_parts = l.dh.splits;
+      l.sum_chunks = round_up(c.d, 32) / 32;
+      l.part_floats = static_cast<uint64_t>(l.rows) * l.sum_chunks * 32;
+      l.sums = take(4ull * l.part_floats * l.sum_parts);
     }
   } else {
-    l.pair_tiles = pair_tiles;
-    l.pairs = take(8ull * l.rows * pair_tiles);
+    l.pairs = take(16ull * l.rows * l.logits.tiles_n);
     l.at_target = take(4ull * l.rows);
   }
-  l.parts = take(part_bytes);
   l.total = at;
   return l;
-}
-
-// The three products' plans. dh has few tiles and the whole piece as its K
-// axis, dw the rows: both are cut along K where tiles are few.
-struct VocabPlans {
-  ProductShape logits, dh, dw;
-  size_t part_bytes;
-};
-VocabPlans vocab_plans(const VocabCall& c, bool gradient, uint32_t words, const DeviceInfo& dev) {
-  VocabPlans p = {};
-  const uint32_t sms = static_cast<uint32_t>(dev.sm_count), n = c.n ? c.n : 1;
-  plan_product(p.logits, n, words, c.d, 1, false, sms, 1);
-  if (gradient) {
-    plan_product(p.dh, n, c.d, words, 1, false, sms, 32);
-    plan_product(p.dw, words, c.d + (c.dbias ? 1 : 0), n, 1, false, sms, 8);
-    // both run in one launch: scratch tiles of one size
-    const uint32_t chunks = round_up(p.dh.bn > p.dw.bn ? p.dh.bn : p.dw.bn, 32) / 32;
-    const size_t tiles = (p.dh.splits > 1 ? p.dh.tiles * p.dh.splits : 0) +
-                         (p.dw.splits > 1 ? p.dw.tiles * p.dw.splits : 0);
-    p.part_bytes = 4ull * kTileM * 32 * chunks * tiles;
-  }
-  return p;
 }
 
 cudaError_t launch_kernel(const void* fn, uint32_t grid, uint32_t block, cudaStream_t stream,
@@ -461,7 +487,7 @@ struct Gathered {
 };
 
 // The rows that take part, h gathered, w copied where TMA cannot read it.
-cudaError_t gather(const VocabCall& c, const VocabLayout& l, char* base, bool gradient,
+cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool gradient,
                    Workspace& ws, const DeviceInfo& dev, Gathered* out) {
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
   uint32_t* row_map = reinterpret_cast<uint32_t*>(base + l.row_map);
@@ -502,141 +528,152 @@ cudaError_t gather(const VocabCall& c, const VocabLayout& l, char* base, bool gr
 }
 
 // Tile rows walked together: their h stays in L2 while the vocabulary passes.
-uint32_t rows_in_l2(uint32_t tiles_m, uint32_t d) {
-  const uint64_t tile = 2ull * kTileM * d, most = (48ull << 20) / tile;
-  const uint32_t g = most < 1 ? 1 : most > tiles_m ? tiles_m : static_cast<uint32_t>(most);
-  return g;
+uint32_t rows_in_l2(const ProductShape& p, bool pair) {
+  const uint64_t tile = 2ull * kTileM * (pair ? 2 : 1) * p.k, most = (48ull << 20) / tile;
+  return most < 1 ? 1 : most > p.tiles_m ? p.tiles_m : static_cast<uint32_t>(most);
+}
+
+template <bool kPair>
+cudaError_t loss_product(const VocabCall& c, const VocabPlan& l, const Gathered& from, char* base,
+                         Workspace& ws, const DeviceInfo& dev) {
+  ProductArgs<LossEpilogue, 1> args = {};
+  ProductShape& p = args.shape[0];
+  p = l.logits;
+  p.bf16 = 1;
+  p.count = reinterpret_cast<const uint32_t*>(base + l.count);
+  p.group_m = rows_in_l2(p, kPair);
+  if (!make_map(&p.a, base + l.h, true, c.d, l.rows, l.ld_h, 1,
+                static_cast<uint64_t>(l.rows) * l.ld_h, kTileM) ||
+      !make_map(&p.b, from.w, true, c.d, c.v, from.ld_w, 1, from.ld_w * c.v, b_box(p, kPair)))
+    return cudaErrorInvalidValue;
+  args.epi[0] = {c.bias, reinterpret_cast<const int32_t*>(base + l.targets), p.count,
+                 reinterpret_cast<float2*>(base + l.pairs),
+                 reinterpret_cast<float*>(base + l.at_target)};
+  args.phases = args.problems[0] = 1;
+  number_items(args, kPair);
+  return launch_product<LossEpilogue, 1, kPair>(args, ws, dev);
+}
+
+// G of the words [v0, v0 + words), then dw's rows and dh's share of them.
+template <bool kPair>
+cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& from, char* base,
+                       uint32_t v0, Workspace& ws, const DeviceInfo& dev) {
+  const uint32_t words = c.v - v0 < l.piece ? c.v - v0 : l.piece;
+  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
+  const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
+  uint16_t* g = reinterpret_cast<uint16_t*>(base + l.g);
+  const char* h = base + l.h;
+  const uint16_t* w = from.w + static_cast<uint64_t>(v0) * from.ld_w;
+  const uint64_t w_all = from.ld_w * words;
+  const uint64_t h_all = static_cast<uint64_t>(l.rows) * l.ld_h;
+  const uint64_t g_all = static_cast<uint64_t>(l.rows) * l.ld_g;
+  const uint32_t tile_m = kPair ? 2 * kTileM : kTileM;
+  {
+    ProductArgs<GradEpilogue, 1> args = {};
+    ProductShape& p = args.shape[0];
+    p = l.logits;
+    p.n = words;
+    p.tiles_n = (words + p.bn - 1) / p.bn;
+    p.tiles = p.tiles_m * p.tiles_n;
+    p.bf16 = 1;
+    p.count = count;
+    p.group_m = rows_in_l2(p, kPair);
+    if (!make_map(&p.a, h, true, c.d, l.rows, l.ld_h, 1, h_all, kTileM) ||
+        !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, b_box(p, kPair)))
+      return cudaErrorInvalidValue;
+    args.epi[0] = {c.bias ? c.bias + v0 : nullptr,
+                   reinterpret_cast<const int32_t*>(base + l.targets),
+                   row_map, count, c.lse, c.row_scale, g, l.ld_g, v0};
+    args.phases = args.problems[0] = 1;
+    number_items(args, kPair);
+    const cudaError_t e = launch_product<GradEpilogue, 1, kPair>(args, ws, dev);
+    if (e != cudaSuccess) return e;
+  }
+  ProductArgs<StoreEpilogue, 2> args = {};
+  {
+    ProductShape& p = args.shape[0];  // dh = G w: the deeper product first
+    p = l.dh;
+    p.k = words;
+    p.group_m = 1;
+    p.b_mn = p.bf16 = 1;
+    p.count = count;
+    if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileM) ||
+        !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, kTileK))
+      return cudaErrorInvalidValue;
+    args.epi[0] = {c.dh, c.lddh, row_map, count, c.n, c.d, row_align(c.dh, c.lddh), nullptr,
+                   l.sum_parts ? reinterpret_cast<float*>(base + l.sums) : nullptr,
+                   l.part_floats, l.sum_chunks, v0 == 0 ? 1u : 0u};
+  }
+  {
+    ProductShape& p = args.shape[1];  // dw = G^T h
+    p = l.dw;
+    p.m = words;
+    p.tiles_m = (words + tile_m - 1) / tile_m;
+    p.tiles = p.tiles_m * p.tiles_n;
+    p.group_m = 1;
+    p.a_mn = p.b_mn = p.bf16 = 1;
+    p.count = count;
+    p.count_is_k = 1;
+    if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileK) ||
+        !make_map(&p.b, h, true, c.d + (c.dbias ? 1 : 0), l.rows, l.ld_h, 1, h_all, kTileK))
+      return cudaErrorInvalidValue;
+    uint16_t* out = c.dw + static_cast<uint64_t>(v0) * c.lddw;
+    args.epi[1] = {out, c.lddw, nullptr, nullptr, words, c.d, row_align(out, c.lddw),
+                   c.dbias ? c.dbias + v0 : nullptr, nullptr, 0, 0, 1};
+  }
+  args.phases = 1;
+  args.problems[0] = 2;
+  number_items(args, kPair);
+  return launch_product<StoreEpilogue, 2, kPair>(args, ws, dev);
 }
 
 }  // namespace
 
 size_t vocab_scratch(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
-  const uint32_t rows = round_up(c.n ? c.n : 1, kTileM);
-  const VocabPlans p = vocab_plans(c, gradient, gradient ? piece_words(rows, c.v) : c.v, dev);
-  return vocab_layout(c, gradient, p.part_bytes, p.logits.tiles_n).total;
+  return vocab_plan(c, gradient, dev).total;
 }
 
 cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev) {
   char* base = ws.model_scratch();
-  VocabPlans plan = vocab_plans(c, false, c.v, dev);
-  const VocabLayout l = vocab_layout(c, false, 0, plan.logits.tiles_n);
+  const VocabPlan l = vocab_plan(c, false, dev);
   Gathered from;
   cudaError_t e = gather(c, l, base, false, ws, dev, &from);
   if (e != cudaSuccess) return e;
-  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
-  const uint16_t* h = reinterpret_cast<const uint16_t*>(base + l.h);
-  ProductArgs<LossEpilogue, 1> args = {};
-  ProductShape& p = args.shape[0];
-  p = plan.logits;
-  p.bf16 = 1;
-  p.count = count;
-  p.group_m = rows_in_l2(p.tiles_m, c.d);
-  if (!make_map(&p.a, h, true, c.d, l.rows, l.ld_h, 1, static_cast<uint64_t>(l.rows) * l.ld_h,
-                kTileM) ||
-      !make_map(&p.b, from.w, true, c.d, c.v, from.ld_w, 1, from.ld_w * c.v, p.bn))
-    return cudaErrorInvalidValue;
-  args.epi[0] = {c.bias, reinterpret_cast<const int32_t*>(base + l.targets), count,
-                 reinterpret_cast<float2*>(base + l.pairs),
-                 reinterpret_cast<float*>(base + l.at_target)};
-  args.problems = 1;
-  e = launch_product(args, ws, dev);
+  e = use_pairs(c) ? loss_product<true>(c, l, from, base, ws, dev)
+                   : loss_product<false>(c, l, from, base, ws, dev);
   if (e != cudaSuccess) return e;
-  const float2* pairs = args.epi[0].pairs;
-  const float* at_target = args.epi[0].at_target;
-  uint32_t tiles = p.tiles_n;
+  const float2* pairs = reinterpret_cast<const float2*>(base + l.pairs);
+  const float* at_target = reinterpret_cast<const float*>(base + l.at_target);
+  uint32_t tiles = 2 * l.logits.tiles_n;
+  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
   const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
   float *loss = c.loss, *lse = c.lse;
   void* params[] = {&pairs, &tiles, &at_target, &row_map, &count, &loss, &lse};
-  return launch_kernel(reinterpret_cast<const void*>(&vocab_join_kernel), (l.rows + 7) / 8, 256,
+  return launch_kernel(reinterpret_cast<const void*>(&vocab_join_kernel), (c.n + 7) / 8, 256,
                        ws.stream, params);
 }
 
 cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const DeviceInfo& dev) {
   char* base = ws.model_scratch();
-  const uint32_t rows = round_up(c.n ? c.n : 1, kTileM);
-  const uint32_t piece = piece_words(rows, c.v);
-  const VocabPlans plan = vocab_plans(c, true, piece, dev);
-  const VocabLayout l = vocab_layout(c, true, plan.part_bytes, 0);
+  const VocabPlan l = vocab_plan(c, true, dev);
   Gathered from;
   cudaError_t e = gather(c, l, base, true, ws, dev, &from);
   if (e != cudaSuccess) return e;
-  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
-  const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
-  const uint16_t* h = reinterpret_cast<const uint16_t*>(base + l.h);
-  uint16_t* g = reinterpret_cast<uint16_t*>(base + l.g);
-  const uint32_t dn = c.d + (c.dbias ? 1 : 0);
-  const uint64_t h_all = static_cast<uint64_t>(l.rows) * l.ld_h;
-  const uint64_t g_all = static_cast<uint64_t>(l.rows) * l.ld_g;
-  for (uint32_t v0 = 0; v0 < c.v; v0 += piece) {
-    const uint32_t words = c.v - v0 < piece ? c.v - v0 : piece;
-    const uint16_t* w = from.w + static_cast<uint64_t>(v0) * from.ld_w;
-    const uint64_t w_all = from.ld_w * words;
-    {
-      ProductArgs<GradEpilogue, 1> args = {};
-      ProductShape& p = args.shape[0];
-      p = plan.logits;
-      p.n = words;
-      p.tiles_n = (words + p.bn - 1) / p.bn;
-      p.tiles = p.tiles_m * p.tiles_n;
-      p.bf16 = 1;
-      p.count = count;
-      p.group_m = rows_in_l2(p.tiles_m, c.d);
-      if (!make_map(&p.a, h, true, c.d, l.rows, l.ld_h, 1, h_all, kTileM) ||
-          !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, p.bn))
-        return cudaErrorInvalidValue;
-      args.epi[0] = {c.bias ? c.bias + v0 : nullptr,
-                     reinterpret_cast<const int32_t*>(base + l.targets),
-                     row_map,
-                     count,
-                     c.lse,
-                     c.row_scale,
-                     g,
-                     l.ld_g,
-                     v0};
-      args.problems = 1;
-      e = launch_product(args, ws, dev);
-      if (e != cudaSuccess) return e;
-    }
-    ProductArgs<StoreEpilogue, 2> args = {};
-    {
-      ProductShape& p = args.shape[0];  // dw = G^T h
-      p = plan.dw;
-      p.m = words;
-      p.tiles_m = (words + kTileM - 1) / kTileM;
-      p.tiles = p.tiles_m * p.tiles_n;
-      p.group_m = 1;
-      p.a_mn = p.b_mn = p.bf16 = 1;
-      p.count = count;
-      p.count_is_k = 1;
-      if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, 64) ||
-          !make_map(&p.b, h, true, dn, l.rows, l.ld_h, 1, h_all, 64))
-        return cudaErrorInvalidValue;
-      uint16_t* out = c.dw + static_cast<uint64_t>(v0) * c.lddw;
-      args.epi[0] = {out, c.lddw, nullptr, nullptr, words, c.d,
-                     c.dbias ? c.dbias + v0 : nullptr, nullptr, 0, 1, 1,
-                     tma_rows(out, c.lddw) ? 1u : 0u};
-    }
-    {
-      ProductShape& p = args.shape[1];  // dh = G w
-      p = plan.dh;
-      p.k = words;
-      p.group_m = 1;
-      p.b_mn = p.bf16 = 1;
-      p.count = count;
-      if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileM) ||
-          !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, 64))
-        return cudaErrorInvalidValue;
-      args.epi[1] = {c.dh, c.lddh, row_map, count, c.n, c.d, nullptr,
-                     piece < c.v ? reinterpret_cast<float*>(base + l.sum) : nullptr, l.ld_sum,
-                     v0 == 0 ? 1u : 0u, v0 + words == c.v ? 1u : 0u,
-                     tma_rows(c.dh, c.lddh) ? 1u : 0u};
-    }
-    args.problems = 2;
-    args.parts = reinterpret_cast<float*>(base + l.parts);
-    e = launch_product(args, ws, dev);
+  for (uint32_t v0 = 0; v0 < c.v; v0 += l.piece) {
+    e = use_pairs(c) ? grad_piece<true>(c, l, from, base, v0, ws, dev)
+                     : grad_piece<false>(c, l, from, base, v0, ws, dev);
     if (e != cudaSuccess) return e;
   }
-  return cudaSuccess;
+  if (!l.sum_parts || c.n == 0) return cudaSuccess;
+  const float* sums = reinterpret_cast<const float*>(base + l.sums);
+  uint64_t part_floats = l.part_floats, ld = c.lddh;
+  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, align = row_align(c.dh, c.lddh);
+  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
+  const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
+  uint16_t* dh = c.dh;
+  void* params[] = {&sums, &part_floats, &parts, &chunks, &row_map, &count, &dh, &ld, &cols, &align};
+  return launch_kernel(reinterpret_cast<const void*>(&vocab_dh_kernel),
+                       (c.n + kTileM - 1) / kTileM * chunks, 128, ws.stream, params);
 }
 
 }  // namespace efs
