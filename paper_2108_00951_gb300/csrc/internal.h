@@ -266,6 +266,11 @@ struct VocabCall {
   uint64_t lddh, lddw;
 };
 size_t vocab_scratch(const VocabCall& c, bool gradient, const DeviceInfo& dev);
+// At most 16 rows (vocab_few.cu).
+bool vocab_few(const VocabCall& c);
+size_t vocab_few_scratch(const VocabCall& c, bool gradient, const DeviceInfo& dev);
+cudaError_t launch_vocab_few_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
+cudaError_t launch_vocab_few_grad(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
 cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
 cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const DeviceInfo& dev);
 

@@ -630,10 +630,12 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
 }  // namespace
 
 size_t vocab_scratch(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
+  if (vocab_few(c)) return vocab_few_scratch(c, gradient, dev);
   return vocab_plan(c, gradient, dev).total;
 }
 
 cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev) {
+  if (vocab_few(c)) return launch_vocab_few_loss(c, ws, dev);
   char* base = ws.model_scratch();
   const VocabPlan l = vocab_plan(c, false, dev);
   Gathered from;
@@ -654,6 +656,7 @@ cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInf
 }
 
 cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const DeviceInfo& dev) {
+  if (vocab_few(c)) return launch_vocab_few_grad(c, ws, dev);
   char* base = ws.model_scratch();
   const VocabPlan l = vocab_plan(c, true, dev);
   Gathered from;
