@@ -281,6 +281,10 @@ struct OrthoMat {
   uint64_t ld_u, ld_m, ld_out;
   uint32_t rows, cols;
 };
+// Matrices that a cluster holds on chip (ortho_small.cu).
+bool ortho_small(const OrthoMat* mats, uint32_t n);
+cudaError_t launch_ortho_small(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
+                               Workspace& ws);
 size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev);
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
                                  Workspace& ws, const DeviceInfo& dev);

@@ -652,13 +652,14 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
 }  // namespace
 
 size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
+  if (ortho_small(mats, n)) return 0;
   return make_plan(mats, n, dev).total;
 }
 
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
                                  Workspace& ws, const DeviceInfo& dev) {
+  if (ortho_small(mats, n)) return launch_ortho_small(mats, n, bf16, mu, ws);
   const Plan plan = make_plan(mats, n, dev);
-  if (plan.groups.empty()) return cudaSuccess;
   char* base = ws.model_scratch();
   cudaError_t e = prepare(mats, plan, bf16, mu, base, ws);
   for (size_t g0 = 0; g0 < plan.groups.size() && e == cudaSuccess; g0 += kOrthoGroups) {

@@ -42,6 +42,7 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
   return a;
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
                    : "memory");
 }
