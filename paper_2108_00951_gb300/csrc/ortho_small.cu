@@ -103,10 +103,47 @@ __device__ __forceinline__ void store_pair_8(uint8_t* hi, uint8_t* lo, const flo
   *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-template <bool kBf16>
-__device__ __forceinline__ float load_u(const SmallMat& t, uint64_t at) {
-  return kBf16 ? bf16_bits_to_f32(__ldg(static_cast<const uint16_t*>(t.u) + at))
-               : __ldg(static_cast<const float*>(t.u) + at);
+// Four entries of the matrix, X's row r, columns c .. c + 3 of which `n` exist:
+// of u (kU) or of the momentum.
+template <bool kBf16, bool kU>
+__device__ __forceinline__ void load_4(const SmallMat& t, uint32_t r, uint32_t c, uint32_t n,
+                                       bool vec, float (&x)[4]) {
+  const uint64_t ld = kU ? t.ld_u : t.ld_m;
+  const uint64_t at = t.tall ? static_cast<uint64_t>(c) * ld + r : r * ld + c;
+  const uint64_t step = t.tall ? ld : 1;
+  if (vec && n == 4) {
+    if (kU && kBf16) {
+      const uint2 w = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(t.u) + at));
+      x[0] = __uint_as_float(w.x << 16), x[1] = __uint_as_float(w.x & 0xffff0000u);
+      x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
+    } else {
+      const float4 y = kU ? __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(t.u) + at))
+                          : *reinterpret_cast<const float4*>(t.m + at);
+      x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j) {
+    x[j] = 0.0f;
+    if (j < n) {
+      if (!kU) x[j] = t.m[at + j * step];
+      else if (kBf16) x[j] = bf16_bits_to_f32(__ldg(static_cast<const uint16_t*>(t.u) + at + j * step));
+      else x[j] = __ldg(static_cast<const float*>(t.u) + at + j * step);
+    }
+  }
+}
+__device__ __forceinline__ void store_m(const SmallMat& t, uint32_t r, uint32_t c, uint32_t n,
+                                        bool vec, const float (&x)[4]) {
+  const uint64_t at = t.tall ? static_cast<uint64_t>(c) * t.ld_m + r : r * t.ld_m + c;
+  const uint64_t step = t.tall ? t.ld_m : 1;
+  if (vec && n == 4) {
+    *reinterpret_cast<float4*>(t.m + at) = make_float4(x[0], x[1], x[2], x[3]);
+    return;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j)
+    if (j < n) t.m[at + j * step] = x[j];
 }
 
 template <bool kBf16>
@@ -141,55 +178,63 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  cluster_arrive();
   const uint32_t tmem = s_tmem, d_sq = tmem, d_x = tmem + 256;
   griddep_wait();
 
-  // Momentum and |U|^2. Entries in the order they lie in memory: along the
-  // columns of X, or (tall) along its rows.
-  const uint32_t entries = t.side * cols, run = t.tall ? t.side : cols;
-  auto place = [&](uint32_t i, uint32_t& r, uint32_t& c) -> uint64_t {
-    const uint32_t a = i / run, b = i - a * run;
-    r = t.tall ? b : a;
-    c = t.tall ? a : b;
-    return t.tall ? static_cast<uint64_t>(c_first + a) * t.ld_u + b
-                  : static_cast<uint64_t>(a) * t.ld_u + c_first + b;
-  };
-  auto place_m = [&](uint32_t i) -> uint64_t {
-    const uint32_t a = i / run, b = i - a * run;
-    return t.tall ? static_cast<uint64_t>(c_first + a) * t.ld_m + b
-                  : static_cast<uint64_t>(a) * t.ld_m + c_first + b;
-  };
+  // Momentum and |U|^2, four columns of X at a time (lanes along the matrix's
+  // rows as they lie in memory). U waits in X's place, the high and the low
+  // halves of its fp32 words where hi and lo will be.
+  const uint32_t c_units = (cols + 3) / 4, units = t.side * c_units;
+  const bool vec_u = !t.tall && t.ld_u % 4 == 0 && c_first % 4 == 0 &&
+                     reinterpret_cast<uintptr_t>(t.u) % (kBf16 ? 8 : 16) == 0;
+  const bool vec_m = !t.tall && t.ld_m % 4 == 0 && reinterpret_cast<uintptr_t>(t.m) % 16 == 0;
   FF total{0.0f, 0.0f};
-  for (uint32_t i0 = tid; i0 < entries; i0 += 8 * kSmallThreads) {
-    float x[8];
+  for (uint32_t i0 = tid; i0 < units; i0 += 4 * kSmallThreads) {
+    float x[4][4];
+    uint32_t r[4], c[4], n[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t i = i0 + j * kSmallThreads;
-      uint32_t r, c;
-      x[j] = i < entries ? load_u<kBf16>(t, place(i, r, c)) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t i = i0 + j * kSmallThreads, by = t.tall ? t.side : c_units, q = i / by;
+      r[j] = t.tall ? i - q * by : q;
+      c[j] = (t.tall ? q : i - q * by) * 4;
+      n[j] = i < units ? min(4u, cols - c[j]) : 0;
+      load_4<kBf16, true>(t, r[j], c_first + c[j], n[j], vec_u, x[j]);
     }
     if (t.m) {
-      float m[8];
+      float m[4][4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t i = i0 + j * kSmallThreads;
-        m[j] = i < entries ? t.m[place_m(i)] : 0.0f;
-      }
+      for (int j = 0; j < 4; ++j) load_4<kBf16, false>(t, r[j], c_first + c[j], n[j], vec_m, m[j]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t i = i0 + j * kSmallThreads;
-        m[j] = __fmaf_rn(args.mu, m[j], x[j]);
-        if (i < entries) t.m[place_m(i)] = m[j];
-        x[j] = __fadd_rn(x[j], m[j]);
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          m[j][k] = __fmaf_rn(args.mu, m[j][k], x[j][k]);
+          x[j][k] = __fadd_rn(x[j][k], m[j][k]);
+        }
+        store_m(t, r[j], c_first + c[j], n[j], vec_m, m[j]);
       }
     }
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = __fmaf_rn(x[j], x[j], s);
+    for (int j = 0; j < 4; ++j) {
+      if (n[j] == 0) continue;
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        s = __fmaf_rn(x[j][k], x[j][k], s);
+        w[k] = __float_as_uint(x[j][k]);
+      }
+      const uint32_t at = c[j] / 64 * kTileBytes + tile_at(r[j], c[j] % 64);
+      *reinterpret_cast<uint2*>(xh + at) =
+          make_uint2(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+      *reinterpret_cast<uint2*>(xl + at) =
+          make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+    }
     total = ff_add(total, FF{s, 0.0f});
   }
   total = block_sum_ff(total, s_ff);
-  cluster_sync();  // the other CTAs have started: their shared memory may be written
+  cluster_wait();  // the other CTAs have started: their shared memory may be written
   if (tid == 0)
     for (uint32_t q = 0; q < ranks; ++q)
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(cluster_addr(&s_norm[rank], q)),
@@ -201,31 +246,20 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   const double norm = sqrt(ff_to_double(sum));
   const float inv = norm == 0.0 ? 0.0f : static_cast<float>(static_cast<double>(kScaleX) / norm);
 
-  // X as hi + lo (second read of U, and of the momentum just written)
-  for (uint32_t i0 = tid; i0 < entries; i0 += 8 * kSmallThreads) {
-    float x[8];
+  // X as hi + lo, in place (zeros where there is no entry)
+  for (uint32_t i = tid; i < t.side * blocks * 8; i += kSmallThreads) {
+    const uint32_t block = i / (t.side * 8), r = i / 8 - block * t.side;
+    const uint32_t at = block * kTileBytes + tile_at(r, i % 8 * 8);
+    const uint4 h = *reinterpret_cast<const uint4*>(xh + at);
+    const uint4 l = *reinterpret_cast<const uint4*>(xl + at);
+    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t i = i0 + j * kSmallThreads;
-      uint32_t r, c;
-      x[j] = 0.0f;
-      if (i < entries) {
-        x[j] = load_u<kBf16>(t, place(i, r, c));
-        if (t.m) x[j] = __fadd_rn(x[j], t.m[place_m(i)]);
-      }
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __fmul_rn(__uint_as_float(__byte_perm(lw[j], hw[j], 0x5410)), inv);
+      v[2 * j + 1] = __fmul_rn(__uint_as_float(__byte_perm(lw[j], hw[j], 0x7632)), inv);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t i = i0 + j * kSmallThreads;
-      if (i < entries) {
-        uint32_t r, c;
-        place(i, r, c);
-        const float y = __fmul_rn(x[j], inv);
-        const uint32_t at = c / 64 * kTileBytes + tile_at(r, c % 64);
-        *reinterpret_cast<uint16_t*>(xh + at) = __half_as_ushort(__float2half_rn(y));
-        *reinterpret_cast<uint16_t*>(xl + at) = __half_as_ushort(__float2half_rn(rest(y)));
-      }
-    }
+    store_pair_8(xh + at, xl + at, v);
   }
 
   // Products: one thread issues, all wait. An operand pair is taken as
