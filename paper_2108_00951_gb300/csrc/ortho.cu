@@ -16,8 +16,10 @@
 // Operands are fp16 with power-of-two scales (X 2^14, A and B 2^13: |X| <= 1.3
 // throughout, so nothing overflows), which keeps 11 bits where bf16 keeps 8:
 // the steps amplify small singular values up to 485 times, and with them any
-// rounding. The linear term a X is taken from an fp32 copy, so that directions
-// the products hardly touch keep their bits; and B is kept as
+// rounding. For the linear term a X the rounding that the fp16 operand leaves is
+// kept too, 8 more bits of each entry (X phases are bound by the bytes they
+// move: 6 an entry, where an fp32 copy beside the operand made it 10), so that
+// directions the products hardly touch keep their bits; and B is kept as
 // B + 2 I, whose diagonal (-0.8 to 2 instead of -2.8 to 0) rounds finer, the
 // term -2 X moving into the linear one. Relative error of the result against
 // 64 bits about 1e-3 (bf16 operands: 1e-2), below the rounding of the bf16
@@ -25,9 +27,6 @@
 // roundings to average over: its operands are pairs hi + lo of fp16 (22 bits)
 // and its products three (hi hi + hi lo + lo hi), within 1e-4; they are small
 // enough for that to cost little.
-//
-// The fp32 copies lie in blocks of 128 rows x 32 columns, four columns of all
-// rows together, as the epilogues read and write them: contiguous per warp.
 #include "product.cuh"
 
 #include <algorithm>
@@ -44,10 +43,34 @@ constexpr float kScaleX = 16384.0f, kScaleA = 8192.0f;
 constexpr int kSteps = 5;
 constexpr uint32_t kExactSide = 128;
 
-// Element (row, col .. col + 3) of a matrix in blocks: float4 units.
-__device__ __forceinline__ uint64_t block_at(uint32_t row, uint32_t col, uint32_t chunks) {
-  return (static_cast<uint64_t>(row / kTileM) * chunks + col / 32) * (8 * kTileM) +
-         (col % 32) / 4 * kTileM + row % kTileM;
+// The 8 bits that fp16 leaves of an fp32 value x: the difference of the two bit
+// patterns, in units of 2^5 (x = its fp16 value, widened, + 32 rest, as
+// integers). Where fp16 is subnormal the difference saturates; those entries
+// are below 2^-14 2^-14 of the largest.
+__device__ __forceinline__ int rest_of(float x, float half) {
+  return (__float_as_int(x) - __float_as_int(half) + 16) >> 5;
+}
+__device__ __forceinline__ uint32_t pack_rest(int a, int b, int c, int d) {
+  uint32_t r;
+  asm("{\n\t.reg .b32 t;\n\t"
+      "cvt.pack.sat.s8.s32.b32 t, %4, %3, 0;\n\t"
+      "cvt.pack.sat.s8.s32.b32 %0, %2, %1, t;\n\t}"
+      : "=r"(r)
+      : "r"(a), "r"(b), "r"(c), "r"(d));
+  return r;
+}
+template <int kByte>
+__device__ __forceinline__ float with_rest(float half, uint32_t word) {
+  uint32_t rest;  // the byte, its sign extended
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(rest) : "r"(word), "n"(0x8880 | 0x1111 * kByte));
+  return __int_as_float(__float_as_int(half) + static_cast<int>(rest << 5));
+}
+// Rests lie in blocks of 128 rows x 32 columns, 16 columns of all rows
+// together, as the epilogues read and write them: contiguous per warp. Unit of
+// (row, col / 16), in 16 bytes.
+__device__ __forceinline__ uint64_t rest_at(uint32_t row, uint32_t col, uint32_t chunks) {
+  return ((static_cast<uint64_t>(row / kTileM) * chunks + col / 32) * 2 + col % 32 / 16) * kTileM +
+         row % kTileM;
 }
 
 // ---- momentum, norm, and the first X
@@ -59,12 +82,12 @@ struct PrepMat {
   const void* u;
   float* m;
   uint16_t* out;  // where the last step writes
-  float* x;       // X in blocks, scaled
-  uint16_t* hi;   // X in fp16, rows ld_x apart
-  uint16_t* lo;   // what hi leaves (exact matrices), or nullptr
+  uint16_t* hi;   // X in fp16, scaled, rows ld_x apart
+  uint16_t* lo;   // what hi leaves in fp16 (exact matrices), or nullptr
+  uint4* rest;    // else its rests
   uint64_t ld_u, ld_m, ld_out;
   uint32_t rows, cols, ld_x;
-  uint32_t chunks;         // 32-column blocks of a row of x
+  uint32_t chunks;         // 32-column blocks of a row
   uint32_t blocks, blocks_n;
   uint32_t blocks_per_cta;
   uint32_t index;          // in the groups' order
@@ -176,11 +199,10 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__
 __device__ __forceinline__ uint16_t half_bits(float x) {
   return __half_as_ushort(__float2half_rn(x));
 }
-__device__ __forceinline__ float half_rest(float x) {
-  return __fsub_rn(x, __half2float(__float2half_rn(x)));
-}
+__device__ __forceinline__ float half_of(float x) { return __half2float(__float2half_rn(x)); }
+__device__ __forceinline__ float half_rest(float x) { return __fsub_rn(x, half_of(x)); }
 
-// X = U / |U|_F, scaled: fp16 rows and, through shared memory, fp32 blocks.
+// X = U / |U|_F, scaled: fp16 rows and what they leave.
 template <bool kBf16>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ PrepArgs a) {
   __shared__ FF s_ff[32];
@@ -211,7 +233,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
       const float4 y = make_float4(__fmul_rn(x[i].x, inv), __fmul_rn(x[i].y, inv),
                                    __fmul_rn(x[i].z, inv), __fmul_rn(x[i].w, inv));
       s_x[unit][r] = y;
-      if (row < t.rows && col < t.ld_x) {  // rows are padded to 8 columns
+      if (row < t.rows && col < t.ld_x) {  // rows are padded
         const uint64_t at = static_cast<uint64_t>(row) * t.ld_x + col;
         *reinterpret_cast<uint2*>(t.hi + at) = make_uint2(pack_f16(y.x, y.y), pack_f16(y.z, y.w));
         if (t.lo)
@@ -220,12 +242,19 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
                          pack_f16(half_rest(y.z), half_rest(y.w)));
       }
     }
+    if (t.lo) continue;  // (uniform)
     __syncthreads();
-    float4* to = reinterpret_cast<float4*>(t.x);
-    for (uint32_t i = threadIdx.x; i < kPrepCols / 4 * kTileM; i += 256) {
+    for (uint32_t i = threadIdx.x; i < kPrepCols / 16 * kTileM; i += 256) {
       const uint32_t u = i / kTileM, r = i % kTileM;
-      if (col0 + u * 4 < t.chunks * 32)
-        to[block_at(tile * kTileM + r, col0 + u * 4, t.chunks)] = s_x[u][r];
+      if (col0 + u * 16 >= t.chunks * 32) break;
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 y = s_x[u * 4 + j][r];
+        w[j] = pack_rest(rest_of(y.x, half_of(y.x)), rest_of(y.y, half_of(y.y)),
+                         rest_of(y.z, half_of(y.z)), rest_of(y.w, half_of(y.w)));
+      }
+      t.rest[rest_at(tile * kTileM + r, col0 + u * 16, t.chunks)] = make_uint4(w[0], w[1], w[2], w[3]);
     }
     __syncthreads();
   }
@@ -234,34 +263,41 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
 // ---- the products' epilogues
 enum : uint32_t { kFormA = 0, kFormB = 1, kFormX = 2 };
 
-// 32 fp32 of the thread's row from blocks, and back.
-__device__ __forceinline__ void load_block(const float4* p, float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float4 x = __ldcg(p + j * kTileM);
-    v[4 * j] = x.x, v[4 * j + 1] = x.y, v[4 * j + 2] = x.z, v[4 * j + 3] = x.w;
-  }
-}
-__device__ __forceinline__ void keep_block(float4* p, const float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    __stcg(p + j * kTileM, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+__device__ __forceinline__ float2 unpack_f16(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 __device__ __forceinline__ void pack_row(const float (&v)[32], uint32_t (&w)[16]) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) w[j] = pack_f16(v[2 * j], v[2 * j + 1]);
+}
+// 32 fp16 of a row (rows are padded to 32 bytes), from L2: other SMs wrote them
+// in this launch.
+__device__ __forceinline__ void load_row(const uint16_t* p, uint32_t left, uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (static_cast<uint32_t>(16 * i) < left)
+      asm volatile("ld.relaxed.gpu.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(w[8 * i]), "=r"(w[8 * i + 1]), "=r"(w[8 * i + 2]), "=r"(w[8 * i + 3]),
+                     "=r"(w[8 * i + 4]), "=r"(w[8 * i + 5]), "=r"(w[8 * i + 6]), "=r"(w[8 * i + 7])
+                   : "l"(p + 16 * i)
+                   : "memory");
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[8 * i + j] = 0;
+  }
 }
 
 struct StepEpilogue {
   struct Params {
     uint32_t form;
     uint32_t exact;         // operands have a second plane
-    uint32_t ld;            // of the fp16 result: rows padded to 8 columns
-    uint32_t chunks;        // 32-column blocks of a row of `blocks`
-    uint64_t plane;         // fp16 elements of a plane
-    uint64_t batch_blocks;  // floats of a matrix in blocks
+    uint32_t ld;            // of the fp16 result: rows padded to 16 columns
+    uint32_t chunks;        // 32-column blocks of a row of `rest`
+    uint64_t plane;         // fp16 elements of a plane of the result
+    uint64_t rest_units;    // of a matrix in `rest`
     uint16_t* to;           // the fp16 result [batch][planes][rows][ld]
-    float* blocks;          // A: written by kFormA, read by kFormB; X: both
+    const uint16_t* from;   // likewise: A (kFormB) or X (kFormX), of to's shape
+    uint4* rest;            // kFormX: what `from` leaves; rewritten for `to`
     uint16_t* const* outs;  // the last step's results, by batch
     const uint64_t* ld_outs;
     uint32_t last_phase;
@@ -281,7 +317,7 @@ struct StepEpilogue {
     pack_row(v, w);
     if (col0 == r0) mirror_block(s.turn, w);
     const uint32_t cols = ld - col0;
-    store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, [&](uint32_t i) -> uint16_t* {
+    store_block<2>(s.turn, w, min(cols, 32u), 16, [&](uint32_t i) -> uint16_t* {
       return r0 + i < n ? out + static_cast<uint64_t>(r0 + i) * ld + col0 : nullptr;
     });
     if (col0 < r0 && r < n) {
@@ -296,8 +332,9 @@ struct StepEpilogue {
                                               Smem& s, const ProductAcc& acc, uint32_t phase) {
     const uint32_t r = it.m0 + row, r0 = it.m0 + (row & ~31u);
     const uint32_t planes = e.exact ? 2 : 1;
-    float4* blocks = reinterpret_cast<float4*>(e.blocks + it.batch * e.batch_blocks) +
-                     static_cast<uint64_t>(it.m0 / kTileM) * e.chunks * (8 * kTileM) + row;
+    const uint16_t* from = e.from + it.batch * planes * e.plane + static_cast<uint64_t>(r) * e.ld;
+    uint4* rests = e.rest + it.batch * e.rest_units +
+                   static_cast<uint64_t>(it.m0 / kTileM) * e.chunks * (2 * kTileM) + row;
     uint16_t* to = e.to + it.batch * planes * e.plane;
     const bool last = e.form == kFormX && phase == e.last_phase;
     uint16_t* out = nullptr;
@@ -310,45 +347,94 @@ struct StepEpilogue {
       align = low % 16 == 0 ? 16 : low % 4 == 0 ? 4 : 2;
     }
     const bool rows_exist = r0 < p.m;
+    auto alive = [&](uint32_t c) {  // the warp's block has entries to store
+      const uint32_t col0 = it.n0 + c * 32;
+      return rows_exist && col0 < p.n && (e.form == kFormX || col0 <= r0 + 31);
+    };
+    uint32_t h[16], l[16];  // of `from`: fp16, and lo or rests; a block ahead of their use
+    auto fetch = [&](uint32_t c) {
+      if (e.form == kFormA || c >= acc.c1 || !alive(c)) return;
+      const uint32_t col0 = it.n0 + c * 32, left = r < p.m ? e.ld - col0 : 0;
+      load_row(from + col0, left, h);
+      if (e.exact) {
+        load_row(from + e.plane + col0, left, l);
+      } else if (e.form == kFormX) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint4 y = __ldcg(rests + (static_cast<uint64_t>(col0 / 32) * 2 + i) * kTileM);
+          l[4 * i] = y.x, l[4 * i + 1] = y.y, l[4 * i + 2] = y.z, l[4 * i + 3] = y.w;
+        }
+      }
+    };
+    fetch(acc.c0);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       const uint32_t col0 = it.n0 + c * 32;
-      float4* mine = blocks + static_cast<uint64_t>(col0 / 32) * (8 * kTileM);
-      const bool live = rows_exist && col0 < p.n && (e.form == kFormX || col0 <= r0 + 31);
-      float x[32], v[32];
-      if (live && e.form != kFormA) load_block(mine, x);  // in flight beside the accumulators
+      const bool live = alive(c);
+      float v[32];
       acc.load(c, v);
-      if (!live) continue;  // (uniform)
+      if (!live) {  // (uniform)
+        fetch(c + 1);
+        continue;
+      }
       if (e.form == kFormX) {
+        // the operand's rounding of x stands in the term that B + 2 I took over
+        constexpr float kOp = -kNsShift;
+        if (e.exact) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          // the operand's rounding of x stands in the term that B + 2 I took over
-          const float h = __half2float(__float2half_rn(x[j]));
-          const float op = e.exact ? __fadd_rn(h, __half2float(__float2half_rn(__fsub_rn(x[j], h)))) : h;
-          v[j] = __fmaf_rn(v[j], 1.0f / kScaleA, __fmaf_rn(kNsA, x[j], __fmul_rn(-kNsShift, op)));
+          for (int j = 0; j < 16; ++j) {
+            const float2 hi = unpack_f16(h[j]), lo = unpack_f16(l[j]);
+            const float x0 = __fadd_rn(hi.x, lo.x), x1 = __fadd_rn(hi.y, lo.y);
+            v[2 * j] = __fmaf_rn(v[2 * j], 1.0f / kScaleA, __fmul_rn(kNsA + kOp, x0));
+            v[2 * j + 1] = __fmaf_rn(v[2 * j + 1], 1.0f / kScaleA, __fmul_rn(kNsA + kOp, x1));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const float2 a = unpack_f16(h[j]), b = unpack_f16(h[j + 1]);
+            const uint32_t w = l[j / 2];
+            const float x0 = with_rest<0>(a.x, w), x1 = with_rest<1>(a.y, w);
+            const float x2 = with_rest<2>(b.x, w), x3 = with_rest<3>(b.y, w);
+            v[2 * j] = __fmaf_rn(v[2 * j], 1.0f / kScaleA, __fmaf_rn(kNsA, x0, __fmul_rn(kOp, a.x)));
+            v[2 * j + 1] = __fmaf_rn(v[2 * j + 1], 1.0f / kScaleA, __fmaf_rn(kNsA, x1, __fmul_rn(kOp, a.y)));
+            v[2 * j + 2] = __fmaf_rn(v[2 * j + 2], 1.0f / kScaleA, __fmaf_rn(kNsA, x2, __fmul_rn(kOp, b.x)));
+            v[2 * j + 3] = __fmaf_rn(v[2 * j + 3], 1.0f / kScaleA, __fmaf_rn(kNsA, x3, __fmul_rn(kOp, b.y)));
+          }
         }
+        fetch(c + 1);
         uint32_t w[16];
         if (last) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             w[j] = pack_bf16(__fmul_rn(v[2 * j], 1.0f / kScaleX), __fmul_rn(v[2 * j + 1], 1.0f / kScaleX));
-          store_block(s.turn, w, p.n - col0, align, [&](uint32_t i) -> uint16_t* {
+          store_block<2>(s.turn, w, min(p.n - col0, 32u), align, [&](uint32_t i) -> uint16_t* {
             return r0 + i < p.m ? out + (r0 + i) * ld_out + col0 : nullptr;
           });
           continue;
         }
-        keep_block(mine, v);
         const uint32_t cols = e.ld - col0;
         auto rows = [&](uint32_t i) -> uint16_t* {
           return r0 + i < p.m ? to + static_cast<uint64_t>(r0 + i) * e.ld + col0 : nullptr;
         };
         pack_row(v, w);
-        store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, rows);
+        if (!e.exact) {
+          uint32_t q[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 a = unpack_f16(w[2 * j]), b = unpack_f16(w[2 * j + 1]);
+            q[j] = pack_rest(rest_of(v[4 * j], a.x), rest_of(v[4 * j + 1], a.y),
+                             rest_of(v[4 * j + 2], b.x), rest_of(v[4 * j + 3], b.y));
+          }
+          uint4* mine = rests + static_cast<uint64_t>(col0 / 32) * (2 * kTileM);
+          __stcg(mine, make_uint4(q[0], q[1], q[2], q[3]));
+          __stcg(mine + kTileM, make_uint4(q[4], q[5], q[6], q[7]));
+        }
+        store_block<2>(s.turn, w, min(cols, 32u), 16, rows);
         if (e.exact) {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = half_rest(v[j]);
           pack_row(v, w);
           to += e.plane;
-          store_block(s.turn, w, cols, cols >= 32 ? 16 : 4, rows);
+          store_block<2>(s.turn, w, min(cols, 32u), 16, rows);
           to -= e.plane;
         }
         continue;
@@ -356,15 +442,22 @@ struct StepEpilogue {
       if (e.form == kFormA) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __fmul_rn(v[j], kScaleA / (kScaleX * kScaleX));
-        keep_block(mine, v);
       } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < 16; ++j) {
           // A as its products read it: errors of b A and c A A cancel in part
-          const float a = e.exact ? x[j] : __half2float(__float2half_rn(x[j]));
-          v[j] = __fmaf_rn(kNsB, a, __fmul_rn(v[j], kNsC / kScaleA));
-          if (col0 + j == r) v[j] = __fmaf_rn(kNsShift, kScaleA, v[j]);
+          float2 a = unpack_f16(h[j]);
+          if (e.exact) {
+            const float2 lo = unpack_f16(l[j]);
+            a = make_float2(__fadd_rn(a.x, lo.x), __fadd_rn(a.y, lo.y));
+          }
+          v[2 * j] = __fmaf_rn(kNsB, a.x, __fmul_rn(v[2 * j], kNsC / kScaleA));
+          v[2 * j + 1] = __fmaf_rn(kNsB, a.y, __fmul_rn(v[2 * j + 1], kNsC / kScaleA));
         }
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (col0 + j == r) v[j] = __fmaf_rn(kNsShift, kScaleA, v[j]);
+        fetch(c + 1);
       }
       store_symmetric(to, e.ld, p.n, r, col0, v, s);
       if (e.exact) {
@@ -387,8 +480,8 @@ constexpr uint32_t kOrthoGroups = 12;  // shapes per launch, at most
 struct Group {
   uint32_t rows = 0, cols = 0, side = 0, ld_x = 0, ld_s = 0, planes = 1;
   std::vector<uint32_t> mats;
-  size_t half[2] = {0, 0}, x = 0, a = 0, a_blocks = 0, b = 0;  // scratch offsets
-  uint64_t x_floats = 0, a_floats = 0;  // of one matrix in blocks
+  size_t half[2] = {0, 0}, rest = 0, a = 0, b = 0;  // scratch offsets
+  uint64_t rest_units = 0;              // of one matrix, 16 bytes each
   uint32_t first = 0;                   // its first matrix, in the groups' order
   bool left() const { return rows <= cols; }
 };
@@ -398,10 +491,6 @@ struct Plan {
   size_t parts = 0, outs = 0, ld_outs = 0, join = 0, total = 0;
   bool pair = false;
 };
-
-uint64_t block_floats(uint32_t rows, uint32_t cols) {
-  return static_cast<uint64_t>(round_up(rows, kTileM)) * round_up(cols, 32);
-}
 
 // The shapes of a launch's products for `count` groups from `g0`; returns the
 // bytes of the scratch that joining K parts takes.
@@ -423,9 +512,9 @@ size_t shape_products(Args& args, const Plan& plan, size_t g0, uint32_t count, d
       ProductShape s = {};
       double mine = cost(g, f) / work[f] * sms;
       if (mine < 1.0) mine = 1.0;
-      if (f == kFormA) plan_product(s, {g.side, g.side, deep, batch, true, plan.pair, mine, 16, terms});
-      if (f == kFormB) plan_product(s, {g.side, g.side, g.side, batch, true, plan.pair, mine, 8, terms});
-      if (f == kFormX) plan_product(s, {g.rows, g.cols, g.side, batch, false, plan.pair, mine, 1, terms});
+      if (f == kFormA) plan_product(s, {g.side, g.side, deep, batch, true, plan.pair, mine, 16, terms, 20.0, true});
+      if (f == kFormB) plan_product(s, {g.side, g.side, g.side, batch, true, plan.pair, mine, 8, terms, 20.0, true});
+      if (f == kFormX) plan_product(s, {g.rows, g.cols, g.side, batch, false, plan.pair, mine, 1, terms, 40.0, true});
       if (f == kFormA) args.shape[kEntryA * count + i] = args.shape[(kEntryA + 1) * count + i] = s;
       if (f == kFormB) args.shape[kEntryB * count + i] = s;
       if (f == kFormX) args.shape[kEntryX * count + i] = args.shape[(kEntryX + 1) * count + i] = s;
@@ -460,8 +549,8 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
       g->rows = mats[i].rows;
       g->cols = mats[i].cols;
       g->side = g->rows < g->cols ? g->rows : g->cols;
-      g->ld_x = round_up(g->cols, 8);
-      g->ld_s = round_up(g->side, 8);
+      g->ld_x = round_up(g->cols, 16);
+      g->ld_s = round_up(g->side, 16);
       g->planes = g->side <= kExactSide ? 2 : 1;
     }
     g->mats.push_back(i);
@@ -488,12 +577,12 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
     const size_t batch = g.mats.size();
     const size_t x = 2ull * batch * g.planes * g.rows * g.ld_x;
     const size_t s = 2ull * batch * g.planes * g.side * g.ld_s;
-    g.x_floats = block_floats(g.rows, g.cols);
-    g.a_floats = block_floats(g.side, g.side);
     for (int i = 0; i < 2; ++i) g.half[i] = take(x);
-    g.x = take(4 * batch * g.x_floats);
+    if (g.planes == 1) {
+      g.rest_units = static_cast<uint64_t>(round_up(g.rows, kTileM)) * round_up(g.cols, 32) / 16;
+      g.rest = take(16 * batch * g.rest_units);
+    }
     g.a = take(s);
-    g.a_blocks = take(4 * batch * g.a_floats);
     g.b = take(s);
     g.first = all;
     all += static_cast<uint32_t>(batch);
@@ -552,7 +641,7 @@ cudaError_t prepare(const OrthoMat* mats, const Plan& plan, bool bf16, float mu,
       t.ld_u = m.ld_u;
       t.ld_m = m.ld_m;
       t.ld_out = m.ld_out;
-      t.x = reinterpret_cast<float*>(base + g.x) + b * g.x_floats;
+      t.rest = reinterpret_cast<uint4*>(base + g.rest) + b * g.rest_units;
       t.hi = reinterpret_cast<uint16_t*>(base + g.half[0]) +
              b * g.planes * g.rows * static_cast<uint64_t>(g.ld_x);
       t.lo = g.planes == 2 ? t.hi + g.rows * static_cast<uint64_t>(g.ld_x) : nullptr;
@@ -609,11 +698,9 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
         map(&s.b, g.half[from], false, left ? b_box(s, pair) : kTileK);
         e.form = kFormA;
         e.ld = g.ld_s;
-        e.chunks = round_up(g.side, 32) / 32;
         e.plane = static_cast<uint64_t>(g.side) * g.ld_s;
-        e.batch_blocks = g.a_floats;
         e.to = reinterpret_cast<uint16_t*>(base + g.a);
-        e.blocks = reinterpret_cast<float*>(base + g.a_blocks);
+        e.from = e.to;  // (not read)
         args.epi[(kEntryA + from) * count + i] = e;
       }
       if (from == 0) {
@@ -621,6 +708,7 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
         map(&s.a, g.a, true, kTileM);
         map(&s.b, g.a, true, b_box(s, pair));
         e.form = kFormB;
+        e.from = e.to;
         e.to = reinterpret_cast<uint16_t*>(base + g.b);
         args.epi[kEntryB * count + i] = e;
       }
@@ -637,9 +725,10 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
       e.ld = g.ld_x;
       e.chunks = round_up(g.cols, 32) / 32;
       e.plane = static_cast<uint64_t>(g.rows) * g.ld_x;
-      e.batch_blocks = g.x_floats;
+      e.rest_units = g.rest_units;
+      e.from = reinterpret_cast<const uint16_t*>(base + g.half[from]);
       e.to = reinterpret_cast<uint16_t*>(base + g.half[from ^ 1u]);
-      e.blocks = reinterpret_cast<float*>(base + g.x);
+      e.rest = reinterpret_cast<uint4*>(base + g.rest);
       args.epi[(kEntryX + from) * count + i] = e;
     }
   }

@@ -40,11 +40,11 @@ bool make_map(CUtensorMap* map, const void* base, bool bf16, uint64_t cols, uint
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The time of a launch is its longest CTA's (or pair's): whole tiles, each of
-// its 128-deep steps (4 cycles per column on the tensor cores, or the cycles
-// that a CTA's share of A and B takes from L2 at 64 bytes a cycle) plus what a
-// tile costs beside them, and for joined K parts the join by one CTA, which
-// reads them at about 64 bytes a cycle too.
+// The time of a launch is its longest CTA's (or pair's): whole tiles, each the
+// longer of its 128-deep steps (4 cycles per column on the tensor cores, or the
+// cycles that a CTA's share of A and B takes from L2 at 64 bytes a cycle) and
+// its epilogue, which runs under the next tile's products; and for K parts the
+// join, or (not joined here) writing and reading their sums.
 void plan_product(ProductShape& p, const ProductWant& w) {
   const uint32_t rows = w.pair ? 2 * kTileM : kTileM;
   p.m = w.m;
@@ -53,7 +53,7 @@ void plan_product(ProductShape& p, const ProductWant& w) {
   p.batch = w.batch;
   p.lower = w.lower ? 1u : 0u;
   p.terms = w.terms;
-  p.join = 1;
+  p.join = w.join ? 1u : 0u;
   p.tiles_m = (w.m + rows - 1) / rows;
   p.group_m = p.tiles_m ? p.tiles_m : 1;
   const double units = w.pair ? w.sms / 2 : w.sms;
@@ -71,8 +71,12 @@ void plan_product(ProductShape& p, const ProductWant& w) {
       if (s > 1 && tiles > 2 * units) break;  // nothing to gain
       const double waves = ceil(tiles * s / units);
       const double deep = static_cast<double>((kts + s - 1) / s);
-      const double t = waves * (deep * step + 1500.0 + 6.0 * bn) +
-                       (s > 1 ? (s + 1) * 8.0 * bn + 2500.0 : 0.0);
+      // an epilogue runs under the next tile's products
+      const double products = deep * step, epilogue = w.epilogue * bn;
+      const double t = waves * (products > epilogue ? products : epilogue) + 600.0 * waves +
+                       (products > epilogue ? epilogue : products) +
+                       (s == 1 ? 0.0 : w.join ? 16.0 * bn + 5000.0
+                                              : s * (8.0 * w.m) * w.n / (20.0 * w.sms) + 4000.0);
       if (p.bn == 0 || t < best * 0.999) {
         best = t;
         p.bn = bn;

@@ -18,10 +18,13 @@
 // CTA loading half: 64 bytes a cycle. Stages are 128 of K deep so that every
 // box has 16 KB, K-major (64 k x 128 rows) or MN-major (64 x 128 k).
 //
-// Parts of K are joined without waiting: each part writes its fp32
-// accumulators to scratch and counts itself in; the last part to arrive adds
-// all parts in their order (so the sum does not depend on which was last) and
-// runs the epilogue.
+// Parts of K (cooperative launches only): each part's CTA writes its fp32
+// accumulators to scratch, counts itself in, waits for the others and then adds
+// all parts, in their order, of its share of the tile's 32 x 32 blocks, whose
+// epilogue it runs. (One CTA joining a tile of 8 parts alone takes 4 us at the
+// 120 GB/s an SM reads.) The parts of a tile are consecutive items, and a CTA
+// takes its items in ascending order, so the lowest unfinished tile never waits
+// for a higher one.
 //
 // A launch may have several phases with a grid barrier between (a cooperative
 // launch): what one phase's epilogues write the next one's TMA reads.
@@ -130,7 +133,7 @@ struct ProductArgs {
   uint32_t phases;
   uint32_t first[kMaxPhases], problems[kMaxPhases], items[kMaxPhases];  // of each phase
   float* parts;         // scratch tiles of split items
-  uint32_t* arrivals;   // by the tile's first scratch tile; zero between launches
+  uint32_t* arrivals;   // by the tile's first scratch tile; zero between tiles
   uint32_t part_chunks; // 32-column chunks per scratch tile
   uint32_t* error;
   uint32_t entries;     // problems in shape[]
@@ -140,7 +143,7 @@ struct ProductArgs {
 
 struct ProductSmem {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2];
-  uint32_t tmem, last;
+  uint32_t tmem, joined;
 };
 
 // What an epilogue reads its accumulators through: 32 columns of the thread's
@@ -187,6 +190,15 @@ struct ProductAcc {
   }
 };
 
+// Waits until a counter has reached `target` (modulo 2^32).
+__device__ __forceinline__ bool wait_count(const uint32_t* word, uint32_t target, uint64_t limit_ns) {
+  const uint64_t t0 = global_timer_ns();
+  uint32_t polls = 0;
+  while (static_cast<int32_t>(ld_acquire_u32(word) - target) < 0)
+    if ((++polls & 63u) == 0 && (polls > (1u << 26) || global_timer_ns() - t0 > limit_ns)) return false;
+  return true;
+}
+
 // Barrier of all CTAs of a cooperative launch: `target` arrivals since the
 // launch began. One word is counted up and polled.
 __device__ __forceinline__ bool phase_barrier(uint32_t* word, uint32_t target, uint64_t limit_ns) {
@@ -195,14 +207,7 @@ __device__ __forceinline__ bool phase_barrier(uint32_t* word, uint32_t target, u
   if (threadIdx.x == 0) {
     __threadfence();
     atomicAdd(word, 1u);
-    const uint64_t t0 = global_timer_ns();
-    uint32_t polls = 0;
-    while (static_cast<int32_t>(ld_acquire_u32(word) - target) < 0) {
-      if ((++polls & 63u) == 0 && (polls > (1u << 26) || global_timer_ns() - t0 > limit_ns)) {
-        ok = false;
-        break;
-      }
-    }
+    ok = wait_count(word, target, limit_ns);
     __threadfence();
   }
   return __syncthreads_and(ok);
@@ -385,10 +390,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         // zeros (the call's results are void: the timeout is latched)
         from.none |= !ok;
         if (!from.none && from.c0 == from.c1) from.arrive();
+        uint32_t block = 0, blocks = 1;
         if (p.splits > 1 && p.join) {
           const uint64_t tile_floats = static_cast<uint64_t>(args.part_chunks) * 32 * kTileM;
-          float* mine = args.parts + static_cast<uint64_t>(it.part) * tile_floats + row * 4;
-          float* dst = mine + it.split * tile_floats;
+          float* mine = args.parts + static_cast<uint64_t>(it.part) * tile_floats;
+          float* dst = mine + it.split * tile_floats + row * 4;
           for (uint32_t c = from.c0; c < from.c1; ++c) {
             float v[32];
             from.load(c, v);
@@ -397,24 +403,39 @@ __global__ void __launch_bounds__(kProductThreads, 1)
               __stcg(reinterpret_cast<float4*>(dst + static_cast<uint64_t>(c) * (32 * kTileM)) + j * kTileM,
                      make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
           }
-          __threadfence();
           asm volatile("bar.sync 2, 256;" ::: "memory");
           if (warp == 2 && lane == 0) {
-            const uint32_t before = atomicAdd(&args.arrivals[it.part], 1u);
-            s.last = before == p.splits - 1 ? 1u : 0u;
-            if (s.last) args.arrivals[it.part] = 0;  // ready for the next launch
+            __threadfence();
+            // every part counts once more when it has seen all of them; the last
+            // of those readies the counter for its next tile
+            uint32_t* counter = &args.arrivals[it.part];
+            atomicAdd(counter, 1u);
+            s.joined = wait_count(counter, p.splits, ok ? args.wait_ns : 0) ? 1u : 0u;
+            if (s.joined && atomicAdd(counter, 1u) == 2 * p.splits - 1) atomicExch(counter, 0u);
             __threadfence();
           }
           asm volatile("bar.sync 2, 256;" ::: "memory");
-          const bool last = s.last != 0;
-          asm volatile("bar.sync 2, 256;" ::: "memory");  // s.last is read before it is written again
-          if (!last) continue;
-          __threadfence();
-          from.parts = mine;
-          from.part_stride = tile_floats;
+          ok = ok && s.joined != 0;
+          asm volatile("bar.sync 2, 256;" ::: "memory");  // read before it is written again
+          if (!ok) continue;
+          block = it.split + (warp - 2) * p.splits;
+          blocks = chunks * 4;
           from.none = false;
+          from.part_stride = tile_floats;
+          from.parts = mine;
         }
-        Epi::tile(p, args.epi[prob], it, row, half, epi_smem[warp - 2], from, ph);
+        // the warp's half of the tile at once, or its 32 x 32 blocks of a joined one
+        for (; block < blocks; block += kEpilogueWarps * p.splits) {
+          uint32_t tile_row = row;
+          ProductAcc at = from;
+          if (from.parts) {
+            at.c0 = block >> 2;
+            at.c1 = at.c0 + 1;
+            tile_row = (block & 3u) * 32 + lane;
+            at.parts = from.parts + tile_row * 4;
+          }
+          Epi::tile(p, args.epi[prob], it, tile_row, half, epi_smem[warp - 2], at, ph);
+        }
       }
     }
     __syncwarp();
@@ -448,7 +469,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 struct TurnSmem {
   alignas(16) uint4 unit[32 * 4];
 };
-template <class RowFn>
+// `cols` of the 32 columns exist. kBatch: how many of the narrower stores are
+// read ahead (registers).
+template <int kBatch, class RowFn>
 __device__ __forceinline__ void store_block(TurnSmem& t, const uint32_t (&w)[16], uint32_t cols,
                                             uint32_t align, RowFn rows) {
   const uint32_t lane = threadIdx.x & 31;
@@ -458,35 +481,59 @@ __device__ __forceinline__ void store_block(TurnSmem& t, const uint32_t (&w)[16]
     t.unit[lane * 4 + (u ^ ((lane >> 1) & 3u))] =
         make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
   __syncwarp();
-  if (align >= 16 && cols >= 32) {
+  // (everything is read before the first store: a store might alias)
+  if (align >= 16 && cols % 8 == 0) {
+    const uint32_t r0 = lane >> 2, u = lane & 3u;
+    uint4 x[4];
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
-      const uint32_t r = i * 8 + (lane >> 2), u = lane & 3u;
-      uint16_t* to = rows(r);
-      const uint4 x = t.unit[r * 4 + (u ^ ((r >> 1) & 3u))];
-      if (to) *reinterpret_cast<uint4*>(to + u * 8) = x;
+      const uint32_t r = i * 8 + r0;
+      x[i] = t.unit[r * 4 + (u ^ ((r >> 1) & 3u))];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      uint16_t* to = rows(i * 8 + r0);
+      if (to && u * 8 < cols) *reinterpret_cast<uint4*>(to + u * 8) = x[i];
     }
   } else if (align >= 4) {
-    const uint32_t col = (lane & 15u) * 2;
-#pragma unroll 8
-    for (uint32_t i = 0; i < 16; ++i) {
-      const uint32_t r = i * 2 + (lane >> 4);
-      uint16_t* to = rows(r);
-      const uint32_t x = reinterpret_cast<const uint32_t*>(
-          &t.unit[r * 4 + ((col >> 3) ^ ((r >> 1) & 3u))])[(col >> 1) & 3u];
-      if (to && col + 1 < cols) *reinterpret_cast<uint32_t*>(to + col) = x;
-      else if (to && col < cols) to[col] = static_cast<uint16_t>(x);
+    const uint32_t r0 = lane >> 4, col = (lane & 15u) * 2;
+    const bool both = col + 1 < cols, one = col < cols;
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < 16; i0 += kBatch) {
+      uint32_t x[kBatch];
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        const uint32_t r = (i0 + i) * 2 + r0;
+        x[i] = reinterpret_cast<const uint32_t*>(
+            &t.unit[r * 4 + ((col >> 3) ^ ((r >> 1) & 3u))])[(col >> 1) & 3u];
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        uint16_t* to = rows((i0 + i) * 2 + r0);
+        if (to && both) *reinterpret_cast<uint32_t*>(to + col) = x[i];
+        else if (to && one) to[col] = static_cast<uint16_t>(x[i]);
+      }
     }
   } else {
-#pragma unroll 8
-    for (uint32_t r = 0; r < 32; ++r) {
-      uint16_t* to = rows(r);
-      const uint16_t x = reinterpret_cast<const uint16_t*>(
-          &t.unit[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3u))])[lane & 7u];
-      if (to && lane < cols) to[lane] = x;
+    const bool in = lane < cols;
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < 32; i0 += kBatch) {
+      uint16_t x[kBatch];
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        const uint32_t r = i0 + i;
+        x[i] = reinterpret_cast<const uint16_t*>(
+            &t.unit[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3u))])[lane & 7u];
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kBatch; ++i) {
+        uint16_t* to = rows(i0 + i);
+        if (to && in) to[lane] = x[i];
+      }
     }
   }
 }
+
 // A lane's row of a symmetric 32 x 32 block of which entries up to the diagonal
 // are given: the others are read from the rows that mirror them.
 __device__ __forceinline__ void mirror_block(TurnSmem& t, uint32_t (&w)[16]) {
@@ -529,6 +576,8 @@ struct ProductWant {
   bool lower, pair;
   double sms;
   uint32_t max_splits, terms;
+  double epilogue;  // cycles per column of a tile (about: 128 rows, 8 warps)
+  bool join;        // K parts are joined by the launch
 };
 void plan_product(ProductShape& p, const ProductWant& w);
 // Rows and columns of B a CTA loads at a time (the box of a K-major operand).

@@ -284,7 +284,7 @@ struct GradEpilogue {
 #pragma unroll
       for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
       uint16_t* out = e.g + static_cast<uint64_t>(r & ~31u) * e.ld_g + col0;
-      store_block(s.turn, w, 32, 16, [&](uint32_t i) { return out + i * e.ld_g; });
+      store_block<8>(s.turn, w, 32, 16, [&](uint32_t i) { return out + i * e.ld_g; });
     }
   }
 };
@@ -343,62 +343,61 @@ struct StoreEpilogue {
         continue;
       }
       if (e.extra && real && e.cols - col0 < 32u) {
-        float x = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x = e.cols - col0 == static_cast<uint32_t>(j) ? v[j] : x;
-        e.extra[dst] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
+        for (int j = 0; j < 32; ++j)
+          if (e.cols - col0 == static_cast<uint32_t>(j))
+            e.extra[dst] = static_cast<uint16_t>(pack_bf16(v[j], 0.0f));
       }
       if (col0 >= e.cols) continue;
       uint32_t w[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-      store_block(s.turn, w, e.cols - col0, e.align, [&](uint32_t i) -> uint16_t* {
-        const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
-        return to == 0xffffffffu ? nullptr : e.out + static_cast<uint64_t>(to) * e.ld + col0;
-      });
+      if (e.row_map) {
+        store_block<8>(s.turn, w, min(32u, e.cols - col0), e.align, [&](uint32_t i) -> uint16_t* {
+          const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
+          return to == 0xffffffffu ? nullptr : e.out + static_cast<uint64_t>(to) * e.ld + col0;
+        });
+      } else {
+        const uint32_t r0 = r - (threadIdx.x & 31);
+        uint16_t* to = e.out + static_cast<uint64_t>(r0) * e.ld + col0;
+        store_block<8>(s.turn, w, min(32u, e.cols - col0), e.align, [&](uint32_t i) -> uint16_t* {
+          return r0 + i < e.rows ? to + i * e.ld : nullptr;
+        });
+      }
     }
   }
 };
 
 // dh from its sums: parts added in order, rounded, rows scattered. A CTA takes
-// a block of 128 rows x 32 columns.
-__global__ void __launch_bounds__(128)
+// 32 rows x 32 columns, a thread four columns of a row.
+__global__ void __launch_bounds__(256)
     vocab_dh_kernel(const float* __restrict__ sums, uint64_t part_floats, uint32_t parts,
                     uint32_t chunks, const uint32_t* __restrict__ row_map,
                     const uint32_t* __restrict__ count, uint16_t* __restrict__ dh, uint64_t ld,
-                    uint32_t cols, uint32_t align) {
-  __shared__ TurnSmem turn[4];
+                    uint32_t cols, uint32_t wide) {
   griddep_wait();
-  const uint32_t tile = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
-  const uint32_t r = tile * kTileM + threadIdx.x;
-  if (tile * kTileM >= *count) return;
-  const bool real = r < *count;
-  const uint32_t dst = real ? row_map[r] : 0xffffffffu;
-  float v[32];
-#pragma unroll
-  for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-  if (real) {
-#pragma unroll 2
-    for (uint32_t s = 0; s < parts; ++s) {
-      const float4* x = sum_block(const_cast<float*>(sums) + s * part_floats, tile, chunks, chunk,
-                                  threadIdx.x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float4 y = __ldcg(x + j * kTileM);
-        v[4 * j] = __fadd_rn(v[4 * j], y.x);
-        v[4 * j + 1] = __fadd_rn(v[4 * j + 1], y.y);
-        v[4 * j + 2] = __fadd_rn(v[4 * j + 2], y.z);
-        v[4 * j + 3] = __fadd_rn(v[4 * j + 3], y.w);
-      }
-    }
+  const uint32_t chunk = blockIdx.x % chunks, unit = threadIdx.x & 7u;
+  const uint32_t r = blockIdx.x / chunks * 32 + (threadIdx.x >> 3), c = chunk * 32 + unit * 4;
+  if (r >= *count || c >= cols) return;
+  const float4* x = sum_block(const_cast<float*>(sums), r / kTileM, chunks, chunk, r % kTileM) +
+                    unit * kTileM;
+  uint16_t* to = dh + static_cast<uint64_t>(row_map[r]) * ld + c;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (uint32_t s = 0; s < parts; ++s) {
+    const float4 y = __ldcg(x + s * (part_floats / 4));
+    v = make_float4(__fadd_rn(v.x, y.x), __fadd_rn(v.y, y.y), __fadd_rn(v.z, y.z),
+                    __fadd_rn(v.w, y.w));
   }
-  uint32_t w[16];
-#pragma unroll
-  for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-  store_block(turn[threadIdx.x >> 5], w, cols - chunk * 32, align, [&](uint32_t i) -> uint16_t* {
-    const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
-    return to == 0xffffffffu ? nullptr : dh + static_cast<uint64_t>(to) * ld + chunk * 32;
-  });
+  const uint2 w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  if (wide && c + 4 <= cols) {
+    *reinterpret_cast<uint2*>(to) = w;
+    return;
+  }
+  to[0] = static_cast<uint16_t>(w.x);
+  if (c + 1 < cols) to[1] = static_cast<uint16_t>(w.x >> 16);
+  if (c + 2 < cols) to[2] = static_cast<uint16_t>(w.y);
+  if (c + 3 < cols) to[3] = static_cast<uint16_t>(w.y >> 16);
 }
 
 constexpr uint32_t round_up(uint32_t x, uint32_t to) { return (x + to - 1) / to * to; }
@@ -453,13 +452,12 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
   l.h = take(2ull * l.rows * l.ld_h);
   if (!tma_rows(c.w, c.ldw)) l.w = take(2ull * c.v * l.ld_w);
   l.piece = gradient ? piece_words(l.rows, c.v) : c.v;
-  plan_product(l.logits, {n, l.piece, c.d, 1, false, pair, sms, 1, 1});
+  plan_product(l.logits, {n, l.piece, c.d, 1, false, pair, sms, 1, 1, 12.0, true});
   if (gradient) {
     l.ld_g = round_up(l.piece, kTileNMax);  // epilogues write whole tiles
     l.g = take(2ull * l.rows * l.ld_g);
-    plan_product(l.dh, {n, c.d, l.piece, 1, false, pair, sms, 32, 1});
-    plan_product(l.dw, {l.piece, dn, n, 1, false, pair, sms, 1, 1});
-    l.dh.join = 0;
+    plan_product(l.dh, {n, c.d, l.piece, 1, false, pair, sms, 32, 1, 12.0, false});
+    plan_product(l.dw, {l.piece, dn, n, 1, false, pair, sms, 1, 1, 12.0, true});
     if (l.dh.splits > 1 || l.piece < c.v) {
       l.sum_parts = l.dh.splits;
       l.sum_chunks = round_up(c.d, 32) / 32;
@@ -670,13 +668,13 @@ cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const Devi
   if (!l.sum_parts || c.n == 0) return cudaSuccess;
   const float* sums = reinterpret_cast<const float*>(base + l.sums);
   uint64_t part_floats = l.part_floats, ld = c.lddh;
-  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, align = row_align(c.dh, c.lddh);
+  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, wide = row_align(c.dh, c.lddh) == 16 ? 1u : 0u;
   const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
   const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
   uint16_t* dh = c.dh;
-  void* params[] = {&sums, &part_floats, &parts, &chunks, &row_map, &count, &dh, &ld, &cols, &align};
+  void* params[] = {&sums, &part_floats, &parts, &chunks, &row_map, &count, &dh, &ld, &cols, &wide};
   return launch_kernel(reinterpret_cast<const void*>(&vocab_dh_kernel),
-                       (c.n + kTileM - 1) / kTileM * chunks, 128, ws.stream, params);
+                       (c.n + 31) / 32 * chunks, 256, ws.stream, params);
 }
 
 }  // namespace efs
