@@ -305,6 +305,11 @@ struct StepEpilogue {
   struct Smem {
     TurnSmem turn;
   };
+  struct Row {};
+  static __device__ __forceinline__ Row prepare(const ProductShape&, const Params&,
+                                                const ProductItem&, uint32_t) {
+    return {};
+  }
 
   // A 32 x 32 block of a symmetric matrix on or below the diagonal, and its
   // mirror image.
@@ -329,7 +334,7 @@ struct StepEpilogue {
 
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
                                               const ProductItem& it, uint32_t row, uint32_t,
-                                              Smem& s, const ProductAcc& acc, uint32_t phase) {
+                                              Smem& s, const ProductAcc& acc, uint32_t phase, Row) {
     const uint32_t r = it.m0 + row, r0 = it.m0 + (row & ~31u);
     const uint32_t planes = e.exact ? 2 : 1;
     const uint16_t* from = e.from + it.batch * planes * e.plane + static_cast<uint64_t>(r) * e.ld;

@@ -71,18 +71,17 @@ struct ProductShape {
   uint32_t item0;             // this problem's first work item of its phase
   uint32_t part0;             // its first scratch tile (splits > 1)
   uint32_t join;              // parts are joined here (else the epilogue gets each)
-  const uint32_t* count;      // device: rows that exist (nullptr: all)
-  uint32_t count_is_k;        // the count bounds K (else M)
+  uint32_t counts;            // the launch's count bounds M (1) or K (2), or nothing (0)
 };
 
 struct ProductItem {
-  uint32_t batch, tn, m0, n0, n_eff, k, k0, kt, kts, part, split;
+  uint32_t batch, tn, m0, n0, n_eff, rows, k, k0, kt, kts, part, split;
   bool skip;
 };
 
 template <bool kPair>
 __device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint32_t item,
-                                                    uint32_t rank) {
+                                                    uint32_t rank, uint32_t count) {
   constexpr uint32_t kRows = kPair ? 2 * kTileM : kTileM;
   ProductItem it;
   uint32_t r = item - p.item0;
@@ -107,13 +106,9 @@ __device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint3
   it.m0 = tm * kRows;
   it.n0 = it.tn * p.bn;
   it.n_eff = min(p.bn, (p.n - min(p.n, it.n0) + 31u) & ~31u);
-  it.skip = false;
-  uint32_t k = p.k;
-  if (p.count) {
-    const uint32_t c = *p.count;
-    if (p.count_is_k) k = min(k, c);
-    else it.skip = it.m0 >= c;
-  }
+  const uint32_t k = p.counts == 2 ? min(p.k, count) : p.k;
+  it.skip = p.counts == 1 && it.m0 >= count;
+  it.rows = p.counts == 1 ? min(p.m, count) : p.m;
   it.m0 += rank * kTileM;
   it.k = k;
   it.kts = (k + kTileK - 1) / kTileK;
@@ -132,6 +127,7 @@ struct ProductArgs {
   typename Epi::Params epi[kMaxProblems];
   uint32_t phases;
   uint32_t first[kMaxPhases], problems[kMaxPhases], items[kMaxPhases];  // of each phase
+  const uint32_t* count;  // device: rows that exist (nullptr: all)
   float* parts;         // scratch tiles of split items
   uint32_t* arrivals;   // by the tile's first scratch tile; zero between tiles
   uint32_t part_chunks; // 32-column chunks per scratch tile
@@ -249,6 +245,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
   tc_fence_after();
   const uint32_t tmem = s.tmem;
   griddep_wait();
+  const uint32_t count = args.count ? *args.count : 0xffffffffu;
   bool ok = true;
   uint32_t stage = 0, phase = 0;    // ring position (producer, MMA)
   uint32_t acc = 0, acc_phase = 0;  // accumulator (MMA, epilogue)
@@ -263,7 +260,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (uint32_t item = unit; item < items && ok; item += units) {
           while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
           const ProductShape& p = args.shape[prob];
-          const ProductItem it = product_item<kPair>(p, item, rank);
+          const ProductItem it = product_item<kPair>(p, item, rank, count);
           if (it.skip) continue;
           const uint32_t half = kPair ? it.n_eff / 2 : it.n_eff;  // columns of B this CTA loads
           const uint32_t b_boxes = (half + 63) / 64, n0 = it.n0 + rank * half;
@@ -316,7 +313,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (uint32_t item = unit; item < items && ok; item += units) {
           while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
           const ProductShape& p = args.shape[prob];
-          const ProductItem it = product_item<kPair>(p, item, rank);
+          const ProductItem it = product_item<kPair>(p, item, rank, count);
           if (it.skip || it.kt == 0) continue;
           if (!mbar_wait(&s.acc_empty[acc], acc_phase ^ 1u, args.wait_ns)) {
             ok = false;
@@ -367,7 +364,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       for (uint32_t item = unit; item < items; item += units) {
         while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
         const ProductShape& p = args.shape[prob];
-        const ProductItem it = product_item<kPair>(p, item, rank);
+        const ProductItem it = product_item<kPair>(p, item, rank, count);
         if (it.skip) continue;
         const uint32_t chunks = it.n_eff / 32, mid = (chunks + 1) / 2;
         ProductAcc from;
@@ -378,6 +375,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         from.splits = p.splits;
         from.tmem = tmem + acc * kTileNMax + ((quarter * 32) << 16);
         from.release = kPair ? cluster_addr(&s.acc_empty[acc], 0) : smem_u32(&s.acc_empty[acc]);
+        const typename Epi::Row state = Epi::prepare(p, args.epi[prob], it, row);
         if (!from.none && ok) {
           ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[acc], acc_phase, args.wait_ns));
           tc_fence_after();
@@ -434,7 +432,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             tile_row = (block & 3u) * 32 + lane;
             at.parts = from.parts + tile_row * 4;
           }
-          Epi::tile(p, args.epi[prob], it, tile_row, half, epi_smem[warp - 2], at, ph);
+          Epi::tile(p, args.epi[prob], it, tile_row, half, epi_smem[warp - 2], at, ph, state);
         }
       }
     }

@@ -27,14 +27,16 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Rows that carry a loss, in their order: row_map[i], targets[i] (int32), and
-// their number. One CTA: the targets are 8 bytes a row, against 2 v d
+// Rows that carry a loss, in their order: row_map[i], targets[i] (int32), for the
+// gradient soft[i] = (-lse / ln 2, scale), and their number. One CTA: the targets are 8 bytes a row, against 2 v d
 // operations. A target >= v is malformed input: latched, the row skipped.
 constexpr int kRowsThreads = 1024;
 __global__ void __launch_bounds__(kRowsThreads, 1)
     vocab_rows_kernel(const int64_t* __restrict__ target, uint32_t n, uint32_t v,
                       uint32_t* __restrict__ row_map, int32_t* __restrict__ targets,
-                      uint32_t* __restrict__ count, float* loss, float* lse, uint32_t* error) {
+                      uint32_t* __restrict__ count, float* loss, float* lse,
+                      const float* __restrict__ row_scale, float2* __restrict__ soft,
+                      uint32_t* error) {
   __shared__ uint32_t s_warp[32];
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t base = 0;
@@ -58,6 +60,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     if (keep) {
       row_map[before] = i;
       targets[before] = static_cast<int32_t>(t);
+      if (soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
+        const float x = lse[i];
+        soft[before] = x == -INFINITY ? make_float2(0.0f, 0.0f)
+                                      : make_float2(__fmul_rn(x, -kLog2e), row_scale[i]);
+      }
     } else if (i < n && loss) {
       loss[i] = 0.0f;
       lse[i] = 0.0f;
@@ -137,20 +144,26 @@ struct LossEpilogue {
   struct Params {
     const uint16_t* bias;
     const int32_t* targets;
-    const uint32_t* count;
     float2* pairs;     // [row][half tile]
     float* at_target;  // [row]
   };
   struct Smem {
     alignas(16) float bias[32];
   };
+  struct Row {
+    int32_t target;
+  };
+  static __device__ __forceinline__ Row prepare(const ProductShape&, const Params& e,
+                                                const ProductItem& it, uint32_t row) {
+    return {it.m0 + row < it.rows ? __ldg(e.targets + it.m0 + row) : -1};
+  }
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
                                               const ProductItem& it, uint32_t row,
                                               uint32_t half, Smem& s, const ProductAcc& acc,
-                                              uint32_t) {
+                                              uint32_t, Row state) {
     const uint32_t r = it.m0 + row;
-    const bool real = r < *e.count;
-    const int32_t target = real ? e.targets[r] : -1;
+    const bool real = r < it.rows;
+    const int32_t target = state.target;
     float m = -INFINITY, sum = 0.0f;
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
@@ -232,10 +245,7 @@ struct GradEpilogue {
   struct Params {
     const uint16_t* bias;      // of the piece
     const int32_t* targets;
-    const uint32_t* row_map;
-    const uint32_t* count;
-    const float* lse;          // by original row
-    const float* row_scale;    // by original row
+    const float2* soft;
     uint16_t* g;               // [row][ld_g]
     uint32_t ld_g;
     uint32_t v0;               // the piece's first word
@@ -244,23 +254,22 @@ struct GradEpilogue {
     alignas(16) float bias[32];
     TurnSmem turn;
   };
-  static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
-                                              const ProductItem& it, uint32_t row,
-                                              uint32_t half, Smem& s, const ProductAcc& acc,
-                                              uint32_t) {
+  struct Row {
+    float2 soft;
+    uint32_t target;  // within the piece
+  };
+  static __device__ __forceinline__ Row prepare(const ProductShape&, const Params& e,
+                                                const ProductItem& it, uint32_t row) {
     const uint32_t r = it.m0 + row;
-    const bool real = r < *e.count;
-    float scale = 0.0f, shift = 0.0f;
-    uint32_t target = 0xffffffffu;
-    bool dead = true;
-    if (real) {
-      const uint32_t src = e.row_map[r];
-      const float lse = e.lse[src];
-      scale = e.row_scale[src];
-      shift = __fmul_rn(lse, -kLog2e);
-      target = static_cast<uint32_t>(e.targets[r]) - e.v0;
-      dead = lse == -INFINITY;  // no word has a probability
-    }
+    if (r >= it.rows) return {make_float2(0.0f, 0.0f), 0xffffffffu};
+    return {__ldg(e.soft + r), static_cast<uint32_t>(__ldg(e.targets + r)) - e.v0};
+  }
+  static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
+                                              const ProductItem& it, uint32_t row, uint32_t,
+                                              Smem& s, const ProductAcc& acc, uint32_t, Row state) {
+    const uint32_t r = it.m0 + row, target = state.target;
+    const float shift = state.soft.x, scale = state.soft.y;
+    const bool dead = scale == 0.0f;  // past the rows, or without a gradient
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
@@ -305,8 +314,7 @@ struct StoreEpilogue {
     uint16_t* out;
     uint64_t ld;
     const uint32_t* row_map;  // or nullptr
-    const uint32_t* count;    // rows that exist (with row_map)
-    uint32_t rows, cols;
+    uint32_t cols;
     uint32_t align;           // of out's rows, in bytes
     uint16_t* extra;          // column `cols`, by row (or nullptr)
     float* sums;              // != nullptr: sums instead of out
@@ -317,12 +325,19 @@ struct StoreEpilogue {
   struct Smem {
     TurnSmem turn;
   };
+  struct Row {
+    uint32_t dst;
+  };
+  static __device__ __forceinline__ Row prepare(const ProductShape&, const Params& e,
+                                                const ProductItem& it, uint32_t row) {
+    const uint32_t r = it.m0 + row;
+    return {r >= it.rows ? 0xffffffffu : e.row_map ? __ldg(e.row_map + r) : r};
+  }
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
                                               const ProductItem& it, uint32_t row, uint32_t,
-                                              Smem& s, const ProductAcc& acc, uint32_t) {
-    const uint32_t r = it.m0 + row;
-    const bool real = r < (e.row_map ? *e.count : e.rows);
-    const uint32_t dst = real ? (e.row_map ? e.row_map[r] : r) : 0xffffffffu;
+                                              Smem& s, const ProductAcc& acc, uint32_t, Row state) {
+    const uint32_t r = it.m0 + row, dst = state.dst;
+    const bool real = r < it.rows;
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
@@ -361,7 +376,7 @@ struct StoreEpilogue {
         const uint32_t r0 = r - (threadIdx.x & 31);
         uint16_t* to = e.out + static_cast<uint64_t>(r0) * e.ld + col0;
         store_block<8>(s.turn, w, min(32u, e.cols - col0), e.align, [&](uint32_t i) -> uint16_t* {
-          return r0 + i < e.rows ? to + i * e.ld : nullptr;
+          return r0 + i < it.rows ? to + i * e.ld : nullptr;
         });
       }
     }
@@ -426,7 +441,7 @@ struct VocabPlan {
   uint32_t sum_chunks, sum_parts;  // of dh's sums (0: dh is stored directly)
   uint64_t part_floats;
   // scratch offsets
-  size_t row_map, targets, count, h, w, pairs, at_target, g, sums, total;
+  size_t row_map, targets, soft, count, h, w, pairs, at_target, g, sums, total;
 };
 
 // The products' plans and the scratch. dh has few tiles and the whole piece as
@@ -449,6 +464,7 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
   l.row_map = take(4ull * l.rows);
   l.targets = take(4ull * l.rows);
   l.count = take(4);
+  if (gradient) l.soft = take(8ull * l.rows);
   l.h = take(2ull * l.rows * l.ld_h);
   if (!tma_rows(c.w, c.ldw)) l.w = take(2ull * c.v * l.ld_w);
   l.piece = gradient ? piece_words(l.rows, c.v) : c.v;
@@ -497,7 +513,10 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
   float* loss = gradient ? nullptr : c.loss;
   float* lse = c.lse;
   {
-    void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &error};
+    const float* row_scale = c.row_scale;
+    float2* soft = gradient ? reinterpret_cast<float2*>(base + l.soft) : nullptr;
+    void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
+                      &error};
     const cudaError_t e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1,
                                         kRowsThreads, ws.stream, params);
     if (e != cudaSuccess) return e;
@@ -538,13 +557,14 @@ cudaError_t loss_product(const VocabCall& c, const VocabPlan& l, const Gathered&
   ProductShape& p = args.shape[0];
   p = l.logits;
   p.bf16 = 1;
-  p.count = reinterpret_cast<const uint32_t*>(base + l.count);
+  p.counts = 1;
+  args.count = reinterpret_cast<const uint32_t*>(base + l.count);
   p.group_m = rows_in_l2(p, kPair);
   if (!make_map(&p.a, base + l.h, true, c.d, l.rows, l.ld_h, 1,
                 static_cast<uint64_t>(l.rows) * l.ld_h, kTileM) ||
       !make_map(&p.b, from.w, true, c.d, c.v, from.ld_w, 1, from.ld_w * c.v, b_box(p, kPair)))
     return cudaErrorInvalidValue;
-  args.epi[0] = {c.bias, reinterpret_cast<const int32_t*>(base + l.targets), p.count,
+  args.epi[0] = {c.bias, reinterpret_cast<const int32_t*>(base + l.targets),
                  reinterpret_cast<float2*>(base + l.pairs),
                  reinterpret_cast<float*>(base + l.at_target)};
   args.phases = args.problems[0] = 1;
@@ -574,14 +594,15 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
     p.tiles_n = (words + p.bn - 1) / p.bn;
     p.tiles = p.tiles_m * p.tiles_n;
     p.bf16 = 1;
-    p.count = count;
+    p.counts = 1;
+    args.count = count;
     p.group_m = rows_in_l2(p, kPair);
     if (!make_map(&p.a, h, true, c.d, l.rows, l.ld_h, 1, h_all, kTileM) ||
         !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, b_box(p, kPair)))
       return cudaErrorInvalidValue;
     args.epi[0] = {c.bias ? c.bias + v0 : nullptr,
                    reinterpret_cast<const int32_t*>(base + l.targets),
-                   row_map, count, c.lse, c.row_scale, g, l.ld_g, v0};
+                   reinterpret_cast<const float2*>(base + l.soft), g, l.ld_g, v0};
     args.phases = args.problems[0] = 1;
     number_items(args, kPair);
     const cudaError_t e = launch_product<GradEpilogue, 1, kPair>(args, ws, dev);
@@ -594,11 +615,11 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
     p.k = words;
     p.group_m = 1;
     p.b_mn = p.bf16 = 1;
-    p.count = count;
+    p.counts = 1;
     if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileM) ||
         !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, kTileK))
       return cudaErrorInvalidValue;
-    args.epi[0] = {c.dh, c.lddh, row_map, count, c.n, c.d, row_align(c.dh, c.lddh), nullptr,
+    args.epi[0] = {c.dh, c.lddh, row_map, c.d, row_align(c.dh, c.lddh), nullptr,
                    l.sum_parts ? reinterpret_cast<float*>(base + l.sums) : nullptr,
                    l.part_floats, l.sum_chunks, v0 == 0 ? 1u : 0u};
   }
@@ -610,15 +631,15 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
     p.tiles = p.tiles_m * p.tiles_n;
     p.group_m = 1;
     p.a_mn = p.b_mn = p.bf16 = 1;
-    p.count = count;
-    p.count_is_k = 1;
+    p.counts = 2;
     if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileK) ||
         !make_map(&p.b, h, true, c.d + (c.dbias ? 1 : 0), l.rows, l.ld_h, 1, h_all, kTileK))
       return cudaErrorInvalidValue;
     uint16_t* out = c.dw + static_cast<uint64_t>(v0) * c.lddw;
-    args.epi[1] = {out, c.lddw, nullptr, nullptr, words, c.d, row_align(out, c.lddw),
+    args.epi[1] = {out, c.lddw, nullptr, c.d, row_align(out, c.lddw),
                    c.dbias ? c.dbias + v0 : nullptr, nullptr, 0, 0, 1};
   }
+  args.count = count;
   args.phases = 1;
   args.problems[0] = 2;
   number_items(args, kPair);
