@@ -83,12 +83,22 @@ template <bool kPair>
 __device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint32_t item,
                                                     uint32_t rank, uint32_t count) {
   constexpr uint32_t kRows = kPair ? 2 * kTileM : kTileM;
+  // (divisions only where there is something to divide: an item's warps all wait
+  // for this)
   ProductItem it;
   uint32_t r = item - p.item0;
-  it.split = r % p.splits;
-  r /= p.splits;
-  it.batch = r / p.tiles;
-  r -= it.batch * p.tiles;
+  it.split = 0;
+  it.batch = 0;
+  if (p.splits > 1) {
+    const uint32_t q = r / p.splits;
+    it.split = r - q * p.splits;
+    r = q;
+  }
+  if (p.batch > 1) {
+    it.batch = r / p.tiles;
+    r -= it.batch * p.tiles;
+  }
+  const uint32_t tile = r;
   uint32_t tm;
   if (p.lower) {  // tile row i holds i + 1 tiles
     uint32_t i = static_cast<uint32_t>(sqrtf(2.0f * static_cast<float>(r) + 0.25f) - 0.5f);
@@ -96,12 +106,19 @@ __device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint3
     while (i * (i + 1) / 2 > r) --i;
     tm = i;
     it.tn = r - i * (i + 1) / 2;
+  } else if (p.group_m == 1) {
+    tm = r / p.tiles_n;
+    it.tn = r - tm * p.tiles_n;
   } else {
     const uint32_t per = p.group_m * p.tiles_n;
-    const uint32_t g = r / per, in = r - g * per;
-    const uint32_t rows = min(p.group_m, p.tiles_m - g * p.group_m);
-    it.tn = in / rows;
-    tm = g * p.group_m + in % rows;
+    uint32_t g = 0, rows = p.tiles_m;
+    if (p.group_m < p.tiles_m) {
+      g = r / per;
+      r -= g * per;
+      rows = min(p.group_m, p.tiles_m - g * p.group_m);
+    }
+    it.tn = r / rows;
+    tm = g * p.group_m + (r - it.tn * rows);
   }
   it.m0 = tm * kRows;
   it.n0 = it.tn * p.bn;
@@ -112,10 +129,14 @@ __device__ __forceinline__ ProductItem product_item(const ProductShape& p, uint3
   it.m0 += rank * kTileM;
   it.k = k;
   it.kts = (k + kTileK - 1) / kTileK;
-  const uint64_t all = static_cast<uint64_t>(it.kts) * p.terms;
-  it.k0 = static_cast<uint32_t>(all * it.split / p.splits);
-  it.kt = static_cast<uint32_t>(all * (it.split + 1) / p.splits) - it.k0;
-  it.part = p.part0 + ((it.batch * p.tiles + r) * (kPair ? 2 : 1) + rank) * p.splits;
+  const uint32_t all = it.kts * p.terms;  // times splits: below 2^32 for any K of this library
+  it.k0 = 0;
+  it.kt = all;
+  if (p.splits > 1) {
+    it.k0 = all * it.split / p.splits;
+    it.kt = all * (it.split + 1) / p.splits - it.k0;
+  }
+  it.part = p.part0 + ((it.batch * p.tiles + tile) * (kPair ? 2 : 1) + rank) * p.splits;
   return it;
 }
 
@@ -444,6 +465,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       if (!ok) break;
     }
   }
+  griddep_launch_dependents();  // (they wait for this grid's end; their launch need not)
   if (!ok) atomicOr(args.error, kDevErrTimeout);
   if (args.phases > 1 && threadIdx.x == 0 &&
       atomicAdd(&args.barrier[1], 1u) == gridDim.x - 1) {  // all are past the last barrier

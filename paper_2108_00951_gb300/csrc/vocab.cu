@@ -76,6 +76,25 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   if (bad) atomicOr(error, kDevErrBadInput);
 }
 
+// 8 elements of a row of `cols` from c on, zeros past its end (with `one`, 1.0
+// in bf16 right after it).
+__device__ __forceinline__ uint4 pack_8(const uint16_t* row, uint32_t c, uint32_t cols, bool vec,
+                                        bool one) {
+  if (c + 8 <= cols) {
+    if (vec) return __ldg(reinterpret_cast<const uint4*>(row + c));
+    if (reinterpret_cast<uintptr_t>(row) % 4 == 0) {
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(row + c);
+      return make_uint4(__ldg(p), __ldg(p + 1), __ldg(p + 2), __ldg(p + 3));
+    }
+  }
+  uint32_t e[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    e[j] = c + j < cols ? __ldg(row + c + j) : (one && c + j == cols) ? 0x3f80u : 0u;
+  return make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16),
+                    e[6] | (e[7] << 16));
+}
+
 // Copies rows of 16-bit elements to rows that TMA can read: dst[i] =
 // src[row_map[i]] (or src[i]), zeros past `cols`, past *count and up to
 // `rows_out`; with `one` the element after the last is 1.0 (bf16). zero_rows
@@ -97,17 +116,7 @@ __global__ void __launch_bounds__(256)
     const uint16_t* from = src + (real ? (row_map ? row_map[i] : i) : 0) * ld;
     uint16_t* to = dst + i * ld_out;
     for (uint32_t c = lane * 8; c < ld_out; c += 256) {
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (real && vec && c + 8 <= cols) {
-        x = __ldg(reinterpret_cast<const uint4*>(from + c));
-      } else if (real) {
-        uint32_t e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          e[j] = c + j < cols ? __ldg(from + c + j) : (one && c + j == cols) ? 0x3f80u : 0u;
-        x = make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16),
-                       e[6] | (e[7] << 16));
-      }
+      const uint4 x = real ? pack_8(from, c, cols, vec, one) : make_uint4(0, 0, 0, 0);
       *reinterpret_cast<uint4*>(to + c) = x;
     }
     if (zero_rows && i < rows) {
@@ -116,6 +125,96 @@ __global__ void __launch_bounds__(256)
         for (uint32_t c = lane; c < cols; c += 32) zero_rows[i * zero_ld + c] = 0;
     }
   }
+}
+
+// Both of the above in one launch, for batches whose targets every CTA can
+// afford to count: a warp takes a row. Rows past the last gathered one are
+// zeroed.
+constexpr uint32_t kGatherRows = 4096;
+struct GatherArgs {
+  const int64_t* target;
+  const uint16_t* h;
+  uint64_t ld;
+  uint32_t n, v, d;
+  uint32_t* row_map;
+  int32_t* targets;
+  uint32_t* count;
+  uint16_t* to;
+  uint32_t ld_to, rows_to;
+  uint32_t one;  // the element after a row's last is 1.0
+  float *loss, *lse;        // the loss call: zero for skipped rows
+  const float* row_scale;   // the gradient's
+  float2* soft;
+  uint16_t* dh;             // likewise: zeroed rows
+  uint64_t ld_dh;
+  uint32_t* error;
+};
+__global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
+  __shared__ uint32_t s_before[8], s_total[8];
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t first = blockIdx.x * 8, i = first + warp;
+  griddep_wait();
+  auto keeps = [&](int64_t t) { return t >= 0 && t < static_cast<int64_t>(a.v); };
+  uint32_t before = 0, total = 0;
+  bool bad = false;
+#pragma unroll 4
+  for (uint32_t j = threadIdx.x; j < a.n; j += 256) {
+    const int64_t t = __ldg(a.target + j);
+    const uint32_t k = keeps(t) ? 1u : 0u;
+    bad |= t >= static_cast<int64_t>(a.v);
+    before += j < first ? k : 0u;
+    total += k;
+  }
+  before = warp_sum(before);
+  total = warp_sum(total);
+  if (lane == 0) {
+    s_before[warp] = before;
+    s_total[warp] = total;
+  }
+  __syncthreads();
+  before = total = 0;
+  for (int w = 0; w < 8; ++w) {
+    before += s_before[w];
+    total += s_total[w];
+  }
+  if (blockIdx.x == 0) {
+    if (threadIdx.x == 0) *a.count = total;
+    if (bad) atomicOr(a.error, kDevErrBadInput);
+  }
+  const bool vec = reinterpret_cast<uintptr_t>(a.h) % 16 == 0 && a.ld % 8 == 0;
+  if (i < a.n) {
+    const int64_t t = __ldg(a.target + i);
+    // of this CTA's rows, those before this warp's
+    const uint32_t mine = __ballot_sync(
+        0xffffffffu, lane < warp && keeps(__ldg(a.target + (lane < warp ? first + lane : i))));
+    if (keeps(t)) {
+      const uint32_t at = before + __popc(mine);
+      if (lane == 0) {
+        a.row_map[at] = i;
+        a.targets[at] = static_cast<int32_t>(t);
+        if (a.soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
+          const float x = a.lse[i];
+          a.soft[at] = x == -INFINITY ? make_float2(0.0f, 0.0f)
+                                      : make_float2(__fmul_rn(x, -kLog2e), a.row_scale[i]);
+        }
+      }
+      const uint16_t* from = a.h + i * a.ld;
+      for (uint32_t c = lane * 8; c < a.ld_to; c += 256)
+        *reinterpret_cast<uint4*>(a.to + static_cast<uint64_t>(at) * a.ld_to + c) =
+            pack_8(from, c, a.d, vec, a.one != 0);
+    } else {
+      if (lane == 0 && a.loss) {
+        a.loss[i] = 0.0f;
+        a.lse[i] = 0.0f;
+      }
+      if (a.dh)
+        for (uint32_t c = lane; c < a.d; c += 32) a.dh[i * a.ld_dh + c] = 0;
+    }
+  }
+  for (uint32_t at = total + i; at < a.rows_to; at += gridDim.x * 8)
+    for (uint32_t c = lane * 8; c < a.ld_to; c += 256)
+      *reinterpret_cast<uint4*>(a.to + static_cast<uint64_t>(at) * a.ld_to + c) =
+          make_uint4(0, 0, 0, 0);
 }
 
 // 32 logits of a row: accumulators plus the bias of their columns (through
@@ -512,15 +611,10 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
   const int64_t* target = c.target;
   float* loss = gradient ? nullptr : c.loss;
   float* lse = c.lse;
-  {
-    const float* row_scale = c.row_scale;
-    float2* soft = gradient ? reinterpret_cast<float2*>(base + l.soft) : nullptr;
-    void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
-                      &error};
-    const cudaError_t e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1,
-                                        kRowsThreads, ws.stream, params);
-    if (e != cudaSuccess) return e;
-  }
+  const float* row_scale = c.row_scale;
+  float2* soft = gradient ? reinterpret_cast<float2*>(base + l.soft) : nullptr;
+  uint16_t* h = reinterpret_cast<uint16_t*>(base + l.h);
+  const bool one = gradient && c.dbias;
   auto pack = [&](const uint16_t* src, uint64_t ld, uint32_t rows, const uint32_t* map,
                   const uint32_t* cnt, uint16_t* dst, uint32_t ld_out, uint32_t rows_out, bool one,
                   uint16_t* zero, uint64_t zero_ld) {
@@ -530,8 +624,23 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
     return launch_kernel(reinterpret_cast<const void*>(&vocab_pack_kernel), grid, 256, ws.stream,
                          params);
   };
-  cudaError_t e = pack(c.h, c.ldh, c.n, row_map, count, reinterpret_cast<uint16_t*>(base + l.h),
-                       l.ld_h, l.rows, gradient && c.dbias, gradient ? c.dh : nullptr, c.lddh);
+  cudaError_t e;
+  if (n <= kGatherRows) {
+    GatherArgs a = {target, c.h,  c.ldh,      n,       v,    d,         row_map, targets,
+                    count,  h,    l.ld_h,     l.rows,  one ? 1u : 0u,   loss,    lse,
+                    row_scale,    soft,       gradient ? c.dh : nullptr, c.lddh, error};
+    void* params[] = {&a};
+    e = launch_kernel(reinterpret_cast<const void*>(&vocab_gather_kernel), n ? (n + 7) / 8 : 1, 256,
+                      ws.stream, params);
+  } else {
+    void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
+                      &error};
+    e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1, kRowsThreads, ws.stream,
+                      params);
+    if (e == cudaSuccess)
+      e = pack(c.h, c.ldh, n, row_map, count, h, l.ld_h, l.rows, one, gradient ? c.dh : nullptr,
+               c.lddh);
+  }
   if (e != cudaSuccess) return e;
   out->w = c.w;
   out->ld_w = c.ldw;
