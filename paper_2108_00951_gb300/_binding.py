@@ -8,6 +8,7 @@ there is no fallback: if the library cannot be loaded, every call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import threading
@@ -415,6 +416,22 @@ def ef_vocab_loss_grad(h, w, target, lse, row_scale, dh_out, dw_out, bias=None, 
         _stream(stream)), "ef_vocab_loss_grad")
 
 
+def _matrices(tensors, name, dtype, shapes):
+    """Device pointers and row strides of matrices, checked as by _rows."""
+    pointers, strides = array.array("Q"), array.array("Q")
+    for t, shape in zip(tensors, shapes):
+        if isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.shape == shape:
+            ld, step = t.stride()
+            if step == 1 and ld >= shape[1] > 0:
+                pointers.append(t.data_ptr())
+                strides.append(ld)
+                continue
+        p, ld = _rows(t, name, dtype, *shape)  # unusual, or refused
+        pointers.append(p)
+        strides.append(ld)
+    return pointers, strides
+
+
 def ef_orthogonalize(updates, outs, momenta=None, momentum=0.0, stream=None):
     """Orthogonalised updates of a list of weight matrices (``ef_orthogonalize``):
     momentum (``momenta`` optional: float32 matrices, updated in place), then
@@ -425,6 +442,7 @@ def ef_orthogonalize(updates, outs, momenta=None, momentum=0.0, stream=None):
     n = len(updates)
     if len(outs) != n or (momenta is not None and len(momenta) != n):
         raise ValueError("updates, outs and momenta differ in length")
+    momentum = _real(momentum)
     if n == 0:
         return
     if not all(isinstance(t, _Tensor) and t.dim() == 2 for t in updates):
@@ -433,20 +451,19 @@ def ef_orthogonalize(updates, outs, momenta=None, momentum=0.0, stream=None):
     if dtype is not torch.float32 and dtype is not torch.bfloat16:
         raise TypeError("updates must be float32 or bfloat16")
     shapes = [t.shape for t in updates]
-    u = [_rows(t, "updates", dtype, *s) for t, s in zip(updates, shapes)]
-    out = [_rows(t, "outs", torch.bfloat16, *s) for t, s in zip(outs, shapes)]
-    m = None
+    rows = array.array("Q", [s[0] for s in shapes])
+    cols = array.array("Q", [s[1] for s in shapes])
+    u, ld_u = _matrices(updates, "updates", dtype, shapes)
+    out, ld_out = _matrices(outs, "outs", torch.bfloat16, shapes)
+    m = ld_m = None
     if momenta is not None:
-        m = [_rows(t, "momenta", torch.float32, *s) for t, s in zip(momenta, shapes)]
-    words = ctypes.c_uint64 * n
+        m, ld_m = _matrices(momenta, "momenta", torch.float32, shapes)
 
-    def column(rows, i):
-        return words(*[r[i] for r in rows])
-    _check(lib.ef_orthogonalize(
-        n, column(shapes, 0), column(shapes, 1), column(u, 0), column(u, 1),
-        int(dtype is torch.bfloat16), None if m is None else column(m, 0),
-        None if m is None else column(m, 1), _real(momentum), column(out, 0), column(out, 1),
-        _stream(stream)), "ef_orthogonalize")
+    def at(words):
+        return None if words is None else words.buffer_info()[0]
+    _check(lib.ef_orthogonalize(n, at(rows), at(cols), at(u), at(ld_u),
+                                int(dtype is torch.bfloat16), at(m), at(ld_m), momentum, at(out),
+                                at(ld_out), _stream(stream)), "ef_orthogonalize")
 
 
 def ef_check_status(stream=None) -> int:

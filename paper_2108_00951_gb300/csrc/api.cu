@@ -433,9 +433,11 @@ ef_status orthogonalize_entry(uint32_t n, const uint64_t* rows, const uint64_t* 
   ef_status st = device_info(dev, &info);
   if (st != EF_OK) return st;
   Workspace* ws = nullptr;
-  st = acquire_model_scratch(stream, ortho_scratch(mats.data(), n, info), &ws);
+  std::shared_ptr<void> plan;
+  st = acquire_model_scratch(stream, ortho_plan(mats.data(), n, info, &plan), &ws);
   if (st != EF_OK) return st;
-  return finish_launch(launch_orthogonalize(mats.data(), n, bf16, momentum, *ws, info), ws);
+  return finish_launch(
+      launch_orthogonalize(mats.data(), n, bf16, momentum, plan.get(), *ws, info), ws);
 }
 
 }  // namespace

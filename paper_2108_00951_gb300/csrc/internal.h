@@ -4,6 +4,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <memory>
 #include <vector>
 #include <cuda_runtime.h>
 
@@ -285,9 +286,11 @@ struct OrthoMat {
 bool ortho_small(const OrthoMat* mats, uint32_t n);
 cudaError_t launch_ortho_small(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
                                Workspace& ws);
-size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev);
+// Returns the scratch a call needs and, for other matrices, its plan.
+size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
+                  std::shared_ptr<void>* plan);
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
-                                 Workspace& ws, const DeviceInfo& dev);
+                                 const void* plan, Workspace& ws, const DeviceInfo& dev);
 
 // Launch bookkeeping.
 // A launch that may begin while the previous kernel on the stream finishes

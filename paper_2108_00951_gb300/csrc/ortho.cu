@@ -488,6 +488,7 @@ struct Group {
   size_t half[2] = {0, 0}, rest = 0, a = 0, b = 0;  // scratch offsets
   uint64_t rest_units = 0;              // of one matrix, 16 bytes each
   uint32_t first = 0;                   // its first matrix, in the groups' order
+  ProductShape shape[3] = {};           // by form
   bool left() const { return rows <= cols; }
 };
 
@@ -497,33 +498,43 @@ struct Plan {
   bool pair = false;
 };
 
-// The shapes of a launch's products for `count` groups from `g0`; returns the
-// bytes of the scratch that joining K parts takes.
-template <class Args>
-size_t shape_products(Args& args, const Plan& plan, size_t g0, uint32_t count, double sms) {
+// The products' shapes of groups [g0, g0 + count), which share a launch: each
+// is planned for its share of the SMs.
+void plan_groups(Plan& plan, size_t g0, size_t count, double sms) {
   double work[3] = {0.0, 0.0, 0.0};
   auto cost = [](const Group& g, int form) {
     const double s = g.side, x = static_cast<double>(g.rows) * g.cols;
     return g.mats.size() * (g.planes * 2 - 1) *
            (form == kFormA ? x * s * 0.5 : form == kFormB ? s * s * s * 0.5 : x * s);
   };
-  for (uint32_t i = 0; i < count; ++i)
-    for (int f = 0; f < 3; ++f) work[f] += cost(plan.groups[g0 + i], f);
-  for (uint32_t i = 0; i < count; ++i) {
-    const Group& g = plan.groups[g0 + i];
+  for (size_t i = g0; i < g0 + count; ++i)
+    for (int f = 0; f < 3; ++f) work[f] += cost(plan.groups[i], f);
+  for (size_t i = g0; i < g0 + count; ++i) {
+    Group& g = plan.groups[i];
     const uint32_t batch = static_cast<uint32_t>(g.mats.size()), terms = g.planes * 2 - 1;
     const uint32_t deep = g.left() ? g.cols : g.rows;
+    const ProductWant want[3] = {
+        {g.side, g.side, deep, batch, true, plan.pair, 0.0, 16, terms, 20.0, true},
+        {g.side, g.side, g.side, batch, true, plan.pair, 0.0, 8, terms, 20.0, true},
+        {g.rows, g.cols, g.side, batch, false, plan.pair, 0.0, 1, terms, 40.0, true}};
     for (int f = 0; f < 3; ++f) {
-      ProductShape s = {};
-      double mine = cost(g, f) / work[f] * sms;
-      if (mine < 1.0) mine = 1.0;
-      if (f == kFormA) plan_product(s, {g.side, g.side, deep, batch, true, plan.pair, mine, 16, terms, 20.0, true});
-      if (f == kFormB) plan_product(s, {g.side, g.side, g.side, batch, true, plan.pair, mine, 8, terms, 20.0, true});
-      if (f == kFormX) plan_product(s, {g.rows, g.cols, g.side, batch, false, plan.pair, mine, 1, terms, 40.0, true});
-      if (f == kFormA) args.shape[kEntryA * count + i] = args.shape[(kEntryA + 1) * count + i] = s;
-      if (f == kFormB) args.shape[kEntryB * count + i] = s;
-      if (f == kFormX) args.shape[kEntryX * count + i] = args.shape[(kEntryX + 1) * count + i] = s;
+      ProductWant w = want[f];
+      w.sms = cost(g, f) / work[f] * sms;
+      if (w.sms < 1.0) w.sms = 1.0;
+      plan_product(g.shape[f], w);
     }
+  }
+}
+
+// Lays them out as a launch's entries and phases; returns the bytes of the
+// scratch that joining K parts takes.
+template <class Args>
+size_t shape_products(Args& args, const Plan& plan, size_t g0, uint32_t count) {
+  for (uint32_t i = 0; i < count; ++i) {
+    const ProductShape* s = plan.groups[g0 + i].shape;
+    args.shape[kEntryA * count + i] = args.shape[(kEntryA + 1) * count + i] = s[kFormA];
+    args.shape[kEntryB * count + i] = s[kFormB];
+    args.shape[kEntryX * count + i] = args.shape[(kEntryX + 1) * count + i] = s[kFormX];
   }
   args.phases = 3 * kSteps;
   for (uint32_t ph = 0; ph < args.phases; ++ph) {
@@ -598,9 +609,11 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
   size_t join = 0;
   for (size_t g0 = 0; g0 < p.groups.size(); g0 += kOrthoGroups) {
     const size_t left = p.groups.size() - g0;
-    std::unique_ptr<StepArgs<kOrthoGroups>> args(new StepArgs<kOrthoGroups>());
-    const size_t bytes =
-        shape_products(*args, p, g0, static_cast<uint32_t>(left < kOrthoGroups ? left : kOrthoGroups), sms);
+    const uint32_t count = static_cast<uint32_t>(left < kOrthoGroups ? left : kOrthoGroups);
+    plan_groups(p, g0, count, sms);
+    std::unique_ptr<StepArgs<kOrthoGroups>> args(new StepArgs<kOrthoGroups>);
+    args->phases = args->entries = 0;
+    const size_t bytes = shape_products(*args, p, g0, count);
     if (bytes > join) join = bytes;
   }
   p.join = take(join);
@@ -677,14 +690,26 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
                   const DeviceInfo& dev) {
   std::unique_ptr<StepArgs<kGroups>> held(new StepArgs<kGroups>());
   StepArgs<kGroups>& args = *held;
-  shape_products(args, plan, g0, count, dev.sm_count);
+  shape_products(args, plan, g0, count);
   const bool pair = plan.pair;
   bool ok = true;
   for (uint32_t i = 0; i < count; ++i) {
     const Group& g = plan.groups[g0 + i];
     const bool left = g.left();
     const uint64_t batch = g.mats.size() * g.planes;
+    struct {
+      size_t at;
+      uint32_t box;
+      const CUtensorMap* map;
+    } known[8];
+    int maps = 0;
     auto map = [&](CUtensorMap* to, size_t at, bool square, uint32_t box) {
+      for (int k = 0; k < maps; ++k)
+        if (known[k].at == at && known[k].box == box) {  // encoding one costs more than a copy
+          *to = *known[k].map;
+          return;
+        }
+      if (maps < 8) known[maps++] = {at, box, to};
       const uint32_t rows = square ? g.side : g.rows, cols = square ? g.side : g.cols;
       const uint32_t ld = square ? g.ld_s : g.ld_x;
       ok = ok && make_map(to, base + at, false, cols, rows, ld, batch,
@@ -745,15 +770,18 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
 
 }  // namespace
 
-size_t ortho_scratch(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
-  if (ortho_small(mats, n)) return 0;
-  return make_plan(mats, n, dev).total;
+size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
+                  std::shared_ptr<void>* plan) {
+  if (ortho_small(mats, n)) return 0;  // no plan, no scratch
+  auto p = std::make_shared<Plan>(make_plan(mats, n, dev));
+  *plan = p;
+  return p->total;
 }
 
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
-                                 Workspace& ws, const DeviceInfo& dev) {
-  if (ortho_small(mats, n)) return launch_ortho_small(mats, n, bf16, mu, ws);
-  const Plan plan = make_plan(mats, n, dev);
+                                 const void* made, Workspace& ws, const DeviceInfo& dev) {
+  if (!made) return launch_ortho_small(mats, n, bf16, mu, ws);
+  const Plan& plan = *static_cast<const Plan*>(made);
   char* base = ws.model_scratch();
   cudaError_t e = prepare(mats, plan, bf16, mu, base, ws);
   for (size_t g0 = 0; g0 < plan.groups.size() && e == cudaSuccess; g0 += kOrthoGroups) {

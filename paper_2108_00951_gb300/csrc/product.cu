@@ -67,7 +67,8 @@ void plan_product(ProductShape& p, const ProductWant& w) {
                                   : p.tiles_m * static_cast<double>((w.n + bn - 1) / bn)) * w.batch;
     const double mma = 4.0 * bn, load = 4.0 * (kTileM + (w.pair ? bn / 2 : bn));
     const double step = mma > load ? mma : load;
-    for (uint32_t s = 1; s <= w.max_splits && s <= (kts ? kts : 1); ++s) {
+    for (uint32_t s : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
+      if (s > 1 && (s > w.max_splits || s > kts)) break;
       if (s > 1 && tiles > 2 * units) break;  // nothing to gain
       const double waves = ceil(tiles * s / units);
       const double deep = static_cast<double>((kts + s - 1) / s);
