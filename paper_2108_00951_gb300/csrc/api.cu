@@ -47,6 +47,7 @@ ef_status device_info(int dev, DeviceInfo* out) {
     topk_init_device(info);
     topk_layerwise_init_device(info);
     aggregate_init_device(info);
+    ortho_small_init_device(info);
     if (info.refine_blocks <= 0 || info.finalize_blocks <= 0) return EF_ERR_CUDA;
     it = g_devices.emplace(dev, info).first;
   }

@@ -225,6 +225,7 @@ struct DeviceInfo {
   int lw_group_per_sm_bf16 = 0;
   int lw_select_per_sm = 0;       // co-resident layer-wise select CTAs per SM
   int agg_stream_slots = 0;       // resident CTAs of the persistent dense sum
+  uint32_t ortho_cluster = 8;     // CTAs of a cluster of the on-chip orthogonalisation, at most
 };
 
 // Per-device set-up of the Top-k kernels (shared-memory opt-in, occupancy).
@@ -236,6 +237,9 @@ void topk_layerwise_init_device(DeviceInfo& info);
 // Per-device set-up of the aggregation kernels (prefer the largest shared
 // memory carve-out, so that 8 of their CTAs are resident per SM).
 void aggregate_init_device(DeviceInfo& info);
+
+// Per-device set-up of the on-chip orthogonalisation (cluster size).
+void ortho_small_init_device(DeviceInfo& info);
 
 // Per-device set-up of the streaming hard-threshold kernels (opts them into
 // their shared-memory ring on the current device and records occupancy).
@@ -283,9 +287,9 @@ struct OrthoMat {
   uint32_t rows, cols;
 };
 // Matrices that a cluster holds on chip (ortho_small.cu).
-bool ortho_small(const OrthoMat* mats, uint32_t n);
+bool ortho_small(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev);
 cudaError_t launch_ortho_small(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
-                               Workspace& ws);
+                               Workspace& ws, const DeviceInfo& dev);
 // Returns the scratch a call needs and, for other matrices, its plan.
 size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
                   std::shared_ptr<void>* plan);

@@ -772,7 +772,7 @@ cudaError_t steps(const Plan& plan, size_t g0, uint32_t count, char* base, Works
 
 size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
                   std::shared_ptr<void>* plan) {
-  if (ortho_small(mats, n)) return 0;  // no plan, no scratch
+  if (ortho_small(mats, n, dev)) return 0;  // no plan, no scratch
   auto p = std::make_shared<Plan>(make_plan(mats, n, dev));
   *plan = p;
   return p->total;
@@ -780,7 +780,7 @@ size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
 
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
                                  const void* made, Workspace& ws, const DeviceInfo& dev) {
-  if (!made) return launch_ortho_small(mats, n, bf16, mu, ws);
+  if (!made) return launch_ortho_small(mats, n, bf16, mu, ws, dev);
   const Plan& plan = *static_cast<const Plan*>(made);
   char* base = ws.model_scratch();
   cudaError_t e = prepare(mats, plan, bf16, mu, base, ws);

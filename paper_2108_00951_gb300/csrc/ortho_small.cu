@@ -32,7 +32,7 @@ constexpr float kScaleX = 16384.0f, kScaleA = 8192.0f;
 constexpr int kSteps = 5;
 constexpr uint32_t kSmallThreads = 256;
 constexpr uint32_t kSmallMats = 64;     // per launch
-constexpr uint32_t kMaxCluster = 8;
+constexpr uint32_t kMaxCluster = 16;  // beyond the portable 8 where a GPU takes it
 constexpr uint32_t kTileBytes = 128 * 128;  // 128 rows of 64 fp16
 constexpr uint32_t kSmallSmem = 200 * 1024;
 // At least this much is asked for, so that one CTA runs per SM: a second one's
@@ -458,10 +458,13 @@ struct SmallShape {
   bool fits;
 };
 // Shared memory for a shorter side of `side` with `blocks` blocks per CTA.
-SmallShape small_shape(uint32_t side, uint32_t len) {
+SmallShape small_shape(uint32_t side, uint32_t len, uint32_t most) {
   SmallShape s = {};
   const uint32_t all = (len + 63) / 64, side32 = (side + 31) & ~31u;
-  s.blocks = (all + kMaxCluster - 1) / kMaxCluster;
+  // up to 8 CTAs while they hold the matrix: a larger cluster exchanges more
+  const uint32_t blocks = side <= 64 ? 4 : side <= 96 ? 3 : 2;
+  if (most > 8 && all <= 8 * blocks) most = 8;
+  s.blocks = (all + most - 1) / most;
   s.ranks = (all + s.blocks - 1) / s.blocks;
   const uint32_t rows_per = (side32 + s.ranks - 1) / s.ranks;
   s.shares_off = s.blocks * 2 * kTileBytes;
@@ -474,21 +477,44 @@ SmallShape small_shape(uint32_t side, uint32_t len) {
 
 }  // namespace
 
+void ortho_small_init_device(DeviceInfo& info) {
+  info.ortho_cluster = 8;
+  const void* fns[] = {reinterpret_cast<const void*>(&ortho_small_kernel<true>),
+                       reinterpret_cast<const void*>(&ortho_small_kernel<false>)};
+  int fit = 0;
+  for (const void* fn : fns) {
+    cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmallSmem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kMaxCluster);
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = kSmallSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kMaxCluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&clusters, fn, &cfg) == cudaSuccess && clusters > 0)
+      ++fit;
+  }
+  cudaGetLastError();
+  if (fit == 2) info.ortho_cluster = kMaxCluster;
+}
+
 // Whether every matrix is one that a cluster holds.
-bool ortho_small(const OrthoMat* mats, uint32_t n) {
+bool ortho_small(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
   for (uint32_t i = 0; i < n; ++i) {
     const uint32_t r = mats[i].rows, c = mats[i].cols;
-    if (r && c && !small_shape(r < c ? r : c, r < c ? c : r).fits) return false;
+    if (r && c && !small_shape(r < c ? r : c, r < c ? c : r, dev.ortho_cluster).fits) return false;
   }
   return true;
 }
 
 cudaError_t launch_ortho_small(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
-                               Workspace& ws) {
+                               Workspace& ws, const DeviceInfo& dev) {
   auto fn = bf16 ? ortho_small_kernel<true> : ortho_small_kernel<false>;
-  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(kSmallSmem));
-  if (e != cudaSuccess) return e;
   // matrices of one layout go into one launch
   std::vector<bool> done(n, false);
   for (uint32_t i = 0; i < n; ++i) {
@@ -503,7 +529,7 @@ cudaError_t launch_ortho_small(const OrthoMat* mats, uint32_t n, bool bf16, floa
       if (done[j] || !m.rows || !m.cols) continue;
       const bool tall = m.rows > m.cols;
       const uint32_t side = tall ? m.cols : m.rows, len = tall ? m.rows : m.cols;
-      const SmallShape s = small_shape(side, len);
+      const SmallShape s = small_shape(side, len, dev.ortho_cluster);
       if (count == 0) {
         args.blocks = s.blocks;
         args.shares_off = s.shares_off;

@@ -17,7 +17,10 @@
 // bf16 as the tensor cores' operand (relative 2^-9, the outputs' own
 // rounding), and used twice: dw's rows of that piece are final, dh adds up over
 // the pieces in fp32. Products read h, w and G as they lie: K-major or
-// MN-major, nothing is transposed.
+// MN-major, nothing is transposed. db is summed from G before it is rounded
+// (its terms cancel: the rows of a frequent word's target against its
+// probabilities elsewhere): over 32 rows in fp32, then in 64-bit fixed point,
+// whose sums do not depend on the order of their atomics.
 #include <cstddef>
 
 #include "product.cuh"
@@ -27,6 +30,15 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The scale of the fixed-point sums of G's columns: |G| <= |r| of its row, so a
+// column's sum is at most sum |r|, which the scale (a power of two) takes to
+// below 2^61.
+__device__ __forceinline__ float fixed_scale(float sum) {
+  if (!(sum > 0.0f) || !(sum < INFINITY)) return 1.0f;
+  const int e = static_cast<int>(__float_as_uint(sum) >> 23) - 127;  // sum < 2^(e + 1)
+  const int k = min(60 - e, 127);
+  return __int_as_float((k + 127) << 23);
+}
 // Rows that carry a loss, in their order: row_map[i], targets[i] (int32), for the
 // gradient soft[i] = (-lse / ln 2, scale), and their number. One CTA: the targets are 8 bytes a row, against 2 v d
 // operations. A target >= v is malformed input: latched, the row skipped.
@@ -36,8 +48,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                       uint32_t* __restrict__ row_map, int32_t* __restrict__ targets,
                       uint32_t* __restrict__ count, float* loss, float* lse,
                       const float* __restrict__ row_scale, float2* __restrict__ soft,
-                      uint32_t* error) {
+                      float* __restrict__ fixed, uint32_t* error) {
   __shared__ uint32_t s_warp[32];
+  __shared__ float s_abs[32];
+  float abs_sum = 0.0f;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t base = 0;
   bool bad = false;
@@ -64,6 +78,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const float x = lse[i];
         soft[before] = x == -INFINITY ? make_float2(0.0f, 0.0f)
                                       : make_float2(__fmul_rn(x, -kLog2e), row_scale[i]);
+        abs_sum = __fadd_rn(abs_sum, fabsf(row_scale[i]));
       }
     } else if (i < n && loss) {
       loss[i] = 0.0f;
@@ -74,12 +89,21 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   }
   if (threadIdx.x == 0) *count = base;
   if (bad) atomicOr(error, kDevErrBadInput);
+  if (fixed) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      abs_sum = __fadd_rn(abs_sum, __shfl_xor_sync(0xffffffffu, abs_sum, o));
+    if (lane == 0) s_abs[warp] = abs_sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 32; ++w) abs_sum = __fadd_rn(abs_sum, s_abs[w]);
+      *fixed = fixed_scale(abs_sum);
+    }
+  }
 }
 
-// 8 elements of a row of `cols` from c on, zeros past its end (with `one`, 1.0
-// in bf16 right after it).
-__device__ __forceinline__ uint4 pack_8(const uint16_t* row, uint32_t c, uint32_t cols, bool vec,
-                                        bool one) {
+// 8 elements of a row of `cols` from c on, zeros past its end.
+__device__ __forceinline__ uint4 pack_8(const uint16_t* row, uint32_t c, uint32_t cols, bool vec) {
   if (c + 8 <= cols) {
     if (vec) return __ldg(reinterpret_cast<const uint4*>(row + c));
     if (reinterpret_cast<uintptr_t>(row) % 4 == 0) {
@@ -90,20 +114,20 @@ __device__ __forceinline__ uint4 pack_8(const uint16_t* row, uint32_t c, uint32_
   uint32_t e[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
-    e[j] = c + j < cols ? __ldg(row + c + j) : (one && c + j == cols) ? 0x3f80u : 0u;
+    e[j] = c + j < cols ? __ldg(row + c + j) : 0u;
   return make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16),
                     e[6] | (e[7] << 16));
 }
 
 // Copies rows of 16-bit elements to rows that TMA can read: dst[i] =
 // src[row_map[i]] (or src[i]), zeros past `cols`, past *count and up to
-// `rows_out`; with `one` the element after the last is 1.0 (bf16). zero_rows
-// (optional): rows whose target is skipped are zeroed there.
+// `rows_out`. zero_rows (optional): rows whose target is skipped are zeroed
+// there.
 __global__ void __launch_bounds__(256)
     vocab_pack_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint32_t cols, uint32_t rows,
                       const uint32_t* __restrict__ row_map, const uint32_t* __restrict__ count,
-                      uint16_t* __restrict__ dst, uint32_t ld_out, uint32_t rows_out, bool one,
-                      uint16_t* zero_rows, uint64_t zero_ld, const int64_t* __restrict__ target,
+                      uint16_t* __restrict__ dst, uint32_t ld_out, uint32_t rows_out, uint16_t* zero_rows,
+                      uint64_t zero_ld, const int64_t* __restrict__ target,
                       uint32_t v) {
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t warps = static_cast<uint64_t>(gridDim.x) * 8;
@@ -116,7 +140,7 @@ __global__ void __launch_bounds__(256)
     const uint16_t* from = src + (real ? (row_map ? row_map[i] : i) : 0) * ld;
     uint16_t* to = dst + i * ld_out;
     for (uint32_t c = lane * 8; c < ld_out; c += 256) {
-      const uint4 x = real ? pack_8(from, c, cols, vec, one) : make_uint4(0, 0, 0, 0);
+      const uint4 x = real ? pack_8(from, c, cols, vec) : make_uint4(0, 0, 0, 0);
       *reinterpret_cast<uint4*>(to + c) = x;
     }
     if (zero_rows && i < rows) {
@@ -125,6 +149,28 @@ __global__ void __launch_bounds__(256)
         for (uint32_t c = lane; c < cols; c += 32) zero_rows[i * zero_ld + c] = 0;
     }
   }
+}
+
+__device__ __forceinline__ float block_sum_8(float x, float* s8) {  // 8 warps, a fixed order
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = __fadd_rn(x, __shfl_xor_sync(0xffffffffu, x, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) s8[threadIdx.x >> 5] = x;
+  __syncthreads();
+  x = 0.0f;
+  for (int w = 0; w < 8; ++w) x = __fadd_rn(x, s8[w]);
+  return x;
+}
+__global__ void __launch_bounds__(256)
+    vocab_db_kernel(const long long* __restrict__ sums, const uint32_t* __restrict__ spoilt,
+                    const float* __restrict__ scale, uint32_t v, uint16_t* __restrict__ db) {
+  griddep_wait();
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= v) return;
+  // (fp32 keeps 24 of the sum's bits; the division by a power of two is exact)
+  const float x = spoilt[i] ? __int_as_float(0x7fffffff)
+                            : __fdiv_rn(__ll2float_rn(sums[i]), *scale);
+  db[i] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
 }
 
 // Both of the above in one launch, for batches whose targets every CTA can
@@ -141,16 +187,18 @@ struct GatherArgs {
   uint32_t* count;
   uint16_t* to;
   uint32_t ld_to, rows_to;
-  uint32_t one;  // the element after a row's last is 1.0
   float *loss, *lse;        // the loss call: zero for skipped rows
   const float* row_scale;   // the gradient's
   float2* soft;
+  float* fixed;             // likewise: the scale of db's sums (or nullptr)
+  uint32_t* zero;           // and those sums and their marks: 3 v words
   uint16_t* dh;             // likewise: zeroed rows
   uint64_t ld_dh;
   uint32_t* error;
 };
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
   __shared__ uint32_t s_before[8], s_total[8];
+  __shared__ float s_abs[8];
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t first = blockIdx.x * 8, i = first + warp;
   griddep_wait();
@@ -180,6 +228,13 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
   if (blockIdx.x == 0) {
     if (threadIdx.x == 0) *a.count = total;
     if (bad) atomicOr(a.error, kDevErrBadInput);
+    if (a.fixed) {
+      float x = 0.0f;
+      for (uint32_t j = threadIdx.x; j < a.n; j += 256)
+        if (keeps(__ldg(a.target + j))) x = __fadd_rn(x, fabsf(a.row_scale[j]));
+      x = block_sum_8(x, s_abs);
+      if (threadIdx.x == 0) *a.fixed = fixed_scale(x);
+    }
   }
   const bool vec = reinterpret_cast<uintptr_t>(a.h) % 16 == 0 && a.ld % 8 == 0;
   if (i < a.n) {
@@ -201,7 +256,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
       const uint16_t* from = a.h + i * a.ld;
       for (uint32_t c = lane * 8; c < a.ld_to; c += 256)
         *reinterpret_cast<uint4*>(a.to + static_cast<uint64_t>(at) * a.ld_to + c) =
-            pack_8(from, c, a.d, vec, a.one != 0);
+            pack_8(from, c, a.d, vec);
     } else {
       if (lane == 0 && a.loss) {
         a.loss[i] = 0.0f;
@@ -211,6 +266,8 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
         for (uint32_t c = lane; c < a.d; c += 32) a.dh[i * a.ld_dh + c] = 0;
     }
   }
+  if (a.fixed)
+    for (uint64_t j = blockIdx.x * 256 + threadIdx.x; j < 3ull * a.v; j += gridDim.x * 256) a.zero[j] = 0;
   for (uint32_t at = total + i; at < a.rows_to; at += gridDim.x * 8)
     for (uint32_t c = lane * 8; c < a.ld_to; c += 256)
       *reinterpret_cast<uint4*>(a.to + static_cast<uint64_t>(at) * a.ld_to + c) =
@@ -339,6 +396,29 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// The sum over the warp's rows of column `lane` of their 32: at every step half
+// of the columns go to the lane that keeps them.
+__device__ __forceinline__ float column_sum(const float (&v)[32]) {
+  const uint32_t lane = threadIdx.x & 31;
+  float x[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const bool up = lane & 16u;
+    const float keep = up ? v[j + 16] : v[j], give = up ? v[j] : v[j + 16];
+    x[j] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, give, 16));
+  }
+#pragma unroll
+  for (int w = 8; w > 0; w >>= 1) {
+#pragma unroll
+    for (int j = 0; j < w; ++j) {
+      const bool up = lane & w;
+      const float keep = up ? x[j + w] : x[j], give = up ? x[j] : x[j + w];
+      x[j] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, give, w));
+    }
+  }
+  return x[0];
+}
+
 // Epilogue of the gradient's logits: G in bf16, one piece of the vocabulary.
 struct GradEpilogue {
   struct Params {
@@ -348,6 +428,9 @@ struct GradEpilogue {
     uint16_t* g;               // [row][ld_g]
     uint32_t ld_g;
     uint32_t v0;               // the piece's first word
+    long long* db;             // of the piece: fixed-point sums of G's columns (or nullptr)
+    uint32_t* spoilt;          // of the piece: columns whose sum is none
+    const float* fixed;
   };
   struct Smem {
     alignas(16) float bias[32];
@@ -387,6 +470,17 @@ struct GradEpilogue {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
       }
+      if (e.db && it.m0 + (row & ~31u) < it.rows) {
+        const float x = __fmul_rn(column_sum(v), *e.fixed);
+        const uint32_t col = col0 + (threadIdx.x & 31);
+        if (col < p.n) {
+          if (fabsf(x) < 4611686018427387904.0f)  // 2^62: an lse that is not these logits' exceeds it
+            atomicAdd(reinterpret_cast<unsigned long long*>(e.db + col),
+                      static_cast<unsigned long long>(__float2ll_rn(x)));
+          else
+            e.spoilt[col] = 1;
+        }
+      }
       // columns past the piece lie past the tensor map's extent: never read
       uint32_t w[16];
 #pragma unroll
@@ -405,9 +499,8 @@ __device__ __forceinline__ float4* sum_block(float* sums, uint32_t row_tile, uin
          (static_cast<uint64_t>(row_tile) * chunks + chunk) * (8 * kTileM) + row;
 }
 
-// Epilogue of dh and dw: rows of bf16 at any alignment, optionally one more
-// column that goes elsewhere (db); or fp32 sums, one set per K part, added to
-// over the pieces of the vocabulary.
+// Epilogue of dh and dw: rows of bf16 at any alignment; or fp32 sums, one set
+// per K part, added to over the pieces of the vocabulary.
 struct StoreEpilogue {
   struct Params {
     uint16_t* out;
@@ -415,7 +508,6 @@ struct StoreEpilogue {
     const uint32_t* row_map;  // or nullptr
     uint32_t cols;
     uint32_t align;           // of out's rows, in bytes
-    uint16_t* extra;          // column `cols`, by row (or nullptr)
     float* sums;              // != nullptr: sums instead of out
     uint64_t part_floats;     // from one part's sums to the next
     uint32_t sum_chunks;      // 32-column chunks of a row
@@ -455,12 +547,6 @@ struct StoreEpilogue {
           }
         }
         continue;
-      }
-      if (e.extra && real && e.cols - col0 < 32u) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (e.cols - col0 == static_cast<uint32_t>(j))
-            e.extra[dst] = static_cast<uint16_t>(pack_bf16(v[j], 0.0f));
       }
       if (col0 >= e.cols) continue;
       uint32_t w[16];
@@ -540,7 +626,7 @@ struct VocabPlan {
   uint32_t sum_chunks, sum_parts;  // of dh's sums (0: dh is stored directly)
   uint64_t part_floats;
   // scratch offsets
-  size_t row_map, targets, soft, count, h, w, pairs, at_target, g, sums, total;
+  size_t row_map, targets, soft, fixed, db, count, h, w, pairs, at_target, g, sums, total;
 };
 
 // The products' plans and the scratch. dh has few tiles and the whole piece as
@@ -550,9 +636,9 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
   VocabPlan l = {};
   const double sms = dev.sm_count;
   const bool pair = use_pairs(c);
-  const uint32_t n = c.n ? c.n : 1, dn = c.d + (c.dbias ? 1 : 0);
+  const uint32_t n = c.n ? c.n : 1;
   l.rows = round_up(n, 2 * kTileM);
-  l.ld_h = round_up(dn, 8);
+  l.ld_h = round_up(c.d, 8);
   l.ld_w = round_up(c.d, 8);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -564,6 +650,10 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
   l.targets = take(4ull * l.rows);
   l.count = take(4);
   if (gradient) l.soft = take(8ull * l.rows);
+  if (gradient && c.dbias) {
+    l.fixed = take(4);
+    l.db = take(12ull * c.v);  // sums, then marks
+  }
   l.h = take(2ull * l.rows * l.ld_h);
   if (!tma_rows(c.w, c.ldw)) l.w = take(2ull * c.v * l.ld_w);
   l.piece = gradient ? piece_words(l.rows, c.v) : c.v;
@@ -572,7 +662,7 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
     l.ld_g = round_up(l.piece, kTileNMax);  // epilogues write whole tiles
     l.g = take(2ull * l.rows * l.ld_g);
     plan_product(l.dh, {n, c.d, l.piece, 1, false, pair, sms, 32, 1, 12.0, false});
-    plan_product(l.dw, {l.piece, dn, n, 1, false, pair, sms, 1, 1, 12.0, true});
+    plan_product(l.dw, {l.piece, c.d, n, 1, false, pair, sms, 1, 1, 12.0, true});
     if (l.dh.splits > 1 || l.piece < c.v) {
       l.sum_parts = l.dh.splits;
       l.sum_chunks = round_up(c.d, 32) / 32;
@@ -614,39 +704,40 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
   const float* row_scale = c.row_scale;
   float2* soft = gradient ? reinterpret_cast<float2*>(base + l.soft) : nullptr;
   uint16_t* h = reinterpret_cast<uint16_t*>(base + l.h);
-  const bool one = gradient && c.dbias;
+  float* fixed = gradient && c.dbias ? reinterpret_cast<float*>(base + l.fixed) : nullptr;
   auto pack = [&](const uint16_t* src, uint64_t ld, uint32_t rows, const uint32_t* map,
-                  const uint32_t* cnt, uint16_t* dst, uint32_t ld_out, uint32_t rows_out, bool one,
+                  const uint32_t* cnt, uint16_t* dst, uint32_t ld_out, uint32_t rows_out,
                   uint16_t* zero, uint64_t zero_ld) {
     const uint32_t want = (rows_out + 7) / 8, grid = want < 8 * sms ? want : 8 * sms;
-    void* params[] = {&src, &ld, &d, &rows, &map, &cnt, &dst, &ld_out, &rows_out, &one, &zero,
+    void* params[] = {&src, &ld, &d, &rows, &map, &cnt, &dst, &ld_out, &rows_out, &zero,
                       &zero_ld, &target, &v};
     return launch_kernel(reinterpret_cast<const void*>(&vocab_pack_kernel), grid, 256, ws.stream,
                          params);
   };
   cudaError_t e;
   if (n <= kGatherRows) {
-    GatherArgs a = {target, c.h,  c.ldh,      n,       v,    d,         row_map, targets,
-                    count,  h,    l.ld_h,     l.rows,  one ? 1u : 0u,   loss,    lse,
-                    row_scale,    soft,       gradient ? c.dh : nullptr, c.lddh, error};
+    GatherArgs a = {target, c.h,    c.ldh, n,   v,         d,    row_map, targets,
+                    count,  h,      l.ld_h, l.rows, loss,  lse,  row_scale, soft,
+                    fixed,  reinterpret_cast<uint32_t*>(base + l.db), gradient ? c.dh : nullptr,
+                    c.lddh, error};
     void* params[] = {&a};
     e = launch_kernel(reinterpret_cast<const void*>(&vocab_gather_kernel), n ? (n + 7) / 8 : 1, 256,
                       ws.stream, params);
   } else {
     void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
-                      &error};
+                      &fixed, &error};
     e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1, kRowsThreads, ws.stream,
                       params);
+    if (e == cudaSuccess && fixed) e = cudaMemsetAsync(base + l.db, 0, 12ull * c.v, ws.stream);
     if (e == cudaSuccess)
-      e = pack(c.h, c.ldh, n, row_map, count, h, l.ld_h, l.rows, one, gradient ? c.dh : nullptr,
-               c.lddh);
+      e = pack(c.h, c.ldh, n, row_map, count, h, l.ld_h, l.rows, gradient ? c.dh : nullptr, c.lddh);
   }
   if (e != cudaSuccess) return e;
   out->w = c.w;
   out->ld_w = c.ldw;
   if (!tma_rows(c.w, c.ldw)) {
     uint16_t* w = reinterpret_cast<uint16_t*>(base + l.w);
-    e = pack(c.w, c.ldw, c.v, nullptr, nullptr, w, l.ld_w, c.v, false, nullptr, 0);
+    e = pack(c.w, c.ldw, c.v, nullptr, nullptr, w, l.ld_w, c.v, nullptr, 0);
     out->w = w;
     out->ld_w = l.ld_w;
   }
@@ -695,6 +786,7 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
   const uint64_t h_all = static_cast<uint64_t>(l.rows) * l.ld_h;
   const uint64_t g_all = static_cast<uint64_t>(l.rows) * l.ld_g;
   const uint32_t tile_m = kPair ? 2 * kTileM : kTileM;
+  long long* db = reinterpret_cast<long long*>(base + l.db);
   {
     ProductArgs<GradEpilogue, 1> args = {};
     ProductShape& p = args.shape[0];
@@ -711,7 +803,10 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
       return cudaErrorInvalidValue;
     args.epi[0] = {c.bias ? c.bias + v0 : nullptr,
                    reinterpret_cast<const int32_t*>(base + l.targets),
-                   reinterpret_cast<const float2*>(base + l.soft), g, l.ld_g, v0};
+                   reinterpret_cast<const float2*>(base + l.soft), g, l.ld_g, v0,
+                   c.dbias ? db + v0 : nullptr,
+                   c.dbias ? reinterpret_cast<uint32_t*>(db + c.v) + v0 : nullptr,
+                   reinterpret_cast<const float*>(base + l.fixed)};
     args.phases = args.problems[0] = 1;
     number_items(args, kPair);
     const cudaError_t e = launch_product<GradEpilogue, 1, kPair>(args, ws, dev);
@@ -728,7 +823,7 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
     if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileM) ||
         !make_map(&p.b, w, true, c.d, words, from.ld_w, 1, w_all, kTileK))
       return cudaErrorInvalidValue;
-    args.epi[0] = {c.dh, c.lddh, row_map, c.d, row_align(c.dh, c.lddh), nullptr,
+    args.epi[0] = {c.dh, c.lddh, row_map, c.d, row_align(c.dh, c.lddh),
                    l.sum_parts ? reinterpret_cast<float*>(base + l.sums) : nullptr,
                    l.part_floats, l.sum_chunks, v0 == 0 ? 1u : 0u};
   }
@@ -742,11 +837,10 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
     p.a_mn = p.b_mn = p.bf16 = 1;
     p.counts = 2;
     if (!make_map(&p.a, g, true, words, l.rows, l.ld_g, 1, g_all, kTileK) ||
-        !make_map(&p.b, h, true, c.d + (c.dbias ? 1 : 0), l.rows, l.ld_h, 1, h_all, kTileK))
+        !make_map(&p.b, h, true, c.d, l.rows, l.ld_h, 1, h_all, kTileK))
       return cudaErrorInvalidValue;
     uint16_t* out = c.dw + static_cast<uint64_t>(v0) * c.lddw;
-    args.epi[1] = {out, c.lddw, nullptr, c.d, row_align(out, c.lddw),
-                   c.dbias ? c.dbias + v0 : nullptr, nullptr, 0, 0, 1};
+    args.epi[1] = {out, c.lddw, nullptr, c.d, row_align(out, c.lddw), nullptr, 0, 0, 1};
   }
   args.count = count;
   args.phases = 1;
@@ -793,6 +887,17 @@ cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const Devi
   for (uint32_t v0 = 0; v0 < c.v; v0 += l.piece) {
     e = use_pairs(c) ? grad_piece<true>(c, l, from, base, v0, ws, dev)
                      : grad_piece<false>(c, l, from, base, v0, ws, dev);
+    if (e != cudaSuccess) return e;
+  }
+  if (c.dbias) {
+    const long long* sums = reinterpret_cast<const long long*>(base + l.db);
+    const uint32_t* spoilt = reinterpret_cast<const uint32_t*>(sums + c.v);
+    const float* fixed = reinterpret_cast<const float*>(base + l.fixed);
+    uint32_t v = c.v;
+    uint16_t* out = c.dbias;
+    void* params[] = {&sums, &spoilt, &fixed, &v, &out};
+    e = launch_kernel(reinterpret_cast<const void*>(&vocab_db_kernel), (c.v + 255) / 256, 256,
+                      ws.stream, params);
     if (e != cudaSuccess) return e;
   }
   if (!l.sum_parts || c.n == 0) return cudaSuccess;
