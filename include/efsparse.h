@@ -469,7 +469,7 @@ ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint
  *   The other arguments as for ef_vocab_loss. The outputs are overwritten and
  *   must not overlap an input or one another.
  *
- * G is rounded to bf16 (relative 2^-9) before its products, which are summed
+ * G is rounded to bf16 (relative 2^-8 at most) before its products, which are summed
  * in fp32 and rounded once. A row whose lse is -inf has no gradient. Scratch:
  * G for a piece of the vocabulary, at most 1 GB (or 4096 n bytes if that is
  * more), the gathered h, and w where its rows are not 16-byte aligned.

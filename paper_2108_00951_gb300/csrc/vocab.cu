@@ -14,7 +14,7 @@
 // the largest logit and the sum of exponentials below it; a row's pairs are
 // then joined in order. Gradient: the vocabulary is taken in pieces; a piece's
 // G is formed in a product's epilogue (logits again, then exp), rounded to
-// bf16 as the tensor cores' operand (relative 2^-9, the outputs' own
+// bf16 as the tensor cores' operand (relative 2^-8 at most, the outputs' own
 // rounding), and used twice: dw's rows of that piece are final, dh adds up over
 // the pieces in fp32. Products read h, w and G as they lie: K-major or
 // MN-major, nothing is transposed. db is summed from G before it is rounded
