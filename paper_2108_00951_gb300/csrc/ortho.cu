@@ -321,10 +321,7 @@ struct StepEpilogue {
     uint32_t w[16];
     pack_row(v, w);
     if (col0 == r0) mirror_block(s.turn, w);
-    const uint32_t cols = ld - col0;
-    store_block<2>(s.turn, w, min(cols, 32u), 16, [&](uint32_t i) -> uint16_t* {
-      return r0 + i < n ? out + static_cast<uint64_t>(r0 + i) * ld + col0 : nullptr;
-    });
+    if (r < n) store_row(out + static_cast<uint64_t>(r) * ld + col0, w, min(ld - col0, 32u));
     if (col0 < r0 && r < n) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
@@ -349,7 +346,7 @@ struct StepEpilogue {
       out = e.outs[it.batch];
       ld_out = e.ld_outs[it.batch];
       const uint64_t low = reinterpret_cast<uintptr_t>(out) | (ld_out * 2);
-      align = low % 16 == 0 ? 16 : low % 4 == 0 ? 4 : 2;
+      align = low % 32 == 0 ? 32 : low % 16 == 0 ? 16 : low % 4 == 0 ? 4 : 2;
     }
     const bool rows_exist = r0 < p.m;
     auto alive = [&](uint32_t c) {  // the warp's block has entries to store
@@ -411,15 +408,18 @@ struct StepEpilogue {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             w[j] = pack_bf16(__fmul_rn(v[2 * j], 1.0f / kScaleX), __fmul_rn(v[2 * j + 1], 1.0f / kScaleX));
-          store_block<2>(s.turn, w, min(p.n - col0, 32u), align, [&](uint32_t i) -> uint16_t* {
-            return r0 + i < p.m ? out + (r0 + i) * ld_out + col0 : nullptr;
-          });
+          const uint32_t cols = min(p.n - col0, 32u);
+          if (align == 32 && cols % 16 == 0) {
+            if (r < p.m) store_row(out + r * ld_out + col0, w, cols);
+          } else {
+            store_block<4>(s.turn, w, cols, align, [&](uint32_t i) -> uint16_t* {
+              return r0 + i < p.m ? out + (r0 + i) * ld_out + col0 : nullptr;
+            });
+          }
           continue;
         }
-        const uint32_t cols = e.ld - col0;
-        auto rows = [&](uint32_t i) -> uint16_t* {
-          return r0 + i < p.m ? to + static_cast<uint64_t>(r0 + i) * e.ld + col0 : nullptr;
-        };
+        const uint32_t cols = min(e.ld - col0, 32u);
+        uint16_t* row_to = to + static_cast<uint64_t>(r) * e.ld + col0;
         pack_row(v, w);
         if (!e.exact) {
           uint32_t q[8];
@@ -433,14 +433,12 @@ struct StepEpilogue {
           __stcg(mine, make_uint4(q[0], q[1], q[2], q[3]));
           __stcg(mine + kTileM, make_uint4(q[4], q[5], q[6], q[7]));
         }
-        store_block<2>(s.turn, w, min(cols, 32u), 16, rows);
+        if (r < p.m) store_row(row_to, w, cols);
         if (e.exact) {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = half_rest(v[j]);
           pack_row(v, w);
-          to += e.plane;
-          store_block<2>(s.turn, w, min(cols, 32u), 16, rows);
-          to -= e.plane;
+          if (r < p.m) store_row(row_to + e.plane, w, cols);
         }
         continue;
       }

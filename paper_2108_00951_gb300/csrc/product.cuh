@@ -481,7 +481,18 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 }
 
 // ------------------------------------------- epilogues' stores of 16-bit rows
-// A warp's 32 x 32 block of 16-bit values, each lane holding one row as 16
+// A lane's 32 columns of its row, at an address on a 32-byte boundary: two
+// stores of a sector each (`cols` a multiple of 16).
+__device__ __forceinline__ void store_row(uint16_t* p, const uint32_t (&w)[16], uint32_t cols) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (static_cast<uint32_t>(16 * i) < cols)
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + 16 * i),
+                   "r"(w[8 * i]), "r"(w[8 * i + 1]), "r"(w[8 * i + 2]), "r"(w[8 * i + 3]),
+                   "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
+                   : "memory");
+}
+// Other rows. A warp's 32 x 32 block of 16-bit values, each lane holding one row as 16
 // words, through 2 KB of shared memory, so that stores cover whole sectors:
 // 4 lanes per row with 16-byte rows (kVec16), 16 lanes per row with 4-byte
 // rows, 32 with 2-byte ones. `rows(i)` gives the destination of block row i
@@ -571,10 +582,10 @@ __device__ __forceinline__ void mirror_block(TurnSmem& t, uint32_t (&w)[16]) {
     if (j > lane) w[j / 2] = j & 1u ? (w[j / 2] & 0xffffu) | (x << 16) : (w[j / 2] & 0xffff0000u) | x;
   }
 }
-// The largest of 16, 4, 2 that every row of 16-bit elements starts on.
+// The largest of 32, 16, 4, 2 that every row of 16-bit elements starts on.
 inline uint32_t row_align(const void* p, uint64_t ld) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(p) | (ld * 2);
-  return x % 16 == 0 ? 16 : x % 4 == 0 ? 4 : 2;
+  return x % 32 == 0 ? 32 : x % 16 == 0 ? 16 : x % 4 == 0 ? 4 : 2;
 }
 
 // ------------------------------------------------------------- host side

@@ -274,23 +274,32 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
           make_uint4(0, 0, 0, 0);
 }
 
-// 32 logits of a row: accumulators plus the bias of their columns (through
-// the warp's 32 floats of shared memory), -inf past the vocabulary.
-__device__ __forceinline__ void add_bias(float (&v)[32], const uint16_t* bias, uint32_t col0,
-                                         uint32_t n, float* s_bias) {
-  if (bias) {
-    const uint32_t lane = threadIdx.x & 31;
-    __syncwarp();
-    s_bias[lane] = col0 + lane < n ? bf16_bits_to_f32(__ldg(bias + col0 + lane)) : 0.0f;
-    __syncwarp();
+// The biases of a warp's columns of a tile, at most 128, staged in its shared
+// memory: loaded before the accumulators are ready.
+struct BiasSmem {
+  alignas(16) float bias[128];
+};
+__device__ __forceinline__ void stage_bias(const uint16_t* bias, uint32_t col0, uint32_t cols,
+                                           uint32_t n, BiasSmem& s) {
+  if (!bias) return;
+  const uint32_t lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 b = reinterpret_cast<const float4*>(s_bias)[j];
-      v[4 * j] = __fadd_rn(v[4 * j], b.x);
-      v[4 * j + 1] = __fadd_rn(v[4 * j + 1], b.y);
-      v[4 * j + 2] = __fadd_rn(v[4 * j + 2], b.z);
-      v[4 * j + 3] = __fadd_rn(v[4 * j + 3], b.w);
-    }
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t c = i * 32 + lane;
+    if (c < cols) s.bias[c] = col0 + c < n ? bf16_bits_to_f32(__ldg(bias + col0 + c)) : 0.0f;
+  }
+  __syncwarp();
+}
+// 32 logits of a row: accumulators plus the staged bias of their columns.
+__device__ __forceinline__ void add_bias(float (&v)[32], const float* bias) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 b = reinterpret_cast<const float4*>(bias)[j];
+    v[4 * j] = __fadd_rn(v[4 * j], b.x);
+    v[4 * j + 1] = __fadd_rn(v[4 * j + 1], b.y);
+    v[4 * j + 2] = __fadd_rn(v[4 * j + 2], b.z);
+    v[4 * j + 3] = __fadd_rn(v[4 * j + 3], b.w);
   }
 }
 
@@ -303,9 +312,7 @@ struct LossEpilogue {
     float2* pairs;     // [row][half tile]
     float* at_target;  // [row]
   };
-  struct Smem {
-    alignas(16) float bias[32];
-  };
+  using Smem = BiasSmem;
   struct Row {
     int32_t target;
   };
@@ -321,11 +328,12 @@ struct LossEpilogue {
     const bool real = r < it.rows;
     const int32_t target = state.target;
     float m = -INFINITY, sum = 0.0f;
+    stage_bias(e.bias, it.n0 + acc.c0 * 32, (acc.c1 - acc.c0) * 32, p.n, s);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
-      add_bias(v, e.bias, col0, p.n, s.bias);
+      if (e.bias) add_bias(v, s.bias + (c - acc.c0) * 32);
       if (col0 + 32 > p.n) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = col0 + j < p.n ? v[j] : -INFINITY;
@@ -432,8 +440,7 @@ struct GradEpilogue {
     uint32_t* spoilt;          // of the piece: columns whose sum is none
     const float* fixed;
   };
-  struct Smem {
-    alignas(16) float bias[32];
+  struct Smem : BiasSmem {
     TurnSmem turn;
   };
   struct Row {
@@ -452,11 +459,12 @@ struct GradEpilogue {
     const uint32_t r = it.m0 + row, target = state.target;
     const float shift = state.soft.x, scale = state.soft.y;
     const bool dead = scale == 0.0f;  // past the rows, or without a gradient
+    stage_bias(e.bias, it.n0 + acc.c0 * 32, (acc.c1 - acc.c0) * 32, p.n, s);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
-      add_bias(v, e.bias, col0, p.n, s.bias);
+      if (e.bias) add_bias(v, s.bias + (c - acc.c0) * 32);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         v[j] = __fmul_rn(exp2_fast(__fmaf_rn(v[j], kLog2e, shift)), scale);
@@ -485,6 +493,8 @@ struct GradEpilogue {
       uint32_t w[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+      // in 64-byte runs: while G stays in L2, stores of one sector a row cost the
+      // two products that read it 8 % (1230 x 50,001 x 1000: 354 us, not 328)
       uint16_t* out = e.g + static_cast<uint64_t>(r & ~31u) * e.ld_g + col0;
       store_block<8>(s.turn, w, 32, 16, [&](uint32_t i) { return out + i * e.ld_g; });
     }
@@ -552,15 +562,18 @@ struct StoreEpilogue {
       uint32_t w[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-      if (e.row_map) {
-        store_block<8>(s.turn, w, min(32u, e.cols - col0), e.align, [&](uint32_t i) -> uint16_t* {
+      const uint32_t left = min(32u, e.cols - col0);
+      if (e.align == 32 && left % 16 == 0) {
+        if (real) store_row(e.out + static_cast<uint64_t>(dst) * e.ld + col0, w, left);
+      } else if (e.row_map) {
+        store_block<8>(s.turn, w, left, e.align, [&](uint32_t i) -> uint16_t* {
           const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
           return to == 0xffffffffu ? nullptr : e.out + static_cast<uint64_t>(to) * e.ld + col0;
         });
       } else {
         const uint32_t r0 = r - (threadIdx.x & 31);
         uint16_t* to = e.out + static_cast<uint64_t>(r0) * e.ld + col0;
-        store_block<8>(s.turn, w, min(32u, e.cols - col0), e.align, [&](uint32_t i) -> uint16_t* {
+        store_block<8>(s.turn, w, left, e.align, [&](uint32_t i) -> uint16_t* {
           return r0 + i < it.rows ? to + i * e.ld : nullptr;
         });
       }
@@ -903,7 +916,7 @@ cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const Devi
   if (!l.sum_parts || c.n == 0) return cudaSuccess;
   const float* sums = reinterpret_cast<const float*>(base + l.sums);
   uint64_t part_floats = l.part_floats, ld = c.lddh;
-  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, wide = row_align(c.dh, c.lddh) == 16 ? 1u : 0u;
+  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, wide = row_align(c.dh, c.lddh) >= 16 ? 1u : 0u;
   const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
   const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
   uint16_t* dh = c.dh;

@@ -20,6 +20,8 @@
 // tokens' hi and lo, and dh = G w, K = 16 words: a warp takes 64 columns and a
 // slice of the words; the slices' sums of dh are added in order by a third
 // kernel.
+#include <algorithm>
+
 #include "product.cuh"
 
 namespace efs {
@@ -693,7 +695,7 @@ size_t vocab_few_scratch(const VocabCall& c, bool gradient, const DeviceInfo& de
 cudaError_t launch_vocab_few_loss(const VocabCall& c, Workspace& ws, const DeviceInfo& dev) {
   const FewPlan p = few_plan(c, false, dev);
   const FewArgs a = few_args(c, p, ws.model_scratch(), ws);
-  const uint32_t align = row_align(c.w, c.ldw);
+  const uint32_t align = std::min(row_align(c.w, c.ldw), 16u);
   return p.nt == 1 ? few_logits<false, 1>(a, p, align, ws) : few_logits<false, 2>(a, p, align, ws);
 }
 
@@ -701,7 +703,7 @@ cudaError_t launch_vocab_few_grad(const VocabCall& c, Workspace& ws, const Devic
   const FewPlan p = few_plan(c, true, dev);
   char* base = ws.model_scratch();
   const FewArgs a = few_args(c, p, base, ws);
-  const uint32_t align = row_align(c.w, c.ldw);
+  const uint32_t align = std::min(row_align(c.w, c.ldw), 16u);
   cudaError_t e = p.nt == 1 ? few_logits<true, 1>(a, p, align, ws)
                             : few_logits<true, 2>(a, p, align, ws);
   if (e != cudaSuccess) return e;
@@ -720,7 +722,7 @@ cudaError_t launch_vocab_few_grad(const VocabCall& c, Workspace& ws, const Devic
   g.slices = p.slices;
   g.slice_groups = p.slice_groups;
   g.dw = c.dw;
-  g.align_dw = row_align(c.dw, c.lddw);
+  g.align_dw = std::min(row_align(c.dw, c.lddw), 16u);
   g.sums = reinterpret_cast<float*>(base + p.sums);
   g.ld_sum = p.windows * kCols;
   e = p.nt == 1 ? few_grad<1>(g, align, dev, ws) : few_grad<2>(g, align, dev, ws);
