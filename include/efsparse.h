@@ -61,7 +61,10 @@
  * choice, written by the device). Memory is therefore bounded by
  * (number of streams used) x that size; ef_workspace_release() frees all
  * workspaces of the current device (for example after a phase that used
- * extra streams), and ef_hard_threshold_noalloc needs none. Calls on
+ * extra streams), and ef_hard_threshold_noalloc needs none. ef_vocab_loss,
+ * ef_vocab_loss_grad and ef_orthogonalize keep their scratch in an allocation of
+ * its own beside that workspace, grown and released likewise; each entry's
+ * comment gives its size. Calls on
  * DIFFERENT streams never share a workspace and may run concurrently; calls
  * on the same stream are ordered by the stream.
  *
@@ -469,10 +472,13 @@ ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint
  *   The other arguments as for ef_vocab_loss. The outputs are overwritten and
  *   must not overlap an input or one another.
  *
- * G is rounded to bf16 (relative 2^-8 at most) before its products, which are summed
- * in fp32 and rounded once. A row whose lse is -inf has no gradient. Scratch:
- * G for a piece of the vocabulary, at most 1 GB (or 4096 n bytes if that is
- * more), the gathered h, and w where its rows are not 16-byte aligned.
+ * dh and dw: G is rounded to bf16 (relative 2^-8 at most; up to 16 rows keep
+ * 16 bits of it) before its products, which are summed in fp32 and rounded
+ * once. dbias is summed from G before that rounding. A row whose lse is -inf
+ * has no gradient. Equal inputs give equal bits. Scratch: G for a piece of the
+ * vocabulary, at most 1 GB (or 4096 n bytes if that is more), the gathered h,
+ * up to 32 fp32 partial sums of dh, and w where its rows are not 16-byte
+ * aligned.
  */
 ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
                              const uint16_t* bias, const int64_t* target, const float* lse,
@@ -505,7 +511,10 @@ ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w,
  * to bf16. |U|_F is summed in fp32 pairs: |U|_F^2 must be within the range of
  * fp32 (a matrix whose squares all underflow gives 0, as a zero matrix does).
  * A NaN or infinity makes its whole matrix NaN. Equal inputs give equal bits.
- * Scratch: about 8 bytes per entry and 4 per entry of the small squares.
+ * Scratch: 5 bytes per entry and 4 per entry of the squares on the shorter
+ * side (both 8 where that side is at most 128), and 64 KB per split tile; none
+ * where every matrix fits on chip (a shorter side of at most 128 and up to
+ * a few thousand columns).
  */
 ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t* cols,
                            const void* const* u, const uint64_t* ld_u, ef_grad_type u_type,

@@ -1,7 +1,7 @@
 // api.cu — the extern "C" boundary declared in include/efsparse.h: host-side
 // argument checks, the per-(device, stream) workspaces, and status reporting.
 // Every compute step runs in the kernels of ht.cu, topk.cu, topk_layerwise.cu
-// and aggregate.cu.
+// and aggregate.cu, and of vocab.cu, vocab_few.cu, ortho.cu and ortho_small.cu.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -726,7 +726,11 @@ ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint
   c.ldw = ldw;
   c.loss = loss_out;
   c.lse = lse_out;
-  return efs::vocab_entry(c, n, v, d, false, reinterpret_cast<cudaStream_t>(stream));
+  try {
+    return efs::vocab_entry(c, n, v, d, false, reinterpret_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return EF_ERR_NO_MEMORY;
+  }
 }
 
 ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
@@ -748,7 +752,11 @@ ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w,
   c.dw = dw_out;
   c.lddw = lddw;
   c.dbias = dbias_out;
-  return efs::vocab_entry(c, n, v, d, true, reinterpret_cast<cudaStream_t>(stream));
+  try {
+    return efs::vocab_entry(c, n, v, d, true, reinterpret_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return EF_ERR_NO_MEMORY;
+  }
 }
 
 ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t* cols,
