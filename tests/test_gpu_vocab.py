@@ -310,3 +310,23 @@ def test_offsets_past_32_bits(n):
     for a in range(0, v, 50000):
         ref_h += p[:, a:a + 50000] @ w[a:a + 50000].double()
     assert float((dh.double() - ref_h).norm() / ref_h.norm()) < 5e-3
+
+
+@pytest.mark.parametrize("d", [1, 63, 64, 65, 129, 511, 640, 1023, 1024, 1025, 2048])
+@pytest.mark.parametrize("n,v", [(1, 17), (8, 2439), (9, 16), (16, 5001)])
+def test_few_rows_at_every_width(n, v, d):
+    h, w, t, r, b = inputs(n, v, d, True, 0.2 if n > 1 else 0.0, pad=d % 3, seed=5)
+    _, lse = loss(h, w, t, b)
+    z, ref, _, g, off = formula(h, w, t, r, b)
+    check_grad(grad(h, w, t, lse, r, b, pad=d % 3), g, h, w, b, off, True)
+    assert efs.ef_check_status() == efs.EF_OK
+
+
+@pytest.mark.parametrize("n,d", [(4, 200), (4, 1100), (40, 200)])
+def test_skipped_rows_have_no_gradient_beside_infinite_weights(n, d):
+    h, w, t, r, _ = inputs(n, 500, d, seed=6)
+    w[7, 3] = float("inf")
+    t[1] = -1
+    _, lse = loss(h, w, t)
+    dh, _, _ = grad(h, w, t, lse, r)
+    assert torch.all(dh[1] == 0)
