@@ -119,34 +119,48 @@ __device__ __forceinline__ uint4 pack_8(const uint16_t* row, uint32_t c, uint32_
                     e[6] | (e[7] << 16));
 }
 
-// Copies rows of 16-bit elements to rows that TMA can read: dst[i] =
-// src[row_map[i]] (or src[i]), zeros past `cols`, past *count and up to
-// `rows_out`. zero_rows (optional): rows whose target is skipped are zeroed
-// there.
+// Copies rows of 16-bit elements to rows that TMA can read, a warp a row: dst[i]
+// = src[row_map[i]] (or src[i]), zeros past `cols` and from `have` up to
+// `rows_out`.
+struct PackArgs {
+  const uint16_t* src;
+  uint64_t ld;
+  uint32_t cols;
+  const uint32_t* row_map;
+  uint16_t* dst;
+  uint32_t ld_out, rows_out;
+};
+__device__ __forceinline__ void pack_row(const PackArgs& a, uint64_t i, uint32_t have, bool vec) {
+  const uint32_t lane = threadIdx.x & 31;
+  const bool real = i < have;
+  const uint16_t* from = a.src + (real ? (a.row_map ? a.row_map[i] : i) : 0) * a.ld;
+  uint16_t* to = a.dst + i * a.ld_out;
+  for (uint32_t c = lane * 8; c < a.ld_out; c += 256) {
+    const uint4 x = real ? pack_8(from, c, a.cols, vec) : make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(to + c) = x;
+  }
+}
+__device__ __forceinline__ bool pack_wide(const PackArgs& a) {
+  return reinterpret_cast<uintptr_t>(a.src) % 16 == 0 && a.ld % 8 == 0;
+}
+// zero_rows (optional): of the `rows` rows, those whose target is skipped are
+// zeroed there.
 __global__ void __launch_bounds__(256)
-    vocab_pack_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint32_t cols, uint32_t rows,
-                      const uint32_t* __restrict__ row_map, const uint32_t* __restrict__ count,
-                      uint16_t* __restrict__ dst, uint32_t ld_out, uint32_t rows_out, uint16_t* zero_rows,
-                      uint64_t zero_ld, const int64_t* __restrict__ target,
+    vocab_pack_kernel(const PackArgs a, uint32_t rows, const uint32_t* __restrict__ count,
+                      uint16_t* zero_rows, uint64_t zero_ld, const int64_t* __restrict__ target,
                       uint32_t v) {
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t warps = static_cast<uint64_t>(gridDim.x) * 8;
-  const bool vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && ld % 8 == 0;
+  const bool vec = pack_wide(a);
   griddep_wait();
   const uint32_t have = count ? *count : rows;
-  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); i < rows_out;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); i < a.rows_out;
        i += warps) {
-    const bool real = i < have;
-    const uint16_t* from = src + (real ? (row_map ? row_map[i] : i) : 0) * ld;
-    uint16_t* to = dst + i * ld_out;
-    for (uint32_t c = lane * 8; c < ld_out; c += 256) {
-      const uint4 x = real ? pack_8(from, c, cols, vec) : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(to + c) = x;
-    }
+    pack_row(a, i, have, vec);
     if (zero_rows && i < rows) {
       const int64_t t = target[i];
       if (t < 0 || t >= static_cast<int64_t>(v))
-        for (uint32_t c = lane; c < cols; c += 32) zero_rows[i * zero_ld + c] = 0;
+        for (uint32_t c = lane; c < a.cols; c += 32) zero_rows[i * zero_ld + c] = 0;
     }
   }
 }
@@ -161,21 +175,9 @@ __device__ __forceinline__ float block_sum_8(float x, float* s8) {  // 8 warps, 
   for (int w = 0; w < 8; ++w) x = __fadd_rn(x, s8[w]);
   return x;
 }
-__global__ void __launch_bounds__(256)
-    vocab_db_kernel(const long long* __restrict__ sums, const uint32_t* __restrict__ spoilt,
-                    const float* __restrict__ scale, uint32_t v, uint16_t* __restrict__ db) {
-  griddep_wait();
-  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= v) return;
-  // (fp32 keeps 24 of the sum's bits; the division by a power of two is exact)
-  const float x = spoilt[i] ? __int_as_float(0x7fffffff)
-                            : __fdiv_rn(__ll2float_rn(sums[i]), *scale);
-  db[i] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
-}
-
-// Both of the above in one launch, for batches whose targets every CTA can
+// Rows found and gathered in one launch, for batches whose targets every CTA can
 // afford to count: a warp takes a row. Rows past the last gathered one are
-// zeroed.
+// zeroed. CTAs past the first `ctas` copy w, where it has to be copied.
 constexpr uint32_t kGatherRows = 4096;
 struct GatherArgs {
   const int64_t* target;
@@ -195,6 +197,8 @@ struct GatherArgs {
   uint16_t* dh;             // likewise: zeroed rows
   uint64_t ld_dh;
   uint32_t* error;
+  uint32_t ctas;
+  PackArgs w;
 };
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
   __shared__ uint32_t s_before[8], s_total[8];
@@ -202,6 +206,13 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t first = blockIdx.x * 8, i = first + warp;
   griddep_wait();
+  if (blockIdx.x >= a.ctas) {
+    const bool wide = pack_wide(a.w);
+    const uint64_t warps = static_cast<uint64_t>(gridDim.x - a.ctas) * 8;
+    for (uint64_t r = i - a.ctas * 8; r < a.w.rows_out; r += warps)
+      pack_row(a.w, r, a.w.rows_out, wide);
+    return;
+  }
   auto keeps = [&](int64_t t) { return t >= 0 && t < static_cast<int64_t>(a.v); };
   uint32_t before = 0, total = 0;
   bool bad = false;
@@ -267,8 +278,8 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
     }
   }
   if (a.fixed)
-    for (uint64_t j = blockIdx.x * 256 + threadIdx.x; j < 3ull * a.v; j += gridDim.x * 256) a.zero[j] = 0;
-  for (uint32_t at = total + i; at < a.rows_to; at += gridDim.x * 8)
+    for (uint64_t j = blockIdx.x * 256 + threadIdx.x; j < 3ull * a.v; j += a.ctas * 256) a.zero[j] = 0;
+  for (uint32_t at = total + i; at < a.rows_to; at += a.ctas * 8)
     for (uint32_t c = lane * 8; c < a.ld_to; c += 256)
       *reinterpret_cast<uint4*>(a.to + static_cast<uint64_t>(at) * a.ld_to + c) =
           make_uint4(0, 0, 0, 0);
@@ -523,8 +534,9 @@ struct StoreEpilogue {
     uint32_t sum_chunks;      // 32-column chunks of a row
     uint32_t first;           // the sums start here
   };
-  struct Smem {
+  union Smem {
     TurnSmem turn;
+    ShiftSmem shift;
   };
   struct Row {
     uint32_t dst;
@@ -539,6 +551,7 @@ struct StoreEpilogue {
                                               Smem& s, const ProductAcc& acc, uint32_t, Row state) {
     const uint32_t r = it.m0 + row, dst = state.dst;
     const bool real = r < it.rows;
+    uint4 carry = make_uint4(0, 0, 0, 0);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
       acc.load(c, v);
@@ -565,52 +578,73 @@ struct StoreEpilogue {
       const uint32_t left = min(32u, e.cols - col0);
       if (e.align == 32 && left % 16 == 0) {
         if (real) store_row(e.out + static_cast<uint64_t>(dst) * e.ld + col0, w, left);
-      } else if (e.row_map) {
-        store_block<8>(s.turn, w, left, e.align, [&](uint32_t i) -> uint16_t* {
-          const uint32_t to = __shfl_sync(0xffffffffu, dst, i);
-          return to == 0xffffffffu ? nullptr : e.out + static_cast<uint64_t>(to) * e.ld + col0;
-        });
-      } else {
-        const uint32_t r0 = r - (threadIdx.x & 31);
-        uint16_t* to = e.out + static_cast<uint64_t>(r0) * e.ld + col0;
-        store_block<8>(s.turn, w, left, e.align, [&](uint32_t i) -> uint16_t* {
-          return r0 + i < it.rows ? to + i * e.ld : nullptr;
-        });
+        continue;
       }
+      const uint32_t r0 = r - (threadIdx.x & 31);
+      auto to = [&](uint32_t i) -> uint16_t* {
+        uint32_t at = r0 + i;
+        if (e.row_map) at = __shfl_sync(0xffffffffu, dst, i);
+        return r0 + i < it.rows ? e.out + static_cast<uint64_t>(at) * e.ld + col0 : nullptr;
+      };
+      if (e.align >= 4 && !(e.align >= 16 && left % 8 == 0))
+        store_shifted(s.shift, w, carry, left, c == acc.c0, c + 1 == acc.c1 || col0 + 32 >= e.cols, to);
+      else
+        store_block<8>(s.turn, w, left, e.align, to);
     }
   }
 };
 
-// dh from its sums: parts added in order, rounded, rows scattered. A CTA takes
-// 32 rows x 32 columns, a thread four columns of a row.
-__global__ void __launch_bounds__(256)
-    vocab_dh_kernel(const float* __restrict__ sums, uint64_t part_floats, uint32_t parts,
-                    uint32_t chunks, const uint32_t* __restrict__ row_map,
-                    const uint32_t* __restrict__ count, uint16_t* __restrict__ dh, uint64_t ld,
-                    uint32_t cols, uint32_t wide) {
+// The gradient's last kernel. dh from its sums: parts added in order, rounded,
+// rows scattered; a CTA takes 32 rows x 32 columns, a thread four columns of a
+// row. CTAs past the first `ctas`: db from its fixed-point sums.
+struct FinishArgs {
+  uint32_t ctas;
+  const float* sums;
+  uint64_t part_floats;
+  uint32_t parts, chunks;
+  const uint32_t *row_map, *count;
+  uint16_t* dh;
+  uint64_t ld;
+  uint32_t cols, wide;
+  const long long* db_sums;
+  const uint32_t* spoilt;
+  const float* scale;
+  uint32_t v;
+  uint16_t* db;
+};
+__global__ void __launch_bounds__(256) vocab_finish_kernel(const FinishArgs a) {
   griddep_wait();
-  const uint32_t chunk = blockIdx.x % chunks, unit = threadIdx.x & 7u;
-  const uint32_t r = blockIdx.x / chunks * 32 + (threadIdx.x >> 3), c = chunk * 32 + unit * 4;
-  if (r >= *count || c >= cols) return;
-  const float4* x = sum_block(const_cast<float*>(sums), r / kTileM, chunks, chunk, r % kTileM) +
+  if (blockIdx.x >= a.ctas) {
+    const uint32_t i = (blockIdx.x - a.ctas) * 256 + threadIdx.x;
+    if (i >= a.v) return;
+    // (fp32 keeps 24 of the sum's bits; the division by a power of two is exact)
+    const float x = a.spoilt[i] ? __int_as_float(0x7fffffff)
+                                : __fdiv_rn(__ll2float_rn(a.db_sums[i]), *a.scale);
+    a.db[i] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
+    return;
+  }
+  const uint32_t chunk = blockIdx.x % a.chunks, unit = threadIdx.x & 7u;
+  const uint32_t r = blockIdx.x / a.chunks * 32 + (threadIdx.x >> 3), c = chunk * 32 + unit * 4;
+  if (r >= *a.count || c >= a.cols) return;
+  const float4* x = sum_block(const_cast<float*>(a.sums), r / kTileM, a.chunks, chunk, r % kTileM) +
                     unit * kTileM;
-  uint16_t* to = dh + static_cast<uint64_t>(row_map[r]) * ld + c;
+  uint16_t* to = a.dh + static_cast<uint64_t>(a.row_map[r]) * a.ld + c;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-  for (uint32_t s = 0; s < parts; ++s) {
-    const float4 y = __ldcg(x + s * (part_floats / 4));
+  for (uint32_t s = 0; s < a.parts; ++s) {
+    const float4 y = __ldcg(x + s * (a.part_floats / 4));
     v = make_float4(__fadd_rn(v.x, y.x), __fadd_rn(v.y, y.y), __fadd_rn(v.z, y.z),
                     __fadd_rn(v.w, y.w));
   }
   const uint2 w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-  if (wide && c + 4 <= cols) {
+  if (a.wide && c + 4 <= a.cols) {
     *reinterpret_cast<uint2*>(to) = w;
     return;
   }
   to[0] = static_cast<uint16_t>(w.x);
-  if (c + 1 < cols) to[1] = static_cast<uint16_t>(w.x >> 16);
-  if (c + 2 < cols) to[2] = static_cast<uint16_t>(w.y);
-  if (c + 3 < cols) to[3] = static_cast<uint16_t>(w.y >> 16);
+  if (c + 1 < a.cols) to[1] = static_cast<uint16_t>(w.x >> 16);
+  if (c + 2 < a.cols) to[2] = static_cast<uint16_t>(w.y);
+  if (c + 3 < a.cols) to[3] = static_cast<uint16_t>(w.y >> 16);
 }
 
 constexpr uint32_t round_up(uint32_t x, uint32_t to) { return (x + to - 1) / to * to; }
@@ -718,42 +752,39 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
   float2* soft = gradient ? reinterpret_cast<float2*>(base + l.soft) : nullptr;
   uint16_t* h = reinterpret_cast<uint16_t*>(base + l.h);
   float* fixed = gradient && c.dbias ? reinterpret_cast<float*>(base + l.fixed) : nullptr;
-  auto pack = [&](const uint16_t* src, uint64_t ld, uint32_t rows, const uint32_t* map,
-                  const uint32_t* cnt, uint16_t* dst, uint32_t ld_out, uint32_t rows_out,
-                  uint16_t* zero, uint64_t zero_ld) {
-    const uint32_t want = (rows_out + 7) / 8, grid = want < 8 * sms ? want : 8 * sms;
-    void* params[] = {&src, &ld, &d, &rows, &map, &cnt, &dst, &ld_out, &rows_out, &zero,
-                      &zero_ld, &target, &v};
+  auto pack = [&](PackArgs a, uint32_t rows, const uint32_t* cnt, uint16_t* zero, uint64_t zero_ld) {
+    const uint32_t want = (a.rows_out + 7) / 8, grid = want < 8 * sms ? want : 8 * sms;
+    void* params[] = {&a, &rows, &cnt, &zero, &zero_ld, &target, &v};
     return launch_kernel(reinterpret_cast<const void*>(&vocab_pack_kernel), grid, 256, ws.stream,
                          params);
   };
-  cudaError_t e;
+  out->w = c.w;
+  out->ld_w = c.ldw;
+  PackArgs copy_w = {};
+  if (!tma_rows(c.w, c.ldw)) {
+    copy_w = {c.w, c.ldw, d, nullptr, reinterpret_cast<uint16_t*>(base + l.w), l.ld_w, v};
+    out->w = copy_w.dst;
+    out->ld_w = l.ld_w;
+  }
   if (n <= kGatherRows) {
+    const uint32_t ctas = n ? (n + 7) / 8 : 1, rows = (v + 7) / 8;
+    const uint32_t more = !copy_w.src ? 0 : rows < 8 * sms ? rows : 8 * sms;
     GatherArgs a = {target, c.h,    c.ldh, n,   v,         d,    row_map, targets,
                     count,  h,      l.ld_h, l.rows, loss,  lse,  row_scale, soft,
                     fixed,  reinterpret_cast<uint32_t*>(base + l.db), gradient ? c.dh : nullptr,
-                    c.lddh, error};
+                    c.lddh, error,  ctas, copy_w};
     void* params[] = {&a};
-    e = launch_kernel(reinterpret_cast<const void*>(&vocab_gather_kernel), n ? (n + 7) / 8 : 1, 256,
-                      ws.stream, params);
-  } else {
-    void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
-                      &fixed, &error};
-    e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1, kRowsThreads, ws.stream,
-                      params);
-    if (e == cudaSuccess && fixed) e = cudaMemsetAsync(base + l.db, 0, 12ull * c.v, ws.stream);
-    if (e == cudaSuccess)
-      e = pack(c.h, c.ldh, n, row_map, count, h, l.ld_h, l.rows, gradient ? c.dh : nullptr, c.lddh);
+    return launch_kernel(reinterpret_cast<const void*>(&vocab_gather_kernel), ctas + more, 256,
+                         ws.stream, params);
   }
-  if (e != cudaSuccess) return e;
-  out->w = c.w;
-  out->ld_w = c.ldw;
-  if (!tma_rows(c.w, c.ldw)) {
-    uint16_t* w = reinterpret_cast<uint16_t*>(base + l.w);
-    e = pack(c.w, c.ldw, c.v, nullptr, nullptr, w, l.ld_w, c.v, nullptr, 0);
-    out->w = w;
-    out->ld_w = l.ld_w;
-  }
+  void* params[] = {&target, &n, &v, &row_map, &targets, &count, &loss, &lse, &row_scale, &soft,
+                    &fixed, &error};
+  cudaError_t e = launch_kernel(reinterpret_cast<const void*>(&vocab_rows_kernel), 1, kRowsThreads,
+                                ws.stream, params);
+  if (e == cudaSuccess && fixed) e = cudaMemsetAsync(base + l.db, 0, 12ull * c.v, ws.stream);
+  if (e == cudaSuccess)
+    e = pack({c.h, c.ldh, d, row_map, h, l.ld_h, l.rows}, n, count, gradient ? c.dh : nullptr, c.lddh);
+  if (e == cudaSuccess && copy_w.src) e = pack(copy_w, v, nullptr, nullptr, 0);
   return e;
 }
 
@@ -902,27 +933,33 @@ cudaError_t launch_vocab_loss_grad(const VocabCall& c, Workspace& ws, const Devi
                      : grad_piece<false>(c, l, from, base, v0, ws, dev);
     if (e != cudaSuccess) return e;
   }
-  if (c.dbias) {
-    const long long* sums = reinterpret_cast<const long long*>(base + l.db);
-    const uint32_t* spoilt = reinterpret_cast<const uint32_t*>(sums + c.v);
-    const float* fixed = reinterpret_cast<const float*>(base + l.fixed);
-    uint32_t v = c.v;
-    uint16_t* out = c.dbias;
-    void* params[] = {&sums, &spoilt, &fixed, &v, &out};
-    e = launch_kernel(reinterpret_cast<const void*>(&vocab_db_kernel), (c.v + 255) / 256, 256,
-                      ws.stream, params);
-    if (e != cudaSuccess) return e;
+  FinishArgs f = {};
+  uint32_t more = 0;
+  if (l.sum_parts && c.n) {
+    f.chunks = l.sum_chunks;
+    f.ctas = (c.n + 31) / 32 * f.chunks;
+    f.sums = reinterpret_cast<const float*>(base + l.sums);
+    f.part_floats = l.part_floats;
+    f.parts = l.sum_parts;
+    f.row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
+    f.count = reinterpret_cast<const uint32_t*>(base + l.count);
+    f.dh = c.dh;
+    f.ld = c.lddh;
+    f.cols = c.d;
+    f.wide = row_align(c.dh, c.lddh) >= 16 ? 1u : 0u;
   }
-  if (!l.sum_parts || c.n == 0) return cudaSuccess;
-  const float* sums = reinterpret_cast<const float*>(base + l.sums);
-  uint64_t part_floats = l.part_floats, ld = c.lddh;
-  uint32_t parts = l.sum_parts, chunks = l.sum_chunks, cols = c.d, wide = row_align(c.dh, c.lddh) >= 16 ? 1u : 0u;
-  const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
-  const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
-  uint16_t* dh = c.dh;
-  void* params[] = {&sums, &part_floats, &parts, &chunks, &row_map, &count, &dh, &ld, &cols, &wide};
-  return launch_kernel(reinterpret_cast<const void*>(&vocab_dh_kernel),
-                       (c.n + 31) / 32 * chunks, 256, ws.stream, params);
+  if (c.dbias) {
+    more = (c.v + 255) / 256;
+    f.db_sums = reinterpret_cast<const long long*>(base + l.db);
+    f.spoilt = reinterpret_cast<const uint32_t*>(f.db_sums + c.v);
+    f.scale = reinterpret_cast<const float*>(base + l.fixed);
+    f.v = c.v;
+    f.db = c.dbias;
+  }
+  if (f.ctas + more == 0) return cudaSuccess;
+  void* params[] = {&f};
+  return launch_kernel(reinterpret_cast<const void*>(&vocab_finish_kernel), f.ctas + more, 256,
+                       ws.stream, params);
 }
 
 }  // namespace efs
