@@ -563,8 +563,9 @@ Plan make_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev) {
       g->rows = mats[i].rows;
       g->cols = mats[i].cols;
       g->side = g->rows < g->cols ? g->rows : g->cols;
-      g->ld_x = round_up(g->cols, 16);
-      g->ld_s = round_up(g->side, 16);
+      // rows on lines of 128 bytes, which TMA reads whole (650 columns: 383 -> 371 us)
+      g->ld_x = round_up(g->cols, 64);
+      g->ld_s = round_up(g->side, 64);
       g->planes = g->side <= kExactSide ? 2 : 1;
     }
     g->mats.push_back(i);
