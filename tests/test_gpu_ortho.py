@@ -181,3 +181,14 @@ def test_refuses_overlap_and_shapes():
         efs.ef_orthogonalize([u.T], [torch.empty(30, 20, device=DEV, dtype=torch.bfloat16)])
     with pytest.raises(TypeError):
         efs.ef_orthogonalize([u, u.bfloat16()], [out, out.clone()])
+
+
+@pytest.mark.parametrize("cols", [(27, 576), (100, 700, 1152), (64, 300, 500, 900, 1152)])
+def test_small_matrices_of_few_and_of_many_shapes(cols):
+    us = [matrix(64 + 16 * (i % 3), c, seed=i) for i, c in enumerate(cols)]
+    moms = [torch.randn_like(u) * 1e-3 for u in us]
+    want = [0.9 * m.double() + u.double() for m, u in zip(moms, us)]
+    outs = run(us, moms, 0.9)
+    for u, m, w, out in zip(us, moms, want, outs):
+        assert float((m.double() - w).abs().max()) <= 2.0 ** -23 * float(w.abs().max())
+        check(u.double() + m.double(), out)
