@@ -161,6 +161,7 @@ struct ProductArgs {
 struct ProductSmem {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2];
   uint32_t tmem, joined;
+  uint32_t failed;  // an epilogue warp's wait ran out
 };
 
 // What an epilogue reads its accumulators through: 32 columns of the thread's
@@ -207,6 +208,26 @@ struct ProductAcc {
   }
 };
 
+// Parts of a joined block summed by several warps, kUnits of its eight groups of
+// four columns each (a lane a row), in the place of the first part: one warp has
+// registers for two parts on their way at a time, and sixteen parts took it 8 us.
+template <int kUnits>
+__device__ __forceinline__ void sum_parts(float4* first, uint64_t stride, uint32_t splits) {
+  float4 sum[kUnits];
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll (16 / kUnits)
+  for (uint32_t s = 0; s < splits; ++s)
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const float4 x = __ldcg(first + s * (stride / 4) + j * kTileM);
+      sum[j] = make_float4(__fadd_rn(sum[j].x, x.x), __fadd_rn(sum[j].y, x.y),
+                           __fadd_rn(sum[j].z, x.z), __fadd_rn(sum[j].w, x.w));
+    }
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) __stcg(first + j * kTileM, sum[j]);
+}
+
 // Waits until a counter has reached `target` (modulo 2^32).
 __device__ __forceinline__ bool wait_count(const uint32_t* word, uint32_t target, uint64_t limit_ns) {
   const uint64_t t0 = global_timer_ns();
@@ -244,6 +265,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
   const uint32_t unit = kPair ? blockIdx.x >> 1 : blockIdx.x;
   const uint32_t units = kPair ? gridDim.x >> 1 : gridDim.x;
   if (threadIdx.x == 0) {
+    s.failed = 0;
     for (uint32_t i = 0; i < R::kStages; ++i) {
       mbar_init(&s.full[i], 1);
       mbar_init(&s.empty[i], 1);
@@ -422,6 +444,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
               __stcg(reinterpret_cast<float4*>(dst + static_cast<uint64_t>(c) * (32 * kTileM)) + j * kTileM,
                      make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
           }
+          if (!ok) s.failed = 1;
           asm volatile("bar.sync 2, 256;" ::: "memory");
           if (warp == 2 && lane == 0) {
             __threadfence();
@@ -429,8 +452,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // of those readies the counter for its next tile
             uint32_t* counter = &args.arrivals[it.part];
             atomicAdd(counter, 1u);
-            s.joined = wait_count(counter, p.splits, ok ? args.wait_ns : 0) ? 1u : 0u;
-            if (s.joined && atomicAdd(counter, 1u) == 2 * p.splits - 1) atomicExch(counter, 0u);
+            const bool here = wait_count(counter, p.splits, ok ? args.wait_ns : 0);
+            s.joined = here && !s.failed ? 1u : 0u;  // (all warps go on alike)
+            if (here && atomicAdd(counter, 1u) == 2 * p.splits - 1) atomicExch(counter, 0u);
             __threadfence();
           }
           asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -442,6 +466,24 @@ __global__ void __launch_bounds__(kProductThreads, 1)
           from.none = false;
           from.part_stride = tile_floats;
           from.parts = mine;
+          // from 8 parts on a CTA has at most half as many blocks as warps: two or
+          // four warps sum a block, and the first of them runs its epilogue
+          if (p.splits >= 8) {
+            const uint32_t share = p.splits >= 16 ? 4 : 2, e = warp - 2;
+            block = it.split + e / share * p.splits;
+            if (block < blocks) {
+              float4* first = reinterpret_cast<float4*>(mine) +
+                              ((block >> 2) * 8 + e % share * (8 / share)) * kTileM +
+                              (block & 3u) * 32 + lane;
+              if (share == 4)
+                sum_parts<2>(first, tile_floats, p.splits);
+              else
+                sum_parts<4>(first, tile_floats, p.splits);
+            }
+            asm volatile("bar.sync 2, 256;" ::: "memory");
+            from.splits = 1;
+            if (e % share) block = blocks;
+          }
         }
         // the warp's half of the tile at once, or its 32 x 32 blocks of a joined one
         for (; block < blocks; block += kEpilogueWarps * p.splits) {
