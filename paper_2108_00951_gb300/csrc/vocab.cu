@@ -21,6 +21,16 @@
 // (its terms cancel: the rows of a frequent word's target against its
 // probabilities elsewhere): over 32 rows in fp32, then in 64-bit fixed point,
 // whose sums do not depend on the order of their atomics.
+//
+// What bounds it: the products. Each epilogue runs under the next tile's, so its
+// 10 to 20 operations an entry are hidden from widths of about 2000 on (8192 x
+// 128,000 x 4096: 4.9 ms, 92 % of the rate that a library product of that kind
+// reaches in a burst; the board's power is at its limit), and show below (4096 x
+// 50,001 x 1024: 275 us, 81 %). The gradient's three products: 8192 x 128,000 x
+// 2048 7.9 ms, 86 %; 4096 x 50,001 x 1024 272 us for G and 484 for dh and dw. G
+// (bf16, 2 n bytes a word) is written once and read twice, mostly from DRAM:
+// 0.5 GB of traffic against 550 GFLOP at 4096 x 16,384 x 2048. Few rows (96 x
+// 65,537 x 1021, 37 us) are bound by w at 5.4 TB/s and by three launches.
 #include <cstddef>
 
 #include "product.cuh"
@@ -40,8 +50,9 @@ __device__ __forceinline__ float fixed_scale(float sum) {
   return __int_as_float((k + 127) << 23);
 }
 // Rows that carry a loss, in their order: row_map[i], targets[i] (int32), for the
-// gradient soft[i] = (-lse / ln 2, scale), and their number. One CTA: the targets are 8 bytes a row, against 2 v d
-// operations. A target >= v is malformed input: latched, the row skipped.
+// gradient soft[i] = (-lse / ln 2, scale), and their number. One CTA: the targets
+// are 8 bytes a row, against 2 v d operations. A target >= v is malformed input:
+// latched, the row skipped.
 constexpr int kRowsThreads = 1024;
 __global__ void __launch_bounds__(kRowsThreads, 1)
     vocab_rows_kernel(const int64_t* __restrict__ target, uint32_t n, uint32_t v,
