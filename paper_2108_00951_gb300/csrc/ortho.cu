@@ -296,6 +296,7 @@ __device__ __forceinline__ void load_row(const uint16_t* p, uint32_t left, uint3
 }
 
 struct StepEpilogue {
+  static constexpr bool kTurns = false;
   struct Params {
     uint32_t form;
     uint32_t exact;         // operands have a second plane

@@ -154,6 +154,7 @@ struct ProductArgs {
   uint32_t part_chunks; // 32-column chunks per scratch tile
   uint32_t* error;
   uint32_t entries;     // problems in shape[]
+  uint32_t turn;        // every other unit takes its items backwards (nothing joined)
   uint32_t* barrier;    // grid barrier: arrivals, CTAs finished (zero between launches)
   uint64_t wait_ns;
 };
@@ -297,10 +298,16 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const uint32_t prob0 = args.first[ph], prob1 = prob0 + args.problems[ph];
     const uint32_t items = args.items[ph];
     uint32_t prob = prob0;
+    // (backwards, the index passes 0 to end above `items`)
+    const bool back = Epi::kTurns && args.turn && (unit & 1u) && unit < items;
+    const uint32_t first = back ? unit + (items - unit - 1) / units * units : unit;
+    const uint32_t step = back ? 0u - units : units;
     if (warp == 0) {
       if (lane == 0) {
         fence_proxy_async();  // operands of this phase may come from the last one's epilogues
-        for (uint32_t item = unit; item < items && ok; item += units) {
+        for (uint32_t item = first; item < items && ok; item += step) {
+          if (Epi::kTurns)
+            while (item < args.shape[prob].item0) --prob;
           while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
           const ProductShape& p = args.shape[prob];
           const ProductItem it = product_item<kPair>(p, item, rank, count);
@@ -353,7 +360,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       }
     } else if (warp == 1) {
       if (lane == 0 && rank == 0) {
-        for (uint32_t item = unit; item < items && ok; item += units) {
+        for (uint32_t item = first; item < items && ok; item += step) {
+          if (Epi::kTurns)
+            while (item < args.shape[prob].item0) --prob;
           while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
           const ProductShape& p = args.shape[prob];
           const ProductItem it = product_item<kPair>(p, item, rank, count);
@@ -404,7 +413,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       const uint32_t quarter = warp & 3u;  // the lanes of tensor memory this warp may read
       const uint32_t half = (warp - 2) >> 2;
       const uint32_t row = quarter * 32 + lane;
-      for (uint32_t item = unit; item < items; item += units) {
+      for (uint32_t item = first; item < items; item += step) {
+        if (Epi::kTurns)
+          while (item < args.shape[prob].item0) --prob;
         while (prob + 1 < prob1 && item >= args.shape[prob + 1].item0) ++prob;
         const ProductShape& p = args.shape[prob];
         const ProductItem it = product_item<kPair>(p, item, rank, count);

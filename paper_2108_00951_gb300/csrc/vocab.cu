@@ -330,6 +330,7 @@ __device__ __forceinline__ void add_bias(float (&v)[32], const float* bias) {
 // Epilogue of the loss: (max, sum of exp(z - max)) of the row over the tile's
 // columns, and the target's logit from the tile that holds it.
 struct LossEpilogue {
+  static constexpr bool kTurns = false;
   struct Params {
     const uint16_t* bias;
     const int32_t* targets;
@@ -453,6 +454,7 @@ __device__ __forceinline__ float column_sum(const float (&v)[32]) {
 
 // Epilogue of the gradient's logits: G in bf16, one piece of the vocabulary.
 struct GradEpilogue {
+  static constexpr bool kTurns = false;
   struct Params {
     const uint16_t* bias;      // of the piece
     const int32_t* targets;
@@ -536,6 +538,7 @@ __device__ __forceinline__ float4* sum_block(float* sums, uint32_t row_tile, uin
 // Epilogue of dh and dw: rows of bf16 at any alignment; or fp32 sums, one set
 // per K part, added to over the pieces of the vocabulary.
 struct StoreEpilogue {
+  static constexpr bool kTurns = true;
   struct Params {
     uint16_t* out;
     uint64_t ld;
@@ -901,6 +904,11 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
   args.count = count;
   args.phases = 1;
   args.problems[0] = 2;
+  // Of few rows dh reads and dw writes: half of the SMs begin with the one, half with
+  // the other (gradient of 64 x 28,869 x 650 93 -> 80 us, 128 x 50,001 x 1024 124 ->
+  // 107, 200 x 28,869 x 656 70 -> 66; 400 x 50,001 x 1024 154 both ways, 1230 x
+  // 50,001 x 1000 299 -> 306).
+  args.turn = c.n <= 2 * kTileM ? 1 : 0;
   number_items(args, kPair);
   return launch_product<StoreEpilogue, 2, kPair>(args, ws, dev);
 }
