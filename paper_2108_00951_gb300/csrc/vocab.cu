@@ -219,6 +219,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t first = blockIdx.x * 8, i = first + warp;
   griddep_wait();
+  griddep_launch_dependents();  // the product's start needs nothing of this: 1 us less
   if (blockIdx.x >= a.ctas) {
     const bool wide = pack_wide(a.w);
     const uint64_t warps = static_cast<uint64_t>(gridDim.x - a.ctas) * 8;
