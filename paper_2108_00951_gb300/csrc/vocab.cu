@@ -30,7 +30,7 @@
 // 2048 7.9 ms, 86 %; 4096 x 50,001 x 1024 272 us for G and 484 for dh and dw. G
 // (bf16, 2 n bytes a word) is written once and read twice, mostly from DRAM:
 // 0.5 GB of traffic against 550 GFLOP at 4096 x 16,384 x 2048. Few rows (96 x
-// 65,537 x 1021, 37 us) are bound by w at 5.4 TB/s and by three launches.
+// 65,537 x 1021, 31 us) are bound by w at 5.4 TB/s and by two launches.
 #include <cstddef>
 
 #include "product.cuh"
@@ -337,14 +337,19 @@ struct LossEpilogue {
     const int32_t* targets;
     float2* pairs;     // [row][half tile]
     float* at_target;  // [row]
+    const int64_t* direct;  // != nullptr: nothing was gathered, all rows' targets
   };
   using Smem = BiasSmem;
   struct Row {
     int32_t target;
   };
-  static __device__ __forceinline__ Row prepare(const ProductShape&, const Params& e,
+  static __device__ __forceinline__ Row prepare(const ProductShape& p, const Params& e,
                                                 const ProductItem& it, uint32_t row) {
-    return {it.m0 + row < it.rows ? __ldg(e.targets + it.m0 + row) : -1};
+    const uint32_t r = it.m0 + row;
+    if (r >= it.rows) return {-1};
+    if (!e.direct) return {__ldg(e.targets + r)};
+    const int64_t t = __ldg(e.direct + r);
+    return {t >= 0 && t < static_cast<int64_t>(p.n) ? static_cast<int32_t>(t) : -1};
   }
   static __device__ __forceinline__ void tile(const ProductShape& p, const Params& e,
                                               const ProductItem& it, uint32_t row,
@@ -396,11 +401,23 @@ __global__ void __launch_bounds__(256)
     vocab_join_kernel(const float2* __restrict__ pairs, uint32_t tiles,
                       const float* __restrict__ at_target, const uint32_t* __restrict__ row_map,
                       const uint32_t* __restrict__ count, float* __restrict__ loss,
-                      float* __restrict__ lse) {
+                      float* __restrict__ lse, const int64_t* __restrict__ direct, uint32_t n,
+                      uint32_t v, uint32_t* error) {
   const uint32_t lane = threadIdx.x & 31;
   griddep_wait();
   const uint32_t r = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= *count) return;
+  if (r >= (direct ? n : *count)) return;
+  if (direct) {  // rows that take no part are here too
+    const int64_t t = direct[r];
+    if (t < 0 || t >= static_cast<int64_t>(v)) {
+      if (lane == 0) {
+        loss[r] = 0.0f;
+        lse[r] = 0.0f;
+        if (t >= 0) atomicOr(error, kDevErrBadInput);
+      }
+      return;
+    }
+  }
   const float2* mine = pairs + static_cast<uint64_t>(r) * tiles;
   float m = -INFINITY;
   bool nan = false;
@@ -424,9 +441,10 @@ __global__ void __launch_bounds__(256)
     float total = m == -INFINITY ? -INFINITY : __fadd_rn(m, logf(sum));
     if (nan) total = __int_as_float(0x7fffffff);
     const float z = at_target[r];
-    lse[row_map[r]] = total;
+    const uint32_t to = direct ? r : row_map[r];
+    lse[to] = total;
     // a target that a bias of -inf rules out has probability 0: loss +inf
-    loss[row_map[r]] = z == -INFINITY && !nan ? INFINITY : __fsub_rn(total, z);
+    loss[to] = z == -INFINITY && !nan ? INFINITY : __fsub_rn(total, z);
   }
 }
 
@@ -683,6 +701,13 @@ uint32_t piece_words(uint32_t rows, uint32_t v) {
 // rows, and with half of them empty it does half the work per SM.
 bool use_pairs(const VocabCall& c) { return c.n > kTileM; }
 
+// The loss of one tile row reads h as it lies where TMA can: gathering its rows
+// would save nothing, and what a skipped row holds stays in that row (32 x 28,869
+// x 656: 17.1 us, gathered 17.9; 96 x 65,537 x 1024: 32.1 and 37.2).
+bool takes_rows(const VocabCall& c) {
+  return c.n >= 1 && c.n <= 2 * kTileM && tma_rows(c.h, c.ldh) && tma_rows(c.w, c.ldw);
+}
+
 struct VocabPlan {
   uint32_t rows;    // rows of the gathered h: n rounded up to whole tiles
   uint32_t ld_h, ld_w, ld_g, piece;
@@ -817,16 +842,20 @@ cudaError_t loss_product(const VocabCall& c, const VocabPlan& l, const Gathered&
   ProductShape& p = args.shape[0];
   p = l.logits;
   p.bf16 = 1;
-  p.counts = 1;
-  args.count = reinterpret_cast<const uint32_t*>(base + l.count);
+  const bool direct = takes_rows(c);
+  if (!direct) {
+    p.counts = 1;
+    args.count = reinterpret_cast<const uint32_t*>(base + l.count);
+  }
   p.group_m = rows_in_l2(p, kPair);
-  if (!make_map(&p.a, base + l.h, true, c.d, l.rows, l.ld_h, 1,
-                static_cast<uint64_t>(l.rows) * l.ld_h, kTileM) ||
+  if (!(direct ? make_map(&p.a, c.h, true, c.d, c.n, c.ldh, 1, c.ldh * c.n, kTileM)
+               : make_map(&p.a, base + l.h, true, c.d, l.rows, l.ld_h, 1,
+                          static_cast<uint64_t>(l.rows) * l.ld_h, kTileM)) ||
       !make_map(&p.b, from.w, true, c.d, c.v, from.ld_w, 1, from.ld_w * c.v, b_box(p, kPair)))
     return cudaErrorInvalidValue;
   args.epi[0] = {c.bias, reinterpret_cast<const int32_t*>(base + l.targets),
                  reinterpret_cast<float2*>(base + l.pairs),
-                 reinterpret_cast<float*>(base + l.at_target)};
+                 reinterpret_cast<float*>(base + l.at_target), direct ? c.target : nullptr};
   args.phases = args.problems[0] = 1;
   number_items(args, kPair);
   return launch_product<LossEpilogue, 1, kPair>(args, ws, dev);
@@ -925,8 +954,8 @@ cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInf
   if (vocab_few(c)) return launch_vocab_few_loss(c, ws, dev);
   char* base = ws.model_scratch();
   const VocabPlan l = vocab_plan(c, false, dev);
-  Gathered from;
-  cudaError_t e = gather(c, l, base, false, ws, dev, &from);
+  Gathered from = {c.w, c.ldw};
+  cudaError_t e = takes_rows(c) ? cudaSuccess : gather(c, l, base, false, ws, dev, &from);
   if (e != cudaSuccess) return e;
   e = use_pairs(c) ? loss_product<true>(c, l, from, base, ws, dev)
                    : loss_product<false>(c, l, from, base, ws, dev);
@@ -937,7 +966,10 @@ cudaError_t launch_vocab_loss(const VocabCall& c, Workspace& ws, const DeviceInf
   const uint32_t* count = reinterpret_cast<const uint32_t*>(base + l.count);
   const uint32_t* row_map = reinterpret_cast<const uint32_t*>(base + l.row_map);
   float *loss = c.loss, *lse = c.lse;
-  void* params[] = {&pairs, &tiles, &at_target, &row_map, &count, &loss, &lse};
+  const int64_t* direct = takes_rows(c) ? c.target : nullptr;
+  uint32_t n = c.n, v = c.v, *error = ws.u32(kOffError);
+  void* params[] = {&pairs, &tiles, &at_target, &row_map, &count,
+                    &loss,  &lse,   &direct,    &n,       &v,     &error};
   return launch_kernel(reinterpret_cast<const void*>(&vocab_join_kernel), (c.n + 7) / 8, 256,
                        ws.stream, params);
 }

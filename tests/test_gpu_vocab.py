@@ -330,3 +330,23 @@ def test_skipped_rows_have_no_gradient_beside_infinite_weights(n, d):
     _, lse = loss(h, w, t)
     dh, _, _ = grad(h, w, t, lse, r)
     assert torch.all(dh[1] == 0)
+
+
+@pytest.mark.parametrize("n", [17, 128, 129, 256, 257])
+@pytest.mark.parametrize("d,pad", [(72, 0), (136, 8), (70, 2)])
+def test_rows_that_lie_on_16_bytes(n, d, pad):
+    h, w, t, r, b = inputs(n, 999, d, True, 0.3, pad, seed=8)
+    t[0], t[n - 1] = -1, 5
+    out, lse = loss(h, w, t, b)
+    _, ref_lse, ref, g, off = formula(h, w, t, r, b)
+    bound = 2 * off + 2.0 ** -18 * (1 + ref_lse.abs() + ref.abs())
+    assert bool(((lse.double() - ref_lse).abs() <= bound).all())
+    assert bool(((out.double() - ref).abs() <= bound).all())
+    h[t < 0] = float("nan")
+    again, lse_again = loss(h, w, t, b)
+    assert torch.equal(again, out) and torch.equal(lse_again, lse)
+    assert efs.ef_check_status() == efs.EF_OK
+    t[3] = 999
+    again, _ = loss(h, w, t, b)
+    assert again[3] == 0 and torch.equal(again[4:], out[4:])
+    assert efs.ef_check_status() == efs.EF_ERR_BAD_INPUT
