@@ -871,15 +871,21 @@ __global__ void __launch_bounds__(256)
   const uint32_t per = (slices + 7) / 8, lo = run * per, hi = min(lo + per, slices);
   const float* p = sums + static_cast<uint64_t>(token) * ld_sum + c;
   const uint64_t stride = static_cast<uint64_t>(tokens) * ld_sum;
+  const int64_t t = target[token];
   float x = 0.0f;
-#pragma unroll 8
-  for (uint32_t s = lo; s < hi; ++s) x = __fadd_rn(x, __ldcg(p + s * stride));
+  for (uint32_t s0 = lo; s0 < hi; s0 += 10) {  // (151 slices: two rounds of loads)
+    float y[10];
+#pragma unroll
+    for (uint32_t j = 0; j < 10; ++j) y[j] = __ldcg(p + min(s0 + j, hi - 1) * stride);
+#pragma unroll
+    for (uint32_t j = 0; j < 10; ++j)
+      if (s0 + j < hi) x = __fadd_rn(x, y[j]);
+  }
   s_part[run][lane] = x;
   __syncthreads();
   if (run == 0 && c < cols) {
     for (int r = 1; r < 8; ++r) x = __fadd_rn(x, s_part[r][lane]);
     // a skipped row's G is 0, but w may hold infinities
-    const int64_t t = target[token];
     if (t < 0 || t >= static_cast<int64_t>(v)) x = 0.0f;
     dh[token * ld + c] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
   }
