@@ -50,7 +50,7 @@ __device__ __forceinline__ float fixed_scale(float sum) {
   return __int_as_float((k + 127) << 23);
 }
 // Rows that carry a loss, in their order: row_map[i], targets[i] (int32), for the
-// gradient soft[i] = (-lse / ln 2, scale), and their number. One CTA: the targets
+// gradient soft[i] = (lse, scale), and their number. One CTA: the targets
 // are 8 bytes a row, against 2 v d operations. A target >= v is malformed input:
 // latched, the row skipped.
 constexpr int kRowsThreads = 1024;
@@ -87,8 +87,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       targets[before] = static_cast<int32_t>(t);
       if (soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
         const float x = lse[i];
-        soft[before] = x == -INFINITY ? make_float2(0.0f, 0.0f)
-                                      : make_float2(__fmul_rn(x, -kLog2e), row_scale[i]);
+        soft[before] = x == -INFINITY ? make_float2(0.0f, 0.0f) : make_float2(x, row_scale[i]);
         abs_sum = __fadd_rn(abs_sum, fabsf(row_scale[i]));
       }
     } else if (i < n && loss) {
@@ -274,8 +273,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
         a.targets[at] = static_cast<int32_t>(t);
         if (a.soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
           const float x = a.lse[i];
-          a.soft[at] = x == -INFINITY ? make_float2(0.0f, 0.0f)
-                                      : make_float2(__fmul_rn(x, -kLog2e), a.row_scale[i]);
+          a.soft[at] = x == -INFINITY ? make_float2(0.0f, 0.0f) : make_float2(x, a.row_scale[i]);
         }
       }
       const uint16_t* from = a.h + i * a.ld;
@@ -326,6 +324,15 @@ __device__ __forceinline__ void add_bias(float (&v)[32], const float* bias) {
     v[4 * j + 2] = __fadd_rn(v[4 * j + 2], b.z);
     v[4 * j + 3] = __fadd_rn(v[4 * j + 3], b.w);
   }
+}
+
+// exp(z - top) is taken as 2^(z log2e + shift), shift = -top log2e. A top beyond
+// 2.35e38 (a mask of the type's lowest value on all the words looked at) takes
+// that out of fp32's range: there z - top replaces z, and the shift is 0.
+__device__ __forceinline__ bool out_of_range(float shift) { return fabsf(shift) == INFINITY; }
+__device__ __forceinline__ void lower_by(float (&v)[32], float top) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = __fsub_rn(v[j], top);
 }
 
 // Epilogue of the loss: (max, sum of exp(z - max)) of the row over the tile's
@@ -380,14 +387,19 @@ struct LossEpilogue {
 #pragma unroll
       for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
       const float higher = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), m);
-      const float shift = higher == -INFINITY ? 0.0f : __fmul_rn(higher, -kLog2e);
+      float shift = higher == -INFINITY ? 0.0f : __fmul_rn(higher, -kLog2e);
+      if (out_of_range(shift)) {
+        lower_by(v, higher);
+        shift = 0.0f;
+      }
       float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(v[j], kLog2e, shift)));
       const float rest = __fadd_rn(__fadd_rn(part[0], part[1]), __fadd_rn(part[2], part[3]));
       // m == higher also covers both -inf (nothing summed so far)
-      const float scale = m == higher ? 1.0f : exp2_fast(__fmaf_rn(m, kLog2e, shift));
+      const float scale =
+          m == higher ? 1.0f : exp2_fast(__fmul_rn(__fsub_rn(m, higher), kLog2e));
       sum = __fmaf_rn(sum, scale, rest);
       m = higher;
     }
@@ -502,7 +514,9 @@ struct GradEpilogue {
                                               const ProductItem& it, uint32_t row, uint32_t,
                                               Smem& s, const ProductAcc& acc, uint32_t, Row state) {
     const uint32_t r = it.m0 + row, target = state.target;
-    const float shift = state.soft.x, scale = state.soft.y;
+    const float lse = state.soft.x, scale = state.soft.y;
+    const bool far = out_of_range(__fmul_rn(lse, -kLog2e));
+    const float shift = far ? 0.0f : __fmul_rn(lse, -kLog2e);
     const bool dead = scale == 0.0f;  // past the rows, or without a gradient
     stage_bias(e.bias, it.n0 + acc.c0 * 32, (acc.c1 - acc.c0) * 32, p.n, s);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
@@ -510,6 +524,7 @@ struct GradEpilogue {
       acc.load(c, v);
       const uint32_t col0 = it.n0 + c * 32;
       if (e.bias) add_bias(v, s.bias + (c - acc.c0) * 32);
+      if (far) lower_by(v, lse);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         v[j] = __fmul_rn(exp2_fast(__fmaf_rn(v[j], kLog2e, shift)), scale);

@@ -203,11 +203,15 @@ __device__ __forceinline__ void stage_h(const FewArgs& a, uint16_t* s_h, uint32_
   }
 }
 
+// exp(z - top), for any finite z and top.
+__device__ __forceinline__ float exp_below(float z, float top) {
+  return exp2_fast(__fmul_rn(__fsub_rn(z, top), kLog2e));
+}
 // (max, sum of exp(z - max)) pairs joined; (-inf, 0) is empty.
 __device__ __forceinline__ void join_pair(float& m, float& s, float m2, float s2) {
   const float top = fmaxf(m, m2);
-  const float a = m == top ? 1.0f : exp2_fast(__fmul_rn(__fsub_rn(m, top), kLog2e));
-  const float b = m2 == top ? 1.0f : exp2_fast(__fmul_rn(__fsub_rn(m2, top), kLog2e));
+  const float a = m == top ? 1.0f : exp_below(m, top);
+  const float b = m2 == top ? 1.0f : exp_below(m2, top);
   // -inf on one side only: a factor 0; on both: factors 1 of empty sums
   s = __fmaf_rn(s, a, __fmul_rn(s2, b));
   m = top;
@@ -219,7 +223,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_kernel(const FewA
   extern __shared__ __align__(16) uint16_t s_dyn[];  // the warps' rings, then h
   __shared__ float2 s_pair[kFewWarps][kTokens];
   __shared__ int64_t s_target[kTokens];
-  __shared__ float s_shift[kTokens], s_scale[kTokens];
+  __shared__ float s_lse[kTokens], s_scale[kTokens];
   __shared__ uint32_t s_last;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t row = lane >> 2, quad = lane & 3u;
@@ -236,7 +240,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_kernel(const FewA
     if (kGrad) {
       float lse = t < a.n ? a.lse[t] : -INFINITY;  // (its load does not wait for the target's)
       if (target < 0) lse = -INFINITY;
-      s_shift[t] = __fmul_rn(lse, -kLog2e);
+      s_lse[t] = lse;
       // a row that is skipped, or has no word with a probability: no gradient
       s_scale[t] = lse == -INFINITY ? 0.0f : a.row_scale[t];
     }
@@ -314,7 +318,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_kernel(const FewA
           const float scale = s_scale[token];
           float g = 0.0f;
           if (scale != 0.0f && v < a.v) {
-            g = __fmul_rn(exp2_fast(__fmaf_rn(z[j], kLog2e, s_shift[token])), scale);
+            g = __fmul_rn(exp_below(z[j], s_lse[token]), scale);
             if (static_cast<int64_t>(v) == s_target[token]) g = __fsub_rn(g, scale);
           }
           z[j] = g;
@@ -663,7 +667,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
   constexpr uint32_t kTokens = 8 * kNT, kPart = kNT * 128;
   extern __shared__ __align__(16) uint16_t s_dyn[];
   __shared__ int64_t s_target[kTokens];
-  __shared__ float s_shift[kTokens], s_scale[kTokens];
+  __shared__ float s_lse[kTokens], s_scale[kTokens];
   const uint32_t lane = threadIdx.x & 31;
   const uint32_t warps = a.windows, team = (threadIdx.x >> 5) / warps, warp = (threadIdx.x >> 5) % warps;
   const uint32_t thread = warp * 32 + lane, threads = warps * 32, c0 = warp * kCols;
@@ -703,7 +707,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
     }
     if (target < 0) lse = -INFINITY;
     s_target[t] = target;
-    s_shift[t] = __fmul_rn(lse, -kLog2e);
+    s_lse[t] = lse;
     // a row that is skipped, or has no word with a probability: no gradient
     s_scale[t] = lse == -INFINITY ? 0.0f : scale;
   }
@@ -802,7 +806,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
           const float scale = s_scale[token];
           float g = 0.0f;
           if (scale != 0.0f && v < a.v) {
-            g = __fmul_rn(exp2_fast(__fmaf_rn(z[t], kLog2e, s_shift[token])), scale);
+            g = __fmul_rn(exp_below(z[t], s_lse[token]), scale);
             if (static_cast<int64_t>(v) == s_target[token]) g = __fsub_rn(g, scale);
           }
           db = __fadd_rn(db, g);
