@@ -8,7 +8,9 @@
 // Rows with a negative target take no part: the rows that do are gathered
 // first (compaction, as everywhere in this library), so a batch of which a
 // share carries no loss costs that share less, and nothing in a skipped row
-// of h, not even a NaN, reaches a result.
+// of h, not even a NaN, reaches a result. To the gradient a row whose
+// log-sum-exp is -inf (no word has a probability) is such a row too: its G is 0,
+// but 0 times an infinity of h or w would not be.
 //
 // Loss: one product whose epilogue keeps, per row and tile of the vocabulary,
 // the largest logit and the sum of exponentials below it; a row's pairs are
@@ -53,6 +55,15 @@ __device__ __forceinline__ float fixed_scale(float sum) {
 // gradient soft[i] = (lse, scale), and their number. One CTA: the targets
 // are 8 bytes a row, against 2 v d operations. A target >= v is malformed input:
 // latched, the row skipped.
+__device__ __forceinline__ bool takes_part(int64_t target, uint32_t v) {
+  return target >= 0 && target < static_cast<int64_t>(v);
+}
+// `lse`: of the gradient's rows (nullptr in the loss call).
+__device__ __forceinline__ bool takes_part(const int64_t* target, const float* lse, uint32_t i,
+                                           uint32_t v) {
+  const float x = lse ? lse[i] : 0.0f;
+  return takes_part(__ldg(target + i), v) && x != -INFINITY;
+}
 constexpr int kRowsThreads = 1024;
 __global__ void __launch_bounds__(kRowsThreads, 1)
     vocab_rows_kernel(const int64_t* __restrict__ target, uint32_t n, uint32_t v,
@@ -70,7 +81,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   for (uint32_t n0 = 0; n0 < n; n0 += kRowsThreads) {
     const uint32_t i = n0 + threadIdx.x;
     const int64_t t = i < n ? target[i] : -1;
-    const bool keep = t >= 0 && t < static_cast<int64_t>(v);
+    const bool keep = i < n && takes_part(target, soft ? lse : nullptr, i, v);
     bad |= t >= static_cast<int64_t>(v);
     const uint32_t ballot = __ballot_sync(0xffffffffu, keep);
     if (lane == 0) s_warp[warp] = __popc(ballot);
@@ -85,9 +96,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     if (keep) {
       row_map[before] = i;
       targets[before] = static_cast<int32_t>(t);
-      if (soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
-        const float x = lse[i];
-        soft[before] = x == -INFINITY ? make_float2(0.0f, 0.0f) : make_float2(x, row_scale[i]);
+      if (soft) {
+        soft[before] = make_float2(lse[i], row_scale[i]);
         abs_sum = __fadd_rn(abs_sum, fabsf(row_scale[i]));
       }
     } else if (i < n && loss) {
@@ -155,12 +165,12 @@ __device__ __forceinline__ void pack_row(const PackArgs& a, uint64_t i, uint32_t
 __device__ __forceinline__ bool pack_wide(const PackArgs& a) {
   return reinterpret_cast<uintptr_t>(a.src) % 16 == 0 && a.ld % 8 == 0;
 }
-// zero_rows (optional): of the `rows` rows, those whose target is skipped are
-// zeroed there.
+// zero_rows (optional): of the `rows` rows, those that take no part are zeroed
+// there.
 __global__ void __launch_bounds__(256)
     vocab_pack_kernel(const PackArgs a, uint32_t rows, const uint32_t* __restrict__ count,
                       uint16_t* zero_rows, uint64_t zero_ld, const int64_t* __restrict__ target,
-                      uint32_t v) {
+                      const float* __restrict__ lse, uint32_t v) {
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t warps = static_cast<uint64_t>(gridDim.x) * 8;
   const bool vec = pack_wide(a);
@@ -169,11 +179,8 @@ __global__ void __launch_bounds__(256)
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); i < a.rows_out;
        i += warps) {
     pack_row(a, i, have, vec);
-    if (zero_rows && i < rows) {
-      const int64_t t = target[i];
-      if (t < 0 || t >= static_cast<int64_t>(v))
-        for (uint32_t c = lane; c < a.cols; c += 32) zero_rows[i * zero_ld + c] = 0;
-    }
+    if (zero_rows && i < rows && !takes_part(target, lse, static_cast<uint32_t>(i), v))
+      for (uint32_t c = lane; c < a.cols; c += 32) zero_rows[i * zero_ld + c] = 0;
   }
 }
 
@@ -226,14 +233,13 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
       pack_row(a.w, r, a.w.rows_out, wide);
     return;
   }
-  auto keeps = [&](int64_t t) { return t >= 0 && t < static_cast<int64_t>(a.v); };
+  auto keeps = [&](uint32_t j) { return takes_part(a.target, a.soft ? a.lse : nullptr, j, a.v); };
   uint32_t before = 0, total = 0;
   bool bad = false;
 #pragma unroll 4
   for (uint32_t j = threadIdx.x; j < a.n; j += 256) {
-    const int64_t t = __ldg(a.target + j);
-    const uint32_t k = keeps(t) ? 1u : 0u;
-    bad |= t >= static_cast<int64_t>(a.v);
+    const uint32_t k = keeps(j) ? 1u : 0u;
+    bad |= __ldg(a.target + j) >= static_cast<int64_t>(a.v);
     before += j < first ? k : 0u;
     total += k;
   }
@@ -255,7 +261,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
     if (a.fixed) {
       float x = 0.0f;
       for (uint32_t j = threadIdx.x; j < a.n; j += 256)
-        if (keeps(__ldg(a.target + j))) x = __fadd_rn(x, fabsf(a.row_scale[j]));
+        if (keeps(j)) x = __fadd_rn(x, fabsf(a.row_scale[j]));
       x = block_sum_8(x, s_abs);
       if (threadIdx.x == 0) *a.fixed = fixed_scale(x);
     }
@@ -265,16 +271,13 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const GatherArgs a) {
     const int64_t t = __ldg(a.target + i);
     // of this CTA's rows, those before this warp's
     const uint32_t mine = __ballot_sync(
-        0xffffffffu, lane < warp && keeps(__ldg(a.target + (lane < warp ? first + lane : i))));
-    if (keeps(t)) {
+        0xffffffffu, lane < warp && keeps(lane < warp ? first + lane : i));
+    if (keeps(i)) {
       const uint32_t at = before + __popc(mine);
       if (lane == 0) {
         a.row_map[at] = i;
         a.targets[at] = static_cast<int32_t>(t);
-        if (a.soft) {  // a row whose lse is -inf has no word with a probability, and no gradient
-          const float x = a.lse[i];
-          a.soft[at] = x == -INFINITY ? make_float2(0.0f, 0.0f) : make_float2(x, a.row_scale[i]);
-        }
+        if (a.soft) a.soft[at] = make_float2(a.lse[i], a.row_scale[i]);
       }
       const uint16_t* from = a.h + i * a.ld;
       for (uint32_t c = lane * 8; c < a.d; c += 256)
@@ -517,7 +520,7 @@ struct GradEpilogue {
     const float lse = state.soft.x, scale = state.soft.y;
     const bool far = out_of_range(__fmul_rn(lse, -kLog2e));
     const float shift = far ? 0.0f : __fmul_rn(lse, -kLog2e);
-    const bool dead = scale == 0.0f;  // past the rows, or without a gradient
+    const bool dead = scale == 0.0f;  // past the rows, or scaled by 0
     stage_bias(e.bias, it.n0 + acc.c0 * 32, (acc.c1 - acc.c0) * 32, p.n, s);
     for (uint32_t c = acc.c0; c < acc.c1; ++c) {
       float v[32];
@@ -810,7 +813,7 @@ cudaError_t gather(const VocabCall& c, const VocabPlan& l, char* base, bool grad
   float* fixed = gradient && c.dbias ? reinterpret_cast<float*>(base + l.fixed) : nullptr;
   auto pack = [&](PackArgs a, uint32_t rows, const uint32_t* cnt, uint16_t* zero, uint64_t zero_ld) {
     const uint32_t want = (a.rows_out + 7) / 8, grid = want < 8 * sms ? want : 8 * sms;
-    void* params[] = {&a, &rows, &cnt, &zero, &zero_ld, &target, &v};
+    void* params[] = {&a, &rows, &cnt, &zero, &zero_ld, &target, &lse, &v};
     return launch_kernel(reinterpret_cast<const void*>(&vocab_pack_kernel), grid, 256, ws.stream,
                          params);
   };

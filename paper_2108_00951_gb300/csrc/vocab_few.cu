@@ -407,9 +407,16 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_kernel(const FewA
   }
 }
 
+// Whether a row has a gradient: a target, and a word with a probability. (Those
+// that have none have G = 0, but their h, or w, may hold infinities.)
+__device__ __forceinline__ bool has_gradient(int64_t target, float lse, uint32_t v) {
+  return target >= 0 && target < static_cast<int64_t>(v) && lse != -INFINITY;
+}
+
 struct FewGradArgs {
   const uint16_t *h, *w;
   const int64_t* target;
+  const float* lse;
   const uint32_t* g;
   uint64_t ldh, ldw, lddw;
   uint32_t n, v, d;
@@ -578,14 +585,14 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_grad_kernel(const
   uint32_t ht[kNT][8];
   {
     uint32_t x[kTokens];
-    int64_t target[kTokens];
+    bool has[kTokens];
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t) target[t] = t < static_cast<int>(a.n) ? a.target[t] : -1;
+    for (int t = 0; t < kTokens; ++t)
+      has[t] = t < static_cast<int>(a.n) && has_gradient(a.target[t], a.lse[t], a.v);
     load_tokens<kTokens>(x, a.h, a.ldh, a.n, c0 + lane * 2, a.d);
 #pragma unroll
     for (int t = 0; t < kTokens; ++t)
-      *reinterpret_cast<uint32_t*>(tile + t * kTileLd + lane * 2) =
-          target[t] >= 0 && target[t] < static_cast<int64_t>(a.v) ? x[t] : 0u;
+      *reinterpret_cast<uint32_t*>(tile + t * kTileLd + lane * 2) = has[t] ? x[t] : 0u;
   }
   __syncwarp();
 #pragma unroll
@@ -691,9 +698,13 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
   // (h's loads start ahead of the ring's copies, which fill the memory pipe; no
   // load waits for a target)
   int64_t targets[kTokens];
+  float lses[kTokens];
   uint32_t x[kTokens];
 #pragma unroll
-  for (uint32_t t = 0; t < kTokens; ++t) targets[t] = t < a.n ? a.target[t] : -1;
+  for (uint32_t t = 0; t < kTokens; ++t) {
+    targets[t] = t < a.n ? a.target[t] : -1;
+    lses[t] = t < a.n ? a.lse[t] : 0.0f;
+  }
   load_tokens<kTokens>(x, a.h, a.ldh, a.n, c0 + lane * 2, a.d);
 #pragma unroll
   for (uint32_t i = 0; i < kOnceDeep - 1; ++i) fetch();
@@ -712,14 +723,15 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
     s_scale[t] = lse == -INFINITY ? 0.0f : scale;
   }
   // h of the warp's columns as the operand of the logits (columns along K) and,
-  // through the ring's last tile, of dw (tokens along K); nothing of a skipped row
+  // through the ring's last tile, of dw (tokens along K); nothing of a row without
+  // a gradient
   uint32_t hk[kNT][8], ht[kNT][8];
   {
     uint16_t* tile = ring + (kOnceDeep - 1) * kTileElemsFew;
 #pragma unroll
     for (uint32_t t = 0; t < kTokens; ++t)
       *reinterpret_cast<uint32_t*>(tile + t * kTileLd + lane * 2) =
-          targets[t] >= 0 && targets[t] < static_cast<int64_t>(a.v) ? x[t] : 0u;
+          has_gradient(targets[t], lses[t], a.v) ? x[t] : 0u;
     __syncwarp();
 #pragma unroll
     for (int t = 0; t < kNT; ++t)
@@ -867,7 +879,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 1) vocab_few_once_kernel(const
 __global__ void __launch_bounds__(256)
     vocab_few_dh_kernel(const float* __restrict__ sums, uint32_t slices, uint32_t tokens,
                         uint32_t ld_sum, uint32_t cols, uint16_t* __restrict__ dh, uint64_t ld,
-                        const int64_t* __restrict__ target, uint32_t v) {
+                        const int64_t* __restrict__ target, const float* __restrict__ lse,
+                        uint32_t v) {
   __shared__ float s_part[8][32];
   const uint32_t lane = threadIdx.x & 31, run = threadIdx.x >> 5;
   const uint32_t c = blockIdx.x * 32 + lane, token = blockIdx.y;
@@ -875,7 +888,7 @@ __global__ void __launch_bounds__(256)
   const uint32_t per = (slices + 7) / 8, lo = run * per, hi = min(lo + per, slices);
   const float* p = sums + static_cast<uint64_t>(token) * ld_sum + c;
   const uint64_t stride = static_cast<uint64_t>(tokens) * ld_sum;
-  const int64_t t = target[token];
+  const bool has = has_gradient(target[token], lse[token], v);
   float x = 0.0f;
   for (uint32_t s0 = lo; s0 < hi; s0 += 10) {  // (151 slices: two rounds of loads)
     float y[10];
@@ -889,8 +902,7 @@ __global__ void __launch_bounds__(256)
   __syncthreads();
   if (run == 0 && c < cols) {
     for (int r = 1; r < 8; ++r) x = __fadd_rn(x, s_part[r][lane]);
-    // a skipped row's G is 0, but w may hold infinities
-    if (t < 0 || t >= static_cast<int64_t>(v)) x = 0.0f;
+    if (!has) x = 0.0f;
     dh[token * ld + c] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
   }
 }
@@ -1068,7 +1080,7 @@ cudaError_t launch_vocab_few_grad(const VocabCall& c, Workspace& ws, const Devic
     const FewArgs a = few_args(c, p, base, ws);
     e = p.nt == 1 ? few_logits<true, 1>(a, p, align, ws) : few_logits<true, 2>(a, p, align, ws);
     if (e != cudaSuccess) return e;
-    FewGradArgs g = {c.h, c.w, c.target, a.g, c.ldh, c.ldw, c.lddw, c.n, c.v, c.d,
+    FewGradArgs g = {c.h, c.w, c.target, c.lse, a.g, c.ldh, c.ldw, c.lddw, c.n, c.v, c.d,
                      p.windows, p.slices, p.slice_groups, c.dw, align_dw, sums, ld};
     e = p.nt == 1 ? few_grad<1>(g, align, dev, ws) : few_grad<2>(g, align, dev, ws);
   }
@@ -1077,8 +1089,9 @@ cudaError_t launch_vocab_few_grad(const VocabCall& c, Workspace& ws, const Devic
   uint16_t* dh = c.dh;
   uint64_t ld_dh = c.lddh;
   const int64_t* target = c.target;
+  const float* lse = c.lse;
   uint32_t v = c.v;
-  void* params[] = {&sums, &slices, &tokens, &ld_sum, &cols, &dh, &ld_dh, &target, &v};
+  void* params[] = {&sums, &slices, &tokens, &ld_sum, &cols, &dh, &ld_dh, &target, &lse, &v};
   e = launch_pdl(reinterpret_cast<const void*>(&vocab_few_dh_kernel), dim3((c.d + 31) / 32, c.n), 256, 0,
                  ws.stream, params, false);
   if (e == cudaSuccess) count_launch();
