@@ -55,6 +55,31 @@ ef_status device_info(int dev, DeviceInfo* out) {
   return EF_OK;
 }
 
+// Whether calls on the stream are being captured into a graph. (The legacy
+// stream answers with an error while another stream is: it is not itself.)
+bool capturing(cudaStream_t stream) {
+  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(stream, &st) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return st != cudaStreamCaptureStatusNone;
+}
+
+// Frees an allocation that growth replaces, or keeps it for the graphs that
+// refer to it.
+void replace_block(char*& block, bool captured, std::vector<char*>& kept) {
+  if (!captured) {
+    cudaFree(block);
+  } else {
+    try {
+      kept.push_back(block);
+    } catch (const std::bad_alloc&) {  // kept all the same, until the process ends
+    }
+  }
+  block = nullptr;
+}
+
 // Find or grow the workspace of (current device, stream). Growth
 // synchronises the stream once; the new header and tile-status array start
 // at zero.
@@ -62,6 +87,7 @@ ef_status acquire_workspace(cudaStream_t stream, uint32_t tiles, uint32_t cand_c
                             size_t offsets, size_t stage, Workspace** out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
+  const bool captured = capturing(stream);
   std::lock_guard<std::mutex> lk(g_mu);
   Workspace*& ws = g_workspaces[std::make_pair(dev, stream)];
   if (!ws) {
@@ -84,17 +110,17 @@ ef_status acquire_workspace(cudaStream_t stream, uint32_t tiles, uint32_t cand_c
   }
   if (!ws->base || tiles > ws->status_tiles || cand_cap > ws->cand_cap ||
       offsets > ws->offsets_cap || stage > ws->stage_cap) {
+    if (ws->base) {
+      if (cudaStreamSynchronize(stream) != cudaSuccess) return EF_ERR_CUDA;
+      replace_block(ws->base, ws->base_captured, ws->old_bases);
+      ws->base_captured = false;
+    }
     Workspace grown = *ws;
     if (tiles > grown.status_tiles) grown.status_tiles = tiles;
     if (cand_cap > grown.cand_cap) grown.cand_cap = cand_cap;
     if (offsets > grown.offsets_cap) grown.offsets_cap = offsets;
     if (stage > grown.stage_cap) grown.stage_cap = stage;
     const size_t bytes = grown.total_bytes();
-    if (ws->base) {
-      if (cudaStreamSynchronize(stream) != cudaSuccess) return EF_ERR_CUDA;
-      cudaFree(ws->base);
-      ws->base = nullptr;
-    }
     void* p = nullptr;
     if (cudaMalloc(&p, bytes) != cudaSuccess) {
       cudaGetLastError();
@@ -124,13 +150,27 @@ ef_status acquire_workspace(cudaStream_t stream, uint32_t tiles, uint32_t cand_c
         cudaMemsetAsync(ws->model_base, 0, kModelArrivalBytes, stream) != cudaSuccess)
       return EF_ERR_CUDA;
   }
+  ws->base_captured |= captured;
   *out = ws;
   return EF_OK;
 }
 
 // The workspace of (current device, stream) with `bytes` of model scratch.
-// Growth synchronises the stream once; the arrival counters start at zero.
+// Growth synchronises the stream once; the arrival counters start at zero. A
+// call that is being captured cannot grow it: its graph would zero the counters
+// at each replay, not now.
 ef_status acquire_model_scratch(cudaStream_t stream, size_t bytes, Workspace** out) {
+  const bool captured = capturing(stream);
+  if (captured) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
+    std::lock_guard<std::mutex> lk(g_mu);
+    const auto it = g_workspaces.find(std::make_pair(dev, stream));
+    if (it == g_workspaces.end() || !it->second->base || !it->second->model_base ||
+        it->second->model_bytes < bytes)
+      return EF_ERR_NO_MEMORY;
+    it->second->model_captured = true;
+  }
   const ef_status st = acquire_workspace(stream, 0, 0, 0, 0, out);
   if (st != EF_OK) return st;
   Workspace* ws = *out;
@@ -138,8 +178,8 @@ ef_status acquire_model_scratch(cudaStream_t stream, size_t bytes, Workspace** o
   if (ws->model_base && ws->model_bytes >= bytes) return EF_OK;
   if (ws->model_base) {
     if (cudaStreamSynchronize(stream) != cudaSuccess) return EF_ERR_CUDA;
-    cudaFree(ws->model_base);
-    ws->model_base = nullptr;
+    replace_block(ws->model_base, ws->model_captured, ws->old_model_bases);
+    ws->model_captured = false;
     ws->model_bytes = 0;
   }
   void* p = nullptr;
@@ -785,14 +825,27 @@ ef_status ef_check_status(ef_stream_t stream) {
     ws = it->second;
   }
   uint32_t bits = 0;
-  uint32_t* dev_err = ws->u32(efs::kOffError);
-  if (cudaMemcpyAsync(&bits, dev_err, sizeof bits, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
-      cudaStreamSynchronize(s) != cudaSuccess)
-    return EF_ERR_CUDA;
+  auto take_bits = [&](char* base) {  // of a workspace's header, which is cleared
+    uint32_t* word = reinterpret_cast<uint32_t*>(base + efs::kOffError);
+    uint32_t x = 0;
+    if (cudaMemcpyAsync(&x, word, sizeof x, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+        cudaStreamSynchronize(s) != cudaSuccess)
+      return false;
+    bits |= x;
+    return x == 0 || (cudaMemsetAsync(word, 0, sizeof x, s) == cudaSuccess &&
+                      cudaStreamSynchronize(s) == cudaSuccess);
+  };
+  if (!take_bits(ws->base)) return EF_ERR_CUDA;
+  for (char* base : ws->old_bases)  // those that replays of graphs write
+    if (!take_bits(base)) return EF_ERR_CUDA;
   if (bits == 0) return EF_OK;
-  if (cudaMemsetAsync(dev_err, 0, sizeof bits, s) != cudaSuccess ||
-      cudaStreamSynchronize(s) != cudaSuccess)
+  // replays clear nothing themselves: counters that a wait left mid-way start again
+  for (char* base : ws->old_model_bases)
+    if (cudaMemsetAsync(base, 0, efs::kModelArrivalBytes, s) != cudaSuccess) return EF_ERR_CUDA;
+  if (ws->model_base &&
+      cudaMemsetAsync(ws->model_base, 0, efs::kModelArrivalBytes, s) != cudaSuccess)
     return EF_ERR_CUDA;
+  if (cudaStreamSynchronize(s) != cudaSuccess) return EF_ERR_CUDA;
   {
     // a wait that ran out, or a selection that stopped early, may leave
     // barrier counters or histograms mid-way: re-clear the workspace before
@@ -824,6 +877,8 @@ ef_status ef_workspace_release(void) {
     if (it->first.first == dev) {
       if (it->second->base) cudaFree(it->second->base);
       if (it->second->model_base) cudaFree(it->second->model_base);
+      for (char* old : it->second->old_bases) cudaFree(old);
+      for (char* old : it->second->old_model_bases) cudaFree(old);
       if (it->second->density_host) cudaFreeHost(it->second->density_host);
       if (it->second->lw) {
         if (it->second->lw->dev) cudaFree(it->second->lw->dev);

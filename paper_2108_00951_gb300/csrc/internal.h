@@ -151,6 +151,10 @@ struct Workspace {
   // launches), then what a call lays out for itself.
   char* model_base = nullptr;
   size_t model_bytes = 0;
+  // A graph keeps the addresses that its calls were captured with: what growth
+  // replaces after that is kept until the workspace is released.
+  bool base_captured = false, model_captured = false;
+  std::vector<char*> old_bases, old_model_bases;
   uint32_t* model_arrivals() const { return reinterpret_cast<uint32_t*>(model_base); }
   char* model_scratch() const { return model_base + kModelArrivalBytes; }
 
