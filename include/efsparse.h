@@ -66,15 +66,15 @@
  * its own beside that workspace, grown and released likewise; each entry's
  * comment gives its size.
  *
- * Graphs: a call may be captured into a CUDA graph once an earlier call on the
- * stream has grown the workspace to its size. The graph holds the workspace's
- * addresses: an allocation that a captured call uses is kept when a later call
- * needs a larger one, until ef_workspace_release(), after which those graphs
- * must not be replayed. Replays are calls on the stream of the capture: order
- * them with its other calls; ef_check_status(stream) reports theirs too. A
- * call of ef_vocab_loss, ef_vocab_loss_grad or ef_orthogonalize that would have
- * to grow its scratch while it is captured returns EF_ERR_NO_MEMORY and leaves
- * the capture valid.
+ * Graphs: a call of ef_vocab_loss, ef_vocab_loss_grad or ef_orthogonalize may be
+ * captured into a CUDA graph once an earlier call on the stream has grown the
+ * scratch to its size (one that would have to grow it while it is captured
+ * returns EF_ERR_NO_MEMORY and leaves the capture valid). The graph holds the
+ * scratch's address: it is kept when a later call needs a larger one, and so is
+ * the workspace that any captured call uses, until ef_workspace_release(), after
+ * which those graphs must not be replayed. Replays are calls on the stream of
+ * the capture: order them with its other calls; ef_check_status(stream) reports
+ * theirs too.
  *
  * Calls on
  * DIFFERENT streams never share a workspace and may run concurrently; calls
