@@ -150,7 +150,7 @@ template <bool kBf16>
 __global__ void __launch_bounds__(kSmallThreads, 1)
     ortho_small_kernel(const __grid_constant__ SmallArgs args) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t s_done;
+  __shared__ uint64_t s_done, s_drained;
   __shared__ uint32_t s_tmem;
   __shared__ FF s_ff[32];
   __shared__ alignas(16) float2 s_norm[kMaxCluster];  // written as 8 bytes by the other CTAs
@@ -170,6 +170,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
   uint8_t* ql = qh + squares * kTileBytes;
   if (tid == 0) {
     mbar_init(&s_done, 1);
+    mbar_init(&s_drained, 1);
     mbar_init_fence();
   }
   if (warp == 0) tmem_alloc<false>(&s_tmem, 512);
@@ -444,7 +445,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1)
       }
     }
   }
-  if (!ok) atomicOr(args.error, kDevErrTimeout);
+  if (!ok) {
+    atomicOr(args.error, kDevErrTimeout);
+    if (tid == 0) {  // a wait ran out: no product may run after the CTA's end
+      mma_commit<false>(&s_drained);
+      mbar_wait(&s_drained, 0, kDrainNs);
+    }
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();

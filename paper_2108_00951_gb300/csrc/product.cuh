@@ -30,7 +30,8 @@
 // launch): what one phase's epilogues write the next one's TMA reads.
 //
 // Every wait on an mbarrier is bounded (tma.cuh); one that runs out latches a
-// timeout, and the CTA ends without its results.
+// timeout, and the CTA ends without its results, after the copies that it has
+// under way have landed and its products are done (bounded likewise).
 #pragma once
 
 #include "internal.h"
@@ -160,7 +161,7 @@ struct ProductArgs {
 };
 
 struct ProductSmem {
-  uint64_t full[6], empty[6], acc_full[2], acc_empty[2];
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drained;
   uint32_t tmem, joined;
   uint32_t failed;  // an epilogue warp's wait ran out
 };
@@ -229,6 +230,9 @@ __device__ __forceinline__ void sum_parts(float4* first, uint64_t stride, uint32
   for (int j = 0; j < kUnits; ++j) __stcg(first + j * kTileM, sum[j]);
 }
 
+// How long a CTA that gives up waits for what it has under way.
+constexpr uint64_t kDrainNs = 10000000;
+
 // Waits until a counter has reached `target` (modulo 2^32).
 __device__ __forceinline__ bool wait_count(const uint32_t* word, uint32_t target, uint64_t limit_ns) {
   const uint64_t t0 = global_timer_ns();
@@ -275,6 +279,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       mbar_init(&s.acc_full[i], 1);
       mbar_init(&s.acc_empty[i], kEpilogueWarps * (kPair ? 2 : 1));
     }
+    mbar_init(&s.drained, 1);
     mbar_init_fence();
   }
   if (warp == 0)
@@ -527,7 +532,25 @@ __global__ void __launch_bounds__(kProductThreads, 1)
   }
   __syncwarp();
   tc_fence_before();
-  __syncthreads();
+  if (!__syncthreads_and(ok)) {
+    // a wait ran out: no copy may land and no product run after the CTA's end
+    if (warp == 0 && lane == 0) {
+      const uint64_t t0 = global_timer_ns();
+      if (rank == 0)  // the last fill of every stage
+        for (uint32_t i = 0; i < R::kStages; ++i)
+          mbar_wait(&s.full[i], i < stage ? phase : phase ^ 1u, kDrainNs);
+      // A pair's copies all count on rank 0's barriers, whose phases stay open where
+      // the two CTAs stopped at different ones: there the time has to do.
+      if (kPair)
+        for (uint32_t i = 0; i < (1u << 20) && global_timer_ns() - t0 < kDrainNs; ++i)
+          __nanosleep(1000);
+    }
+    if (warp == 1 && lane == 0 && rank == 0) {
+      mma_commit<kPair>(&s.drained);
+      mbar_wait(&s.drained, 0, kDrainNs);
+    }
+    __syncthreads();
+  }
   if (kPair) cluster_sync();  // the other CTA's shared memory may be in use until here
   tc_fence_after();
   if (warp == 1) tmem_free<kPair>(tmem, 512);
