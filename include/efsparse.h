@@ -465,6 +465,11 @@ ef_status ef_hard_threshold_noalloc(const float* g, float* e, float gamma, float
  * exact, sums fp32. A word of logit -inf has probability 0: a target on one
  * has loss +inf; a row of nothing else has lse -inf. NaN and +inf logits make
  * the row's loss and lse NaN. The outputs must not overlap an input.
+ *
+ * Overlap, in this entry and the next two: matrices whose rows have one stride
+ * in bytes, such as column blocks of a buffer, overlap where they share an
+ * element, others where the address ranges do from their first element to
+ * their last.
  */
 ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
                         const uint16_t* bias, const int64_t* target, uint64_t n, uint64_t v,

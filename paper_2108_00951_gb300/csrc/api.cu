@@ -360,9 +360,31 @@ ef_status topk_layerwise_entry(const void* g, bool bf16, float* e, float gamma, 
                        ws);
 }
 
-// Bytes a matrix of 16-bit elements spans.
-size_t span16(uint64_t rows, uint64_t cols, uint64_t ld) {
-  return rows ? static_cast<size_t>((rows - 1) * ld + cols) * 2 : 0;
+// A matrix in memory, in bytes: rows of `width`, `stride` apart.
+struct Rows {
+  uintptr_t at;
+  uint64_t rows, width, stride;
+  // (2^57 bytes from there: past any address; and nothing overflows)
+  uintptr_t end() const {
+    const uint64_t most = 1ull << 57;
+    return at + (rows - 1 > most / stride ? most : (rows - 1) * stride + width);
+  }
+};
+Rows rows_of(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t size) {
+  return {reinterpret_cast<uintptr_t>(p), p && cols ? rows : 0, cols * size, ld * size};
+}
+Rows vector_of(const void* p, uint64_t bytes) { return rows_of(p, 1, bytes, bytes, 1); }
+
+// Whether two matrices overlap: where their rows have one stride (column blocks
+// of a buffer), whether they share a byte; else whether the ranges do that they
+// lie in.
+bool overlaps(const Rows& a, const Rows& b) {
+  if (a.rows == 0 || b.rows == 0 || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
+  const uint64_t stride = a.rows > 1 ? a.stride : b.stride;
+  const uint64_t apart = b.at >= a.at ? (b.at - a.at) % stride : stride - (a.at - b.at - 1) % stride - 1;
+  return apart < a.width || b.width > stride - apart;
 }
 
 constexpr uint64_t kMaxRows = 1u << 30, kMaxWords = 1u << 30, kMaxWidth = 1u << 20;
@@ -385,31 +407,31 @@ ef_status vocab_entry(VocabCall c, uint64_t n, uint64_t v, uint64_t d, bool grad
   c.n = static_cast<uint32_t>(n);
   c.v = static_cast<uint32_t>(v);
   c.d = static_cast<uint32_t>(d);
-  const void* in[] = {c.h, c.w, c.bias, c.target, gradient ? c.lse : nullptr, c.row_scale};
-  const size_t in_n[] = {span16(n, d, c.ldh), span16(v, d, c.ldw), v * 2, n * 8, n * 4, n * 4};
-  const void* outs[3];
-  size_t out_n[3];
+  const Rows in[] = {rows_of(c.h, n, d, c.ldh, 2), rows_of(c.w, v, d, c.ldw, 2),
+                     vector_of(c.bias, v * 2),     vector_of(c.target, n * 8),
+                     vector_of(gradient ? c.lse : nullptr, n * 4), vector_of(c.row_scale, n * 4)};
+  Rows outs[3];
   if (gradient) {
     if (!c.dw || !aligned(c.dw, 2) || c.lddw < d || c.lddw > kMaxLd) return EF_ERR_INVALID_ARG;
     if (!aligned(c.dbias, 2) || (c.dbias && !c.bias)) return EF_ERR_INVALID_ARG;
     if (n && (!c.dh || !aligned(c.dh, 2) || c.lddh < d || c.lddh > kMaxLd || !c.row_scale ||
               !aligned(c.row_scale, 4)))
       return EF_ERR_INVALID_ARG;
-    outs[0] = c.dh, out_n[0] = span16(n, d, c.lddh);
-    outs[1] = c.dw, out_n[1] = span16(v, d, c.lddw);
-    outs[2] = c.dbias, out_n[2] = v * 2;
+    outs[0] = rows_of(c.dh, n, d, c.lddh, 2);
+    outs[1] = rows_of(c.dw, v, d, c.lddw, 2);
+    outs[2] = vector_of(c.dbias, v * 2);
   } else {
     if (n == 0) return EF_OK;
     if (!c.loss || !aligned(c.loss, 4)) return EF_ERR_INVALID_ARG;
-    outs[0] = c.loss, out_n[0] = n * 4;
-    outs[1] = c.lse, out_n[1] = n * 4;
-    outs[2] = nullptr, out_n[2] = 0;
+    outs[0] = vector_of(c.loss, n * 4);
+    outs[1] = vector_of(c.lse, n * 4);
+    outs[2] = vector_of(nullptr, 0);
   }
   for (int o = 0; o < 3; ++o) {
-    for (int i = 0; i < 6; ++i)
-      if (overlaps(outs[o], out_n[o], in[i], in_n[i])) return EF_ERR_INVALID_ARG;
+    for (const Rows& i : in)
+      if (overlaps(outs[o], i)) return EF_ERR_INVALID_ARG;
     for (int q = o + 1; q < 3; ++q)
-      if (overlaps(outs[o], out_n[o], outs[q], out_n[q])) return EF_ERR_INVALID_ARG;
+      if (overlaps(outs[o], outs[q])) return EF_ERR_INVALID_ARG;
   }
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
@@ -434,11 +456,12 @@ ef_status orthogonalize_entry(uint32_t n, const uint64_t* rows, const uint64_t* 
   if (!rows || !cols || !u || !ld_u || !out || !ld_out || (m && !ld_m)) return EF_ERR_INVALID_ARG;
   const size_t usz = bf16 ? 2 : 4;
   std::vector<OrthoMat> mats(n);
-  std::vector<std::pair<uintptr_t, std::pair<uintptr_t, bool>>> spans;  // begin, (end, written)
-  auto span = [&](const void* p, uint64_t r, uint64_t c, uint64_t ld, size_t size, bool written) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    spans.push_back({at, {at + ((r - 1) * ld + c) * size, written}});
+  struct Used {
+    Rows rows;
+    bool written;
   };
+  std::vector<Used> used;
+  used.reserve(3ull * n);
   for (uint32_t i = 0; i < n; ++i) {
     OrthoMat& t = mats[i];
     if (rows[i] > kMaxSide || cols[i] > kMaxSide) return EF_ERR_INVALID_ARG;
@@ -455,18 +478,25 @@ ef_status orthogonalize_entry(uint32_t n, const uint64_t* rows, const uint64_t* 
     if (!aligned(t.u, usz) || !aligned(t.m, 4) || !aligned(t.out, 2)) return EF_ERR_INVALID_ARG;
     if (t.ld_u < t.cols || t.ld_out < t.cols || (m && t.ld_m < t.cols)) return EF_ERR_INVALID_ARG;
     if (t.ld_u > kMaxLd || t.ld_out > kMaxLd || t.ld_m > kMaxLd) return EF_ERR_INVALID_ARG;
-    span(t.u, t.rows, t.cols, t.ld_u, usz, false);
-    if (m) span(t.m, t.rows, t.cols, t.ld_m, 4, true);
-    span(t.out, t.rows, t.cols, t.ld_out, 2, true);
+    used.push_back({rows_of(t.u, t.rows, t.cols, t.ld_u, usz), false});
+    if (m) used.push_back({rows_of(t.m, t.rows, t.cols, t.ld_m, 4), true});
+    used.push_back({rows_of(t.out, t.rows, t.cols, t.ld_out, 2), true});
   }
-  if (spans.empty()) return EF_OK;
-  // nothing written may overlap anything else: by start, the furthest end so far
-  std::sort(spans.begin(), spans.end());
-  uintptr_t end_any = 0, end_written = 0;
-  for (const auto& s : spans) {
-    if (s.first < (s.second.second ? end_any : end_written)) return EF_ERR_INVALID_ARG;
-    if (s.second.first > end_any) end_any = s.second.first;
-    if (s.second.second && s.second.first > end_written) end_written = s.second.first;
+  if (used.empty()) return EF_OK;
+  // nothing written may overlap anything else: by start, against those before that
+  // reach that far
+  std::sort(used.begin(), used.end(),
+            [](const Used& x, const Used& y) { return x.rows.at < y.rows.at; });
+  std::vector<Used> open;
+  for (const Used& s : used) {
+    size_t kept = 0;
+    for (const Used& o : open) {
+      if (o.rows.end() <= s.rows.at) continue;
+      if ((o.written || s.written) && overlaps(o.rows, s.rows)) return EF_ERR_INVALID_ARG;
+      open[kept++] = o;
+    }
+    open.resize(kept);
+    open.push_back(s);
   }
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return EF_ERR_CUDA;
