@@ -550,7 +550,7 @@ size_t shape_products(Args& args, const Plan& plan, size_t g0, uint32_t count) {
     args.first[ph] = entry * count;
     args.problems[ph] = count;
   }
-  return number_items(args, plan.pair);
+  return number_items(args, plan.pair, kPartCounters);
 }
 
 // Kernel parameters for 1, 4 or kOrthoGroups shapes: a launch copies them.

@@ -35,11 +35,11 @@
 #pragma once
 
 #include "internal.h"
+#include "product_items.h"
 #include "tensor.cuh"
 
 namespace efs {
 
-constexpr uint32_t kTileM = 128;    // rows of a CTA's tile: lanes of tensor memory
 constexpr uint32_t kTileNMax = 256; // columns of a tile, at most
 constexpr uint32_t kTileK = 128;    // per stage: two 128-byte swizzle rows of 16-bit elements
 constexpr uint32_t kEpilogueWarps = 8;
@@ -751,33 +751,8 @@ void plan_product(ProductShape& p, const ProductWant& w);
 // Rows and columns of B a CTA loads at a time (the box of a K-major operand).
 inline uint32_t b_box(const ProductShape& p, bool pair) { return pair ? p.bn / 2 : p.bn; }
 
-// Numbers the items of each phase's problems and the scratch tiles of split
-// ones; returns the scratch tiles' bytes.
-template <class Args>
-size_t number_items(Args& args, bool pair) {
-  size_t most = 0;
-  uint32_t chunks = 0;
-  for (uint32_t ph = 0; ph < args.phases; ++ph) {
-    uint32_t items = 0, parts = 0;
-    for (uint32_t i = args.first[ph]; i < args.first[ph] + args.problems[ph]; ++i) {
-      ProductShape& p = args.shape[i];
-      p.item0 = items;
-      p.part0 = parts;
-      items += p.tiles * p.batch * p.splits;
-      if (p.splits > 1 && p.join) {
-        parts += p.tiles * p.batch * p.splits * (pair ? 2 : 1);
-        chunks = p.bn / 32 > chunks ? p.bn / 32 : chunks;
-      }
-    }
-    args.items[ph] = items;
-    most = parts > most ? parts : most;
-  }
-  args.part_chunks = chunks;
-  for (uint32_t ph = 0; ph < args.phases; ++ph)
-    if (args.first[ph] + args.problems[ph] > args.entries)
-      args.entries = args.first[ph] + args.problems[ph];
-  return most > kModelArrivals - 2 ? ~static_cast<size_t>(0) : most * chunks * 32 * kTileM * 4;
-}
+// Arrival counters of joined K parts; two words after them are the grid barrier.
+constexpr uint32_t kPartCounters = kModelArrivals - 2;
 
 // The caller has numbered the items and set args.parts.
 template <class Epi, int kMaxProblems, bool kPair>
@@ -789,7 +764,7 @@ cudaError_t launch_product(ProductArgs<Epi, kMaxProblems>& args, Workspace& ws,
   if (items == 0) return cudaSuccess;
   args.arrivals = ws.model_arrivals();
   args.error = ws.u32(kOffError);
-  args.barrier = ws.model_arrivals() + kModelArrivals - 2;
+  args.barrier = ws.model_arrivals() + kPartCounters;
   args.wait_ns = wait_limit_ns();
   auto fn = product_kernel<Epi, kMaxProblems, kPair>;
   constexpr uint32_t smem = Ring<kPair>::kBytes + 1024;

@@ -875,7 +875,7 @@ cudaError_t loss_product(const VocabCall& c, const VocabPlan& l, const Gathered&
                  reinterpret_cast<float2*>(base + l.pairs),
                  reinterpret_cast<float*>(base + l.at_target), direct ? c.target : nullptr};
   args.phases = args.problems[0] = 1;
-  number_items(args, kPair);
+  number_items(args, kPair, kPartCounters);
   return launch_product<LossEpilogue, 1, kPair>(args, ws, dev);
 }
 
@@ -915,7 +915,7 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
                    c.dbias ? reinterpret_cast<uint32_t*>(db + c.v) + v0 : nullptr,
                    reinterpret_cast<const float*>(base + l.fixed)};
     args.phases = args.problems[0] = 1;
-    number_items(args, kPair);
+    number_items(args, kPair, kPartCounters);
     const cudaError_t e = launch_product<GradEpilogue, 1, kPair>(args, ws, dev);
     if (e != cudaSuccess) return e;
   }
@@ -957,7 +957,7 @@ cudaError_t grad_piece(const VocabCall& c, const VocabPlan& l, const Gathered& f
   // 107, 200 x 28,869 x 656 70 -> 66; 400 x 50,001 x 1024 154 both ways, 1230 x
   // 50,001 x 1000 299 -> 306).
   args.turn = c.n <= 2 * kTileM ? 1 : 0;
-  number_items(args, kPair);
+  number_items(args, kPair, kPartCounters);
   return launch_product<StoreEpilogue, 2, kPair>(args, ws, dev);
 }
 
