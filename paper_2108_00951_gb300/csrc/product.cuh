@@ -46,7 +46,7 @@ constexpr uint32_t kEpilogueWarps = 8;
 constexpr uint32_t kProductThreads = (2 + kEpilogueWarps) * 32;
 constexpr uint32_t kBoxMnBytes = 64 * kTileK * 2;  // an MN-major box: 64 elements x 128 k
 
-// Stages of the ring: 192 KB either way.
+// Stages of the ring: 192 KB either way (a pair's are smaller, and more).
 template <bool kPair>
 struct Ring {
   static constexpr uint32_t kStages = kPair ? 3 : 2;
@@ -161,7 +161,7 @@ struct ProductArgs {
 };
 
 struct ProductSmem {
-  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drained;
+  uint64_t full[Ring<true>::kStages], empty[Ring<true>::kStages], acc_full[2], acc_empty[2], drained;
   uint32_t tmem, joined;
   uint32_t failed;  // an epilogue warp's wait ran out
 };

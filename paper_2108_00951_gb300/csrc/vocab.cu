@@ -752,15 +752,17 @@ VocabPlan vocab_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
     at += align256(bytes);
     return here;
   };
-  l.row_map = take(4ull * l.rows);
-  l.targets = take(4ull * l.rows);
-  l.count = take(4);
+  if (gradient || !takes_rows(c)) {  // the gathered rows
+    l.row_map = take(4ull * l.rows);
+    l.targets = take(4ull * l.rows);
+    l.count = take(4);
+    l.h = take(2ull * l.rows * l.ld_h);
+  }
   if (gradient) l.soft = take(8ull * l.rows);
   if (gradient && c.dbias) {
     l.fixed = take(4);
     l.db = take(12ull * c.v);  // sums, then marks
   }
-  l.h = take(2ull * l.rows * l.ld_h);
   if (!tma_rows(c.w, c.ldw)) l.w = take(2ull * c.v * l.ld_w);
   l.piece = gradient ? piece_words(l.rows, c.v) : c.v;
   plan_product(l.logits, {n, l.piece, c.d, 1, false, pair, sms, 1, 1, 12.0, true});

@@ -44,7 +44,6 @@ constexpr uint32_t kCols = 64;            // columns of a tile
 constexpr uint32_t kTileLd = kCols + 8;   // its row stride in shared memory: no bank conflicts
 constexpr uint32_t kRing = 4;             // tiles of a warp's ring
 constexpr uint32_t kTileElemsFew = 16 * kTileLd;
-constexpr uint32_t kMaxSlices = 512;      // of the words, in the second pass
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                           uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -935,7 +934,7 @@ FewPlan few_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
   p.windows = d_pad / kCols;
   // One pass where a CTA's warps cover the columns.
   p.once = gradient && p.windows <= kFewWarps;
-  if (!p.once) {
+  if (!gradient) {
     p.pairs = take(sizeof(float2) * p.ctas * tokens);
     p.at_target = take(sizeof(float) * tokens);
   }
@@ -948,9 +947,7 @@ FewPlan few_plan(const VocabCall& c, bool gradient, const DeviceInfo& dev) {
       const uint32_t used = (groups + p.slice_groups - 1) / p.slice_groups;
       p.slices = (used + p.teams - 1) / p.teams;  // CTAs
     } else {
-      uint32_t slices = kFewWarps * sms / p.windows;  // 16 warps per SM
-      if (slices < 1) slices = 1;
-      if (slices > kMaxSlices) slices = kMaxSlices;
+      const uint32_t slices = kFewWarps * sms / p.windows;  // 16 warps per SM, 17 to 71 windows
       p.slice_groups = (groups + slices - 1) / slices;
       p.slices = (groups + p.slice_groups - 1) / p.slice_groups;
     }
