@@ -84,8 +84,8 @@
  * call below 1024, see ef_test_set_stream_kernel) the streaming kernel's CTAs
  * wait (bounded) only for lower-numbered CTAs of the same launch, which the
  * device dispatches first; kernels that wait on every CTA
- * of their grid (the Top-k select, the layer-wise select with teams) are
- * cooperative launches. If kernels on other streams or other processes (MPS)
+ * of their grid (the Top-k select, the layer-wise select with teams, the phases
+ * of ef_orthogonalize) are cooperative launches. If kernels on other streams or other processes (MPS)
  * hold SMs long enough that a CTA cannot start within the bound (2 s), the
  * call fails with EF_ERR_TIMEOUT (reported by ef_check_status); it never
  * hangs and never returns a wrong result. From there on, the streaming
@@ -461,10 +461,18 @@ ef_status ef_hard_threshold_noalloc(const float* g, float* e, float gamma, float
  *   loss_out   [out] fp32[n].  lse_out [out] fp32[n].
  *
  * h, w, bias may start at any 2-byte boundary; rows on 16-byte boundaries
- * (ldw a multiple of 8, w 16-byte aligned) save a copy of w. Products are
- * exact, sums fp32. A word of logit -inf has probability 0: a target on one
- * has loss +inf; a row of nothing else has lse -inf. NaN and +inf logits make
- * the row's loss and lse NaN. The outputs must not overlap an input.
+ * (ldw a multiple of 8, w 16-byte aligned) save a copy of w in calls of more
+ * than 16 rows. Products are exact, sums fp32: the tensor cores add 16 products
+ * to a sum at a time and may truncate, so a logit is off by at most
+ * (d / 16 + 4) 2^-23 of the sum of its terms' magnitudes. A word of logit -inf
+ * has probability 0: a target on one has loss +inf; a row of nothing else has
+ * lse -inf. (A mask of bf16's lowest value works likewise, but a row of nothing
+ * else has the mask's value as its lse, in fp32, and loss 0.) NaN and +inf
+ * logits make the row's loss and lse NaN. The outputs must not overlap an input.
+ * Scratch, with n rounded up to 256 and d to 64: up to 16 rows (of at most 4536
+ * columns up to 8 rows, of 2232 up to 16) 20 KB; else 2 n d bytes of gathered h
+ * and 8 n (neither where there are at most 256 rows and h and w lie on 16
+ * bytes), 4 n, 16 n per 64 to 256 words, and 2 v d where w has to be copied.
  *
  * Overlap, in this entry and the next two: matrices whose rows have one stride
  * in bytes, such as column blocks of a buffer, overlap where they share an
@@ -489,13 +497,19 @@ ef_status ef_vocab_loss(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint
  *   The other arguments as for ef_vocab_loss. The outputs are overwritten and
  *   must not overlap an input or one another.
  *
- * dh and dw: G is rounded to bf16 (relative 2^-8 at most; up to 16 rows keep
- * 16 bits of it) before its products, which are summed in fp32 and rounded
- * once. dbias is summed from G before that rounding. A row whose lse is -inf
- * has no gradient. Equal inputs give equal bits. Scratch: G for a piece of the
- * vocabulary, at most 1 GB (or 4096 n bytes if that is more), the gathered h,
- * up to 32 fp32 partial sums of dh, and w where its rows are not 16-byte
- * aligned.
+ * dh and dw: G is rounded to bf16 (relative 2^-8 at most; up to 8 rows of at
+ * most 4536 columns, and up to 16 of at most 2232, keep 16 bits of it) before
+ * its products, which are summed in fp32 and rounded once. dbias is summed from
+ * G before that rounding, above 16 rows in steps of 2^-60 of the sum of
+ * |row_scale| or finer. A row whose lse is -inf has no gradient: it takes no
+ * part, as a row with a negative target. Equal inputs give equal bits.
+ * Scratch, n and d rounded as above: G for a piece of the vocabulary, at most
+ * 1 GB (or 4096 n bytes if that is more), 2 n d of gathered h and 16 n, up to 32
+ * fp32 partial sums of dh (4 n d each), 12 v with dbias, and 2 v d where w has to
+ * be copied. Of the few rows that keep 16 bits: up to 1024 columns a partial sum
+ * of dh (64 d bytes, 32 up to 8 rows) per SM, beyond that 143 of them at most and
+ * 64 bytes a word. It stays allocated until a larger call or
+ * ef_workspace_release().
  */
 ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w, uint64_t ldw,
                              const uint16_t* bias, const int64_t* target, const float* lse,
@@ -526,12 +540,18 @@ ef_status ef_vocab_loss_grad(const uint16_t* h, uint64_t ldh, const uint16_t* w,
  * Products have fp16 operands (scaled, 11 bits) and fp32 sums; the result is
  * within about 2e-3 of the exact one (2-norm, relative), before its rounding
  * to bf16. |U|_F is summed in fp32 pairs: |U|_F^2 must be within the range of
- * fp32 (a matrix whose squares all underflow gives 0, as a zero matrix does).
+ * fp32, and entries below 1e-19, whose squares are subnormal, lose bits in it (a
+ * matrix whose squares all underflow gives 0, as a zero matrix does).
  * A NaN or infinity makes its whole matrix NaN. Equal inputs give equal bits.
- * Scratch: 5 bytes per entry and 4 per entry of the squares on the shorter
- * side (both 8 where that side is at most 128), and 64 KB per split tile; none
- * where every matrix fits on chip (a shorter side of at most 128 and up to
- * a few thousand columns).
+ * A call is one cooperative launch per 12 shapes, whose CTAs wait (bounded) for
+ * one another, beside two launches per 48 matrices.
+ * None of that where every matrix fits on chip (a shorter side of at most 128 and,
+ * with it, up to 2048 to 4096 columns) in at most three layouts of a cluster: a
+ * launch per layout and 64 matrices, no scratch. Otherwise scratch, with columns
+ * rounded up to 64 (much for a tall matrix of few): 5 bytes per entry and 4 per
+ * entry of the square on the shorter side (8 and 8 where that side is at most
+ * 128), 4 KB a matrix, and 64 KB for each of the at most 16 parts of a
+ * 128 x 128 tile that is cut along its depth (256 KB of a 256 x 256 one).
  */
 ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t* cols,
                            const void* const* u, const uint64_t* ld_u, ef_grad_type u_type,
