@@ -30,11 +30,11 @@
 //
 // What bounds it: matrices of a few thousand a side the tensor cores and the
 // power they draw (VGG-16's three fully connected ones 6.8 ms, 63 % of the burst
-// rate of a library product). Smaller ones the phases: a grid barrier and the
+// rate of a library product, at the board's cap: 1358 W, 1.61 GHz). Smaller ones the phases: a grid barrier and the
 // start of the pipeline take 3 us each, the join of K parts 4; and where the
 // shorter side is a few hundred, L2: an X tile of 256 x 256 x 512 moves 450 KB
 // through each SM in 4.9 us. 256 x 2304: 151 us, ten a phase; ResNet-18's 21
-// matrices 366 (A 19, B 11, X 31 a step); six of 2600 x 650 372.
+// matrices 370 (A 19.5, B 12, X 32.7 a step); six of 2600 x 650 375.
 #include "product.cuh"
 
 #include <algorithm>

@@ -20,7 +20,7 @@
 // roundings out). dw = G^T h has K = the tokens' hi and lo, dh = G w K = 16
 // words; partial sums of dh are added in order by a kernel of their own.
 // - Up to 1024 columns: one pass over w (vocab_few_once_kernel).
-//   5 x 28,869 x 650: 24 us with w in L2, 31.5 without, 75 MB read and written.
+//   5 x 28,869 x 650: 24 us with w in L2, 32.5 without, 75 MB read and written.
 // - Wider rows, whose columns do not fit an SM's warps: the logits leave G in
 //   memory, 32 or 64 bytes a word, and a second pass over w (from L2 while w is
 //   below about 100 MB) gives a warp 64 columns and a slice of the words. On
