@@ -34,6 +34,8 @@
 // under way have landed and its products are done (bounded likewise).
 #pragma once
 
+#include <atomic>
+
 #include "internal.h"
 #include "product_items.h"
 #include "tensor.cuh"
@@ -771,7 +773,8 @@ cudaError_t launch_product(ProductArgs<Epi, kMaxProblems>& args, Workspace& ws,
   static_assert(smem + sizeof(typename Epi::Smem) * kEpilogueWarps + 512 <= 227 * 1024,
                 "stages and epilogue buffers fit an SM");
   static_assert(sizeof(args) <= 32764, "kernel parameters");
-  static bool ready[64] = {};  // per device: opted into the ring's shared memory
+  // per device: opted into the ring's shared memory (by any of its threads)
+  static std::atomic<bool> ready[64] = {};
   if (ws.device >= 64 || !ready[ws.device]) {
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
