@@ -351,7 +351,7 @@ def _encode(x, key, random):
     e = torch.frexp(mag.amax(dim=1)).exponent.sub_(1).clamp_(min=LEAST)
     e = torch.where(mag.amax(dim=1) > 0, e, LEAST)
     low = (e - top + 1)[:, None]  # the exponent of f = 1
-    at = torch.maximum(torch.frexp(mag).exponent - 1, low)
+    at = torch.where(mag > 0, torch.maximum(torch.frexp(mag).exponent - 1, low), low)
     up = 0.5 if random is None else (random.float() + 0.5) / 65536.0
     code = (at - low) * 8 + torch.floor(mag * _power(3 - at) + up).to(torch.int32)
     if key == "v":
