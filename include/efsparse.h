@@ -62,14 +62,15 @@
  * (number of streams used) x that size; ef_workspace_release() frees all
  * workspaces of the current device (for example after a phase that used
  * extra streams), and ef_hard_threshold_noalloc needs none. ef_vocab_loss,
- * ef_vocab_loss_grad and ef_orthogonalize keep their scratch in an allocation of
- * its own beside that workspace, grown and released likewise; each entry's
- * comment gives its size.
+ * ef_vocab_loss_grad, ef_orthogonalize, ef_embed, ef_embed_grad and
+ * ef_layer_norm_grad keep their scratch in an allocation of its own beside that
+ * workspace, grown and released likewise; each entry's comment gives its size.
  *
- * Graphs: a call of ef_vocab_loss, ef_vocab_loss_grad or ef_orthogonalize may be
- * captured into a CUDA graph once an earlier call on the stream has grown the
- * scratch to its size (one that would have to grow it while it is captured
- * returns EF_ERR_NO_MEMORY and leaves the capture valid). The graph holds the
+ * Graphs: a call of ef_vocab_loss, ef_vocab_loss_grad, ef_orthogonalize, ef_embed,
+ * ef_embed_grad or ef_layer_norm_grad may be captured into a CUDA graph once an
+ * earlier call on the stream has grown the scratch to its size (one that would
+ * have to grow it while it is captured returns EF_ERR_NO_MEMORY and leaves the
+ * capture valid). The graph holds the
  * scratch's address: it is kept when a later call needs a larger one, and so is
  * the workspace that any captured call uses, until ef_workspace_release(), after
  * which those graphs must not be replayed. Replays are calls on the stream of
@@ -557,6 +558,157 @@ ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t*
                            const void* const* u, const uint64_t* ld_u, ef_grad_type u_type,
                            float* const* m, const uint64_t* ld_m, float momentum,
                            uint16_t* const* out, const uint64_t* ld_out, ef_stream_t stream);
+
+/*
+ * ef_embed — rows of an embedding table by token:
+ *
+ *     out[i] = scale table[token[i]]
+ *
+ *   table      [in]  fp32 or bf16 (table_type) [v][d], rows ld_table apart.
+ *   token      [in]  int64[n]; a negative one is padding: its row of out is 0. A
+ *                    token >= v is latched as EF_ERR_BAD_INPUT, its row is 0.
+ *   n, v, d    0 <= n <= 2^30, 1 <= v <= 2^30, 1 <= d <= 2^20.
+ *   scale      finite.
+ *   out        [out] fp32 or bf16 (out_type) [n][d], rows ld_out apart, rounded
+ *                    once from the fp32 product; must not overlap an input.
+ *
+ * Here and in the next entries: row strides are in elements, at least d and at
+ * most 2^36; pointers are aligned to their elements (rows on 16-byte boundaries
+ * are fastest, then rows of an even number of elements). Equal inputs give
+ * equal bits. Scratch: a call on a new stream allocates its workspace.
+ */
+ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type,
+                   const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale, void* out,
+                   uint64_t ld_out, ef_grad_type out_type, ef_stream_t stream);
+
+/*
+ * ef_embed_grad — gradient of an embedding table:
+ *
+ *     dtable[w] = scale sum over i with token[i] = w of dout[i]
+ *
+ *   dout       [in]  fp32 or bf16 (dout_type) [n][d], rows ld_dout apart. Rows of
+ *                    padding (negative tokens) are not used, nor are rows of a
+ *                    token >= v, which is latched as EF_ERR_BAD_INPUT.
+ *   accumulate 0: all v rows of dtable are written, zero where no token is w.
+ *              Else the sums are added to what is there (the decoder's gradient
+ *              of tied weights); rows whose token does not occur stay untouched.
+ *   dtable     [in/out] fp32 or bf16 (dtable_type) [v][d], rows ld_dtable apart;
+ *                    must not overlap an input.
+ *
+ * Sums are fp32, in an order that n, v, d and the tokens fix, rounded once.
+ * Scratch above 2048 tokens: 16 bytes a token, a fp32 row of d for each 16
+ * tokens (each 64 from 65,536 tokens on), and at most 2.4 MB.
+ */
+ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
+                        const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,
+                        int accumulate, void* dtable_out, uint64_t ld_dtable,
+                        ef_grad_type dtable_type, ef_stream_t stream);
+
+/*
+ * ef_layer_norm — layer norm over rows of d values:
+ *
+ *     mean = sum x / d,  rstd = (sum (x - mean)^2 / d + eps)^(-1/2),
+ *     y = (x - mean) rstd weight + bias
+ *
+ *   x          [in]  fp32 or bf16 (x_type) [n][d], rows ldx apart.
+ *   weight, bias [in] fp32 or bf16 (w_type) [d], each may be NULL (1 and 0).
+ *   eps        finite, at least 0.
+ *   n, d       0 <= n <= 2^30, 1 <= d <= 2^20.
+ *   y          [out] fp32 or bf16 (y_type) [n][d], rows ldy apart.
+ *   mean_out, rstd_out [out] fp32[n] for ef_layer_norm_grad, each may be NULL.
+ *   No output may overlap an input or another.
+ *
+ * Both sums are fp32, the second over differences from the mean. A NaN or an
+ * infinity makes its row NaN. No scratch; may be captured at any time.
+ */
+ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
+                        const void* bias, ef_grad_type w_type, float eps, uint64_t n, uint64_t d,
+                        void* y_out, uint64_t ldy, ef_grad_type y_type, float* mean_out,
+                        float* rstd_out, ef_stream_t stream);
+
+/*
+ * ef_layer_norm_grad — gradient of layer norm, with x' = (x - mean) rstd and
+ * q = dy weight:
+ *
+ *     dx = rstd (q - sum q / d - x' sum(q x') / d)
+ *     dweight = sum over rows of dy x',   dbias = sum over rows of dy
+ *
+ *   x, weight  [in]  as given to ef_layer_norm; mean, rstd as it wrote them.
+ *   dy         [in]  fp32 or bf16 (dy_type) [n][d], rows lddy apart.
+ *   dx_out     [out] of x's type [n][d], rows lddx apart, or NULL.
+ *   dweight_out, dbias_out [out] of w_type [d], each may be NULL.
+ *   No output may overlap an input or another.
+ *
+ * Sums are fp32, those over rows by CTAs and then over the CTAs in order.
+ * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA, of which
+ * there are at most four an SM (1216 shares of longer rows than 28,000).
+ */
+ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
+                             ef_grad_type w_type, const float* mean, const float* rstd,
+                             const void* dy, uint64_t lddy, ef_grad_type dy_type, uint64_t n,
+                             uint64_t d, void* dx_out, uint64_t lddx, void* dweight_out,
+                             void* dbias_out, ef_stream_t stream);
+
+/*
+ * ef_adamw — one AdamW step over a list of tensors, in one launch per 400 of
+ * them (for example with the gradient that an exchange has summed):
+ *
+ *     g <- grad_scale g,  m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *     p <- p (1 - lr weight_decay)
+ *          - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *
+ *   n_tensors  0 <= n_tensors <= 2^20. The following are HOST arrays of that many.
+ *   numel      at most 2^32 - 4096 each; a tensor without entries is passed over.
+ *   p          [in/out] DEVICE pointers, fp32.
+ *   g          [in]  DEVICE pointers, fp32 or bf16 (g_type).
+ *   m, v       [in/out] DEVICE pointers, fp32; or codes of 8 bits (uint8) where
+ *                    m_exponents and v_exponents are given.
+ *   m_exponents, v_exponents [in/out] DEVICE pointers, uint8[ceil(numel / 128)], or NULL.
+ *                    States in 8 bits start as zeros in codes and exponents.
+ *   copies     [out] DEVICE pointers, bf16[numel]: p rounded (for the next step's
+ *                    products), or NULL.
+ *   lr, eps, weight_decay finite, eps at least 0; beta1, beta2 in [0, 1).
+ *   step       the step's number, from 1 on.
+ *   seed       of the rounding of 8-bit states; unused without them.
+ *   lr_dev, step_dev, grad_scale [in] one fp32, int64, fp32 in device memory, or
+ *                    NULL: where given, they are read when the step runs, in
+ *                    place of lr and step (a step below 1 counts as 1) and as the
+ *                    factor of g, so that a captured call's replays can differ.
+ *   Pointers are aligned to their elements (all of a tensor's on 16 bytes, its
+ *   codes on 4, is fastest). Nothing that is written may overlap anything else.
+ *
+ * m and v are fp32, each operation rounded by itself; p is updated within
+ * 2^-20 of the update. A NaN or infinity stays within its entry.
+ *
+ * States in 8 bits: 128 consecutive entries of a tensor share a byte E + 127, E
+ * the exponent of their largest magnitude (at least -92). A code is an exponent
+ * field f above three bits k (m: a sign and 4 bits of f; v: 5 bits) and
+ * stands for (8 + k) 2^(E - top + f - 3), or k 2^(E - top - 2) where f = 0, top = 14 in m and
+ * 30 in v. Rounding is stochastic, with 16 random bits that seed, step and the
+ * entry's place fix: on the average a state moves as one in fp32 does. A positive v
+ * is held as a positive one. What is not below 2^127 is held as NaN (the
+ * highest code). No scratch; may be captured at any time. Equal inputs give
+ * equal bits.
+ */
+ef_status ef_adamw(uint32_t n_tensors, const uint64_t* numel, float* const* p,
+                   const void* const* g, ef_grad_type g_type, void* const* m, void* const* v,
+                   uint8_t* const* m_exponents, uint8_t* const* v_exponents,
+                   uint16_t* const* copies, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, uint64_t step, uint64_t seed, const float* lr_dev,
+                   const int64_t* step_dev, const float* grad_scale, ef_stream_t stream);
+
+/*
+ * ef_adamw_states — the values that 8-bit states stand for, for example for a
+ * checkpoint (exact in fp32 and, being 4 significant bits, in bf16).
+ *
+ *   m, v, m_exponents, v_exponents [in] HOST arrays of DEVICE pointers as ef_adamw has them.
+ *   m_out, v_out [out] HOST arrays of DEVICE pointers, fp32 or bf16 (out_type)
+ *                    [numel]; must not overlap anything else.
+ */
+ef_status ef_adamw_states(uint32_t n_tensors, const uint64_t* numel, const uint8_t* const* m,
+                          const uint8_t* const* v, const uint8_t* const* m_exponents,
+                          const uint8_t* const* v_exponents, void* const* m_out,
+                          void* const* v_out, ef_grad_type out_type, ef_stream_t stream);
 
 /*
  * ef_check_status — synchronise `stream`, then return and clear the device-side

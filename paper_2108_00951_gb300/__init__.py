@@ -9,6 +9,7 @@ Python binding of that library (torch supplies device memory and streams)
 plus the seeded synthetic workloads used by the tests and the benchmark.
 """
 from ._binding import (  # noqa: F401
+    BLOCK,
     EF_ERR_BAD_INPUT,
     EF_ERR_CUDA,
     EF_ERR_INVALID_ARG,
@@ -17,8 +18,15 @@ from ._binding import (  # noqa: F401
     EF_OK,
     TILE,
     EfError,
+    TensorList,
+    ef_adamw,
+    ef_adamw_states,
     ef_check_status,
+    ef_embed,
+    ef_embed_grad,
     ef_hard_threshold,
+    ef_layer_norm,
+    ef_layer_norm_grad,
     ef_orthogonalize,
     ef_scaled_round,
     ef_kernel_launches,
@@ -29,6 +37,7 @@ from ._binding import (  # noqa: F401
     ef_vocab_loss,
     ef_vocab_loss_grad,
     ef_workspace_release,
+    exponents_for,
     library_path,
     int_aggregate,
     load_library,

@@ -55,6 +55,7 @@ def load_library(build_if_missing: bool = True):
             _build.build()
         lib = ctypes.CDLL(path)
         vp, u64, f32, u32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_float, ctypes.c_uint32
+        f64 = ctypes.c_double
         sig = {
             "ef_hard_threshold": [vp, vp, f32, f32, u64, vp, vp, vp, vp],
             "ef_hard_threshold_bf16": [vp, vp, f32, f32, u64, vp, vp, vp, vp],
@@ -83,6 +84,16 @@ def load_library(build_if_missing: bool = True):
             "ef_vocab_loss_grad": [vp, u64, vp, u64, vp, vp, vp, vp, u64, u64, u64, vp, u64, vp,
                                    u64, vp, vp],
             "ef_orthogonalize": [u32, vp, vp, vp, vp, ctypes.c_int, vp, vp, f32, vp, vp, vp],
+            "ef_embed": [vp, u64, ctypes.c_int, vp, u64, u64, u64, f32, vp, u64, ctypes.c_int, vp],
+            "ef_embed_grad": [vp, u64, ctypes.c_int, vp, u64, u64, u64, f32, ctypes.c_int, vp, u64,
+                              ctypes.c_int, vp],
+            "ef_layer_norm": [vp, u64, ctypes.c_int, vp, vp, ctypes.c_int, f32, u64, u64, vp, u64,
+                              ctypes.c_int, vp, vp, vp],
+            "ef_layer_norm_grad": [vp, u64, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp, u64,
+                                   ctypes.c_int, u64, u64, vp, u64, vp, vp, vp],
+            "ef_adamw": [u32, vp, vp, vp, ctypes.c_int, vp, vp, vp, vp, vp, f64, f64, f64, f64, f64,
+                         u64, u64, vp, vp, vp, vp],
+            "ef_adamw_states": [u32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp],
             "ef_check_status": [vp],
             "ef_workspace_release": [],
         }
@@ -464,6 +475,282 @@ def ef_orthogonalize(updates, outs, momenta=None, momentum=0.0, stream=None):
     _check(lib.ef_orthogonalize(n, at(rows), at(cols), at(u), at(ld_u),
                                 int(dtype is torch.bfloat16), at(m), at(ld_m), momentum, at(out),
                                 at(ld_out), _stream(stream)), "ef_orthogonalize")
+
+
+_KINDS = {torch.float32: 0, torch.bfloat16: 1}  # ef_grad_type
+
+
+def _here():
+    """The current device: what these entries' tensors must be on."""
+    return torch.cuda.current_device() if _current_device is None else _current_device()
+
+
+def _matrix(t, name, shape, dev):
+    """(device pointer, row stride, ef_grad_type) of a float32 or bfloat16 matrix of
+    this shape on the device whose rows are contiguous; 0 for an empty one."""
+    if (isinstance(t, _Tensor) and t.shape == shape and t.get_device() == dev
+            and t.dtype in _KINDS):
+        ld, step = t.stride()
+        if step == 1 and ld >= shape[1] > 0 < shape[0]:
+            return t.data_ptr(), ld, _KINDS[t.dtype]
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dtype not in _KINDS:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on another device than the current one" % name)
+    return (*_rows(t, name, t.dtype, *shape), _KINDS[t.dtype])
+
+
+def _vector(t, name, dtype, numel, dev):
+    """The device pointer of a contiguous tensor of this dtype on the device, with at
+    least `numel` entries; None for None."""
+    if t is None:
+        return None
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev:
+        if t.numel() >= numel and t.is_contiguous():
+            return t.data_ptr() or None
+    elif isinstance(t, _Tensor) and t.is_cuda and t.get_device() != dev:
+        raise ValueError("%s is on another device than the current one" % name)
+    return _dev(t, name, dtype, numel)
+
+
+def _dims(t, name):
+    if not isinstance(t, _Tensor) or t.dim() != 2:
+        raise TypeError("%s must be a matrix" % name)
+    return t.shape
+
+
+def _tokens(t, n, dev):
+    if not isinstance(t, _Tensor) or t.dim() != 1 or t.shape[0] != n:
+        raise ValueError("token must be a vector with an entry per row")
+    return _vector(t, "token", torch.int64, n, dev)
+
+
+def ef_embed(table, token, out, scale=1.0, stream=None):
+    """Rows of an embedding table by token (``ef_embed``): ``out[i] = scale *
+    table[token[i]]``, a row of zeros where the token is negative.
+
+    ``table`` [v, d] and ``out`` [n, d] float32 or bfloat16, rows contiguous at any
+    row stride; ``token`` int64 [n].
+    """
+    lib = load_library()
+    dev = _here()
+    (v, d), (n, width) = _dims(table, "table"), _dims(out, "out")
+    if width != d:
+        raise ValueError("table and out differ in width")
+    _check(lib.ef_embed(*_matrix(table, "table", (v, d), dev), _tokens(token, n, dev), n, v, d,
+                        _real(scale), *_matrix(out, "out", (n, d), dev), _stream(stream)),
+           "ef_embed")
+
+
+def ef_embed_grad(dout, token, dtable_out, scale=1.0, accumulate=False, stream=None):
+    """Gradient of an embedding table (``ef_embed_grad``): ``scale`` times the sums
+    of the rows of ``dout`` [n, d] of one token, written to ``dtable_out`` [v, d]
+    (zeros elsewhere) or, with ``accumulate``, added to it. float32 or bfloat16,
+    rows contiguous at any row stride; ``token`` int64 [n]."""
+    lib = load_library()
+    dev = _here()
+    (n, d), (v, width) = _dims(dout, "dout"), _dims(dtable_out, "dtable_out")
+    if width != d:
+        raise ValueError("dout and dtable_out differ in width")
+    _check(lib.ef_embed_grad(*_matrix(dout, "dout", (n, d), dev), _tokens(token, n, dev), n, v, d,
+                             _real(scale), 1 if accumulate else 0,
+                             *_matrix(dtable_out, "dtable_out", (v, d), dev), _stream(stream)),
+           "ef_embed_grad")
+
+
+def _weights(dev, d, *named):
+    """Device pointers of weight vectors of one dtype (or None), and that dtype."""
+    kind, pointers = None, []
+    for t, name in named:
+        if t is not None:
+            if not isinstance(t, _Tensor) or t.dtype not in _KINDS:
+                raise TypeError("%s must be a float32 or bfloat16 tensor" % name)
+            kind = kind or t.dtype
+            if t.dim() != 1 or t.shape[0] != d:
+                raise ValueError("%s must have an entry per column" % name)
+            pointers.append(_vector(t, name, kind, d, dev))
+        else:
+            pointers.append(None)
+    return pointers, _KINDS[kind] if kind else 0
+
+
+def ef_layer_norm(x, y_out, weight=None, bias=None, eps=1e-5, mean_out=None, rstd_out=None,
+                  stream=None):
+    """Layer norm over the rows of ``x`` (``ef_layer_norm``). ``x``, ``y_out`` [n, d]
+    float32 or bfloat16, rows contiguous at any row stride; ``weight``, ``bias``
+    [d] of one dtype, or None; ``mean_out``, ``rstd_out`` float32 [>= n] for the
+    gradient, or None."""
+    lib = load_library()
+    dev = _here()
+    n, d = shape = _dims(x, "x")
+    (w, b), kind = _weights(dev, d, (weight, "weight"), (bias, "bias"))
+    _check(lib.ef_layer_norm(*_matrix(x, "x", shape, dev), w, b, kind, _real(eps), n, d,
+                             *_matrix(y_out, "y_out", shape, dev),
+                             _vector(mean_out, "mean_out", torch.float32, n, dev),
+                             _vector(rstd_out, "rstd_out", torch.float32, n, dev), _stream(stream)),
+           "ef_layer_norm")
+
+
+def ef_layer_norm_grad(x, mean, rstd, dy, dx_out=None, weight=None, dweight_out=None,
+                       dbias_out=None, stream=None):
+    """Gradient of layer norm (``ef_layer_norm_grad``): ``mean`` and ``rstd`` as
+    written by ``ef_layer_norm`` for ``x`` and ``weight``; ``dx_out`` [n, d] of x's
+    dtype, ``dweight_out`` and ``dbias_out`` [d] of the weight's, each optional."""
+    lib = load_library()
+    dev = _here()
+    n, d = shape = _dims(x, "x")
+    (w, dw, db), kind = _weights(dev, d, (weight, "weight"), (dweight_out, "dweight_out"),
+                                 (dbias_out, "dbias_out"))
+    at, ld, x_kind = _matrix(x, "x", shape, dev)
+    dx, ld_dx = None, d
+    if dx_out is not None:
+        dx, ld_dx, dx_kind = _matrix(dx_out, "dx_out", shape, dev)
+        if dx_kind != x_kind:
+            raise TypeError("dx_out must be %s, got %s" % (x.dtype, dx_out.dtype))
+    if n and (mean is None or rstd is None):
+        raise TypeError("mean and rstd must be CUDA tensors")
+    _check(lib.ef_layer_norm_grad(
+        at, ld, x_kind, w, kind, _vector(mean, "mean", torch.float32, n, dev),
+        _vector(rstd, "rstd", torch.float32, n, dev), *_matrix(dy, "dy", shape, dev), n, d, dx,
+        ld_dx, dw, db, _stream(stream)), "ef_layer_norm_grad")
+
+
+class TensorList:
+    """Tensors of a model as ``ef_adamw`` takes them: contiguous CUDA tensors of one
+    dtype on one device, checked once. It holds the tensors, and their addresses
+    as they are now (a tensor whose storage is replaced needs a new list)."""
+
+    __slots__ = ("tensors", "dtype", "device", "numel", "pointers", "_sizes", "_at", "_blocks")
+
+    def __init__(self, tensors, name="tensors"):
+        self.tensors = tuple(tensors)
+        self.dtype = self.device = None
+        self.numel, self.pointers = array.array("Q"), array.array("Q")
+        for t in self.tensors:
+            if not isinstance(t, _Tensor) or not t.is_cuda:
+                raise TypeError("%s must be CUDA tensors" % name)
+            if self.dtype is None:
+                self.dtype, self.device = t.dtype, t.get_device()
+            if t.dtype is not self.dtype:
+                raise TypeError("%s must be of one dtype, got %s and %s" % (name, self.dtype, t.dtype))
+            if t.get_device() != self.device:
+                raise ValueError("%s must be on one device" % name)
+            if not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % name)
+            self.numel.append(t.numel())
+            self.pointers.append(t.data_ptr())
+        self._sizes = self.numel.tobytes()
+        self._blocks = None  # (sizes of the exponents of 8-bit states, once asked for)
+        self._at = self.pointers.buffer_info()[0]
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def __iter__(self):
+        return iter(self.tensors)
+
+    def __getitem__(self, i):
+        return self.tensors[i]
+
+
+def _list(tensors, name, dtypes, like, dev, sizes=None):
+    """A TensorList of one of the dtypes on the device; as long as `like` and of its
+    sizes (or of the bytes `sizes` of an array of them)."""
+    x = tensors if type(tensors) is TensorList else TensorList(tensors, name)
+    if not x.tensors:
+        if like is None or not like.tensors:
+            return x
+    elif x.dtype not in dtypes:
+        raise TypeError("%s must be %s, got %s" % (name, " or ".join(map(str, dtypes)), x.dtype))
+    elif x.device != dev:
+        raise ValueError("%s are on another device than the current one" % name)
+    if like is not None and x._sizes != (like._sizes if sizes is None else sizes):
+        raise ValueError("%s differ from the other lists in number or sizes" % name)
+    return x
+
+
+BLOCK = 128  # entries of an 8-bit state that share an exponent
+
+
+def exponents_for(numel: int) -> int:
+    """Length of the exponents of an 8-bit state of this size: ceil(numel / BLOCK)."""
+    return (int(numel) + BLOCK - 1) // BLOCK
+
+
+def _blocks(x):
+    if x._blocks is None:
+        x._blocks = array.array("Q", [exponents_for(n) for n in x.numel]).tobytes()
+    return x._blocks
+
+
+_F32, _U8, _GRADS = (torch.float32,), (torch.uint8,), (torch.float32, torch.bfloat16)
+
+
+def ef_adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+             m_exponents=None, v_exponents=None, copies=None, grad_scale=None, seed=0, stream=None):
+    """One AdamW step over lists of tensors (``ef_adamw``); a list may be a
+    ``TensorList``, which is checked once.
+
+    ``params`` float32, updated in place; ``grads`` float32 or bfloat16; ``m``, ``v``
+    float32, or uint8 codes with uint8 ``m_exponents``, ``v_exponents`` (of
+    ``exponents_for(numel)`` entries; all zero at the start), whose stochastic
+    rounding ``seed`` and the step fix; ``copies`` optional bfloat16: the new
+    parameters, rounded. ``step`` counts from 1; ``step`` and ``lr`` may be CUDA
+    tensors of one int64 and one float32, and ``grad_scale`` one of a float32 that
+    multiplies the gradients: they are read when the step runs (by a captured
+    call at each replay).
+    """
+    lib = load_library()
+    dev = _here()
+    p = _list(params, "params", _F32, None, dev)
+    g = _list(grads, "grads", _GRADS, p, dev)
+    state = _F32 if m_exponents is None and v_exponents is None else _U8
+    ms, vs = _list(m, "m", state, p, dev), _list(v, "v", state, p, dev)
+    me = ve = c = None
+    if state is _U8:
+        if m_exponents is None or v_exponents is None:
+            raise ValueError("m_exponents and v_exponents come together")
+        sizes = _blocks(p)
+        me = _list(m_exponents, "m_exponents", _U8, p, dev, sizes)
+        ve = _list(v_exponents, "v_exponents", _U8, p, dev, sizes)
+    if copies is not None:
+        c = _list(copies, "copies", (torch.bfloat16,), p, dev)
+    lr_dev = step_dev = None
+    if isinstance(lr, _Tensor):
+        lr_dev, lr = _vector(lr, "lr", torch.float32, 1, dev), 0.0
+    if isinstance(step, _Tensor):
+        step_dev, step = _vector(step, "step", torch.int64, 1, dev), 1
+    elif step < 0:
+        raise ValueError("step counts from 1")
+    _check(lib.ef_adamw(len(p.tensors), p.numel.buffer_info()[0], p._at, g._at,
+                        1 if g.dtype is torch.bfloat16 else 0, ms._at, vs._at,
+                        None if me is None else me._at, None if ve is None else ve._at,
+                        None if c is None else c._at, float(lr), float(beta1), float(beta2),
+                        float(eps), float(weight_decay), int(step),
+                        int(seed) & 0xFFFFFFFFFFFFFFFF, lr_dev, step_dev,
+                        _vector(grad_scale, "grad_scale", torch.float32, 1, dev), _stream(stream)),
+           "ef_adamw")
+
+
+def ef_adamw_states(m, v, m_exponents, v_exponents, m_out, v_out, stream=None):
+    """The values that 8-bit states stand for (``ef_adamw_states``): lists as
+    ``ef_adamw`` takes them to ``m_out`` and ``v_out``, lists of float32 or
+    bfloat16 tensors (exact in both)."""
+    lib = load_library()
+    dev = _here()
+    ms = _list(m, "m", _U8, None, dev)
+    vs = _list(v, "v", _U8, ms, dev)
+    sizes = _blocks(ms)
+    me = _list(m_exponents, "m_exponents", _U8, ms, dev, sizes)
+    ve = _list(v_exponents, "v_exponents", _U8, ms, dev, sizes)
+    mo, vo = _list(m_out, "m_out", _GRADS, ms, dev), _list(v_out, "v_out", _GRADS, ms, dev)
+    if mo.dtype is not vo.dtype:
+        raise TypeError("m_out and v_out differ in dtype")
+    _check(lib.ef_adamw_states(len(ms.tensors), ms.numel.buffer_info()[0], ms._at, vs._at, me._at,
+                               ve._at, mo._at, vo._at, 1 if mo.dtype is torch.bfloat16 else 0,
+                               _stream(stream)), "ef_adamw_states")
 
 
 def ef_check_status(stream=None) -> int:

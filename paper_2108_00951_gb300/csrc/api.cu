@@ -1,7 +1,8 @@
 // api.cu — the extern "C" boundary declared in include/efsparse.h: host-side
 // argument checks, the per-(device, stream) workspaces, and status reporting.
 // Every compute step runs in the kernels of ht.cu, topk.cu, topk_layerwise.cu
-// and aggregate.cu, and of vocab.cu, vocab_few.cu, ortho.cu and ortho_small.cu.
+// and aggregate.cu, of vocab.cu, vocab_few.cu, ortho.cu and ortho_small.cu, and of
+// embed.cu, embed_grad.cu, norm.cu, norm_grad.cu and adamw.cu.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -511,6 +512,329 @@ ef_status orthogonalize_entry(uint32_t n, const uint64_t* rows, const uint64_t* 
       launch_orthogonalize(mats.data(), n, bf16, momentum, plan.get(), *ws, info), ws);
 }
 
+// ---- the rest of a language-model training step ----
+bool grad_type_ok(ef_grad_type t) { return t == EF_GRAD_F32 || t == EF_GRAD_BF16; }
+uint64_t size_of(ef_grad_type t) { return t == EF_GRAD_BF16 ? 2 : 4; }
+
+ef_status this_device(DeviceInfo* info) {
+  int dev = 0;
+  return cudaGetDevice(&dev) != cudaSuccess ? EF_ERR_CUDA : device_info(dev, info);
+}
+
+// Whether an output overlaps an input or another output.
+template <int I, int O>
+bool any_overlap(const Rows (&in)[I], const Rows (&out)[O]) {
+  for (int o = 0; o < O; ++o) {
+    for (const Rows& i : in)
+      if (overlaps(out[o], i)) return true;
+    for (int q = o + 1; q < O; ++q)
+      if (overlaps(out[o], out[q])) return true;
+  }
+  return false;
+}
+
+bool matrix_ok(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t size) {
+  return ld >= cols && ld <= kMaxLd && (rows == 0 || (p && aligned(p, size)));
+}
+
+ef_status embed_entry(const void* table, uint64_t ld_table, ef_grad_type table_type,
+                      const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,
+                      void* out, uint64_t ld_out, ef_grad_type out_type, cudaStream_t stream) {
+  if (!grad_type_ok(table_type) || !grad_type_ok(out_type) || !std::isfinite(scale) ||
+      n > kMaxRows || v == 0 || v > kMaxWords || d == 0 || d > kMaxWidth ||
+      !matrix_ok(table, v, d, ld_table, size_of(table_type)) ||
+      !matrix_ok(out, n, d, ld_out, size_of(out_type)) || !aligned(token, 8))
+    return EF_ERR_INVALID_ARG;
+  if (n == 0) return EF_OK;
+  if (!token) return EF_ERR_INVALID_ARG;
+  const Rows in[] = {rows_of(table, v, d, ld_table, size_of(table_type)), vector_of(token, n * 8)};
+  const Rows outs[] = {rows_of(out, n, d, ld_out, size_of(out_type))};
+  if (any_overlap(in, outs)) return EF_ERR_INVALID_ARG;
+  EmbedCall c = {};
+  c.table = table;
+  c.out = out;
+  c.token = token;
+  c.ld_table = ld_table;
+  c.ld_out = ld_out;
+  c.n = static_cast<uint32_t>(n);
+  c.v = static_cast<uint32_t>(v);
+  c.d = static_cast<uint32_t>(d);
+  c.scale = scale;
+  c.table_bf16 = table_type == EF_GRAD_BF16;
+  c.out_bf16 = out_type == EF_GRAD_BF16;
+  DeviceInfo info;
+  ef_status st = this_device(&info);
+  if (st != EF_OK) return st;
+  Workspace* ws = nullptr;
+  st = acquire_model_scratch(stream, 0, &ws);
+  return st != EF_OK ? st : finish_launch(launch_embed(c, *ws, info), ws);
+}
+
+ef_status embed_grad_entry(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
+                           const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,
+                           int accumulate, void* dtable, uint64_t ld_dtable,
+                           ef_grad_type dtable_type, cudaStream_t stream) {
+  if (!grad_type_ok(dout_type) || !grad_type_ok(dtable_type) || !std::isfinite(scale) ||
+      n > kMaxRows || v == 0 || v > kMaxWords || d == 0 || d > kMaxWidth ||
+      !matrix_ok(dout, n, d, ld_dout, size_of(dout_type)) ||
+      !matrix_ok(dtable, v, d, ld_dtable, size_of(dtable_type)) || !aligned(token, 8) ||
+      (n && !token))
+    return EF_ERR_INVALID_ARG;
+  const Rows in[] = {rows_of(dout, n, d, ld_dout, size_of(dout_type)), vector_of(token, n * 8)};
+  const Rows outs[] = {rows_of(dtable, v, d, ld_dtable, size_of(dtable_type))};
+  if (any_overlap(in, outs)) return EF_ERR_INVALID_ARG;
+  if (n == 0 && accumulate) return EF_OK;
+  EmbedGradCall c = {};
+  c.dout = dout;
+  c.dtable = dtable;
+  c.token = token;
+  c.ld_dout = ld_dout;
+  c.ld_dtable = ld_dtable;
+  c.n = static_cast<uint32_t>(n);
+  c.v = static_cast<uint32_t>(v);
+  c.d = static_cast<uint32_t>(d);
+  c.scale = scale;
+  c.dout_bf16 = dout_type == EF_GRAD_BF16;
+  c.dtable_bf16 = dtable_type == EF_GRAD_BF16;
+  c.add = accumulate != 0;
+  DeviceInfo info;
+  ef_status st = this_device(&info);
+  if (st != EF_OK) return st;
+  Workspace* ws = nullptr;
+  st = acquire_model_scratch(stream, embed_grad_scratch(c, info), &ws);
+  return st != EF_OK ? st : finish_launch(launch_embed_grad(c, *ws, info), ws);
+}
+
+ef_status layer_norm_entry(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
+                           const void* bias, ef_grad_type w_type, float eps, uint64_t n, uint64_t d,
+                           void* y, uint64_t ldy, ef_grad_type y_type, float* mean, float* rstd,
+                           cudaStream_t stream) {
+  if (!grad_type_ok(x_type) || !grad_type_ok(w_type) || !grad_type_ok(y_type)) return EF_ERR_INVALID_ARG;
+  const uint64_t xs = size_of(x_type), wsz = size_of(w_type), ys = size_of(y_type);
+  if (!(eps >= 0.0f) || !std::isfinite(eps) || n > kMaxRows || d == 0 || d > kMaxWidth ||
+      !matrix_ok(x, n, d, ldx, xs) || !matrix_ok(y, n, d, ldy, ys) || !aligned(weight, wsz) ||
+      !aligned(bias, wsz) || !aligned(mean, 4) || !aligned(rstd, 4))
+    return EF_ERR_INVALID_ARG;
+  if (n == 0) return EF_OK;
+  const Rows in[] = {rows_of(x, n, d, ldx, xs), vector_of(weight, d * wsz), vector_of(bias, d * wsz)};
+  const Rows outs[] = {rows_of(y, n, d, ldy, ys), vector_of(mean, n * 4), vector_of(rstd, n * 4)};
+  if (any_overlap(in, outs)) return EF_ERR_INVALID_ARG;
+  NormCall c = {};
+  c.x = x;
+  c.y = y;
+  c.w = weight;
+  c.b = bias;
+  c.mean = mean;
+  c.rstd = rstd;
+  c.ldx = ldx;
+  c.ldy = ldy;
+  c.eps = eps;
+  c.n = static_cast<uint32_t>(n);
+  c.d = static_cast<uint32_t>(d);
+  c.x_bf16 = x_type == EF_GRAD_BF16;
+  c.y_bf16 = y_type == EF_GRAD_BF16;
+  c.w_bf16 = w_type == EF_GRAD_BF16;
+  return launch_layer_norm(c, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
+}
+
+ef_status layer_norm_grad_entry(const void* x, uint64_t ldx, ef_grad_type x_type,
+                                const void* weight, ef_grad_type w_type, const float* mean,
+                                const float* rstd, const void* dy, uint64_t lddy,
+                                ef_grad_type dy_type, uint64_t n, uint64_t d, void* dx,
+                                uint64_t lddx, void* dweight, void* dbias, cudaStream_t stream) {
+  if (!grad_type_ok(x_type) || !grad_type_ok(w_type) || !grad_type_ok(dy_type)) return EF_ERR_INVALID_ARG;
+  const uint64_t xs = size_of(x_type), wsz = size_of(w_type), ys = size_of(dy_type);
+  if (n > kMaxRows || d == 0 || d > kMaxWidth || !matrix_ok(x, n, d, ldx, xs) ||
+      !matrix_ok(dy, n, d, lddy, ys) || (dx && !matrix_ok(dx, n, d, lddx, xs)) ||
+      !aligned(weight, wsz) || !aligned(dweight, wsz) || !aligned(dbias, wsz) ||
+      !aligned(mean, 4) || !aligned(rstd, 4) || (n && (!mean || !rstd)))
+    return EF_ERR_INVALID_ARG;
+  const Rows in[] = {rows_of(x, n, d, ldx, xs), rows_of(dy, n, d, lddy, ys),
+                     vector_of(weight, d * wsz), vector_of(mean, n * 4), vector_of(rstd, n * 4)};
+  const Rows outs[] = {rows_of(dx, n, d, lddx, xs), vector_of(dweight, d * wsz),
+                       vector_of(dbias, d * wsz)};
+  if (any_overlap(in, outs)) return EF_ERR_INVALID_ARG;
+  if (!dweight && !dbias && (!dx || n == 0)) return EF_OK;
+  NormGradCall c = {};
+  c.x = x;
+  c.dy = dy;
+  c.dx = dx;
+  c.w = weight;
+  c.dw = dweight;
+  c.db = dbias;
+  c.mean = mean;
+  c.rstd = rstd;
+  c.ldx = ldx;
+  c.lddy = lddy;
+  c.lddx = lddx;
+  c.n = static_cast<uint32_t>(n);
+  c.d = static_cast<uint32_t>(d);
+  c.x_bf16 = x_type == EF_GRAD_BF16;
+  c.y_bf16 = dy_type == EF_GRAD_BF16;
+  c.w_bf16 = w_type == EF_GRAD_BF16;
+  DeviceInfo info;
+  ef_status st = this_device(&info);
+  if (st != EF_OK) return st;
+  Workspace* ws = nullptr;
+  const size_t bytes = norm_grad_scratch(c, info);
+  if (bytes && (st = acquire_model_scratch(stream, bytes, &ws)) != EF_OK) return st;
+  const cudaError_t err = launch_layer_norm_grad(c, ws, stream, info);
+  if (ws) return finish_launch(err, ws);
+  return err == cudaSuccess ? EF_OK : EF_ERR_CUDA;
+}
+
+// The address ranges of a call over lists of tensors. Lists as models have them, each
+// ascending in its own stretch of memory, are checked in one pass; others by
+// sorting all ranges.
+class Ranges {
+ public:
+  explicit Ranges(size_t most) { all_.reserve(most); }
+  void begin_list() { lists_.push_back({UINTPTR_MAX, 0}); }
+  void add(const void* p, uint64_t bytes, bool written) {
+    if (!p || bytes == 0) return;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    List& l = lists_.back();
+    ascending_ &= at >= l.end;
+    l.at = std::min(l.at, at);
+    l.end = std::max(l.end, at + bytes);
+    all_.push_back({at, at + bytes, written});
+  }
+  // Whether anything written overlaps anything else.
+  bool overlap() {
+    std::sort(lists_.begin(), lists_.end(), [](const List& x, const List& y) { return x.at < y.at; });
+    bool apart = ascending_;
+    for (size_t i = 1; i < lists_.size(); ++i) apart &= lists_[i].at >= lists_[i - 1].end || lists_[i].end == 0;
+    if (apart) return false;
+    std::sort(all_.begin(), all_.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
+    uintptr_t any = 0, write = 0;  // how far those before reach
+    for (const Range& r : all_) {
+      if (r.at < write || (r.written && r.at < any)) return true;
+      any = std::max(any, r.end);
+      if (r.written) write = std::max(write, r.end);
+    }
+    return false;
+  }
+
+ private:
+  struct List {
+    uintptr_t at, end;
+  };
+  struct Range {
+    uintptr_t at, end;
+    bool written;
+  };
+  std::vector<List> lists_;
+  std::vector<Range> all_;
+  bool ascending_ = true;
+};
+
+constexpr uint32_t kMaxTensors = 1u << 20;
+
+ef_status adamw_entry(uint32_t n, const uint64_t* numel, float* const* p, const void* const* g,
+                      ef_grad_type g_type, void* const* m, void* const* v, uint8_t* const* me,
+                      uint8_t* const* ve, uint16_t* const* copy, AdamCall c, cudaStream_t stream) {
+  if (n > kMaxTensors || !grad_type_ok(g_type) || !std::isfinite(c.lr) || !std::isfinite(c.decay) ||
+      !(c.b1 >= 0.0 && c.b1 < 1.0) || !(c.b2 >= 0.0 && c.b2 < 1.0) || !(c.eps >= 0.0) ||
+      !std::isfinite(c.eps) || (c.step == 0 && !c.step_dev) || !aligned(c.lr_dev, 4) ||
+      !aligned(c.step_dev, 8) || !aligned(c.grad_scale, 4) || (me == nullptr) != (ve == nullptr))
+    return EF_ERR_INVALID_ARG;
+  if (n == 0) return EF_OK;
+  if (!numel || !p || !g || !m || !v) return EF_ERR_INVALID_ARG;
+  c.g_bf16 = g_type == EF_GRAD_BF16;
+  c.eight = me != nullptr;
+  const uint64_t state = c.eight ? 1 : 4;
+  std::vector<AdamTensor> t(n);
+  bool any = false;
+  for (uint32_t i = 0; i < n; ++i) {
+    if (numel[i] > kMaxD - 4095) return EF_ERR_INVALID_ARG;
+    t[i].numel = static_cast<uint32_t>(numel[i]);
+    if (numel[i] == 0) continue;
+    any = true;
+    t[i].p = p[i];
+    t[i].g = g[i];
+    t[i].m = m[i];
+    t[i].v = v[i];
+    t[i].copy = copy ? copy[i] : nullptr;
+    t[i].me = me ? me[i] : nullptr;
+    t[i].ve = ve ? ve[i] : nullptr;
+    if (!p[i] || !g[i] || !m[i] || !v[i] || (copy && !copy[i]) || (me && (!me[i] || !ve[i])) ||
+        !aligned(p[i], 4) || !aligned(g[i], size_of(g_type)) || !aligned(m[i], state) ||
+        !aligned(v[i], state) || !aligned(t[i].copy, 2))
+      return EF_ERR_INVALID_ARG;
+  }
+  if (!any) return EF_OK;
+  Ranges ranges(7ull * n + 3);
+  auto list = [&](auto&& at, uint64_t size, bool written, uint64_t per) {
+    ranges.begin_list();
+    for (const AdamTensor& x : t) ranges.add(at(x), (x.numel + per - 1) / per * size, written);
+  };
+  list([](const AdamTensor& x) { return x.p; }, 4, true, 1);
+  list([](const AdamTensor& x) { return x.g; }, size_of(g_type), false, 1);
+  list([](const AdamTensor& x) { return x.m; }, state, true, 1);
+  list([](const AdamTensor& x) { return x.v; }, state, true, 1);
+  list([](const AdamTensor& x) { return x.copy; }, 2, true, 1);
+  list([](const AdamTensor& x) { return x.me; }, 1, true, 128);
+  list([](const AdamTensor& x) { return x.ve; }, 1, true, 128);
+  const std::pair<const void*, uint64_t> scalars[] = {{c.lr_dev, 4}, {c.step_dev, 8}, {c.grad_scale, 4}};
+  for (const auto& x : scalars) {
+    ranges.begin_list();
+    ranges.add(x.first, x.second, false);
+  }
+  if (ranges.overlap()) return EF_ERR_INVALID_ARG;
+  return launch_adamw(t.data(), n, c, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
+}
+
+ef_status adamw_states_entry(uint32_t n, const uint64_t* numel, const uint8_t* const* m,
+                             const uint8_t* const* v, const uint8_t* const* me,
+                             const uint8_t* const* ve, void* const* m_out, void* const* v_out,
+                             ef_grad_type out_type, cudaStream_t stream) {
+  if (n > kMaxTensors || !grad_type_ok(out_type)) return EF_ERR_INVALID_ARG;
+  if (n == 0) return EF_OK;
+  if (!numel || !m || !v || !me || !ve || !m_out || !v_out) return EF_ERR_INVALID_ARG;
+  const uint64_t size = size_of(out_type);
+  std::vector<AdamStates> t(n);
+  for (uint32_t i = 0; i < n; ++i) {
+    if (numel[i] > kMaxD - 4095) return EF_ERR_INVALID_ARG;
+    t[i].numel = static_cast<uint32_t>(numel[i]);
+    if (numel[i] == 0) continue;
+    t[i].m = m[i];
+    t[i].v = v[i];
+    t[i].me = me[i];
+    t[i].ve = ve[i];
+    t[i].m_out = m_out[i];
+    t[i].v_out = v_out[i];
+    if (!m[i] || !v[i] || !me[i] || !ve[i] || !m_out[i] || !v_out[i] || !aligned(m_out[i], size) ||
+        !aligned(v_out[i], size))
+      return EF_ERR_INVALID_ARG;
+  }
+  Ranges ranges(6ull * n);
+  auto list = [&](auto&& at, uint64_t bytes, bool written, uint64_t per) {
+    ranges.begin_list();
+    for (const AdamStates& x : t) ranges.add(at(x), (x.numel + per - 1) / per * bytes, written);
+  };
+  list([](const AdamStates& x) { return x.m; }, 1, false, 1);
+  list([](const AdamStates& x) { return x.v; }, 1, false, 1);
+  list([](const AdamStates& x) { return x.me; }, 1, false, 128);
+  list([](const AdamStates& x) { return x.ve; }, 1, false, 128);
+  list([](const AdamStates& x) { return x.m_out; }, size, true, 1);
+  list([](const AdamStates& x) { return x.v_out; }, size, true, 1);
+  if (ranges.overlap()) return EF_ERR_INVALID_ARG;
+  return launch_adamw_states(t.data(), n, out_type == EF_GRAD_BF16, stream) == cudaSuccess ? EF_OK
+                                                                                            : EF_ERR_CUDA;
+}
+
+// An entry's body, with what it may throw as a status.
+template <typename F>
+ef_status guarded(F&& body) {
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return EF_ERR_NO_MEMORY;
+  } catch (...) {
+    return EF_ERR_CUDA;
+  }
+}
+
 }  // namespace
 
 // A launch that may begin while the previous kernel on the stream finishes
@@ -840,6 +1164,81 @@ ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t*
   } catch (const std::bad_alloc&) {
     return EF_ERR_NO_MEMORY;
   }
+}
+
+ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type,
+                   const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale, void* out,
+                   uint64_t ld_out, ef_grad_type out_type, ef_stream_t stream) {
+  return efs::guarded([&] {
+    return efs::embed_entry(table, ld_table, table_type, token, n, v, d, scale, out, ld_out,
+                            out_type, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
+                        const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,
+                        int accumulate, void* dtable_out, uint64_t ld_dtable,
+                        ef_grad_type dtable_type, ef_stream_t stream) {
+  return efs::guarded([&] {
+    return efs::embed_grad_entry(dout, ld_dout, dout_type, token, n, v, d, scale, accumulate,
+                                 dtable_out, ld_dtable, dtable_type,
+                                 reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
+                        const void* bias, ef_grad_type w_type, float eps, uint64_t n, uint64_t d,
+                        void* y_out, uint64_t ldy, ef_grad_type y_type, float* mean_out,
+                        float* rstd_out, ef_stream_t stream) {
+  return efs::guarded([&] {
+    return efs::layer_norm_entry(x, ldx, x_type, weight, bias, w_type, eps, n, d, y_out, ldy,
+                                 y_type, mean_out, rstd_out, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
+                             ef_grad_type w_type, const float* mean, const float* rstd,
+                             const void* dy, uint64_t lddy, ef_grad_type dy_type, uint64_t n,
+                             uint64_t d, void* dx_out, uint64_t lddx, void* dweight_out,
+                             void* dbias_out, ef_stream_t stream) {
+  return efs::guarded([&] {
+    return efs::layer_norm_grad_entry(x, ldx, x_type, weight, w_type, mean, rstd, dy, lddy, dy_type,
+                                      n, d, dx_out, lddx, dweight_out, dbias_out,
+                                      reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+ef_status ef_adamw(uint32_t n_tensors, const uint64_t* numel, float* const* p,
+                   const void* const* g, ef_grad_type g_type, void* const* m, void* const* v,
+                   uint8_t* const* m_exponents, uint8_t* const* v_exponents,
+                   uint16_t* const* copies, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, uint64_t step, uint64_t seed, const float* lr_dev,
+                   const int64_t* step_dev, const float* grad_scale, ef_stream_t stream) {
+  efs::AdamCall c = {};
+  c.lr = lr;
+  c.b1 = beta1;
+  c.b2 = beta2;
+  c.eps = eps;
+  c.decay = weight_decay;
+  c.step = step;
+  c.seed = seed;
+  c.lr_dev = lr_dev;
+  c.step_dev = step_dev;
+  c.grad_scale = grad_scale;
+  return efs::guarded([&] {
+    return efs::adamw_entry(n_tensors, numel, p, g, g_type, m, v, m_exponents, v_exponents, copies,
+                            c, reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+ef_status ef_adamw_states(uint32_t n_tensors, const uint64_t* numel, const uint8_t* const* m,
+                          const uint8_t* const* v, const uint8_t* const* m_exponents,
+                          const uint8_t* const* v_exponents, void* const* m_out,
+                          void* const* v_out, ef_grad_type out_type, ef_stream_t stream) {
+  return efs::guarded([&] {
+    return efs::adamw_states_entry(n_tensors, numel, m, v, m_exponents, v_exponents, m_out, v_out,
+                                   out_type, reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 ef_status ef_check_status(ef_stream_t stream) {

@@ -1,0 +1,586 @@
+// embed_grad.cu — the gradient of an embedding table: row w is the scaled sum of
+// the rows of dout whose token is w, in the order of their positions, in fp32.
+//
+// What bounds it: reading dout once and writing the table's gradient once (or, where
+// it is added to, the rows that occur). Sums run in a fixed order, without
+// floating-point atomics.
+//
+// Up to kFewTokens tokens: one launch. A CTA per position looks through all
+// tokens; if its own occurs before, another CTA has it, else it sums the rows of
+// all its occurrences. Further CTAs write the rows that do not occur.
+//
+// More: the positions are sorted by token (stable, least digit first: a histogram
+// of the first digit, then one launch per digit, in which each CTA finds where its
+// part of the positions goes from the counts of the parts before it and counts
+// the next digit where they arrive). Then a warp takes 256 columns of a piece of
+// the sorted positions, adds up rows and writes a row's sum when the token
+// changes. A token that goes on past its piece leaves a share, and a last launch
+// joins those in order.
+#include <algorithm>
+
+#include "internal.h"
+#include "vec_io.cuh"
+
+namespace efs {
+namespace {
+
+constexpr uint32_t kFewTokens = 2048;
+constexpr int kThreadsFew = 256;
+constexpr uint32_t kSlice = 256;        // columns a warp takes: 8 a lane
+constexpr int kLane = 8;
+constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
+constexpr int kSortThreads = 512;
+constexpr uint32_t kSortTile = 2048;    // positions that a sorting CTA ranks at a time
+constexpr int kMaxBins = 512, kMaxPasses = 4;  // (31 bits: four digits of 8)
+constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
+
+// A lane's 8 columns of a slice: vectors of V, 32 V apart.
+template <int V>
+__device__ __forceinline__ uint32_t column(uint32_t slice, int k, uint32_t lane) {
+  return slice * kSlice + (k * 32 + lane) * V;
+}
+
+template <typename T, int V>
+struct RowPart {
+  Vec<T, V> x[kLane / V];
+  __device__ __forceinline__ void load(const T* row, uint32_t slice, uint32_t lane, uint32_t d) {
+#pragma unroll
+    for (int k = 0; k < kLane / V; ++k) {
+      const uint32_t c = column<V>(slice, k, lane);
+      if (c < d) x[k].load(row + c);
+      else x[k].clear();
+    }
+  }
+  __device__ __forceinline__ void add_to(float (&sum)[kLane]) const {
+#pragma unroll
+    for (int k = 0; k < kLane / V; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[k * V + j] += x[k].get(j);
+  }
+};
+
+// scale sum, or that added to what is there; rounded once.
+template <typename T, int V>
+__device__ __forceinline__ void write_row(const EmbedGradCall& a, uint64_t row, uint32_t slice,
+                                          uint32_t lane, const float (&sum)[kLane]) {
+  T* to = static_cast<T*>(a.dtable) + row * a.ld_dtable;
+#pragma unroll
+  for (int k = 0; k < kLane / V; ++k) {
+    const uint32_t c = column<V>(slice, k, lane);
+    if (c < a.d) {
+      float f[V];
+      Vec<T, V> o;
+      if (a.add) {
+        o.load_own(to + c);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = fmaf(sum[k * V + j], a.scale, o.get(j));
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = sum[k * V + j] * a.scale;
+      }
+      o.round(f);
+      o.store(to + c);
+    }
+  }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void zero_row(const EmbedGradCall& a, uint64_t row, uint32_t lane) {
+  T* to = static_cast<T*>(a.dtable) + row * a.ld_dtable;
+  Vec<T, V> o;
+  o.clear();
+#pragma unroll 4
+  for (uint32_t c = lane * V; c < a.d; c += 32 * V) o.store(to + c);
+}
+
+// ------------------------------------------------------------- few tokens
+// CTA i < n: position i. The others: rows of the table, `rows` each.
+template <typename D, typename T, int V>
+__global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const EmbedGradCall a, uint32_t rows, uint32_t* error) {
+  __shared__ uint32_t mask[kRowsCta / 32 > kFewTokens / 32 ? kRowsCta / 32 : kFewTokens / 32];
+  __shared__ float part[kThreadsFew / 32][kSlice];
+  const uint32_t t = threadIdx.x, lane = t & 31u, warp = t >> 5;
+  constexpr uint32_t kWarps = kThreadsFew / 32;
+  if (blockIdx.x >= a.n) {  // zeros
+    const uint64_t lo = static_cast<uint64_t>(blockIdx.x - a.n) * rows;
+    const uint64_t hi = min(lo + rows, static_cast<uint64_t>(a.v));
+    for (uint32_t i = t; i < (rows + 31) / 32; i += kThreadsFew) mask[i] = 0u;
+    __syncthreads();
+    for (uint32_t i = t; i < a.n; i += kThreadsFew) {
+      const int64_t w = __ldg(reinterpret_cast<const long long*>(a.token) + i);
+      if (w >= static_cast<int64_t>(lo) && w < static_cast<int64_t>(hi))
+        atomicOr(&mask[(w - lo) / 32], 1u << ((w - lo) & 31));
+    }
+    __syncthreads();
+    for (uint64_t r = lo + warp; r < hi; r += kWarps)
+      if (!(mask[(r - lo) / 32] >> ((r - lo) & 31) & 1u)) zero_row<T, V>(a, r, lane);
+    return;
+  }
+  const uint32_t i = blockIdx.x;
+  const int64_t own = __ldg(reinterpret_cast<const long long*>(a.token) + i);
+  if (own >= static_cast<int64_t>(a.v) && t == 0) atomicOr(error, kDevErrBadInput);
+  if (own < 0 || own >= static_cast<int64_t>(a.v)) return;
+  bool before = false;
+  uint32_t count = 0;
+  for (uint32_t j = t; j < (a.n + 31u) / 32u * 32u; j += kThreadsFew) {
+    const bool same = j < a.n && __ldg(reinterpret_cast<const long long*>(a.token) + j) == own;
+    before |= same && j < i;
+    const uint32_t m = __ballot_sync(0xffffffffu, same);
+    if (lane == 0) mask[j / 32] = m;
+    count += __popc(m);
+  }
+  if (__syncthreads_or(before)) return;
+  // slices of columns over the warps; with fewer slices than warps, several warps
+  // share one, each taking every R-th occurrence
+  const uint32_t slices = (a.d + kSlice - 1) / kSlice;
+  uint32_t groups = 1;
+  while (groups * 2 * slices <= kWarps) groups *= 2;
+  const uint32_t group = warp % groups;
+  for (uint32_t s0 = 0; s0 < slices; s0 += kWarps / groups) {
+    const uint32_t slice = s0 + warp / groups;
+    float sum[kLane] = {};
+    if (slice < slices) {
+      uint32_t seen = 0;
+      RowPart<D, V> row[4];
+      uint32_t held = 0;
+      for (uint32_t word = i / 32; word < (a.n + 31u) / 32u; ++word) {
+        uint32_t m = mask[word];
+        while (m) {
+          const uint32_t at = word * 32 + __ffs(m) - 1;
+          m &= m - 1;
+          if (seen++ % groups != group) continue;
+          // (an index that is no constant would put the rows into local memory)
+          const D* from = static_cast<const D*>(a.dout) + static_cast<uint64_t>(at) * a.ld_dout;
+          if (held == 0) row[0].load(from, slice, lane, a.d);
+          else if (held == 1) row[1].load(from, slice, lane, a.d);
+          else if (held == 2) row[2].load(from, slice, lane, a.d);
+          else row[3].load(from, slice, lane, a.d);
+          if (++held == 4) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) row[q].add_to(sum);
+            held = 0;
+          }
+        }
+      }
+      if (held > 0) row[0].add_to(sum);
+      if (held > 1) row[1].add_to(sum);
+      if (held > 2) row[2].add_to(sum);
+    }
+    if (groups > 1) {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) part[warp][j * 32 + lane] = sum[j];
+      __syncthreads();
+      if (group == 0) {
+        for (uint32_t g = 1; g < groups; ++g)
+#pragma unroll
+          for (int j = 0; j < kLane; ++j) sum[j] += part[warp + g][j * 32 + lane];
+      }
+      __syncthreads();
+    }
+    if (group == 0 && slice < slices) write_row<T, V>(a, static_cast<uint64_t>(own), slice, lane, sum);
+  }
+}
+
+// ------------------------------------------------------------------ sorting
+struct Sort {
+  uint32_t n, v, bits, passes, parts, per;  // per: positions a part takes
+  uint32_t* hist[kMaxPasses];  // [parts][bins] of each digit
+  uint32_t *key[2], *pos[2];
+  uint32_t* error;
+  const int64_t* token;
+};
+
+__device__ __forceinline__ uint32_t digit_of(const Sort& s, uint32_t key, uint32_t pass) {
+  return (key >> (pass * s.bits)) & ((1u << s.bits) - 1u);
+}
+
+// Counts of the first digit by part, and zeros for the counts of the others.
+__global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s) {
+  __shared__ uint32_t hist[kMaxBins];
+  const uint32_t bins = 1u << s.bits, t = threadIdx.x;
+  for (uint32_t b = t; b < bins; b += kSortThreads) hist[b] = 0u;
+  __syncthreads();
+  const uint32_t lo = blockIdx.x * s.per, hi = min(lo + s.per, s.n);
+  bool bad = false;
+#pragma unroll 4
+  for (uint32_t i = lo + t; i < hi; i += kSortThreads) {
+    const int64_t w = __ldg(reinterpret_cast<const long long*>(s.token) + i);
+    bad |= w >= static_cast<int64_t>(s.v);
+    const uint32_t key = w < 0 || w >= static_cast<int64_t>(s.v) ? s.v : static_cast<uint32_t>(w);
+    s.key[0][i] = key;
+    atomicAdd(&hist[digit_of(s, key, 0)], 1u);
+  }
+  if (bad) atomicOr(s.error, kDevErrBadInput);
+  __syncthreads();
+  for (uint32_t b = t; b < bins; b += kSortThreads) {
+    s.hist[0][blockIdx.x * bins + b] = hist[b];
+    for (uint32_t p = 1; p < s.passes; ++p) s.hist[p][blockIdx.x * bins + b] = 0u;
+  }
+}
+
+// One digit. Positions keep their order: a warp takes consecutive ones, and a
+// position's rank is the number of equal digits before it in its warp, in the
+// warps before, in the tiles before and in the parts before.
+__global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort s, uint32_t pass) {
+  constexpr int kWarps = kSortThreads / 32, kPer = kSortTile / kSortThreads;
+  __shared__ uint32_t base[kMaxBins];           // where the part's next position of a digit goes
+  __shared__ uint16_t count[kWarps][kMaxBins];
+  __shared__ uint32_t sums[kWarps];
+  griddep_wait();
+  const uint32_t bins = 1u << s.bits, t = threadIdx.x, lane = t & 31u, warp = t >> 5;
+  const bool last = pass + 1u == s.passes;
+  const uint32_t* hist = s.hist[pass];
+  uint32_t* next = s.hist[last ? pass : pass + 1u];
+  const uint32_t* keys = s.key[pass & 1u];
+  const uint32_t* from = s.pos[pass & 1u];
+  uint32_t *keys_out = s.key[(pass + 1u) & 1u], *to = s.pos[(pass + 1u) & 1u];
+  {  // a thread a digit: the parts before, then all parts; and the digits before
+    uint32_t before = 0, all = 0;
+    if (t < bins) {
+#pragma unroll 8
+      for (uint32_t p = 0; p < s.parts; ++p) {
+        const uint32_t c = hist[p * bins + t];
+        before += p < blockIdx.x ? c : 0u;
+        all += c;
+      }
+    }
+    uint32_t scan = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
+      if (lane >= static_cast<uint32_t>(o)) scan += x;
+    }
+    if (lane == 31) sums[warp] = scan;
+    __syncthreads();
+    uint32_t under = 0;
+    for (uint32_t w = 0; w < warp; ++w) under += sums[w];
+    if (t < bins) base[t] = under + scan - all + before;
+  }
+  const uint32_t lo = blockIdx.x * s.per, hi = min(lo + s.per, s.n);
+  for (uint32_t tile = lo; tile < hi; tile += kSortTile) {
+    for (uint32_t i = t; i < kWarps * bins; i += kSortThreads) count[i >> s.bits][i & (bins - 1u)] = 0;
+    uint32_t key[kPer], rank[kPer], digit[kPer], pos[kPer];
+    const uint32_t at = tile + warp * (32 * kPer) + lane;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const uint32_t i = at + 32 * k;
+      key[k] = i < hi ? keys[i] : 0u;
+      pos[k] = i < hi ? (pass ? from[i] : i) : 0u;
+      digit[k] = i < hi ? digit_of(s, key[k], pass) : bins;  // (no digit)
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const uint32_t same = __match_any_sync(0xffffffffu, digit[k]);
+      const bool in = digit[k] < bins;
+      const uint32_t had = in ? count[warp][digit[k]] : 0u;
+      rank[k] = had + __popc(same & lanemask_lt());
+      __syncwarp();
+      if (in && (same & lanemask_lt()) == 0u) count[warp][digit[k]] = static_cast<uint16_t>(had + __popc(same));
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t total = 0;
+    if (t < bins) {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const uint32_t c = count[w][t];
+        count[w][t] = static_cast<uint16_t>(total);
+        total += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (digit[k] < bins) {
+        const uint32_t out = base[digit[k]] + count[warp][digit[k]] + rank[k];
+        keys_out[out] = key[k];
+        to[out] = pos[k];
+        if (!last) atomicAdd(&next[(out / s.per) * bins + digit_of(s, key[k], pass + 1u)], 1u);
+      }
+    }
+    __syncthreads();
+    if (t < bins) base[t] += total;
+  }
+}
+
+// ------------------------------------------------------------------ summing
+struct Sum {
+  const uint32_t *key, *pos;
+  float* shares;          // [pieces][2][d]: a token from the piece before, one that goes on
+  uint32_t piece, pieces, slices, warps;  // positions a piece; warps that sum
+  uint32_t rows;          // rows a CTA of zeros takes
+};
+
+// The first position whose token is at least `key`.
+__device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t n, uint32_t key) {
+  uint32_t lo = 0, hi = n;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (__ldg(keys + mid) < key) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+template <typename D, typename T, int V>
+__global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, const Sum s) {
+  griddep_wait();
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const uint32_t sum_ctas = (s.warps + 7) / 8;
+  if (blockIdx.x >= sum_ctas) {  // zeros, where a row's token does not occur
+    const uint64_t lo = static_cast<uint64_t>(blockIdx.x - sum_ctas) * s.rows;
+    const uint64_t hi = min(lo + s.rows, static_cast<uint64_t>(a.v));
+    for (uint64_t r = lo + warp * 32; r < hi; r += 256) {
+      bool absent = false;
+      if (r + lane < hi) {
+        const uint32_t row = static_cast<uint32_t>(r) + lane, at = first_of(s.key, a.n, row);
+        absent = at == a.n || __ldg(s.key + at) != row;
+      }
+      uint32_t m = __ballot_sync(0xffffffffu, absent);
+      while (m) {
+        zero_row<T, V>(a, r + __ffs(m) - 1, lane);
+        m &= m - 1;
+      }
+    }
+    return;
+  }
+  const uint32_t item = blockIdx.x * 8 + warp;
+  if (item >= s.warps) return;
+  const uint32_t slice = item % s.slices, piece = item / s.slices;
+  const uint32_t lo = piece * s.piece, hi = min(lo + s.piece, a.n);
+  float sum[kLane] = {};
+  uint32_t token = __ldg(s.key + lo);
+  bool goes_on = lo > 0 && __ldg(s.key + lo - 1) == token;  // from the piece before
+  auto flush = [&](bool on) {  // `on`: the token goes on in the next piece
+    if (token < a.v) {
+      if (goes_on || on) {
+        float* to = s.shares + (static_cast<uint64_t>(piece) * 2 + (goes_on ? 0 : 1)) * a.d;
+#pragma unroll
+        for (int k = 0; k < kLane / V; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const uint32_t c = column<V>(slice, k, lane) + j;
+            if (c < a.d) to[c] = sum[k * V + j];
+          }
+      } else {
+        write_row<T, V>(a, token, slice, lane, sum);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) sum[j] = 0.0f;
+    goes_on = false;
+  };
+  for (uint32_t base = lo; base < hi; base += 32) {
+    const uint32_t count = min(32u, hi - base);
+    const uint32_t my_key = lane < count ? __ldg(s.key + base + lane) : 0u;
+    const uint32_t my_pos = lane < count ? __ldg(s.pos + base + lane) : 0u;
+    for (uint32_t e = 0; e < count; e += 4) {
+      RowPart<D, V> row[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
+        const uint32_t pos = __shfl_sync(0xffffffffu, my_pos, (e + q) & 31u);
+        if (e + q < count && key < a.v)
+          row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(pos) * a.ld_dout, slice, lane, a.d);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
+        if (e + q < count) {
+          if (key != token) {
+            flush(false);
+            token = key;
+          }
+          if (key < a.v) row[q].add_to(sum);
+        }
+      }
+    }
+  }
+  flush(hi < a.n && __ldg(s.key + hi) == token);
+}
+
+// The shares of a token that goes on past the piece it begins in, joined in order.
+// A CTA takes eight pieces and one slice; a token of more than kShort shares is
+// added up by all its warps, each taking a run of them.
+constexpr uint32_t kShort = 16;
+template <typename T, int V>
+__global__ void __launch_bounds__(256) embed_join_kernel(const EmbedGradCall a, const Sum s) {
+  __shared__ uint32_t ends[8];
+  __shared__ float part[8][kSlice];
+  griddep_wait();
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const uint32_t slice = blockIdx.x % s.slices, first = blockIdx.x / s.slices * 8;
+  const uint32_t piece = first + warp;
+  uint32_t end = 0;  // the last piece with a share of the token that piece's last one is
+  uint32_t token = 0;
+  if (piece + 1 < s.pieces) {
+    const uint32_t lo = piece * s.piece, hi = lo + s.piece;
+    token = __ldg(s.key + hi - 1);
+    const bool begins = lo == 0 || __ldg(s.key + lo - 1) != token;
+    if (token < a.v && begins && __ldg(s.key + hi) == token) {
+      end = piece + 1;
+      if (end + 1 < s.pieces && __ldg(s.key + min(hi + s.piece, a.n - 1)) == token)
+        end = (hi + first_of(s.key + hi, a.n - hi, token + 1) - 1) / s.piece;
+    }
+  }
+  auto add = [&](uint32_t share, float (&sum)[kLane]) {
+    const float* from = s.shares + static_cast<uint64_t>(share) * a.d + slice * kSlice;
+#pragma unroll
+    for (int j = 0; j < kLane; ++j)
+      if (slice * kSlice + j * 32 + lane < a.d) sum[j] += from[j * 32 + lane];
+  };
+  auto write = [&](uint32_t row, const float (&sum)[kLane]) {
+    T* to = static_cast<T*>(a.dtable) + static_cast<uint64_t>(row) * a.ld_dtable + slice * kSlice;
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      const uint32_t c = j * 32 + lane;
+      if (slice * kSlice + c < a.d) store_rounded(to + c, a.add ? fmaf(sum[j], a.scale, widen(to[c])) : sum[j] * a.scale);
+    }
+  };
+  if (lane == 0) ends[warp] = end;
+  if (end && end - piece <= kShort) {
+    float sum[kLane] = {};
+    add(2 * piece + 1, sum);
+#pragma unroll 4
+    for (uint32_t q = piece + 1; q <= end; ++q) add(2 * q, sum);
+    write(token, sum);
+  }
+  __syncthreads();
+  for (uint32_t w = 0; w < 8; ++w) {
+    const uint32_t p = first + w, e = ends[w];
+    if (e == 0 || e - p <= kShort) continue;
+    const uint32_t per = (e - p + 7) / 8, lo = p + 1 + warp * per, hi = min(lo + per, e + 1);
+    float sum[kLane] = {};
+    if (warp == 0) add(2 * p + 1, sum);
+#pragma unroll 4
+    for (uint32_t q = lo; q < hi; ++q) add(2 * q, sum);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) part[warp][j * 32 + lane] = sum[j];
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j)
+        for (uint32_t q = 1; q < 8; ++q) sum[j] += part[q][j * 32 + lane];
+      write(__ldg(s.key + p * s.piece + s.piece - 1), sum);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ planning
+struct Plan {
+  bool few;
+  uint32_t v;  // values per vector
+  Sort sort;
+  Sum sum;
+  size_t hist, key, shares, bytes;  // sizes, in bytes
+};
+
+Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
+  Plan p = {};
+  const uint32_t dsize = c.dout_bf16 ? 2 : 4, tsize = c.dtable_bf16 ? 2 : 4;
+  auto allow = [&](uint32_t v) {
+    auto rows = [&](const void* q, uint64_t ld, uint64_t size) {
+      return (reinterpret_cast<uintptr_t>(q) | ld * size) % (size * v) == 0;
+    };
+    return c.d % v == 0 && rows(c.dout, c.n > 1 ? c.ld_dout : 0, dsize) &&
+           rows(c.dtable, c.v > 1 ? c.ld_dtable : 0, tsize);
+  };
+  const uint32_t wide = c.dout_bf16 && c.dtable_bf16 ? 8 : 4;
+  p.v = allow(wide) ? wide : allow(2) ? 2 : 1;
+  p.few = c.n <= kFewTokens;
+  const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
+  p.sum.rows = std::max(8u, std::min((c.v + 4 * sms - 1) / (4 * sms), kRowsCta));
+  if (p.few) return p;
+  Sort& s = p.sort;
+  uint32_t bits = 1;
+  while (bits < 31 && (c.v >> bits) != 0) ++bits;  // of the keys, v itself among them
+  s.passes = (bits + 8) / 9;
+  s.bits = (bits + s.passes - 1) / s.passes;
+  s.n = c.n;
+  s.v = c.v;
+  s.per = ((c.n + kMaxParts - 1) / kMaxParts + kSortTile - 1) / kSortTile * kSortTile;
+  s.parts = (c.n + s.per - 1) / s.per;
+  Sum& m = p.sum;
+  m.piece = c.n < 65536 ? 32 : 128;
+  m.pieces = (c.n + m.piece - 1) / m.piece;
+  m.slices = (c.d + kSlice - 1) / kSlice;
+  m.warps = m.pieces * m.slices;
+  auto round = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
+  p.hist = round(static_cast<size_t>(s.parts) * (4u << s.bits));
+  p.key = round(static_cast<size_t>(c.n) * 4);
+  p.shares = round(static_cast<size_t>(m.pieces) * 2 * c.d * 4);
+  p.bytes = kMaxPasses * p.hist + 4 * p.key + p.shares;
+  return p;
+}
+
+template <typename D, typename T, int V>
+cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
+  const uint32_t zeros = c.add ? 0 : (c.v + p.sum.rows - 1) / p.sum.rows;
+  EmbedGradCall a = c;
+  if (p.few) {
+    if (c.n + zeros == 0) return cudaSuccess;
+    count_launch();
+    embed_grad_few_kernel<D, T, V><<<c.n + zeros, kThreadsFew, 0, stream>>>(a, p.sum.rows, p.sort.error);
+    return cudaGetLastError();
+  }
+  Sum s = p.sum;
+  void* params[] = {&a, &s};
+  count_launch();
+  cudaError_t err = launch_pdl(reinterpret_cast<const void*>(embed_sum_kernel<D, T, V>),
+                               dim3((s.warps + 7) / 8 + zeros), 256, 0, stream, params, false);
+  if (err != cudaSuccess) return err;
+  count_launch();
+  return launch_pdl(reinterpret_cast<const void*>(embed_join_kernel<T, V>),
+                    dim3((s.pieces + 7) / 8 * s.slices), 256, 0, stream, params, false);
+}
+
+template <typename D, typename T>
+cudaError_t launch_typed(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
+  constexpr uint32_t kWide = sizeof(D) == 2 && sizeof(T) == 2 ? 8 : 4;
+  if (p.v == kWide) return launch<D, T, kWide>(c, p, stream);
+  return p.v == 2 ? launch<D, T, 2>(c, p, stream) : launch<D, T, 1>(c, p, stream);
+}
+
+}  // namespace
+
+size_t embed_grad_scratch(const EmbedGradCall& c, const DeviceInfo& dev) { return plan_of(c, dev).bytes; }
+
+cudaError_t launch_embed_grad(const EmbedGradCall& c, Workspace& ws, const DeviceInfo& dev) {
+  Plan p = plan_of(c, dev);
+  p.sort.error = ws.u32(kOffError);
+  cudaError_t err = cudaSuccess;
+  if (!p.few) {
+    Sort& s = p.sort;
+    char* at = ws.model_scratch();
+    for (int i = 0; i < kMaxPasses; ++i) {
+      s.hist[i] = reinterpret_cast<uint32_t*>(at);
+      at += p.hist;
+    }
+    for (int i = 0; i < 2; ++i) {
+      s.key[i] = reinterpret_cast<uint32_t*>(at);
+      s.pos[i] = reinterpret_cast<uint32_t*>(at + p.key);
+      at += 2 * p.key;
+    }
+    p.sum.shares = reinterpret_cast<float*>(at);
+    p.sum.key = s.key[s.passes & 1u];
+    p.sum.pos = s.pos[s.passes & 1u];
+    s.token = c.token;
+    count_launch();
+    embed_count_kernel<<<s.parts, kSortThreads, 0, ws.stream>>>(s);
+    if ((err = cudaGetLastError()) != cudaSuccess) return err;
+    for (uint32_t pass = 0; pass < s.passes; ++pass) {
+      count_launch();
+      void* params[] = {&s, &pass};
+      err = launch_pdl(reinterpret_cast<const void*>(embed_scatter_kernel), dim3(s.parts), kSortThreads,
+                       0, ws.stream, params, false);
+      if (err != cudaSuccess) return err;
+    }
+  }
+  if (c.dout_bf16)
+    return c.dtable_bf16 ? launch_typed<bf16_t, bf16_t>(c, p, ws.stream) : launch_typed<bf16_t, float>(c, p, ws.stream);
+  return c.dtable_bf16 ? launch_typed<float, bf16_t>(c, p, ws.stream) : launch_typed<float, float>(c, p, ws.stream);
+}
+
+}  // namespace efs

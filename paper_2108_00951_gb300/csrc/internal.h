@@ -300,6 +300,84 @@ size_t ortho_plan(const OrthoMat* mats, uint32_t n, const DeviceInfo& dev,
 cudaError_t launch_orthogonalize(const OrthoMat* mats, uint32_t n, bool bf16, float mu,
                                  const void* plan, Workspace& ws, const DeviceInfo& dev);
 
+// Layer norm (norm.cu, norm_grad.cu). Types: fp32, or bf16 where the flag says so.
+struct NormCall {
+  const void* x;         // [n][ldx]
+  void* y;               // [n][ldy]
+  const void *w, *b;     // [d] or nullptr
+  float *mean, *rstd;    // [n] or nullptr
+  uint64_t ldx, ldy;
+  float eps;
+  uint32_t n, d;
+  bool x_bf16, y_bf16, w_bf16;
+  bool w_wide, b_wide;   // (the launcher's: on the boundary of the kernel's vectors)
+};
+cudaError_t launch_layer_norm(const NormCall& c, cudaStream_t stream);
+struct NormGradCall {
+  const void *x, *dy;    // [n][ldx], [n][lddy]
+  void* dx;              // [n][lddx], of x's type, or nullptr
+  const void* w;         // [d] or nullptr
+  void *dw, *db;         // [d] or nullptr, of w's type
+  const float *mean, *rstd;  // [n]
+  float* shares;         // (the launcher's: [parts][2][d])
+  uint64_t ldx, lddy, lddx;
+  uint32_t n, d;
+  bool x_bf16, y_bf16, w_bf16, w_wide;
+};
+size_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev);
+// ws: needed where there is scratch.
+cudaError_t launch_layer_norm_grad(NormGradCall c, Workspace* ws, cudaStream_t stream,
+                                   const DeviceInfo& dev);
+
+// Embedding rows by token and their gradient (embed.cu, embed_grad.cu).
+struct EmbedCall {
+  const void* table;     // [v][ld_table]
+  void* out;             // [n][ld_out]
+  const int64_t* token;  // [n]
+  uint64_t ld_table, ld_out;
+  uint32_t n, v, d;
+  float scale;
+  bool table_bf16, out_bf16;
+};
+cudaError_t launch_embed(const EmbedCall& c, Workspace& ws, const DeviceInfo& dev);
+struct EmbedGradCall {
+  const void* dout;      // [n][ld_dout]
+  void* dtable;          // [v][ld_dtable]
+  const int64_t* token;  // [n]
+  uint64_t ld_dout, ld_dtable;
+  uint32_t n, v, d;
+  float scale;
+  bool dout_bf16, dtable_bf16, add;
+};
+size_t embed_grad_scratch(const EmbedGradCall& c, const DeviceInfo& dev);
+cudaError_t launch_embed_grad(const EmbedGradCall& c, Workspace& ws, const DeviceInfo& dev);
+
+// AdamW over a list of tensors (adamw.cu).
+struct AdamTensor {
+  float* p;
+  const void* g;         // fp32 or bf16
+  void *m, *v;           // fp32, or codes of 8 bits with exponents me, ve
+  uint16_t* copy;        // bf16 or nullptr
+  uint8_t *me, *ve;
+  uint32_t numel;
+};
+struct AdamCall {
+  double lr, b1, b2, eps, decay;
+  uint64_t step, seed;
+  const float* lr_dev;        // or nullptr
+  const int64_t* step_dev;    // or nullptr
+  const float* grad_scale;    // or nullptr
+  bool g_bf16, eight;
+};
+cudaError_t launch_adamw(const AdamTensor* t, uint32_t n, const AdamCall& c, cudaStream_t stream);
+// The values that 8-bit states stand for.
+struct AdamStates {
+  const uint8_t *m, *v, *me, *ve;
+  void *m_out, *v_out;
+  uint32_t numel;
+};
+cudaError_t launch_adamw_states(const AdamStates* t, uint32_t n, bool out_bf16, cudaStream_t stream);
+
 // Launch bookkeeping.
 // A launch that may begin while the previous kernel on the stream finishes
 // (programmatic dependent launch: the kernel waits for its predecessor with

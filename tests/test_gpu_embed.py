@@ -1,0 +1,184 @@
+"""Embedding rows by token and the table's gradient, against the formulas in 64 bits.
+
+Bounds. A row of the lookup is one fp32 product, rounded to the output's type. A
+sum of k rows in fp32 is off by at most k 2^-24 of the sum of their magnitudes,
+its product with the scale (and its addition to what was there) by 2^-24 of the
+result, then the result is rounded to the table's type."""
+import pytest
+import torch
+
+import paper_2108_00951_gb300 as efs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def matrix(rows, cols, dtype, pad=0, offset=0, gen=None, scale=1.0):
+    buf = torch.full((rows * (cols + pad) + offset,), 7.0, device=DEV, dtype=dtype)
+    m = buf[offset:].view(rows, cols + pad)[:, :cols]
+    if gen is not None:
+        m.copy_(torch.randn(rows, cols, device=DEV, generator=gen) * scale)
+    return m, buf
+
+
+def around(m, buf, offset):
+    """The entries of buf outside its matrix."""
+    keep = torch.ones_like(buf, dtype=torch.bool)
+    cols = m.shape[1]
+    keep[offset:].view(m.shape[0], -1)[:, :cols] = False
+    return buf[keep]
+
+
+def tokens(n, v, gen, padding=0.2):
+    t = torch.exp(torch.rand(n, device=DEV, generator=gen) * torch.log(torch.tensor(float(v)))).long() - 1
+    t = t.clamp(0, v - 1)
+    t[torch.rand(n, device=DEV, generator=gen) < padding] = -1 - torch.randint(0, 1 << 40, (1,)).item()
+    return t
+
+
+LAYOUTS = [(BF16, BF16, 0, 0), (F32, F32, 0, 0), (F32, BF16, 2, 2), (BF16, F32, 3, 1), (BF16, BF16, 6, 2)]
+
+
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (1, 50, 650), (16, 28869, 650), (3, 7, 1023), (700, 31, 8),
+                                   (513, 1000, 96), (5000, 300, 257), (2, 3, 9000)])
+@pytest.mark.parametrize("tt,ot,pad,offset", LAYOUTS)
+def test_lookup(n, v, d, tt, ot, pad, offset):
+    g = torch.Generator(device=DEV).manual_seed(n + v + d)
+    table, _ = matrix(v, d, tt, pad, offset, g)
+    out, buf = matrix(n, d, ot, pad, offset)
+    t = tokens(n, v, g)
+    efs.ef_embed(table, t, out, scale=1.7)
+    ref = table.double()[t.clamp(min=0)] * float(torch.tensor(1.7)) * (t >= 0)[:, None]
+    off = (out.double() - ref).abs()
+    assert bool((off <= (torch.finfo(ot).eps / 2 + 2.0 ** -24) * (1 + 2.0 ** -8) * ref.abs()).all())
+    assert bool((around(out, buf, offset) == 7.0).all())
+    assert efs.ef_check_status() == efs.EF_OK
+
+
+def check_gradient(n, v, d, dt, tt, pad, offset, add, seed=0, t=None, scale=0.37):
+    g = torch.Generator(device=DEV).manual_seed(n + v + d + seed)
+    dout, _ = matrix(n, d, dt, pad, offset, g)
+    dtable, buf = matrix(v, d, tt, pad, offset, g if add else None)
+    t = tokens(n, v, g) if t is None else t
+    before = dtable.double().clone()
+    dout[t < 0] = float("nan")  # (padding is not used)
+    efs.ef_embed_grad(dout, t, dtable, scale=scale, accumulate=add)
+    keep = t >= 0
+    s = float(torch.tensor(scale))
+    rows = dout[keep].double()
+    zero = torch.zeros(v, d, device=DEV, dtype=torch.float64)
+    ref = zero.index_add(0, t[keep], rows) * s
+    mag = zero.index_add(0, t[keep], rows.abs()) * s
+    count = torch.zeros(v, device=DEV, dtype=torch.float64).index_add(0, t[keep], torch.ones_like(rows[:, 0]))
+    if add:
+        untouched = count == 0
+        assert torch.equal(dtable[untouched].double(), before[untouched])
+        ref = ref + before
+    bound = (count[:, None] + 2) * 2.0 ** -24 * mag + (torch.finfo(tt).eps / 2) * ref.abs() * (1 + 2.0 ** -8)
+    # (the addition to what was there may round a sum that then cancels)
+    bound = bound + 2.0 ** -24 * ref.abs() + 2.0 ** -140
+    assert bool(((dtable.double() - ref).abs() <= bound).all())
+    assert bool((around(dtable, buf, offset) == 7.0).all())
+    assert efs.ef_check_status() == efs.EF_OK
+    return dout, t, dtable
+
+
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (2, 5, 3), (700, 900, 650), (33, 4000, 1001), (2048, 40, 72),
+                                   (2049, 300, 257), (2500, 1, 8), (4096, 511, 96), (4097, 512, 130),
+                                   (10000, 100000, 33), (70001, 3000, 64), (20000, 300000, 16)])
+@pytest.mark.parametrize("dt,tt,pad,offset", LAYOUTS)
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient(n, v, d, dt, tt, pad, offset, add):
+    check_gradient(n, v, d, dt, tt, pad, offset, add)
+
+
+@pytest.mark.parametrize("n", [600, 2048, 2049, 40000, 65536, 131075])
+@pytest.mark.parametrize("kind", ["one", "none", "two", "runs", "last"])
+def test_gradient_of_uneven_tokens(n, kind):
+    v, d = 777, 300
+    t = {"one": torch.full((n,), 5, device=DEV), "none": torch.full((n,), -1, device=DEV),
+         "two": torch.arange(n, device=DEV) % 2 * (v - 1),
+         "runs": (torch.arange(n, device=DEV) // 97) % v,
+         "last": torch.where(torch.arange(n, device=DEV) == n - 1, v - 1, 3)}[kind]
+    check_gradient(n, v, d, BF16, F32, 0, 0, False, t=t)
+    check_gradient(n, v, d, F32, BF16, 0, 0, True, t=t)
+
+
+def test_many_digits():
+    """Words beyond two digits of nine bits, and beyond three."""
+    for v in ((1 << 18) - 1, 1 << 18, (1 << 27) + 5):
+        g = torch.Generator(device=DEV).manual_seed(v)
+        n, d = 5000, 4
+        t = torch.randint(0, v, (n,), device=DEV, generator=g)
+        t[:1000] = t[1000:2000]
+        t[17] = v - 1
+        dout = torch.randn(n, d, device=DEV, generator=g)
+        dtable = torch.full((v, d), 3.0, device=DEV)
+        efs.ef_embed_grad(dout, t, dtable, accumulate=True)
+        words, at = torch.unique(t, return_inverse=True)
+        ref = torch.zeros(len(words), d, device=DEV, dtype=torch.float64).index_add(0, at, dout.double()) + 3.0
+        assert bool(((dtable[words].double() - ref).abs() < 8 * 2.0 ** -22).all())
+        dtable[words] = 3.0
+        assert bool((dtable == 3.0).all())
+        del dtable
+
+
+@pytest.mark.parametrize("n", [300, 9000])
+def test_equal_inputs_give_equal_bits(n):
+    g = torch.Generator(device=DEV).manual_seed(n)
+    dout = torch.randn(n, 320, device=DEV, generator=g)
+    t = tokens(n, 200, g)
+    out = [torch.empty(200, 320, device=DEV) for _ in range(3)]
+    for o in out:
+        efs.ef_embed_grad(dout, t, o)
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+
+
+@pytest.mark.parametrize("n", [5, 300, 5000])
+def test_bad_tokens_are_latched(n):
+    v, d = 100, 24
+    g = torch.Generator(device=DEV).manual_seed(n)
+    t = torch.randint(0, v, (n,), device=DEV, generator=g)
+    good = t.clone()
+    t[n // 2], good[n // 2] = v, -1
+    t[0], good[0] = 1 << 62, -1
+    table = torch.randn(v, d, device=DEV, generator=g)
+    out, want = torch.empty(n, d, device=DEV), torch.empty(n, d, device=DEV)
+    efs.ef_embed(table, t, out)
+    assert efs.ef_check_status() == efs.EF_ERR_BAD_INPUT
+    efs.ef_embed(table, good, want)
+    assert efs.ef_check_status() == efs.EF_OK
+    assert torch.equal(out, want)
+    dt, want = torch.empty(v, d, device=DEV), torch.empty(v, d, device=DEV)
+    efs.ef_embed_grad(out, t, dt)
+    assert efs.ef_check_status() == efs.EF_ERR_BAD_INPUT
+    efs.ef_embed_grad(out, good, want)
+    assert efs.ef_check_status() == efs.EF_OK
+    assert torch.equal(dt, want)
+
+
+def test_no_tokens():
+    table = torch.randn(30, 8, device=DEV)
+    none = torch.empty(0, dtype=torch.int64, device=DEV)
+    efs.ef_embed(table, none, torch.empty(0, 8, device=DEV))
+    out = torch.full((30, 8), 2.0, device=DEV)
+    efs.ef_embed_grad(torch.empty(0, 8, device=DEV), none, out, accumulate=True)
+    assert bool((out == 2.0).all())
+    efs.ef_embed_grad(torch.empty(0, 8, device=DEV), none, out)
+    assert bool((out == 0.0).all())
+
+
+def test_gradient_is_the_lookups():
+    """<dout, lookup(table)> is linear in the table; its slope is the gradient."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    n, v, d = 3000, 400, 40
+    t, dout = tokens(n, v, g), torch.randn(n, d, device=DEV, generator=g)
+    dt, out = torch.empty(v, d, device=DEV), torch.empty(n, d, device=DEV)
+    efs.ef_embed_grad(dout, t, dt, scale=1.5)
+    for _ in range(5):
+        way = torch.randn(v, d, device=DEV, generator=g)
+        efs.ef_embed(way, t, out, scale=1.5)
+        left, right = (dout.double() * out).sum(), (dt.double() * way).sum()
+        size = (dout.double() * out).abs().sum()
+        assert abs(float(left - right)) < 3000 * 2.0 ** -24 * float(size)
