@@ -634,7 +634,10 @@ ef_status layer_norm_entry(const void* x, uint64_t ldx, ef_grad_type x_type, con
   c.x_bf16 = x_type == EF_GRAD_BF16;
   c.y_bf16 = y_type == EF_GRAD_BF16;
   c.w_bf16 = w_type == EF_GRAD_BF16;
-  return launch_layer_norm(c, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
+  DeviceInfo info;
+  const ef_status st = this_device(&info);
+  if (st != EF_OK) return st;
+  return launch_layer_norm(c, info, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
 }
 
 ef_status layer_norm_grad_entry(const void* x, uint64_t ldx, ef_grad_type x_type,
@@ -676,7 +679,8 @@ ef_status layer_norm_grad_entry(const void* x, uint64_t ldx, ef_grad_type x_type
   ef_status st = this_device(&info);
   if (st != EF_OK) return st;
   Workspace* ws = nullptr;
-  const size_t bytes = norm_grad_scratch(c, info);
+  size_t bytes = 0;
+  if (norm_grad_scratch(c, info, &bytes) != cudaSuccess) return EF_ERR_CUDA;
   if (bytes && (st = acquire_model_scratch(stream, bytes, &ws)) != EF_OK) return st;
   const cudaError_t err = launch_layer_norm_grad(c, ws, stream, info);
   if (ws) return finish_launch(err, ws);

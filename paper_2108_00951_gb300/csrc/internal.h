@@ -312,7 +312,7 @@ struct NormCall {
   bool x_bf16, y_bf16, w_bf16;
   bool w_wide, b_wide;   // (the launcher's: on the boundary of the kernel's vectors)
 };
-cudaError_t launch_layer_norm(const NormCall& c, cudaStream_t stream);
+cudaError_t launch_layer_norm(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream);
 struct NormGradCall {
   const void *x, *dy;    // [n][ldx], [n][lddy]
   void* dx;              // [n][lddx], of x's type, or nullptr
@@ -324,7 +324,7 @@ struct NormGradCall {
   uint32_t n, d;
   bool x_bf16, y_bf16, w_bf16, w_wide;
 };
-size_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev);
+cudaError_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev, size_t* bytes);
 // ws: needed where there is scratch.
 cudaError_t launch_layer_norm_grad(NormGradCall c, Workspace* ws, cudaStream_t stream,
                                    const DeviceInfo& dev);

@@ -3,66 +3,104 @@
 //
 // Both sums are fp32 over values that stay in registers, the second after the
 // mean is known (a difference of squares would lose the variance of rows whose
-// mean is large). What bounds it: reading x and writing y once. A row of at most
-// 1024 values lies in a warp (no barrier), one of at most 8192 in a CTA's
-// registers; a longer one is read three times, twice out of L1 and L2.
+// mean is large). What bounds it: reading x and writing y once. A warp (rows of at
+// most 1024 values, no barrier) or a CTA (at most 8192) takes rows a stride apart; the
+// next ones are on their way into a ring in shared memory meanwhile, and the
+// weights stay in registers. A longer row is read three times, twice out of L1
+// and L2.
+#include <algorithm>
+#include <map>
+#include <mutex>
+#include <tuple>
+
 #include "norm.cuh"
 
 namespace efs {
 namespace {
 
+constexpr uint32_t kWarpsPerCta = 4;
+// Rows that a group has in its ring, with K V values of a row a thread.
+template <int E, bool WARP>
+constexpr int kRing = !WARP ? 4 : E == 8 ? 8 : E == 16 ? 4 : 3;
+
 template <typename X, typename Y, int V, int K, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : kNormMaxThreads)
-    norm_kernel(const NormCall a) {
+__global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) norm_kernel(const NormCall a) {
+  constexpr int S = kRing<V * K, WARP>;
+  extern __shared__ __align__(16) char ring[];
   __shared__ float room[2][32];
   const uint32_t group = WARP ? 32u : blockDim.x;
   const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x;
-  const uint32_t row = WARP ? blockIdx.x * 4u + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= a.n) return;
-  const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx;
-  Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy;
-  Vec<X, V> in[K];
+  const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
+  const uint32_t first = WARP ? blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5) : blockIdx.x;
+  const uint32_t place = row_place(a.d, sizeof(X));
+  char* rows = ring + (WARP ? (threadIdx.x >> 5) * S * place : 0u);
+  auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
+  auto fetch = [&](uint32_t row, uint32_t slot) {
+    if (row < a.n) fetch_row(rows + slot * place, x_row(row), a.d * sizeof(X), t, group);
+    fetch_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
+  float w[K][V], b[K][V];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t c = (k * group + t) * V;
-    if (c < a.d) in[k].load(x + c);
-    else in[k].clear();
+    if (c < a.d) {
+      load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+      load_weights<V>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
+    }
   }
-  float sum = 0.0f;
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) sum += in[k].get(j);
   const float inv = 1.0f / static_cast<float>(a.d);
-  const float mean = (WARP ? warp_sum(sum) : cta_sum(sum, room[0])) * inv;
-  sum = 0.0f;
+  uint32_t slot = 0;
+  for (uint32_t row = first; row < a.n; row += groups) {
+    fetch_wait<S - 2>();
+    if (WARP) __syncwarp();
+    else __syncthreads();
+    // (all threads are done with the row before: its place is free)
+    fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
+    const char* in_row = rows + slot * place + row_lead(x_row(row));
+    slot = slot == S - 1 ? 0 : slot + 1;
+    Vec<X, V> in[K];
+    float sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    if ((k * group + t) * V < a.d)
+    for (int k = 0; k < K; ++k) {
+      const uint32_t c = (k * group + t) * V;
+      if (c < a.d) {
+        in[k] = staged<X, V>(in_row, c);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float off = in[k].get(j) - mean;
-        sum = fmaf(off, off, sum);
+        for (int j = 0; j < V; ++j) sum += in[k].get(j);
       }
-  }
-  const float var = (WARP ? warp_sum(sum) : cta_sum(sum, room[1])) * inv;
-  const float rstd = 1.0f / sqrtf(var + a.eps);
+    }
+    const float mean = (WARP ? warp_sum(sum) : cta_sum(sum, room[0])) * inv;
+    sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const uint32_t c = (k * group + t) * V;
-    if (c >= a.d) break;
-    float w[V], b[V], out[V];
-    load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w);
-    load_weights<V>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b);
+    for (int k = 0; k < K; ++k) {
+      if ((k * group + t) * V < a.d)
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = fmaf((in[k].get(j) - mean) * rstd, w[j], b[j]);
-    Vec<Y, V> o;
-    o.round(out);
-    o.store(y + c);
-  }
-  if (t == 0) {
-    if (a.mean) a.mean[row] = mean;
-    if (a.rstd) a.rstd[row] = rstd;
+        for (int j = 0; j < V; ++j) {
+          const float off = in[k].get(j) - mean;
+          sum = fmaf(off, off, sum);
+        }
+    }
+    const float var = (WARP ? warp_sum(sum) : cta_sum(sum, room[1])) * inv;
+    const float rstd = 1.0f / sqrtf(var + a.eps);
+    Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t c = (k * group + t) * V;
+      if (c < a.d) {
+        float out[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = fmaf((in[k].get(j) - mean) * rstd, w[k][j], b[k][j]);
+        Vec<Y, V> o;
+        o.round(out);
+        o.store(y + c);
+      }
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
   }
 }
 
@@ -97,48 +135,79 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
   }
 }
 
-template <typename X, typename Y, int V>
-cudaError_t launch(const NormCall& c, cudaStream_t stream) {
-  const uint32_t rows4 = (c.n + 3) / 4;
-  if (c.d <= 256) {
-    norm_kernel<X, Y, V, 8 / V, true><<<rows4, 128, 0, stream>>>(c);
-  } else if (c.d <= 512) {
-    norm_kernel<X, Y, V, 16 / V, true><<<rows4, 128, 0, stream>>>(c);
-  } else if (c.d <= 1024) {
-    norm_kernel<X, Y, V, 32 / V, true><<<rows4, 128, 0, stream>>>(c);
-  } else {
-    const uint32_t threads = ((c.d + 15) / 16 + 31) / 32 * 32;
-    norm_kernel<X, Y, V, 16 / V, false><<<c.n, threads, 0, stream>>>(c);
-  }
+template <typename X, typename Y, int V, int K, bool WARP>
+cudaError_t launch_rows(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
+  const uint32_t warps = WARP ? kWarpsPerCta : 1;  // groups of a CTA
+  const uint32_t threads =
+      WARP ? 32 * kWarpsPerCta : ((c.d + kNormPerThread - 1) / kNormPerThread + 31) / 32 * 32;
+  const uint32_t smem = warps * kRing<V * K, WARP> * row_place(c.d, sizeof(X));
+  const void* fn = reinterpret_cast<const void*>(norm_kernel<X, Y, V, K, WARP>);
+  uint32_t per_sm = 0;
+  const cudaError_t err = resident_ctas(fn, threads, smem, &per_sm);
+  if (err != cudaSuccess) return err;
+  const uint32_t grid = std::min((c.n + warps - 1) / warps, per_sm * static_cast<uint32_t>(dev.sm_count));
+  norm_kernel<X, Y, V, K, WARP><<<grid, threads, smem, stream>>>(c);
   return cudaGetLastError();
 }
 
+template <typename X, typename Y, int V>
+cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
+  if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, true>(c, dev, stream);
+  if (c.d <= 512) return launch_rows<X, Y, V, 16 / V, true>(c, dev, stream);
+  if (c.d <= kNormWarpWidth) return launch_rows<X, Y, V, 32 / V, true>(c, dev, stream);
+  return launch_rows<X, Y, V, kNormPerThread / V, false>(c, dev, stream);
+}
+
 template <typename X, typename Y>
-cudaError_t launch_typed(NormCall c, cudaStream_t stream) {
-  if (c.d > 16 * kNormMaxThreads) {
+cudaError_t launch_typed(NormCall c, const DeviceInfo& dev, cudaStream_t stream) {
+  if (c.d > kNormCtaWidth) {
     norm_long_kernel<X, Y><<<c.n, 1024, 0, stream>>>(c);
     return cudaGetLastError();
   }
   constexpr uint32_t kWide = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
   auto allow = [&](uint32_t v) {
-    return c.d % v == 0 && rows_allow(reinterpret_cast<uintptr_t>(c.x), c.n > 1 ? c.ldx : 0, sizeof(X), v) &&
-           rows_allow(reinterpret_cast<uintptr_t>(c.y), c.n > 1 ? c.ldy : 0, sizeof(Y), v);
+    return c.d % v == 0 && rows_allow(c.x, c.n > 1 ? c.ldx : 0, sizeof(X), v) &&
+           rows_allow(c.y, c.n > 1 ? c.ldy : 0, sizeof(Y), v);
   };
   const uint32_t v = allow(kWide) ? kWide : allow(2) ? 2 : 1;
-  const uint64_t wsize = c.w_bf16 ? 2 : 4, part = c.w_bf16 ? v : (v > 4 ? 4 : v);
-  c.w_wide = rows_allow(reinterpret_cast<uintptr_t>(c.w), 0, wsize, part);
-  c.b_wide = rows_allow(reinterpret_cast<uintptr_t>(c.b), 0, wsize, part);
-  if (v == kWide) return launch<X, Y, kWide>(c, stream);
-  return v == 2 ? launch<X, Y, 2>(c, stream) : launch<X, Y, 1>(c, stream);
+  const uint64_t wsize = c.w_bf16 ? 2 : 4;
+  const uint32_t part = c.w_bf16 ? v : std::min(v, 4u);
+  c.w_wide = rows_allow(c.w, 0, wsize, part);
+  c.b_wide = rows_allow(c.b, 0, wsize, part);
+  if (v == kWide) return launch<X, Y, kWide>(c, dev, stream);
+  return v == 2 ? launch<X, Y, 2>(c, dev, stream) : launch<X, Y, 1>(c, dev, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_layer_norm(const NormCall& c, cudaStream_t stream) {
+cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t* ctas) {
+  static std::mutex mu;
+  static std::map<std::tuple<int, const void*, uint32_t, uint32_t>, uint32_t> known;
+  int dev = 0, n = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  std::lock_guard<std::mutex> lk(mu);
+  const auto key = std::make_tuple(dev, kernel, threads, smem);
+  const auto it = known.find(key);
+  if (it != known.end()) {
+    *ctas = it->second;
+    return cudaSuccess;
+  }
+  // (an opt-in stays: the largest asked for, whatever order sizes come in)
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  if (err == cudaSuccess) err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem);
+  if (err != cudaSuccess) return err;
+  if (n < 1) return cudaErrorLaunchOutOfResources;
+  known.emplace(key, static_cast<uint32_t>(n));
+  *ctas = static_cast<uint32_t>(n);
+  return cudaSuccess;
+}
+
+cudaError_t launch_layer_norm(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
   count_launch();
   if (c.x_bf16)
-    return c.y_bf16 ? launch_typed<bf16_t, bf16_t>(c, stream) : launch_typed<bf16_t, float>(c, stream);
-  return c.y_bf16 ? launch_typed<float, bf16_t>(c, stream) : launch_typed<float, float>(c, stream);
+    return c.y_bf16 ? launch_typed<bf16_t, bf16_t>(c, dev, stream) : launch_typed<bf16_t, float>(c, dev, stream);
+  return c.y_bf16 ? launch_typed<float, bf16_t>(c, dev, stream) : launch_typed<float, float>(c, dev, stream);
 }
 
 }  // namespace efs

@@ -5,10 +5,11 @@
 //   dw = sum over rows of dy x',   db = sum over rows of dy.
 //
 // What bounds it: reading x and dy and writing dx once. A warp (rows of at most
-// 1024 values) or a CTA takes rows a stride apart and keeps its columns' shares
-// of dw and db in registers, or in shared memory for long rows; the CTAs' shares
-// are joined by a second kernel in the order of the CTAs, so equal inputs give
-// equal bits.
+// 1024 values) or a CTA (at most 8192) takes rows a stride apart, the next ones on
+// their way into a ring in shared memory, and keeps its columns' shares of dw and
+// db in registers (in shared memory for longer rows); the CTAs' shares are
+// joined by a second kernel in the order of the CTAs, so equal inputs give equal
+// bits.
 #include <algorithm>
 
 #include "norm.cuh"
@@ -16,8 +17,11 @@
 namespace efs {
 namespace {
 
-constexpr int kWarpsPerCta = 8;
+constexpr uint32_t kWarpsPerCta = 8;
 constexpr uint32_t kJoinColumns = 32, kJoinRows = 8;
+// Rows that a group has in its ring, with E values of a row a thread.
+template <int E, bool WARP>
+constexpr int kRing = !WARP ? 3 : E == 8 ? 6 : E == 16 ? 4 : 3;
 
 // A share of columns c of dw and db; the only one is the result.
 __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t share, uint32_t parts,
@@ -38,40 +42,61 @@ __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t shar
   }
 }
 
-// Rows of at most 32 V K values, a warp each.
-template <typename X, typename Y, int V, int K>
-__global__ void __launch_bounds__(32 * kWarpsPerCta) norm_grad_warp_kernel(const NormGradCall a) {
-  extern __shared__ float shares[];  // [kWarpsPerCta][d]
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const float inv = 1.0f / static_cast<float>(a.d);
-  float dw[K][V] = {}, db[K][V] = {};
-  for (uint32_t row = blockIdx.x * kWarpsPerCta + warp; row < a.n; row += gridDim.x * kWarpsPerCta) {
-    const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx;
-    const Y* dy = static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy;
-    Vec<X, V> xs[K];
-    Vec<Y, V> dys[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * 32 + lane) * V;
-      if (c < a.d) {
-        xs[k].load(x + c);
-        dys[k].load(dy + c);
-      } else {
-        xs[k].clear();
-        dys[k].clear();
-      }
+// Rows of at most K V times the threads of a group (a warp, or a CTA).
+template <typename X, typename Y, int V, int K, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
+    norm_grad_kernel(const NormGradCall a) {
+  constexpr int S = kRing<V * K, WARP>;
+  extern __shared__ __align__(16) char ring[];
+  __shared__ float room[64];
+  const uint32_t group = WARP ? 32u : blockDim.x;
+  const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x, warp = threadIdx.x >> 5;
+  const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
+  const uint32_t first = WARP ? blockIdx.x * kWarpsPerCta + warp : blockIdx.x;
+  const uint32_t x_place = row_place(a.d, sizeof(X)), place = x_place + row_place(a.d, sizeof(Y));
+  char* rows = ring + (WARP ? warp * S * place : 0u);
+  auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
+  auto dy_row = [&](uint32_t row) { return static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy; };
+  auto fetch = [&](uint32_t row, uint32_t slot) {
+    if (row < a.n) {
+      fetch_row(rows + slot * place, x_row(row), a.d * sizeof(X), t, group);
+      fetch_row(rows + slot * place + x_place, dy_row(row), a.d * sizeof(Y), t, group);
     }
-    const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+    fetch_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
+  float mean = 0.0f, rstd = 0.0f;
+  if (first < a.n) mean = __ldg(a.mean + first), rstd = __ldg(a.rstd + first);
+  float w[K][V], dw[K][V] = {}, db[K][V] = {};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t c = (k * group + t) * V;
+    if (c < a.d) load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+  }
+  const float inv = 1.0f / static_cast<float>(a.d);
+  uint32_t slot = 0;
+  for (uint32_t row = first; row < a.n; row += groups) {
+    fetch_wait<S - 2>();
+    if (WARP) __syncwarp();
+    else __syncthreads();
+    // (all threads are done with the row before: its place is free)
+    fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
+    const float mu = mean, r = rstd;
+    if (row + groups < a.n) mean = __ldg(a.mean + row + groups), rstd = __ldg(a.rstd + row + groups);
+    const char* xs = rows + slot * place + row_lead(x_row(row));
+    const char* dys = rows + slot * place + x_place + row_lead(dy_row(row));
+    slot = slot == S - 1 ? 0 : slot + 1;
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * 32 + lane) * V;
+      const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        float w[V];
-        load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w);
+        const Vec<X, V> x = staged<X, V>(xs, c);
+        const Vec<Y, V> dy = staged<Y, V>(dys, c);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float hat = (xs[k].get(j) - mean) * rstd, g = dys[k].get(j), q = g * w[j];
+          const float hat = (x.get(j) - mu) * r, g = dy.get(j), q = g * w[k][j];
           s1 += q;
           s2 = fmaf(q, hat, s2);
           dw[k][j] = fmaf(g, hat, dw[k][j]);
@@ -80,19 +105,28 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta) norm_grad_warp_kernel(const
       }
     }
     if (!a.dx) continue;
-    s1 = warp_sum(s1) * inv;
-    s2 = warp_sum(s2) * inv;
+    if (WARP) {
+      s1 = warp_sum(s1);
+      s2 = warp_sum(s2);
+    } else {
+      const float2 s = cta_sum2(s1, s2, room);
+      s1 = s.x;
+      s2 = s.y;
+    }
+    s1 *= inv;
+    s2 *= inv;
     X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * 32 + lane) * V;
+      const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        float w[V], out[V];
-        load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w);
+        const Vec<X, V> x = staged<X, V>(xs, c);
+        const Vec<Y, V> dy = staged<Y, V>(dys, c);
+        float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float hat = (xs[k].get(j) - mean) * rstd;
-          out[j] = rstd * (fmaf(dys[k].get(j), w[j], -s1) - hat * s2);
+          const float hat = (x.get(j) - mu) * r;
+          out[j] = r * (fmaf(dy.get(j), w[k][j], -s1) - hat * s2);
         }
         Vec<X, V> o;
         o.round(out);
@@ -101,8 +135,21 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta) norm_grad_warp_kernel(const
     }
   }
   if (!a.dw && !a.db) return;
-  // the warps' shares, summed in their order
-  float sums[K * V * 32 / (32 * kWarpsPerCta)];
+  if (!WARP) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const uint32_t c = (k * group + t) * V + j;
+        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j], db[k][j]);
+      }
+    return;
+  }
+  // the warps' shares, summed in their order (in the ring's place: at least as large)
+  fetch_wait<0>();
+  float* shares = reinterpret_cast<float*>(ring);  // [kWarpsPerCta][d]
+  constexpr int kOut = (V * K + kWarpsPerCta - 1) / kWarpsPerCta;
+  float sums[kOut];
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
@@ -110,100 +157,22 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta) norm_grad_warp_kernel(const
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const uint32_t c = (k * 32 + lane) * V + j;
+        const uint32_t c = (k * 32 + t) * V + j;
         if (c < a.d) shares[warp * a.d + c] = which ? db[k][j] : dw[k][j];
       }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < K * V / kWarpsPerCta; ++i) {
+    for (int i = 0; i < kOut; ++i) {
       const uint32_t c = i * 32 * kWarpsPerCta + threadIdx.x;
       if (c < a.d) {
         float s = 0.0f;
 #pragma unroll
-        for (int r = 0; r < kWarpsPerCta; ++r) s += shares[r * a.d + c];
+        for (uint32_t q = 0; q < kWarpsPerCta; ++q) s += shares[q * a.d + c];
         if (which) write_share(a, blockIdx.x, gridDim.x, c, sums[i], s);
         else sums[i] = s;
       }
     }
   }
-}
-
-// Rows of at most V K times the threads, a CTA each; the next row is loaded
-// before this one's sums are joined.
-template <typename X, typename Y, int V, int K>
-__global__ void __launch_bounds__(kNormMaxThreads) norm_grad_cta_kernel(const NormGradCall a) {
-  __shared__ float room[2][64];
-  const float inv = 1.0f / static_cast<float>(a.d);
-  const uint32_t threads = blockDim.x, t = threadIdx.x;
-  float dw[K][V] = {}, db[K][V] = {};
-  Vec<X, V> xs[K];
-  Vec<Y, V> dys[K];
-  float mean = 0.0f, rstd = 0.0f;
-  auto load = [&](uint32_t row) {
-    const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx;
-    const Y* dy = static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * threads + t) * V;
-      if (c < a.d) {
-        xs[k].load(x + c);
-        dys[k].load(dy + c);
-      } else {
-        xs[k].clear();
-        dys[k].clear();
-      }
-    }
-    mean = __ldg(a.mean + row);
-    rstd = __ldg(a.rstd + row);
-  };
-  uint32_t parity = 0;
-  if (blockIdx.x < a.n) load(blockIdx.x);
-  for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x, parity ^= 1u) {
-    float hat[K][V], q[K][V], s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * threads + t) * V;
-      float w[V];
-      if (c < a.d) {
-        load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float g = dys[k].get(j);
-          hat[k][j] = (xs[k].get(j) - mean) * rstd;
-          q[k][j] = g * w[j];
-          s1 += q[k][j];
-          s2 = fmaf(q[k][j], hat[k][j], s2);
-          dw[k][j] = fmaf(g, hat[k][j], dw[k][j]);
-          db[k][j] += g;
-        }
-      }
-    }
-    const float scale = rstd;
-    if (row + gridDim.x < a.n) load(row + gridDim.x);
-    if (!a.dx) continue;
-    const float2 s = cta_sum2(s1, s2, room[parity]);
-    X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * threads + t) * V;
-      if (c < a.d) {
-        float out[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = scale * (q[k][j] - s.x * inv - hat[k][j] * (s.y * inv));
-        Vec<X, V> o;
-        o.round(out);
-        o.store(dx + c);
-      }
-    }
-  }
-  if (!a.dw && !a.db) return;
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const uint32_t c = (k * threads + t) * V + j;
-      if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j], db[k][j]);
-    }
 }
 
 // Rows of any length, a CTA each, read twice (the second time out of L2). SHARES:
@@ -299,46 +268,58 @@ __global__ void __launch_bounds__(kJoinColumns * kJoinRows) norm_join_kernel(con
 
 constexpr uint32_t kSharesWidth = 28000;  // columns whose shares fit shared memory
 
-// How many CTAs take the rows, and how many shares of dw and db they leave.
-struct Grid {
-  uint32_t ctas, parts;
+// A call's kernel, its CTAs, and how many shares of dw and db they leave.
+struct Plan {
+  const void* kernel;
+  uint32_t v, ctas, threads, smem, parts;
 };
-Grid grid_of(const NormGradCall& c, const DeviceInfo& dev) {
-  const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
-  if (c.n == 0) return {0, 0};
-  if (c.d <= 1024) {
-    const uint32_t grid = std::min((c.n + kWarpsPerCta - 1) / kWarpsPerCta, sms * (c.d <= 512 ? 2 : 1));
-    return {grid, grid};
-  }
-  if (c.d <= 16 * kNormMaxThreads) {
-    const uint32_t grid = std::min(c.n, sms * (c.d <= 2048 ? 4 : c.d <= 4096 ? 2 : 1));
-    return {grid, grid};
-  }
-  const uint32_t grid = std::min(c.n, sms);
-  if (c.d <= kSharesWidth) return {grid, grid};
-  const uint32_t wide = (c.d + 1023) / 1024;
-  return {grid, std::min((c.n + 15) / 16, (8 * sms + wide - 1) / wide)};
-}
 
+template <typename X, typename Y, int V, int K, bool WARP>
+cudaError_t plan_rows(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
+  const uint32_t warps = WARP ? kWarpsPerCta : 1;  // groups of a CTA
+  p.kernel = reinterpret_cast<const void*>(norm_grad_kernel<X, Y, V, K, WARP>);
+  p.threads = WARP ? 32 * kWarpsPerCta : ((c.d + kNormPerThread - 1) / kNormPerThread + 31) / 32 * 32;
+  p.smem = warps * kRing<V * K, WARP> * (row_place(c.d, sizeof(X)) + row_place(c.d, sizeof(Y)));
+  uint32_t per_sm = 0;
+  const cudaError_t err = resident_ctas(p.kernel, p.threads, p.smem, &per_sm);
+  p.parts = p.ctas = std::min((c.n + warps - 1) / warps, per_sm * static_cast<uint32_t>(dev.sm_count));
+  return err;
+}
 template <typename X, typename Y, int V>
-cudaError_t launch(const NormGradCall& c, uint32_t grid, cudaStream_t stream) {
-  const uint32_t smem = c.d * kWarpsPerCta * 4;
-  if (c.d <= 256) {
-    norm_grad_warp_kernel<X, Y, V, 8 / V><<<grid, 256, smem, stream>>>(c);
-  } else if (c.d <= 512) {
-    norm_grad_warp_kernel<X, Y, V, 16 / V><<<grid, 256, smem, stream>>>(c);
-  } else if (c.d <= 1024) {
-    norm_grad_warp_kernel<X, Y, V, 32 / V><<<grid, 256, smem, stream>>>(c);
-  } else if (c.d <= 8 * kNormMaxThreads) {
-    norm_grad_cta_kernel<X, Y, V, 8 / V><<<grid, ((c.d + 7) / 8 + 31) / 32 * 32, 0, stream>>>(c);
-  } else {
-    norm_grad_cta_kernel<X, Y, V, 16 / V><<<grid, ((c.d + 15) / 16 + 31) / 32 * 32, 0, stream>>>(c);
+cudaError_t plan_width(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
+  if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, true>(c, dev, p);
+  if (c.d <= 512) return plan_rows<X, Y, V, 16 / V, true>(c, dev, p);
+  if (c.d <= kNormWarpWidth) return plan_rows<X, Y, V, 32 / V, true>(c, dev, p);
+  return plan_rows<X, Y, V, kNormPerThread / V, false>(c, dev, p);
+}
+template <typename X, typename Y>
+cudaError_t plan_typed(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
+  constexpr uint32_t kWide = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
+  const bool many = c.n > 1;
+  auto allow = [&](uint32_t v) {
+    return c.d % v == 0 && rows_allow(c.x, many ? c.ldx : 0, sizeof(X), v) &&
+           rows_allow(c.dy, many ? c.lddy : 0, sizeof(Y), v) &&
+           rows_allow(c.dx, many && c.dx ? c.lddx : 0, sizeof(X), v);
+  };
+  p.v = allow(kWide) ? kWide : allow(2) ? 2 : 1;
+  if (p.v == kWide) return plan_width<X, Y, kWide>(c, dev, p);
+  return p.v == 2 ? plan_width<X, Y, 2>(c, dev, p) : plan_width<X, Y, 1>(c, dev, p);
+}
+cudaError_t plan_of(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
+  p = {};
+  if (c.n == 0) return cudaSuccess;
+  if (c.d <= kNormCtaWidth) {
+    if (c.x_bf16) return c.y_bf16 ? plan_typed<bf16_t, bf16_t>(c, dev, p) : plan_typed<bf16_t, float>(c, dev, p);
+    return c.y_bf16 ? plan_typed<float, bf16_t>(c, dev, p) : plan_typed<float, float>(c, dev, p);
   }
-  return cudaGetLastError();
+  const uint32_t sms = static_cast<uint32_t>(dev.sm_count), wide = (c.d + 1023) / 1024;
+  p.parts = p.ctas = std::min(c.n, sms);
+  if (c.d > kSharesWidth) p.parts = std::min((c.n + 15) / 16, (8 * sms + wide - 1) / wide);
+  return cudaSuccess;
 }
 
 template <typename X, typename Y>
-cudaError_t launch_long(const NormGradCall& c, const Grid& grid, cudaStream_t stream) {
+cudaError_t launch_long(const NormGradCall& c, const Plan& p, cudaStream_t stream) {
   cudaError_t err = cudaSuccess;
   const bool shares = c.dw || c.db;
   if (shares && c.d <= kSharesWidth) {
@@ -346,63 +327,52 @@ cudaError_t launch_long(const NormGradCall& c, const Grid& grid, cudaStream_t st
                                cudaFuncAttributeMaxDynamicSharedMemorySize, kSharesWidth * 8);
     if (err != cudaSuccess) return err;
     count_launch();
-    norm_grad_long_kernel<X, Y, true><<<grid.ctas, 1024, c.d * 8, stream>>>(c);
+    norm_grad_long_kernel<X, Y, true><<<p.ctas, 1024, c.d * 8, stream>>>(c);
     return cudaGetLastError();
   }
   if (c.dx) {
     count_launch();
-    norm_grad_long_kernel<X, Y, false><<<grid.ctas, 1024, 0, stream>>>(c);
+    norm_grad_long_kernel<X, Y, false><<<p.ctas, 1024, 0, stream>>>(c);
     if ((err = cudaGetLastError()) != cudaSuccess) return err;
   }
   if (shares) {
     count_launch();
     norm_grad_columns_kernel<X, Y>
-        <<<dim3((c.d + 1023) / 1024, grid.parts), 256, 0, stream>>>(c, grid.parts);
+        <<<dim3((c.d + 1023) / 1024, p.parts), 256, 0, stream>>>(c, p.parts);
     err = cudaGetLastError();
   }
   return err;
 }
 
-template <typename X, typename Y>
-cudaError_t launch_typed(NormGradCall c, const Grid& grid, cudaStream_t stream) {
-  if (c.n == 0) return cudaSuccess;
-  if (c.d > 16 * kNormMaxThreads) return launch_long<X, Y>(c, grid, stream);
-  constexpr uint32_t kWide = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
-  const bool many = c.n > 1;
-  auto allow = [&](uint32_t v) {
-    return c.d % v == 0 &&
-           rows_allow(reinterpret_cast<uintptr_t>(c.x), many ? c.ldx : 0, sizeof(X), v) &&
-           rows_allow(reinterpret_cast<uintptr_t>(c.dy), many ? c.lddy : 0, sizeof(Y), v) &&
-           rows_allow(reinterpret_cast<uintptr_t>(c.dx), many ? c.lddx : 0, sizeof(X), v);
-  };
-  const uint32_t v = allow(kWide) ? kWide : allow(2) ? 2 : 1;
-  c.w_wide = rows_allow(reinterpret_cast<uintptr_t>(c.w), 0, c.w_bf16 ? 2 : 4,
-                        c.w_bf16 ? v : (v > 4 ? 4 : v));
-  count_launch();
-  if (v == kWide) return launch<X, Y, kWide>(c, grid.ctas, stream);
-  return v == 2 ? launch<X, Y, 2>(c, grid.ctas, stream) : launch<X, Y, 1>(c, grid.ctas, stream);
-}
-
 }  // namespace
 
-size_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev) {
-  if (!c.dw && !c.db) return 0;
-  const uint32_t parts = grid_of(c, dev).parts;
-  return parts > 1 ? static_cast<size_t>(parts) * 2 * c.d * sizeof(float) : 0;
+cudaError_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev, size_t* bytes) {
+  Plan p;
+  const cudaError_t err = plan_of(c, dev, p);
+  *bytes = (c.dw || c.db) && p.parts > 1 ? static_cast<size_t>(p.parts) * 2 * c.d * sizeof(float) : 0;
+  return err;
 }
 
 cudaError_t launch_layer_norm_grad(NormGradCall c, Workspace* ws, cudaStream_t stream,
                                    const DeviceInfo& dev) {
-  Grid grid = grid_of(c, dev);
+  Plan p;
+  cudaError_t err = plan_of(c, dev, p);
+  if (err != cudaSuccess) return err;
   c.shares = ws ? reinterpret_cast<float*>(ws->model_scratch()) : nullptr;
-  cudaError_t err;
-  if (c.x_bf16)
-    err = c.y_bf16 ? launch_typed<bf16_t, bf16_t>(c, grid, stream) : launch_typed<bf16_t, float>(c, grid, stream);
-  else
-    err = c.y_bf16 ? launch_typed<float, bf16_t>(c, grid, stream) : launch_typed<float, float>(c, grid, stream);
-  if (err != cudaSuccess || (!c.dw && !c.db) || grid.parts == 1) return err;
+  if (c.n == 0) {
+  } else if (p.kernel) {
+    c.w_wide = rows_allow(c.w, 0, c.w_bf16 ? 2 : 4, c.w_bf16 ? p.v : std::min(p.v, 4u));
+    void* params[] = {&c};
+    count_launch();
+    err = cudaLaunchKernel(p.kernel, dim3(p.ctas), dim3(p.threads), params, p.smem, stream);
+  } else if (c.x_bf16) {
+    err = c.y_bf16 ? launch_long<bf16_t, bf16_t>(c, p, stream) : launch_long<bf16_t, float>(c, p, stream);
+  } else {
+    err = c.y_bf16 ? launch_long<float, bf16_t>(c, p, stream) : launch_long<float, float>(c, p, stream);
+  }
+  if (err != cudaSuccess || (!c.dw && !c.db) || p.parts == 1) return err;
   count_launch();
-  void* params[] = {&c, &grid.parts};
+  void* params[] = {&c, &p.parts};
   return launch_pdl(reinterpret_cast<const void*>(norm_join_kernel),
                     dim3((2 * c.d + kJoinColumns - 1) / kJoinColumns), kJoinColumns * kJoinRows, 0,
                     stream, params, false);
