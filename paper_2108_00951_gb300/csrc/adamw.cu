@@ -70,42 +70,113 @@ struct Hyper {
 
 // One entry: m and v as they are kept in fp32 (each operation rounded by itself),
 // p by approximate root and quotient (2^-22 of the update, lr times which is far
-// below p's last place).
+// below p's last place). (Packed in pairs the operations would be half as many, but
+// the assembler fuses packed products and sums, whatever rounding they name.)
 __device__ __forceinline__ void update(const Hyper& h, float& p, float g, float& m, float& v) {
+  g *= h.scale;
   m = m * h.b1 + g * h.c1;
   v = v * h.b2 + g * g * h.c2;
-  float root;
+  float root, inverse;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
-  const float u = __fdividef(m, fmaf(root, h.root, h.eps));
-  p = fmaf(-h.step_size, u, p * h.keep);
+  // (of 2^-75 or more, or 0: nothing to flush)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, h.root, h.eps)));
+  p = fmaf(-h.step_size, m * inverse, p * h.keep);
 }
 
-template <bool SIGNED>
-__device__ __forceinline__ float decode(uint32_t code, float f) {
-  const uint32_t a = SIGNED ? code & 127u : code;
-  float x = __uint_as_float(a << 20) * power(126) * f;
-  if (a == (SIGNED ? 127u : 255u)) x = __int_as_float(0x7fffffff);
-  return SIGNED && (code & 128u) ? -x : x;
+// A code's value from byte j of a word, in units of f: 2^(127 + E - top), which is
+// in fp32's range for E up to top; above, the rest of it comes after.
+__device__ __forceinline__ float decode_m(uint32_t word, int j, float f) {
+  const int t = static_cast<int>(__byte_perm(word, 0u, 0x0444u | (j << 12)));  // the byte on top
+  return __int_as_float((t >> 4) & 0x87f00000) * f;
 }
-// The factor of a block's values: 2^(E - top + 1).
-__device__ __forceinline__ float decode_factor(uint32_t e, int top) {
-  return power(max(static_cast<int>(e) - 127, kLeast) - top + 1);
+__device__ __forceinline__ float decode_v(uint32_t word, int j, float f) {
+  return __uint_as_float(__byte_perm(word, 0u, 0x4044u | (j << 8)) << 4) * f;
 }
+__device__ __forceinline__ void decode(uint32_t mc, uint32_t vc, int em, int ev, float (&m)[4], float (&v)[4]) {
+  const float fm = power(127 + min(em, kTopM) - kTopM), fv = power(127 + min(ev, kTopV) - kTopV);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m[j] = decode_m(mc, j, fm), v[j] = decode_v(vc, j, fv);
+  if (em > kTopM || ev > kTopV) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] *= power(max(em - kTopM, 0));
+      v[j] *= power(max(ev - kTopV, 0));
+    }
+  }
+  // the codes of NaN: a byte of m with seven ones, one of v with eight
+  if ((((mc & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) | ((~vc - 0x01010101u) & vc & 0x80808080u)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (((mc >> (8 * j)) & 127u) == 127u) m[j] = __int_as_float(0x7fffffff);
+      if (((vc >> (8 * j)) & 255u) == 255u) v[j] = __int_as_float(0x7fffffff);
+    }
+  }
+}
+__device__ __forceinline__ int exponent_of(uint32_t e) { return max(static_cast<int>(e) - 127, kLeast); }
 
-// The bits of |x| where it can be held, 0 elsewhere (NaN, or 2^127 and more).
-__device__ __forceinline__ uint32_t held_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-  return b < 0x7f000000u ? b : 0u;
+constexpr uint32_t kTooLarge = 0x7f000000u;  // the bits of 2^127: not held from there on
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t held_bits(float x) { return magnitude(x) < kTooLarge ? magnitude(x) : 0u; }
+
+// The code of x >= 0 in the top byte; f: 2^(top - 127 - E); `random`: 16 bits, 8 places up, and a
+// half below them. (The product is truncated, so that a small code rounds up for
+// the right random numbers exactly.)
+__device__ __forceinline__ uint32_t encode(float x, float f, uint32_t random) {
+  return __float_as_uint(__fmul_rz(x, f)) * 16u + random;
 }
-// f: 2^(top - 1 - E).
-template <bool SIGNED>
-__device__ __forceinline__ uint32_t encode(float x, float f, uint32_t random16) {
-  // (truncated, so that a small code rounds up for the right random numbers exactly)
-  const float z = __fmul_rz(fabsf(x) * f, power(-126));
-  uint32_t code = (__float_as_uint(z) + (random16 << 4) + 8u) >> 20;
-  if (!SIGNED && x > 0.0f && code == 0u) code = 1u;
-  if (!(fabsf(x) < 0x1p127f)) code = SIGNED ? 127u : 255u;
-  return SIGNED ? code | (__float_as_uint(x) >> 31 << 7) : code;
+// Largest E for which f is a normal number; blocks beyond are scaled down first.
+constexpr int kPlainM = kTopM - 1, kPlainV = kTopV - 1;
+
+// Codes and exponents of a block's states, a lane four entries at..at + 3 gap (those
+// below hi).
+__device__ __forceinline__ void encode(float (&m)[4], float (&v)[4], uint32_t at, uint32_t gap, uint32_t hi,
+                                       uint32_t key, uint32_t& mc, uint32_t& vc, int& em, int& ev) {
+  uint32_t top_m = 0u, top_v = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (gap == 1u || at + gap * j < hi) {
+      top_m = max(top_m, magnitude(m[j]));
+      top_v = max(top_v, __float_as_uint(v[j]));  // (never negative)
+    }
+  }
+  top_m = __reduce_max_sync(0xffffffffu, top_m);
+  top_v = __reduce_max_sync(0xffffffffu, top_v);
+  const bool too_large = max(top_m, top_v) >= kTooLarge;  // of the whole block
+  if (too_large) {
+    top_m = top_v = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (gap == 1u || at + gap * j < hi) {
+        top_m = max(top_m, held_bits(m[j]));
+        top_v = max(top_v, held_bits(v[j]));
+      }
+    }
+    top_m = __reduce_max_sync(0xffffffffu, top_m);
+    top_v = __reduce_max_sync(0xffffffffu, top_v);
+  }
+  em = max(static_cast<int>(top_m >> 23) - 127, kLeast);
+  ev = max(static_cast<int>(top_v >> 23) - 127, kLeast);
+  float down_m = 1.0f, down_v = 1.0f;
+  int dm = em, dv = ev;
+  if (em > kPlainM) down_m = power(-114), dm -= 114;
+  if (ev > kPlainV) down_v = power(-98), dv -= 98;
+  const float fm = power(kTopM - 127 - dm), fv = power(kTopV - 127 - dv);
+  uint32_t ms[4], vs[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t r = mix32(at + gap * j + key);
+    float x = fabsf(m[j]), y = v[j];
+    if (em > kPlainM) x *= down_m;
+    if (ev > kPlainV) y *= down_v;
+    ms[j] = (encode(x, fm, __byte_perm(r, 0x80u, 0x5104u)) & 0x7f000000u) | (__float_as_uint(m[j]) & 0x80000000u);
+    vs[j] = max(encode(y, fv, __byte_perm(r, 0x80u, 0x5324u)), v[j] > 0.0f ? 1u << 24 : 0u);
+    if (too_large) {
+      if (magnitude(m[j]) >= kTooLarge) ms[j] = 0x7f000000u | (__float_as_uint(m[j]) & 0x80000000u);
+      if (magnitude(v[j]) >= kTooLarge) vs[j] = 0xff000000u;
+    }
+  }
+  mc = __byte_perm(__byte_perm(ms[0], ms[1], 0x0073u), __byte_perm(ms[2], ms[3], 0x0073u), 0x5410u);
+  vc = __byte_perm(__byte_perm(vs[0], vs[1], 0x0073u), __byte_perm(vs[2], vs[3], 0x0073u), 0x5410u);
 }
 
 template <typename A>
@@ -160,12 +231,11 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
       gs.load(g + at);
       ms.load_own(m + at);
       vs.load_own(v + at);
-      float po[4], mo[4], vo[4];
+      float po[4], go[4], mo[4], vo[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        po[j] = ps.get(j), mo[j] = ms.get(j), vo[j] = vs.get(j);
-        update(h, po[j], gs.get(j) * h.scale, mo[j], vo[j]);
-      }
+      for (int j = 0; j < 4; ++j) po[j] = ps.get(j), go[j] = gs.get(j), mo[j] = ms.get(j), vo[j] = vs.get(j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) update(h, po[j], go[j], mo[j], vo[j]);
       ps.round(po);
       ms.round(mo);
       vs.round(vo);
@@ -183,7 +253,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
 #pragma unroll 4
   for (uint32_t at = i + threadIdx.x; at < hi; at += kAdamThreads) {
     float po = p[at], mo = m[at], vo = v[at];
-    update(h, po, widen(g[at]) * h.scale, mo, vo);
+    update(h, po, widen(g[at]), mo, vo);
     p[at] = po;
     m[at] = mo;
     v[at] = vo;
@@ -191,10 +261,17 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   }
 }
 
-// A warp takes a block of 128 entries at a time, four a lane: consecutive where
-// the pointers allow vectors, else 32 apart.
+// A warp takes four blocks of 128 entries, eight apart, and a lane four entries of each:
+// consecutive where the pointers allow vectors, else 32 apart. Everything is
+// loaded before the first store. The piece's exponents are read by each warp at
+// once and written by the CTA at once: bytes of one sector, read and written one
+// by one from several SMs, took most of the time (25.6 M entries: 317 us).
+constexpr int kBlocksWarp = kPiece / kBlock / (kAdamThreads / 32);
+static_assert(kPiece / kBlock == 32, "a lane an exponent");
+
 template <typename G, int N>
 __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_constant__ AdamArgs<N> a) {
+  __shared__ uint8_t exponents[2][kPiece / kBlock];
   const uint32_t which = find_entry(a, blockIdx.x);
   const Entry& e = a.entry[which];
   const uint32_t lo = (blockIdx.x - e.first) * kPiece, hi = min(lo + kPiece, e.t.numel);
@@ -202,67 +279,63 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
   float* p = e.t.p;
   const G* g = static_cast<const G*>(e.t.g);
   uint8_t *m = static_cast<uint8_t*>(e.t.m), *v = static_cast<uint8_t*>(e.t.v);
-  uint32_t step;
-  const Hyper h = hyper_of(a, step);
-  const uint32_t key = mix32(mix32(a.seed + step) + 0x9E3779B9u * (a.first_tensor + which));
-#pragma unroll 2
-  for (uint32_t b = lo / kBlock + warp; b * kBlock < hi; b += kAdamThreads / 32) {
-    const uint32_t base = b * kBlock;
-    const bool wide = e.wide && base + kBlock <= hi;
-    const uint32_t at = wide ? base + lane * 4 : base + lane, gap = wide ? 1u : 32u;
-    float po[4], go[4], mo[4], vo[4];
-    uint32_t mc = 0u, vc = 0u;
-    if (wide) {
+  const uint32_t first = lo / kBlock, blocks = (hi - lo + kBlock - 1) / kBlock;
+  const uint32_t my_em = lane < blocks ? e.t.me[first + lane] : 0u;
+  const uint32_t my_ev = lane < blocks ? e.t.ve[first + lane] : 0u;
+  float po[kBlocksWarp][4], go[kBlocksWarp][4];
+  uint32_t mc[kBlocksWarp], vc[kBlocksWarp];
+#pragma unroll
+  for (int q = 0; q < kBlocksWarp; ++q) {
+    const uint32_t base = lo + (q * (kAdamThreads / 32) + warp) * kBlock;
+    mc[q] = vc[q] = 0u;
+    if (e.wide && base + kBlock <= hi) {
+      const uint32_t at = base + lane * 4;
       Vec<float, 4> ps;
       Vec<G, 4> gs;
       ps.load_own(p + at);
       gs.load(g + at);
-      mc = *reinterpret_cast<const uint32_t*>(m + at);
-      vc = *reinterpret_cast<const uint32_t*>(v + at);
+      mc[q] = *reinterpret_cast<const uint32_t*>(m + at);
+      vc[q] = *reinterpret_cast<const uint32_t*>(v + at);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) po[j] = ps.get(j), go[j] = gs.get(j);
+      for (int j = 0; j < 4; ++j) po[q][j] = ps.get(j), go[q][j] = gs.get(j);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t i = at + 32u * j;
+        const uint32_t i = base + lane + 32u * j;
         const bool in = i < hi;
-        po[j] = in ? p[i] : 0.0f;
-        go[j] = in ? widen(g[i]) : 0.0f;
-        mc |= (in ? m[i] : 0u) << (8 * j);
-        vc |= (in ? v[i] : 0u) << (8 * j);
+        po[q][j] = in ? p[i] : 0.0f;
+        go[q][j] = in ? widen(g[i]) : 0.0f;
+        mc[q] |= (in ? m[i] : 0u) << (8 * j);
+        vc[q] |= (in ? v[i] : 0u) << (8 * j);
       }
     }
-    const float fm = decode_factor(e.t.me[b], kTopM), fv = decode_factor(e.t.ve[b], kTopV);
-    uint32_t top_m = 0u, top_v = 0u;
+  }
+  uint32_t step;
+  const Hyper h = hyper_of(a, step);
+  const uint32_t key = mix32(mix32(a.seed + step) + 0x9E3779B9u * (a.first_tensor + which));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      mo[j] = decode<true>((mc >> (8 * j)) & 255u, fm);
-      vo[j] = decode<false>((vc >> (8 * j)) & 255u, fv);
-      update(h, po[j], go[j] * h.scale, mo[j], vo[j]);
-      if (wide || at + 32u * j < hi) {
-        top_m = max(top_m, held_bits(mo[j]));
-        top_v = max(top_v, held_bits(vo[j]));
-      }
-    }
-    const int em = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top_m) >> 23) - 127, kLeast);
-    const int ev = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top_v) >> 23) - 127, kLeast);
-    const float dm = power(kTopM - 1 - em), dv = power(kTopV - 1 - ev);
-    mc = vc = 0u;
+  for (int q = 0; q < kBlocksWarp; ++q) {
+    const uint32_t block = q * (kAdamThreads / 32) + warp, base = lo + block * kBlock;
+    int em = exponent_of(__shfl_sync(0xffffffffu, my_em, block));
+    int ev = exponent_of(__shfl_sync(0xffffffffu, my_ev, block));
+    if (base >= hi) break;
+    const bool wide = e.wide && base + kBlock <= hi;
+    const uint32_t at = wide ? base + lane * 4 : base + lane, gap = wide ? 1u : 32u;
+    float mo[4], vo[4];
+    decode(mc[q], vc[q], em, ev, mo, vo);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t r = mix32(at + gap * j + key);
-      mc |= encode<true>(mo[j], dm, r & 0xffffu) << (8 * j);
-      vc |= encode<false>(vo[j], dv, r >> 16) << (8 * j);
-    }
+    for (int j = 0; j < 4; ++j) update(h, po[q][j], go[q][j], mo[j], vo[j]);
+    uint32_t mn, vn;
+    encode(mo, vo, at, gap, hi, key, mn, vn, em, ev);
     if (wide) {
       Vec<float, 4> ps;
-      ps.round(po);
+      ps.round(po[q]);
       ps.store(p + at);
-      *reinterpret_cast<uint32_t*>(m + at) = mc;
-      *reinterpret_cast<uint32_t*>(v + at) = vc;
+      *reinterpret_cast<uint32_t*>(m + at) = mn;
+      *reinterpret_cast<uint32_t*>(v + at) = vn;
       if (e.t.copy) {
         Vec<bf16_t, 4> c;
-        c.round(po);
+        c.round(po[q]);
         c.store(e.t.copy + at);
       }
     } else {
@@ -270,17 +343,23 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
       for (int j = 0; j < 4; ++j) {
         const uint32_t i = at + 32u * j;
         if (i < hi) {
-          p[i] = po[j];
-          m[i] = static_cast<uint8_t>(mc >> (8 * j));
-          v[i] = static_cast<uint8_t>(vc >> (8 * j));
-          if (e.t.copy) e.t.copy[i] = round_bf16(po[j]);
+          p[i] = po[q][j];
+          m[i] = static_cast<uint8_t>(mn >> (8 * j));
+          v[i] = static_cast<uint8_t>(vn >> (8 * j));
+          if (e.t.copy) e.t.copy[i] = round_bf16(po[q][j]);
         }
       }
     }
     if (lane == 0) {
-      e.t.me[b] = static_cast<uint8_t>(em + 127);
-      e.t.ve[b] = static_cast<uint8_t>(ev + 127);
+      exponents[0][block] = static_cast<uint8_t>(em + 127);
+      exponents[1][block] = static_cast<uint8_t>(ev + 127);
     }
+  }
+  // (each warp has read the old ones before it stored its own)
+  __syncthreads();
+  if (warp == 0 && lane < blocks) {
+    e.t.me[first + lane] = exponents[0][lane];
+    e.t.ve[first + lane] = exponents[1][lane];
   }
 }
 
@@ -301,18 +380,12 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_states_kernel(const __grid
   T *m = static_cast<T*>(e.t.m_out), *v = static_cast<T*>(e.t.v_out);
   uint32_t i = lo;
   if (e.wide) {
-#pragma unroll 2
+#pragma unroll 4
     for (uint32_t at = lo + threadIdx.x * 4; at + 4 <= hi; at += kAdamThreads * 4) {
       const uint32_t mc = __ldg(reinterpret_cast<const uint32_t*>(e.t.m + at));
       const uint32_t vc = __ldg(reinterpret_cast<const uint32_t*>(e.t.v + at));
-      const float fm = decode_factor(__ldg(e.t.me + at / kBlock), kTopM);
-      const float fv = decode_factor(__ldg(e.t.ve + at / kBlock), kTopV);
       float mo[4], vo[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        mo[j] = decode<true>((mc >> (8 * j)) & 255u, fm);
-        vo[j] = decode<false>((vc >> (8 * j)) & 255u, fv);
-      }
+      decode(mc, vc, exponent_of(__ldg(e.t.me + at / kBlock)), exponent_of(__ldg(e.t.ve + at / kBlock)), mo, vo);
       Vec<T, 4> ms, vs;
       ms.round(mo);
       vs.round(vo);
@@ -321,10 +394,13 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_states_kernel(const __grid
     }
     i = hi & ~3u;
   }
-#pragma unroll 4
+#pragma unroll 2
   for (uint32_t at = i + threadIdx.x; at < hi; at += kAdamThreads) {
-    store_rounded(m + at, decode<true>(__ldg(e.t.m + at), decode_factor(__ldg(e.t.me + at / kBlock), kTopM)));
-    store_rounded(v + at, decode<false>(__ldg(e.t.v + at), decode_factor(__ldg(e.t.ve + at / kBlock), kTopV)));
+    float mo[4], vo[4];
+    decode(__ldg(e.t.m + at), __ldg(e.t.v + at), exponent_of(__ldg(e.t.me + at / kBlock)),
+           exponent_of(__ldg(e.t.ve + at / kBlock)), mo, vo);
+    store_rounded(m + at, mo[0]);
+    store_rounded(v + at, vo[0]);
   }
 }
 

@@ -25,9 +25,10 @@ constexpr int kRing = !WARP ? 4 : E == 8 ? 8 : E == 16 ? 4 : 3;
 
 template <typename X, typename Y, int V, int K, bool WARP>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) norm_kernel(const NormCall a) {
-  constexpr int S = kRing<V * K, WARP>;
+  constexpr int S = kRing<V * K, WARP>, W = V > 1 ? 2 : 1;
+  using L = Lane<W>;
   extern __shared__ __align__(16) char ring[];
-  __shared__ float room[2][32];
+  __shared__ __align__(16) float room[2][32];
   const uint32_t group = WARP ? 32u : blockDim.x;
   const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x;
   const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
@@ -41,16 +42,20 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) no
   };
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
-  float w[K][V], b[K][V];
+  L w[K][V / W], b[K][V / W];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t c = (k * group + t) * V;
     if (c < a.d) {
-      load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
-      load_weights<V>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
+      load_weights<V, W>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+      load_weights<V, W>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
     }
   }
   const float inv = 1.0f / static_cast<float>(a.d);
+  if (!WARP) {
+    clear_room(room[0], 64);
+    __syncthreads();
+  }
   uint32_t slot = 0;
   for (uint32_t row = first; row < a.n; row += groups) {
     fetch_wait<S - 2>();
@@ -60,40 +65,44 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) no
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const char* in_row = rows + slot * place + row_lead(x_row(row));
     slot = slot == S - 1 ? 0 : slot + 1;
-    Vec<X, V> in[K];
-    float sum = 0.0f;
+    L x[K][V / W], sums = L::all(0.0f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        in[k] = staged<X, V>(in_row, c);
+        const Vec<X, V> in = staged<X, V>(in_row, c);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum += in[k].get(j);
+        for (int j = 0; j < V / W; ++j) {
+          x[k][j] = in.template lane<W>(j);
+          sums = sums + x[k][j];
+        }
       }
     }
-    const float mean = (WARP ? warp_sum(sum) : cta_sum(sum, room[0])) * inv;
-    sum = 0.0f;
+    const float mean = (WARP ? warp_sum(sums.sum()) : cta_sum(sums.sum(), room[0])) * inv;
+    const L minus = L::all(-mean);
+    sums = L::all(0.0f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if ((k * group + t) * V < a.d)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float off = in[k].get(j) - mean;
-          sum = fmaf(off, off, sum);
+        for (int j = 0; j < V / W; ++j) {
+          x[k][j] = x[k][j] + minus;
+          sums = fma(x[k][j], x[k][j], sums);
         }
     }
-    const float var = (WARP ? warp_sum(sum) : cta_sum(sum, room[1])) * inv;
-    const float rstd = 1.0f / sqrtf(var + a.eps);
+    const float var = (WARP ? warp_sum(sums.sum()) : cta_sum(sums.sum(), room[1])) * inv;
+    const float rstd = inverse_root(var + a.eps);
+    const L r = L::all(rstd);
     Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        float out[V];
+        L out[V / W];
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = fmaf((in[k].get(j) - mean) * rstd, w[k][j], b[k][j]);
+        for (int j = 0; j < V / W; ++j) out[j] = fma(x[k][j] * r, w[k][j], b[k][j]);
         Vec<Y, V> o;
-        o.round(out);
+        o.template round<W>(out);
         o.store(y + c);
       }
     }
@@ -107,7 +116,9 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) no
 // Rows of any length, a CTA each.
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
-  __shared__ float room[2][32];
+  __shared__ __align__(16) float room[2][32];
+  clear_room(room[0], 64);
+  __syncthreads();
   const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(blockIdx.x) * a.ldx;
   Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(blockIdx.x) * a.ldy;
   const float inv = 1.0f / static_cast<float>(a.d);
@@ -121,7 +132,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
     const float off = widen(__ldg(x + c)) - mean;
     sum = fmaf(off, off, sum);
   }
-  const float rstd = 1.0f / sqrtf(cta_sum(sum, room[1]) * inv + a.eps);
+  const float rstd = inverse_root(cta_sum(sum, room[1]) * inv + a.eps);
 #pragma unroll 4
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
     float w[1], b[1];

@@ -86,25 +86,59 @@ __device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide
   }
 }
 
-// Sums of `a` and `b` over the threads of a CTA, in a fixed order; `room`: 64
-// floats that no other sum uses before the next barrier.
+template <int V, int W>
+__device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide, uint32_t c,
+                                             float none, Lane<W> (&out)[V / W]) {
+  float f[V];
+  load_weights<V>(w, bf16, wide, c, none, f);
+#pragma unroll
+  for (int i = 0; i < V / W; ++i) out[i] = Lane<W>::of(f + i * W);
+}
+
+// The sum of `a` over the threads of a CTA, in a fixed order. `room`: 32 floats, zero from the
+// last warp's on, that no other sum uses before the next barrier but one.
+__device__ __forceinline__ float cta_sum(float a, float* room) {
+  a = warp_sum(a);
+  const uint32_t warps = (blockDim.x + 31) >> 5;
+  if ((threadIdx.x & 31u) == 0) room[threadIdx.x >> 5] = a;
+  __syncthreads();
+  a = 0.0f;
+  for (uint32_t i = 0; i < warps; i += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(room + i);
+    a += (x.x + x.y) + (x.z + x.w);
+  }
+  return a;
+}
+// Two of them; `room` as above, 64 floats.
 __device__ __forceinline__ float2 cta_sum2(float a, float b, float* room) {
   a = warp_sum(a);
   b = warp_sum(b);
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
-  if (lane == 0) room[warp] = a, room[32 + warp] = b;
+  const uint32_t warps = (blockDim.x + 31) >> 5;
+  if ((threadIdx.x & 31u) == 0) {
+    room[threadIdx.x >> 5] = a;
+    room[32 + (threadIdx.x >> 5)] = b;
+  }
   __syncthreads();
-  a = lane < warps ? room[lane] : 0.0f;
-  b = lane < warps ? room[32 + lane] : 0.0f;
-  return make_float2(warp_sum(a), warp_sum(b));
+  a = b = 0.0f;
+  for (uint32_t i = 0; i < warps; i += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(room + i);
+    const float4 y = *reinterpret_cast<const float4*>(room + 32 + i);
+    a += (x.x + x.y) + (x.z + x.w);
+    b += (y.x + y.y) + (y.z + y.w);
+  }
+  return make_float2(a, b);
 }
-__device__ __forceinline__ float cta_sum(float a, float* room) {
-  a = warp_sum(a);
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
-  if (lane == 0) room[warp] = a;
-  __syncthreads();
-  a = lane < warps ? room[lane] : 0.0f;
-  return warp_sum(a);
+// Zeros for a sum's room, seen by all after the CTA's next barrier.
+__device__ __forceinline__ void clear_room(float* room, uint32_t floats) {
+  if (threadIdx.x < floats) room[threadIdx.x] = 0.0f;
+}
+
+// (var + eps)^(-1/2): the approximate root and one Newton step. Infinity for 0, as the
+// exact one is (the step would make it NaN).
+__device__ __forceinline__ float inverse_root(float x) {
+  const float y = rsqrtf(x);
+  const float z = y * fmaf(-0.5f * x * y, y, 1.5f);
+  return x > 1e-35f && x < 1e35f ? z : y;
 }
 
 // The widest vectors that rows of a type allow: as many values as every pointer

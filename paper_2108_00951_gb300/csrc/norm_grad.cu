@@ -46,9 +46,10 @@ __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t shar
 template <typename X, typename Y, int V, int K, bool WARP>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
     norm_grad_kernel(const NormGradCall a) {
-  constexpr int S = kRing<V * K, WARP>;
+  constexpr int S = kRing<V * K, WARP>, W = V > 1 ? 2 : 1;
+  using L = Lane<W>;
   extern __shared__ __align__(16) char ring[];
-  __shared__ float room[64];
+  __shared__ __align__(16) float room[64];
   const uint32_t group = WARP ? 32u : blockDim.x;
   const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x, warp = threadIdx.x >> 5;
   const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
@@ -68,13 +69,19 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
   float mean = 0.0f, rstd = 0.0f;
   if (first < a.n) mean = __ldg(a.mean + first), rstd = __ldg(a.rstd + first);
-  float w[K][V], dw[K][V] = {}, db[K][V] = {};
+  L w[K][V / W], dw[K][V / W], db[K][V / W];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t c = (k * group + t) * V;
-    if (c < a.d) load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+    if (c < a.d) load_weights<V, W>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+#pragma unroll
+    for (int j = 0; j < V / W; ++j) dw[k][j] = db[k][j] = L::all(0.0f);
   }
   const float inv = 1.0f / static_cast<float>(a.d);
+  if (!WARP) {
+    clear_room(room, 64);
+    __syncthreads();
+  }
   uint32_t slot = 0;
   for (uint32_t row = first; row < a.n; row += groups) {
     fetch_wait<S - 2>();
@@ -87,7 +94,11 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
     const char* xs = rows + slot * place + row_lead(x_row(row));
     const char* dys = rows + slot * place + x_place + row_lead(dy_row(row));
     slot = slot == S - 1 ? 0 : slot + 1;
-    float s1 = 0.0f, s2 = 0.0f;
+    // (a CTA's threads keep x' and q; a warp's, which have more columns, compute them again)
+    constexpr int kKept = WARP ? 1 : K;
+    L hat[kKept][V / W], q[kKept][V / W];
+    const L minus = L::all(-mu), scale = L::all(r);
+    L sum1 = L::all(0.0f), sum2 = L::all(0.0f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
@@ -95,41 +106,49 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
         const Vec<X, V> x = staged<X, V>(xs, c);
         const Vec<Y, V> dy = staged<Y, V>(dys, c);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float hat = (x.get(j) - mu) * r, g = dy.get(j), q = g * w[k][j];
-          s1 += q;
-          s2 = fmaf(q, hat, s2);
-          dw[k][j] = fmaf(g, hat, dw[k][j]);
-          db[k][j] += g;
+        for (int j = 0; j < V / W; ++j) {
+          const L h = (x.template lane<W>(j) + minus) * scale, g = dy.template lane<W>(j);
+          const L p = g * w[k][j];
+          sum1 = sum1 + p;
+          sum2 = fma(p, h, sum2);
+          dw[k][j] = fma(g, h, dw[k][j]);
+          db[k][j] = db[k][j] + g;
+          if (!WARP) hat[k % kKept][j] = h, q[k % kKept][j] = p;
         }
       }
     }
     if (!a.dx) continue;
+    float s1, s2;
     if (WARP) {
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
+      s1 = warp_sum(sum1.sum());
+      s2 = warp_sum(sum2.sum());
     } else {
-      const float2 s = cta_sum2(s1, s2, room);
+      const float2 s = cta_sum2(sum1.sum(), sum2.sum(), room);
       s1 = s.x;
       s2 = s.y;
     }
-    s1 *= inv;
-    s2 *= inv;
+    const L m1 = L::all(-s1 * inv), m2 = L::all(-s2 * inv);
     X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        const Vec<X, V> x = staged<X, V>(xs, c);
-        const Vec<Y, V> dy = staged<Y, V>(dys, c);
-        float out[V];
+        L out[V / W];
+        if (WARP) {
+          const Vec<X, V> x = staged<X, V>(xs, c);
+          const Vec<Y, V> dy = staged<Y, V>(dys, c);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float hat = (x.get(j) - mu) * r;
-          out[j] = r * (fmaf(dy.get(j), w[k][j], -s1) - hat * s2);
+          for (int j = 0; j < V / W; ++j) {
+            const L h = (x.template lane<W>(j) + minus) * scale;
+            out[j] = scale * fma(m2, h, fma(dy.template lane<W>(j), w[k][j], m1));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < V / W; ++j)
+            out[j] = scale * fma(m2, hat[k % kKept][j], q[k % kKept][j] + m1);
         }
         Vec<X, V> o;
-        o.round(out);
+        o.template round<W>(out);
         o.store(dx + c);
       }
     }
@@ -141,7 +160,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const uint32_t c = (k * group + t) * V + j;
-        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j], db[k][j]);
+        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j / W].get(j % W), db[k][j / W].get(j % W));
       }
     return;
   }
@@ -158,7 +177,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const uint32_t c = (k * 32 + t) * V + j;
-        if (c < a.d) shares[warp * a.d + c] = which ? db[k][j] : dw[k][j];
+        if (c < a.d) shares[warp * a.d + c] = (which ? db[k][j / W] : dw[k][j / W]).get(j % W);
       }
     __syncthreads();
 #pragma unroll
@@ -181,8 +200,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
 template <typename X, typename Y, bool SHARES>
 __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall a) {
   extern __shared__ float shares[];  // [2][d]
-  __shared__ float room[2][64];
+  __shared__ __align__(16) float room[2][64];
   const float inv = 1.0f / static_cast<float>(a.d);
+  clear_room(room[0], 128);
+  __syncthreads();
   if (SHARES)
     for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) shares[c] = shares[a.d + c] = 0.0f;
   uint32_t parity = 0;
