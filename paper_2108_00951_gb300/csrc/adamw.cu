@@ -92,25 +92,33 @@ __device__ __forceinline__ float decode_m(uint32_t word, int j, float f) {
 __device__ __forceinline__ float decode_v(uint32_t word, int j, float f) {
   return __uint_as_float(__byte_perm(word, 0u, 0x4044u | (j << 8)) << 4) * f;
 }
+// What few blocks hold (NaN, or E above top), out of the way of the others' registers.
+struct States {
+  float m[4], v[4];
+};
+__device__ __noinline__ States decode_rare(uint32_t mc, uint32_t vc, int em, int ev) {
+  States s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    s.m[j] = decode_m(mc, j, power(127 + min(em, kTopM) - kTopM)) * power(max(em - kTopM, 0));
+    s.v[j] = decode_v(vc, j, power(127 + min(ev, kTopV) - kTopV)) * power(max(ev - kTopV, 0));
+    if (((mc >> (8 * j)) & 127u) == 127u) s.m[j] = __int_as_float(0x7fffffff);
+    if (((vc >> (8 * j)) & 255u) == 255u) s.v[j] = __int_as_float(0x7fffffff);
+  }
+  return s;
+}
 __device__ __forceinline__ void decode(uint32_t mc, uint32_t vc, int em, int ev, float (&m)[4], float (&v)[4]) {
-  const float fm = power(127 + min(em, kTopM) - kTopM), fv = power(127 + min(ev, kTopV) - kTopV);
+  // a byte of m with seven ones, or one of v with eight
+  const uint32_t nan = (((mc & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) | ((~vc - 0x01010101u) & vc & 0x80808080u);
+  if (nan || em > kTopM || ev > kTopV) {
+    const States s = decode_rare(mc, vc, em, ev);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = s.m[j], v[j] = s.v[j];
+    return;
+  }
+  const float fm = power(127 + em - kTopM), fv = power(127 + ev - kTopV);
 #pragma unroll
   for (int j = 0; j < 4; ++j) m[j] = decode_m(mc, j, fm), v[j] = decode_v(vc, j, fv);
-  if (em > kTopM || ev > kTopV) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      m[j] *= power(max(em - kTopM, 0));
-      v[j] *= power(max(ev - kTopV, 0));
-    }
-  }
-  // the codes of NaN: a byte of m with seven ones, one of v with eight
-  if ((((mc & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) | ((~vc - 0x01010101u) & vc & 0x80808080u)) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (((mc >> (8 * j)) & 127u) == 127u) m[j] = __int_as_float(0x7fffffff);
-      if (((vc >> (8 * j)) & 255u) == 255u) v[j] = __int_as_float(0x7fffffff);
-    }
-  }
 }
 __device__ __forceinline__ int exponent_of(uint32_t e) { return max(static_cast<int>(e) - 127, kLeast); }
 
@@ -124,13 +132,54 @@ __device__ __forceinline__ uint32_t held_bits(float x) { return magnitude(x) < k
 __device__ __forceinline__ uint32_t encode(float x, float f, uint32_t random) {
   return __float_as_uint(__fmul_rz(x, f)) * 16u + random;
 }
-// Largest E for which f is a normal number; blocks beyond are scaled down first.
-constexpr int kPlainM = kTopM - 1, kPlainV = kTopV - 1;
+__device__ __forceinline__ uint32_t encode_m(float m, float scaled, float f, uint32_t r) {
+  return (encode(fabsf(scaled), f, __byte_perm(r, 0x80u, 0x5104u)) & 0x7f000000u) |
+         (__float_as_uint(m) & 0x80000000u);
+}
+__device__ __forceinline__ uint32_t encode_v(float scaled, float f, uint32_t r) {
+  return encode(scaled, f, __byte_perm(r, 0x80u, 0x5324u));
+}
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
+  return __byte_perm(__byte_perm(x[0], x[1], 0x0073u), __byte_perm(x[2], x[3], 0x0073u), 0x5410u);
+}
 
-// Codes and exponents of a block's states, a lane four entries at..at + 3 gap (those
-// below hi).
-__device__ __forceinline__ void encode(float (&m)[4], float (&v)[4], uint32_t at, uint32_t gap, uint32_t hi,
-                                       uint32_t key, uint32_t& mc, uint32_t& vc, int& em, int& ev) {
+// Codes and exponents of a block's states: a lane has four entries from `at` on, `gap`
+// apart, those below hi.
+struct Codes {
+  uint32_t m, v;
+  int em, ev;
+};
+// Any block: values too large to be held, and an E for which f is no normal number
+// (the block is scaled down first; its entries stay normal numbers, or are far too
+// small to be held).
+__device__ __noinline__ Codes encode_rare(States s, uint32_t at, uint32_t gap, uint32_t hi, uint32_t key) {
+  uint32_t top_m = 0u, top_v = 0u, ms[4], vs[4];
+  for (int j = 0; j < 4; ++j) {
+    if (gap == 1u || at + gap * j < hi) {
+      top_m = max(top_m, held_bits(s.m[j]));
+      top_v = max(top_v, held_bits(s.v[j]));
+    }
+  }
+  Codes c;
+  c.em = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top_m) >> 23) - 127, kLeast);
+  c.ev = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top_v) >> 23) - 127, kLeast);
+  const int down_m = c.em >= kTopM ? 114 : 0, down_v = c.ev >= kTopV ? 98 : 0;
+  const float fm = power(kTopM - 127 - (c.em - down_m)), fv = power(kTopV - 127 - (c.ev - down_v));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t r = mix32(at + gap * j + key);
+    ms[j] = encode_m(s.m[j], s.m[j] * power(-down_m), fm, r);
+    vs[j] = max(encode_v(s.v[j] * power(-down_v), fv, r), s.v[j] > 0.0f ? 1u << 24 : 0u);
+    if (magnitude(s.m[j]) >= kTooLarge) ms[j] = 0x7f000000u | (__float_as_uint(s.m[j]) & 0x80000000u);
+    if (magnitude(s.v[j]) >= kTooLarge) vs[j] = 0xff000000u;
+  }
+  c.m = top_bytes(ms);
+  c.v = top_bytes(vs);
+  return c;
+}
+__device__ __forceinline__ Codes encode(const float (&m)[4], const float (&v)[4], uint32_t at, uint32_t gap,
+                                        uint32_t hi, uint32_t key) {
   uint32_t top_m = 0u, top_v = 0u;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -141,42 +190,30 @@ __device__ __forceinline__ void encode(float (&m)[4], float (&v)[4], uint32_t at
   }
   top_m = __reduce_max_sync(0xffffffffu, top_m);
   top_v = __reduce_max_sync(0xffffffffu, top_v);
-  const bool too_large = max(top_m, top_v) >= kTooLarge;  // of the whole block
-  if (too_large) {
-    top_m = top_v = 0u;
+  if (top_m >= (127u + kTopM) << 23 || top_v >= (127u + kTopV) << 23) {  // of the whole block
+    States s;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (gap == 1u || at + gap * j < hi) {
-        top_m = max(top_m, held_bits(m[j]));
-        top_v = max(top_v, held_bits(v[j]));
-      }
-    }
-    top_m = __reduce_max_sync(0xffffffffu, top_m);
-    top_v = __reduce_max_sync(0xffffffffu, top_v);
+    for (int j = 0; j < 4; ++j) s.m[j] = m[j], s.v[j] = v[j];
+    return encode_rare(s, at, gap, hi, key);
   }
-  em = max(static_cast<int>(top_m >> 23) - 127, kLeast);
-  ev = max(static_cast<int>(top_v >> 23) - 127, kLeast);
-  float down_m = 1.0f, down_v = 1.0f;
-  int dm = em, dv = ev;
-  if (em > kPlainM) down_m = power(-114), dm -= 114;
-  if (ev > kPlainV) down_v = power(-98), dv -= 98;
-  const float fm = power(kTopM - 127 - dm), fv = power(kTopV - 127 - dv);
+  Codes c;
+  c.em = max(static_cast<int>(top_m >> 23) - 127, kLeast);
+  c.ev = max(static_cast<int>(top_v >> 23) - 127, kLeast);
+  const float fm = power(kTopM - 127 - c.em), fv = power(kTopV - 127 - c.ev);
   uint32_t ms[4], vs[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t r = mix32(at + gap * j + key);
-    float x = fabsf(m[j]), y = v[j];
-    if (em > kPlainM) x *= down_m;
-    if (ev > kPlainV) y *= down_v;
-    ms[j] = (encode(x, fm, __byte_perm(r, 0x80u, 0x5104u)) & 0x7f000000u) | (__float_as_uint(m[j]) & 0x80000000u);
-    vs[j] = max(encode(y, fv, __byte_perm(r, 0x80u, 0x5324u)), v[j] > 0.0f ? 1u << 24 : 0u);
-    if (too_large) {
-      if (magnitude(m[j]) >= kTooLarge) ms[j] = 0x7f000000u | (__float_as_uint(m[j]) & 0x80000000u);
-      if (magnitude(v[j]) >= kTooLarge) vs[j] = 0xff000000u;
-    }
+    ms[j] = encode_m(m[j], m[j], fm, r);
+    vs[j] = encode_v(v[j], fv, r);
   }
-  mc = __byte_perm(__byte_perm(ms[0], ms[1], 0x0073u), __byte_perm(ms[2], ms[3], 0x0073u), 0x5410u);
-  vc = __byte_perm(__byte_perm(vs[0], vs[1], 0x0073u), __byte_perm(vs[2], vs[3], 0x0073u), 0x5410u);
+  if (min(min(vs[0], vs[1]), min(vs[2], vs[3])) < 1u << 24) {  // a positive v is held as one
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vs[j] = max(vs[j], v[j] > 0.0f ? 1u << 24 : 0u);
+  }
+  c.m = top_bytes(ms);
+  c.v = top_bytes(vs);
+  return c;
 }
 
 template <typename A>
@@ -316,8 +353,8 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
 #pragma unroll
   for (int q = 0; q < kBlocksWarp; ++q) {
     const uint32_t block = q * (kAdamThreads / 32) + warp, base = lo + block * kBlock;
-    int em = exponent_of(__shfl_sync(0xffffffffu, my_em, block));
-    int ev = exponent_of(__shfl_sync(0xffffffffu, my_ev, block));
+    const int em = exponent_of(__shfl_sync(0xffffffffu, my_em, block));
+    const int ev = exponent_of(__shfl_sync(0xffffffffu, my_ev, block));
     if (base >= hi) break;
     const bool wide = e.wide && base + kBlock <= hi;
     const uint32_t at = wide ? base + lane * 4 : base + lane, gap = wide ? 1u : 32u;
@@ -325,18 +362,17 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
     decode(mc[q], vc[q], em, ev, mo, vo);
 #pragma unroll
     for (int j = 0; j < 4; ++j) update(h, po[q][j], go[q][j], mo[j], vo[j]);
-    uint32_t mn, vn;
-    encode(mo, vo, at, gap, hi, key, mn, vn, em, ev);
+    const Codes c = encode(mo, vo, at, gap, hi, key);
     if (wide) {
       Vec<float, 4> ps;
       ps.round(po[q]);
       ps.store(p + at);
-      *reinterpret_cast<uint32_t*>(m + at) = mn;
-      *reinterpret_cast<uint32_t*>(v + at) = vn;
+      *reinterpret_cast<uint32_t*>(m + at) = c.m;
+      *reinterpret_cast<uint32_t*>(v + at) = c.v;
       if (e.t.copy) {
-        Vec<bf16_t, 4> c;
-        c.round(po[q]);
-        c.store(e.t.copy + at);
+        Vec<bf16_t, 4> rounded;
+        rounded.round(po[q]);
+        rounded.store(e.t.copy + at);
       }
     } else {
 #pragma unroll
@@ -344,15 +380,15 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
         const uint32_t i = at + 32u * j;
         if (i < hi) {
           p[i] = po[q][j];
-          m[i] = static_cast<uint8_t>(mn >> (8 * j));
-          v[i] = static_cast<uint8_t>(vn >> (8 * j));
+          m[i] = static_cast<uint8_t>(c.m >> (8 * j));
+          v[i] = static_cast<uint8_t>(c.v >> (8 * j));
           if (e.t.copy) e.t.copy[i] = round_bf16(po[q][j]);
         }
       }
     }
     if (lane == 0) {
-      exponents[0][block] = static_cast<uint8_t>(em + 127);
-      exponents[1][block] = static_cast<uint8_t>(ev + 127);
+      exponents[0][block] = static_cast<uint8_t>(c.em + 127);
+      exponents[1][block] = static_cast<uint8_t>(c.ev + 127);
     }
   }
   // (each warp has read the old ones before it stored its own)
@@ -380,19 +416,31 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_states_kernel(const __grid
   T *m = static_cast<T*>(e.t.m_out), *v = static_cast<T*>(e.t.v_out);
   uint32_t i = lo;
   if (e.wide) {
-#pragma unroll 4
-    for (uint32_t at = lo + threadIdx.x * 4; at + 4 <= hi; at += kAdamThreads * 4) {
-      const uint32_t mc = __ldg(reinterpret_cast<const uint32_t*>(e.t.m + at));
-      const uint32_t vc = __ldg(reinterpret_cast<const uint32_t*>(e.t.v + at));
-      float mo[4], vo[4];
-      decode(mc, vc, exponent_of(__ldg(e.t.me + at / kBlock)), exponent_of(__ldg(e.t.ve + at / kBlock)), mo, vo);
-      Vec<T, 4> ms, vs;
-      ms.round(mo);
-      vs.round(vo);
-      ms.store(m + at);
-      vs.store(v + at);
+    // eight entries a thread at a time
+#pragma unroll
+    for (uint32_t q = 0; q < kPiece / (8 * kAdamThreads); ++q) {
+      const uint32_t at = lo + (q * kAdamThreads + threadIdx.x) * 8;
+      if (at + 8 > hi) break;
+      const uint2 mc = __ldg(reinterpret_cast<const uint2*>(e.t.m + at));
+      const uint2 vc = __ldg(reinterpret_cast<const uint2*>(e.t.v + at));
+      const int em = exponent_of(__ldg(e.t.me + at / kBlock)), ev = exponent_of(__ldg(e.t.ve + at / kBlock));
+      float mo[2][4], vo[2][4];
+      decode(mc.x, vc.x, em, ev, mo[0], vo[0]);
+      decode(mc.y, vc.y, em, ev, mo[1], vo[1]);
+      constexpr int kVec = 16 / sizeof(T);  // values of 16 bytes
+#pragma unroll
+      for (int j = 0; j < 8; j += kVec) {
+        float f[kVec], h[kVec];
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) f[k] = mo[(j + k) / 4][(j + k) % 4], h[k] = vo[(j + k) / 4][(j + k) % 4];
+        Vec<T, kVec> ms, vs;
+        ms.round(f);
+        vs.round(h);
+        ms.store(m + at + j);
+        vs.store(v + at + j);
+      }
     }
-    i = hi & ~3u;
+    i = hi & ~7u;
   }
 #pragma unroll 2
   for (uint32_t at = i + threadIdx.x; at < hi; at += kAdamThreads) {
@@ -472,7 +520,7 @@ template <typename T, int N>
 cudaError_t states_in(const AdamStates* t, uint32_t n, cudaStream_t stream) {
   StatesArgs<N> a;
   auto wide = [&](const AdamStates& x) -> uint32_t {
-    return on(x.m, 4) && on(x.v, 4) && on(x.m_out, sizeof(T) * 4) && on(x.v_out, sizeof(T) * 4);
+    return on(x.m, 8) && on(x.v, 8) && on(x.m_out, 16) && on(x.v_out, 16);
   };
   for (uint32_t next = 0; next < n;) {
     const uint32_t ctas = fill(a, N, t, n, next, wide);
