@@ -30,7 +30,6 @@ constexpr uint32_t kSlice = 256;        // columns a warp takes: 8 a lane
 constexpr int kLane = 8;
 constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
 constexpr int kSortThreads = 512;
-constexpr uint32_t kSortTile = 2048;    // positions that a sorting CTA ranks at a time
 constexpr int kMaxBins = 512, kMaxPasses = 4;  // (31 bits: four digits of 8)
 constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
 
@@ -84,23 +83,31 @@ __device__ __forceinline__ void write_row(const EmbedGradCall& a, uint64_t row, 
   }
 }
 
-template <typename T, int V>
+// Zeros over a row, 16 bytes at a time between its first and last boundary.
+template <typename T>
 __device__ __forceinline__ void zero_row(const EmbedGradCall& a, uint64_t row, uint32_t lane) {
   T* to = static_cast<T*>(a.dtable) + row * a.ld_dtable;
-  Vec<T, V> o;
-  o.clear();
+  constexpr uint32_t kPer = 16 / sizeof(T);
+  const uint32_t lead = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(to) % 16 / sizeof(T));
+  const uint32_t head = min(lead ? kPer - lead : 0u, a.d), body = (a.d - head) / kPer * kPer;
+  if (lane < head) to[lane] = 0;
 #pragma unroll 4
-  for (uint32_t c = lane * V; c < a.d; c += 32 * V) o.store(to + c);
+  for (uint32_t c = head + lane * kPer; c < head + body; c += 32 * kPer)
+    *reinterpret_cast<uint4*>(to + c) = make_uint4(0u, 0u, 0u, 0u);
+  if (head + body + lane < a.d) to[head + body + lane] = 0;
 }
 
 // ------------------------------------------------------------- few tokens
 // CTA i < n: position i. The others: rows of the table, `rows` each.
 template <typename D, typename T, int V>
 __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const EmbedGradCall a, uint32_t rows, uint32_t* error) {
-  __shared__ uint32_t mask[kRowsCta / 32 > kFewTokens / 32 ? kRowsCta / 32 : kFewTokens / 32];
-  __shared__ float part[kThreadsFew / 32][kSlice];
-  const uint32_t t = threadIdx.x, lane = t & 31u, warp = t >> 5;
   constexpr uint32_t kWarps = kThreadsFew / 32;
+  constexpr int kAhead = V > 1 ? 8 : 4;  // rows on their way
+  __shared__ uint32_t mask[kRowsCta / 32 > kFewTokens / 32 ? kRowsCta / 32 : kFewTokens / 32];
+  __shared__ uint16_t list[kFewTokens];
+  __shared__ float part[kWarps][kSlice];
+  __shared__ uint32_t total;
+  const uint32_t t = threadIdx.x, lane = t & 31u, warp = t >> 5;
   if (blockIdx.x >= a.n) {  // zeros
     const uint64_t lo = static_cast<uint64_t>(blockIdx.x - a.n) * rows;
     const uint64_t hi = min(lo + rows, static_cast<uint64_t>(a.v));
@@ -113,77 +120,81 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
     }
     __syncthreads();
     for (uint64_t r = lo + warp; r < hi; r += kWarps)
-      if (!(mask[(r - lo) / 32] >> ((r - lo) & 31) & 1u)) zero_row<T, V>(a, r, lane);
+      if (!(mask[(r - lo) / 32] >> ((r - lo) & 31) & 1u)) zero_row<T>(a, r, lane);
     return;
   }
   const uint32_t i = blockIdx.x;
   const int64_t own = __ldg(reinterpret_cast<const long long*>(a.token) + i);
-  if (own >= static_cast<int64_t>(a.v) && t == 0) atomicOr(error, kDevErrBadInput);
-  if (own < 0 || own >= static_cast<int64_t>(a.v)) return;
+  const uint32_t words = (a.n + 31u) / 32u;
   bool before = false;
-  uint32_t count = 0;
-  for (uint32_t j = t; j < (a.n + 31u) / 32u * 32u; j += kThreadsFew) {
+  for (uint32_t j = t; j < words * 32u; j += kThreadsFew) {
     const bool same = j < a.n && __ldg(reinterpret_cast<const long long*>(a.token) + j) == own;
     before |= same && j < i;
     const uint32_t m = __ballot_sync(0xffffffffu, same);
     if (lane == 0) mask[j / 32] = m;
-    count += __popc(m);
   }
+  if (own >= static_cast<int64_t>(a.v) && t == 0) atomicOr(error, kDevErrBadInput);
+  if (own < 0 || own >= static_cast<int64_t>(a.v)) return;
   if (__syncthreads_or(before)) return;
-  // slices of columns over the warps; with fewer slices than warps, several warps
-  // share one, each taking every R-th occurrence
-  const uint32_t slices = (a.d + kSlice - 1) / kSlice;
-  uint32_t groups = 1;
-  while (groups * 2 * slices <= kWarps) groups *= 2;
-  const uint32_t group = warp % groups;
-  for (uint32_t s0 = 0; s0 < slices; s0 += kWarps / groups) {
-    const uint32_t slice = s0 + warp / groups;
-    float sum[kLane] = {};
-    if (slice < slices) {
-      uint32_t seen = 0;
-      RowPart<D, V> row[4];
-      uint32_t held = 0;
-      for (uint32_t word = i / 32; word < (a.n + 31u) / 32u; ++word) {
-        uint32_t m = mask[word];
-        while (m) {
-          const uint32_t at = word * 32 + __ffs(m) - 1;
-          m &= m - 1;
-          if (seen++ % groups != group) continue;
-          // (an index that is no constant would put the rows into local memory)
-          const D* from = static_cast<const D*>(a.dout) + static_cast<uint64_t>(at) * a.ld_dout;
-          if (held == 0) row[0].load(from, slice, lane, a.d);
-          else if (held == 1) row[1].load(from, slice, lane, a.d);
-          else if (held == 2) row[2].load(from, slice, lane, a.d);
-          else row[3].load(from, slice, lane, a.d);
-          if (++held == 4) {
+  if (warp == 0) {  // the positions, in order
+    uint32_t at = 0;
+    for (uint32_t base = 0; base < words; base += 32) {
+      uint32_t m = base + lane < words ? mask[base + lane] : 0u;
+      const uint32_t count = __popc(m);
+      uint32_t scan = count;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) row[q].add_to(sum);
-            held = 0;
-          }
-        }
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= static_cast<uint32_t>(o)) scan += x;
       }
-      if (held > 0) row[0].add_to(sum);
-      if (held > 1) row[1].add_to(sum);
-      if (held > 2) row[2].add_to(sum);
+      for (uint32_t k = at + scan - count; m; m &= m - 1)
+        list[k++] = static_cast<uint16_t>((base + lane) * 32 + __ffs(m) - 1);
+      at += __shfl_sync(0xffffffffu, scan, 31);
     }
-    if (groups > 1) {
+    if (lane == 0) total = at;
+  }
+  __syncthreads();
+  // slices of columns over the warps; with fewer slices than warps, groups of warps
+  // have all slices, each taking every groups-th occurrence
+  const uint32_t slices = (a.d + kSlice - 1) / kSlice;
+  const uint32_t groups = slices < kWarps ? min(kWarps / slices, total) : 1u;
+  const uint32_t group = slices < kWarps ? warp / slices : 0u;
+  for (uint32_t s0 = 0; s0 < slices; s0 += kWarps) {
+    const uint32_t slice = slices < kWarps ? warp % slices : s0 + warp;
+    const bool work = group < groups && slice < slices;
+    float sum[kLane] = {};
+    if (work) {
+      for (uint32_t k = group; k < total; k += groups * kAhead) {
+        RowPart<D, V> row[kAhead];
 #pragma unroll
-      for (int j = 0; j < kLane; ++j) part[warp][j * 32 + lane] = sum[j];
+        for (int q = 0; q < kAhead; ++q)
+          if (k + q * groups < total)
+            row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(list[k + q * groups]) * a.ld_dout,
+                        slice, lane, a.d);
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+          if (k + q * groups < total) row[q].add_to(sum);
+      }
+    }
+    if (groups > 1) {  // (then all slices are had at once)
+      if (work && group > 0) {
+#pragma unroll
+        for (int j = 0; j < kLane; ++j) part[warp][j * 32 + lane] = sum[j];
+      }
       __syncthreads();
-      if (group == 0) {
+      if (work && group == 0) {
         for (uint32_t g = 1; g < groups; ++g)
 #pragma unroll
-          for (int j = 0; j < kLane; ++j) sum[j] += part[warp + g][j * 32 + lane];
+          for (int j = 0; j < kLane; ++j) sum[j] += part[g * slices + warp][j * 32 + lane];
       }
-      __syncthreads();
     }
-    if (group == 0 && slice < slices) write_row<T, V>(a, static_cast<uint64_t>(own), slice, lane, sum);
+    if (work && group == 0) write_row<T, V>(a, static_cast<uint64_t>(own), slice, lane, sum);
   }
 }
 
 // ------------------------------------------------------------------ sorting
 struct Sort {
-  uint32_t n, v, bits, passes, parts, per;  // per: positions a part takes
+  uint32_t n, v, bits, passes, parts, per;  // per: positions a part takes (tiles of 512 R)
   uint32_t* hist[kMaxPasses];  // [parts][bins] of each digit
   uint32_t *key[2], *pos[2];
   uint32_t* error;
@@ -221,10 +232,12 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s)
 // One digit. Positions keep their order: a warp takes consecutive ones, and a
 // position's rank is the number of equal digits before it in its warp, in the
 // warps before, in the tiles before and in the parts before.
+template <int kPer>
 __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort s, uint32_t pass) {
-  constexpr int kWarps = kSortThreads / 32, kPer = kSortTile / kSortThreads;
+  constexpr int kWarps = kSortThreads / 32;
+  constexpr uint32_t kSortTile = kSortThreads * kPer;
   __shared__ uint32_t base[kMaxBins];           // where the part's next position of a digit goes
-  __shared__ uint16_t count[kWarps][kMaxBins];
+  __shared__ __align__(16) uint16_t count[kWarps][kMaxBins];
   __shared__ uint32_t sums[kWarps];
   griddep_wait();
   const uint32_t bins = 1u << s.bits, t = threadIdx.x, lane = t & 31u, warp = t >> 5;
@@ -237,11 +250,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
   {  // a thread a digit: the parts before, then all parts; and the digits before
     uint32_t before = 0, all = 0;
     if (t < bins) {
-#pragma unroll 8
-      for (uint32_t p = 0; p < s.parts; ++p) {
-        const uint32_t c = hist[p * bins + t];
-        before += p < blockIdx.x ? c : 0u;
-        all += c;
+      constexpr int kAhead = 32;  // (a load takes half a microsecond: few rounds of many)
+      for (uint32_t p0 = 0; p0 < s.parts; p0 += kAhead) {
+        uint32_t c[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) c[q] = p0 + q < s.parts ? __ldcg(hist + (p0 + q) * bins + t) : 0u;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          before += p0 + q < blockIdx.x ? c[q] : 0u;
+          all += c[q];
+        }
       }
     }
     uint32_t scan = all;
@@ -258,7 +276,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
   }
   const uint32_t lo = blockIdx.x * s.per, hi = min(lo + s.per, s.n);
   for (uint32_t tile = lo; tile < hi; tile += kSortTile) {
-    for (uint32_t i = t; i < kWarps * bins; i += kSortThreads) count[i >> s.bits][i & (bins - 1u)] = 0;
+    for (uint32_t i = t; i < kWarps * kMaxBins / 8; i += kSortThreads)
+      reinterpret_cast<uint4*>(&count[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
     uint32_t key[kPer], rank[kPer], digit[kPer], pos[kPer];
     const uint32_t at = tile + warp * (32 * kPer) + lane;
 #pragma unroll
@@ -339,12 +358,13 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, c
       }
       uint32_t m = __ballot_sync(0xffffffffu, absent);
       while (m) {
-        zero_row<T, V>(a, r + __ffs(m) - 1, lane);
+        zero_row<T>(a, r + __ffs(m) - 1, lane);
         m &= m - 1;
       }
     }
     return;
   }
+  constexpr int kAhead = V > 2 ? 8 : 4;  // rows on their way
   const uint32_t item = blockIdx.x * 8 + warp;
   if (item >= s.warps) return;
   const uint32_t slice = item % s.slices, piece = item / s.slices;
@@ -375,17 +395,17 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, c
     const uint32_t count = min(32u, hi - base);
     const uint32_t my_key = lane < count ? __ldg(s.key + base + lane) : 0u;
     const uint32_t my_pos = lane < count ? __ldg(s.pos + base + lane) : 0u;
-    for (uint32_t e = 0; e < count; e += 4) {
-      RowPart<D, V> row[4];
+    for (uint32_t e = 0; e < count; e += kAhead) {
+      RowPart<D, V> row[kAhead];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < kAhead; ++q) {
         const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
         const uint32_t pos = __shfl_sync(0xffffffffu, my_pos, (e + q) & 31u);
         if (e + q < count && key < a.v)
           row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(pos) * a.ld_dout, slice, lane, a.d);
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < kAhead; ++q) {
         const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
         if (e + q < count) {
           if (key != token) {
@@ -418,10 +438,18 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const EmbedGradCall a, 
     const uint32_t lo = piece * s.piece, hi = lo + s.piece;
     token = __ldg(s.key + hi - 1);
     const bool begins = lo == 0 || __ldg(s.key + lo - 1) != token;
-    if (token < a.v && begins && __ldg(s.key + hi) == token) {
-      end = piece + 1;
-      if (end + 1 < s.pieces && __ldg(s.key + min(hi + s.piece, a.n - 1)) == token)
-        end = (hi + first_of(s.key + hi, a.n - hi, token + 1) - 1) / s.piece;
+    if (token < a.v && begins) {  // (the same in all lanes) the pieces after this that begin with it
+      end = piece;
+      while (true) {
+        const uint32_t next = end + 1 + lane;
+        const uint32_t m = __ballot_sync(0xffffffffu, next < s.pieces && __ldg(s.key + next * s.piece) == token);
+        if (m != 0xffffffffu) {
+          end += __ffs(~m) - 1;
+          break;
+        }
+        end += 32;
+      }
+      if (end == piece) end = 0;
     }
   }
   auto add = [&](uint32_t share, float (&sum)[kLane]) {
@@ -471,7 +499,8 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const EmbedGradCall a, 
 // ------------------------------------------------------------------ planning
 struct Plan {
   bool few;
-  uint32_t v;  // values per vector
+  uint32_t v;       // values per vector
+  uint32_t rounds;  // positions that a sorting thread ranks at a time
   Sort sort;
   Sum sum;
   size_t hist, key, shares, bytes;  // sizes, in bytes
@@ -487,8 +516,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
     return c.d % v == 0 && rows(c.dout, c.n > 1 ? c.ld_dout : 0, dsize) &&
            rows(c.dtable, c.v > 1 ? c.ld_dtable : 0, tsize);
   };
-  const uint32_t wide = c.dout_bf16 && c.dtable_bf16 ? 8 : 4;
-  p.v = allow(wide) ? wide : allow(2) ? 2 : 1;
+  p.v = allow(8) ? 8 : allow(4) ? 4 : allow(2) ? 2 : 1;
   p.few = c.n <= kFewTokens;
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
   p.sum.rows = std::max(8u, std::min((c.v + 4 * sms - 1) / (4 * sms), kRowsCta));
@@ -500,10 +528,12 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   s.bits = (bits + s.passes - 1) / s.passes;
   s.n = c.n;
   s.v = c.v;
-  s.per = ((c.n + kMaxParts - 1) / kMaxParts + kSortTile - 1) / kSortTile * kSortTile;
+  p.rounds = c.n <= 32768 ? 1 : 4;
+  const uint32_t tile = kSortThreads * p.rounds;
+  s.per = ((c.n + kMaxParts - 1) / kMaxParts + tile - 1) / tile * tile;
   s.parts = (c.n + s.per - 1) / s.per;
   Sum& m = p.sum;
-  m.piece = c.n < 65536 ? 32 : 128;
+  m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : 128;
   m.pieces = (c.n + m.piece - 1) / m.piece;
   m.slices = (c.d + kSlice - 1) / kSlice;
   m.warps = m.pieces * m.slices;
@@ -538,8 +568,8 @@ cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
 
 template <typename D, typename T>
 cudaError_t launch_typed(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
-  constexpr uint32_t kWide = sizeof(D) == 2 && sizeof(T) == 2 ? 8 : 4;
-  if (p.v == kWide) return launch<D, T, kWide>(c, p, stream);
+  if (p.v == 8) return launch<D, T, 8>(c, p, stream);
+  if (p.v == 4) return launch<D, T, 4>(c, p, stream);
   return p.v == 2 ? launch<D, T, 2>(c, p, stream) : launch<D, T, 1>(c, p, stream);
 }
 
@@ -573,8 +603,9 @@ cudaError_t launch_embed_grad(const EmbedGradCall& c, Workspace& ws, const Devic
     for (uint32_t pass = 0; pass < s.passes; ++pass) {
       count_launch();
       void* params[] = {&s, &pass};
-      err = launch_pdl(reinterpret_cast<const void*>(embed_scatter_kernel), dim3(s.parts), kSortThreads,
-                       0, ws.stream, params, false);
+      err = launch_pdl(p.rounds == 1 ? reinterpret_cast<const void*>(embed_scatter_kernel<1>)
+                                     : reinterpret_cast<const void*>(embed_scatter_kernel<4>),
+                       dim3(s.parts), kSortThreads, 0, ws.stream, params, false);
       if (err != cudaSuccess) return err;
     }
   }

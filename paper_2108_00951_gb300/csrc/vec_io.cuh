@@ -74,12 +74,13 @@ __device__ __forceinline__ Lane<2> fma(Lane<2> a, Lane<2> b, Lane<2> c) {
 }
 
 // V values of T as they lie in memory, at an address that is a multiple of
-// their size (2, 4, 8 or 16 bytes).
+// their size (2 to 32 bytes).
 template <typename T, int V>
 struct Vec {
   static constexpr int kBytes = static_cast<int>(sizeof(T)) * V;
   static constexpr int kWords = kBytes < 4 ? 1 : kBytes / 4;
-  static_assert(kBytes == 2 || kBytes == 4 || kBytes == 8 || kBytes == 16, "one load");
+  static_assert(kBytes == 2 || kBytes == 4 || kBytes == 8 || kBytes == 16 || kBytes == 32,
+                "one load");
   uint32_t w[kWords];
 
   __device__ __forceinline__ void clear() {
@@ -88,7 +89,11 @@ struct Vec {
   }
   // Of memory that nothing writes while the kernel runs.
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (kBytes == 16) {
+    if constexpr (kBytes == 32) {
+      asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                   : "l"(p));
+    } else if constexpr (kBytes == 16) {
       const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
       w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
     } else if constexpr (kBytes == 8) {
@@ -102,7 +107,12 @@ struct Vec {
   }
   // Of memory that the kernel writes too.
   __device__ __forceinline__ void load_own(const T* p) {
-    if constexpr (kBytes == 16) {
+    if constexpr (kBytes == 32) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                   : "l"(p)
+                   : "memory");
+    } else if constexpr (kBytes == 16) {
       const uint4 x = *reinterpret_cast<const uint4*>(p);
       w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
     } else if constexpr (kBytes == 8) {
@@ -115,7 +125,11 @@ struct Vec {
     }
   }
   __device__ __forceinline__ void store(T* p) const {
-    if constexpr (kBytes == 16) {
+    if constexpr (kBytes == 32) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+                   "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else if constexpr (kBytes == 16) {
       *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else if constexpr (kBytes == 8) {
       *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
