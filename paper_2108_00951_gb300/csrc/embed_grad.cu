@@ -9,13 +9,12 @@
 // tokens; if its own occurs before, another CTA has it, else it sums the rows of
 // all its occurrences. Further CTAs write the rows that do not occur.
 //
-// More: the positions are sorted by token (stable, least digit first: a histogram
-// of the first digit, then one launch per digit, in which each CTA finds where its
-// part of the positions goes from the counts of the parts before it and counts
-// the next digit where they arrive). Then a warp takes 256 columns of a piece of
-// the sorted positions, adds up rows and writes a row's sum when the token
-// changes. A token that goes on past its piece leaves a share, and a last launch
-// joins those in order.
+// More: the positions are sorted by token (stable, least digit first: for each digit
+// a launch that counts it by parts of the positions, and one in which each CTA
+// finds where its part goes from the counts of the parts before it). Then a warp
+// takes 256 columns of a piece of the sorted positions, adds up rows and writes a
+// row's sum when the token changes. A token that goes on past its piece leaves a
+// share; the warp that leaves a token's last one joins them, in their order.
 #include <algorithm>
 
 #include "internal.h"
@@ -30,7 +29,7 @@ constexpr uint32_t kSlice = 256;        // columns a warp takes: 8 a lane
 constexpr int kLane = 8;
 constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
 constexpr int kSortThreads = 512;
-constexpr int kMaxBins = 512, kMaxPasses = 4;  // (31 bits: four digits of 8)
+constexpr int kMaxBins = 512;
 constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
 
 // A lane's 8 columns of a slice: vectors of V, 32 V apart.
@@ -195,38 +194,51 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
 // ------------------------------------------------------------------ sorting
 struct Sort {
   uint32_t n, v, bits, passes, parts, per;  // per: positions a part takes (tiles of 512 R)
-  uint32_t* hist[kMaxPasses];  // [parts][bins] of each digit
+  uint32_t* hist;         // [parts][bins] of a digit
   uint32_t *key[2], *pos[2];
   uint32_t* error;
   const int64_t* token;
+  uint32_t *arrived, arrivals;  // of the shares: see Sum
 };
 
 __device__ __forceinline__ uint32_t digit_of(const Sort& s, uint32_t key, uint32_t pass) {
   return (key >> (pass * s.bits)) & ((1u << s.bits) - 1u);
 }
 
-// Counts of the first digit by part, and zeros for the counts of the others.
-__global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s) {
+// Counts of a digit by part. The first launch makes the keys of the tokens, too, and
+// zeros for the arrivals of shares.
+__global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s, uint32_t pass) {
   __shared__ uint32_t hist[kMaxBins];
   const uint32_t bins = 1u << s.bits, t = threadIdx.x;
   for (uint32_t b = t; b < bins; b += kSortThreads) hist[b] = 0u;
+  if (pass == 0)
+    for (uint32_t i = blockIdx.x * kSortThreads + t; i < s.arrivals; i += gridDim.x * kSortThreads) s.arrived[i] = 0u;
+  griddep_wait();
   __syncthreads();
   const uint32_t lo = blockIdx.x * s.per, hi = min(lo + s.per, s.n);
   bool bad = false;
 #pragma unroll 4
-  for (uint32_t i = lo + t; i < hi; i += kSortThreads) {
-    const int64_t w = __ldg(reinterpret_cast<const long long*>(s.token) + i);
-    bad |= w >= static_cast<int64_t>(s.v);
-    const uint32_t key = w < 0 || w >= static_cast<int64_t>(s.v) ? s.v : static_cast<uint32_t>(w);
-    s.key[0][i] = key;
-    atomicAdd(&hist[digit_of(s, key, 0)], 1u);
+  for (uint32_t i0 = lo; i0 < hi; i0 += kSortThreads) {
+    const uint32_t i = i0 + t;
+    uint32_t key = s.v;
+    if (i < hi) {
+      if (pass == 0) {
+        const int64_t w = __ldg(reinterpret_cast<const long long*>(s.token) + i);
+        bad |= w >= static_cast<int64_t>(s.v);
+        if (w >= 0 && w < static_cast<int64_t>(s.v)) key = static_cast<uint32_t>(w);
+        s.key[0][i] = key;
+      } else {
+        key = __ldcg(s.key[pass & 1u] + i);
+      }
+    }
+    // (frequent tokens: a warp's equal digits are one addition)
+    const uint32_t digit = i < hi ? digit_of(s, key, pass) : bins;
+    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    if (digit < bins && (same & lanemask_lt()) == 0u) atomicAdd(&hist[digit], static_cast<uint32_t>(__popc(same)));
   }
   if (bad) atomicOr(s.error, kDevErrBadInput);
   __syncthreads();
-  for (uint32_t b = t; b < bins; b += kSortThreads) {
-    s.hist[0][blockIdx.x * bins + b] = hist[b];
-    for (uint32_t p = 1; p < s.passes; ++p) s.hist[p][blockIdx.x * bins + b] = 0u;
-  }
+  for (uint32_t b = t; b < bins; b += kSortThreads) s.hist[blockIdx.x * bins + b] = hist[b];
 }
 
 // One digit. Positions keep their order: a warp takes consecutive ones, and a
@@ -241,9 +253,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
   __shared__ uint32_t sums[kWarps];
   griddep_wait();
   const uint32_t bins = 1u << s.bits, t = threadIdx.x, lane = t & 31u, warp = t >> 5;
-  const bool last = pass + 1u == s.passes;
-  const uint32_t* hist = s.hist[pass];
-  uint32_t* next = s.hist[last ? pass : pass + 1u];
+  const uint32_t* hist = s.hist;
   const uint32_t* keys = s.key[pass & 1u];
   const uint32_t* from = s.pos[pass & 1u];
   uint32_t *keys_out = s.key[(pass + 1u) & 1u], *to = s.pos[(pass + 1u) & 1u];
@@ -315,7 +325,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
         const uint32_t out = base[digit[k]] + count[warp][digit[k]] + rank[k];
         keys_out[out] = key[k];
         to[out] = pos[k];
-        if (!last) atomicAdd(&next[(out / s.per) * bins + digit_of(s, key[k], pass + 1u)], 1u);
       }
     }
     __syncthreads();
@@ -327,6 +336,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
 struct Sum {
   const uint32_t *key, *pos;
   float* shares;          // [pieces][2][d]: a token from the piece before, one that goes on
+  uint32_t* arrived;      // [pieces][slices]: shares of the token that begins and goes on there
   uint32_t piece, pieces, slices, warps;  // positions a piece; warps that sum
   uint32_t rows;          // rows a CTA of zeros takes
 };
@@ -340,6 +350,75 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t n, u
     else hi = mid;
   }
   return lo;
+}
+
+// A warp's share of a token that several pieces have: slot 0 of its piece where it
+// has come from the piece before, else slot 1.
+template <int V>
+__device__ __forceinline__ void leave_share(const EmbedGradCall& a, const Sum& s, uint32_t piece, uint32_t slice,
+                                            uint32_t lane, bool came, const float (&sum)[kLane]) {
+  float* to = s.shares + (static_cast<uint64_t>(piece) * 2 + (came ? 0 : 1)) * a.d;
+#pragma unroll
+  for (int k = 0; k < kLane / V; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const uint32_t c = column<V>(slice, k, lane) + j;
+      if (c < a.d) to[c] = sum[k * V + j];
+    }
+}
+
+// The pieces that begin with the token from piece q + 1 on, or (back) those before q that
+// end with it: how many there are without a gap.
+__device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t token, uint32_t q, uint32_t lane, bool back) {
+  uint32_t run = 0;
+  while (true) {
+    const uint32_t step = run + 1 + lane;
+    bool same = false;
+    if (back) same = step <= q && __ldg(s.key + (q - step + 1) * s.piece - 1) == token;
+    else same = q + step < s.pieces && __ldg(s.key + (q + step) * s.piece) == token;
+    const uint32_t m = __ballot_sync(0xffffffffu, same);
+    if (m != 0xffffffffu) return run + __ffs(~m) - 1;
+    run += 32;
+  }
+}
+
+// Where a token's shares are all there with this warp's: their sum, in order of the pieces.
+template <typename T, int V>
+__device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s, uint32_t token, uint32_t piece,
+                                         uint32_t slice, uint32_t lane, bool came, bool on) {
+  const uint32_t before = came ? run_of(s, token, piece, lane, true) : 0u;
+  const uint32_t after = on ? run_of(s, token, piece, lane, false) : 0u;
+  const uint32_t first = piece - before, shares = before + 1 + after;
+  uint32_t had = 0;
+  __syncwarp();
+  if (lane == 0) {
+    __threadfence();
+    had = atomicAdd(s.arrived + static_cast<uint64_t>(first) * s.slices + slice, 1u);
+    __threadfence();
+  }
+  if (__shfl_sync(0xffffffffu, had, 0) + 1 != shares) return;
+  float sum[kLane] = {};
+  constexpr uint32_t kAhead = 4;  // shares on their way
+  for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {
+    float x[kAhead][kLane];
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; ++q) {
+      const float* from = s.shares + (static_cast<uint64_t>(first + q0 + q) * 2 + (q0 + q == 0 ? 1 : 0)) * a.d;
+#pragma unroll
+      for (int k = 0; k < kLane / V; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const uint32_t c = column<V>(slice, k, lane) + j;
+          x[q][k * V + j] = q0 + q < shares && c < a.d ? __ldcg(from + c) : 0.0f;
+        }
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; ++q)
+      if (q0 + q < shares)
+#pragma unroll
+        for (int j = 0; j < kLane; ++j) sum[j] += x[q][j];
+  }
+  write_row<T, V>(a, token, slice, lane, sum);
 }
 
 template <typename D, typename T, int V>
@@ -375,14 +454,8 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, c
   auto flush = [&](bool on) {  // `on`: the token goes on in the next piece
     if (token < a.v) {
       if (goes_on || on) {
-        float* to = s.shares + (static_cast<uint64_t>(piece) * 2 + (goes_on ? 0 : 1)) * a.d;
-#pragma unroll
-        for (int k = 0; k < kLane / V; ++k)
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const uint32_t c = column<V>(slice, k, lane) + j;
-            if (c < a.d) to[c] = sum[k * V + j];
-          }
+        leave_share<V>(a, s, piece, slice, lane, goes_on, sum);
+        join_shares<T, V>(a, s, token, piece, slice, lane, goes_on, on);
       } else {
         write_row<T, V>(a, token, slice, lane, sum);
       }
@@ -418,82 +491,6 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, c
     }
   }
   flush(hi < a.n && __ldg(s.key + hi) == token);
-}
-
-// The shares of a token that goes on past the piece it begins in, joined in order.
-// A CTA takes eight pieces and one slice; a token of more than kShort shares is
-// added up by all its warps, each taking a run of them.
-constexpr uint32_t kShort = 16;
-template <typename T, int V>
-__global__ void __launch_bounds__(256) embed_join_kernel(const EmbedGradCall a, const Sum s) {
-  __shared__ uint32_t ends[8];
-  __shared__ float part[8][kSlice];
-  griddep_wait();
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const uint32_t slice = blockIdx.x % s.slices, first = blockIdx.x / s.slices * 8;
-  const uint32_t piece = first + warp;
-  uint32_t end = 0;  // the last piece with a share of the token that piece's last one is
-  uint32_t token = 0;
-  if (piece + 1 < s.pieces) {
-    const uint32_t lo = piece * s.piece, hi = lo + s.piece;
-    token = __ldg(s.key + hi - 1);
-    const bool begins = lo == 0 || __ldg(s.key + lo - 1) != token;
-    if (token < a.v && begins) {  // (the same in all lanes) the pieces after this that begin with it
-      end = piece;
-      while (true) {
-        const uint32_t next = end + 1 + lane;
-        const uint32_t m = __ballot_sync(0xffffffffu, next < s.pieces && __ldg(s.key + next * s.piece) == token);
-        if (m != 0xffffffffu) {
-          end += __ffs(~m) - 1;
-          break;
-        }
-        end += 32;
-      }
-      if (end == piece) end = 0;
-    }
-  }
-  auto add = [&](uint32_t share, float (&sum)[kLane]) {
-    const float* from = s.shares + static_cast<uint64_t>(share) * a.d + slice * kSlice;
-#pragma unroll
-    for (int j = 0; j < kLane; ++j)
-      if (slice * kSlice + j * 32 + lane < a.d) sum[j] += from[j * 32 + lane];
-  };
-  auto write = [&](uint32_t row, const float (&sum)[kLane]) {
-    T* to = static_cast<T*>(a.dtable) + static_cast<uint64_t>(row) * a.ld_dtable + slice * kSlice;
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      const uint32_t c = j * 32 + lane;
-      if (slice * kSlice + c < a.d) store_rounded(to + c, a.add ? fmaf(sum[j], a.scale, widen(to[c])) : sum[j] * a.scale);
-    }
-  };
-  if (lane == 0) ends[warp] = end;
-  if (end && end - piece <= kShort) {
-    float sum[kLane] = {};
-    add(2 * piece + 1, sum);
-#pragma unroll 4
-    for (uint32_t q = piece + 1; q <= end; ++q) add(2 * q, sum);
-    write(token, sum);
-  }
-  __syncthreads();
-  for (uint32_t w = 0; w < 8; ++w) {
-    const uint32_t p = first + w, e = ends[w];
-    if (e == 0 || e - p <= kShort) continue;
-    const uint32_t per = (e - p + 7) / 8, lo = p + 1 + warp * per, hi = min(lo + per, e + 1);
-    float sum[kLane] = {};
-    if (warp == 0) add(2 * p + 1, sum);
-#pragma unroll 4
-    for (uint32_t q = lo; q < hi; ++q) add(2 * q, sum);
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) part[warp][j * 32 + lane] = sum[j];
-    __syncthreads();
-    if (warp == 0) {
-#pragma unroll
-      for (int j = 0; j < kLane; ++j)
-        for (uint32_t q = 1; q < 8; ++q) sum[j] += part[q][j * 32 + lane];
-      write(__ldg(s.key + p * s.piece + s.piece - 1), sum);
-    }
-    __syncthreads();
-  }
 }
 
 // ------------------------------------------------------------------ planning
@@ -541,7 +538,8 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   p.hist = round(static_cast<size_t>(s.parts) * (4u << s.bits));
   p.key = round(static_cast<size_t>(c.n) * 4);
   p.shares = round(static_cast<size_t>(m.pieces) * 2 * c.d * 4);
-  p.bytes = kMaxPasses * p.hist + 4 * p.key + p.shares;
+  s.arrivals = m.warps;
+  p.bytes = p.hist + 4 * p.key + p.shares + round(static_cast<size_t>(s.arrivals) * 4);
   return p;
 }
 
@@ -558,12 +556,8 @@ cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   Sum s = p.sum;
   void* params[] = {&a, &s};
   count_launch();
-  cudaError_t err = launch_pdl(reinterpret_cast<const void*>(embed_sum_kernel<D, T, V>),
-                               dim3((s.warps + 7) / 8 + zeros), 256, 0, stream, params, false);
-  if (err != cudaSuccess) return err;
-  count_launch();
-  return launch_pdl(reinterpret_cast<const void*>(embed_join_kernel<T, V>),
-                    dim3((s.pieces + 7) / 8 * s.slices), 256, 0, stream, params, false);
+  return launch_pdl(reinterpret_cast<const void*>(embed_sum_kernel<D, T, V>),
+                    dim3((s.warps + 7) / 8 + zeros), 256, 0, stream, params, false);
 }
 
 template <typename D, typename T>
@@ -584,28 +578,30 @@ cudaError_t launch_embed_grad(const EmbedGradCall& c, Workspace& ws, const Devic
   if (!p.few) {
     Sort& s = p.sort;
     char* at = ws.model_scratch();
-    for (int i = 0; i < kMaxPasses; ++i) {
-      s.hist[i] = reinterpret_cast<uint32_t*>(at);
-      at += p.hist;
-    }
+    s.hist = reinterpret_cast<uint32_t*>(at);
+    at += p.hist;
     for (int i = 0; i < 2; ++i) {
       s.key[i] = reinterpret_cast<uint32_t*>(at);
       s.pos[i] = reinterpret_cast<uint32_t*>(at + p.key);
       at += 2 * p.key;
     }
     p.sum.shares = reinterpret_cast<float*>(at);
+    p.sum.arrived = s.arrived = reinterpret_cast<uint32_t*>(at + p.shares);
     p.sum.key = s.key[s.passes & 1u];
     p.sum.pos = s.pos[s.passes & 1u];
     s.token = c.token;
-    count_launch();
-    embed_count_kernel<<<s.parts, kSortThreads, 0, ws.stream>>>(s);
-    if ((err = cudaGetLastError()) != cudaSuccess) return err;
     for (uint32_t pass = 0; pass < s.passes; ++pass) {
-      count_launch();
       void* params[] = {&s, &pass};
-      err = launch_pdl(p.rounds == 1 ? reinterpret_cast<const void*>(embed_scatter_kernel<1>)
-                                     : reinterpret_cast<const void*>(embed_scatter_kernel<4>),
-                       dim3(s.parts), kSortThreads, 0, ws.stream, params, false);
+      const void* scatter = p.rounds == 1 ? reinterpret_cast<const void*>(embed_scatter_kernel<1>)
+                                          : reinterpret_cast<const void*>(embed_scatter_kernel<4>);
+      count_launch();
+      if (pass == 0) embed_count_kernel<<<s.parts, kSortThreads, 0, ws.stream>>>(s, pass);
+      else err = launch_pdl(reinterpret_cast<const void*>(embed_count_kernel), dim3(s.parts), kSortThreads, 0,
+                            ws.stream, params, false);
+      if (err == cudaSuccess) err = cudaGetLastError();
+      if (err != cudaSuccess) return err;
+      count_launch();
+      err = launch_pdl(scatter, dim3(s.parts), kSortThreads, 0, ws.stream, params, false);
       if (err != cudaSuccess) return err;
     }
   }
