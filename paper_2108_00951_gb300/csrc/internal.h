@@ -379,6 +379,9 @@ struct AdamStates {
 cudaError_t launch_adamw_states(const AdamStates* t, uint32_t n, bool out_bf16, cudaStream_t stream);
 
 // Launch bookkeeping.
+// CTAs of a kernel that an SM holds, with the kernel opted into that much shared
+// memory on the current device; asked once per kernel, device and size (norm.cu).
+cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t* ctas);
 // A launch that may begin while the previous kernel on the stream finishes
 // (programmatic dependent launch: the kernel waits for its predecessor with
 // griddepcontrol.wait before reading what it wrote), optionally cooperative.

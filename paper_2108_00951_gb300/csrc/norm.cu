@@ -194,14 +194,26 @@ cudaError_t launch_typed(NormCall c, const DeviceInfo& dev, cudaStream_t stream)
 cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t* ctas) {
   static std::mutex mu;
   static std::map<std::tuple<int, const void*, uint32_t, uint32_t>, uint32_t> known;
+  struct Last {  // what a thread asked for last, by kernel
+    const void* kernel;
+    int dev;
+    uint32_t threads, smem, ctas;
+  };
+  static thread_local Last last[16] = {};
   int dev = 0, n = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
+  Last& l = last[(reinterpret_cast<uintptr_t>(kernel) >> 4) % 16];
+  if (l.kernel == kernel && l.dev == dev && l.threads == threads && l.smem == smem) {
+    *ctas = l.ctas;
+    return cudaSuccess;
+  }
   std::lock_guard<std::mutex> lk(mu);
   const auto key = std::make_tuple(dev, kernel, threads, smem);
   const auto it = known.find(key);
   if (it != known.end()) {
     *ctas = it->second;
+    l = {kernel, dev, threads, smem, it->second};
     return cudaSuccess;
   }
   // (an opt-in stays: the largest asked for, whatever order sizes come in)
