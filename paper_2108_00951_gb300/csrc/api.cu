@@ -4,6 +4,7 @@
 // and aggregate.cu, of vocab.cu, vocab_few.cu, ortho.cu and ortho_small.cu, and of
 // embed.cu, embed_grad.cu, norm.cu, norm_grad.cu and adamw.cu.
 #include <algorithm>
+#include <array>
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -687,50 +688,55 @@ ef_status layer_norm_grad_entry(const void* x, uint64_t ldx, ef_grad_type x_type
   return err == cudaSuccess ? EF_OK : EF_ERR_CUDA;
 }
 
-// The address ranges of a call over lists of tensors. Lists as models have them, each
-// ascending in its own stretch of memory, are checked in one pass; others by
-// sorting all ranges.
-class Ranges {
- public:
-  explicit Ranges(size_t most) { all_.reserve(most); }
-  void begin_list() { lists_.push_back({UINTPTR_MAX, 0}); }
-  void add(const void* p, uint64_t bytes, bool written) {
-    if (!p || bytes == 0) return;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    List& l = lists_.back();
-    ascending_ &= at >= l.end;
-    l.at = std::min(l.at, at);
-    l.end = std::max(l.end, at + bytes);
-    all_.push_back({at, at + bytes, written});
-  }
-  // Whether anything written overlaps anything else.
-  bool overlap() {
-    std::sort(lists_.begin(), lists_.end(), [](const List& x, const List& y) { return x.at < y.at; });
-    bool apart = ascending_;
-    for (size_t i = 1; i < lists_.size(); ++i) apart &= lists_[i].at >= lists_[i - 1].end || lists_[i].end == 0;
-    if (apart) return false;
-    std::sort(all_.begin(), all_.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
-    uintptr_t any = 0, write = 0;  // how far those before reach
-    for (const Range& r : all_) {
-      if (r.at < write || (r.written && r.at < any)) return true;
-      any = std::max(any, r.end);
-      if (r.written) write = std::max(write, r.end);
-    }
-    return false;
-  }
-
- private:
-  struct List {
-    uintptr_t at, end;
-  };
-  struct Range {
-    uintptr_t at, end;
-    bool written;
-  };
-  std::vector<List> lists_;
-  std::vector<Range> all_;
-  bool ascending_ = true;
+// Whether anything written overlaps anything else among the arrays of lists of tensors:
+// range(l, i) is that of tensor i in list l. Lists as models have them, each ascending in
+// its own stretch of memory, are seen to be apart in one pass; others by sorting.
+struct Range {
+  uintptr_t at;
+  uint64_t bytes;  // 0: none
+  bool written;
 };
+template <typename F>
+bool lists_overlap(uint32_t lists, uint32_t n, F range) {
+  struct Span {
+    uintptr_t at, end;
+  };
+  std::array<Span, 10> spans;
+  uint32_t used = 0;
+  bool apart = true;
+  for (uint32_t l = 0; l < lists && apart; ++l) {
+    Span s = {UINTPTR_MAX, 0};
+    for (uint32_t i = 0; i < n; ++i) {
+      const Range r = range(l, i);
+      if (r.bytes == 0) continue;
+      apart &= r.at >= s.end;
+      s.at = std::min(s.at, r.at);
+      s.end = std::max(s.end, r.at + r.bytes);
+    }
+    for (uint32_t q = 0; q < used; ++q) apart &= s.at >= spans[q].end || spans[q].at >= s.end;
+    if (s.end) spans[used++] = s;
+  }
+  if (apart) return false;
+  std::vector<Range> all;
+  all.reserve(static_cast<size_t>(lists) * n);
+  for (uint32_t l = 0; l < lists; ++l)
+    for (uint32_t i = 0; i < n; ++i) {
+      const Range r = range(l, i);
+      if (r.bytes) all.push_back(r);
+    }
+  std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
+  uintptr_t any = 0, write = 0;  // how far those before reach
+  for (const Range& r : all) {
+    if (r.at < write || (r.written && r.at < any)) return true;
+    any = std::max(any, r.at + r.bytes);
+    if (r.written) write = std::max(write, r.at + r.bytes);
+  }
+  return false;
+}
+Range range_of(const void* p, uint64_t bytes, bool written) {
+  return {reinterpret_cast<uintptr_t>(p), p ? bytes : 0, written};
+}
+uint64_t blocks_of(uint64_t numel) { return (numel + 127) / 128; }
 
 constexpr uint32_t kMaxTensors = 1u << 20;
 
@@ -747,7 +753,8 @@ ef_status adamw_entry(uint32_t n, const uint64_t* numel, float* const* p, const 
   c.g_bf16 = g_type == EF_GRAD_BF16;
   c.eight = me != nullptr;
   const uint64_t state = c.eight ? 1 : 4;
-  std::vector<AdamTensor> t(n);
+  static thread_local std::vector<AdamTensor> t;  // (kept for its memory)
+  t.assign(n, AdamTensor());
   bool any = false;
   for (uint32_t i = 0; i < n; ++i) {
     if (numel[i] > kMaxD - 4095) return EF_ERR_INVALID_ARG;
@@ -767,24 +774,24 @@ ef_status adamw_entry(uint32_t n, const uint64_t* numel, float* const* p, const 
       return EF_ERR_INVALID_ARG;
   }
   if (!any) return EF_OK;
-  Ranges ranges(7ull * n + 3);
-  auto list = [&](auto&& at, uint64_t size, bool written, uint64_t per) {
-    ranges.begin_list();
-    for (const AdamTensor& x : t) ranges.add(at(x), (x.numel + per - 1) / per * size, written);
+  const uint64_t gsize = size_of(g_type);
+  const auto range = [&](uint32_t l, uint32_t i) {
+    const AdamTensor& x = t[i];
+    const uint64_t k = x.numel;
+    switch (l) {
+      case 0: return range_of(x.p, k * 4, true);
+      case 1: return range_of(x.g, k * gsize, false);
+      case 2: return range_of(x.m, k * state, true);
+      case 3: return range_of(x.v, k * state, true);
+      case 4: return range_of(x.copy, k * 2, true);
+      case 5: return range_of(x.me, blocks_of(k), true);
+      case 6: return range_of(x.ve, blocks_of(k), true);
+      case 7: return range_of(i ? nullptr : c.lr_dev, 4, false);
+      case 8: return range_of(i ? nullptr : c.step_dev, 8, false);
+      default: return range_of(i ? nullptr : c.grad_scale, 4, false);
+    }
   };
-  list([](const AdamTensor& x) { return x.p; }, 4, true, 1);
-  list([](const AdamTensor& x) { return x.g; }, size_of(g_type), false, 1);
-  list([](const AdamTensor& x) { return x.m; }, state, true, 1);
-  list([](const AdamTensor& x) { return x.v; }, state, true, 1);
-  list([](const AdamTensor& x) { return x.copy; }, 2, true, 1);
-  list([](const AdamTensor& x) { return x.me; }, 1, true, 128);
-  list([](const AdamTensor& x) { return x.ve; }, 1, true, 128);
-  const std::pair<const void*, uint64_t> scalars[] = {{c.lr_dev, 4}, {c.step_dev, 8}, {c.grad_scale, 4}};
-  for (const auto& x : scalars) {
-    ranges.begin_list();
-    ranges.add(x.first, x.second, false);
-  }
-  if (ranges.overlap()) return EF_ERR_INVALID_ARG;
+  if (lists_overlap(10, n, range)) return EF_ERR_INVALID_ARG;
   return launch_adamw(t.data(), n, c, stream) == cudaSuccess ? EF_OK : EF_ERR_CUDA;
 }
 
@@ -796,7 +803,8 @@ ef_status adamw_states_entry(uint32_t n, const uint64_t* numel, const uint8_t* c
   if (n == 0) return EF_OK;
   if (!numel || !m || !v || !me || !ve || !m_out || !v_out) return EF_ERR_INVALID_ARG;
   const uint64_t size = size_of(out_type);
-  std::vector<AdamStates> t(n);
+  static thread_local std::vector<AdamStates> t;  // (kept for its memory)
+  t.assign(n, AdamStates());
   for (uint32_t i = 0; i < n; ++i) {
     if (numel[i] > kMaxD - 4095) return EF_ERR_INVALID_ARG;
     t[i].numel = static_cast<uint32_t>(numel[i]);
@@ -811,18 +819,19 @@ ef_status adamw_states_entry(uint32_t n, const uint64_t* numel, const uint8_t* c
         !aligned(v_out[i], size))
       return EF_ERR_INVALID_ARG;
   }
-  Ranges ranges(6ull * n);
-  auto list = [&](auto&& at, uint64_t bytes, bool written, uint64_t per) {
-    ranges.begin_list();
-    for (const AdamStates& x : t) ranges.add(at(x), (x.numel + per - 1) / per * bytes, written);
+  const auto range = [&](uint32_t l, uint32_t i) {
+    const AdamStates& x = t[i];
+    const uint64_t k = x.numel;
+    switch (l) {
+      case 0: return range_of(x.m, k, false);
+      case 1: return range_of(x.v, k, false);
+      case 2: return range_of(x.me, blocks_of(k), false);
+      case 3: return range_of(x.ve, blocks_of(k), false);
+      case 4: return range_of(x.m_out, k * size, true);
+      default: return range_of(x.v_out, k * size, true);
+    }
   };
-  list([](const AdamStates& x) { return x.m; }, 1, false, 1);
-  list([](const AdamStates& x) { return x.v; }, 1, false, 1);
-  list([](const AdamStates& x) { return x.me; }, 1, false, 128);
-  list([](const AdamStates& x) { return x.ve; }, 1, false, 128);
-  list([](const AdamStates& x) { return x.m_out; }, size, true, 1);
-  list([](const AdamStates& x) { return x.v_out; }, size, true, 1);
-  if (ranges.overlap()) return EF_ERR_INVALID_ARG;
+  if (lists_overlap(6, n, range)) return EF_ERR_INVALID_ARG;
   return launch_adamw_states(t.data(), n, out_type == EF_GRAD_BF16, stream) == cudaSuccess ? EF_OK
                                                                                             : EF_ERR_CUDA;
 }

@@ -310,7 +310,8 @@ struct NormCall {
   float eps;
   uint32_t n, d;
   bool x_bf16, y_bf16, w_bf16;
-  bool w_wide, b_wide;   // (the launcher's: on the boundary of the kernel's vectors)
+  uint32_t warps;        // (the launcher's: of a row; and whether the weights lie on the
+  bool w_wide, b_wide;   // boundaries of the kernel's vectors)
 };
 cudaError_t launch_layer_norm(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream);
 struct NormGradCall {
@@ -321,7 +322,7 @@ struct NormGradCall {
   const float *mean, *rstd;  // [n]
   float* shares;         // (the launcher's: [parts][2][d])
   uint64_t ldx, lddy, lddx;
-  uint32_t n, d;
+  uint32_t n, d, warps;  // (warps, w_wide: as above)
   bool x_bf16, y_bf16, w_bf16, w_wide;
 };
 cudaError_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev, size_t* bytes);

@@ -3,11 +3,10 @@
 //
 // Both sums are fp32 over values that stay in registers, the second after the
 // mean is known (a difference of squares would lose the variance of rows whose
-// mean is large). What bounds it: reading x and writing y once. A warp (rows of at
-// most 1024 values, no barrier) or a CTA (at most 8192) takes rows a stride apart; the
-// next ones are on their way into a ring in shared memory meanwhile, and the
-// weights stay in registers. A longer row is read three times, twice out of L1
-// and L2.
+// mean is large). What bounds it: reading x and writing y once. One to eight warps (rows
+// of up to 8192 values) take rows a stride apart; the next ones are on their way into a
+// ring in shared memory meanwhile, and the weights stay in registers. A longer row is
+// read three times, twice out of L1 and L2.
 #include <algorithm>
 #include <map>
 #include <mutex>
@@ -18,23 +17,22 @@
 namespace efs {
 namespace {
 
-constexpr uint32_t kWarpsPerCta = 4;
-// Rows that a group has in its ring, with K V values of a row a thread.
-template <int E, bool WARP>
-constexpr int kRing = !WARP ? 4 : E == 8 ? 8 : E == 16 ? 4 : 3;
+// Rows that a group has in its ring, with E values of a row a thread.
+template <int E>
+constexpr int kRing = E == 8 ? 8 : 4;
 
-template <typename X, typename Y, int V, int K, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) norm_kernel(const NormCall a) {
-  constexpr int S = kRing<V * K, WARP>, W = V > 1 ? 2 : 1;
-  using L = Lane<W>;
+template <typename X, typename Y, int V, int K>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
+  constexpr int S = kRing<V * K>;
+  constexpr bool kAll = V * K == 32;  // a CTA has one row at a time
   extern __shared__ __align__(16) char ring[];
-  __shared__ __align__(16) float room[2][32];
-  const uint32_t group = WARP ? 32u : blockDim.x;
-  const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x;
-  const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
-  const uint32_t first = WARP ? blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5) : blockIdx.x;
+  __shared__ __align__(16) float room[2][16];
+  const RowGroup<kAll> g(a.warps);
+  const uint32_t group = g.threads(), t = g.t;
+  const uint32_t per_cta = kAll ? 1u : blockDim.x / group, groups = gridDim.x * per_cta;
+  const uint32_t first = blockIdx.x * per_cta + g.index;
   const uint32_t place = row_place(a.d, sizeof(X));
-  char* rows = ring + (WARP ? (threadIdx.x >> 5) * S * place : 0u);
+  char* rows = ring + g.index * S * place;
   auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
   auto fetch = [&](uint32_t row, uint32_t slot) {
     if (row < a.n) fetch_row(rows + slot * place, x_row(row), a.d * sizeof(X), t, group);
@@ -42,67 +40,57 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) no
   };
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
-  L w[K][V / W], b[K][V / W];
+  float w[K][V], b[K][V];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t c = (k * group + t) * V;
     if (c < a.d) {
-      load_weights<V, W>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
-      load_weights<V, W>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
+      load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+      load_weights<V>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
     }
   }
   const float inv = 1.0f / static_cast<float>(a.d);
-  if (!WARP) {
-    clear_room(room[0], 64);
-    __syncthreads();
-  }
   uint32_t slot = 0;
   for (uint32_t row = first; row < a.n; row += groups) {
     fetch_wait<S - 2>();
-    if (WARP) __syncwarp();
-    else __syncthreads();
+    g.sync();
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const char* in_row = rows + slot * place + row_lead(x_row(row));
     slot = slot == S - 1 ? 0 : slot + 1;
-    L x[K][V / W], sums = L::all(0.0f);
+    float x[K][V], sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
         const Vec<X, V> in = staged<X, V>(in_row, c);
 #pragma unroll
-        for (int j = 0; j < V / W; ++j) {
-          x[k][j] = in.template lane<W>(j);
-          sums = sums + x[k][j];
-        }
+        for (int j = 0; j < V; ++j) sum += x[k][j] = in.get(j);
       }
     }
-    const float mean = (WARP ? warp_sum(sums.sum()) : cta_sum(sums.sum(), room[0])) * inv;
-    const L minus = L::all(-mean);
-    sums = L::all(0.0f);
+    const float mean = group_sum(g, sum, room[0]) * inv;
+    sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if ((k * group + t) * V < a.d)
 #pragma unroll
-        for (int j = 0; j < V / W; ++j) {
-          x[k][j] = x[k][j] + minus;
-          sums = fma(x[k][j], x[k][j], sums);
+        for (int j = 0; j < V; ++j) {
+          x[k][j] -= mean;
+          sum = fmaf(x[k][j], x[k][j], sum);
         }
     }
-    const float var = (WARP ? warp_sum(sums.sum()) : cta_sum(sums.sum(), room[1])) * inv;
+    const float var = group_sum(g, sum, room[1]) * inv;
     const float rstd = inverse_root(var + a.eps);
-    const L r = L::all(rstd);
     Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        L out[V / W];
+        float out[V];
 #pragma unroll
-        for (int j = 0; j < V / W; ++j) out[j] = fma(x[k][j] * r, w[k][j], b[k][j]);
+        for (int j = 0; j < V; ++j) out[j] = fmaf(x[k][j] * rstd, w[k][j], b[k][j]);
         Vec<Y, V> o;
-        o.template round<W>(out);
+        o.round(out);
         o.store(y + c);
       }
     }
@@ -116,23 +104,21 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads) no
 // Rows of any length, a CTA each.
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
-  __shared__ __align__(16) float room[2][32];
-  clear_room(room[0], 64);
-  __syncthreads();
+  __shared__ float room[2][64];
   const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(blockIdx.x) * a.ldx;
   Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(blockIdx.x) * a.ldy;
   const float inv = 1.0f / static_cast<float>(a.d);
   float sum = 0.0f;
 #pragma unroll 8
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) sum += widen(__ldg(x + c));
-  const float mean = cta_sum(sum, room[0]) * inv;
+  const float mean = cta_sum2(sum, 0.0f, room[0]).x * inv;
   sum = 0.0f;
 #pragma unroll 8
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
     const float off = widen(__ldg(x + c)) - mean;
     sum = fmaf(off, off, sum);
   }
-  const float rstd = inverse_root(cta_sum(sum, room[1]) * inv + a.eps);
+  const float rstd = inverse_root(cta_sum2(sum, 0.0f, room[1]).x * inv + a.eps);
 #pragma unroll 4
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
     float w[1], b[1];
@@ -146,32 +132,32 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
   }
 }
 
-template <typename X, typename Y, int V, int K, bool WARP>
-cudaError_t launch_rows(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
-  const uint32_t warps = WARP ? kWarpsPerCta : 1;  // groups of a CTA
-  const uint32_t threads =
-      WARP ? 32 * kWarpsPerCta : ((c.d + kNormPerThread - 1) / kNormPerThread + 31) / 32 * 32;
-  const uint32_t smem = warps * kRing<V * K, WARP> * row_place(c.d, sizeof(X));
-  const void* fn = reinterpret_cast<const void*>(norm_kernel<X, Y, V, K, WARP>);
+template <typename X, typename Y, int V, int K>
+cudaError_t launch_rows(NormCall c, const DeviceInfo& dev, cudaStream_t stream) {
+  c.warps = row_warps(c.d, V * K);
+  const uint32_t threads = V * K == 32 ? c.warps * 32 : kNormThreads, per_cta = threads / (c.warps * 32);
+  const uint32_t smem = per_cta * kRing<V * K> * row_place(c.d, sizeof(X));
+  const void* fn = reinterpret_cast<const void*>(norm_kernel<X, Y, V, K>);
   uint32_t per_sm = 0;
   const cudaError_t err = resident_ctas(fn, threads, smem, &per_sm);
   if (err != cudaSuccess) return err;
-  const uint32_t grid = std::min((c.n + warps - 1) / warps, per_sm * static_cast<uint32_t>(dev.sm_count));
-  norm_kernel<X, Y, V, K, WARP><<<grid, threads, smem, stream>>>(c);
+  const uint32_t grid = std::min((c.n + per_cta - 1) / per_cta, per_sm * static_cast<uint32_t>(dev.sm_count));
+  norm_kernel<X, Y, V, K><<<grid, threads, smem, stream>>>(c);
   return cudaGetLastError();
 }
 
 template <typename X, typename Y, int V>
 cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
-  if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, true>(c, dev, stream);
-  if (c.d <= 512) return launch_rows<X, Y, V, 16 / V, true>(c, dev, stream);
-  if (c.d <= kNormWarpWidth) return launch_rows<X, Y, V, 32 / V, true>(c, dev, stream);
-  return launch_rows<X, Y, V, kNormPerThread / V, false>(c, dev, stream);
+  // Values of a row that a thread holds: fewer warps a row add up and wait less
+  // (32,768 x 4096: 16 a thread 126 us, 32 81), more have more rows at once
+  if (c.d <= 256) return launch_rows<X, Y, V, 8 / V>(c, dev, stream);
+  if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V>(c, dev, stream);
+  return launch_rows<X, Y, V, 32 / V>(c, dev, stream);
 }
 
 template <typename X, typename Y>
 cudaError_t launch_typed(NormCall c, const DeviceInfo& dev, cudaStream_t stream) {
-  if (c.d > kNormCtaWidth) {
+  if (c.d > kNormRowWidth) {
     norm_long_kernel<X, Y><<<c.n, 1024, 0, stream>>>(c);
     return cudaGetLastError();
   }

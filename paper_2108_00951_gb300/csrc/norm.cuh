@@ -8,10 +8,32 @@
 
 namespace efs {
 
-constexpr uint32_t kNormMaxThreads = 512;
-constexpr uint32_t kNormPerThread = 16;   // values of a row that a thread of a CTA holds
-constexpr uint32_t kNormCtaWidth = kNormMaxThreads * kNormPerThread;  // longest row in a CTA's registers
-constexpr uint32_t kNormWarpWidth = 1024; // longest row of a warp
+constexpr uint32_t kNormThreads = 256;    // of a CTA that has several rows at once
+constexpr uint32_t kNormRowWidth = 8192;  // longest row that threads hold
+
+// The threads that have a row together: 1, 2, 4 or 8 warps of a CTA, with which no
+// other threads of the CTA wait. ALL: the whole CTA.
+template <bool ALL>
+struct RowGroup {
+  uint32_t warps, index, t;  // warps of the group, its number in the CTA, this thread's in the group
+  __device__ __forceinline__ explicit RowGroup(uint32_t of_row) {
+    warps = ALL ? blockDim.x >> 5 : of_row;
+    index = ALL ? 0u : threadIdx.x / (warps * 32u);
+    t = threadIdx.x - index * warps * 32u;
+  }
+  __device__ __forceinline__ uint32_t threads() const { return warps * 32u; }
+  __device__ __forceinline__ void sync() const {
+    if (ALL) __syncthreads();
+    else if (warps == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(index + 1u), "r"(warps * 32u) : "memory");
+  }
+};
+// Warps for rows of d values with `per` a thread: a power of two.
+inline uint32_t row_warps(uint32_t d, uint32_t per) {
+  uint32_t warps = 1;
+  while (warps * 32 * per < d) warps *= 2;
+  return warps;
+}
 
 // V values of a weight vector of either type, or `none` where there is no vector.
 template <int V>
@@ -49,51 +71,50 @@ __device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide
   }
 }
 
-template <int V, int W>
-__device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide, uint32_t c,
-                                             float none, Lane<W> (&out)[V / W]) {
-  float f[V];
-  load_weights<V>(w, bf16, wide, c, none, f);
-#pragma unroll
-  for (int i = 0; i < V / W; ++i) out[i] = Lane<W>::of(f + i * W);
-}
-
-// The sum of `a` over the threads of a CTA, in a fixed order. `room`: 32 floats, zero from the
-// last warp's on, that no other sum uses before the next barrier but one.
-__device__ __forceinline__ float cta_sum(float a, float* room) {
+// Sums over the threads of a group, in a fixed order. `room`: 16 floats of the
+// CTA's a sum, which no other sum uses before the group's next barrier but one.
+template <bool ALL>
+__device__ __forceinline__ float group_sum(const RowGroup<ALL>& g, float a, float* room) {
   a = warp_sum(a);
-  const uint32_t warps = (blockDim.x + 31) >> 5;
+  if (g.warps == 1) return a;
   if ((threadIdx.x & 31u) == 0) room[threadIdx.x >> 5] = a;
-  __syncthreads();
+  g.sync();
+  const float* mine = room + g.index * g.warps;
   a = 0.0f;
-  for (uint32_t i = 0; i < warps; i += 4) {
-    const float4 x = *reinterpret_cast<const float4*>(room + i);
-    a += (x.x + x.y) + (x.z + x.w);
+  for (uint32_t i = 0; i < g.warps; i += 2) {
+    const float2 x = *reinterpret_cast<const float2*>(mine + i);
+    a += x.x + x.y;
   }
   return a;
 }
-// Two of them; `room` as above, 64 floats.
-__device__ __forceinline__ float2 cta_sum2(float a, float b, float* room) {
+// Two of them; `room`: 32 floats.
+template <bool ALL>
+__device__ __forceinline__ float2 group_sum2(const RowGroup<ALL>& g, float a, float b, float* room) {
   a = warp_sum(a);
   b = warp_sum(b);
-  const uint32_t warps = (blockDim.x + 31) >> 5;
-  if ((threadIdx.x & 31u) == 0) {
-    room[threadIdx.x >> 5] = a;
-    room[32 + (threadIdx.x >> 5)] = b;
-  }
-  __syncthreads();
+  if (g.warps == 1) return make_float2(a, b);
+  if ((threadIdx.x & 31u) == 0) *reinterpret_cast<float2*>(room + 2 * (threadIdx.x >> 5)) = make_float2(a, b);
+  g.sync();
+  const float* mine = room + 2 * g.index * g.warps;
   a = b = 0.0f;
-  for (uint32_t i = 0; i < warps; i += 4) {
-    const float4 x = *reinterpret_cast<const float4*>(room + i);
-    const float4 y = *reinterpret_cast<const float4*>(room + 32 + i);
-    a += (x.x + x.y) + (x.z + x.w);
-    b += (y.x + y.y) + (y.z + y.w);
+  for (uint32_t i = 0; i < 2 * g.warps; i += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(mine + i);
+    a += x.x + x.z;
+    b += x.y + x.w;
   }
   return make_float2(a, b);
 }
-// Zeros for a sum's room, seen by all after the CTA's next barrier.
-__device__ __forceinline__ void clear_room(float* room, uint32_t floats) {
-  if (threadIdx.x < floats) room[threadIdx.x] = 0.0f;
+
+// The same over a CTA (of rows that no group's registers hold).
+__device__ __forceinline__ float2 cta_sum2(float a, float b, float* room) {
+  a = warp_sum(a);
+  b = warp_sum(b);
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (lane == 0) room[warp] = a, room[32 + warp] = b;
+  __syncthreads();
+  a = lane < warps ? room[lane] : 0.0f;
+  b = lane < warps ? room[32 + lane] : 0.0f;
+  return make_float2(warp_sum(a), warp_sum(b));
 }
 
 // (var + eps)^(-1/2): the approximate root and one Newton step. Infinity for 0, as the

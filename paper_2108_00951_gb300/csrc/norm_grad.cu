@@ -4,12 +4,11 @@
 //   dx = rstd (q - sum q / d - x' sum(q x') / d),
 //   dw = sum over rows of dy x',   db = sum over rows of dy.
 //
-// What bounds it: reading x and dy and writing dx once. A warp (rows of at most
-// 1024 values) or a CTA (at most 8192) takes rows a stride apart, the next ones on
-// their way into a ring in shared memory, and keeps its columns' shares of dw and
-// db in registers (in shared memory for longer rows); the CTAs' shares are
-// joined by a second kernel in the order of the CTAs, so equal inputs give equal
-// bits.
+// What bounds it: reading x and dy and writing dx once. One to eight warps (rows of up to
+// 8192 values) take rows a stride apart, the next ones on their way into a ring in
+// shared memory, and keep their columns' shares of dw and db in registers (in shared
+// memory for longer rows); the CTAs' shares are joined by a second kernel in the order
+// of the CTAs, so equal inputs give equal bits.
 #include <algorithm>
 
 #include "norm.cuh"
@@ -17,11 +16,10 @@
 namespace efs {
 namespace {
 
-constexpr uint32_t kWarpsPerCta = 8;
-constexpr uint32_t kJoinColumns = 32, kJoinRows = 8;
+constexpr uint32_t kJoinColumns = 32, kJoinRows = 16;
 // Rows that a group has in its ring, with E values of a row a thread.
-template <int E, bool WARP>
-constexpr int kRing = !WARP ? 3 : E == 8 ? 6 : E == 16 ? 4 : 3;
+template <int E>
+constexpr int kRing = E == 8 ? 6 : 3;
 
 // A share of columns c of dw and db; the only one is the result.
 __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t share, uint32_t parts,
@@ -42,20 +40,19 @@ __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t shar
   }
 }
 
-// Rows of at most K V times the threads of a group (a warp, or a CTA).
-template <typename X, typename Y, int V, int K, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
+// Rows of at most K V times the threads of a group.
+template <typename X, typename Y, int V, int K, bool ALL>
+__global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormThreads, ALL && V * K == 16 ? 2 : 1)
     norm_grad_kernel(const NormGradCall a) {
-  constexpr int S = kRing<V * K, WARP>, W = V > 1 ? 2 : 1;
-  using L = Lane<W>;
+  constexpr int S = kRing<V * K>;
   extern __shared__ __align__(16) char ring[];
-  __shared__ __align__(16) float room[64];
-  const uint32_t group = WARP ? 32u : blockDim.x;
-  const uint32_t t = WARP ? threadIdx.x & 31u : threadIdx.x, warp = threadIdx.x >> 5;
-  const uint32_t groups = WARP ? gridDim.x * kWarpsPerCta : gridDim.x;
-  const uint32_t first = WARP ? blockIdx.x * kWarpsPerCta + warp : blockIdx.x;
+  __shared__ __align__(16) float room[32];
+  const RowGroup<ALL> of(a.warps);
+  const uint32_t group = of.threads(), t = of.t;
+  const uint32_t per_cta = ALL ? 1u : blockDim.x / group, groups = gridDim.x * per_cta;
+  const uint32_t first = blockIdx.x * per_cta + of.index;
   const uint32_t x_place = row_place(a.d, sizeof(X)), place = x_place + row_place(a.d, sizeof(Y));
-  char* rows = ring + (WARP ? warp * S * place : 0u);
+  char* rows = ring + of.index * S * place;
   auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
   auto dy_row = [&](uint32_t row) { return static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy; };
   auto fetch = [&](uint32_t row, uint32_t slot) {
@@ -69,24 +66,17 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
   float mean = 0.0f, rstd = 0.0f;
   if (first < a.n) mean = __ldg(a.mean + first), rstd = __ldg(a.rstd + first);
-  L w[K][V / W], dw[K][V / W], db[K][V / W];
+  float w[K][V], dw[K][V] = {}, db[K][V] = {};
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t c = (k * group + t) * V;
-    if (c < a.d) load_weights<V, W>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
-#pragma unroll
-    for (int j = 0; j < V / W; ++j) dw[k][j] = db[k][j] = L::all(0.0f);
+    if (c < a.d) load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
   }
   const float inv = 1.0f / static_cast<float>(a.d);
-  if (!WARP) {
-    clear_room(room, 64);
-    __syncthreads();
-  }
   uint32_t slot = 0;
   for (uint32_t row = first; row < a.n; row += groups) {
     fetch_wait<S - 2>();
-    if (WARP) __syncwarp();
-    else __syncthreads();
+    of.sync();
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const float mu = mean, r = rstd;
@@ -94,11 +84,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
     const char* xs = rows + slot * place + row_lead(x_row(row));
     const char* dys = rows + slot * place + x_place + row_lead(dy_row(row));
     slot = slot == S - 1 ? 0 : slot + 1;
-    // (a CTA's threads keep x' and q; a warp's, which have more columns, compute them again)
-    constexpr int kKept = WARP ? 1 : K;
-    L hat[kKept][V / W], q[kKept][V / W];
-    const L minus = L::all(-mu), scale = L::all(r);
-    L sum1 = L::all(0.0f), sum2 = L::all(0.0f);
+    float hat[K][V], q[K][V], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
@@ -106,91 +92,68 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
         const Vec<X, V> x = staged<X, V>(xs, c);
         const Vec<Y, V> dy = staged<Y, V>(dys, c);
 #pragma unroll
-        for (int j = 0; j < V / W; ++j) {
-          const L h = (x.template lane<W>(j) + minus) * scale, g = dy.template lane<W>(j);
-          const L p = g * w[k][j];
-          sum1 = sum1 + p;
-          sum2 = fma(p, h, sum2);
-          dw[k][j] = fma(g, h, dw[k][j]);
-          db[k][j] = db[k][j] + g;
-          if (!WARP) hat[k % kKept][j] = h, q[k % kKept][j] = p;
+        for (int j = 0; j < V; ++j) {
+          const float g = dy.get(j);
+          hat[k][j] = (x.get(j) - mu) * r;
+          q[k][j] = g * w[k][j];
+          s1 += q[k][j];
+          s2 = fmaf(q[k][j], hat[k][j], s2);
+          dw[k][j] = fmaf(g, hat[k][j], dw[k][j]);
+          db[k][j] += g;
         }
       }
     }
     if (!a.dx) continue;
-    float s1, s2;
-    if (WARP) {
-      s1 = warp_sum(sum1.sum());
-      s2 = warp_sum(sum2.sum());
-    } else {
-      const float2 s = cta_sum2(sum1.sum(), sum2.sum(), room);
-      s1 = s.x;
-      s2 = s.y;
-    }
-    const L m1 = L::all(-s1 * inv), m2 = L::all(-s2 * inv);
+    const float2 s = group_sum2(of, s1, s2, room);
+    const float m1 = s.x * inv, m2 = s.y * inv;
     X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t c = (k * group + t) * V;
       if (c < a.d) {
-        L out[V / W];
-        if (WARP) {
-          const Vec<X, V> x = staged<X, V>(xs, c);
-          const Vec<Y, V> dy = staged<Y, V>(dys, c);
+        float out[V];
 #pragma unroll
-          for (int j = 0; j < V / W; ++j) {
-            const L h = (x.template lane<W>(j) + minus) * scale;
-            out[j] = scale * fma(m2, h, fma(dy.template lane<W>(j), w[k][j], m1));
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < V / W; ++j)
-            out[j] = scale * fma(m2, hat[k % kKept][j], q[k % kKept][j] + m1);
-        }
+        for (int j = 0; j < V; ++j) out[j] = r * fmaf(-m2, hat[k][j], q[k][j] - m1);
         Vec<X, V> o;
-        o.template round<W>(out);
+        o.round(out);
         o.store(dx + c);
       }
     }
   }
+  griddep_launch_dependents();  // (the join, which waits for this kernel's end)
   if (!a.dw && !a.db) return;
-  if (!WARP) {
+  if (per_cta == 1) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const uint32_t c = (k * group + t) * V + j;
-        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j / W].get(j % W), db[k][j / W].get(j % W));
+        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j], db[k][j]);
       }
     return;
   }
-  // the warps' shares, summed in their order (in the ring's place: at least as large)
+  // the groups' shares, summed in their order (in the ring's place, which is larger)
   fetch_wait<0>();
-  float* shares = reinterpret_cast<float*>(ring);  // [kWarpsPerCta][d]
-  constexpr int kOut = (V * K + kWarpsPerCta - 1) / kWarpsPerCta;
-  float sums[kOut];
+  float* shares = reinterpret_cast<float*>(ring);  // [2][per_cta][d]
+  __syncthreads();
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    __syncthreads();
+  for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const uint32_t c = (k * 32 + t) * V + j;
-        if (c < a.d) shares[warp * a.d + c] = (which ? db[k][j / W] : dw[k][j / W]).get(j % W);
-      }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kOut; ++i) {
-      const uint32_t c = i * 32 * kWarpsPerCta + threadIdx.x;
+    for (int j = 0; j < V; ++j) {
+      const uint32_t c = (k * group + t) * V + j;
       if (c < a.d) {
-        float s = 0.0f;
-#pragma unroll
-        for (uint32_t q = 0; q < kWarpsPerCta; ++q) s += shares[q * a.d + c];
-        if (which) write_share(a, blockIdx.x, gridDim.x, c, sums[i], s);
-        else sums[i] = s;
+        shares[of.index * a.d + c] = dw[k][j];
+        shares[(per_cta + of.index) * a.d + c] = db[k][j];
       }
     }
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
+    float w_sum = 0.0f, b_sum = 0.0f;
+    for (uint32_t q = 0; q < per_cta; ++q) {
+      w_sum += shares[q * a.d + c];
+      b_sum += shares[(per_cta + q) * a.d + c];
+    }
+    write_share(a, blockIdx.x, gridDim.x, c, w_sum, b_sum);
   }
 }
 
@@ -200,10 +163,8 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpsPerCta : kNormMaxThreads)
 template <typename X, typename Y, bool SHARES>
 __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall a) {
   extern __shared__ float shares[];  // [2][d]
-  __shared__ __align__(16) float room[2][64];
+  __shared__ float room[2][64];
   const float inv = 1.0f / static_cast<float>(a.d);
-  clear_room(room[0], 128);
-  __syncthreads();
   if (SHARES)
     for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) shares[c] = shares[a.d + c] = 0.0f;
   uint32_t parity = 0;
@@ -261,8 +222,8 @@ __global__ void __launch_bounds__(256) norm_grad_columns_kernel(const NormGradCa
   }
 }
 
-// The sum of the CTAs' shares: 32 columns of dw or db per CTA, eight warps each
-// taking every eighth share.
+// The sum of the CTAs' shares: 32 columns of dw or db per CTA, 16 warps each
+// taking every 16th share.
 __global__ void __launch_bounds__(kJoinColumns * kJoinRows) norm_join_kernel(const NormGradCall a, uint32_t parts) {
   __shared__ float sums[kJoinRows][kJoinColumns];
   griddep_wait();
@@ -292,26 +253,27 @@ constexpr uint32_t kSharesWidth = 28000;  // columns whose shares fit shared mem
 // A call's kernel, its CTAs, and how many shares of dw and db they leave.
 struct Plan {
   const void* kernel;
-  uint32_t v, ctas, threads, smem, parts;
+  uint32_t v, warps, ctas, threads, smem, parts;
 };
 
-template <typename X, typename Y, int V, int K, bool WARP>
+template <typename X, typename Y, int V, int K, bool ALL>
 cudaError_t plan_rows(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
-  const uint32_t warps = WARP ? kWarpsPerCta : 1;  // groups of a CTA
-  p.kernel = reinterpret_cast<const void*>(norm_grad_kernel<X, Y, V, K, WARP>);
-  p.threads = WARP ? 32 * kWarpsPerCta : ((c.d + kNormPerThread - 1) / kNormPerThread + 31) / 32 * 32;
-  p.smem = warps * kRing<V * K, WARP> * (row_place(c.d, sizeof(X)) + row_place(c.d, sizeof(Y)));
+  p.kernel = reinterpret_cast<const void*>(norm_grad_kernel<X, Y, V, K, ALL>);
+  p.warps = row_warps(c.d, V * K);
+  p.threads = ALL ? p.warps * 32 : kNormThreads;
+  const uint32_t per_cta = p.threads / (p.warps * 32);
+  p.smem = per_cta * kRing<V * K> * (row_place(c.d, sizeof(X)) + row_place(c.d, sizeof(Y)));
   uint32_t per_sm = 0;
   const cudaError_t err = resident_ctas(p.kernel, p.threads, p.smem, &per_sm);
-  p.parts = p.ctas = std::min((c.n + warps - 1) / warps, per_sm * static_cast<uint32_t>(dev.sm_count));
+  p.parts = p.ctas = std::min((c.n + per_cta - 1) / per_cta, per_sm * static_cast<uint32_t>(dev.sm_count));
   return err;
 }
 template <typename X, typename Y, int V>
 cudaError_t plan_width(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
-  if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, true>(c, dev, p);
-  if (c.d <= 512) return plan_rows<X, Y, V, 16 / V, true>(c, dev, p);
-  if (c.d <= kNormWarpWidth) return plan_rows<X, Y, V, 32 / V, true>(c, dev, p);
-  return plan_rows<X, Y, V, kNormPerThread / V, false>(c, dev, p);
+  if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, false>(c, dev, p);
+  if (c.d <= 2048) return plan_rows<X, Y, V, 16 / V, false>(c, dev, p);
+  if (c.d <= 4096) return plan_rows<X, Y, V, 16 / V, true>(c, dev, p);
+  return plan_rows<X, Y, V, 32 / V, true>(c, dev, p);
 }
 template <typename X, typename Y>
 cudaError_t plan_typed(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
@@ -329,7 +291,7 @@ cudaError_t plan_typed(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
 cudaError_t plan_of(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
   p = {};
   if (c.n == 0) return cudaSuccess;
-  if (c.d <= kNormCtaWidth) {
+  if (c.d <= kNormRowWidth) {
     if (c.x_bf16) return c.y_bf16 ? plan_typed<bf16_t, bf16_t>(c, dev, p) : plan_typed<bf16_t, float>(c, dev, p);
     return c.y_bf16 ? plan_typed<float, bf16_t>(c, dev, p) : plan_typed<float, float>(c, dev, p);
   }
@@ -382,6 +344,7 @@ cudaError_t launch_layer_norm_grad(NormGradCall c, Workspace* ws, cudaStream_t s
   c.shares = ws ? reinterpret_cast<float*>(ws->model_scratch()) : nullptr;
   if (c.n == 0) {
   } else if (p.kernel) {
+    c.warps = p.warps;
     c.w_wide = rows_allow(c.w, 0, c.w_bf16 ? 2 : 4, c.w_bf16 ? p.v : std::min(p.v, 4u));
     void* params[] = {&c};
     count_launch();

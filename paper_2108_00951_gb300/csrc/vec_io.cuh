@@ -23,56 +23,6 @@ __device__ __forceinline__ float widen(bf16_t x) { return bf16_bits_to_f32(x); }
 __device__ __forceinline__ void store_rounded(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store_rounded(bf16_t* p, float x) { *p = round_bf16(x); }
 
-// One fp32 value, or two that one instruction works on (add, mul, fma .f32x2): a
-// kernel that is bound by issuing instructions needs half of them.
-template <int W>
-struct Lane;
-template <>
-struct Lane<1> {
-  float v;
-  __device__ __forceinline__ float sum() const { return v; }
-  __device__ __forceinline__ float get(int) const { return v; }
-  static __device__ __forceinline__ Lane of(const float* f) { return {f[0]}; }
-  static __device__ __forceinline__ Lane all(float f) { return {f}; }
-};
-template <>
-struct Lane<2> {
-  unsigned long long v;
-  __device__ __forceinline__ float get(int i) const {
-    float lo, hi;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-    return i ? hi : lo;
-  }
-  __device__ __forceinline__ float sum() const { return get(0) + get(1); }
-  static __device__ __forceinline__ Lane of(const float* f) {
-    Lane r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(f[0]), "f"(f[1]));
-    return r;
-  }
-  static __device__ __forceinline__ Lane all(float f) {
-    const float both[2] = {f, f};
-    return of(both);
-  }
-};
-__device__ __forceinline__ Lane<1> operator+(Lane<1> a, Lane<1> b) { return {a.v + b.v}; }
-__device__ __forceinline__ Lane<1> operator*(Lane<1> a, Lane<1> b) { return {a.v * b.v}; }
-__device__ __forceinline__ Lane<1> fma(Lane<1> a, Lane<1> b, Lane<1> c) { return {fmaf(a.v, b.v, c.v)}; }
-__device__ __forceinline__ Lane<2> operator+(Lane<2> a, Lane<2> b) {
-  Lane<2> r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Lane<2> operator*(Lane<2> a, Lane<2> b) {
-  Lane<2> r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Lane<2> fma(Lane<2> a, Lane<2> b, Lane<2> c) {
-  Lane<2> r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-
 // V values of T as they lie in memory, at an address that is a multiple of
 // their size (2 to 32 bytes).
 template <typename T, int V>
@@ -142,19 +92,6 @@ struct Vec {
   __device__ __forceinline__ float get(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
     return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
-  }
-  // Value i W and the W - 1 after it.
-  template <int W>
-  __device__ __forceinline__ Lane<W> lane(int i) const {
-    const float f[2] = {get(i * W), W > 1 ? get(i * W + W - 1) : 0.0f};
-    return Lane<W>::of(f);
-  }
-  template <int W>
-  __device__ __forceinline__ void round(const Lane<W> (&x)[V / W]) {
-    float f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = x[i / W].get(i % W);
-    round(f);
   }
   __device__ __forceinline__ void round(const float (&f)[V]) {
     if constexpr (sizeof(T) == 4) {
