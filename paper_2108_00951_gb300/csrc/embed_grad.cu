@@ -25,46 +25,50 @@ namespace {
 
 constexpr uint32_t kFewTokens = 2048;
 constexpr int kThreadsFew = 256;
-constexpr uint32_t kSlice = 256;        // columns a warp takes: 8 a lane
-constexpr int kLane = 8;
+constexpr int kLane = 8, kLaneMany = 16;  // columns a lane takes of a row: slices of 256, or 1024
+constexpr uint32_t kSlice = 32 * kLane;
+constexpr uint32_t kSumWarps = 8, kAheadMany = 4;
+constexpr uint32_t kPieceMany = 128;
+constexpr uint32_t kZeroRows = 64;
 constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
 constexpr int kSortThreads = 512;
 constexpr int kMaxBins = 512;
 constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
+constexpr uint32_t kPieceMost = 128;    // sorted positions that a warp adds up, at most
 
-// A lane's 8 columns of a slice: vectors of V, 32 V apart.
-template <int V>
+// A lane's L columns of a slice: vectors of V, 32 V apart.
+template <int V, int L>
 __device__ __forceinline__ uint32_t column(uint32_t slice, int k, uint32_t lane) {
-  return slice * kSlice + (k * 32 + lane) * V;
+  return slice * (32 * L) + (k * 32 + lane) * V;
 }
 
-template <typename T, int V>
+template <typename T, int V, int L>
 struct RowPart {
-  Vec<T, V> x[kLane / V];
+  Vec<T, V> x[L / V];
   __device__ __forceinline__ void load(const T* row, uint32_t slice, uint32_t lane, uint32_t d) {
 #pragma unroll
-    for (int k = 0; k < kLane / V; ++k) {
-      const uint32_t c = column<V>(slice, k, lane);
+    for (int k = 0; k < L / V; ++k) {
+      const uint32_t c = column<V, L>(slice, k, lane);
       if (c < d) x[k].load(row + c);
       else x[k].clear();
     }
   }
-  __device__ __forceinline__ void add_to(float (&sum)[kLane]) const {
+  __device__ __forceinline__ void add_to(float (&sum)[L]) const {
 #pragma unroll
-    for (int k = 0; k < kLane / V; ++k)
+    for (int k = 0; k < L / V; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[k * V + j] += x[k].get(j);
   }
 };
 
 // scale sum, or that added to what is there; rounded once.
-template <typename T, int V>
+template <typename T, int V, int L>
 __device__ __forceinline__ void write_row(const EmbedGradCall& a, uint64_t row, uint32_t slice,
-                                          uint32_t lane, const float (&sum)[kLane]) {
+                                          uint32_t lane, const float (&sum)[L]) {
   T* to = static_cast<T*>(a.dtable) + row * a.ld_dtable;
 #pragma unroll
-  for (int k = 0; k < kLane / V; ++k) {
-    const uint32_t c = column<V>(slice, k, lane);
+  for (int k = 0; k < L / V; ++k) {
+    const uint32_t c = column<V, L>(slice, k, lane);
     if (c < a.d) {
       float f[V];
       Vec<T, V> o;
@@ -164,7 +168,7 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
     float sum[kLane] = {};
     if (work) {
       for (uint32_t k = group; k < total; k += groups * kAhead) {
-        RowPart<D, V> row[kAhead];
+        RowPart<D, V, kLane> row[kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
           if (k + q * groups < total)
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
           for (int j = 0; j < kLane; ++j) sum[j] += part[g * slices + warp][j * 32 + lane];
       }
     }
-    if (work && group == 0) write_row<T, V>(a, static_cast<uint64_t>(own), slice, lane, sum);
+    if (work && group == 0) write_row<T, V, kLane>(a, static_cast<uint64_t>(own), slice, lane, sum);
   }
 }
 
@@ -354,17 +358,22 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t n, u
 
 // A warp's share of a token that several pieces have: slot 0 of its piece where it
 // has come from the piece before, else slot 1.
-template <int V>
+template <int V, int L>
 __device__ __forceinline__ void leave_share(const EmbedGradCall& a, const Sum& s, uint32_t piece, uint32_t slice,
-                                            uint32_t lane, bool came, const float (&sum)[kLane]) {
+                                            uint32_t lane, bool came, const float (&sum)[L]) {
   float* to = s.shares + (static_cast<uint64_t>(piece) * 2 + (came ? 0 : 1)) * a.d;
 #pragma unroll
-  for (int k = 0; k < kLane / V; ++k)
+  for (int k = 0; k < L / V; ++k) {
+    const uint32_t c = column<V, L>(slice, k, lane);
+    if (c < a.d) {
+      float f[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const uint32_t c = column<V>(slice, k, lane) + j;
-      if (c < a.d) to[c] = sum[k * V + j];
+      for (int j = 0; j < V; ++j) f[j] = sum[k * V + j];
+      Vec<float, V> x;
+      x.round(f);
+      x.store(to + c);
     }
+  }
 }
 
 // The pieces that begin with the token from piece q + 1 on, or (back) those before q that
@@ -382,33 +391,32 @@ __device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t token, uint32_
   }
 }
 
-// Where a token's shares are all there with this warp's: their sum, in order of the pieces.
-template <typename T, int V>
+// Where a token's shares are all there with this warp's: their sum, in order of the
+// pieces. (Lane 0 has made the warp's shares visible.)
+template <typename T, int V, int L>
 __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s, uint32_t token, uint32_t piece,
-                                         uint32_t slice, uint32_t lane, bool came, bool on) {
+                                            uint32_t slice, uint32_t lane, bool came, bool on) {
   const uint32_t before = came ? run_of(s, token, piece, lane, true) : 0u;
   const uint32_t after = on ? run_of(s, token, piece, lane, false) : 0u;
   const uint32_t first = piece - before, shares = before + 1 + after;
   uint32_t had = 0;
-  __syncwarp();
   if (lane == 0) {
-    __threadfence();
     had = atomicAdd(s.arrived + static_cast<uint64_t>(first) * s.slices + slice, 1u);
     __threadfence();
   }
   if (__shfl_sync(0xffffffffu, had, 0) + 1 != shares) return;
-  float sum[kLane] = {};
-  constexpr uint32_t kAhead = 4;  // shares on their way
+  float sum[L] = {};
+  constexpr uint32_t kAhead = L == kLane ? 4 : 2;  // shares on their way
   for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {
-    float x[kAhead][kLane];
+    float x[kAhead][L];
 #pragma unroll
     for (uint32_t q = 0; q < kAhead; ++q) {
       const float* from = s.shares + (static_cast<uint64_t>(first + q0 + q) * 2 + (q0 + q == 0 ? 1 : 0)) * a.d;
 #pragma unroll
-      for (int k = 0; k < kLane / V; ++k)
+      for (int k = 0; k < L / V; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const uint32_t c = column<V>(slice, k, lane) + j;
+          const uint32_t c = column<V, L>(slice, k, lane) + j;
           x[q][k * V + j] = q0 + q < shares && c < a.d ? __ldcg(from + c) : 0.0f;
         }
     }
@@ -416,81 +424,83 @@ __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s
     for (uint32_t q = 0; q < kAhead; ++q)
       if (q0 + q < shares)
 #pragma unroll
-        for (int j = 0; j < kLane; ++j) sum[j] += x[q][j];
+        for (int j = 0; j < L; ++j) sum[j] += x[q][j];
   }
-  write_row<T, V>(a, token, slice, lane, sum);
+  write_row<T, V, L>(a, token, slice, lane, sum);
 }
 
-template <typename D, typename T, int V>
-__global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedGradCall a, const Sum s) {
+template <typename D, typename T, int V, int L>
+__global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGradCall a, const Sum s) {
+  __shared__ uint32_t room[kSumWarps][2][kPieceMost];
   griddep_wait();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const uint32_t sum_ctas = (s.warps + 7) / 8;
+  const uint32_t sum_ctas = (s.warps + kSumWarps - 1) / kSumWarps;
   if (blockIdx.x >= sum_ctas) {  // zeros, where a row's token does not occur
     const uint64_t lo = static_cast<uint64_t>(blockIdx.x - sum_ctas) * s.rows;
     const uint64_t hi = min(lo + s.rows, static_cast<uint64_t>(a.v));
-    for (uint64_t r = lo + warp * 32; r < hi; r += 256) {
-      bool absent = false;
-      if (r + lane < hi) {
-        const uint32_t row = static_cast<uint32_t>(r) + lane, at = first_of(s.key, a.n, row);
-        absent = at == a.n || __ldg(s.key + at) != row;
-      }
-      uint32_t m = __ballot_sync(0xffffffffu, absent);
-      while (m) {
-        zero_row<T>(a, r + __ffs(m) - 1, lane);
-        m &= m - 1;
-      }
+    __shared__ uint8_t occurs[kZeroRows];
+    if (lo + threadIdx.x < hi && threadIdx.x < kZeroRows) {
+      const uint32_t row = static_cast<uint32_t>(lo) + threadIdx.x, at = first_of(s.key, a.n, row);
+      occurs[threadIdx.x] = at < a.n && __ldg(s.key + at) == row;
     }
+    __syncthreads();
+    for (uint64_t r = lo + warp; r < hi; r += kSumWarps)
+      if (!occurs[r - lo]) zero_row<T>(a, r, lane);
     return;
   }
-  constexpr int kAhead = V > 2 ? 8 : 4;  // rows on their way
-  const uint32_t item = blockIdx.x * 8 + warp;
+  const uint32_t item = blockIdx.x * kSumWarps + warp;
   if (item >= s.warps) return;
   const uint32_t slice = item % s.slices, piece = item / s.slices;
-  const uint32_t lo = piece * s.piece, hi = min(lo + s.piece, a.n);
-  float sum[kLane] = {};
-  uint32_t token = __ldg(s.key + lo);
-  bool goes_on = lo > 0 && __ldg(s.key + lo - 1) == token;  // from the piece before
-  auto flush = [&](bool on) {  // `on`: the token goes on in the next piece
-    if (token < a.v) {
-      if (goes_on || on) {
-        leave_share<V>(a, s, piece, slice, lane, goes_on, sum);
-        join_shares<T, V>(a, s, token, piece, slice, lane, goes_on, on);
-      } else {
-        write_row<T, V>(a, token, slice, lane, sum);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) sum[j] = 0.0f;
-    goes_on = false;
-  };
-  for (uint32_t base = lo; base < hi; base += 32) {
-    const uint32_t count = min(32u, hi - base);
-    const uint32_t my_key = lane < count ? __ldg(s.key + base + lane) : 0u;
-    const uint32_t my_pos = lane < count ? __ldg(s.pos + base + lane) : 0u;
-    for (uint32_t e = 0; e < count; e += kAhead) {
-      RowPart<D, V> row[kAhead];
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
-        const uint32_t pos = __shfl_sync(0xffffffffu, my_pos, (e + q) & 31u);
-        if (e + q < count && key < a.v)
-          row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(pos) * a.ld_dout, slice, lane, a.d);
-      }
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const uint32_t key = __shfl_sync(0xffffffffu, my_key, (e + q) & 31u);
-        if (e + q < count) {
-          if (key != token) {
-            flush(false);
-            token = key;
-          }
-          if (key < a.v) row[q].add_to(sum);
-        }
-      }
-    }
+  const uint32_t lo = piece * s.piece, count = min(s.piece, a.n - lo);
+  uint32_t *keys = room[warp][0], *at = room[warp][1];
+  for (uint32_t i = lane; i < count; i += 32) {
+    keys[i] = __ldg(s.key + lo + i);
+    at[i] = __ldg(s.pos + lo + i);
   }
-  flush(hi < a.n && __ldg(s.key + hi) == token);
+  const uint32_t last = lo > 0 ? __ldg(s.key + lo - 1) : a.v, next = lo + count < a.n ? __ldg(s.key + lo + count) : a.v;
+  __syncwarp();
+  constexpr uint32_t kAhead = L == kLane ? (sizeof(D) == 2 && V > 2 ? 8 : 4) : (sizeof(D) == 2 ? kAheadMany : kAheadMany / 2);  // rows on their way
+  RowPart<D, V, L> rows[kAhead];
+  auto load = [&](RowPart<D, V, L> (&row)[kAhead], uint32_t i0) {
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; ++q)
+      if (i0 + q < count && keys[i0 + q] < a.v)
+        row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(at[i0 + q]) * a.ld_dout, slice, lane, a.d);
+  };
+  float sum[L] = {};
+  const uint32_t first = keys[0];
+  const bool came = first < a.v && last == first;  // the first token has come from the piece before
+  uint32_t token = first;
+  bool shared = came;                              // so its sum is a share
+  auto add = [&](const RowPart<D, V, L> (&row)[kAhead], uint32_t i0) {
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; ++q) {
+      if (i0 + q < count) {
+        const uint32_t key = keys[i0 + q];
+        if (key != token) {
+          if (shared) leave_share<V, L>(a, s, piece, slice, lane, true, sum);
+          else if (token < a.v) write_row<T, V, L>(a, token, slice, lane, sum);
+          token = key;
+          shared = false;
+#pragma unroll
+          for (int j = 0; j < L; ++j) sum[j] = 0.0f;
+        }
+        if (key < a.v) row[q].add_to(sum);
+      }
+    }
+  };
+  for (uint32_t i = 0; i < count; i += kAhead) {
+    load(rows, i);
+    add(rows, i);
+  }
+  const bool on = token < a.v && next == token;  // the last token goes on in the next piece
+  if (shared || on) leave_share<V, L>(a, s, piece, slice, lane, shared, sum);
+  else if (token < a.v) write_row<T, V, L>(a, token, slice, lane, sum);
+  if (!came && !on) return;
+  __syncwarp();
+  if (lane == 0) __threadfence();
+  if (came) join_shares<T, V, L>(a, s, first, piece, slice, lane, true, shared && on);
+  if (on && !shared) join_shares<T, V, L>(a, s, token, piece, slice, lane, false, true);
 }
 
 // ------------------------------------------------------------------ planning
@@ -498,6 +508,7 @@ struct Plan {
   bool few;
   uint32_t v;       // values per vector
   uint32_t rounds;  // positions that a sorting thread ranks at a time
+  uint32_t lane;    // columns that a summing lane takes
   Sort sort;
   Sum sum;
   size_t hist, key, shares, bytes;  // sizes, in bytes
@@ -518,6 +529,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
   p.sum.rows = std::max(8u, std::min((c.v + 4 * sms - 1) / (4 * sms), kRowsCta));
   if (p.few) return p;
+  p.sum.rows = kZeroRows;
   Sort& s = p.sort;
   uint32_t bits = 1;
   while (bits < 31 && (c.v >> bits) != 0) ++bits;  // of the keys, v itself among them
@@ -530,9 +542,12 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   s.per = ((c.n + kMaxParts - 1) / kMaxParts + tile - 1) / tile * tile;
   s.parts = (c.n + s.per - 1) / s.per;
   Sum& m = p.sum;
-  m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : 128;
+  m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : kPieceMost;
   m.pieces = (c.n + m.piece - 1) / m.piece;
-  m.slices = (c.d + kSlice - 1) / kSlice;
+  p.lane = c.n >= 65536 && p.v >= 4 && c.d > 2 * kSlice ? kLaneMany : kLane;
+  if (p.lane == kLaneMany) m.piece = kPieceMany;
+  m.pieces = (c.n + m.piece - 1) / m.piece;
+  m.slices = (c.d + 32 * p.lane - 1) / (32 * p.lane);
   m.warps = m.pieces * m.slices;
   auto round = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
   p.hist = round(static_cast<size_t>(s.parts) * (4u << s.bits));
@@ -545,7 +560,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
 
 template <typename D, typename T, int V>
 cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
-  const uint32_t zeros = c.add ? 0 : (c.v + p.sum.rows - 1) / p.sum.rows;
+  uint32_t zeros = c.add ? 0 : (c.v + p.sum.rows - 1) / p.sum.rows;
   EmbedGradCall a = c;
   if (p.few) {
     if (c.n + zeros == 0) return cudaSuccess;
@@ -556,8 +571,11 @@ cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   Sum s = p.sum;
   void* params[] = {&a, &s};
   count_launch();
-  return launch_pdl(reinterpret_cast<const void*>(embed_sum_kernel<D, T, V>),
-                    dim3((s.warps + 7) / 8 + zeros), 256, 0, stream, params, false);
+  const void* kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLane>);
+  if constexpr (V >= 4)
+    if (p.lane == kLaneMany) kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLaneMany>);
+  return launch_pdl(kernel,
+                    dim3((s.warps + kSumWarps - 1) / kSumWarps + zeros), 32 * kSumWarps, 0, stream, params, false);
 }
 
 template <typename D, typename T>
