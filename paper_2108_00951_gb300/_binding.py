@@ -482,12 +482,9 @@ _KINDS = {torch.float32: 0, torch.bfloat16: 1}  # ef_grad_type
 
 # These entries' calls are on the path of single tokens and small layers, where a
 # kernel takes 2 us: a tensor's checks are a handful of attribute reads in one
-# expression, and what does not pass them goes to a function that says why. Measured
-# on the Grace host of a GB300, us a call with its kernel: ef_layer_norm 7.9 -> 5.9,
-# ef_embed 7.2 -> 5.6.
-def _here():
-    """The current device: what these entries' tensors must be on."""
-    return torch.cuda.current_device() if _current_device is None else _current_device()
+# expression, and what does not pass them goes to a function that says why.
+# (_here: the current device, which these entries' tensors must be on.)
+_here = torch.cuda.current_device if _current_device is None else _current_device
 
 
 def _on_device(t, name, dev):
@@ -531,12 +528,8 @@ def _vector(t, name, dtype, numel, dev):
     return _dev(t, name, dtype, numel)
 
 
-def _shape(t, name):
-    try:
-        n, d = shape = t.shape
-        return n, d, shape
-    except (AttributeError, ValueError):
-        raise TypeError("%s must be a matrix" % name) from None
+def _no_matrix(name):
+    return TypeError("%s must be a matrix" % name)
 
 
 def _tokens(t, n, dev):
@@ -560,14 +553,19 @@ def ef_embed(table, token, out, scale=1.0, stream=None):
     """
     lib = _lib or load_library()
     dev = _here()
-    v, d, of_table = _shape(table, "table")
-    n, width, of_out = _shape(out, "out")
+    try:
+        v, d = of_table = table.shape
+        n, width = of_out = out.shape
+    except (AttributeError, ValueError):
+        raise _no_matrix("table and out") from None
     if width != d:
         raise ValueError("table and out differ in width")
     at, ld, kind = _matrix(table, "table", of_table, dev)
     to, ld_out, out_kind = _matrix(out, "out", of_out, dev)
-    _check(lib.ef_embed(at, ld, kind, _tokens(token, n, dev), n, v, d, _real(scale), to, ld_out,
-                        out_kind, _stream(stream)), "ef_embed")
+    status = lib.ef_embed(at, ld, kind, _tokens(token, n, dev), n, v, d, _real(scale), to, ld_out,
+                          out_kind, _raw_stream(dev) if stream is None else _stream(stream))
+    if status:
+        _check(status, "ef_embed")
 
 
 def ef_embed_grad(dout, token, dtable_out, scale=1.0, accumulate=False, stream=None):
@@ -577,15 +575,20 @@ def ef_embed_grad(dout, token, dtable_out, scale=1.0, accumulate=False, stream=N
     rows contiguous at any row stride; ``token`` int64 [n]."""
     lib = _lib or load_library()
     dev = _here()
-    n, d, of_dout = _shape(dout, "dout")
-    v, width, of_table = _shape(dtable_out, "dtable_out")
+    try:
+        n, d = of_dout = dout.shape
+        v, width = of_table = dtable_out.shape
+    except (AttributeError, ValueError):
+        raise _no_matrix("dout and dtable_out") from None
     if width != d:
         raise ValueError("dout and dtable_out differ in width")
     at, ld, kind = _matrix(dout, "dout", of_dout, dev)
     to, ld_out, out_kind = _matrix(dtable_out, "dtable_out", of_table, dev)
-    _check(lib.ef_embed_grad(at, ld, kind, _tokens(token, n, dev), n, v, d, _real(scale),
-                             1 if accumulate else 0, to, ld_out, out_kind, _stream(stream)),
-           "ef_embed_grad")
+    status = lib.ef_embed_grad(at, ld, kind, _tokens(token, n, dev), n, v, d, _real(scale),
+                               1 if accumulate else 0, to, ld_out, out_kind,
+                               _raw_stream(dev) if stream is None else _stream(stream))
+    if status:
+        _check(status, "ef_embed_grad")
 
 
 def _weight(t, name, dtype, d, dev):
@@ -605,14 +608,12 @@ def _weight(t, name, dtype, d, dev):
     return _dev(t, name, dtype, d)
 
 
-def _weight_kind(*named):
-    """The dtype of the first weight vector that is given, and its ef_grad_type."""
-    for t, name in named:
-        if t is not None:
-            if not isinstance(t, _Tensor) or t.dtype not in _KINDS:
-                raise TypeError("%s must be a float32 or bfloat16 tensor" % name)
-            return t.dtype, _KINDS[t.dtype]
-    return torch.float32, 0
+def _kind_of(t, name):
+    """The ef_grad_type of a weight vector."""
+    try:
+        return _KINDS[t.dtype]
+    except (AttributeError, KeyError):
+        raise TypeError("%s must be a float32 or bfloat16 tensor" % name) from None
 
 
 def ef_layer_norm(x, y_out, weight=None, bias=None, eps=1e-5, mean_out=None, rstd_out=None,
@@ -623,15 +624,28 @@ def ef_layer_norm(x, y_out, weight=None, bias=None, eps=1e-5, mean_out=None, rst
     gradient, or None."""
     lib = _lib or load_library()
     dev = _here()
-    n, d, shape = _shape(x, "x")
-    dtype, kind = _weight_kind((weight, "weight"), (bias, "bias"))
+    try:
+        n, d = shape = x.shape
+    except (AttributeError, ValueError):
+        raise _no_matrix("x") from None
+    w = b = None
+    kind = 0
+    if weight is not None:
+        kind = _kind_of(weight, "weight")
+        w = _weight(weight, "weight", weight.dtype, d, dev)
+    if bias is not None:
+        if weight is None:
+            kind = _kind_of(bias, "bias")
+        b = _weight(bias, "bias", (bias if weight is None else weight).dtype, d, dev)
     at, ld, x_kind = _matrix(x, "x", shape, dev)
     to, ld_y, y_kind = _matrix(y_out, "y_out", shape, dev)
-    _check(lib.ef_layer_norm(at, ld, x_kind, _weight(weight, "weight", dtype, d, dev),
-                             _weight(bias, "bias", dtype, d, dev), kind, _real(eps), n, d, to, ld_y,
-                             y_kind, _vector(mean_out, "mean_out", torch.float32, n, dev),
-                             _vector(rstd_out, "rstd_out", torch.float32, n, dev), _stream(stream)),
-           "ef_layer_norm")
+    status = lib.ef_layer_norm(
+        at, ld, x_kind, w, b, kind, eps if type(eps) is float else _real(eps), n, d, to, ld_y, y_kind,
+        None if mean_out is None else _vector(mean_out, "mean_out", torch.float32, n, dev),
+        None if rstd_out is None else _vector(rstd_out, "rstd_out", torch.float32, n, dev),
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if status:
+        _check(status, "ef_layer_norm")
 
 
 def ef_layer_norm_grad(x, mean, rstd, dy, dx_out=None, weight=None, dweight_out=None,
@@ -641,9 +655,15 @@ def ef_layer_norm_grad(x, mean, rstd, dy, dx_out=None, weight=None, dweight_out=
     dtype, ``dweight_out`` and ``dbias_out`` [d] of the weight's, each optional."""
     lib = _lib or load_library()
     dev = _here()
-    n, d, shape = _shape(x, "x")
-    dtype, kind = _weight_kind((weight, "weight"), (dweight_out, "dweight_out"),
-                               (dbias_out, "dbias_out"))
+    try:
+        n, d = shape = x.shape
+    except (AttributeError, ValueError):
+        raise _no_matrix("x") from None
+    dtype, kind = None, 0
+    for t, name in ((weight, "weight"), (dweight_out, "dweight_out"), (dbias_out, "dbias_out")):
+        if t is not None:
+            kind, dtype = _kind_of(t, name), t.dtype
+            break
     at, ld, x_kind = _matrix(x, "x", shape, dev)
     dx, ld_dx = None, d
     if dx_out is not None:
@@ -653,11 +673,14 @@ def ef_layer_norm_grad(x, mean, rstd, dy, dx_out=None, weight=None, dweight_out=
     if n and (mean is None or rstd is None):
         raise TypeError("mean and rstd must be CUDA tensors")
     dy_at, ld_dy, dy_kind = _matrix(dy, "dy", shape, dev)
-    _check(lib.ef_layer_norm_grad(
+    status = lib.ef_layer_norm_grad(
         at, ld, x_kind, _weight(weight, "weight", dtype, d, dev), kind,
         _vector(mean, "mean", torch.float32, n, dev), _vector(rstd, "rstd", torch.float32, n, dev),
         dy_at, ld_dy, dy_kind, n, d, dx, ld_dx, _weight(dweight_out, "dweight_out", dtype, d, dev),
-        _weight(dbias_out, "dbias_out", dtype, d, dev), _stream(stream)), "ef_layer_norm_grad")
+        _weight(dbias_out, "dbias_out", dtype, d, dev),
+        _raw_stream(dev) if stream is None else _stream(stream))
+    if status:
+        _check(status, "ef_layer_norm_grad")
 
 
 class TensorList:
@@ -702,6 +725,9 @@ def _list(tensors, name, dtypes, like, dev, sizes=None):
     """A TensorList of one of the dtypes on the device; as long as `like` and of its
     sizes (or of the bytes `sizes` of an array of them)."""
     x = tensors if type(tensors) is TensorList else TensorList(tensors, name)
+    if x.dtype in dtypes and x.device == dev and (
+            like is None or x._sizes == (like._sizes if sizes is None else sizes)):
+        return x
     if not x.tensors:
         if like is None or not like.tensors:
             return x

@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s,
     const uint32_t same = __match_any_sync(0xffffffffu, digit);
     if (digit < bins && (same & lanemask_lt()) == 0u) atomicAdd(&hist[digit], static_cast<uint32_t>(__popc(same)));
   }
+  griddep_launch_dependents();  // (the scatter, which waits for this kernel's end)
   if (bad) atomicOr(s.error, kDevErrBadInput);
   __syncthreads();
   for (uint32_t b = t; b < bins; b += kSortThreads) s.hist[blockIdx.x * bins + b] = hist[b];
@@ -288,6 +289,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
     for (uint32_t w = 0; w < warp; ++w) under += sums[w];
     if (t < bins) base[t] = under + scan - all + before;
   }
+  griddep_launch_dependents();
   const uint32_t lo = blockIdx.x * s.per, hi = min(lo + s.per, s.n);
   for (uint32_t tile = lo; tile < hi; tile += kSortTile) {
     for (uint32_t i = t; i < kWarps * kMaxBins / 8; i += kSortThreads)
