@@ -596,8 +596,8 @@ ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type
  *                    must not overlap an input.
  *
  * Sums are fp32, in an order that n, v, d and the tokens fix, rounded once.
- * Scratch above 2048 tokens: 16 bytes a token, a fp32 row of d for each 16
- * tokens (each 64 from 65,536 tokens on), and at most 2.4 MB.
+ * Scratch above 2048 tokens: 16 bytes a token, a fp32 row of d for each 8 tokens
+ * (16 from 16,385 on, 64 from 65,536 on), and at most 3 MB beside.
  */
 ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
                         const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,
@@ -618,8 +618,9 @@ ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_ty
  *   mean_out, rstd_out [out] fp32[n] for ef_layer_norm_grad, each may be NULL.
  *   No output may overlap an input or another.
  *
- * Both sums are fp32, the second over differences from the mean. A NaN or an
- * infinity makes its row NaN. No scratch; may be captured at any time.
+ * Both sums are fp32, the second over differences from the mean (whose squares,
+ * and the sum of them, have to be in fp32's range). A NaN or an infinity makes its
+ * row NaN. No scratch; may be captured at any time.
  */
 ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
                         const void* bias, ef_grad_type w_type, float eps, uint64_t n, uint64_t d,
@@ -640,8 +641,9 @@ ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const 
  *   No output may overlap an input or another.
  *
  * Sums are fp32, those over rows by CTAs and then over the CTAs in order.
- * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA, of which
- * there are at most four an SM (1216 shares of longer rows than 28,000).
+ * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA, of which there
+ * are at most eight an SM (rows of more than 28,000 columns: at most one for each 16
+ * rows, and at most 8 an SM for all columns).
  */
 ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
                              ef_grad_type w_type, const float* mean, const float* rstd,
@@ -667,7 +669,8 @@ ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, c
  *                    States in 8 bits start as zeros in codes and exponents.
  *   copies     [out] DEVICE pointers, bf16[numel]: p rounded (for the next step's
  *                    products), or NULL.
- *   lr, eps, weight_decay finite, eps at least 0; beta1, beta2 in [0, 1).
+ *   lr, eps, weight_decay finite, eps 0 or a normal positive number of fp32; beta1,
+ *                    beta2 in [0, 1).
  *   step       the step's number, from 1 on.
  *   seed       of the rounding of 8-bit states; unused without them.
  *   lr_dev, step_dev, grad_scale [in] one fp32, int64, fp32 in device memory, or

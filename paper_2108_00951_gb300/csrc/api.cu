@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <array>
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <map>
@@ -744,8 +745,8 @@ ef_status adamw_entry(uint32_t n, const uint64_t* numel, float* const* p, const 
                       ef_grad_type g_type, void* const* m, void* const* v, uint8_t* const* me,
                       uint8_t* const* ve, uint16_t* const* copy, AdamCall c, cudaStream_t stream) {
   if (n > kMaxTensors || !grad_type_ok(g_type) || !std::isfinite(c.lr) || !std::isfinite(c.decay) ||
-      !(c.b1 >= 0.0 && c.b1 < 1.0) || !(c.b2 >= 0.0 && c.b2 < 1.0) || !(c.eps >= 0.0) ||
-      !std::isfinite(c.eps) || (c.step == 0 && !c.step_dev) || !aligned(c.lr_dev, 4) ||
+      !(c.b1 >= 0.0 && c.b1 < 1.0) || !(c.b2 >= 0.0 && c.b2 < 1.0) || !std::isfinite(c.eps) ||
+      !(c.eps == 0.0 || c.eps >= FLT_MIN) || (c.step == 0 && !c.step_dev) || !aligned(c.lr_dev, 4) ||
       !aligned(c.step_dev, 8) || !aligned(c.grad_scale, 4) || (me == nullptr) != (ve == nullptr))
     return EF_ERR_INVALID_ARG;
   if (n == 0) return EF_OK;

@@ -406,7 +406,9 @@ __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s
     had = atomicAdd(s.arrived + static_cast<uint64_t>(first) * s.slices + slice, 1u);
     __threadfence();
   }
-  if (__shfl_sync(0xffffffffu, had, 0) + 1 != shares) return;
+  had = __shfl_sync(0xffffffffu, had, 0);
+  if (had + 1 != shares) return;
+  __syncwarp();  // (lane 0 has seen the others' shares, and so have all)
   float sum[L] = {};
   constexpr uint32_t kAhead = L == kLane ? 4 : 2;  // shares on their way
   for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {

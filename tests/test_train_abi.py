@@ -82,7 +82,7 @@ def adamw(n=2, numel=(100, 300), p=(A, A + 400), g=(B, B + 400), gt=0, m=(C, C +
 
 @pytest.mark.parametrize("kw", [
     dict(n=(1 << 20) + 1), dict(gt=2), dict(lr=NAN), dict(lr=INF), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0),
-    dict(b2=NAN), dict(eps=-1e-9), dict(eps=INF), dict(wd=NAN), dict(step=0), dict(lr_dev=F + 2),
+    dict(b2=NAN), dict(eps=-1e-9), dict(eps=1e-39), dict(eps=INF), dict(wd=NAN), dict(step=0), dict(lr_dev=F + 2),
     dict(step_dev=F + 4), dict(scale=F + 1), dict(numel=None), dict(p=None), dict(g=None), dict(m=None), dict(v=None),
     dict(p=(0, A)), dict(g=(B, 0)), dict(m=(C + 2, C + 400)), dict(copy=(E, 0)), dict(copy=(E + 1, E + 200)),
     dict(g=(B + 1, B + 400), gt=1), dict(me=(F, F + 1)), dict(ve=(F, F + 1)), dict(me=(F, 0), ve=(G, G + 1)),
