@@ -310,8 +310,10 @@ struct NormCall {
   float eps;
   uint32_t n, d;
   bool x_bf16, y_bf16, w_bf16;
-  uint32_t warps;        // (the launcher's: of a row; and whether the weights lie on the
-  bool w_wide, b_wide;   // boundaries of the kernel's vectors)
+  // the launcher's: a row's threads in a CTA, its CTAs, the columns that each of them has;
+  // whether the weights lie on the boundaries of the kernel's vectors
+  uint32_t threads, cluster, part;
+  bool w_wide, b_wide;
 };
 cudaError_t launch_layer_norm(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream);
 struct NormGradCall {
@@ -322,7 +324,7 @@ struct NormGradCall {
   const float *mean, *rstd;  // [n]
   float* shares;         // (the launcher's: [parts][2][d])
   uint64_t ldx, lddy, lddx;
-  uint32_t n, d, warps;  // (warps, w_wide: as above)
+  uint32_t n, d, threads, cluster, part;  // (as above)
   bool x_bf16, y_bf16, w_bf16, w_wide;
 };
 cudaError_t norm_grad_scratch(const NormGradCall& c, const DeviceInfo& dev, size_t* bytes);
@@ -380,9 +382,11 @@ struct AdamStates {
 cudaError_t launch_adamw_states(const AdamStates* t, uint32_t n, bool out_bf16, cudaStream_t stream);
 
 // Launch bookkeeping.
-// CTAs of a kernel that an SM holds, with the kernel opted into that much shared
-// memory on the current device; asked once per kernel, device and size (norm.cu).
-cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t* ctas);
+// CTAs (or clusters of CTAs) of a kernel that the device holds at once, with the kernel
+// opted into that much shared memory on the current device; asked once per kernel,
+// device and size (norm.cu).
+cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t cluster,
+                          const DeviceInfo& info, uint32_t* count);
 // A launch that may begin while the previous kernel on the stream finishes
 // (programmatic dependent launch: the kernel waits for its predecessor with
 // griddepcontrol.wait before reading what it wrote), optionally cooperative.

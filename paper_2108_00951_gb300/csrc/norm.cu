@@ -3,10 +3,11 @@
 //
 // Both sums are fp32 over values that stay in registers, the second after the
 // mean is known (a difference of squares would lose the variance of rows whose
-// mean is large). What bounds it: reading x and writing y once. One to eight warps (rows
-// of up to 8192 values) take rows a stride apart; the next ones are on their way into a
-// ring in shared memory meanwhile, and the weights stay in registers. A longer row is
-// read three times, twice out of L1 and L2.
+// mean is large). What bounds it: reading x and writing y once. A row of up to 256
+// values lies in lanes of a warp, of up to 2048 in warps, of up to 8192 in a CTA, of up to
+// 65,536 in a cluster of CTAs; they take rows a stride apart, the next ones on their way
+// into a ring in shared memory meanwhile, and the weights stay in registers. A
+// longer row is read three times by one CTA, twice out of L2.
 #include <algorithm>
 #include <map>
 #include <mutex>
@@ -21,21 +22,23 @@ namespace {
 template <int E>
 constexpr int kRing = E == 8 ? 8 : 4;
 
-template <typename X, typename Y, int V, int K>
+template <typename X, typename Y, int V, int K, RowKind KIND>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
   constexpr int S = kRing<V * K>;
-  constexpr bool kAll = V * K == 32;  // a CTA has one row at a time
   extern __shared__ __align__(16) char ring[];
-  __shared__ __align__(16) float room[2][16];
-  const RowGroup<kAll> g(a.warps);
-  const uint32_t group = g.threads(), t = g.t;
-  const uint32_t per_cta = kAll ? 1u : blockDim.x / group, groups = gridDim.x * per_cta;
-  const uint32_t first = blockIdx.x * per_cta + g.index;
-  const uint32_t place = row_place(a.d, sizeof(X));
+  __shared__ RowRoom room;
+  const RowGroup<KIND> g(a.threads);
+  const RowPart part = row_part(a.d, a.part, a.cluster);
+  const uint32_t per_cta = KIND == kRowAll ? 1u : blockDim.x / g.threads, t = g.t;
+  const uint32_t groups = gridDim.x / a.cluster * per_cta;
+  const uint32_t first = blockIdx.x / a.cluster * per_cta + g.index;
+  const uint32_t place = row_place(a.part, sizeof(X));
   char* rows = ring + g.index * S * place;
-  auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
+  auto x_row = [&](uint32_t row) {
+    return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx + part.first;
+  };
   auto fetch = [&](uint32_t row, uint32_t slot) {
-    if (row < a.n) fetch_row(rows + slot * place, x_row(row), a.d * sizeof(X), t, group);
+    if (row < a.n) fetch_row(rows + slot * place, x_row(row), part.columns * sizeof(X), t, g.threads);
     fetch_commit();
   };
 #pragma unroll
@@ -43,49 +46,53 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
   float w[K][V], b[K][V];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t c = (k * group + t) * V;
-    if (c < a.d) {
-      load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
-      load_weights<V>(a.b, a.w_bf16, a.b_wide, c, 0.0f, b[k]);
+    const uint32_t c = (k * g.threads + t) * V;
+    if (c < part.columns) {
+      load_weights<V>(a.w, a.w_bf16, a.w_wide, part.first + c, 1.0f, w[k]);
+      load_weights<V>(a.b, a.w_bf16, a.b_wide, part.first + c, 0.0f, b[k]);
     }
   }
   const float inv = 1.0f / static_cast<float>(a.d);
-  uint32_t slot = 0;
-  for (uint32_t row = first; row < a.n; row += groups) {
+  if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
+  uint32_t slot = 0, parity = 0;
+  // (the lanes of a warp go through its rows together: to the last round of the warp's first)
+  const uint32_t ahead = KIND == kRowLanes ? g.index % (32u / g.threads) : 0u;
+  for (uint32_t row = first; row - ahead < a.n; row += groups) {
     fetch_wait<S - 2>();
     g.sync();
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
-    const char* in_row = rows + slot * place + row_lead(x_row(row));
+    const bool in = KIND != kRowLanes || row < a.n;
+    const char* in_row = rows + slot * place + (in ? row_lead(x_row(row)) : 0u);
     slot = slot == S - 1 ? 0 : slot + 1;
     float x[K][V], sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * group + t) * V;
-      if (c < a.d) {
-        const Vec<X, V> in = staged<X, V>(in_row, c);
+      const uint32_t c = (k * g.threads + t) * V;
+      if (in && c < part.columns) {
+        const Vec<X, V> v = staged<X, V>(in_row, c);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum += x[k][j] = in.get(j);
+        for (int j = 0; j < V; ++j) sum += x[k][j] = v.get(j);
       }
     }
-    const float mean = group_sum(g, sum, room[0]) * inv;
+    const float mean = row_sum<KIND, false>(g, sum, 0.0f, room, 0, a.cluster, parity).x * inv;
     sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if ((k * group + t) * V < a.d)
+      if (in && (k * g.threads + t) * V < part.columns)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           x[k][j] -= mean;
           sum = fmaf(x[k][j], x[k][j], sum);
         }
     }
-    const float var = group_sum(g, sum, room[1]) * inv;
+    const float var = row_sum<KIND, false>(g, sum, 0.0f, room, 1, a.cluster, parity).x * inv;
     const float rstd = inverse_root(var + a.eps);
-    Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy;
+    Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy + part.first;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * group + t) * V;
-      if (c < a.d) {
+      const uint32_t c = (k * g.threads + t) * V;
+      if (in && c < part.columns) {
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) out[j] = fmaf(x[k][j] * rstd, w[k][j], b[k][j]);
@@ -94,7 +101,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
         o.store(y + c);
       }
     }
-    if (t == 0) {
+    if (t == 0 && part.first == 0 && in) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
@@ -132,27 +139,25 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
   }
 }
 
-template <typename X, typename Y, int V, int K>
-cudaError_t launch_rows(NormCall c, const DeviceInfo& dev, cudaStream_t stream) {
-  c.warps = row_warps(c.d, V * K);
-  const uint32_t threads = V * K == 32 ? c.warps * 32 : kNormThreads, per_cta = threads / (c.warps * 32);
-  const uint32_t smem = per_cta * kRing<V * K> * row_place(c.d, sizeof(X));
-  const void* fn = reinterpret_cast<const void*>(norm_kernel<X, Y, V, K>);
-  uint32_t per_sm = 0;
-  const cudaError_t err = resident_ctas(fn, threads, smem, &per_sm);
+template <typename X, typename Y, int V, int K, RowKind KIND>
+cudaError_t launch_rows(NormCall c, uint32_t most, const DeviceInfo& dev, cudaStream_t stream) {
+  RowPlan p;
+  plan_row(p, reinterpret_cast<const void*>(norm_kernel<X, Y, V, K, KIND>), KIND, V * K, c.d, most);
+  const cudaError_t err = plan_groups(p, kRing<V * K> * row_place(p.part, sizeof(X)), c.n, dev);
   if (err != cudaSuccess) return err;
-  const uint32_t grid = std::min((c.n + per_cta - 1) / per_cta, per_sm * static_cast<uint32_t>(dev.sm_count));
-  norm_kernel<X, Y, V, K><<<grid, threads, smem, stream>>>(c);
-  return cudaGetLastError();
+  c.threads = p.threads;
+  c.cluster = p.cluster;
+  c.part = p.part;
+  return launch_row(p, &c, stream);
 }
 
 template <typename X, typename Y, int V>
 cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
   // Values of a row that a thread holds: fewer warps a row add up and wait less
   // (32,768 x 4096: 16 a thread 126 us, 32 81), more have more rows at once
-  if (c.d <= 256) return launch_rows<X, Y, V, 8 / V>(c, dev, stream);
-  if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V>(c, dev, stream);
-  return launch_rows<X, Y, V, 32 / V>(c, dev, stream);
+  if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, stream);
+  if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, stream);
+  return launch_rows<X, Y, V, 32 / V, kRowAll>(c, 32 * kNormThreads, dev, stream);
 }
 
 template <typename X, typename Y>
@@ -161,54 +166,73 @@ cudaError_t launch_typed(NormCall c, const DeviceInfo& dev, cudaStream_t stream)
     norm_long_kernel<X, Y><<<c.n, 1024, 0, stream>>>(c);
     return cudaGetLastError();
   }
-  constexpr uint32_t kWide = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
+  constexpr bool kBoth16 = sizeof(X) == 2 && sizeof(Y) == 2;
   auto allow = [&](uint32_t v) {
     return c.d % v == 0 && rows_allow(c.x, c.n > 1 ? c.ldx : 0, sizeof(X), v) &&
            rows_allow(c.y, c.n > 1 ? c.ldy : 0, sizeof(Y), v);
   };
-  const uint32_t v = allow(kWide) ? kWide : allow(2) ? 2 : 1;
+  const uint32_t v = kBoth16 && allow(8) ? 8 : allow(4) ? 4 : allow(2) ? 2 : 1;
   const uint64_t wsize = c.w_bf16 ? 2 : 4;
-  const uint32_t part = c.w_bf16 ? v : std::min(v, 4u);
-  c.w_wide = rows_allow(c.w, 0, wsize, part);
-  c.b_wide = rows_allow(c.b, 0, wsize, part);
-  if (v == kWide) return launch<X, Y, kWide>(c, dev, stream);
+  const uint32_t vec = c.w_bf16 ? v : std::min(v, 4u);
+  c.w_wide = rows_allow(c.w, 0, wsize, vec);
+  c.b_wide = rows_allow(c.b, 0, wsize, vec);
+  if constexpr (kBoth16)
+    if (v == 8) return launch<X, Y, 8>(c, dev, stream);
+  if (v == 4) return launch<X, Y, 4>(c, dev, stream);
   return v == 2 ? launch<X, Y, 2>(c, dev, stream) : launch<X, Y, 1>(c, dev, stream);
 }
 
 }  // namespace
 
-cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t* ctas) {
+cudaError_t resident_ctas(const void* kernel, uint32_t threads, uint32_t smem, uint32_t cluster,
+                          const DeviceInfo& info, uint32_t* count) {
+  using Key = std::tuple<int, const void*, uint32_t, uint32_t, uint32_t>;
   static std::mutex mu;
-  static std::map<std::tuple<int, const void*, uint32_t, uint32_t>, uint32_t> known;
+  static std::map<Key, uint32_t> known;
   struct Last {  // what a thread asked for last, by kernel
-    const void* kernel;
-    int dev;
-    uint32_t threads, smem, ctas;
+    Key key;
+    uint32_t count;
   };
   static thread_local Last last[16] = {};
   int dev = 0, n = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
+  const Key key(dev, kernel, threads, smem, cluster);
   Last& l = last[(reinterpret_cast<uintptr_t>(kernel) >> 4) % 16];
-  if (l.kernel == kernel && l.dev == dev && l.threads == threads && l.smem == smem) {
-    *ctas = l.ctas;
+  if (l.count && l.key == key) {
+    *count = l.count;
     return cudaSuccess;
   }
   std::lock_guard<std::mutex> lk(mu);
-  const auto key = std::make_tuple(dev, kernel, threads, smem);
   const auto it = known.find(key);
   if (it != known.end()) {
-    *ctas = it->second;
-    l = {kernel, dev, threads, smem, it->second};
+    *count = it->second;
+    l = {key, it->second};
     return cudaSuccess;
   }
   // (an opt-in stays: the largest asked for, whatever order sizes come in)
   err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-  if (err == cudaSuccess) err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem);
+  if (err != cudaSuccess) return err;
+  if (cluster == 1) {
+    err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem);
+    n *= info.sm_count;
+  } else {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster * static_cast<uint32_t>(info.sm_count));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    err = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+  }
   if (err != cudaSuccess) return err;
   if (n < 1) return cudaErrorLaunchOutOfResources;
   known.emplace(key, static_cast<uint32_t>(n));
-  *ctas = static_cast<uint32_t>(n);
+  *count = static_cast<uint32_t>(n);
   return cudaSuccess;
 }
 

@@ -1,38 +1,53 @@
-// norm.cuh — what layer norm's forward and backward kernels share: rows that come
-// through a ring in shared memory, their columns over the lanes of a warp or the
-// threads of a CTA, the weights, sums.
+// norm.cuh — what layer norm's forward and backward kernels share: a row's columns
+// over lanes, warps, a CTA or a cluster; the weights; sums.
 #pragma once
+
+#include <algorithm>
 
 #include "internal.h"
 #include "row_ring.cuh"
+#include "tensor.cuh"
 
 namespace efs {
 
-constexpr uint32_t kNormThreads = 256;    // of a CTA that has several rows at once
-constexpr uint32_t kNormRowWidth = 8192;  // longest row that threads hold
+constexpr uint32_t kNormThreads = 256;      // of a CTA, at most
+constexpr uint32_t kNormCluster = 8;        // CTAs that have a row together, at most
+constexpr uint32_t kNormRowWidth = 65536;   // longest row that threads hold
 
-// The threads that have a row together: 1, 2, 4 or 8 warps of a CTA, with which no
-// other threads of the CTA wait. ALL: the whole CTA.
-template <bool ALL>
+// The threads of a CTA that have a row (or a CTA's part of one) together, with which no
+// others wait: 1 to 32 lanes of a warp, a number of whole warps, or all.
+enum RowKind { kRowLanes, kRowWarps, kRowAll };
+template <RowKind KIND>
 struct RowGroup {
-  uint32_t warps, index, t;  // warps of the group, its number in the CTA, this thread's in the group
+  uint32_t threads, index, t;  // how many, the group's number in the CTA, this thread's in the group
   __device__ __forceinline__ explicit RowGroup(uint32_t of_row) {
-    warps = ALL ? blockDim.x >> 5 : of_row;
-    index = ALL ? 0u : threadIdx.x / (warps * 32u);
-    t = threadIdx.x - index * warps * 32u;
+    threads = KIND == kRowAll ? blockDim.x : of_row;
+    index = KIND == kRowAll ? 0u : threadIdx.x / threads;
+    t = threadIdx.x - index * threads;
   }
-  __device__ __forceinline__ uint32_t threads() const { return warps * 32u; }
   __device__ __forceinline__ void sync() const {
-    if (ALL) __syncthreads();
-    else if (warps == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(index + 1u), "r"(warps * 32u) : "memory");
+    if (KIND == kRowAll) __syncthreads();
+    else if (KIND == kRowLanes || threads == 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(index + 1u), "r"(threads) : "memory");
   }
 };
-// Warps for rows of d values with `per` a thread: a power of two.
-inline uint32_t row_warps(uint32_t d, uint32_t per) {
-  uint32_t warps = 1;
-  while (warps * 32 * per < d) warps *= 2;
-  return warps;
+// Threads for `columns` with `values` a thread.
+inline uint32_t row_threads(RowKind kind, uint32_t columns, uint32_t values) {
+  const uint32_t least = (columns + values - 1) / values;
+  if (kind != kRowLanes) return (least + 31) / 32 * 32;
+  uint32_t lanes = 1;
+  while (lanes < least) lanes *= 2;
+  return lanes;
+}
+
+// What the CTAs of a cluster have of a row: `part` columns each.
+struct RowPart {
+  uint32_t first, columns;  // of this CTA
+};
+__device__ __forceinline__ RowPart row_part(uint32_t d, uint32_t part, uint32_t cluster) {
+  if (cluster == 1) return {0u, d};
+  const uint32_t first = blockIdx.x % cluster * part;
+  return {first, min(part, d - first)};
 }
 
 // V values of a weight vector of either type, or `none` where there is no vector.
@@ -71,41 +86,57 @@ __device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide
   }
 }
 
-// Sums over the threads of a group, in a fixed order. `room`: 16 floats of the
-// CTA's a sum, which no other sum uses before the group's next barrier but one.
-template <bool ALL>
-__device__ __forceinline__ float group_sum(const RowGroup<ALL>& g, float a, float* room) {
-  a = warp_sum(a);
-  if (g.warps == 1) return a;
-  if ((threadIdx.x & 31u) == 0) room[threadIdx.x >> 5] = a;
-  g.sync();
-  const float* mine = room + g.index * g.warps;
-  a = 0.0f;
-  for (uint32_t i = 0; i < g.warps; i += 2) {
-    const float2 x = *reinterpret_cast<const float2*>(mine + i);
-    a += x.x + x.y;
+// The sum of a value (or of TWO) over a row's threads, in a fixed order, across the CTAs of a
+// cluster too. `Room` lies in shared memory; no sum writes what a thread may still read
+// of the one before, as long as the group meets between two rows.
+struct __align__(16) RowRoom {
+  float2 warp[2][kNormThreads / 32];       // by the sum's number in the row
+  float2 peer[2][kNormCluster];            // by the parity of the cluster's sums
+};
+template <RowKind KIND, bool TWO>
+__device__ __forceinline__ float2 row_sum(const RowGroup<KIND>& g, float a, float b, RowRoom& room, uint32_t which,
+                                          uint32_t cluster, uint32_t& parity) {
+  if (KIND == kRowLanes) {
+    for (uint32_t o = g.threads >> 1; o > 0; o >>= 1) {
+      a += __shfl_xor_sync(0xffffffffu, a, o);
+      if (TWO) b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    return make_float2(a, b);
   }
-  return a;
-}
-// Two of them; `room`: 32 floats.
-template <bool ALL>
-__device__ __forceinline__ float2 group_sum2(const RowGroup<ALL>& g, float a, float b, float* room) {
   a = warp_sum(a);
-  b = warp_sum(b);
-  if (g.warps == 1) return make_float2(a, b);
-  if ((threadIdx.x & 31u) == 0) *reinterpret_cast<float2*>(room + 2 * (threadIdx.x >> 5)) = make_float2(a, b);
-  g.sync();
-  const float* mine = room + 2 * g.index * g.warps;
-  a = b = 0.0f;
-  for (uint32_t i = 0; i < 2 * g.warps; i += 4) {
-    const float4 x = *reinterpret_cast<const float4*>(mine + i);
-    a += x.x + x.z;
-    b += x.y + x.w;
+  if (TWO) b = warp_sum(b);
+  if (KIND == kRowAll || g.threads > 32) {
+    const uint32_t warps = g.threads >> 5;
+    float2* mine = room.warp[which] + g.index * warps;
+    if ((threadIdx.x & 31u) == 0) mine[g.t >> 5] = make_float2(a, b);
+    g.sync();
+    a = b = 0.0f;
+#pragma unroll 4
+    for (uint32_t i = 0; i < warps; ++i) {
+      const float2 x = mine[i];
+      a += x.x;
+      if (TWO) b += x.y;
+    }
+  }
+  if (KIND == kRowAll && cluster > 1) {
+    if (threadIdx.x < cluster)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(
+                       cluster_addr(&room.peer[parity][blockIdx.x % cluster], threadIdx.x)),
+                   "f"(a), "f"(b)
+                   : "memory");
+    cluster_sync();
+    a = b = 0.0f;
+    for (uint32_t i = 0; i < cluster; ++i) {
+      const float2 x = room.peer[parity][i];
+      a += x.x;
+      if (TWO) b += x.y;
+    }
+    parity ^= 1u;
   }
   return make_float2(a, b);
 }
 
-// The same over a CTA (of rows that no group's registers hold).
+// The same over a CTA (of rows that no threads hold).
 __device__ __forceinline__ float2 cta_sum2(float a, float b, float* room) {
   a = warp_sum(a);
   b = warp_sum(b);
@@ -129,6 +160,50 @@ __device__ __forceinline__ float inverse_root(float x) {
 // and stride (in bytes) and the width are multiples of.
 inline bool rows_allow(const void* at, uint64_t ld, uint64_t size, uint32_t v) {
   return (reinterpret_cast<uintptr_t>(at) | ld * size) % (size * v) == 0;
+}
+
+// How the rows of a call are spread.
+struct RowPlan {
+  const void* kernel;
+  uint32_t threads;   // of a row in a CTA
+  uint32_t cluster;   // CTAs of a row
+  uint32_t part;      // columns of a row in a CTA
+  uint32_t per_cta;   // rows that a CTA has at once
+  uint32_t groups;    // rows that are had at once
+  uint32_t smem;
+};
+// `values`: of a row in a thread; `most`: columns in a CTA.
+inline void plan_row(RowPlan& p, const void* kernel, RowKind kind, uint32_t values, uint32_t d, uint32_t most) {
+  p.kernel = kernel;
+  p.cluster = (d + most - 1) / most;
+  p.part = p.cluster == 1 ? d : ((d + p.cluster - 1) / p.cluster + 15) / 16 * 16;
+  p.threads = row_threads(kind, p.part, values);
+  p.per_cta = kind == kRowAll ? 1 : kNormThreads / p.threads;
+}
+// `ring`: bytes of shared memory of a row's threads.
+inline cudaError_t plan_groups(RowPlan& p, uint32_t ring, uint32_t n, const DeviceInfo& dev) {
+  p.smem = p.per_cta * ring;
+  uint32_t resident = 0;
+  const cudaError_t err = resident_ctas(p.kernel, p.per_cta * p.threads, p.smem, p.cluster, dev, &resident);
+  p.groups = std::min((n + p.per_cta - 1) / p.per_cta, resident);
+  return err;
+}
+inline cudaError_t launch_row(const RowPlan& p, void* params, cudaStream_t stream) {
+  void* args[] = {params};
+  const dim3 grid(p.groups * p.cluster), block(p.per_cta * p.threads);
+  if (p.cluster == 1) return cudaLaunchKernel(p.kernel, grid, block, args, p.smem, stream);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = p.smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = p.cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelExC(&cfg, p.kernel, args);
 }
 
 }  // namespace efs

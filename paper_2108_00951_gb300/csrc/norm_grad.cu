@@ -4,11 +4,11 @@
 //   dx = rstd (q - sum q / d - x' sum(q x') / d),
 //   dw = sum over rows of dy x',   db = sum over rows of dy.
 //
-// What bounds it: reading x and dy and writing dx once. One to eight warps (rows of up to
-// 8192 values) take rows a stride apart, the next ones on their way into a ring in
-// shared memory, and keep their columns' shares of dw and db in registers (in shared
-// memory for longer rows); the CTAs' shares are joined by a second kernel in the order
-// of the CTAs, so equal inputs give equal bits.
+// What bounds it: reading x and dy and writing dx once. Rows are spread as in the
+// forward pass (norm.cu), the next ones on their way into a ring in shared memory; a
+// row's threads keep their columns' shares of dw and db in registers (of rows
+// beyond 65,536 values a kernel of its own adds them up), and a second kernel joins
+// the CTAs' shares in the order of the CTAs, so equal inputs give equal bits.
 #include <algorithm>
 
 #include "norm.cuh"
@@ -40,25 +40,28 @@ __device__ __forceinline__ void write_share(const NormGradCall& a, uint32_t shar
   }
 }
 
-// Rows of at most K V times the threads of a group.
-template <typename X, typename Y, int V, int K, bool ALL>
-__global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormThreads, ALL && V * K == 16 ? 2 : 1)
-    norm_grad_kernel(const NormGradCall a) {
+template <typename X, typename Y, int V, int K, RowKind KIND>
+__global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_kernel(const NormGradCall a) {
   constexpr int S = kRing<V * K>;
   extern __shared__ __align__(16) char ring[];
-  __shared__ __align__(16) float room[32];
-  const RowGroup<ALL> of(a.warps);
-  const uint32_t group = of.threads(), t = of.t;
-  const uint32_t per_cta = ALL ? 1u : blockDim.x / group, groups = gridDim.x * per_cta;
-  const uint32_t first = blockIdx.x * per_cta + of.index;
-  const uint32_t x_place = row_place(a.d, sizeof(X)), place = x_place + row_place(a.d, sizeof(Y));
+  __shared__ RowRoom room;
+  const RowGroup<KIND> of(a.threads);
+  const RowPart part = row_part(a.d, a.part, a.cluster);
+  const uint32_t per_cta = KIND == kRowAll ? 1u : blockDim.x / of.threads, t = of.t;
+  const uint32_t parts = gridDim.x / a.cluster, share = blockIdx.x / a.cluster;
+  const uint32_t groups = parts * per_cta, first = share * per_cta + of.index;
+  const uint32_t x_place = row_place(a.part, sizeof(X)), place = x_place + row_place(a.part, sizeof(Y));
   char* rows = ring + of.index * S * place;
-  auto x_row = [&](uint32_t row) { return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx; };
-  auto dy_row = [&](uint32_t row) { return static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy; };
+  auto x_row = [&](uint32_t row) {
+    return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx + part.first;
+  };
+  auto dy_row = [&](uint32_t row) {
+    return static_cast<const Y*>(a.dy) + static_cast<uint64_t>(row) * a.lddy + part.first;
+  };
   auto fetch = [&](uint32_t row, uint32_t slot) {
     if (row < a.n) {
-      fetch_row(rows + slot * place, x_row(row), a.d * sizeof(X), t, group);
-      fetch_row(rows + slot * place + x_place, dy_row(row), a.d * sizeof(Y), t, group);
+      fetch_row(rows + slot * place, x_row(row), part.columns * sizeof(X), t, of.threads);
+      fetch_row(rows + slot * place + x_place, dy_row(row), part.columns * sizeof(Y), t, of.threads);
     }
     fetch_commit();
   };
@@ -69,26 +72,30 @@ __global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormTh
   float w[K][V], dw[K][V] = {}, db[K][V] = {};
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t c = (k * group + t) * V;
-    if (c < a.d) load_weights<V>(a.w, a.w_bf16, a.w_wide, c, 1.0f, w[k]);
+    const uint32_t c = (k * of.threads + t) * V;
+    if (c < part.columns) load_weights<V>(a.w, a.w_bf16, a.w_wide, part.first + c, 1.0f, w[k]);
   }
   const float inv = 1.0f / static_cast<float>(a.d);
-  uint32_t slot = 0;
-  for (uint32_t row = first; row < a.n; row += groups) {
+  if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
+  uint32_t slot = 0, parity = 0;
+  // (the lanes of a warp go through its rows together: to the last round of the warp's first)
+  const uint32_t ahead = KIND == kRowLanes ? of.index % (32u / of.threads) : 0u;
+  for (uint32_t row = first; row - ahead < a.n; row += groups) {
     fetch_wait<S - 2>();
     of.sync();
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const float mu = mean, r = rstd;
     if (row + groups < a.n) mean = __ldg(a.mean + row + groups), rstd = __ldg(a.rstd + row + groups);
-    const char* xs = rows + slot * place + row_lead(x_row(row));
-    const char* dys = rows + slot * place + x_place + row_lead(dy_row(row));
+    const bool in = KIND != kRowLanes || row < a.n;
+    const char* xs = rows + slot * place + (in ? row_lead(x_row(row)) : 0u);
+    const char* dys = rows + slot * place + x_place + (in ? row_lead(dy_row(row)) : 0u);
     slot = slot == S - 1 ? 0 : slot + 1;
     float hat[K][V], q[K][V], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * group + t) * V;
-      if (c < a.d) {
+      const uint32_t c = (k * of.threads + t) * V;
+      if (in && c < part.columns) {
         const Vec<X, V> x = staged<X, V>(xs, c);
         const Vec<Y, V> dy = staged<Y, V>(dys, c);
 #pragma unroll
@@ -104,13 +111,13 @@ __global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormTh
       }
     }
     if (!a.dx) continue;
-    const float2 s = group_sum2(of, s1, s2, room);
+    const float2 s = row_sum<KIND, true>(of, s1, s2, room, 0, a.cluster, parity);
     const float m1 = s.x * inv, m2 = s.y * inv;
-    X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
+    X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx + part.first;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * group + t) * V;
-      if (c < a.d) {
+      const uint32_t c = (k * of.threads + t) * V;
+      if (in && c < part.columns) {
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) out[j] = r * fmaf(-m2, hat[k][j], q[k][j] - m1);
@@ -127,8 +134,8 @@ __global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormTh
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const uint32_t c = (k * group + t) * V + j;
-        if (c < a.d) write_share(a, blockIdx.x, gridDim.x, c, dw[k][j], db[k][j]);
+        const uint32_t c = (k * of.threads + t) * V + j;
+        if (c < part.columns) write_share(a, share, parts, part.first + c, dw[k][j], db[k][j]);
       }
     return;
   }
@@ -140,7 +147,7 @@ __global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormTh
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const uint32_t c = (k * group + t) * V + j;
+      const uint32_t c = (k * of.threads + t) * V + j;
       if (c < a.d) {
         shares[of.index * a.d + c] = dw[k][j];
         shares[(per_cta + of.index) * a.d + c] = db[k][j];
@@ -153,20 +160,15 @@ __global__ void __launch_bounds__(ALL || V * K < 16 ? kNormThreads : 2 * kNormTh
       w_sum += shares[q * a.d + c];
       b_sum += shares[(per_cta + q) * a.d + c];
     }
-    write_share(a, blockIdx.x, gridDim.x, c, w_sum, b_sum);
+    write_share(a, share, parts, c, w_sum, b_sum);
   }
 }
 
-// Rows of any length, a CTA each, read twice (the second time out of L2). SHARES:
-// the columns' shares of dw and db lie in shared memory, each the business of
-// one thread.
-template <typename X, typename Y, bool SHARES>
+// dx of rows of any length, a CTA each, read twice (the second time out of L2).
+template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall a) {
-  extern __shared__ float shares[];  // [2][d]
   __shared__ float room[2][64];
   const float inv = 1.0f / static_cast<float>(a.d);
-  if (SHARES)
-    for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) shares[c] = shares[a.d + c] = 0.0f;
   uint32_t parity = 0;
   for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x, parity ^= 1u) {
     const X* x = static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx;
@@ -177,15 +179,10 @@ __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall
     for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
       float w[1];
       load_weights<1>(a.w, a.w_bf16, true, c, 1.0f, w);
-      const float hat = (widen(__ldg(x + c)) - mean) * rstd, g = widen(__ldg(dy + c));
-      s1 = fmaf(g, w[0], s1);
-      s2 = fmaf(g * w[0], hat, s2);
-      if (SHARES) {
-        shares[c] = fmaf(g, hat, shares[c]);
-        shares[a.d + c] += g;
-      }
+      const float hat = (widen(__ldg(x + c)) - mean) * rstd, q = widen(__ldg(dy + c)) * w[0];
+      s1 += q;
+      s2 = fmaf(q, hat, s2);
     }
-    if (!a.dx) continue;
     const float2 s = cta_sum2(s1, s2, room[parity]);
     X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
 #pragma unroll 4
@@ -196,9 +193,6 @@ __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall
       store_rounded(dx + c, rstd * (widen(__ldg(dy + c)) * w[0] - s.x * inv - hat * (s.y * inv)));
     }
   }
-  if (SHARES)
-    for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x)
-      write_share(a, blockIdx.x, gridDim.x, c, shares[c], shares[a.d + c]);
 }
 
 // dw and db of very long rows: 1024 columns and a part of the rows per CTA.
@@ -248,44 +242,44 @@ __global__ void __launch_bounds__(kJoinColumns * kJoinRows) norm_join_kernel(con
   else static_cast<float*>(out)[at] = s;
 }
 
-constexpr uint32_t kSharesWidth = 28000;  // columns whose shares fit shared memory
-
-// A call's kernel, its CTAs, and how many shares of dw and db they leave.
+// A call's kernel, how its rows are spread, and how many shares of dw and db they leave.
 struct Plan {
-  const void* kernel;
-  uint32_t v, warps, ctas, threads, smem, parts;
+  RowPlan rows;  // (no kernel: rows that no threads hold)
+  uint32_t v, parts;
 };
 
-template <typename X, typename Y, int V, int K, bool ALL>
-cudaError_t plan_rows(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
-  p.kernel = reinterpret_cast<const void*>(norm_grad_kernel<X, Y, V, K, ALL>);
-  p.warps = row_warps(c.d, V * K);
-  p.threads = ALL ? p.warps * 32 : kNormThreads;
-  const uint32_t per_cta = p.threads / (p.warps * 32);
-  p.smem = per_cta * kRing<V * K> * (row_place(c.d, sizeof(X)) + row_place(c.d, sizeof(Y)));
-  uint32_t per_sm = 0;
-  const cudaError_t err = resident_ctas(p.kernel, p.threads, p.smem, &per_sm);
-  p.parts = p.ctas = std::min((c.n + per_cta - 1) / per_cta, per_sm * static_cast<uint32_t>(dev.sm_count));
+template <typename X, typename Y, int V, int K, RowKind KIND>
+cudaError_t plan_rows(const NormGradCall& c, uint32_t most, const DeviceInfo& dev, Plan& p) {
+  plan_row(p.rows, reinterpret_cast<const void*>(norm_grad_kernel<X, Y, V, K, KIND>), KIND, V * K, c.d, most);
+  const cudaError_t err = plan_groups(
+      p.rows, kRing<V * K> * (row_place(p.rows.part, sizeof(X)) + row_place(p.rows.part, sizeof(Y))), c.n, dev);
+  p.parts = p.rows.groups;
   return err;
 }
 template <typename X, typename Y, int V>
 cudaError_t plan_width(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
-  if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, false>(c, dev, p);
-  if (c.d <= 2048) return plan_rows<X, Y, V, 16 / V, false>(c, dev, p);
-  if (c.d <= 4096) return plan_rows<X, Y, V, 16 / V, true>(c, dev, p);
-  return plan_rows<X, Y, V, 32 / V, true>(c, dev, p);
+  if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, p);
+  if (c.d <= 2048) return plan_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, p);
+  // 16 values a thread leave two CTAs an SM (32,768 x 4096: 157 us, with 32 205), but a CTA
+  // without a cluster waits less (16,384 x 8192: 172 with 32, 226 with 16 and two CTAs)
+  constexpr uint32_t kFew = 16 * kNormThreads, kMany = 32 * kNormThreads;
+  if (c.d <= kFew || (c.d > kMany && c.d <= kFew * kNormCluster))
+    return plan_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, p);
+  return plan_rows<X, Y, V, 32 / V, kRowAll>(c, kMany, dev, p);
 }
 template <typename X, typename Y>
 cudaError_t plan_typed(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
-  constexpr uint32_t kWide = sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
+  constexpr bool kBoth16 = sizeof(X) == 2 && sizeof(Y) == 2;
   const bool many = c.n > 1;
   auto allow = [&](uint32_t v) {
     return c.d % v == 0 && rows_allow(c.x, many ? c.ldx : 0, sizeof(X), v) &&
            rows_allow(c.dy, many ? c.lddy : 0, sizeof(Y), v) &&
            rows_allow(c.dx, many && c.dx ? c.lddx : 0, sizeof(X), v);
   };
-  p.v = allow(kWide) ? kWide : allow(2) ? 2 : 1;
-  if (p.v == kWide) return plan_width<X, Y, kWide>(c, dev, p);
+  p.v = kBoth16 && allow(8) ? 8 : allow(4) ? 4 : allow(2) ? 2 : 1;
+  if constexpr (kBoth16)
+    if (p.v == 8) return plan_width<X, Y, 8>(c, dev, p);
+  if (p.v == 4) return plan_width<X, Y, 4>(c, dev, p);
   return p.v == 2 ? plan_width<X, Y, 2>(c, dev, p) : plan_width<X, Y, 1>(c, dev, p);
 }
 cudaError_t plan_of(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
@@ -296,32 +290,22 @@ cudaError_t plan_of(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
     return c.y_bf16 ? plan_typed<float, bf16_t>(c, dev, p) : plan_typed<float, float>(c, dev, p);
   }
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count), wide = (c.d + 1023) / 1024;
-  p.parts = p.ctas = std::min(c.n, sms);
-  if (c.d > kSharesWidth) p.parts = std::min((c.n + 15) / 16, (8 * sms + wide - 1) / wide);
+  p.rows.groups = std::min(c.n, sms);
+  p.parts = std::min((c.n + 15) / 16, (8 * sms + wide - 1) / wide);
   return cudaSuccess;
 }
 
 template <typename X, typename Y>
 cudaError_t launch_long(const NormGradCall& c, const Plan& p, cudaStream_t stream) {
   cudaError_t err = cudaSuccess;
-  const bool shares = c.dw || c.db;
-  if (shares && c.d <= kSharesWidth) {
-    err = cudaFuncSetAttribute(norm_grad_long_kernel<X, Y, true>,
-                               cudaFuncAttributeMaxDynamicSharedMemorySize, kSharesWidth * 8);
-    if (err != cudaSuccess) return err;
-    count_launch();
-    norm_grad_long_kernel<X, Y, true><<<p.ctas, 1024, c.d * 8, stream>>>(c);
-    return cudaGetLastError();
-  }
   if (c.dx) {
     count_launch();
-    norm_grad_long_kernel<X, Y, false><<<p.ctas, 1024, 0, stream>>>(c);
+    norm_grad_long_kernel<X, Y><<<p.rows.groups, 1024, 0, stream>>>(c);
     if ((err = cudaGetLastError()) != cudaSuccess) return err;
   }
-  if (shares) {
+  if (c.dw || c.db) {
     count_launch();
-    norm_grad_columns_kernel<X, Y>
-        <<<dim3((c.d + 1023) / 1024, p.parts), 256, 0, stream>>>(c, p.parts);
+    norm_grad_columns_kernel<X, Y><<<dim3((c.d + 1023) / 1024, p.parts), 256, 0, stream>>>(c, p.parts);
     err = cudaGetLastError();
   }
   return err;
@@ -343,12 +327,13 @@ cudaError_t launch_layer_norm_grad(NormGradCall c, Workspace* ws, cudaStream_t s
   if (err != cudaSuccess) return err;
   c.shares = ws ? reinterpret_cast<float*>(ws->model_scratch()) : nullptr;
   if (c.n == 0) {
-  } else if (p.kernel) {
-    c.warps = p.warps;
+  } else if (p.rows.kernel) {
+    c.threads = p.rows.threads;
+    c.cluster = p.rows.cluster;
+    c.part = p.rows.part;
     c.w_wide = rows_allow(c.w, 0, c.w_bf16 ? 2 : 4, c.w_bf16 ? p.v : std::min(p.v, 4u));
-    void* params[] = {&c};
     count_launch();
-    err = cudaLaunchKernel(p.kernel, dim3(p.ctas), dim3(p.threads), params, p.smem, stream);
+    err = launch_row(p.rows, &c, stream);
   } else if (c.x_bf16) {
     err = c.y_bf16 ? launch_long<bf16_t, bf16_t>(c, p, stream) : launch_long<bf16_t, float>(c, p, stream);
   } else {
