@@ -597,7 +597,8 @@ ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type
  *
  * Sums are fp32, in an order that n, v, d and the tokens fix, rounded once.
  * Scratch above 2048 tokens: 16 bytes a token, a fp32 row of d for each 8 tokens
- * (16 from 16,385 on, 64 from 65,536 on), and at most 3 MB beside.
+ * (16 from 16,385 on, 64 from 65,536 on, 32 where they are added), and at most 3 MB
+ * beside.
  */
 ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
                         const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,

@@ -27,8 +27,7 @@ constexpr uint32_t kFewTokens = 2048;
 constexpr int kThreadsFew = 256;
 constexpr int kLane = 8, kLaneMany = 16;  // columns a lane takes of a row: slices of 256, or 1024
 constexpr uint32_t kSlice = 32 * kLane;
-constexpr uint32_t kSumWarps = 8, kAheadMany = 4;
-constexpr uint32_t kPieceMany = 128;
+constexpr uint32_t kSumWarps = 8;       // of a summing CTA
 constexpr uint32_t kZeroRows = 64;
 constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
 constexpr int kSortThreads = 512;
@@ -53,6 +52,14 @@ struct RowPart {
       else x[k].clear();
     }
   }
+  // Of a row that the kernel writes.
+  __device__ __forceinline__ void load_own(const T* row, uint32_t slice, uint32_t lane, uint32_t d) {
+#pragma unroll
+    for (int k = 0; k < L / V; ++k) {
+      const uint32_t c = column<V, L>(slice, k, lane);
+      if (c < d) x[k].load_own(row + c);
+    }
+  }
   __device__ __forceinline__ void add_to(float (&sum)[L]) const {
 #pragma unroll
     for (int k = 0; k < L / V; ++k)
@@ -61,25 +68,20 @@ struct RowPart {
   }
 };
 
-// scale sum, or that added to what is there; rounded once.
-template <typename T, int V, int L>
-__device__ __forceinline__ void write_row(const EmbedGradCall& a, uint64_t row, uint32_t slice,
-                                          uint32_t lane, const float (&sum)[L]) {
+// scale sum, or (ADD) that added to what was there; rounded once.
+template <typename T, int V, int L, bool ADD>
+__device__ __forceinline__ void write_row(const EmbedGradCall& a, uint64_t row, uint32_t slice, uint32_t lane,
+                                          const float (&sum)[L], const RowPart<T, V, L>& there) {
   T* to = static_cast<T*>(a.dtable) + row * a.ld_dtable;
 #pragma unroll
   for (int k = 0; k < L / V; ++k) {
     const uint32_t c = column<V, L>(slice, k, lane);
     if (c < a.d) {
       float f[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        f[j] = ADD ? fmaf(sum[k * V + j], a.scale, there.x[k].get(j)) : sum[k * V + j] * a.scale;
       Vec<T, V> o;
-      if (a.add) {
-        o.load_own(to + c);
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = fmaf(sum[k * V + j], a.scale, o.get(j));
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = sum[k * V + j] * a.scale;
-      }
       o.round(f);
       o.store(to + c);
     }
@@ -102,7 +104,7 @@ __device__ __forceinline__ void zero_row(const EmbedGradCall& a, uint64_t row, u
 
 // ------------------------------------------------------------- few tokens
 // CTA i < n: position i. The others: rows of the table, `rows` each.
-template <typename D, typename T, int V>
+template <typename D, typename T, int V, bool ADD>
 __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const EmbedGradCall a, uint32_t rows, uint32_t* error) {
   constexpr uint32_t kWarps = kThreadsFew / 32;
   constexpr int kAhead = V > 1 ? 8 : 4;  // rows on their way
@@ -166,6 +168,9 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
     const uint32_t slice = slices < kWarps ? warp % slices : s0 + warp;
     const bool work = group < groups && slice < slices;
     float sum[kLane] = {};
+    RowPart<T, V, kLane> there;
+    if (ADD && work && group == 0)
+      there.load_own(static_cast<T*>(a.dtable) + own * a.ld_dtable, slice, lane, a.d);
     if (work) {
       for (uint32_t k = group; k < total; k += groups * kAhead) {
         RowPart<D, V, kLane> row[kAhead];
@@ -191,7 +196,7 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
           for (int j = 0; j < kLane; ++j) sum[j] += part[g * slices + warp][j * 32 + lane];
       }
     }
-    if (work && group == 0) write_row<T, V, kLane>(a, static_cast<uint64_t>(own), slice, lane, sum);
+    if (work && group == 0) write_row<T, V, kLane, ADD>(a, static_cast<uint64_t>(own), slice, lane, sum, there);
   }
 }
 
@@ -395,7 +400,7 @@ __device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t token, uint32_
 
 // Where a token's shares are all there with this warp's: their sum, in order of the
 // pieces. (Lane 0 has made the warp's shares visible.)
-template <typename T, int V, int L>
+template <typename T, int V, int L, bool ADD>
 __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s, uint32_t token, uint32_t piece,
                                             uint32_t slice, uint32_t lane, bool came, bool on) {
   const uint32_t before = came ? run_of(s, token, piece, lane, true) : 0u;
@@ -410,6 +415,9 @@ __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s
   if (had + 1 != shares) return;
   __syncwarp();  // (lane 0 has seen the others' shares, and so have all)
   float sum[L] = {};
+  RowPart<T, V, L> there;
+  if (ADD)
+    there.load_own(static_cast<T*>(a.dtable) + static_cast<uint64_t>(token) * a.ld_dtable, slice, lane, a.d);
   constexpr uint32_t kAhead = L == kLane ? 4 : 2;  // shares on their way
   for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {
     float x[kAhead][L];
@@ -430,10 +438,10 @@ __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s
 #pragma unroll
         for (int j = 0; j < L; ++j) sum[j] += x[q][j];
   }
-  write_row<T, V, L>(a, token, slice, lane, sum);
+  write_row<T, V, L, ADD>(a, token, slice, lane, sum, there);
 }
 
-template <typename D, typename T, int V, int L>
+template <typename D, typename T, int V, int L, bool ADD>
 __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGradCall a, const Sum s) {
   __shared__ uint32_t room[kSumWarps][2][kPieceMost];
   griddep_wait();
@@ -463,48 +471,59 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGr
   }
   const uint32_t last = lo > 0 ? __ldg(s.key + lo - 1) : a.v, next = lo + count < a.n ? __ldg(s.key + lo + count) : a.v;
   __syncwarp();
-  constexpr uint32_t kAhead = L == kLane ? (sizeof(D) == 2 && V > 2 ? 8 : 4) : (sizeof(D) == 2 ? kAheadMany : kAheadMany / 2);  // rows on their way
+  // rows on their way; and (ADD) the rows of the table that sums end in meanwhile
+  constexpr uint32_t kAhead = sizeof(D) == 2 && V > 2 && L == kLane && !ADD ? 8 : L == kLane || sizeof(D) == 2 ? 4 : 2;
   RowPart<D, V, L> rows[kAhead];
-  auto load = [&](RowPart<D, V, L> (&row)[kAhead], uint32_t i0) {
-#pragma unroll
-    for (uint32_t q = 0; q < kAhead; ++q)
-      if (i0 + q < count && keys[i0 + q] < a.v)
-        row[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(at[i0 + q]) * a.ld_dout, slice, lane, a.d);
-  };
+  RowPart<T, V, L> there[ADD ? kAhead : 1];
   float sum[L] = {};
-  const uint32_t first = keys[0];
+  const uint32_t first = keys[0], end = keys[count - 1];
   const bool came = first < a.v && last == first;  // the first token has come from the piece before
+  const bool on = end < a.v && next == end;        // the last one goes on in the next piece
+  bool share = came;                               // the sum at hand is a share
   uint32_t token = first;
-  bool shared = came;                              // so its sum is a share
-  auto add = [&](const RowPart<D, V, L> (&row)[kAhead], uint32_t i0) {
+  auto finish = [&](bool goes_on, const RowPart<T, V, L>& was) {
+    if (share || goes_on) leave_share<V, L>(a, s, piece, slice, lane, share, sum);
+    else if (token < a.v) write_row<T, V, L, ADD>(a, token, slice, lane, sum, was);
+  };
+  for (uint32_t i0 = 0; i0 < count; i0 += kAhead) {
 #pragma unroll
     for (uint32_t q = 0; q < kAhead; ++q) {
-      if (i0 + q < count) {
-        const uint32_t key = keys[i0 + q];
+      const uint32_t i = i0 + q;
+      if (i < count && keys[i] < a.v) {
+        rows[q].load(static_cast<const D*>(a.dout) + static_cast<uint64_t>(at[i]) * a.ld_dout, slice, lane, a.d);
+        if (ADD && (i + 1 == count || keys[i + 1] != keys[i]))
+          there[ADD ? q : 0].load_own(static_cast<const T*>(a.dtable) + static_cast<uint64_t>(keys[i]) * a.ld_dtable,
+                                      slice, lane, a.d);
+      }
+    }
+    // A sum is written at its last row where the table's row has come for it (ADD), else
+    // when the next one begins (131,075 x 1024: 153 us; at the last row 167).
+#pragma unroll
+    for (uint32_t q = 0; q < kAhead; ++q) {
+      const uint32_t i = i0 + q;
+      if (i < count) {
+        const uint32_t key = keys[i];
+        if (!ADD && key != token) finish(false, there[0]);
         if (key != token) {
-          if (shared) leave_share<V, L>(a, s, piece, slice, lane, true, sum);
-          else if (token < a.v) write_row<T, V, L>(a, token, slice, lane, sum);
           token = key;
-          shared = false;
+          share = false;
 #pragma unroll
           for (int j = 0; j < L; ++j) sum[j] = 0.0f;
         }
-        if (key < a.v) row[q].add_to(sum);
+        if (key < a.v) {
+          rows[q].add_to(sum);
+          if (ADD && (i + 1 == count || keys[i + 1] != key)) finish(i + 1 == count && on, there[ADD ? q : 0]);
+        }
       }
     }
-  };
-  for (uint32_t i = 0; i < count; i += kAhead) {
-    load(rows, i);
-    add(rows, i);
   }
-  const bool on = token < a.v && next == token;  // the last token goes on in the next piece
-  if (shared || on) leave_share<V, L>(a, s, piece, slice, lane, shared, sum);
-  else if (token < a.v) write_row<T, V, L>(a, token, slice, lane, sum);
+  if (!ADD) finish(on, there[0]);
   if (!came && !on) return;
   __syncwarp();
   if (lane == 0) __threadfence();
-  if (came) join_shares<T, V, L>(a, s, first, piece, slice, lane, true, shared && on);
-  if (on && !shared) join_shares<T, V, L>(a, s, token, piece, slice, lane, false, true);
+  const bool whole = came && first == end;  // one token, with one share
+  if (came) join_shares<T, V, L, ADD>(a, s, first, piece, slice, lane, true, whole && on);
+  if (on && !whole) join_shares<T, V, L, ADD>(a, s, end, piece, slice, lane, false, true);
 }
 
 // ------------------------------------------------------------------ planning
@@ -528,7 +547,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
     return c.d % v == 0 && rows(c.dout, c.n > 1 ? c.ld_dout : 0, dsize) &&
            rows(c.dtable, c.v > 1 ? c.ld_dtable : 0, tsize);
   };
-  p.v = allow(8) ? 8 : allow(4) ? 4 : allow(2) ? 2 : 1;
+  p.v = allow(8) ? 8 : allow(2) ? 2 : 1;
   p.few = c.n <= kFewTokens;
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
   p.sum.rows = std::max(8u, std::min((c.v + 4 * sms - 1) / (4 * sms), kRowsCta));
@@ -546,12 +565,13 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   s.per = ((c.n + kMaxParts - 1) / kMaxParts + tile - 1) / tile * tile;
   s.parts = (c.n + s.per - 1) / s.per;
   Sum& m = p.sum;
-  m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : kPieceMost;
-  m.pieces = (c.n + m.piece - 1) / m.piece;
-  p.lane = c.n >= 65536 && p.v >= 4 && c.d > 2 * kSlice ? kLaneMany : kLane;
-  if (p.lane == kLaneMany) m.piece = kPieceMany;
-  m.pieces = (c.n + m.piece - 1) / m.piece;
+  // (16 columns a lane, and the rows that they are added to, would leave a CTA an SM)
+  p.lane = c.n >= 65536 && p.v == 8 && c.d > 2 * kSlice && !c.add ? kLaneMany : kLane;
   m.slices = (c.d + 32 * p.lane - 1) / (32 * p.lane);
+  // positions a piece: many warps of short lists, few shares of long ones (131,075 x 1024:
+  // 153 us with 128, 161 with 64; added to 512 columns, 65,536: 75 and 59)
+  m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : c.add ? kPieceMost / 2 : kPieceMost;
+  m.pieces = (c.n + m.piece - 1) / m.piece;
   m.warps = m.pieces * m.slices;
   auto round = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
   p.hist = round(static_cast<size_t>(s.parts) * (4u << s.bits));
@@ -562,30 +582,33 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   return p;
 }
 
-template <typename D, typename T, int V>
+template <typename D, typename T, int V, bool ADD>
 cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   uint32_t zeros = c.add ? 0 : (c.v + p.sum.rows - 1) / p.sum.rows;
   EmbedGradCall a = c;
   if (p.few) {
     if (c.n + zeros == 0) return cudaSuccess;
     count_launch();
-    embed_grad_few_kernel<D, T, V><<<c.n + zeros, kThreadsFew, 0, stream>>>(a, p.sum.rows, p.sort.error);
+    embed_grad_few_kernel<D, T, V, ADD><<<c.n + zeros, kThreadsFew, 0, stream>>>(a, p.sum.rows, p.sort.error);
     return cudaGetLastError();
   }
   Sum s = p.sum;
   void* params[] = {&a, &s};
   count_launch();
-  const void* kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLane>);
-  if constexpr (V >= 4)
-    if (p.lane == kLaneMany) kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLaneMany>);
+  const void* kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLane, ADD>);
+  if constexpr (V == 8)
+    if (p.lane == kLaneMany) kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLaneMany, ADD>);
   return launch_pdl(kernel,
                     dim3((s.warps + kSumWarps - 1) / kSumWarps + zeros), 32 * kSumWarps, 0, stream, params, false);
 }
 
+template <typename D, typename T, int V>
+cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
+  return c.add ? launch<D, T, V, true>(c, p, stream) : launch<D, T, V, false>(c, p, stream);
+}
 template <typename D, typename T>
 cudaError_t launch_typed(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   if (p.v == 8) return launch<D, T, 8>(c, p, stream);
-  if (p.v == 4) return launch<D, T, 4>(c, p, stream);
   return p.v == 2 ? launch<D, T, 2>(c, p, stream) : launch<D, T, 1>(c, p, stream);
 }
 
