@@ -642,9 +642,9 @@ ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const 
  *   No output may overlap an input or another.
  *
  * Sums are fp32, those over rows by CTAs and then over the CTAs in order.
- * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA, of which there
- * are at most eight an SM (rows of more than 28,000 columns: at most one for each 16
- * rows, and at most 8 an SM for all columns).
+ * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA (per cluster above
+ * 4096 columns), of which there are at most eight an SM; rows of more than 65,536
+ * columns: 8 d for each 16 rows, at most 8 MB an SM for all columns.
  */
 ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
                              ef_grad_type w_type, const float* mean, const float* rstd,

@@ -4,8 +4,10 @@ The hot path of the paper's method — one error-feedback compression step per
 worker (a = e + gamma g, hard-threshold or Top-k selection, ordered
 compaction into (index, value) pairs, residual e <- a - C(a)) and the
 worker-ordered sparse aggregation — runs in hand-written CUDA kernels for
-sm_103a behind the C ABI of ``include/efsparse.h``. This package is the thin
-Python binding of that library (torch supplies device memory and streams)
+sm_103a behind the C ABI of ``include/efsparse.h``, and with it the operators of
+a language-model training step around the exchange: lookups, layer norm, the loss
+over a vocabulary, their gradients, orthogonalised and AdamW updates. This package
+is the thin Python binding of that library (torch supplies device memory and streams)
 plus the seeded synthetic workloads used by the tests and the benchmark.
 """
 from ._binding import (  # noqa: F401

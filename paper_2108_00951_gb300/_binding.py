@@ -659,25 +659,31 @@ def ef_layer_norm_grad(x, mean, rstd, dy, dx_out=None, weight=None, dweight_out=
         n, d = shape = x.shape
     except (AttributeError, ValueError):
         raise _no_matrix("x") from None
-    dtype, kind = None, 0
-    for t, name in ((weight, "weight"), (dweight_out, "dweight_out"), (dbias_out, "dbias_out")):
-        if t is not None:
-            kind, dtype = _kind_of(t, name), t.dtype
-            break
     at, ld, x_kind = _matrix(x, "x", shape, dev)
+    dy_at, ld_dy, dy_kind = _matrix(dy, "dy", shape, dev)
     dx, ld_dx = None, d
     if dx_out is not None:
         dx, ld_dx, dx_kind = _matrix(dx_out, "dx_out", shape, dev)
         if dx_kind != x_kind:
             raise TypeError("dx_out must be %s, got %s" % (x.dtype, dx_out.dtype))
+    w = dw = db = dtype = None
+    kind = 0
+    if weight is not None:
+        kind, dtype = _kind_of(weight, "weight"), weight.dtype
+        w = _weight(weight, "weight", dtype, d, dev)
+    if dweight_out is not None:
+        if dtype is None:
+            kind, dtype = _kind_of(dweight_out, "dweight_out"), dweight_out.dtype
+        dw = _weight(dweight_out, "dweight_out", dtype, d, dev)
+    if dbias_out is not None:
+        if dtype is None:
+            kind, dtype = _kind_of(dbias_out, "dbias_out"), dbias_out.dtype
+        db = _weight(dbias_out, "dbias_out", dtype, d, dev)
     if n and (mean is None or rstd is None):
         raise TypeError("mean and rstd must be CUDA tensors")
-    dy_at, ld_dy, dy_kind = _matrix(dy, "dy", shape, dev)
     status = lib.ef_layer_norm_grad(
-        at, ld, x_kind, _weight(weight, "weight", dtype, d, dev), kind,
-        _vector(mean, "mean", torch.float32, n, dev), _vector(rstd, "rstd", torch.float32, n, dev),
-        dy_at, ld_dy, dy_kind, n, d, dx, ld_dx, _weight(dweight_out, "dweight_out", dtype, d, dev),
-        _weight(dbias_out, "dbias_out", dtype, d, dev),
+        at, ld, x_kind, w, kind, _vector(mean, "mean", torch.float32, n, dev),
+        _vector(rstd, "rstd", torch.float32, n, dev), dy_at, ld_dy, dy_kind, n, d, dx, ld_dx, dw, db,
         _raw_stream(dev) if stream is None else _stream(stream))
     if status:
         _check(status, "ef_layer_norm_grad")
@@ -691,25 +697,28 @@ class TensorList:
     __slots__ = ("tensors", "dtype", "device", "numel", "pointers", "_sizes", "_at", "_blocks")
 
     def __init__(self, tensors, name="tensors"):
-        self.tensors = tuple(tensors)
+        self.tensors = tensors = tuple(tensors)
         self.dtype = self.device = None
-        self.numel, self.pointers = array.array("Q"), array.array("Q")
+        if tensors and isinstance(tensors[0], _Tensor):
+            self.dtype, self.device = tensors[0].dtype, tensors[0].get_device()
+        if not all(isinstance(t, _Tensor) and t.dtype is self.dtype and t.is_contiguous()
+                   and t.get_device() == self.device >= 0 for t in tensors):
+            self._refuse(name)
+        self.numel = array.array("Q", [t.numel() for t in tensors])
+        self.pointers = array.array("Q", [t.data_ptr() for t in tensors])
+        self._sizes = self.numel.tobytes()
+        self._blocks = None  # (sizes of the exponents of 8-bit states, once asked for)
+        self._at = self.pointers.buffer_info()[0]
+
+    def _refuse(self, name):
         for t in self.tensors:
             if not isinstance(t, _Tensor) or not t.is_cuda:
                 raise TypeError("%s must be CUDA tensors" % name)
-            if self.dtype is None:
-                self.dtype, self.device = t.dtype, t.get_device()
             if t.dtype is not self.dtype:
                 raise TypeError("%s must be of one dtype, got %s and %s" % (name, self.dtype, t.dtype))
             if t.get_device() != self.device:
                 raise ValueError("%s must be on one device" % name)
-            if not t.is_contiguous():
-                raise ValueError("%s must be contiguous" % name)
-            self.numel.append(t.numel())
-            self.pointers.append(t.data_ptr())
-        self._sizes = self.numel.tobytes()
-        self._blocks = None  # (sizes of the exponents of 8-bit states, once asked for)
-        self._at = self.pointers.buffer_info()[0]
+        raise ValueError("%s must be contiguous" % name)
 
     def __len__(self):
         return len(self.tensors)
