@@ -12,7 +12,7 @@
 // More: the positions are sorted by token (stable, least digit first: for each digit
 // a launch that counts it by parts of the positions, and one in which each CTA
 // finds where its part goes from the counts of the parts before it). Then a warp
-// takes 256 columns of a piece of the sorted positions, adds up rows and writes a
+// takes 256 or 512 columns of a piece of the sorted positions, adds up rows and writes a
 // row's sum when the token changes. A token that goes on past its piece leaves a
 // share; the warp that leaves a token's last one joins them, in their order.
 #include <algorithm>
@@ -25,11 +25,11 @@ namespace {
 
 constexpr uint32_t kFewTokens = 2048;
 constexpr int kThreadsFew = 256;
-constexpr int kLane = 8, kLaneMany = 16;  // columns a lane takes of a row: slices of 256, or 1024
+constexpr int kLane = 8, kLaneMany = 16;  // columns a lane takes of a row: slices of 256, or 512
 constexpr uint32_t kSlice = 32 * kLane;
 constexpr uint32_t kSumWarps = 8;       // of a summing CTA
-constexpr uint32_t kZeroRows = 64;
-constexpr uint32_t kRowsCta = 8192;     // rows that a CTA writing zeros takes, at most
+constexpr uint32_t kZeroRows = 64;       // rows that a CTA of zeros takes beside sums
+constexpr uint32_t kRowsCta = 8192;     // and of a few tokens, at most
 constexpr int kSortThreads = 512;
 constexpr int kMaxBins = 512;
 constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
@@ -384,18 +384,17 @@ __device__ __forceinline__ void leave_share(const EmbedGradCall& a, const Sum& s
 }
 
 // The pieces that begin with the token from piece q + 1 on, or (back) those before q that
-// end with it: how many there are without a gap.
-__device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t token, uint32_t q, uint32_t lane, bool back) {
-  uint32_t run = 0;
-  while (true) {
-    const uint32_t step = run + 1 + lane;
-    bool same = false;
-    if (back) same = step <= q && __ldg(s.key + (q - step + 1) * s.piece - 1) == token;
-    else same = q + step < s.pieces && __ldg(s.key + (q + step) * s.piece) == token;
-    const uint32_t m = __ballot_sync(0xffffffffu, same);
-    if (m != 0xffffffffu) return run + __ffs(~m) - 1;
-    run += 32;
-  }
+// end with it: how many there are without a gap. Most runs end within a look at 32
+// pieces; the ends of long ones are searched.
+__device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t n, uint32_t token, uint32_t q, uint32_t lane,
+                                           bool back) {
+  const uint32_t step = 1 + lane;
+  bool same = false;
+  if (back) same = step <= q && __ldg(s.key + (q - step + 1) * s.piece - 1) == token;
+  else same = q + step < s.pieces && __ldg(s.key + (q + step) * s.piece) == token;
+  const uint32_t m = __ballot_sync(0xffffffffu, same);
+  if (m != 0xffffffffu) return __ffs(~m) - 1;
+  return back ? q - first_of(s.key, n, token) / s.piece : (first_of(s.key, n, token + 1) - 1) / s.piece - q;
 }
 
 // Where a token's shares are all there with this warp's: their sum, in order of the
@@ -403,8 +402,8 @@ __device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t token, uint32_
 template <typename T, int V, int L, bool ADD>
 __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s, uint32_t token, uint32_t piece,
                                             uint32_t slice, uint32_t lane, bool came, bool on) {
-  const uint32_t before = came ? run_of(s, token, piece, lane, true) : 0u;
-  const uint32_t after = on ? run_of(s, token, piece, lane, false) : 0u;
+  const uint32_t before = came ? run_of(s, a.n, token, piece, lane, true) : 0u;
+  const uint32_t after = on ? run_of(s, a.n, token, piece, lane, false) : 0u;
   const uint32_t first = piece - before, shares = before + 1 + after;
   uint32_t had = 0;
   if (lane == 0) {

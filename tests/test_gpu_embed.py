@@ -105,6 +105,19 @@ def test_gradient_of_uneven_tokens(n, kind):
     check_gradient(n, v, d, F32, BF16, 0, 0, True, t=t)
 
 
+def test_long_lists():
+    """Sorting CTAs of several tiles, and tokens with thousands of shares."""
+    for n, v, d in ((700003, 5000, 8), (620000, 3, 40)):
+        g = torch.Generator(device=DEV).manual_seed(n)
+        t = tokens(n, v, g, padding=0.01)
+        check_gradient(n, v, d, BF16, F32, 0, 0, False, t=t)
+        check_gradient(n, v, d, F32, BF16, 0, 0, True, t=t)
+    t = torch.full((400000,), 1, device=DEV)
+    t[-1] = 2
+    check_gradient(400000, 4, 24, BF16, F32, 0, 0, False, t=t)
+    check_gradient(400000, 4, 600, BF16, BF16, 0, 0, False, t=t)
+
+
 def test_many_digits():
     """Words beyond two digits of nine bits, and beyond three."""
     for v in ((1 << 18) - 1, 1 << 18, (1 << 27) + 5):
