@@ -44,14 +44,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
   float w[K][V], b[K][V];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const uint32_t c = (k * g.threads + t) * V;
-    if (c < part.columns) {
-      load_weights<V>(a.w, a.w_bf16, a.w_wide, part.first + c, 1.0f, w[k]);
-      load_weights<V>(a.b, a.w_bf16, a.b_wide, part.first + c, 0.0f, b[k]);
-    }
-  }
+  load_weights(a.w, a.w_bf16, a.w_wide, part.first, t * V, g.threads * V, part.columns, 1.0f, w);
+  load_weights(a.b, a.w_bf16, a.b_wide, part.first, t * V, g.threads * V, part.columns, 0.0f, b);
   const float inv = 1.0f / static_cast<float>(a.d);
   if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
   uint32_t slot = 0, parity = 0;
@@ -128,10 +122,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
   const float rstd = inverse_root(cta_sum2(sum, 0.0f, room[1]).x * inv + a.eps);
 #pragma unroll 4
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
-    float w[1], b[1];
-    load_weights<1>(a.w, a.w_bf16, true, c, 1.0f, w);
-    load_weights<1>(a.b, a.w_bf16, true, c, 0.0f, b);
-    store_rounded(y + c, fmaf((widen(__ldg(x + c)) - mean) * rstd, w[0], b[0]));
+    const float w = load_weight(a.w, a.w_bf16, c, 1.0f), b = load_weight(a.b, a.w_bf16, c, 0.0f);
+    store_rounded(y + c, fmaf((widen(__ldg(x + c)) - mean) * rstd, w, b));
   }
   if (threadIdx.x == 0) {
     if (a.mean) a.mean[blockIdx.x] = mean;
@@ -157,7 +149,12 @@ cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream
   // (32,768 x 4096: 16 a thread 126 us, 32 81), more have more rows at once
   if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, stream);
   if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, stream);
-  return launch_rows<X, Y, V, 32 / V, kRowAll>(c, 32 * kNormThreads, dev, stream);
+  // A few long rows of narrow vectors wait for one thread's values: 255 x 24,209 35.6 us with 32
+  // a thread, 23.1 with 16; but 4096 x 9001 119 and 128, and 255 x 24,576 (vectors of 8) 11.3 and 12.6
+  constexpr uint32_t kMany = 32 * kNormThreads, kFew = 16 * kNormThreads;
+  if (V < 8 && c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
+    return launch_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, stream);
+  return launch_rows<X, Y, V, 32 / V, kRowAll>(c, kMany, dev, stream);
 }
 
 template <typename X, typename Y>

@@ -50,40 +50,46 @@ __device__ __forceinline__ RowPart row_part(uint32_t d, uint32_t part, uint32_t 
   return {first, min(part, d - first)};
 }
 
-// V values of a weight vector of either type, or `none` where there is no vector.
-template <int V>
-__device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide, uint32_t c,
-                                             float none, float (&out)[V]) {
+// A thread's K vectors of V values, `step` columns apart, of a weight vector of either type, or
+// `none` where there is no vector. (All are on their way before one is widened: with a vector
+// at a time, both passes over 3 rows of 7398 with bf16 weights take 19.7 us, so 11.3.)
+template <typename T, int V, int PART, int K>
+__device__ __forceinline__ void load_vectors(const T* w, uint32_t c, uint32_t step, uint32_t columns,
+                                             float (&out)[K][V]) {
+  Vec<T, PART> x[K][V / PART];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (c + k * step < columns)
+#pragma unroll
+      for (int i = 0; i < V / PART; ++i) x[k][i].load(w + c + k * step + i * PART);
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (c + k * step < columns)
+#pragma unroll
+      for (int j = 0; j < V; ++j) out[k][j] = x[k][j / PART].get(j % PART);
+}
+template <int V, int K>
+__device__ __forceinline__ void load_weights(const void* w, bool bf16, bool wide, uint32_t first, uint32_t c,
+                                             uint32_t step, uint32_t columns, float none, float (&out)[K][V]) {
   if (!w) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = none;
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) out[k][j] = none;
   } else if (bf16) {
-    const bf16_t* p = static_cast<const bf16_t*>(w) + c;
-    if (wide) {
-      Vec<bf16_t, V> x;
-      x.load(p);
-#pragma unroll
-      for (int j = 0; j < V; ++j) out[j] = x.get(j);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) out[j] = bf16_bits_to_f32(__ldg(p + j));
-    }
+    const bf16_t* p = static_cast<const bf16_t*>(w) + first;
+    if (wide) load_vectors<bf16_t, V, V>(p, c, step, columns, out);
+    else load_vectors<bf16_t, V, 1>(p, c, step, columns, out);
   } else {
-    const float* p = static_cast<const float*>(w) + c;
-    constexpr int kPart = V > 4 ? 4 : V;
-    if (wide) {
-#pragma unroll
-      for (int j = 0; j < V; j += kPart) {
-        Vec<float, kPart> x;
-        x.load(p + j);
-#pragma unroll
-        for (int i = 0; i < kPart; ++i) out[j + i] = x.get(i);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) out[j] = __ldg(p + j);
-    }
+    const float* p = static_cast<const float*>(w) + first;
+    if (wide) load_vectors<float, V, (V > 4 ? 4 : V)>(p, c, step, columns, out);
+    else load_vectors<float, V, 1>(p, c, step, columns, out);
   }
+}
+// One value of it.
+__device__ __forceinline__ float load_weight(const void* w, bool bf16, uint32_t c, float none) {
+  if (!w) return none;
+  return bf16 ? bf16_bits_to_f32(__ldg(static_cast<const bf16_t*>(w) + c)) : __ldg(static_cast<const float*>(w) + c);
 }
 
 // The sum of a value (or of TWO) over a row's threads, in a fixed order, across the CTAs of a

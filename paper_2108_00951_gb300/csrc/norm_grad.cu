@@ -70,11 +70,7 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
   float mean = 0.0f, rstd = 0.0f;
   if (first < a.n) mean = __ldg(a.mean + first), rstd = __ldg(a.rstd + first);
   float w[K][V], dw[K][V] = {}, db[K][V] = {};
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const uint32_t c = (k * of.threads + t) * V;
-    if (c < part.columns) load_weights<V>(a.w, a.w_bf16, a.w_wide, part.first + c, 1.0f, w[k]);
-  }
+  load_weights(a.w, a.w_bf16, a.w_wide, part.first, t * V, of.threads * V, part.columns, 1.0f, w);
   const float inv = 1.0f / static_cast<float>(a.d);
   if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
   uint32_t slot = 0, parity = 0;
@@ -177,9 +173,8 @@ __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll 4
     for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
-      float w[1];
-      load_weights<1>(a.w, a.w_bf16, true, c, 1.0f, w);
-      const float hat = (widen(__ldg(x + c)) - mean) * rstd, q = widen(__ldg(dy + c)) * w[0];
+      const float w = load_weight(a.w, a.w_bf16, c, 1.0f);
+      const float hat = (widen(__ldg(x + c)) - mean) * rstd, q = widen(__ldg(dy + c)) * w;
       s1 += q;
       s2 = fmaf(q, hat, s2);
     }
@@ -187,10 +182,9 @@ __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradCall
     X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx;
 #pragma unroll 4
     for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
-      float w[1];
-      load_weights<1>(a.w, a.w_bf16, true, c, 1.0f, w);
+      const float w = load_weight(a.w, a.w_bf16, c, 1.0f);
       const float hat = (widen(__ldg(x + c)) - mean) * rstd;
-      store_rounded(dx + c, rstd * (widen(__ldg(dy + c)) * w[0] - s.x * inv - hat * (s.y * inv)));
+      store_rounded(dx + c, rstd * (widen(__ldg(dy + c)) * w - s.x * inv - hat * (s.y * inv)));
     }
   }
 }
