@@ -596,9 +596,9 @@ ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type
  *                    must not overlap an input.
  *
  * Sums are fp32, in an order that n, v, d and the tokens fix, rounded once.
- * Scratch above 2048 tokens: 16 bytes a token, a fp32 row of d for each 8 tokens
- * (16 from 16,385 on, 64 from 65,536 on, 32 where they are added), and at most 3 MB
- * beside.
+ * Scratch above 2048 tokens, and above 256 of more than 2,359,296 values: 16 bytes a
+ * token, a fp32 row of d for each 8 tokens (16 from 16,385 on, 64 from 65,536 on, 32
+ * where they are added), and at most 1 MB and a twentieth of that beside.
  */
 ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_type,
                         const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale,

@@ -5,7 +5,7 @@
 // it is added to, the rows that occur). Sums run in a fixed order, without
 // floating-point atomics.
 //
-// Up to kFewTokens tokens: one launch. A CTA per position looks through all
+// Up to kFewTokens tokens of kFewValues values: one launch. A CTA per position looks through all
 // tokens; if its own occurs before, another CTA has it, else it sums the rows of
 // all its occurrences. Further CTAs write the rows that do not occur.
 //
@@ -23,7 +23,11 @@
 namespace efs {
 namespace {
 
+// A CTA adds up a frequent word's rows by itself: of wide rows, fewer (of 350 words with 2164
+// columns, 1024 positions take 12 us, sorted 14; 2000 take 19, sorted 15; 2000 of 650 columns
+// 12 and 15).
 constexpr uint32_t kFewTokens = 2048;
+constexpr uint64_t kFewValues = uint64_t{9} << 18;
 constexpr int kThreadsFew = 256;
 constexpr int kLane = 8, kLaneMany = 16;  // columns a lane takes of a row: slices of 256, or 512
 constexpr uint32_t kSlice = 32 * kLane;
@@ -33,6 +37,7 @@ constexpr uint32_t kRowsCta = 8192;     // and of a few tokens, at most
 constexpr int kSortThreads = 512;
 constexpr int kMaxBins = 512;
 constexpr uint32_t kMaxParts = 296;     // sorting CTAs, at most
+constexpr uint32_t kJoin = 16;          // shares that are joined at a time
 constexpr uint32_t kPieceMost = 128;    // sorted positions that a warp adds up, at most
 
 // A lane's L columns of a slice: vectors of V, 32 V apart.
@@ -103,9 +108,10 @@ __device__ __forceinline__ void zero_row(const EmbedGradCall& a, uint64_t row, u
 }
 
 // ------------------------------------------------------------- few tokens
-// CTA i < n: position i. The others: rows of the table, `rows` each.
+// CTAs by position, `chunks` of the columns each (566 positions of 350 words, 2164 columns:
+// 16.5 us with all columns in one, 10.2 in three). The others: rows of the table, `rows` each.
 template <typename D, typename T, int V, bool ADD>
-__global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const EmbedGradCall a, uint32_t rows, uint32_t* error) {
+__global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const EmbedGradCall a, uint32_t rows, uint32_t chunks, uint32_t* error) {
   constexpr uint32_t kWarps = kThreadsFew / 32;
   constexpr int kAhead = V > 1 ? 8 : 4;  // rows on their way
   __shared__ uint32_t mask[kRowsCta / 32 > kFewTokens / 32 ? kRowsCta / 32 : kFewTokens / 32];
@@ -113,8 +119,8 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
   __shared__ float part[kWarps][kSlice];
   __shared__ uint32_t total;
   const uint32_t t = threadIdx.x, lane = t & 31u, warp = t >> 5;
-  if (blockIdx.x >= a.n) {  // zeros
-    const uint64_t lo = static_cast<uint64_t>(blockIdx.x - a.n) * rows;
+  if (blockIdx.x >= a.n * chunks) {  // zeros
+    const uint64_t lo = static_cast<uint64_t>(blockIdx.x - a.n * chunks) * rows;
     const uint64_t hi = min(lo + rows, static_cast<uint64_t>(a.v));
     for (uint32_t i = t; i < (rows + 31) / 32; i += kThreadsFew) mask[i] = 0u;
     __syncthreads();
@@ -128,15 +134,27 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
       if (!(mask[(r - lo) / 32] >> ((r - lo) & 31) & 1u)) zero_row<T>(a, r, lane);
     return;
   }
-  const uint32_t i = blockIdx.x;
+  const uint32_t i = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
   const int64_t own = __ldg(reinterpret_cast<const long long*>(a.token) + i);
   const uint32_t words = (a.n + 31u) / 32u;
+  constexpr uint32_t kLooks = kFewTokens / kThreadsFew;
+  int64_t other[kLooks];
+#pragma unroll
+  for (uint32_t k = 0; k < kLooks; ++k) {
+    const uint32_t j = k * kThreadsFew + t;
+    other[k] = j < a.n ? __ldg(reinterpret_cast<const long long*>(a.token) + j) : -1;
+  }
+  if (__syncthreads_or(t < i && other[0] == own)) return;  // (frequent words are soon met)
   bool before = false;
-  for (uint32_t j = t; j < words * 32u; j += kThreadsFew) {
-    const bool same = j < a.n && __ldg(reinterpret_cast<const long long*>(a.token) + j) == own;
-    before |= same && j < i;
-    const uint32_t m = __ballot_sync(0xffffffffu, same);
-    if (lane == 0) mask[j / 32] = m;
+#pragma unroll
+  for (uint32_t k = 0; k < kLooks; ++k) {
+    const uint32_t j = k * kThreadsFew + t;
+    if (j < words * 32u) {
+      const bool same = j < a.n && other[k] == own;
+      before |= same && j < i;
+      const uint32_t m = __ballot_sync(0xffffffffu, same);
+      if (lane == 0) mask[j / 32] = m;
+    }
   }
   if (own >= static_cast<int64_t>(a.v) && t == 0) atomicOr(error, kDevErrBadInput);
   if (own < 0 || own >= static_cast<int64_t>(a.v)) return;
@@ -159,14 +177,16 @@ __global__ void __launch_bounds__(kThreadsFew) embed_grad_few_kernel(const Embed
     if (lane == 0) total = at;
   }
   __syncthreads();
-  // slices of columns over the warps; with fewer slices than warps, groups of warps
-  // have all slices, each taking every groups-th occurrence
-  const uint32_t slices = (a.d + kSlice - 1) / kSlice;
+  // the chunk's slices of columns over the warps; with fewer slices than warps, groups of
+  // warps have all of them, each taking every groups-th occurrence
+  const uint64_t all = (a.d + kSlice - 1) / kSlice;
+  const uint32_t from = static_cast<uint32_t>(chunk * all / chunks);
+  const uint32_t slices = static_cast<uint32_t>((chunk + 1) * all / chunks) - from;
   const uint32_t groups = slices < kWarps ? min(kWarps / slices, total) : 1u;
   const uint32_t group = slices < kWarps ? warp / slices : 0u;
   for (uint32_t s0 = 0; s0 < slices; s0 += kWarps) {
-    const uint32_t slice = slices < kWarps ? warp % slices : s0 + warp;
-    const bool work = group < groups && slice < slices;
+    const uint32_t at = slices < kWarps ? warp % slices : s0 + warp, slice = from + at;
+    const bool work = group < groups && at < slices;
     float sum[kLane] = {};
     RowPart<T, V, kLane> there;
     if (ADD && work && group == 0)
@@ -347,7 +367,9 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
 struct Sum {
   const uint32_t *key, *pos;
   float* shares;          // [pieces][2][d]: a token from the piece before, one that goes on
-  uint32_t* arrived;      // [pieces][slices]: shares of the token that begins and goes on there
+  // [pieces][3][slices]: shares of a join whose first is the piece's, from the piece before
+  // or going on; joins of the token that begins and goes on there
+  uint32_t* arrived;
   uint32_t piece, pieces, slices, warps;  // positions a piece; warps that sum
   uint32_t rows;          // rows a CTA of zeros takes
 };
@@ -363,16 +385,13 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t n, u
   return lo;
 }
 
-// A warp's share of a token that several pieces have: slot 0 of its piece where it
-// has come from the piece before, else slot 1.
+// A sum's columns to a share's place, and from it (which this kernel writes, too).
 template <int V, int L>
-__device__ __forceinline__ void leave_share(const EmbedGradCall& a, const Sum& s, uint32_t piece, uint32_t slice,
-                                            uint32_t lane, bool came, const float (&sum)[L]) {
-  float* to = s.shares + (static_cast<uint64_t>(piece) * 2 + (came ? 0 : 1)) * a.d;
+__device__ __forceinline__ void write_share(float* to, uint32_t slice, uint32_t lane, uint32_t d, const float (&sum)[L]) {
 #pragma unroll
   for (int k = 0; k < L / V; ++k) {
     const uint32_t c = column<V, L>(slice, k, lane);
-    if (c < a.d) {
+    if (c < d) {
       float f[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) f[j] = sum[k * V + j];
@@ -381,6 +400,33 @@ __device__ __forceinline__ void leave_share(const EmbedGradCall& a, const Sum& s
       x.store(to + c);
     }
   }
+}
+template <int V, int L>
+__device__ __forceinline__ void read_share(const float* from, uint32_t slice, uint32_t lane, uint32_t d, float (&x)[L]) {
+#pragma unroll
+  for (int k = 0; k < L / V; ++k) {
+    const uint32_t c = column<V, L>(slice, k, lane);
+    if (c < d) {
+      if constexpr (V == 8) {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+          const float4 f = __ldcg(reinterpret_cast<const float4*>(from + c + h));
+          x[k * V + h] = f.x, x[k * V + h + 1] = f.y, x[k * V + h + 2] = f.z, x[k * V + h + 3] = f.w;
+        }
+      } else if constexpr (V == 2) {
+        const float2 f = __ldcg(reinterpret_cast<const float2*>(from + c));
+        x[k * V] = f.x, x[k * V + 1] = f.y;
+      } else {
+        x[k] = __ldcg(from + c);
+      }
+    }
+  }
+}
+
+// A warp's share of a token that several pieces have: slot 0 of its piece where it
+// has come from the piece before, else slot 1.
+__device__ __forceinline__ float* share_at(const Sum& s, uint32_t piece, uint32_t slot, uint32_t d) {
+  return s.shares + (static_cast<uint64_t>(piece) * 2 + slot) * d;
 }
 
 // The pieces that begin with the token from piece q + 1 on, or (back) those before q that
@@ -397,47 +443,67 @@ __device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t n, uint32_t to
   return back ? q - first_of(s.key, n, token) / s.piece : (first_of(s.key, n, token + 1) - 1) / s.piece - q;
 }
 
+// Whether this warp is the last of `of` at a counter. It then sees what the others have left.
+__device__ __forceinline__ bool last_of(uint32_t* arrived, uint32_t of, uint32_t lane) {
+  uint32_t had = 0;
+  if (lane == 0) {
+    had = atomicAdd(arrived, 1u);
+    __threadfence();
+  }
+  had = __shfl_sync(0xffffffffu, had, 0);
+  __syncwarp();  // (what lane 0 has seen, all have)
+  return had + 1 == of;
+}
+
 // Where a token's shares are all there with this warp's: their sum, in order of the
-// pieces. (Lane 0 has made the warp's shares visible.)
+// pieces, kJoin at a time; the sums of kJoin, left in the place of their first, likewise
+// (one after another, the 150 shares of a word that 48,135 have 4800 times take 10 us more).
+// (Lane 0 has made the warp's shares visible.)
 template <typename T, int V, int L, bool ADD>
 __device__ __forceinline__ void join_shares(const EmbedGradCall& a, const Sum& s, uint32_t token, uint32_t piece,
                                             uint32_t slice, uint32_t lane, bool came, bool on) {
   const uint32_t before = came ? run_of(s, a.n, token, piece, lane, true) : 0u;
   const uint32_t after = on ? run_of(s, a.n, token, piece, lane, false) : 0u;
-  const uint32_t first = piece - before, shares = before + 1 + after;
-  uint32_t had = 0;
-  if (lane == 0) {
-    had = atomicAdd(s.arrived + static_cast<uint64_t>(first) * s.slices + slice, 1u);
-    __threadfence();
-  }
-  had = __shfl_sync(0xffffffffu, had, 0);
-  if (had + 1 != shares) return;
-  __syncwarp();  // (lane 0 has seen the others' shares, and so have all)
-  float sum[L] = {};
+  uint32_t first = piece - before, shares = before + 1 + after;  // of the run
+  const uint32_t head = first, joins = (shares + kJoin - 1) / kJoin, join = before / kJoin;
+  auto counter = [&](uint32_t at, uint32_t of) { return s.arrived + (static_cast<uint64_t>(at) * 3 + of) * s.slices + slice; };
+  first += join * kJoin;  // of the join
+  shares = min(shares - join * kJoin, kJoin);
+  uint32_t step = 1;
+  if (!last_of(counter(first, join ? 0 : 1), shares, lane)) return;
   RowPart<T, V, L> there;
-  if (ADD)
+  if (ADD && joins == 1)
     there.load_own(static_cast<T*>(a.dtable) + static_cast<uint64_t>(token) * a.ld_dtable, slice, lane, a.d);
-  constexpr uint32_t kAhead = L == kLane ? 4 : 2;  // shares on their way
-  for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {
-    float x[kAhead][L];
+  constexpr uint32_t kAhead = 32 / L;  // shares on their way
+  while (true) {
+    float sum[L] = {};
+    for (uint32_t q0 = 0; q0 < shares; q0 += kAhead) {
+      float x[kAhead][L];
 #pragma unroll
-    for (uint32_t q = 0; q < kAhead; ++q) {
-      const float* from = s.shares + (static_cast<uint64_t>(first + q0 + q) * 2 + (q0 + q == 0 ? 1 : 0)) * a.d;
+      for (uint32_t q = 0; q < kAhead; ++q) {
+        const uint32_t at = first + (q0 + q) * step;
+        if (q0 + q < shares) read_share<V, L>(share_at(s, at, at == head ? 1 : 0, a.d), slice, lane, a.d, x[q]);
+      }
 #pragma unroll
-      for (int k = 0; k < L / V; ++k)
+      for (uint32_t q = 0; q < kAhead; ++q)
+        if (q0 + q < shares)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const uint32_t c = column<V, L>(slice, k, lane) + j;
-          x[q][k * V + j] = q0 + q < shares && c < a.d ? __ldcg(from + c) : 0.0f;
-        }
+          for (int j = 0; j < L; ++j) sum[j] += x[q][j];
     }
-#pragma unroll
-    for (uint32_t q = 0; q < kAhead; ++q)
-      if (q0 + q < shares)
-#pragma unroll
-        for (int j = 0; j < L; ++j) sum[j] += x[q][j];
+    if (step > 1 || joins == 1) {
+      write_row<T, V, L, ADD>(a, token, slice, lane, sum, there);
+      return;
+    }
+    write_share<V, L>(share_at(s, first, first == head ? 1 : 0, a.d), slice, lane, a.d, sum);
+    __syncwarp();
+    if (lane == 0) __threadfence();
+    if (!last_of(counter(head, 2), joins, lane)) return;
+    if (ADD)
+      there.load_own(static_cast<T*>(a.dtable) + static_cast<uint64_t>(token) * a.ld_dtable, slice, lane, a.d);
+    first = head;
+    shares = joins;
+    step = kJoin;
   }
-  write_row<T, V, L, ADD>(a, token, slice, lane, sum, there);
 }
 
 template <typename D, typename T, int V, int L, bool ADD>
@@ -481,7 +547,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGr
   bool share = came;                               // the sum at hand is a share
   uint32_t token = first;
   auto finish = [&](bool goes_on, const RowPart<T, V, L>& was) {
-    if (share || goes_on) leave_share<V, L>(a, s, piece, slice, lane, share, sum);
+    if (share || goes_on) write_share<V, L>(share_at(s, piece, share ? 0 : 1, a.d), slice, lane, a.d, sum);
     else if (token < a.v) write_row<T, V, L, ADD>(a, token, slice, lane, sum, was);
   };
   for (uint32_t i0 = 0; i0 < count; i0 += kAhead) {
@@ -531,6 +597,7 @@ struct Plan {
   uint32_t v;       // values per vector
   uint32_t rounds;  // positions that a sorting thread ranks at a time
   uint32_t lane;    // columns that a summing lane takes
+  uint32_t chunks;  // of the columns, of few tokens
   Sort sort;
   Sum sum;
   size_t hist, key, shares, bytes;  // sizes, in bytes
@@ -547,10 +614,17 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
            rows(c.dtable, c.v > 1 ? c.ld_dtable : 0, tsize);
   };
   p.v = allow(8) ? 8 : allow(2) ? 2 : 1;
-  p.few = c.n <= kFewTokens;
+  p.few = c.n <= kFewTokens && static_cast<uint64_t>(c.n) * c.d <= std::max(kFewValues, uint64_t{256} * c.d);
   const uint32_t sms = static_cast<uint32_t>(dev.sm_count);
   p.sum.rows = std::max(8u, std::min((c.v + 4 * sms - 1) / (4 * sms), kRowsCta));
-  if (p.few) return p;
+  if (p.few) {
+    // Each chunk's CTAs look through all tokens: up to 32 CTAs an SM, and narrow chunks only where
+    // words are met often (2000 x 650: of 350 words 11.8 us with 2 slices, 17.3 with 4; of 33,278
+    // 23.9 and 19.3).
+    const uint32_t slices = (c.d + kSlice - 1) / kSlice, span = c.n >= c.v ? 2 : 4;
+    p.chunks = std::max(1u, std::min((slices + span - 1) / span, 32 * sms / std::max(c.n, 1u)));
+    return p;
+  }
   p.sum.rows = kZeroRows;
   Sort& s = p.sort;
   uint32_t bits = 1;
@@ -576,7 +650,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   p.hist = round(static_cast<size_t>(s.parts) * (4u << s.bits));
   p.key = round(static_cast<size_t>(c.n) * 4);
   p.shares = round(static_cast<size_t>(m.pieces) * 2 * c.d * 4);
-  s.arrivals = m.warps;
+  s.arrivals = 3 * m.warps;
   p.bytes = p.hist + 4 * p.key + p.shares + round(static_cast<size_t>(s.arrivals) * 4);
   return p;
 }
@@ -588,7 +662,8 @@ cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   if (p.few) {
     if (c.n + zeros == 0) return cudaSuccess;
     count_launch();
-    embed_grad_few_kernel<D, T, V, ADD><<<c.n + zeros, kThreadsFew, 0, stream>>>(a, p.sum.rows, p.sort.error);
+    embed_grad_few_kernel<D, T, V, ADD>
+        <<<c.n * p.chunks + zeros, kThreadsFew, 0, stream>>>(a, p.sum.rows, p.chunks, p.sort.error);
     return cudaGetLastError();
   }
   Sum s = p.sum;

@@ -118,6 +118,31 @@ def test_long_lists():
     check_gradient(400000, 4, 600, BF16, BF16, 0, 0, False, t=t)
 
 
+@pytest.mark.parametrize("seed", range(4))
+def test_runs_of_many_pieces(seed):
+    """Words that go on over some, 16, 17 and many pieces of the sorted list, and begin where
+    the last piece of another one lies."""
+    g = torch.Generator().manual_seed(seed)
+    runs = [16 * 16, 16 * 17, 16 * 16 - 1, 16 * 16 + 1, 16 * 17 + 1, 1, 16 * 32, 16 * 33 + 5, 3, 16 * 48 + 2, 17, 16]
+    runs += torch.randint(1, 1200, (16,), generator=g).tolist()
+    for factor in (1, 4):  # pieces of 16 positions and of more
+        t = torch.repeat_interleave(torch.arange(len(runs)) + 1, torch.tensor(runs) * factor)
+        t = torch.cat([torch.full((seed * 5,), 0), t])
+        t = t[torch.randperm(t.numel(), generator=g)].to(DEV)
+        check_gradient(t.numel(), len(runs) + 2, 40, BF16, F32, 0, 0, False, t=t)
+        check_gradient(t.numel(), len(runs) + 2, 33, F32, BF16, 0, 0, True, t=t)
+        check_gradient(t.numel(), len(runs) + 2, 520, BF16, BF16, 0, 0, True, t=t)
+        check_gradient(t.numel(), len(runs) + 2, 520, BF16, BF16, 0, 0, False, t=t)
+
+
+@pytest.mark.parametrize("n,v,d", [(500, 60, 5000), (1000, 300, 2500), (1200, 30, 700), (90, 20, 9999), (257, 40, 9217),
+                                   (256, 40, 9300)])
+def test_gradient_of_wide_rows(n, v, d):
+    check_gradient(n, v, d, BF16, F32, 0, 0, False)
+    check_gradient(n, v, d, F32, BF16, 0, 0, True)
+    check_gradient(n, v, d, F32, BF16, 3, 1, False)
+
+
 def test_many_digits():
     """Words beyond two digits of nine bits, and beyond three."""
     for v in ((1 << 18) - 1, 1 << 18, (1 << 27) + 5):
