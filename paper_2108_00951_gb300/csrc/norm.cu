@@ -22,13 +22,16 @@ namespace {
 template <int E>
 constexpr int kRing = E == 8 ? 8 : 4;
 
+// (32 values a thread in 128 registers, narrow vectors with some of them spilled: 2000 x 9001 fp32
+// 50 us, in 192 registers 76)
 template <typename X, typename Y, int V, int K, RowKind KIND>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
+__global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel(const NormCall a) {
   constexpr int S = kRing<V * K>;
   extern __shared__ __align__(16) char ring[];
   __shared__ RowRoom room;
   const RowGroup<KIND> g(a.threads);
   const RowPart part = row_part(a.d, a.part, a.cluster);
+  const RowColumns<KIND, V> of(g, part.columns);
   const uint32_t per_cta = KIND == kRowAll ? 1u : blockDim.x / g.threads, t = g.t;
   const uint32_t groups = gridDim.x / a.cluster * per_cta;
   const uint32_t first = blockIdx.x / a.cluster * per_cta + g.index;
@@ -44,8 +47,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(first + s * groups, s);
   float w[K][V], b[K][V];
-  load_weights(a.w, a.w_bf16, a.w_wide, part.first, t * V, g.threads * V, part.columns, 1.0f, w);
-  load_weights(a.b, a.w_bf16, a.b_wide, part.first, t * V, g.threads * V, part.columns, 0.0f, b);
+  load_weights(a.w, a.w_bf16, a.w_wide, part.first, of.first, of.step(), of.end, 1.0f, w);
+  load_weights(a.b, a.w_bf16, a.b_wide, part.first, of.first, of.step(), of.end, 0.0f, b);
   const float inv = 1.0f / static_cast<float>(a.d);
   if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
   uint32_t slot = 0, parity = 0;
@@ -57,14 +60,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const bool in = KIND != kRowLanes || row < a.n;
-    const char* in_row = rows + slot * place + (in ? row_lead(x_row(row)) : 0u);
+    const char* in_row = rows + slot * place + (in ? row_lead(x_row(row)) : 0u) + of.first * sizeof(X);
     slot = slot == S - 1 ? 0 : slot + 1;
     float x[K][V], sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * g.threads + t) * V;
-      if (in && c < part.columns) {
-        const Vec<X, V> v = staged<X, V>(in_row, c);
+      if (in && of.has(k)) {
+        const Vec<X, V> v = staged<X, V>(in_row, of.off(k));
 #pragma unroll
         for (int j = 0; j < V; ++j) sum += x[k][j] = v.get(j);
       }
@@ -73,7 +75,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
     sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (in && (k * g.threads + t) * V < part.columns)
+      if (in && of.has(k))
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           x[k][j] -= mean;
@@ -82,17 +84,16 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormCall a) {
     }
     const float var = row_sum<KIND, false>(g, sum, 0.0f, room, 1, a.cluster, parity).x * inv;
     const float rstd = inverse_root(var + a.eps);
-    Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy + part.first;
+    Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy + part.first + of.first;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * g.threads + t) * V;
-      if (in && c < part.columns) {
+      if (in && of.has(k)) {
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) out[j] = fmaf(x[k][j] * rstd, w[k][j], b[k][j]);
         Vec<Y, V> o;
         o.round(out);
-        o.store(y + c);
+        o.store(y + of.off(k));
       }
     }
     if (t == 0 && part.first == 0 && in) {
@@ -149,10 +150,11 @@ cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream
   // (32,768 x 4096: 16 a thread 126 us, 32 81), more have more rows at once
   if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, stream);
   if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, stream);
-  // A few long rows of narrow vectors wait for one thread's values: 255 x 24,209 35.6 us with 32
-  // a thread, 23.1 with 16; but 4096 x 9001 119 and 128, and 255 x 24,576 (vectors of 8) 11.3 and 12.6
+  // Of a few long rows with narrow vectors, a thread's values are the wait: 255 x 24,209 fp32
+  // 27.5 us with 32 a thread, 22.1 with 16 (30 x 9001 6.2 and 4.3; but 700 x 9001 23.9 and 25.0, and
+  // 255 x 16,388, vectors of 4, 13.5 and 15.9)
   constexpr uint32_t kMany = 32 * kNormThreads, kFew = 16 * kNormThreads;
-  if (V < 8 && c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
+  if (V < 4 && c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
     return launch_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, stream);
   return launch_rows<X, Y, V, 32 / V, kRowAll>(c, kMany, dev, stream);
 }

@@ -50,6 +50,22 @@ __device__ __forceinline__ RowPart row_part(uint32_t d, uint32_t part, uint32_t 
   return {first, min(part, d - first)};
 }
 
+// A thread's columns of a row, or of a CTA's part of one: K vectors of V, `step` apart. A warp's
+// columns lie together, so that its steps are constants of the addresses.
+template <RowKind KIND, int V>
+struct RowColumns {
+  uint32_t first, end, lanes;
+  __device__ __forceinline__ RowColumns(const RowGroup<KIND>& g, uint32_t columns) : first(g.t * V), end(columns), lanes(g.threads) {
+    if (KIND == kRowLanes) return;
+    const uint32_t per = (columns + g.threads * V - 1) / (g.threads * V) * (32 * V), warp = g.t >> 5;
+    first = warp * per + (g.t & 31u) * V;
+    end = min(columns, (warp + 1) * per);
+  }
+  __device__ __forceinline__ uint32_t step() const { return KIND == kRowLanes ? lanes * V : 32u * V; }
+  __device__ __forceinline__ uint32_t off(int k) const { return k * step(); }  // from the first
+  __device__ __forceinline__ bool has(int k) const { return first + off(k) < end; }
+};
+
 // A thread's K vectors of V values, `step` columns apart, of a weight vector of either type, or
 // `none` where there is no vector. (All are on their way before one is widened: with a vector
 // at a time, both passes over 3 rows of 7398 with bf16 weights take 19.7 us, so 11.3.)

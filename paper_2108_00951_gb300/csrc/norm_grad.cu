@@ -45,13 +45,14 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
   constexpr int S = kRing<V * K>;
   extern __shared__ __align__(16) char ring[];
   __shared__ RowRoom room;
-  const RowGroup<KIND> of(a.threads);
+  const RowGroup<KIND> g(a.threads);
   const RowPart part = row_part(a.d, a.part, a.cluster);
-  const uint32_t per_cta = KIND == kRowAll ? 1u : blockDim.x / of.threads, t = of.t;
+  const RowColumns<KIND, V> of(g, part.columns);
+  const uint32_t per_cta = KIND == kRowAll ? 1u : blockDim.x / g.threads, t = g.t;
   const uint32_t parts = gridDim.x / a.cluster, share = blockIdx.x / a.cluster;
-  const uint32_t groups = parts * per_cta, first = share * per_cta + of.index;
+  const uint32_t groups = parts * per_cta, first = share * per_cta + g.index;
   const uint32_t x_place = row_place(a.part, sizeof(X)), place = x_place + row_place(a.part, sizeof(Y));
-  char* rows = ring + of.index * S * place;
+  char* rows = ring + g.index * S * place;
   auto x_row = [&](uint32_t row) {
     return static_cast<const X*>(a.x) + static_cast<uint64_t>(row) * a.ldx + part.first;
   };
@@ -60,8 +61,8 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
   };
   auto fetch = [&](uint32_t row, uint32_t slot) {
     if (row < a.n) {
-      fetch_row(rows + slot * place, x_row(row), part.columns * sizeof(X), t, of.threads);
-      fetch_row(rows + slot * place + x_place, dy_row(row), part.columns * sizeof(Y), t, of.threads);
+      fetch_row(rows + slot * place, x_row(row), part.columns * sizeof(X), t, g.threads);
+      fetch_row(rows + slot * place + x_place, dy_row(row), part.columns * sizeof(Y), t, g.threads);
     }
     fetch_commit();
   };
@@ -70,56 +71,54 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
   float mean = 0.0f, rstd = 0.0f;
   if (first < a.n) mean = __ldg(a.mean + first), rstd = __ldg(a.rstd + first);
   float w[K][V], dw[K][V] = {}, db[K][V] = {};
-  load_weights(a.w, a.w_bf16, a.w_wide, part.first, t * V, of.threads * V, part.columns, 1.0f, w);
+  load_weights(a.w, a.w_bf16, a.w_wide, part.first, of.first, of.step(), of.end, 1.0f, w);
   const float inv = 1.0f / static_cast<float>(a.d);
   if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
   uint32_t slot = 0, parity = 0;
   // (the lanes of a warp go through its rows together: to the last round of the warp's first)
-  const uint32_t ahead = KIND == kRowLanes ? of.index % (32u / of.threads) : 0u;
+  const uint32_t ahead = KIND == kRowLanes ? g.index % (32u / g.threads) : 0u;
   for (uint32_t row = first; row - ahead < a.n; row += groups) {
     fetch_wait<S - 2>();
-    of.sync();
+    g.sync();
     // (all threads are done with the row before: its place is free)
     fetch(row + (S - 1) * groups, slot == 0 ? S - 1 : slot - 1);
     const float mu = mean, r = rstd;
     if (row + groups < a.n) mean = __ldg(a.mean + row + groups), rstd = __ldg(a.rstd + row + groups);
     const bool in = KIND != kRowLanes || row < a.n;
-    const char* xs = rows + slot * place + (in ? row_lead(x_row(row)) : 0u);
-    const char* dys = rows + slot * place + x_place + (in ? row_lead(dy_row(row)) : 0u);
+    const char* xs = rows + slot * place + (in ? row_lead(x_row(row)) : 0u) + of.first * sizeof(X);
+    const char* dys = rows + slot * place + x_place + (in ? row_lead(dy_row(row)) : 0u) + of.first * sizeof(Y);
     slot = slot == S - 1 ? 0 : slot + 1;
     float hat[K][V], q[K][V], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * of.threads + t) * V;
-      if (in && c < part.columns) {
-        const Vec<X, V> x = staged<X, V>(xs, c);
-        const Vec<Y, V> dy = staged<Y, V>(dys, c);
+      if (in && of.has(k)) {
+        const Vec<X, V> x = staged<X, V>(xs, of.off(k));
+        const Vec<Y, V> dy = staged<Y, V>(dys, of.off(k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float g = dy.get(j);
+          const float dyj = dy.get(j);
           hat[k][j] = (x.get(j) - mu) * r;
-          q[k][j] = g * w[k][j];
+          q[k][j] = dyj * w[k][j];
           s1 += q[k][j];
           s2 = fmaf(q[k][j], hat[k][j], s2);
-          dw[k][j] = fmaf(g, hat[k][j], dw[k][j]);
-          db[k][j] += g;
+          dw[k][j] = fmaf(dyj, hat[k][j], dw[k][j]);
+          db[k][j] += dyj;
         }
       }
     }
     if (!a.dx) continue;
-    const float2 s = row_sum<KIND, true>(of, s1, s2, room, 0, a.cluster, parity);
+    const float2 s = row_sum<KIND, true>(g, s1, s2, room, 0, a.cluster, parity);
     const float m1 = s.x * inv, m2 = s.y * inv;
-    X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx + part.first;
+    X* dx = static_cast<X*>(a.dx) + static_cast<uint64_t>(row) * a.lddx + part.first + of.first;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t c = (k * of.threads + t) * V;
-      if (in && c < part.columns) {
+      if (in && of.has(k)) {
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) out[j] = r * fmaf(-m2, hat[k][j], q[k][j] - m1);
         Vec<X, V> o;
         o.round(out);
-        o.store(dx + c);
+        o.store(dx + of.off(k));
       }
     }
   }
@@ -130,8 +129,8 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const uint32_t c = (k * of.threads + t) * V + j;
-        if (c < part.columns) write_share(a, share, parts, part.first + c, dw[k][j], db[k][j]);
+        const uint32_t c = of.first + of.off(k) + j;
+        if (of.has(k)) write_share(a, share, parts, part.first + c, dw[k][j], db[k][j]);
       }
     return;
   }
@@ -143,10 +142,10 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 16 ? 2 : 1) norm_grad_k
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const uint32_t c = (k * of.threads + t) * V + j;
-      if (c < a.d) {
-        shares[of.index * a.d + c] = dw[k][j];
-        shares[(per_cta + of.index) * a.d + c] = db[k][j];
+      const uint32_t c = of.first + of.off(k) + j;
+      if (of.has(k)) {
+        shares[g.index * a.d + c] = dw[k][j];
+        shares[(per_cta + g.index) * a.d + c] = db[k][j];
       }
     }
   __syncthreads();
