@@ -260,10 +260,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s,
         key = __ldcg(s.key[pass & 1u] + i);
       }
     }
-    // (frequent tokens: a warp's equal digits are one addition)
-    const uint32_t digit = i < hi ? digit_of(s, key, pass) : bins;
-    const uint32_t same = __match_any_sync(0xffffffffu, digit);
-    if (digit < bins && (same & lanemask_lt()) == 0u) atomicAdd(&hist[digit], static_cast<uint32_t>(__popc(same)));
+    // (131,072 x 1024: 119 us; with a warp's equal digits matched to be one addition 121)
+    if (i < hi) atomicAdd(&hist[digit_of(s, key, pass)], 1u);
   }
   griddep_launch_dependents();  // (the scatter, which waits for this kernel's end)
   if (bad) atomicOr(s.error, kDevErrBadInput);

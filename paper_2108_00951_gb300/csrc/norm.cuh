@@ -55,7 +55,8 @@ __device__ __forceinline__ RowPart row_part(uint32_t d, uint32_t part, uint32_t 
 template <RowKind KIND, int V>
 struct RowColumns {
   uint32_t first, end, lanes;
-  __device__ __forceinline__ RowColumns(const RowGroup<KIND>& g, uint32_t columns) : first(g.t * V), end(columns), lanes(g.threads) {
+  __device__ __forceinline__ RowColumns(const RowGroup<KIND>& g, uint32_t columns)
+      : first(g.t * V), end(columns), lanes(g.threads) {
     if (KIND == kRowLanes) return;
     const uint32_t per = (columns + g.threads * V - 1) / (g.threads * V) * (32 * V), warp = g.t >> 5;
     first = warp * per + (g.t & 31u) * V;
