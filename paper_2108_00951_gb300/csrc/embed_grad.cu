@@ -640,7 +640,7 @@ Plan plan_of(const EmbedGradCall& c, const DeviceInfo& dev) {
   p.lane = c.n >= 65536 && p.v == 8 && c.d > 2 * kSlice && !c.add ? kLaneMany : kLane;
   m.slices = (c.d + 32 * p.lane - 1) / (32 * p.lane);
   // positions a piece: many warps of short lists, few shares of long ones (131,075 x 1024:
-  // 153 us with 128, 161 with 64; added to 512 columns, 65,536: 75 and 59)
+  // 149 us with 128, 154 with 64; added, 131,072 x 1001 154 with 64, 157 with 32)
   m.piece = c.n <= 16384 ? 16 : c.n < 65536 ? 32 : c.add ? kPieceMost / 2 : kPieceMost;
   m.pieces = (c.n + m.piece - 1) / m.piece;
   m.warps = m.pieces * m.slices;
