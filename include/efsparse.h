@@ -619,9 +619,11 @@ ef_status ef_embed_grad(const void* dout, uint64_t ld_dout, ef_grad_type dout_ty
  *   mean_out, rstd_out [out] fp32[n] for ef_layer_norm_grad, each may be NULL.
  *   No output may overlap an input or another.
  *
- * Both sums are fp32, the second over differences from the mean (whose squares,
- * and the sum of them, have to be in fp32's range). A NaN or an infinity makes its
- * row NaN. No scratch; may be captured at any time.
+ * Both sums are fp32, the second over differences from the mean (the sum of x, the
+ * squares and the sum of them have to be in fp32's range). In an fp32 row whose mean is beyond
+ * four deviations the mean of the differences is taken off again, so that what is
+ * subtracted is as exact as in a row without a mean; a row of one value gives
+ * y = bias. A NaN or an infinity makes its row NaN. No scratch; may be captured at any time.
  */
 ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
                         const void* bias, ef_grad_type w_type, float eps, uint64_t n, uint64_t d,

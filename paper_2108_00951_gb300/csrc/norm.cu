@@ -3,7 +3,12 @@
 //
 // Both sums are fp32 over values that stay in registers, the second after the
 // mean is known (a difference of squares would lose the variance of rows whose
-// mean is large). What bounds it: reading x and writing y once. A row of up to 256
+// mean is large). rstd makes much of a last place of a large mean: of a row of 1000.0 it is 0.02 of
+// y, of one near 1e5 all of it. So the product with 1 / d is corrected by its remainder,
+// sum - mean d, and rows of fp32 (bf16 values of one magnitude add up exactly) whose mean is beyond four
+// deviations by the mean of their differences, which are exact there; below, what the sum
+// loses is at most 5 (depth + 2) 2^-24 deviations. What bounds it: reading x and writing y
+// once. A row of up to 256
 // values lies in lanes of a warp, of up to 2048 in warps, of up to 8192 in a CTA, of up to
 // 65,536 in a cluster of CTAs; they take rows a stride apart, the next ones on their way
 // into a ring in shared memory meanwhile, and the weights stay in registers. A
@@ -21,6 +26,16 @@ namespace {
 // Rows that a group has in its ring, with E values of a row a thread.
 template <int E>
 constexpr int kRing = E == 8 ? 8 : 4;
+
+// The mean c of a row's differences from what its sum gave for a mean (divided: exact for a row of
+// one value), and rstd without c^2 in the variance.
+struct Correction {
+  float c, rstd;
+};
+__device__ __forceinline__ Correction correction(float sum, float squares, uint32_t d, float inv, float eps) {
+  const float c = sum / static_cast<float>(d), left = fmaf(-sum, c, squares);
+  return {c, inverse_root((left < 0.0f ? 0.0f : left) * inv + eps)};  // (a NaN stays)
+}
 
 // (32 values a thread in 128 registers, narrow vectors with some of them spilled: 2000 x 9001 fp32
 // 50 us, in 192 registers 76)
@@ -49,7 +64,7 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel
   float w[K][V], b[K][V];
   load_weights(a.w, a.w_bf16, a.w_wide, part.first, of.first, of.step(), of.end, 1.0f, w);
   load_weights(a.b, a.w_bf16, a.b_wide, part.first, of.first, of.step(), of.end, 0.0f, b);
-  const float inv = 1.0f / static_cast<float>(a.d);
+  const float width = static_cast<float>(a.d), inv = 1.0f / width;
   if (KIND == kRowAll && a.cluster > 1) cluster_sync();  // (the others' shared memory is theirs)
   uint32_t slot = 0, parity = 0;
   // (the lanes of a warp go through its rows together: to the last round of the warp's first)
@@ -71,7 +86,9 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel
         for (int j = 0; j < V; ++j) sum += x[k][j] = v.get(j);
       }
     }
-    const float mean = row_sum<KIND, false>(g, sum, 0.0f, room, 0, a.cluster, parity).x * inv;
+    // (the fused product has the remainder exactly: the mean of a row of one value whose sum is exact is exact)
+    const float total = row_sum<KIND, false>(g, sum, 0.0f, room, 0, a.cluster, parity).x, near = total * inv;
+    const float mean = fmaf(fmaf(-near, width, total), inv, near);
     sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -82,8 +99,8 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel
           sum = fmaf(x[k][j], x[k][j], sum);
         }
     }
-    const float var = row_sum<KIND, false>(g, sum, 0.0f, room, 1, a.cluster, parity).x * inv;
-    const float rstd = inverse_root(var + a.eps);
+    const float squares = row_sum<KIND, false>(g, sum, 0.0f, room, 1, a.cluster, parity).x;
+    const float var = squares * inv, rstd = inverse_root(var + a.eps);
     Y* y = static_cast<Y*>(a.y) + static_cast<uint64_t>(row) * a.ldy + part.first + of.first;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -100,6 +117,38 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
+    // A large mean: the row again, from its place in the ring. (All of a row's threads have the same
+    // sums; the lanes of a warp go together. As a branch around the last pass, its values in
+    // registers, it takes 2000 x 9001 from 42 to 50 us; for every row 32,768 x 4096 from 85 to 96.)
+    const bool large = sizeof(X) == 4 && in && mean * mean > 16.0f * var;
+    if (sizeof(X) == 4 && __builtin_expect(KIND == kRowLanes ? __any_sync(0xffffffffu, large) : large, 0)) {
+      sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (in && of.has(k)) {
+          const Vec<X, V> v = staged<X, V>(in_row, of.off(k));
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum += x[k][j] = v.get(j) - mean;
+        }
+      }
+      sum = row_sum<KIND, false>(g, sum, 0.0f, room, 0, a.cluster, parity).x;
+      const Correction by = correction(sum, squares, a.d, inv, a.eps);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (large && of.has(k)) {
+          float out[V];
+#pragma unroll
+          for (int j = 0; j < V; ++j) out[j] = fmaf((x[k][j] - by.c) * by.rstd, w[k][j], b[k][j]);
+          Vec<Y, V> o;
+          o.round(out);
+          o.store(y + of.off(k));
+        }
+      }
+      if (t == 0 && part.first == 0 && large) {
+        if (a.mean) a.mean[row] = mean + by.c;
+        if (a.rstd) a.rstd[row] = by.rstd;
+      }
+    }
   }
 }
 
@@ -114,21 +163,24 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormCall a) {
 #pragma unroll 8
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) sum += widen(__ldg(x + c));
   const float mean = cta_sum2(sum, 0.0f, room[0]).x * inv;
+  float squares = 0.0f;
   sum = 0.0f;
 #pragma unroll 8
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
     const float off = widen(__ldg(x + c)) - mean;
-    sum = fmaf(off, off, sum);
+    sum += off;
+    squares = fmaf(off, off, squares);
   }
-  const float rstd = inverse_root(cta_sum2(sum, 0.0f, room[1]).x * inv + a.eps);
+  const float2 sums = cta_sum2(sum, squares, room[1]);
+  const Correction by = correction(sums.x, sums.y, a.d, inv, a.eps);  // (of every row)
 #pragma unroll 4
   for (uint32_t c = threadIdx.x; c < a.d; c += blockDim.x) {
     const float w = load_weight(a.w, a.w_bf16, c, 1.0f), b = load_weight(a.b, a.w_bf16, c, 0.0f);
-    store_rounded(y + c, fmaf((widen(__ldg(x + c)) - mean) * rstd, w, b));
+    store_rounded(y + c, fmaf((widen(__ldg(x + c)) - mean - by.c) * by.rstd, w, b));
   }
   if (threadIdx.x == 0) {
-    if (a.mean) a.mean[blockIdx.x] = mean;
-    if (a.rstd) a.rstd[blockIdx.x] = rstd;
+    if (a.mean) a.mean[blockIdx.x] = mean + by.c;
+    if (a.rstd) a.rstd[blockIdx.x] = by.rstd;
   }
 }
 

@@ -191,3 +191,60 @@ def test_equal_inputs_give_equal_bits(n, d):
         outs.append((dx, dw, db))
     for a in outs[1:]:
         assert all(torch.equal(p, q) for p, q in zip(a, outs[0]))
+
+
+def rows_at(d):
+    """Additions that a row's sum runs through, as above."""
+    return max(32, d // 1024) + 20
+
+
+@pytest.mark.parametrize("d", [1, 7, 13, 41, 55, 257, 1001, 2049, 4099, 9001, 33001, 70001])
+@pytest.mark.parametrize("xt", [F32, BF16])
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+def test_rows_of_one_value(d, xt, eps):
+    """A row of one value is its mean exactly, and y the bias. bf16 (8 bits) adds up exactly to 65,536
+    columns; else the sum's mean is off by k places of the value, k at most the additions, and the
+    differences, k places each, are added exactly (d k < 2^24) and divided exactly. Their squares may be off by (additions + 3) u of k^2 places^2."""
+    values = torch.tensor([1000.0, 1e4, 0.1, 1e5, -3.0, 100000.1, 1e-3], device=DEV)
+    x = values[:, None].expand(-1, d).to(xt).contiguous()
+    g = torch.Generator(device=DEV).manual_seed(d)
+    w, b = weights(d, F32, g), weights(d, F32, g)
+    y = torch.empty(len(x), d, device=DEV)
+    mean, rstd = torch.empty(len(x), device=DEV), torch.empty(len(x), device=DEV)
+    efs.ef_layer_norm(x, y, w, b, eps, mean, rstd)
+    assert torch.equal(mean, x[:, 0].float())
+    assert torch.equal(y, b.expand_as(y))
+    k = (rows_at(d) + 2) * 2 * U * x[:, 0].double().abs()
+    left = (rows_at(d) + 3) * U * k * k
+    eps = float(torch.tensor(eps))
+    want = eps ** -0.5
+    assert bool((rstd.double() <= want * (1 + 3 * U)).all())
+    assert bool((rstd.double() >= (eps + left).rsqrt() * (1 - 3 * U)).all())
+
+
+@pytest.mark.parametrize("d", [7, 41, 55, 64, 200, 650, 1001, 3000, 4096, 9000, 9001, 33000, 70001])
+@pytest.mark.parametrize("shift", [1e3, 1e5, -3e4])
+def test_what_is_subtracted_is_the_mean_of_large_rows(d, shift):
+    """With m the mean of the row's sum, off by at most e = (depth + 2) u avg|x|, t = x - m is off by u |t|,
+    its mean c by dc = (depth + 3) u (avg|x - mean| + e), and x - m - c by dc + u (|x - mean| + |t|); the
+    squares' mean less c^2 by (depth + 6) u (var + e^2) + 2 e dc + dc^2."""
+    g = torch.Generator(device=DEV).manual_seed(d)
+    n, depth, eps = 23, rows_at(d), 1e-5
+    x = torch.randn(n, d, device=DEV, generator=g) + shift
+    w, b = weights(d, F32, g), weights(d, F32, g)
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    efs.ef_layer_norm(x, y, w, b, eps, mean, rstd)
+    xx, ww, bb, eps = x.double(), w.double(), b.double(), float(torch.tensor(eps))
+    mu = xx.mean(1, keepdim=True)
+    t = xx - mu
+    var = t.square().mean(1, keepdim=True)
+    rs = (var + eps).rsqrt()
+    e = (depth + 2) * U * xx.abs().mean(1, keepdim=True)
+    dc = (depth + 3) * U * (t.abs().mean(1, keepdim=True) + e)
+    dr = ((depth + 6) * U * (var + e * e) + 2 * e * dc + dc * dc) / (2 * (var + eps)) * 1.01 + 3 * U
+    assert bool(((mean[:, None].double() - mu).abs() <= dc + U * (mu.abs() + dc)).all())
+    assert bool(((rstd[:, None].double() - rs).abs() <= dr * rs).all())
+    hat = t * rs
+    bound = ww.abs() * (hat.abs() * (dr + 3 * U) + rs * (dc + U * (2 * t.abs() + e)))
+    bound = bound + 2 * U * ((hat * ww).abs() + bb.abs())
+    assert bool(((y.double() - (hat * ww + bb)).abs() <= bound).all())
