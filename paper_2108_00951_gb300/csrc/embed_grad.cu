@@ -363,6 +363,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const Sort 
 
 // ------------------------------------------------------------------ summing
 struct Sum {
+  // (read by ordinary loads: the launch that writes them may still run when the sums' begins)
   const uint32_t *key, *pos;
   float* shares;          // [pieces][2][d]: a token from the piece before, one that goes on
   // [pieces][3][slices]: shares of a join whose first is the piece's, from the piece before
@@ -377,7 +378,7 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t n, u
   uint32_t lo = 0, hi = n;
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2;
-    if (__ldg(keys + mid) < key) lo = mid + 1;
+    if (keys[mid] < key) lo = mid + 1;
     else hi = mid;
   }
   return lo;
@@ -434,8 +435,8 @@ __device__ __forceinline__ uint32_t run_of(const Sum& s, uint32_t n, uint32_t to
                                            bool back) {
   const uint32_t step = 1 + lane;
   bool same = false;
-  if (back) same = step <= q && __ldg(s.key + (q - step + 1) * s.piece - 1) == token;
-  else same = q + step < s.pieces && __ldg(s.key + (q + step) * s.piece) == token;
+  if (back) same = step <= q && s.key[(q - step + 1) * s.piece - 1] == token;
+  else same = q + step < s.pieces && s.key[(q + step) * s.piece] == token;
   const uint32_t m = __ballot_sync(0xffffffffu, same);
   if (m != 0xffffffffu) return __ffs(~m) - 1;
   return back ? q - first_of(s.key, n, token) / s.piece : (first_of(s.key, n, token + 1) - 1) / s.piece - q;
@@ -516,7 +517,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGr
     __shared__ uint8_t occurs[kZeroRows];
     if (lo + threadIdx.x < hi && threadIdx.x < kZeroRows) {
       const uint32_t row = static_cast<uint32_t>(lo) + threadIdx.x, at = first_of(s.key, a.n, row);
-      occurs[threadIdx.x] = at < a.n && __ldg(s.key + at) == row;
+      occurs[threadIdx.x] = at < a.n && s.key[at] == row;
     }
     __syncthreads();
     for (uint64_t r = lo + warp; r < hi; r += kSumWarps)
@@ -529,10 +530,10 @@ __global__ void __launch_bounds__(32 * kSumWarps) embed_sum_kernel(const EmbedGr
   const uint32_t lo = piece * s.piece, count = min(s.piece, a.n - lo);
   uint32_t *keys = room[warp][0], *at = room[warp][1];
   for (uint32_t i = lane; i < count; i += 32) {
-    keys[i] = __ldg(s.key + lo + i);
-    at[i] = __ldg(s.pos + lo + i);
+    keys[i] = s.key[lo + i];
+    at[i] = s.pos[lo + i];
   }
-  const uint32_t last = lo > 0 ? __ldg(s.key + lo - 1) : a.v, next = lo + count < a.n ? __ldg(s.key + lo + count) : a.v;
+  const uint32_t last = lo > 0 ? s.key[lo - 1] : a.v, next = lo + count < a.n ? s.key[lo + count] : a.v;
   __syncwarp();
   // rows on their way; and (ADD) the rows of the table that sums end in meanwhile
   constexpr uint32_t kAhead = sizeof(D) == 2 && V > 2 && L == kLane && !ADD ? 8 : L == kLane || sizeof(D) == 2 ? 4 : 2;

@@ -220,3 +220,24 @@ def test_gradient_is_the_lookups():
         left, right = (dout.double() * out).sum(), (dt.double() * way).sum()
         size = (dout.double() * out).abs().sum()
         assert abs(float(left - right)) < 3000 * 2.0 ** -24 * float(size)
+
+
+@pytest.mark.parametrize("n,v,d", [(2100, 300, 40), (9000, 5000, 136), (70000, 3000, 64)])
+@pytest.mark.parametrize("add", [False, True])
+def test_lists_one_after_another(n, v, d, add):
+    """Sorted lists of one scratch, each launch begun as the one before ends: none sees another's."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    lists = [tokens(n, v, g) for _ in range(8)]
+    dout = torch.randn(n, d, device=DEV, generator=g)
+    out = [torch.ones(v, d, device=DEV) for _ in lists]
+    torch.cuda.synchronize()
+    for t, o in zip(lists, out):
+        efs.ef_embed_grad(dout, t, o, accumulate=add)
+    zero = torch.zeros(v, d, device=DEV, dtype=torch.float64)
+    for t, o in zip(lists, out):
+        keep = t >= 0
+        ref = zero.index_add(0, t[keep], dout[keep].double()) + float(add)
+        mag = zero.index_add(0, t[keep], dout[keep].double().abs()) + float(add)
+        count = zero.index_add(0, t[keep], torch.ones(int(keep.sum()), d, device=DEV, dtype=torch.float64))
+        assert bool(((o.double() - ref).abs() <= (count + 2) * 2.0 ** -24 * mag).all())
+    assert efs.ef_check_status() == efs.EF_OK
