@@ -248,3 +248,67 @@ def test_what_is_subtracted_is_the_mean_of_large_rows(d, shift):
     bound = ww.abs() * (hat.abs() * (dr + 3 * U) + rs * (dc + U * (2 * t.abs() + e)))
     bound = bound + 2 * U * ((hat * ww).abs() + bb.abs())
     assert bool(((y.double() - (hat * ww + bb)).abs() <= bound).all())
+
+
+# groups that take more rows than their ring has places, and the ends of the last round part full:
+# lanes (8 places forward, 6 back), warps (4, 3), a CTA of 16 and of 32 values a thread, clusters
+TALL = [(1100003, 3), (270001, 64), (90001, 200), (12001, 650), (5001, 2048), (3001, 4096), (1501, 8192),
+        (1201, 10000), (521, 24576), (303, 24209), (300, 32768)]
+
+
+@pytest.mark.parametrize("n,d", TALL)
+@pytest.mark.parametrize("xt,yt,wt,pad,offset", [(BF16, BF16, F32, 0, 0), (F32, BF16, BF16, 3, 1)])
+def test_rows_go_round_the_ring(n, d, xt, yt, wt, pad, offset):
+    check(n, d, xt, yt, wt, pad, offset)
+
+
+@pytest.mark.parametrize("n,d", [(40000, 24), (90001, 200), (12001, 650), (3001, 4095), (700, 8192), (520, 10000), (9, 70001)])
+@pytest.mark.parametrize("xt", [F32, BF16])
+def test_large_means_in_some_rows_of_many(n, d, xt):
+    """Rows that are corrected among rows that are not: each as it is by itself."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    x = torch.randn(n, d, device=DEV, generator=g)
+    x += torch.where(torch.rand(n, 1, device=DEV, generator=g) < 0.3, 500.0, 0.0)
+    x[1], x = 77.7, x.to(xt)
+    x[1] = x[1, 0]
+    w, b = weights(d, F32, g), weights(d, F32, g)
+    y, mean, rstd = (torch.empty(s, device=DEV) for s in ((n, d), (n,), (n,)))
+    efs.ef_layer_norm(x, y, w, b, 1e-5, mean, rstd)
+    assert torch.equal(y[1], b) and float(mean[1]) == float(x[1, 0])
+    for i in (0, 1, 2, n // 2, n - 2, n - 1):
+        y1, m1, r1 = torch.empty(1, d, device=DEV), torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+        # (as many rows, so that the same kernel takes it)
+        efs.ef_layer_norm(x[i:i + 1].expand(n, d).contiguous(), full := torch.empty(n, d, device=DEV), w, b, 1e-5,
+                          ms := torch.empty(n, device=DEV), rs := torch.empty(n, device=DEV))
+        for rows, one in ((full, y[i]), (ms, mean[i]), (rs, rstd[i])):
+            assert torch.equal(rows, one.expand_as(rows))
+
+
+@pytest.mark.parametrize("n,d", [(5, 3), (300, 24), (40, 650), (9, 2048), (6, 4097), (4, 9000), (3, 70001)])
+@pytest.mark.parametrize("xt,yt", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("pad,offset", [(3, 1), (8, 8), (1, 2)])
+def test_nothing_beside_the_rows_is_written(n, d, xt, yt, pad, offset):
+    g = torch.Generator(device=DEV).manual_seed(d)
+
+    def guarded(dtype):
+        buf = torch.full((offset + n * (d + pad) + 5,), 7.0, device=DEV, dtype=dtype)
+        rows = buf[offset:offset + n * (d + pad)].view(n, d + pad)
+        return buf, rows[:, :d]
+
+    def rest(buf, m):
+        keep = torch.ones_like(buf, dtype=torch.bool)
+        keep[offset:offset + n * (d + pad)].view(n, d + pad)[:, :d] = False
+        return buf[keep]
+    x = torch.randn(n, d, device=DEV, generator=g).to(xt)
+    x[0] += 300.0
+    dy = torch.randn(n, d, device=DEV, generator=g).to(yt)
+    (by, y), (bx, dx) = guarded(yt), guarded(xt)
+    vectors = torch.full((6, d + 16), 7.0, device=DEV)
+    mean, rstd = torch.full((n + 4,), 7.0, device=DEV), torch.full((n + 4,), 7.0, device=DEV)
+    efs.ef_layer_norm(x, y, None, None, 1e-5, mean, rstd)
+    efs.ef_layer_norm_grad(x, mean, rstd, dy, dx, None, vectors[1, :d], vectors[4, :d])
+    assert bool((rest(by, y) == 7.0).all()) and bool((rest(bx, dx) == 7.0).all())
+    assert bool((mean[n:] == 7.0).all()) and bool((rstd[n:] == 7.0).all())
+    assert bool((vectors[[0, 2, 3, 5]] == 7.0).all()) and bool((vectors[[1, 4], d:] == 7.0).all())
+    assert not bool((vectors[[1, 4], :d] == 7.0).all()) and bool(dx.isfinite().all())
+    assert efs.ef_check_status() == efs.EF_OK
