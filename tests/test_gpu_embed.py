@@ -241,3 +241,26 @@ def test_lists_one_after_another(n, v, d, add):
         count = zero.index_add(0, t[keep], torch.ones(int(keep.sum()), d, device=DEV, dtype=torch.float64))
         assert bool(((o.double() - ref).abs() <= (count + 2) * 2.0 ** -24 * mag).all())
     assert efs.ef_check_status() == efs.EF_OK
+
+
+@pytest.mark.parametrize("n,v,d", [(65536, 3000, 520), (70001, 40, 1024), (65536, 50001, 1000)])
+@pytest.mark.parametrize("dt,tt", [(BF16, BF16), (BF16, F32), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("add", [False, True])
+def test_long_lists_of_wide_rows(n, v, d, dt, tt, add):
+    """Lists from 65,536 tokens on, whose lanes take 16 columns where nothing is added."""
+    check_gradient(n, v, d, dt, tt, 0, 0, add)
+
+
+@pytest.mark.parametrize("dt,tt", [(BF16, BF16), (BF16, F32), (F32, BF16), (F32, F32)])
+def test_runs_of_many_pieces_of_wide_rows(dt, tt):
+    """Words that end, go on and begin in pieces of 128 positions, some of them whole."""
+    g = torch.Generator().manual_seed(9)
+    runs = [128 * 16, 128 * 17, 128 * 16 - 1, 128 * 16 + 1, 128 * 17 + 1, 1, 128 * 33 + 5, 3, 128, 127, 129, 17, 128 * 40 + 2]
+    runs += torch.randint(1, 400, (230,), generator=g).tolist()
+    t = torch.repeat_interleave(torch.arange(len(runs)) + 1, torch.tensor(runs))
+    t = torch.cat([t, torch.full((70001 - t.numel(),), len(runs) + 1)]) if t.numel() < 70001 else t
+    t = t[torch.randperm(t.numel(), generator=g)].to(DEV)
+    assert t.numel() >= 65536
+    check_gradient(t.numel(), len(runs) + 3, 520, dt, tt, 0, 0, False, t=t)
+    t[::7] = -1
+    check_gradient(t.numel(), len(runs) + 3, 1024, dt, tt, 0, 0, False, t=t)
