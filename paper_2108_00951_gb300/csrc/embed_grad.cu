@@ -669,7 +669,7 @@ cudaError_t launch(const EmbedGradCall& c, const Plan& p, cudaStream_t stream) {
   void* params[] = {&a, &s};
   count_launch();
   const void* kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLane, ADD>);
-  if constexpr (V == 8)
+  if constexpr (V == 8 && !ADD)  // (as planned)
     if (p.lane == kLaneMany) kernel = reinterpret_cast<const void*>(embed_sum_kernel<D, T, V, kLaneMany, ADD>);
   return launch_pdl(kernel,
                     dim3((s.warps + kSumWarps - 1) / kSumWarps + zeros), 32 * kSumWarps, 0, stream, params, false);

@@ -206,8 +206,9 @@ cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream
   // 27.5 us with 32 a thread, 22.1 with 16 (30 x 9001 6.2 and 4.3; but 700 x 9001 23.9 and 25.0, and
   // 255 x 16,388, vectors of 4, 13.5 and 15.9)
   constexpr uint32_t kMany = 32 * kNormThreads, kFew = 16 * kNormThreads;
-  if (V < 4 && c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
-    return launch_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, stream);
+  if constexpr (V < 4)
+    if (c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
+      return launch_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, stream);
   return launch_rows<X, Y, V, 32 / V, kRowAll>(c, kMany, dev, stream);
 }
 
