@@ -573,9 +573,11 @@ ef_status ef_orthogonalize(uint32_t n_mat, const uint64_t* rows, const uint64_t*
  *                    once from the fp32 product; must not overlap an input.
  *
  * Here and in the next entries: row strides are in elements, at least d and at
- * most 2^36; pointers are aligned to their elements (rows on 16-byte boundaries
- * are fastest, then rows of an even number of elements). Equal inputs give
- * equal bits. Scratch: a call on a new stream allocates its workspace.
+ * most 2^36; pointers are aligned to their elements (fastest where d, the strides and
+ * the pointers are multiples of eight elements, then of four in layer norm and in fp32
+ * lookups, then of two). Equal calls give equal bits on one device; sums run in an order
+ * that sizes, alignment and the number of SMs fix. Scratch: a call on a new stream
+ * allocates its workspace.
  */
 ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type,
                    const int64_t* token, uint64_t n, uint64_t v, uint64_t d, float scale, void* out,
@@ -595,7 +597,8 @@ ef_status ef_embed(const void* table, uint64_t ld_table, ef_grad_type table_type
  *   dtable     [in/out] fp32 or bf16 (dtable_type) [v][d], rows ld_dtable apart;
  *                    must not overlap an input.
  *
- * Sums are fp32, in an order that n, v, d and the tokens fix, rounded once.
+ * Sums are fp32, in an order that n, v, d, the tokens, accumulate and the device's
+ * number of SMs fix, rounded once.
  * Scratch above 2048 tokens, and above 256 of more than 2,359,296 values: 16 bytes a
  * token, a fp32 row of d for each 8 tokens (16 from 16,385 on, 64 from 65,536 on, 32
  * where they are added), and at most 1 MB and a twentieth of that beside.
@@ -646,7 +649,7 @@ ef_status ef_layer_norm(const void* x, uint64_t ldx, ef_grad_type x_type, const 
  * Sums are fp32, those over rows by CTAs and then over the CTAs in order.
  * Scratch, where dweight or dbias is asked for: 8 d bytes per CTA (per cluster above
  * 4096 columns), of which there are at most eight an SM; rows of more than 65,536
- * columns: 8 d for each 16 rows, at most 8 MB an SM for all columns.
+ * columns: 8 d for each 16 rows, at most 64 KB an SM and 8 d beside.
  */
 ef_status ef_layer_norm_grad(const void* x, uint64_t ldx, ef_grad_type x_type, const void* weight,
                              ef_grad_type w_type, const float* mean, const float* rstd,

@@ -1,9 +1,11 @@
 // embed_grad.cu — the gradient of an embedding table: row w is the scaled sum of
-// the rows of dout whose token is w, in the order of their positions, in fp32.
+// the rows of dout whose token is w, in fp32.
 //
 // What bounds it: reading dout once and writing the table's gradient once (or, where
 // it is added to, the rows that occur). Sums run in a fixed order, without
-// floating-point atomics.
+// floating-point atomics: by groups of positions (every few-th occurrence, or those in
+// one piece of the sorted list), each in the order of its positions, then over the groups. The sizes, the
+// tokens, whether sums are added and the number of SMs fix the groups.
 //
 // Up to kFewTokens tokens of kFewValues values: one launch. A CTA per position looks through all
 // tokens; if its own occurs before, another CTA has it, else it sums the rows of
@@ -260,7 +262,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const Sort s,
         key = __ldcg(s.key[pass & 1u] + i);
       }
     }
-    // (131,072 x 1024: 119 us; with a warp's equal digits matched to be one addition 121)
+    // (131,072 x 1024: 118 us, with 95 % of it padding, one digit, 87; with a warp's equal digits matched to be
+    // one addition 121 and 88)
     if (i < hi) atomicAdd(&hist[digit_of(s, key, pass)], 1u);
   }
   griddep_launch_dependents();  // (the scatter, which waits for this kernel's end)

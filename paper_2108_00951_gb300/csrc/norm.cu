@@ -38,7 +38,7 @@ __device__ __forceinline__ Correction correction(float sum, float squares, uint3
 }
 
 // (32 values a thread in 128 registers, narrow vectors with some of them spilled: 2000 x 9001 fp32
-// 50 us, in 192 registers 76)
+// 49 us, in 192 registers 75)
 template <typename X, typename Y, int V, int K, RowKind KIND>
 __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel(const NormCall a) {
   constexpr int S = kRing<V * K>;
@@ -199,12 +199,12 @@ cudaError_t launch_rows(NormCall c, uint32_t most, const DeviceInfo& dev, cudaSt
 template <typename X, typename Y, int V>
 cudaError_t launch(const NormCall& c, const DeviceInfo& dev, cudaStream_t stream) {
   // Values of a row that a thread holds: fewer warps a row add up and wait less
-  // (32,768 x 4096: 16 a thread 126 us, 32 81), more have more rows at once
+  // (32,768 x 4096: 16 a thread 110 us, 32 85), more have more rows at once
   if (c.d <= 256) return launch_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, stream);
   if (c.d <= 2048) return launch_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, stream);
   // Of a few long rows with narrow vectors, a thread's values are the wait: 255 x 24,209 fp32
-  // 27.5 us with 32 a thread, 22.1 with 16 (30 x 9001 6.2 and 4.3; but 700 x 9001 23.9 and 25.0, and
-  // 255 x 16,388, vectors of 4, 13.5 and 15.9)
+  // 26.4 us with 32 a thread, 22.5 with 16 (30 x 9001 6.2 and 4.3; but 700 x 9001 23.5 and 25.1, and
+  // 255 x 16,388, vectors of 4, 13.8 and 13.3: not worth their kernels)
   constexpr uint32_t kMany = 32 * kNormThreads, kFew = 16 * kNormThreads;
   if constexpr (V < 4)
     if (c.d > kMany && c.d <= kFew * kNormCluster && c.n <= 2u * dev.sm_count)
