@@ -6,8 +6,8 @@
 // loads before the first store (65,536 rows of 1024 bf16 values: 27.5 us, 89 % of the
 // floor); with few rows the slices are short, so that the latency of one load after
 // the token's is all there is. Rows of at most 32 vectors, which would leave lanes idle,
-// go vector by vector over the threads (1,000,000 rows of 64 fp32 values: 148 us by slices, 62; of
-// bf16 32). Vectors need the width, too, to be whole ones: odd widths go value by value.
+// go vector by vector over the threads (1,000,000 rows of 64 bf16 values: 144 us by slices, 32;
+// fp32 139 and 62). Vectors need the width, too, to be whole ones: odd widths go value by value.
 #include "internal.h"
 #include "vec_io.cuh"
 

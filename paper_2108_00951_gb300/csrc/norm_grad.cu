@@ -253,8 +253,9 @@ template <typename X, typename Y, int V>
 cudaError_t plan_width(const NormGradCall& c, const DeviceInfo& dev, Plan& p) {
   if (c.d <= 256) return plan_rows<X, Y, V, 8 / V, kRowLanes>(c, 256, dev, p);
   if (c.d <= 2048) return plan_rows<X, Y, V, 16 / V, kRowWarps>(c, 2048, dev, p);
-  // 16 values a thread leave two CTAs an SM (32,768 x 4096: 157 us, with 32 205), but a CTA
-  // without a cluster waits less (16,384 x 8192: 172 with 32, 226 with 16 and two CTAs)
+  // 16 values a thread leave two CTAs an SM (both passes over 20,000 x 2501: 166 us, with 32 220; 20,000 x 3001
+  // fp32 230 and 262; wide vectors lose less by 32, or nothing: 32,768 x 4096 250 with either, fp32 460 and
+  // 423), but a CTA without a cluster waits less (16,384 x 8192: 264 with 32, 311 with 16 and two CTAs)
   constexpr uint32_t kFew = 16 * kNormThreads, kMany = 32 * kNormThreads;
   if (c.d <= kFew || (c.d > kMany && c.d <= kFew * kNormCluster))
     return plan_rows<X, Y, V, 16 / V, kRowAll>(c, kFew, dev, p);
