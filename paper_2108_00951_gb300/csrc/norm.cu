@@ -3,16 +3,18 @@
 //
 // Both sums are fp32 over values that stay in registers, the second after the
 // mean is known (a difference of squares would lose the variance of rows whose
-// mean is large). rstd makes much of a last place of a large mean: of a row of 1000.0 it is 0.02 of
-// y, of one near 1e5 all of it. So the product with 1 / d is corrected by its remainder,
-// sum - mean d, and rows of fp32 (bf16 values of one magnitude add up exactly) whose mean is beyond four
-// deviations by the mean of their differences, which are exact there; below, what the sum
-// loses is at most 5 (depth + 2) 2^-24 deviations. What bounds it: reading x and writing y
-// once. A row of up to 256
-// values lies in lanes of a warp, of up to 2048 in warps, of up to 8192 in a CTA, of up to
-// 65,536 in a cluster of CTAs; they take rows a stride apart, the next ones on their way
-// into a ring in shared memory meanwhile, and the weights stay in registers. A
-// longer row is read three times by one CTA, twice out of L2.
+// mean is large). rstd makes much of a last place of a large mean: of a row of
+// 1000.0 it is 0.02 of y, of one near 1e5 all of it. So the product with 1 / d is
+// corrected by its remainder, sum - mean d, and an fp32 row whose mean is beyond four
+// deviations by the mean of its differences, which are exact there (bf16 values of
+// one magnitude add up exactly); below, what the sum loses is at most
+// 5 (depth + 2) 2^-24 deviations, depth its additions one after another.
+//
+// What bounds it: reading x and writing y once. A row of up to 256 values lies in
+// lanes of a warp, of up to 2048 in warps, of up to 8192 in a CTA, of up to 65,536 in a
+// cluster of CTAs; they take rows a stride apart, the next ones on their way into
+// a ring in shared memory meanwhile, and the weights stay in registers. A longer
+// row is read three times by one CTA, twice out of L2.
 #include <algorithm>
 #include <map>
 #include <mutex>
@@ -86,7 +88,8 @@ __global__ void __launch_bounds__(kNormThreads, V * K == 32 ? 2 : 0) norm_kernel
         for (int j = 0; j < V; ++j) sum += x[k][j] = v.get(j);
       }
     }
-    // (the fused product has the remainder exactly: the mean of a row of one value whose sum is exact is exact)
+    // (the fused product has the remainder exactly: of a row of one value, summed exactly, the
+    // mean is that value)
     const float total = row_sum<KIND, false>(g, sum, 0.0f, room, 0, a.cluster, parity).x, near = total * inv;
     const float mean = fmaf(fmaf(-near, width, total), inv, near);
     sum = 0.0f;
